@@ -81,3 +81,104 @@ def skrull_attention(q, k, v, plan):
             i = plan.info
             return native(q, k, v, plan, i.total_q, i.total_k, i.num_q_heads, i.num_kv_heads, i.head_dim)
     return _SkrullAttention.apply(q, k, v, plan)
+
+
+# ---- rotary positions, norm, loss: the same, on the binding's calls ----------------------------------------------------
+
+_KINDS = {"layer": B.NORM_LAYER, "rms": B.NORM_RMS}
+
+
+def _workspace(n, device):
+    return torch.empty(max(int(n), 16), dtype=torch.uint8, device=device)
+
+
+class _SkrullRotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, plan, rotary, k_rows):
+        ctx.plan, ctx.rotary, ctx.k_rows = plan, rotary, k_rows
+        out = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k)]
+        B.skrull_rotary(plan, rotary, q, k, *out, k_rows=k_rows)
+        return tuple(out)
+
+    @staticmethod
+    def backward(ctx, dq, dk):
+        given = [_rows_of_heads(t) for t in (dq, dk)]
+        out = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in given]
+        B.skrull_rotary(ctx.plan, ctx.rotary, *given, *out, inverse=True, k_rows=ctx.k_rows)
+        return out[0], out[1], None, None, None
+
+
+def _rows_of_heads(t):
+    """`t` [rows, heads, head_dim] as the library takes it: strides as they are where it can."""
+    heads, d = t.shape[1:]
+    fits = t.stride(2) == 1 and (heads == 1 or t.stride(1) == d) and t.stride(0) >= heads * d and t.stride(0) % 8 == 0 and t.data_ptr() % 16 == 0
+    return t if fits else t.contiguous()
+
+
+def skrull_rotary(q, k, plan, rotary, k_rows=B.ROWS_K):
+    """q and k turned by the positions of the rows of `plan` (a binding.Plan); differentiable.  `rotary`: from
+    binding.skrull_rotary_init.  k holds the gathered prefixes, or with k_rows=binding.ROWS_Q this rank's own tokens.
+    q and k may be parts of one projection's rows; what comes back is contiguous, as skrull_attention takes it."""
+    return _SkrullRotary.apply(_rows_of_heads(q), _rows_of_heads(k), plan, rotary, k_rows)
+
+
+class _SkrullNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps, kind):
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        mean, rstd = torch.empty((2, x.shape[0]), dtype=torch.float32, device=x.device)
+        B.skrull_norm_fwd(x, weight, bias, y, mean, rstd, eps, kind)
+        ctx.kind, ctx.bias = kind, bias is not None
+        ctx.save_for_backward(x, weight, mean, rstd)
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, weight, mean, rstd = ctx.saved_tensors
+        dy = dy if dy.stride(1) == 1 and dy.stride(0) >= dy.shape[1] else dy.contiguous()
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        need_w, need_b = ctx.needs_input_grad[1], ctx.bias and ctx.needs_input_grad[2]
+        dw = torch.empty_like(weight) if need_w else None
+        db = torch.empty_like(weight) if need_b else None
+        ws = _workspace(B.skrull_norm_workspace(x, weight, ctx.kind), x.device) if need_w or need_b else None
+        B.skrull_norm_bwd(x, weight, mean, rstd, dy, dx, dw, db, ws, ctx.kind)
+        return dx, dw, db, None, None
+
+
+def skrull_norm(x, weight, bias=None, eps=1e-5, kind="layer"):
+    """The norm of the rows of x [rows, cols] (bf16 or fp32) with weight and bias [cols]: "layer", or "rms" without mean and
+    bias; differentiable with respect to x, weight and bias."""
+    if kind not in _KINDS:
+        raise ValueError(f"kind must be one of {sorted(_KINDS)}")
+    if x.dim() != 2:
+        raise ValueError("x must be [rows, cols]")
+    if x.stride(1) != 1 or x.stride(0) < x.shape[1]:
+        x = x.contiguous()
+    return _SkrullNorm.apply(x, weight.contiguous(), None if bias is None else bias.contiguous(), eps, _KINDS[kind])
+
+
+class _SkrullCrossEntropy(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, target):
+        loss, lse = (torch.empty(x.shape[0], dtype=torch.float32, device=x.device) for _ in range(2))
+        B.skrull_loss_fwd(x, weight, target, loss, lse, _workspace(B.skrull_loss_workspace(x, weight, False), x.device))
+        ctx.save_for_backward(x, weight, target, lse)
+        return loss
+
+    @staticmethod
+    def backward(ctx, d_loss):
+        x, weight, target, lse = ctx.saved_tensors
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if ctx.needs_input_grad[0] else None
+        dw = torch.empty_like(weight) if ctx.needs_input_grad[1] else None
+        B.skrull_loss_bwd(x, weight, target, lse, d_loss.contiguous(), dx, dw,
+                          _workspace(B.skrull_loss_workspace(x, weight, True), x.device))
+        return dx, dw, None
+
+
+def skrull_cross_entropy(x, weight, target):
+    """The softmax cross entropy of each row of x [rows, hidden] times the vocabulary's weight [vocab, hidden] against
+    target [rows] (int64; a negative one: the row has none, and a loss of 0), fp32 [rows], without keeping the logits;
+    differentiable with respect to x and weight."""
+    if x.dim() == 2 and (x.stride(1) != 1 or x.stride(0) < x.shape[1]):
+        x = x.contiguous()
+    return _SkrullCrossEntropy.apply(x, weight.contiguous(), target.contiguous())

@@ -16,6 +16,11 @@ SKRULL_OK, SKRULL_EINVAL, SKRULL_ENOMEM, SKRULL_EHIP, SKRULL_EUNSUPPORTED, SKRUL
 (ARRAY_CU_Q, ARRAY_CU_K, ARRAY_Q_BEGIN, ARRAY_Q_LEN, ARRAY_KV_LEN, ARRAY_FWD_ITEMS, ARRAY_DKV_ITEMS,
  ARRAY_SHARES_KV) = range(8)
 CUT_CONTIGUOUS, CUT_TWO_CHUNKS = 0, 1
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_NTK, ROTARY_PARTS = range(4)
+ROWS_Q, ROWS_K = 0, 1
+NORM_RMS, NORM_LAYER = 0, 1
+TYPE_BF16, TYPE_FP32 = 0, 1
 
 EXPORTED_SYMBOLS = ("skrull_attn_plan", "skrull_attn_plan_info", "skrull_attn_plan_export",
                     "skrull_attn_fwd", "skrull_attn_bwd", "skrull_attn_bwd_static", "skrull_attn_plan_destroy",
@@ -23,6 +28,9 @@ EXPORTED_SYMBOLS = ("skrull_attn_plan", "skrull_attn_plan_info", "skrull_attn_pl
                     "skrull_attn_mfma_ceiling", "skrull_attn_trace", "skrull_attn_trace_layout",
                     "skrull_dacp_schedule", "skrull_dacp_rank_batch",
                     "skrull_gds_binpack", "skrull_gds_schedule", "skrull_gds_micro_batch")
+# the operators around attention (skrull_rotary.h, skrull_norm.h, skrull_loss.h)
+OPERATOR_SYMBOLS = ("skrull_rotary_check", "skrull_rotary", "skrull_norm_fwd", "skrull_norm_workspace", "skrull_norm_bwd",
+                    "skrull_loss_workspace", "skrull_loss_fwd", "skrull_loss_bwd")
 
 
 class Problem(ctypes.Structure):
@@ -68,6 +76,29 @@ class PlanInfo(ctypes.Structure):
 
 class FlopsModel(ctypes.Structure):
     _fields_ = [("hidden", ctypes.c_int64), ("hidden_kv", ctypes.c_int64), ("batch", ctypes.c_int64)]
+
+
+class Rotary(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("scaling", ctypes.c_int32), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("original_length", ctypes.c_double), ("low_turns", ctypes.c_double), ("high_turns", ctypes.c_double),
+                ("amplitude", ctypes.c_double)]
+
+
+class RotaryTensor(ctypes.Structure):
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("in_stride", ctypes.c_int64),
+                ("out_stride", ctypes.c_int64), ("heads", ctypes.c_int32), ("rows", ctypes.c_int32)]
+
+
+class Norm(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int32), ("kind", ctypes.c_int32), ("type", ctypes.c_int32),
+                ("weight_type", ctypes.c_int32), ("eps", ctypes.c_float), ("x_stride", ctypes.c_int64),
+                ("y_stride", ctypes.c_int64), ("dy_stride", ctypes.c_int64), ("dx_stride", ctypes.c_int64)]
+
+
+class Loss(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("hidden", ctypes.c_int32), ("vocab", ctypes.c_int32),
+                ("x_stride", ctypes.c_int64)]
 
 
 class SkrullError(RuntimeError):
@@ -133,6 +164,18 @@ def lib():
         L.skrull_gds_schedule.restype = ctypes.c_int
         L.skrull_gds_micro_batch.argtypes = [ctypes.c_int32, i32p, i32p, ctypes.c_int32, i32p, i32p]
         L.skrull_gds_micro_batch.restype = ctypes.c_int
+        L.skrull_rotary_check.argtypes = [ctypes.POINTER(Rotary)]
+        L.skrull_rotary.argtypes = [vp, ctypes.POINTER(Rotary), ctypes.POINTER(RotaryTensor), ctypes.POINTER(RotaryTensor),
+                                    ctypes.c_int, vp]
+        norm, loss = ctypes.POINTER(Norm), ctypes.POINTER(Loss)
+        L.skrull_norm_fwd.argtypes = [norm] + [vp] * 7
+        L.skrull_norm_workspace.argtypes = [norm]
+        L.skrull_norm_bwd.argtypes = [norm] + [vp] * 9 + [ctypes.c_size_t, vp]
+        L.skrull_loss_workspace.argtypes = [loss, ctypes.c_int]
+        L.skrull_loss_fwd.argtypes = [loss] + [vp] * 6 + [ctypes.c_size_t, vp]
+        L.skrull_loss_bwd.argtypes = [loss] + [vp] * 8 + [ctypes.c_size_t, vp]
+        for name in OPERATOR_SYMBOLS:
+            getattr(L, name).restype = ctypes.c_int64 if name.endswith("workspace") else ctypes.c_int
         _lib = L
     return _lib
 
@@ -357,3 +400,146 @@ def skrull_gds_micro_batch(seq_len, micro_batch, index) -> np.ndarray:
     _check(lib().skrull_gds_micro_batch(int(S.shape[0]), S.ctypes.data_as(i32p), M.ctypes.data_as(i32p),
                                         int(index), out.ctypes.data_as(i32p), ctypes.byref(n)))
     return out[:n.value].copy()
+
+
+# ---- rotary positions, norm, loss ---------------------------------------------------------------------------------
+# These take strided tensors, so shapes, types and devices are checked here; a tensor on another device than the
+# current one is refused, as the library refuses a plan of another device.
+
+def _refuse(why):
+    raise SkrullError(SKRULL_EINVAL, f"invalid argument ({why})")
+
+
+def _on_current_device(*tensors):
+    import torch
+    for t in tensors:
+        if t is not None and not (t.is_cuda and t.device.index == torch.cuda.current_device()):
+            _refuse(f"a tensor is on {t.device}, not on the current GPU")
+
+
+def skrull_rotary_init(head_dim, rotary_dim=None, layout=ROTARY_HALF, base=10000.0, scaling=ROTARY_PLAIN, factor=1.0,
+                       original_length=0.0, low_turns=0.0, high_turns=0.0, amplitude=1.0) -> Rotary:
+    """What skrull_rotary needs to know of the model, checked."""
+    r = Rotary(int(head_dim), int(head_dim if rotary_dim is None else rotary_dim), int(layout), int(scaling), float(base),
+               float(factor), float(original_length), float(low_turns), float(high_turns), float(amplitude))
+    _check(lib().skrull_rotary_check(ctypes.byref(r)))
+    return r
+
+
+def _rotary_tensor(plan, x, out, rows):
+    import torch
+    want = plan.total_q if rows == ROWS_Q else plan.total_k
+    for t in (x, out):
+        if t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[0] != want or t.shape[2] != plan.head_dim or t.shape != x.shape:
+            _refuse(f"a tensor of bf16 [{want}, heads, {plan.head_dim}] is needed, got {t.dtype} {list(t.shape)}")
+        if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != plan.head_dim):
+            _refuse("the heads of a row must be contiguous")
+    # (a single row's stride says nothing)
+    width = x.shape[1] * plan.head_dim
+    strides = [t.stride(0) if want > 1 else width for t in (x, out)]
+    return RotaryTensor(_ptr(x), _ptr(out), strides[0], strides[1], x.shape[1], rows)
+
+
+def skrull_rotary(plan: Plan, rotary: Rotary, q, k, q_out, k_out, inverse=False, k_rows=ROWS_K, stream=None):
+    """q_out, k_out = q, k turned by the positions of the plan's rows (`inverse`: turned back).  q or k may be None.  k_rows: whether
+    k holds the gathered prefixes (ROWS_K) or this rank's own tokens (ROWS_Q)."""
+    _on_current_device(q, k, q_out, k_out)
+    t = [_rotary_tensor(plan, x, out, rows) for x, out, rows in ((q, q_out, ROWS_Q), (k, k_out, k_rows)) if x is not None]
+    if not t:
+        _refuse("neither q nor k")
+    _check(lib().skrull_rotary(plan.handle, ctypes.byref(rotary), ctypes.byref(t[0]),
+                               ctypes.byref(t[1]) if len(t) > 1 else None, int(bool(inverse)), _stream_ptr(stream)))
+
+
+def _type_of(t):
+    import torch
+    if t.dtype == torch.bfloat16:
+        return TYPE_BF16
+    if t.dtype == torch.float32:
+        return TYPE_FP32
+    _refuse(f"bf16 and fp32 are taken, got {t.dtype}")
+
+
+def _norm_of(x, weight, eps, kind, **rows) -> Norm:
+    p = Norm(x.shape[0] if x.dim() == 2 else -1, x.shape[-1], int(kind), _type_of(x), _type_of(weight), float(eps))
+    for name, t in dict(rows, x=x).items():
+        if t.dim() != 2 or t.shape != x.shape or t.dtype != x.dtype or (t.shape[1] > 1 and t.stride(1) != 1):
+            _refuse(f"{name} must be {x.dtype} [rows, cols] with contiguous rows, as x is")
+        setattr(p, name + "_stride", t.stride(0) if t.shape[0] > 1 else t.shape[1])
+    return p
+
+
+def _vector(t, n, dtype, name):
+    if t is not None and (t.shape != (n,) or t.dtype != dtype or not t.is_contiguous()):
+        _refuse(f"{name} must be contiguous {dtype} [{n}]")
+    return None if t is None else _ptr(t)
+
+
+def skrull_norm_fwd(x, weight, bias, y, mean, rstd, eps=1e-5, kind=NORM_LAYER, stream=None):
+    """y = the norm of the rows of x; mean and rstd (fp32 [rows], may be None) for the backward."""
+    import torch
+    _on_current_device(x, weight, bias, y, mean, rstd)
+    p = _norm_of(x, weight, eps, kind, y=y)
+    cols, wt, rows = p.cols, weight.dtype, p.rows
+    _check(lib().skrull_norm_fwd(ctypes.byref(p), _ptr(x), _vector(weight, cols, wt, "weight"), _vector(bias, cols, wt, "bias"), _ptr(y),
+                                 _vector(mean, rows, torch.float32, "mean"), _vector(rstd, rows, torch.float32, "rstd"), _stream_ptr(stream)))
+
+
+def skrull_norm_workspace(x, weight, kind=NORM_LAYER) -> int:
+    """Bytes that skrull_norm_bwd asks for."""
+    return int(lib().skrull_norm_workspace(ctypes.byref(_norm_of(x, weight, 0.0, kind))))
+
+
+def skrull_norm_bwd(x, weight, mean, rstd, dy, dx, dweight, dbias, workspace, kind=NORM_LAYER, stream=None):
+    """dx, and dweight and dbias where they are wanted (else None)."""
+    import torch
+    _on_current_device(x, weight, mean, rstd, dy, dx, dweight, dbias, workspace)
+    p = _norm_of(x, weight, 0.0, kind, dy=dy, dx=dx)
+    cols, wt, rows = p.cols, weight.dtype, p.rows
+    _check(lib().skrull_norm_bwd(ctypes.byref(p), _ptr(x), _vector(weight, cols, wt, "weight"), _vector(mean, rows, torch.float32, "mean"),
+                                 _vector(rstd, rows, torch.float32, "rstd"), _ptr(dy), _ptr(dx), _vector(dweight, cols, wt, "dweight"),
+                                 _vector(dbias, cols, wt, "dbias"), None if workspace is None else _ptr(workspace),
+                                 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+
+
+def _loss_of(x, weight, target) -> Loss:
+    import torch
+    if x.dim() != 2 or x.dtype != torch.bfloat16 or x.stride(1) != 1:
+        _refuse(f"x must be bf16 [rows, hidden] with contiguous rows, got {x.dtype} {list(x.shape)}")
+    if weight.dtype != torch.bfloat16 or weight.dim() != 2 or weight.shape[1] != x.shape[1] or not weight.is_contiguous():
+        _refuse(f"weight must be contiguous bf16 [vocab, {x.shape[1]}], got {weight.dtype} {list(weight.shape)}")
+    if target is not None and (target.dtype != torch.int64 or target.shape != (x.shape[0],) or not target.is_contiguous()):
+        _refuse(f"target must be contiguous int64 [{x.shape[0]}], got {target.dtype} {list(target.shape)}")
+    return Loss(x.shape[0], x.shape[1], weight.shape[0], x.stride(0) if x.shape[0] > 1 else x.shape[1])
+
+
+def skrull_loss_workspace(x, weight, backward: bool) -> int:
+    """Bytes that skrull_loss_fwd or skrull_loss_bwd asks for; SkrullError where the sizes are outside the limits."""
+    n = int(lib().skrull_loss_workspace(ctypes.byref(_loss_of(x, weight, None)), int(backward)))
+    if n == 0:
+        _check(SKRULL_EINVAL)
+    return n
+
+
+def skrull_loss_fwd(x, weight, target, loss, lse, workspace, stream=None):
+    """loss, lse (fp32 [rows]) of the rows x against the vocabulary's weight; rows with a negative target have none."""
+    import torch
+    _on_current_device(x, weight, target, loss, lse, workspace)
+    p = _loss_of(x, weight, target)
+    _check(lib().skrull_loss_fwd(ctypes.byref(p), _ptr(x), _ptr(weight), _ptr(target), _vector(loss, p.rows, torch.float32, "loss"),
+                                 _vector(lse, p.rows, torch.float32, "lse"), _ptr(workspace),
+                                 workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+
+
+def skrull_loss_bwd(x, weight, target, lse, d_loss, dx, dweight, workspace, stream=None):
+    """dx and dweight (either may be None) for the gradient d_loss (fp32 [rows])."""
+    import torch
+    _on_current_device(x, weight, target, lse, d_loss, dx, dweight, workspace)
+    p = _loss_of(x, weight, target)
+    for name, t, like in (("dx", dx, x), ("dweight", dweight, weight)):
+        if t is not None and (t.dtype != torch.bfloat16 or t.shape != like.shape or not t.is_contiguous()):
+            _refuse(f"{name} must be contiguous bf16 {list(like.shape)}")
+    _check(lib().skrull_loss_bwd(ctypes.byref(p), _ptr(x), _ptr(weight), _ptr(target), _vector(lse, p.rows, torch.float32, "lse"),
+                                 _vector(d_loss, p.rows, torch.float32, "d_loss"), None if dx is None else _ptr(dx),
+                                 None if dweight is None else _ptr(dweight), _ptr(workspace),
+                                 workspace.numel() * workspace.element_size(), _stream_ptr(stream)))

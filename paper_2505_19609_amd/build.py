@@ -14,7 +14,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libskrull_attn.so")
 AUTOGRAD = os.path.join(HERE, "_autograd.so")
-SOURCES = ["api.hip", "plan.hip", "fwd.hip", "bwd.hip", "probe.hip", "dacp.cpp", "gds.cpp"]
+SOURCES = ["api.hip", "plan.hip", "fwd.hip", "bwd.hip", "probe.hip", "rotary.hip", "norm.hip", "loss.hip", "dacp.cpp", "gds.cpp"]
 # packed fp32 VALU ops are switched off for all device code
 FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-I" + os.path.join(ROOT, "include"),
          "-I" + CSRC, "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -5,6 +5,7 @@
 // most, for the allocations and grids) and the tuning choices documented in the header,
 // which it takes from the totals that the plan kernels return.
 #include <math.h>
+#include <stdarg.h>
 #include <stdio.h>
 #include <stdlib.h>
 #include <string.h>
@@ -13,7 +14,7 @@
 #include <mutex>
 #include <new>
 
-#include "common.h"
+#include "ops.h"
 #include "skrull_dacp.h"
 
 namespace {
@@ -154,6 +155,32 @@ int check_plan_device(const skrull_attn_plan_t *plan)
 }
 
 }  // namespace
+
+int refuse(const char *format, ...)
+{
+    va_list args;
+    va_start(args, format);
+    vsnprintf(g_err, sizeof g_err, format, args);
+    va_end(args);
+    return SKRULL_EINVAL;
+}
+
+int launch_failed(hipError_t e, const char *what) { return hip_fail(e, what); }
+
+int current_device(int *compute_units)
+{
+    static std::atomic<int> known[kMaxDevices];  // compute units of the devices that were looked up
+    int dev = -1;
+    if (hipGetDevice(&dev) == hipSuccess && dev >= 0 && dev < kMaxDevices) {
+        *compute_units = known[dev].load(std::memory_order_relaxed);
+        if (*compute_units > 0) return SKRULL_OK;
+    }
+    if (int rc = check_device(&dev, compute_units)) return rc;
+    if (dev >= 0 && dev < kMaxDevices) known[dev].store(*compute_units, std::memory_order_relaxed);
+    return SKRULL_OK;
+}
+
+int plan_on_current_device(const skrull_attn_plan_t *plan) { return check_plan_device(plan); }
 
 extern "C" {
 

@@ -1,0 +1,685 @@
+// Softmax cross entropy of packed rows times a vocabulary's weight, with its gradients (include/skrull_loss.h).
+//
+// Rows that have a target are gathered first (X: as many rows as there are, then zeros to a whole tile, hidden values
+// padded with zeros to whole steps), so rows without one cost nothing and odd strides and alignments stay out of the products.
+// How many there are only the device knows: every kernel reads it and works out its own tiles.
+//
+// Four products of the same shape, all on one tile kernel:
+//   logits   z^T = W X^T           the forward keeps, per row and strip of 128 words, the largest logit and the sum of exponentials;
+//            and again             the backward writes dz = d (exp(z - lse) - [word = target]) in bf16, a piece of the vocabulary at a time
+//   dX       dz W                  fp32, added up over the pieces (and over parts of the vocabulary where there are few tiles)
+//   dW^T     X^T dz                a piece's rows of dW are complete after one product
+// What bounds them is the matrix pipe: 2 T V H operations each, against 2 (T + V) H bytes.
+//
+// A workgroup is 4 wavefronts, one per SIMD, and forms a tile of 256 x 256: each wavefront 128 x 128, 4 x 4 results of
+// v_mfma_f32_32x32x16_bf16 in 256 accumulator registers, so that an operand fragment read from LDS feeds four products.  Steps of 64 along
+// the contraction lie in two LDS buffers of 64 KB, filled by loads that write LDS directly; a step's fragments are read one
+// sixteenth-step ahead of the products, and the one barrier of a step stands where a buffer has been read to its last fragment.
+#include <math.h>
+
+#include "ops.h"
+#include "skrull_loss.h"
+#include "tiles.h"
+
+namespace {
+
+constexpr int kTile = 256;       // rows and columns of a result tile
+constexpr int kStep = 64;        // of the contraction
+constexpr int kOperandBytes = kTile * kStep * 2, kBufferBytes = 2 * kOperandBytes;
+constexpr int kGrid = 256;       // workgroups: one per compute unit, each as much LDS as allows no second one
+constexpr int kStrip = 128;      // words whose largest logit and sum the forward keeps together
+constexpr int64_t kPieceBytes = (int64_t)2 << 30;  // of dz at most
+constexpr int kMaxPieceWords = 1 << 20;            // (32-bit offsets within a tile of dz)
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+enum Kind { kForward, kAgain, kDx, kDw };
+
+struct LossArgs {
+    const uint16_t *x;       // gathered rows [.., Hp]
+    const uint16_t *w;       // [V, H]
+    uint16_t *dz;            // [.., vc]
+    const int32_t *n_rows;   // rows that have a target
+    const int32_t *target;   // of the gathered rows
+    const float *lse, *d;    // of the gathered rows (kAgain)
+    float *z_target;         // of the gathered rows (kForward)
+    float2 *strips;          // [strips][Tp] (kForward)
+    float *slabs;            // [splits][rows][Hp] (kDx)
+    uint16_t *dw;            // [V, H] (kDw)
+    int64_t Tp;
+    int32_t V, H, Hp, v0, vc;
+    int32_t first;           // kDx: the first piece (slabs are written, not added to)
+};
+
+// How many parts the vocabulary of a piece is cut into for dX, so that all compute units have a tile: the partial sums are slabs
+// of their own, added up at the end in order.
+__host__ __device__ inline int dx_splits(int tiles, int steps)
+{
+    const int s = kGrid / tiles;
+    return s < 1 ? 1 : s > steps ? steps : s;
+}
+
+// Where an operand's step lies and how much of its matrix is behind that address.
+struct Source {
+    const unsigned char *at;
+    int64_t left;
+    uint32_t pitch;       // bytes between rows
+    int64_t step;         // bytes from one step to the next
+    __device__ __forceinline__ i32x4 words() const
+    {
+        const int64_t n = left < 0 ? 0 : left > 0x7fffffff ? 0x7fffffff : left;
+        return rsrc_words(at, (uint32_t)n);
+    }
+    __device__ __forceinline__ void next() { at += step; left -= step; }
+};
+
+// A tile's operand in LDS, 32 KB, in one of two forms.  Its 16-byte pieces are laid out by the loads (slot = lane), so the
+// arrangement is made on the global side: a lane fetches the piece that belongs where it writes.
+//   ROWS  256 rows x 64 of the contraction (128 bytes a row): piece c of row r lies at c ^ (r / 2 & 7), so 16 rows' pieces of
+//         one c, which are read together, are 16 different slots of the 256 bytes that the banks span.
+//   COLS  64 of the contraction x 256 columns (512 bytes a row): piece c of row r lies at c ^ (r & 3) << 2, so the 4 rows x 64 bytes
+//         that a transposing read takes together are 16 different slots too.
+template <bool COLS>
+struct Operand {
+    int load[2];     // byte offsets of this lane's pieces in the tile's matrix: of even and odd instructions
+    int read[4];     // LDS offsets of its fragments: ROWS by sixteenth-step, COLS by block of 32 columns
+
+    __device__ __forceinline__ void init(int lane, int wave, int part, uint32_t pitch)
+    {
+        const int n = lane & 31, h = lane >> 5;
+        if (!COLS) {
+#pragma unroll
+            for (int o = 0; o < 2; ++o) load[o] = (wave * 64 + (lane >> 3)) * (int)pitch + (((lane & 7) ^ (4 * o + (lane >> 4))) << 4);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) read[k] = (part * 128 + n) * 128 + (((2 * k + h) ^ ((n >> 1) & 7)) << 4);
+        } else {
+#pragma unroll
+            for (int o = 0; o < 2; ++o) load[o] = (wave * 16 + (lane >> 5)) * (int)pitch + (((lane & 31) ^ ((2 * o + (lane >> 5)) << 2)) << 4);
+            const int s = lane & 15;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                read[t] = (8 * h + (s >> 2)) * 512 + ((4 * (4 * part + (t ^ (s >> 2))) + 2 * ((n >> 4) & 1) + ((s & 3) >> 1)) << 4) + 8 * (s & 1);
+        }
+    }
+    // 8 instructions of a wavefront fill a quarter of the tile.  `tail`: elements of the contraction that are left, where
+    // rows may end inside the step (ROWS): what is behind them reads as zero.
+    __device__ __forceinline__ void fetch(const Source &src, uint32_t lds, int wave, int lane, int tail, int q) const
+    {
+        int off = load[q & 1];
+        if (!COLS && tail < kStep) {
+            const int piece = (lane & 7) ^ (4 * (q & 1) + (lane >> 4));
+            if (piece * 8 >= tail) off = (int)0x80000000;   // (past every descriptor's end)
+        }
+        dma_b128(src.words(), lds + (wave * 8 + q) * 1024, off, (int)(q * (COLS ? 2 : 8) * src.pitch));
+    }
+    // fragment b (32 rows or columns) of sixteenth-step k: 8 consecutive elements of the contraction
+    __device__ __forceinline__ bf16x8 get(const unsigned char *t, int b, int k) const
+    {
+        if (!COLS) return *(const bf16x8 *)(t + read[k] + b * 4096);
+        typedef s16x4 __attribute__((address_space(3))) * lds_ptr_t;
+        const unsigned char *p = t + read[b] + k * 8192;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)p);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(p + 2048));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
+
+// The tiles of a product and their operands.
+template <Kind K>
+struct Product {
+    int mt, nt, splits, steps, total;   // tiles of M and N; parts of the contraction, steps of a part
+
+    __device__ __forceinline__ void init(const LossArgs &p, int n_rows)
+    {
+        const int row_tiles = max(1, (n_rows + kTile - 1) / kTile), h_tiles = (p.H + kTile - 1) / kTile;
+        splits = 1;
+        if (K == kForward || K == kAgain) {
+            mt = K == kForward ? (p.V + kTile - 1) / kTile : p.vc / kTile;
+            nt = row_tiles;
+            steps = p.Hp / kStep;
+        } else if (K == kDx) {
+            mt = row_tiles;
+            nt = h_tiles;
+            splits = dx_splits(mt * nt, p.vc / kStep);
+            steps = (p.vc / kStep + splits - 1) / splits;
+        } else {
+            mt = h_tiles;
+            nt = p.vc / kTile;
+            steps = max(1, (n_rows + kStep - 1) / kStep);
+        }
+        total = mt * nt * splits;
+    }
+    // Tiles in the order of work: blocks of 8 tiles of M, through all of N.  Neighbours in it run at the same time on one die, 8 x 4 tiles
+    // that share their operands in its L2.
+    __device__ __forceinline__ void locate(int i, int &m, int &n, int &s) const
+    {
+        s = i / (mt * nt);
+        i -= s * (mt * nt);
+        const int block = i / (8 * nt), r = i - block * (8 * nt), width = min(8, mt - block * 8);
+        n = r / width;
+        m = block * 8 + r - n * width;
+    }
+    // steps of part s (the last one may have fewer, or none)
+    __device__ __forceinline__ int steps_of(const LossArgs &p, int s) const
+    {
+        return K == kDx ? max(0, min(steps, p.vc / kStep - s * steps)) : steps;
+    }
+    __device__ __forceinline__ void sources(const LossArgs &p, int m, int n, int s, Source &a, Source &b) const
+    {
+        const int64_t H2 = (int64_t)p.H * 2, Hp2 = (int64_t)p.Hp * 2, vc2 = (int64_t)p.vc * 2;
+        if (K == kForward || K == kAgain) {
+            const int64_t v = p.v0 + (int64_t)m * kTile;
+            a = Source{(const unsigned char *)p.w + v * H2, min((int64_t)kTile, p.V - v) * H2, (uint32_t)H2, kStep * 2};
+            b = Source{(const unsigned char *)p.x + (int64_t)n * kTile * Hp2, kTile * Hp2, (uint32_t)Hp2, kStep * 2};
+        } else if (K == kDx) {
+            const int64_t k0 = (int64_t)s * steps * kStep;
+            a = Source{(const unsigned char *)p.dz + (int64_t)m * kTile * vc2 + k0 * 2, kTile * vc2 - k0 * 2, (uint32_t)vc2, kStep * 2};
+            b = Source{(const unsigned char *)p.w + (p.v0 + k0) * H2 + n * kTile * 2, (p.V - p.v0 - k0) * H2 - n * kTile * 2, (uint32_t)H2, kStep * H2};
+        } else {
+            const int64_t rows = (int64_t)steps * kStep;
+            a = Source{(const unsigned char *)p.x + m * kTile * 2, rows * Hp2 - m * kTile * 2, (uint32_t)Hp2, kStep * Hp2};
+            b = Source{(const unsigned char *)p.dz + (int64_t)n * kTile * 2, rows * vc2 - (int64_t)n * kTile * 2, (uint32_t)vc2, kStep * vc2};
+        }
+    }
+};
+
+// A result that lies in an accumulator register.  (Read as ordinary values, all 256 were copied to vector registers at the end of the loop,
+// and what was there before went to scratch memory.)
+__device__ __forceinline__ float result(float f)
+{
+    float r;
+    asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(r) : "a"(f));
+    return r;
+}
+
+template <Kind K>
+__global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
+{
+    constexpr bool A_COLS = K == kDw, B_COLS = K == kDx || K == kDw;
+    __shared__ __align__(1024) unsigned char lds[2 * kBufferBytes];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1;
+    const int n = lane & 31, h = lane >> 5;
+    const int n_rows = __builtin_amdgcn_readfirstlane(*p.n_rows);
+    Product<K> work;
+    work.init(p, n_rows);
+
+    const uint32_t a_pitch = (uint32_t)(K == kDx ? p.vc : K == kDw ? p.Hp : p.H) * 2, b_pitch = (uint32_t)(K == kDx ? p.H : K == kDw ? p.vc : p.Hp) * 2;
+    Operand<A_COLS> A;
+    Operand<B_COLS> B;
+    A.init(lane, wave, wm, a_pitch);
+    B.init(lane, wave, wn, b_pitch);
+    const uint32_t lds0 = lds_addr(lds);
+
+    const int die = blockIdx.x & 7, per_die = (work.total + 7) / 8;
+    const int end = min(work.total, (die + 1) * per_die);
+    for (int i = die * per_die + (blockIdx.x >> 3); i < end; i += gridDim.x >> 3) {
+        int m, nn, s;
+        work.locate(i, m, nn, s);
+        const int steps = work.steps_of(p, s);
+        Source sa, sb;
+        work.sources(p, m, nn, s, sa, sb);
+        f32x16 acc[4][4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[x][y][v] = 0.0f;
+        const int a_tail = K == kForward || K == kAgain ? p.H : 0x7fffffff;   // elements of the contraction
+
+        auto fetch = [&](int step, int q) {
+            const uint32_t to = lds0 + (step & 1) * kBufferBytes;
+            A.fetch(sa, to, wave, lane, a_tail - step * kStep, q);
+            B.fetch(sb, to + kOperandBytes, wave, lane, kStep, q);
+        };
+        __syncthreads();   // the tile before has been read
+        if (steps > 0) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) fetch(0, q);
+            sa.next();
+            sb.next();
+        }
+        if (steps > 1) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) fetch(1, q);
+            sa.next();
+            sb.next();
+        }
+        for (int step = 0; step < steps; ++step) {
+            // 16 loads of the next step may be under way
+            if (step + 1 < steps) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            const unsigned char *ta = lds + (step & 1) * kBufferBytes, *tb = ta + kOperandBytes;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                bf16x8 a[4], b[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) { a[x] = A.get(ta, x, k); b[x] = B.get(tb, x, k); }
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) acc[x][y] = mfma32(a[x], b[y], acc[x][y]);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (step + 2 < steps) {
+#pragma unroll
+                for (int q = 0; q < 8; ++q) fetch(step + 2, q);
+                sa.next();
+                sb.next();
+            }
+        }
+
+        // (the compiler does not see that what follows reads results of the matrix pipe: the distance it would keep)
+        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+        // acc[x][y][v] is row 128 wm + 32 x + 8 (v / 4) + 4 h + v % 4 and column 128 wn + 32 y + n of the tile
+        if (K == kForward) {
+            const int strip = m * 2 + wm;
+            const int words = p.V - strip * kStrip - 4 * h;   // of the strip, from this lane's first one on
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const int row = nn * kTile + wn * 128 + y * 32 + n;
+                SB();
+                float most = -INFINITY;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    SB();
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        if (x * 32 + 8 * (v >> 2) + (v & 3) < words) most = fmaxf(most, result(acc[x][y][v]));
+                }
+                most = fmaxf(most, __shfl_xor(most, 32));
+                // (no word at all, or an infinite logit: nothing is subtracted, so the sum is 0 or infinite and not NaN)
+                const float shift = fabsf(most) < INFINITY ? most * kLog2e : 0.0f;
+                float sum = 0.0f;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    SB();
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const float e = fast_exp2(result(acc[x][y][v]) * kLog2e - shift);
+                        sum += x * 32 + 8 * (v >> 2) + (v & 3) < words ? e : 0.0f;
+                    }
+                }
+                sum += __shfl_xor(sum, 32);
+                if (h == 0) p.strips[(int64_t)strip * p.Tp + row] = make_float2(most, sum);
+                const int t = p.target[row] - (m * kTile + wm * kStrip);   // (gathered rows are padded to whole tiles)
+                if (__any(t >= 0 && t < kStrip)) {
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v)
+                            if (t == x * 32 + 8 * (v >> 2) + 4 * h + (v & 3) && row < n_rows) p.z_target[row] = result(acc[x][y][v]);
+                }
+            }
+        } else if (K == kAgain) {
+            const int word0 = p.v0 + m * kTile + wm * kStrip + 4 * h;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const int row = nn * kTile + wn * 128 + y * 32 + n;
+                const float lse = p.lse[row] * kLog2e, d = p.d[row];
+                const int t = p.target[row] - word0;
+                uint16_t *out = p.dz + (int64_t)row * p.vc + (word0 - p.v0);
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        SB();
+                        float e[4];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const int word = x * 32 + 8 * g + r;
+                            float f = fast_exp2(result(acc[x][y][4 * g + r]) * kLog2e - lse);
+                            if (word == t) f -= 1.0f;
+                            e[r] = word0 + word < p.V ? f * d : 0.0f;
+                        }
+                        *(uint2 *)(out + x * 32 + 8 * g) = make_uint2(pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]));
+                    }
+            }
+        } else if (K == kDx) {
+            float *out = p.slabs + ((int64_t)(s * work.mt + m) * kTile + wm * 128) * p.Hp + nn * kTile + wn * 128;   // (the same for all lanes)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                if (nn * kTile + wn * 128 + y * 32 + n < p.H) {
+                    const uint32_t mine = 4 * h * p.Hp + y * 32 + n;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            SB();
+                            float *rows = out + (x * 32 + 8 * g) * p.Hp;
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                float *to = rows + r * p.Hp + mine, f = result(acc[x][y][4 * g + r]);
+                                *to = p.first ? f : *to + f;
+                            }
+                        }
+                }
+            }
+        } else {
+            const int col0 = m * kTile + wm * 128 + 4 * h;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const int word = p.v0 + nn * kTile + wn * 128 + y * 32 + n;
+                if (word < p.V) {
+                    uint16_t *out = p.dw + (int64_t)word * p.H + col0;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+#pragma unroll
+                        for (int g = 0; g < 4; ++g)
+                            if (col0 + x * 32 + 8 * g < p.H)
+                                *(uint2 *)(out + x * 32 + 8 * g) = make_uint2(pack_bf16(result(acc[x][y][4 * g]), result(acc[x][y][4 * g + 1])),
+                                                                              pack_bf16(result(acc[x][y][4 * g + 2]), result(acc[x][y][4 * g + 3])));
+                }
+            }
+        }
+    }
+}
+
+// Which rows have a target, in order: one workgroup, 8 rows to a thread at a time.
+struct RowsArgs {
+    const int64_t *target;   // [T]
+    const float *lse, *d;    // [T], backward
+    int64_t T;
+    int32_t V;
+    int32_t *n_rows, *slot, *row, *target_of;  // count; [T] gathered row or -1; [Tp] its row; [Tp] its target
+    float *lse_of, *d_of;    // [Tp], backward
+    float *loss, *lse_out;   // [T], forward: zeros where there is no target
+    float *z_target;         // [Tp], forward: NaN until the product finds the target's word
+};
+template <bool BACKWARD>
+__global__ __launch_bounds__(1024) void loss_rows_kernel(const RowsArgs a)
+{
+    constexpr int EACH = 8;
+    __shared__ int counts[16];
+    __shared__ int before;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (threadIdx.x == 0) before = 0;
+    __syncthreads();
+    for (int64_t base = 0; base < a.T; base += 1024 * EACH) {
+        const int64_t t0 = base + threadIdx.x * EACH;
+        int64_t target[EACH];
+        int mine = 0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            target[i] = t0 + i < a.T ? a.target[t0 + i] : -1;
+            mine += target[i] >= 0;
+        }
+        int upto = mine;   // of this thread and those before it in the wavefront
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+            const int o = __shfl_up(upto, m);
+            if (lane >= m) upto += o;
+        }
+        if (lane == 63) counts[wave] = upto;
+        __syncthreads();
+        int at = before + upto - mine;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) at += k < wave ? counts[k] : 0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int64_t t = t0 + i;
+            if (t >= a.T) break;
+            if (target[i] < 0) {
+                a.slot[t] = -1;
+                if (!BACKWARD) { a.loss[t] = 0.0f; a.lse_out[t] = 0.0f; }
+                continue;
+            }
+            const bool outside = target[i] >= a.V;
+            a.slot[t] = at;
+            a.row[at] = (int32_t)t;
+            a.target_of[at] = outside ? -1 : (int32_t)target[i];
+            if (BACKWARD) {
+                a.lse_of[at] = a.lse[t];
+                a.d_of[at] = outside ? NAN : a.d[t];
+            } else {
+                a.z_target[at] = NAN;
+            }
+            ++at;
+        }
+        __syncthreads();
+        if (threadIdx.x == 1023) before = at;
+        __syncthreads();
+    }
+    const int n = before, padded = max(1, (n + kTile - 1) / kTile) * kTile;
+    if (threadIdx.x == 0) *a.n_rows = n;
+    for (int i = n + threadIdx.x; i < padded; i += 1024) {   // rows that fill the last tile: no gradient, no word
+        a.target_of[i] = -1;
+        if (BACKWARD) { a.lse_of[i] = 0.0f; a.d_of[i] = 0.0f; }
+    }
+}
+
+// X: the gathered rows, padded with zeros.
+__global__ __launch_bounds__(256) void loss_gather_kernel(const uint16_t *x, int64_t x_stride, int wide, const int32_t *n_rows, const int32_t *row,
+                                                          uint16_t *out, int H, int Hp)
+{
+    const int n = *n_rows, padded = max(1, (n + kTile - 1) / kTile) * kTile;
+    for (int r = blockIdx.x; r < padded; r += gridDim.x) {
+        const uint16_t *in = r < n ? x + (int64_t)row[r] * x_stride : nullptr;
+        uint16_t *to = out + (int64_t)r * Hp;
+        for (int c = threadIdx.x * 8; c < Hp; c += 256 * 8) {
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (in && c < H) {
+                if (wide) {
+                    v = *(const uint4 *)(in + c);
+                } else {
+                    uint16_t e[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) e[i] = in[c + i];
+                    v = make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
+                }
+            }
+            *(uint4 *)(to + c) = v;
+        }
+    }
+}
+
+// lse and loss from the strips: 64 rows to a workgroup, 16 wavefronts share the strips.
+__global__ __launch_bounds__(1024) void loss_sums_kernel(const float2 *strips, int n_strips, int64_t Tp, const int32_t *n_rows, const int32_t *row,
+                                                         const float *z_target, float *loss, float *lse)
+{
+    __shared__ float2 part[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = blockIdx.x * 64 + lane, n = *n_rows;
+    if ((int)blockIdx.x * 64 >= n) return;
+    // largest logit and the sum of exponentials relative to it (0 where that is not finite)
+    auto shift_of = [](float most) { return fabsf(most) < INFINITY ? most : 0.0f; };
+    auto add = [&](float &most, float &sum, float2 b) {
+        const float m = fmaxf(most, b.x), s = shift_of(m);
+        sum = sum * fast_exp2((shift_of(most) - s) * kLog2e) + b.y * fast_exp2((shift_of(b.x) - s) * kLog2e);
+        most = m;
+    };
+    float most = -INFINITY, sum = 0.0f;
+#pragma unroll 4
+    for (int i = wave; i < n_strips; i += 16) add(most, sum, strips[(int64_t)i * Tp + r]);   // (r is within the padded rows)
+    part[wave][lane] = make_float2(most, sum);
+    __syncthreads();
+    if (wave == 0 && r < n) {
+#pragma unroll
+        for (int k = 1; k < 16; ++k) add(most, sum, part[k][lane]);
+        const float l = shift_of(most) + logf(sum);
+        const int t = row[r];
+        lse[t] = l;
+        loss[t] = l - z_target[r];
+    }
+}
+
+// dx of every row: the parts' sums, or zeros.
+__global__ __launch_bounds__(256) void loss_dx_kernel(const float *slabs, const int32_t *n_rows, const int32_t *slot, uint16_t *dx, int64_t T, int H, int Hp,
+                                                      int steps)
+{
+    const int tiles = max(1, (*n_rows + kTile - 1) / kTile), splits = dx_splits(tiles * ((H + kTile - 1) / kTile), steps);
+    const int64_t slab = (int64_t)tiles * kTile * Hp;
+    for (int64_t t = blockIdx.x; t < T; t += gridDim.x) {
+        const int s = slot[t];
+        for (int c = threadIdx.x * 8; c < H; c += 256 * 8) {
+            float f[8] = {};
+            if (s >= 0) {
+                const float *from = slabs + (int64_t)s * Hp + c;
+                for (int k = 0; k < splits; ++k, from += slab) {
+                    const float4 u = ((const float4 *)from)[0], v = ((const float4 *)from)[1];
+                    f[0] += u.x; f[1] += u.y; f[2] += u.z; f[3] += u.w; f[4] += v.x; f[5] += v.y; f[6] += v.z; f[7] += v.w;
+                }
+            }
+            *(uint4 *)(dx + t * H + c) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+        }
+    }
+}
+
+// The workspace, from sizes alone.
+struct Layout {
+    int64_t Tp, Hp, vc, pieces;
+    int64_t n_rows, slot, row, target, lse, d, z_target, x, strips, dz, slabs, bytes;
+    Layout(const skrull_loss_t &p, bool backward)
+    {
+        Tp = (p.rows + kTile - 1) / kTile * kTile;
+        if (Tp == 0) Tp = kTile;
+        Hp = (p.hidden + kStep - 1) / kStep * kStep;
+        const int64_t words = ((int64_t)p.vocab + kTile - 1) / kTile * kTile;
+        int64_t most = kPieceBytes / (Tp * 2) / kTile * kTile;
+        most = most < kTile ? kTile : most > kMaxPieceWords ? kMaxPieceWords : most;
+        pieces = (words + most - 1) / most;
+        vc = (words / kTile + pieces - 1) / pieces * kTile;
+        pieces = (words + vc - 1) / vc;
+        bytes = 0;
+        auto take = [&](int64_t n) { const int64_t at = bytes; bytes += (n + 255) & ~(int64_t)255; return at; };
+        n_rows = take(4);
+        slot = take(p.rows * 4);
+        row = take(Tp * 4);
+        target = take(Tp * 4);
+        x = take(Tp * Hp * 2);
+        lse = d = z_target = strips = dz = slabs = 0;
+        if (backward) {
+            lse = take(Tp * 4);
+            d = take(Tp * 4);
+            dz = take(Tp * vc * 2);
+            // (parts of the vocabulary are made only where there are fewer tiles than compute units)
+            const int64_t h_tiles = (p.hidden + kTile - 1) / kTile, parted = kGrid / h_tiles * kTile;
+            slabs = take((Tp > parted ? Tp : parted) * Hp * 4);
+        } else {
+            z_target = take(Tp * 4);
+            strips = take(words / kStrip * Tp * 8);
+        }
+    }
+};
+
+int check(const skrull_loss_t *p)
+{
+    if (!p) return refuse("loss: null pointer");
+    if (p->rows < 0 || p->rows > 1 << 24) return refuse("loss: %lld rows", (long long)p->rows);
+    if (p->hidden < 8 || p->hidden > 65536 || p->hidden % 8 != 0) return refuse("loss: hidden %d is not a multiple of 8 from 8 to 65536", p->hidden);
+    if (p->vocab < 1 || p->vocab > 1 << 24) return refuse("loss: vocab %d", p->vocab);
+    if (p->x_stride < p->hidden || p->x_stride > (int64_t)1 << 32) return refuse("loss: x_stride %lld", (long long)p->x_stride);
+    return SKRULL_OK;
+}
+
+// Gathers the rows; the first two kernels of either direction.
+template <bool BACKWARD>
+hipError_t gather(const skrull_loss_t &p, const Layout &l, unsigned char *ws, const void *x, const int64_t *target, const float *lse, const float *d,
+                  float *loss, float *lse_out, hipStream_t st)
+{
+    RowsArgs a = {};
+    a.target = target; a.lse = lse; a.d = d; a.T = p.rows; a.V = p.vocab;
+    a.n_rows = (int32_t *)(ws + l.n_rows); a.slot = (int32_t *)(ws + l.slot); a.row = (int32_t *)(ws + l.row); a.target_of = (int32_t *)(ws + l.target);
+    a.lse_of = (float *)(ws + l.lse); a.d_of = (float *)(ws + l.d); a.loss = loss; a.lse_out = lse_out; a.z_target = (float *)(ws + l.z_target);
+    loss_rows_kernel<BACKWARD><<<1, 1024, 0, st>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int wide = aligned_to(x, 16) && p.x_stride % 8 == 0;
+    loss_gather_kernel<<<(int)(l.Tp < 2048 ? l.Tp : 2048), 256, 0, st>>>((const uint16_t *)x, p.x_stride, wide, a.n_rows, a.row, (uint16_t *)(ws + l.x), p.hidden, (int)l.Hp);
+    return hipGetLastError();
+}
+
+LossArgs args_of(const skrull_loss_t &p, const Layout &l, unsigned char *ws, const void *w)
+{
+    LossArgs a = {};
+    a.x = (const uint16_t *)(ws + l.x); a.w = (const uint16_t *)w;
+    a.n_rows = (const int32_t *)(ws + l.n_rows); a.target = (const int32_t *)(ws + l.target);
+    a.Tp = l.Tp; a.V = p.vocab; a.H = p.hidden; a.Hp = (int32_t)l.Hp;
+    return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t skrull_loss_workspace(const skrull_loss_t *p, int backward)
+{
+    return check(p) == SKRULL_OK ? Layout(*p, backward != 0).bytes : 0;
+}
+
+int skrull_loss_fwd(const skrull_loss_t *p, const void *x, const void *w, const int64_t *target, float *loss, float *lse,
+                    void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (int rc = check(p)) return rc;
+    if (p->rows == 0) return SKRULL_OK;
+    if (!x || !aligned_to(x, 2) || !w || !aligned_to(w, 16) || !target || !aligned_to(target, 8) || !loss || !aligned_to(loss, 4) || !lse ||
+        !aligned_to(lse, 4) || !workspace || !aligned_to(workspace, 16))
+        return refuse("loss: null or misaligned pointer");
+    const Layout l(*p, false);
+    if ((int64_t)workspace_bytes < l.bytes) return refuse("loss: workspace below %lld bytes", (long long)l.bytes);
+    int compute_units = 0;
+    if (int rc = current_device(&compute_units)) return rc;
+    unsigned char *ws = (unsigned char *)workspace;
+    hipStream_t st = (hipStream_t)hip_stream;
+    hipError_t e = gather<false>(*p, l, ws, x, target, nullptr, nullptr, loss, lse, st);
+    if (e == hipSuccess) {
+        LossArgs a = args_of(*p, l, ws, w);
+        a.z_target = (float *)(ws + l.z_target);
+        a.strips = (float2 *)(ws + l.strips);
+        loss_product_kernel<kForward><<<kGrid, 256, 0, st>>>(a);
+        e = hipGetLastError();
+        if (e == hipSuccess) {
+            loss_sums_kernel<<<(int)(l.Tp / 64), 1024, 0, st>>>(a.strips, (p->vocab + kTile - 1) / kTile * 2, l.Tp, a.n_rows, (const int32_t *)(ws + l.row), a.z_target, loss, lse);
+            e = hipGetLastError();
+        }
+    }
+    return e == hipSuccess ? SKRULL_OK : launch_failed(e, "loss launch");
+}
+
+int skrull_loss_bwd(const skrull_loss_t *p, const void *x, const void *w, const int64_t *target, const float *lse, const float *d_loss,
+                    void *dx, void *dw, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (int rc = check(p)) return rc;
+    if (!dx && !dw) return SKRULL_OK;
+    if (!w || !aligned_to(w, 16) || !aligned_to(dx, 16) || !aligned_to(dw, 16) || !workspace || !aligned_to(workspace, 16))
+        return refuse("loss: null or misaligned pointer");
+    if (p->rows > 0 && (!x || !aligned_to(x, 2) || !target || !aligned_to(target, 8) || !lse || !aligned_to(lse, 4) || !d_loss || !aligned_to(d_loss, 4)))
+        return refuse("loss: null or misaligned pointer");
+    const Layout l(*p, true);
+    if ((int64_t)workspace_bytes < l.bytes) return refuse("loss: workspace below %lld bytes", (long long)l.bytes);
+    int compute_units = 0;
+    if (int rc = current_device(&compute_units)) return rc;
+    unsigned char *ws = (unsigned char *)workspace;
+    hipStream_t st = (hipStream_t)hip_stream;
+    hipError_t e = gather<true>(*p, l, ws, x, target, lse, d_loss, nullptr, nullptr, st);
+    LossArgs a = args_of(*p, l, ws, w);
+    a.lse = (const float *)(ws + l.lse);
+    a.d = (const float *)(ws + l.d);
+    a.dz = (uint16_t *)(ws + l.dz);
+    a.slabs = (float *)(ws + l.slabs);
+    a.dw = (uint16_t *)dw;
+    a.vc = (int32_t)l.vc;
+    for (int64_t i = 0; i < l.pieces && e == hipSuccess; ++i) {
+        a.v0 = (int32_t)(i * l.vc);
+        a.first = i == 0;
+        loss_product_kernel<kAgain><<<kGrid, 256, 0, st>>>(a);
+        e = hipGetLastError();
+        if (e == hipSuccess && dx) {
+            loss_product_kernel<kDx><<<kGrid, 256, 0, st>>>(a);
+            e = hipGetLastError();
+        }
+        if (e == hipSuccess && dw) {
+            loss_product_kernel<kDw><<<kGrid, 256, 0, st>>>(a);
+            e = hipGetLastError();
+        }
+    }
+    if (e == hipSuccess && dx && p->rows > 0) {
+        loss_dx_kernel<<<(int)(p->rows < 4096 ? p->rows : 4096), 256, 0, st>>>(a.slabs, a.n_rows, (const int32_t *)(ws + l.slot), (uint16_t *)dx, p->rows, p->hidden, (int)l.Hp, (int)(l.vc / kStep));
+        e = hipGetLastError();
+    }
+    return e == hipSuccess ? SKRULL_OK : launch_failed(e, "loss launch");
+}
+
+}  // extern "C"

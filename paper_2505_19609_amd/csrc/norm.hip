@@ -1,0 +1,433 @@
+// The norm of packed rows, forward and backward (include/skrull_norm.h).
+//
+// What bounds it: memory.  The forward reads x and writes y, the backward reads x and dy and writes dx, each once: a row stays in the
+// registers of the lanes that share it from its load to its store, so the sums cost no second read.  Lanes keep the same columns for
+// all rows of their workgroup, so w is read once per workgroup, and dw and db are summed over the rows in registers; what the workgroups
+// have is added up by a second kernel in a fixed order (no atomics).
+//
+// A row belongs to 64 lanes (up to 1,024 columns), 256 (up to 4,096) or 1,024 (up to 8,192), each with one or two pieces of 8 columns: so a row's
+// values, weights and gradients fit the registers at every width.  (1,024 lanes of two pieces, for 16,384 columns, do not: the backward spilled.)
+#include <hip/hip_runtime.h>
+
+#include <math.h>
+
+#include "mfma.h"
+#include "ops.h"
+#include "skrull_norm.h"
+
+namespace {
+
+struct NormArgs {
+    const void *x, *w, *b, *dy;
+    void *y;                 // y, or dx
+    float *mean, *rstd;
+    float *partial;          // [workgroups][dw, then db: cols each], or null
+    int64_t x_stride, y_stride, dy_stride;
+    int64_t rows;
+    int32_t cols, weight_type, wide;  // wide: 16-byte loads and stores are aligned
+    float eps, inv_cols;
+};
+
+__device__ __forceinline__ float bf16_at(uint16_t u) { return __builtin_bit_cast(float, (uint32_t)u << 16); }
+__device__ __forceinline__ uint16_t to_bf16(float f) { return (uint16_t)pack_bf16(f, f); }
+
+struct Bf16 {
+    typedef uint16_t type;
+    static __device__ __forceinline__ float get(uint16_t u) { return bf16_at(u); }
+    static __device__ __forceinline__ uint16_t put(float f) { return to_bf16(f); }
+    static __device__ __forceinline__ void load8(const uint16_t *p, float f[8])
+    {
+        const uint4 v = *(const uint4 *)p;
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] = __builtin_bit_cast(float, w[i] << 16);
+            f[2 * i + 1] = __builtin_bit_cast(float, w[i] & 0xffff0000u);
+        }
+    }
+    static __device__ __forceinline__ void store8(uint16_t *p, const float f[8])
+    {
+        *(uint4 *)p = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+    }
+};
+struct Fp32 {
+    typedef float type;
+    static __device__ __forceinline__ float get(float u) { return u; }
+    static __device__ __forceinline__ float put(float f) { return f; }
+    static __device__ __forceinline__ void load8(const float *p, float f[8])
+    {
+        const float4 a = ((const float4 *)p)[0], b = ((const float4 *)p)[1];
+        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    }
+    static __device__ __forceinline__ void store8(float *p, const float f[8])
+    {
+        ((float4 *)p)[0] = make_float4(f[0], f[1], f[2], f[3]);
+        ((float4 *)p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+    }
+};
+
+// Columns col .. col+7 of a row (or of w), zero behind the last one.
+template <class T>
+__device__ __forceinline__ void load_piece(const typename T::type *row, int col, int cols, bool wide, float f[8])
+{
+    if (wide) {
+        if (col < cols) {
+            T::load8(row + col, f);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = 0.0f;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = col + i < cols ? T::get(row[col + i]) : 0.0f;
+}
+template <class T>
+__device__ __forceinline__ void store_piece(typename T::type *row, int col, int cols, bool wide, const float f[8])
+{
+    if (wide) {
+        if (col < cols) T::store8(row + col, f);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (col + i < cols) row[col + i] = T::put(f[i]);
+}
+__device__ __forceinline__ void load_weight(const void *w, int type, int col, int cols, float f[8])
+{
+    if (type == SKRULL_TYPE_BF16) load_piece<Bf16>((const uint16_t *)w, col, cols, false, f);
+    else load_piece<Fp32>((const float *)w, col, cols, false, f);
+}
+
+// Sums of N values over the lanes of a row, in every lane.  `lds`: room for 2 x 16 x N floats of this row, used by turns.
+template <int WAVES, int N>
+__device__ __forceinline__ void row_sums(float v[N], float *lds, int &turn)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int m = 32; m >= 1; m >>= 1) v[i] += __shfl_xor(v[i], m);
+    if constexpr (WAVES > 1) {
+        float *mine = lds + turn * (WAVES * N);
+        turn ^= 1;   // (the next sums use the other half, so one barrier is enough)
+        const int wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) mine[wave * N + i] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float s = 0.0f;
+#pragma unroll
+            for (int k = 0; k < WAVES; ++k) s += mine[k * N + i];
+            v[i] = s;
+        }
+    }
+}
+
+template <class T, int WAVES, int C, bool CENTER>
+__global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void norm_fwd_kernel(const NormArgs a)
+{
+    constexpr int ROWS = WAVES == 1 ? 4 : 1;   // rows of a workgroup at a time
+    __shared__ float lds[2 * WAVES];
+    int turn = 0;
+    const int slot = ROWS > 1 ? threadIdx.x >> 6 : 0, lane = ROWS > 1 ? threadIdx.x & 63 : threadIdx.x;
+    float w[C][8], b[C][8];
+    int col[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        col[c] = (c * 64 * WAVES + lane) * 8;
+        load_weight(a.w, a.weight_type, col[c], a.cols, w[c]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[c][i] = 0.0f;
+        if (a.b) load_weight(a.b, a.weight_type, col[c], a.cols, b[c]);
+    }
+    for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < a.rows; row0 += (int64_t)gridDim.x * ROWS) {
+        const int64_t row = row0 + slot;
+        if (ROWS > 1 && row >= a.rows) return;   // (a wavefront to a row: nobody waits for it)
+        const typename T::type *xr = (const typename T::type *)a.x + row * a.x_stride;
+        float x[C][8];
+#pragma unroll
+        for (int c = 0; c < C; ++c) load_piece<T>(xr, col[c], a.cols, a.wide, x[c]);
+        float mean = 0.0f;
+        if constexpr (CENTER) {
+            float s[1] = {0.0f};
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[0] += x[c][i];
+            row_sums<WAVES, 1>(s, lds, turn);
+            mean = s[0] * a.inv_cols;
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[c][i] = col[c] + i < a.cols ? x[c][i] - mean : 0.0f;
+        }
+        float q[1] = {0.0f};
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[0] += x[c][i] * x[c][i];
+        row_sums<WAVES, 1>(q, lds, turn);
+        const float rstd = 1.0f / sqrtf(q[0] * a.inv_cols + a.eps);
+        if (lane == 0) {
+            if (CENTER && a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+        typename T::type *yr = (typename T::type *)a.y + row * a.y_stride;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            float y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = x[c][i] * rstd * w[c][i] + b[c][i];
+            store_piece<T>(yr, col[c], a.cols, a.wide, y);
+        }
+    }
+}
+
+template <class T, int WAVES, int C, bool CENTER>
+__global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void norm_bwd_kernel(const NormArgs a)
+{
+    constexpr int ROWS = WAVES == 1 ? 4 : 1;
+    __shared__ float lds[2 * WAVES * 2];
+    int turn = 0;
+    const int slot = ROWS > 1 ? threadIdx.x >> 6 : 0, lane = ROWS > 1 ? threadIdx.x & 63 : threadIdx.x;
+    float w[C][8], dw[C][8], db[C][8];
+    int col[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        col[c] = (c * 64 * WAVES + lane) * 8;
+        load_weight(a.w, a.weight_type, col[c], a.cols, w[c]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[c][i] = db[c][i] = 0.0f;
+    }
+    for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < a.rows; row0 += (int64_t)gridDim.x * ROWS) {
+        const int64_t row = row0 + slot;
+        if (ROWS > 1 && row >= a.rows) break;
+        const float mean = CENTER ? a.mean[row] : 0.0f, rstd = a.rstd[row];
+        const typename T::type *xr = (const typename T::type *)a.x + row * a.x_stride;
+        const typename T::type *dr = (const typename T::type *)a.dy + row * a.dy_stride;
+        float h[C][8], g[C][8];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            load_piece<T>(xr, col[c], a.cols, a.wide, h[c]);
+            load_piece<T>(dr, col[c], a.cols, a.wide, g[c]);
+        }
+        float s[2] = {0.0f, 0.0f};   // sum g h, sum g
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                h[c][i] = (h[c][i] - mean) * rstd;
+                dw[c][i] += g[c][i] * h[c][i];
+                if (CENTER) db[c][i] += g[c][i];
+                g[c][i] *= w[c][i];   // (zero behind the last column, whatever h is there)
+                s[0] += g[c][i] * h[c][i];
+                if (CENTER) s[1] += g[c][i];
+            }
+        if constexpr (CENTER) row_sums<WAVES, 2>(s, lds, turn);
+        else row_sums<WAVES, 1>(s, lds, turn);
+        const float m0 = s[0] * a.inv_cols, m1 = CENTER ? s[1] * a.inv_cols : 0.0f;
+        typename T::type *out = (typename T::type *)a.y + row * a.y_stride;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            float dx[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dx[i] = (g[c][i] - m1 - h[c][i] * m0) * rstd;
+            store_piece<T>(out, col[c], a.cols, a.wide, dx);
+        }
+    }
+    if (!a.partial) return;
+    // each wavefront of a row's own (ROWS of them where a row is one wavefront's) has a line of the partial sums
+    float *line = a.partial + (int64_t)(blockIdx.x * ROWS + slot) * 2 * a.cols;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (col[c] + i < a.cols) {
+                line[col[c] + i] = dw[c][i];
+                if (CENTER) line[a.cols + col[c] + i] = db[c][i];
+            }
+}
+
+// dw and db from the partial sums: 64 columns to a workgroup, 16 wavefronts share the lines, in the order of their number.
+__global__ __launch_bounds__(1024) void norm_sums_kernel(const float *partial, int lines, int cols, void *dw, void *db, int weight_type)
+{
+    __shared__ float part[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+    void *out = blockIdx.y ? db : dw;
+    if (!out) return;   // (the whole workgroup)
+    float s = 0.0f;
+    if (c < cols) {
+        const float *p = partial + blockIdx.y * (int64_t)cols + c;
+#pragma unroll 8
+        for (int i = wave; i < lines; i += 16) s += p[(int64_t)i * 2 * cols];
+    }
+    part[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && c < cols) {
+        s = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) s += part[k][lane];
+        if (weight_type == SKRULL_TYPE_BF16) ((uint16_t *)out)[c] = to_bf16(s);
+        else ((float *)out)[c] = s;
+    }
+}
+
+int size_of(int type) { return type == SKRULL_TYPE_BF16 ? 2 : 4; }
+
+int check(const skrull_norm_t *p)
+{
+    if (!p) return refuse("norm: null pointer");
+    if (p->rows < 0 || p->rows > INT32_MAX) return refuse("norm: %lld rows", (long long)p->rows);
+    if (p->cols < 1 || p->cols > SKRULL_NORM_MAX_COLS) return refuse("norm: %d columns, at most %d", p->cols, SKRULL_NORM_MAX_COLS);
+    if (p->kind != SKRULL_NORM_RMS && p->kind != SKRULL_NORM_LAYER) return refuse("norm: unknown kind %d", p->kind);
+    if (p->type != SKRULL_TYPE_BF16 && p->type != SKRULL_TYPE_FP32) return refuse("norm: unknown type %d", p->type);
+    if (p->weight_type != SKRULL_TYPE_BF16 && p->weight_type != SKRULL_TYPE_FP32) return refuse("norm: unknown weight_type %d", p->weight_type);
+    if (!isfinite(p->eps) || !(p->eps >= 0.0f)) return refuse("norm: eps must be finite and not negative");
+    return SKRULL_OK;
+}
+
+int check_rows(const char *name, const void *ptr, int64_t stride, const skrull_norm_t *p)
+{
+    if (!ptr || !aligned_to(ptr, size_of(p->type))) return refuse("norm: %s is null or misaligned", name);
+    if (stride < p->cols || stride > INT64_MAX / 8 / (p->rows + 1)) return refuse("norm: stride of %s", name);
+    return SKRULL_OK;
+}
+int check_weight(const char *name, const void *ptr, const skrull_norm_t *p)
+{
+    if (ptr && !aligned_to(ptr, size_of(p->weight_type))) return refuse("norm: %s is misaligned", name);
+    return SKRULL_OK;
+}
+int check_apart(const char *out_name, const void *out, int64_t out_stride, const char *in_name, const void *in, int64_t in_stride, const skrull_norm_t *p)
+{
+    if (p->rows == 0 || (in == out && in_stride == out_stride)) return SKRULL_OK;
+    const int64_t s = size_of(p->type);
+    if (overlap(in, ((p->rows - 1) * in_stride + p->cols) * s, out, ((p->rows - 1) * out_stride + p->cols) * s))
+        return refuse("norm: %s overlaps %s", out_name, in_name);
+    return SKRULL_OK;
+}
+
+bool wide_rows(const void *ptr, int64_t stride, const skrull_norm_t *p)
+{
+    return aligned_to(ptr, 16) && stride * size_of(p->type) % 16 == 0;
+}
+
+int waves_of(int cols) { return cols <= 1024 ? 1 : cols <= 4096 ? 4 : 16; }
+
+// Workgroups of the backward, and lines of partial sums: as many as the chip holds at once twice over at the most.
+constexpr int kComputeUnits = 256;
+int64_t bwd_blocks(const skrull_norm_t *p)
+{
+    const int waves = waves_of(p->cols), rows = waves == 1 ? 4 : 1;
+    const int64_t most = waves == 16 ? kComputeUnits : 2 * kComputeUnits, need = (p->rows + rows - 1) / rows;
+    return need < most ? need : most;
+}
+int64_t lines_of(const skrull_norm_t *p) { return bwd_blocks(p) * (waves_of(p->cols) == 1 ? 4 : 1); }
+
+template <class T, bool CENTER>
+void launch(bool backward, const NormArgs &a, int blocks, hipStream_t st)
+{
+    const int cols = a.cols;
+#define SKRULL_NORM_CASE(WAVES, C)                                                                                                     \
+    do {                                                                                                                               \
+        if (backward) norm_bwd_kernel<T, WAVES, C, CENTER><<<blocks, WAVES == 16 ? 1024 : 256, 0, st>>>(a);                            \
+        else norm_fwd_kernel<T, WAVES, C, CENTER><<<blocks, WAVES == 16 ? 1024 : 256, 0, st>>>(a);                                     \
+    } while (0)
+    if (cols <= 512) SKRULL_NORM_CASE(1, 1);
+    else if (cols <= 1024) SKRULL_NORM_CASE(1, 2);
+    else if (cols <= 2048) SKRULL_NORM_CASE(4, 1);
+    else if (cols <= 4096) SKRULL_NORM_CASE(4, 2);
+    else SKRULL_NORM_CASE(16, 1);
+#undef SKRULL_NORM_CASE
+}
+void launch(bool backward, const skrull_norm_t *p, const NormArgs &a, int blocks, hipStream_t st)
+{
+    if (p->type == SKRULL_TYPE_BF16) {
+        if (p->kind == SKRULL_NORM_LAYER) launch<Bf16, true>(backward, a, blocks, st);
+        else launch<Bf16, false>(backward, a, blocks, st);
+    } else {
+        if (p->kind == SKRULL_NORM_LAYER) launch<Fp32, true>(backward, a, blocks, st);
+        else launch<Fp32, false>(backward, a, blocks, st);
+    }
+}
+
+}  // namespace
+
+extern "C" {
+
+int skrull_norm_fwd(const skrull_norm_t *p, const void *x, const void *w, const void *b, void *y, float *mean, float *rstd, void *hip_stream)
+{
+    if (int rc = check(p)) return rc;
+    if (p->rows == 0) return SKRULL_OK;
+    if (int rc = check_rows("x", x, p->x_stride, p)) return rc;
+    if (int rc = check_rows("y", y, p->y_stride, p)) return rc;
+    if (!w) return refuse("norm: w is null");
+    if (int rc = check_weight("w", w, p)) return rc;
+    if (int rc = check_weight("b", b, p)) return rc;
+    if (b && p->kind == SKRULL_NORM_RMS) return refuse("norm: no bias without a mean (SKRULL_NORM_RMS)");
+    if (!aligned_to(mean, 4) || !aligned_to(rstd, 4)) return refuse("norm: mean or rstd is misaligned");
+    if (int rc = check_apart("y", y, p->y_stride, "x", x, p->x_stride, p)) return rc;
+    int compute_units = 0;
+    if (int rc = current_device(&compute_units)) return rc;
+    NormArgs a = {};
+    a.x = x; a.w = w; a.b = b; a.y = y; a.mean = mean; a.rstd = rstd;
+    a.x_stride = p->x_stride; a.y_stride = p->y_stride; a.rows = p->rows; a.cols = p->cols; a.weight_type = p->weight_type;
+    a.wide = p->cols % 8 == 0 && wide_rows(x, p->x_stride, p) && wide_rows(y, p->y_stride, p);
+    a.eps = p->eps; a.inv_cols = 1.0f / (float)p->cols;
+    const int waves = waves_of(p->cols), rows = waves == 1 ? 4 : 1;
+    const int64_t most = (int64_t)compute_units * (waves == 16 ? 2 : 8), need = (p->rows + rows - 1) / rows;
+    launch(false, p, a, (int)(need < most ? need : most), (hipStream_t)hip_stream);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? SKRULL_OK : launch_failed(e, "norm launch");
+}
+
+int64_t skrull_norm_workspace(const skrull_norm_t *p)
+{
+    return check(p) == SKRULL_OK ? lines_of(p) * 2 * p->cols * 4 + 16 : 0;
+}
+
+int skrull_norm_bwd(const skrull_norm_t *p, const void *x, const void *w, const float *mean, const float *rstd, const void *dy,
+                    void *dx, void *dw, void *db, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (int rc = check(p)) return rc;
+    if (int rc = check_weight("dw", dw, p)) return rc;
+    if (int rc = check_weight("db", db, p)) return rc;
+    const bool sums = dw || db;
+    if (db && p->kind == SKRULL_NORM_RMS) return refuse("norm: no gradient of a bias without a mean (SKRULL_NORM_RMS)");
+    if (sums && (!workspace || !aligned_to(workspace, 16) || (int64_t)workspace_bytes < skrull_norm_workspace(p)))
+        return refuse("norm: workspace is null, misaligned or below %lld bytes", (long long)skrull_norm_workspace(p));
+    if (p->rows > 0) {
+        if (int rc = check_rows("x", x, p->x_stride, p)) return rc;
+        if (int rc = check_rows("dy", dy, p->dy_stride, p)) return rc;
+        if (int rc = check_rows("dx", dx, p->dx_stride, p)) return rc;
+        if (!w) return refuse("norm: w is null");
+        if (int rc = check_weight("w", w, p)) return rc;
+        if (!rstd || !aligned_to(rstd, 4) || (p->kind == SKRULL_NORM_LAYER && (!mean || !aligned_to(mean, 4))))
+            return refuse("norm: mean or rstd is null or misaligned");
+        if (int rc = check_apart("dx", dx, p->dx_stride, "x", x, p->x_stride, p)) return rc;
+        if (int rc = check_apart("dx", dx, p->dx_stride, "dy", dy, p->dy_stride, p)) return rc;
+    }
+    int compute_units = 0;
+    if (int rc = current_device(&compute_units)) return rc;
+    hipStream_t st = (hipStream_t)hip_stream;
+    hipError_t e = hipSuccess;
+    if (p->rows > 0) {
+        NormArgs a = {};
+        a.x = x; a.w = w; a.dy = dy; a.y = dx; a.mean = const_cast<float *>(mean); a.rstd = const_cast<float *>(rstd);
+        a.partial = sums ? (float *)workspace : nullptr;
+        a.x_stride = p->x_stride; a.y_stride = p->dx_stride; a.dy_stride = p->dy_stride; a.rows = p->rows; a.cols = p->cols;
+        a.weight_type = p->weight_type;
+        a.wide = p->cols % 8 == 0 && wide_rows(x, p->x_stride, p) && wide_rows(dy, p->dy_stride, p) && wide_rows(dx, p->dx_stride, p);
+        a.inv_cols = 1.0f / (float)p->cols;
+        launch(true, p, a, (int)bwd_blocks(p), st);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess && sums) {
+        norm_sums_kernel<<<dim3((unsigned)((p->cols + 63) / 64), 2), 1024, 0, st>>>((const float *)workspace, (int)lines_of(p), p->cols, dw, db, p->weight_type);
+        e = hipGetLastError();
+    }
+    return e == hipSuccess ? SKRULL_OK : launch_failed(e, "norm launch");
+}
+
+}  // extern "C"

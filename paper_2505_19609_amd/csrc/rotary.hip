@@ -1,0 +1,217 @@
+// Rotary positions of a plan's packed rows (include/skrull_rotary.h).
+//
+// What bounds it: every element of Q and K is read and written once, 4 bytes, and meets two products; the
+// sines and cosines are one pair per (row, pair of elements), shared by all heads of the row.  So a workgroup takes a few whole rows,
+// forms their sines and cosines once into LDS and streams the heads through, 16 bytes per load and store.  The positions come from
+// the plan's descriptor (which segment a row is in), so nothing but the tensors themselves is read per element.
+#include <math.h>
+
+#include <hip/hip_bf16.h>
+
+#include "mfma.h"
+#include "ops.h"
+#include "skrull_rotary.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxRows = 32;    // rows of a workgroup at most
+constexpr int kMaxPairs = 64;   // head_dim / 2
+
+struct Tensor {
+    const uint16_t *in;
+    uint16_t *out;
+    int64_t in_stride, out_stride;
+    const int32_t *cu;      // [NS+1] first row of each segment
+    const int32_t *begin;   // [NS] position of its first row, or null: 0
+    int32_t heads, rows, rows_per_block, blocks;
+    uint64_t inv_row;       // ceil(2^40 / units of a row)
+};
+
+struct Args {
+    Tensor t[2];
+    int32_t NS, head_dim, rotary_dim, scaling, copies;   // copies: `out` is other memory, the elements that are not turned go along
+    uint64_t inv_unit;      // ceil(2^40 / units of a head)
+    double log2_base, factor, turns_scale, low_turns, high_turns;   // turns_scale: original_length
+    float amplitude, sign;
+};
+
+// x / d with inv = ceil(2^40 / d): exact while x * d < 2^40
+__device__ __forceinline__ int quotient40(int x, uint64_t inv) { return (int)(((uint64_t)(uint32_t)x * inv) >> 40); }
+
+// Turns per position of pair i.
+__device__ double turns_of(const Args &a, int i)
+{
+    constexpr double kTurn = 0.15915494309189533577;  // 1 / (2 pi)
+    const double f = exp2(-a.log2_base * (double)(2 * i) / (double)a.rotary_dim) * kTurn;
+    if (a.scaling == SKRULL_ROTARY_LINEAR) return f / a.factor;
+    if (a.scaling == SKRULL_ROTARY_PARTS) {
+        const double g = fmin(fmax((a.turns_scale * f - a.low_turns) / (a.high_turns - a.low_turns), 0.0), 1.0);
+        return f * (g + (1.0 - g) / a.factor);
+    }
+    return f;
+}
+
+__device__ __forceinline__ float lo_of(uint32_t u) { return __builtin_bit_cast(float, u << 16); }
+__device__ __forceinline__ float hi_of(uint32_t u) { return __builtin_bit_cast(float, u & 0xffff0000u); }
+
+template <bool INTERLEAVED>
+__global__ __launch_bounds__(kThreads) void rotary_kernel(const Args a)
+{
+    __shared__ double freq[kMaxPairs];
+    __shared__ int pos[kMaxRows];
+    __shared__ float2 turn[kMaxRows * kMaxPairs];   // cos, sin
+    const int which = (int)blockIdx.x >= a.t[0].blocks;
+    const Tensor &t = a.t[which];
+    const int row0 = ((int)blockIdx.x - (which ? a.t[0].blocks : 0)) * t.rows_per_block;
+    const int rows = min(t.rows_per_block, t.rows - row0);
+    const int pairs = a.rotary_dim / 2;
+    const int tid = threadIdx.x;
+
+    if (tid < pairs) freq[tid] = turns_of(a, tid);
+    if (tid >= kThreads - kMaxRows && tid - (kThreads - kMaxRows) < rows) {   // (other wavefronts than those of the frequencies)
+        const int r = tid - (kThreads - kMaxRows), row = row0 + r;
+        int lo = 0, hi = a.NS;   // the last segment that begins at or before the row
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (t.cu[mid] <= row) lo = mid;
+            else hi = mid;
+        }
+        pos[r] = row - t.cu[lo] + (t.begin ? t.begin[lo] : 0);
+    }
+    __syncthreads();
+    for (int i = tid; i < rows * pairs; i += kThreads) {
+        const int r = i / pairs, p = i - r * pairs;
+        const double turns = (double)pos[r] * freq[p];
+        float s, c;
+        sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
+        turn[i] = make_float2(c * a.amplitude, s * a.amplitude * a.sign);
+    }
+    __syncthreads();
+
+    // A unit is what a lane moves at a time.  Half layout: 8 pairs (two pieces of 16 bytes), then the pieces behind rotary_dim;
+    // interleaved: a piece of 16 bytes, 4 pairs.
+    const int turned = INTERLEAVED ? a.rotary_dim / 8 : a.rotary_dim / 16;
+    const int units = turned + (a.copies >> which & 1 ? (a.head_dim - a.rotary_dim) / 8 : 0);
+    const int row_units = units * t.heads;
+    for (int i = tid; i < rows * row_units; i += kThreads) {
+        const int r = quotient40(i, t.inv_row), x = i - r * row_units;
+        const int head = units == turned ? x / turned : x / units, u = x - head * units;
+        const uint16_t *in = t.in + (int64_t)(row0 + r) * t.in_stride + (int64_t)head * a.head_dim;
+        uint16_t *out = t.out + (int64_t)(row0 + r) * t.out_stride + (int64_t)head * a.head_dim;
+        if (u >= turned) {
+            const int e = a.rotary_dim + (u - turned) * 8;
+            *(uint4 *)(out + e) = *(const uint4 *)(in + e);
+        } else if (INTERLEAVED) {
+            const uint4 v = *(const uint4 *)(in + u * 8);
+            const float2 *cs = turn + r * pairs + u * 4;
+            uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float x0 = lo_of(w[j]), x1 = hi_of(w[j]), c = cs[j].x, s = cs[j].y;
+                w[j] = pack_bf16(x0 * c - x1 * s, x0 * s + x1 * c);
+            }
+            *(uint4 *)(out + u * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+            const int e0 = u * 8, e1 = e0 + pairs;
+            const uint4 v0 = *(const uint4 *)(in + e0), v1 = *(const uint4 *)(in + e1);
+            const float2 *cs = turn + r * pairs + e0;
+            uint32_t a0[4] = {v0.x, v0.y, v0.z, v0.w}, a1[4] = {v1.x, v1.y, v1.z, v1.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float p0 = lo_of(a0[j]), p1 = hi_of(a0[j]), q0 = lo_of(a1[j]), q1 = hi_of(a1[j]);
+                const float c0 = cs[2 * j].x, s0 = cs[2 * j].y, c1 = cs[2 * j + 1].x, s1 = cs[2 * j + 1].y;
+                a0[j] = pack_bf16(p0 * c0 - q0 * s0, p1 * c1 - q1 * s1);
+                a1[j] = pack_bf16(p0 * s0 + q0 * c0, p1 * s1 + q1 * c1);
+            }
+            *(uint4 *)(out + e0) = make_uint4(a0[0], a0[1], a0[2], a0[3]);
+            *(uint4 *)(out + e1) = make_uint4(a1[0], a1[1], a1[2], a1[3]);
+        }
+    }
+}
+
+uint64_t inverse40(int d) { return ((1ull << 40) + (uint64_t)d - 1) / (uint64_t)d; }
+
+}  // namespace
+
+extern "C" {
+
+int skrull_rotary_check(const skrull_rotary_t *r)
+{
+    if (!r) return refuse("rotary: null pointer");
+    if (r->head_dim != 64 && r->head_dim != 128) return refuse("rotary: head_dim %d is not 64 or 128", r->head_dim);
+    if (r->rotary_dim < 16 || r->rotary_dim > r->head_dim || r->rotary_dim % 16 != 0)
+        return refuse("rotary: rotary_dim %d is not a multiple of 16 from 16 to head_dim", r->rotary_dim);
+    if (r->layout != SKRULL_ROTARY_HALF && r->layout != SKRULL_ROTARY_INTERLEAVED) return refuse("rotary: unknown layout %d", r->layout);
+    if (r->scaling < SKRULL_ROTARY_PLAIN || r->scaling > SKRULL_ROTARY_PARTS) return refuse("rotary: unknown scaling %d", r->scaling);
+    if (!isfinite(r->base) || !(r->base > 1.0)) return refuse("rotary: base must be finite and above 1");
+    if (!isfinite(r->factor) || !(r->factor >= 1.0)) return refuse("rotary: factor must be finite and at least 1");
+    if (r->scaling == SKRULL_ROTARY_PLAIN && r->factor != 1.0) return refuse("rotary: a factor needs a scaling");
+    if (!isfinite(r->amplitude) || !(r->amplitude > 0.0)) return refuse("rotary: amplitude must be finite and positive");
+    if (r->scaling == SKRULL_ROTARY_PARTS) {
+        if (!isfinite(r->original_length) || !(r->original_length > 0.0)) return refuse("rotary: original_length must be finite and positive");
+        if (!isfinite(r->low_turns) || !isfinite(r->high_turns) || !(r->low_turns >= 0.0) || !(r->low_turns < r->high_turns))
+            return refuse("rotary: low_turns and high_turns must be finite, 0 <= low_turns < high_turns");
+    }
+    return SKRULL_OK;
+}
+
+int skrull_rotary(const skrull_attn_plan_t *plan, const skrull_rotary_t *r, const skrull_rotary_tensor_t *first,
+                  const skrull_rotary_tensor_t *second, int inverse, void *hip_stream)
+{
+    if (!plan || !first) return refuse("rotary: null pointer");
+    if (int rc = skrull_rotary_check(r)) return rc;
+    if (r->head_dim != plan->d) return refuse("rotary: head_dim %d, the plan's is %d", r->head_dim, plan->d);
+    Args a = {};
+    a.NS = plan->NS;
+    a.head_dim = r->head_dim;
+    a.rotary_dim = r->rotary_dim;
+    a.scaling = r->scaling;
+    a.log2_base = log2(r->base);
+    if (r->scaling == SKRULL_ROTARY_NTK && r->rotary_dim > 2)
+        a.log2_base += log2(r->factor) * (double)r->rotary_dim / (double)(r->rotary_dim - 2);
+    a.factor = r->factor;
+    a.turns_scale = r->original_length;
+    a.low_turns = r->low_turns;
+    a.high_turns = r->high_turns;
+    a.amplitude = (float)r->amplitude;
+    a.sign = inverse ? -1.0f : 1.0f;
+    const skrull_rotary_tensor_t *given[2] = {first, second};
+    int64_t blocks = 0;
+    for (int i = 0; i < 2; ++i) {
+        const skrull_rotary_tensor_t *g = given[i];
+        if (!g) continue;
+        Tensor &t = a.t[i];
+        if (!g->in || !g->out || !aligned_to(g->in, 16) || !aligned_to(g->out, 16)) return refuse("rotary: tensor %d is null or not 16-byte aligned", i);
+        if (g->heads < 1 || g->heads > 4096) return refuse("rotary: tensor %d has %d heads", i, g->heads);
+        if (g->rows != SKRULL_ROWS_Q && g->rows != SKRULL_ROWS_K) return refuse("rotary: tensor %d is of unknown rows %d", i, g->rows);
+        const int64_t width = (int64_t)g->heads * r->head_dim;
+        if (g->in_stride < width || g->out_stride < width || g->in_stride % 8 != 0 || g->out_stride % 8 != 0)
+            return refuse("rotary: strides of tensor %d must be multiples of 8 and at least heads * head_dim", i);
+        t.rows = g->rows == SKRULL_ROWS_Q ? plan->total_q : plan->total_k;
+        const int64_t in_bytes = ((t.rows - 1) * g->in_stride + width) * 2, out_bytes = ((t.rows - 1) * g->out_stride + width) * 2;
+        const bool in_place = g->in == g->out && g->in_stride == g->out_stride;
+        if (!in_place && overlap(g->in, in_bytes, g->out, out_bytes)) return refuse("rotary: out of tensor %d overlaps its in", i);
+        if (!in_place) a.copies |= 1 << i;
+        t.in = (const uint16_t *)g->in;
+        t.out = (uint16_t *)g->out;
+        t.in_stride = g->in_stride;
+        t.out_stride = g->out_stride;
+        t.cu = g->rows == SKRULL_ROWS_Q ? plan->cu_q : plan->cu_k;
+        t.begin = g->rows == SKRULL_ROWS_Q ? plan->q_begin : nullptr;
+        t.heads = g->heads;
+        t.rows_per_block = (int32_t)(width >= 8192 ? 4 : width >= 4096 ? 8 : width >= 2048 ? 16 : 32);
+        t.blocks = (t.rows + t.rows_per_block - 1) / t.rows_per_block;
+        const int turned = r->rotary_dim / (r->layout == SKRULL_ROTARY_INTERLEAVED ? 8 : 16);
+        t.inv_row = inverse40(g->heads * (turned + (in_place ? 0 : (r->head_dim - r->rotary_dim) / 8)));
+        blocks += t.blocks;
+    }
+    if (int rc = plan_on_current_device(plan)) return rc;
+    if (blocks > INT32_MAX) return refuse("rotary: too many rows");
+    if (r->layout == SKRULL_ROTARY_INTERLEAVED) rotary_kernel<true><<<(int)blocks, kThreads, 0, (hipStream_t)hip_stream>>>(a);
+    else rotary_kernel<false><<<(int)blocks, kThreads, 0, (hipStream_t)hip_stream>>>(a);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? SKRULL_OK : launch_failed(e, "rotary launch");
+}
+
+}  // extern "C"

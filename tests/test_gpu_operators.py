@@ -1,0 +1,591 @@
+"""Rotary positions, norm and loss on the GPU against plain implementations in 64 bits.
+
+Tolerances are bounds, not observations: a rounding to bf16 is off by at most 2^-8 of the value, one of fp32 by 2^-24, and a sum of n
+fp32 terms by at most n 2^-24 of the sum of their magnitudes; TINY covers results below bf16's normal numbers."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+
+pytestmark = pytest.mark.gpu
+
+BF16, FP32, TINY = 2.0 ** -8, 2.0 ** -24, 1e-30
+
+
+def _randn(gen, *shape, dtype=torch.bfloat16, scale=1.0):
+    return (torch.randn(shape, generator=gen, device="cuda") * scale).to(dtype)
+
+
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _within(got, want, tolerance, what):
+    assert got.shape == want.shape, what
+    assert torch.isfinite(got).all(), what
+    excess = ((got.double() - want).abs() - tolerance).max().item() if want.numel() else 0.0
+    assert excess <= 0.0, (what, excess, (got.double() - want).abs().max().item())
+
+
+def _padded(t, pad=24, fill=float("nan")):
+    """The rows of `t` inside wider ones: (the wider tensor, a view that equals t)."""
+    wide = torch.full((t.shape[0], t[0].numel() + pad), fill, dtype=t.dtype, device=t.device)
+    view = wide[:, :t[0].numel()].unflatten(1, t.shape[1:]) if t.dim() == 3 else wide[:, :t.shape[1]]
+    view.copy_(t)
+    return wide, view
+
+
+# ---- rotary ---------------------------------------------------------------------------------------------------------
+
+def _positions(seq_len, degree, index, cut):
+    q, k = [], []
+    for s, n, r, z in zip(seq_len, degree, index, cut):
+        chunks, end = n * (1 + z), 0
+        for i in ([r, 2 * n - 1 - r] if z else [r]):
+            begin, end = i * s // chunks, (i + 1) * s // chunks
+            q += range(begin, end)
+        k += range(end)
+    return np.asarray(q), np.asarray(k)
+
+
+def _frequencies(r, base, scaling="plain", factor=1.0, original=0.0, low=0.0, high=0.0):
+    if scaling == "ntk":
+        base = base * factor ** (r / (r - 2))
+    f = base ** (-np.arange(0, r, 2) / r)
+    if scaling == "linear":
+        f = f / factor
+    if scaling == "parts":
+        g = np.clip((original * f / (2 * math.pi) - low) / (high - low), 0, 1)
+        f = f * (g + (1 - g) / factor)
+    return f
+
+
+def _turned(x, pos, f, interleaved, amplitude=1.0, inverse=False):
+    x = x.double()
+    y = x.clone(memory_format=torch.contiguous_format)
+    size = x.abs()
+    n = len(f)
+    t = torch.from_numpy(pos[:, None] * f[None, :]).cuda()[:, None]
+    a = torch.arange(n, device="cuda") * (2 if interleaved else 1)
+    b = a + (1 if interleaved else n)
+    c, s = amplitude * t.cos(), amplitude * t.sin() * (-1 if inverse else 1)
+    y[..., a], y[..., b] = x[..., a] * c - x[..., b] * s, x[..., a] * s + x[..., b] * c
+    size = size.clone()
+    size[..., a] = size[..., b] = amplitude * (x[..., a].abs() + x[..., b].abs())
+    return y, size
+
+
+SHAPES = [   # lengths, degrees, indices, cuts
+    ([1], [1], [0], [0]),
+    ([37, 128, 256, 511], [1] * 4, [0] * 4, [0] * 4),
+    ([1] * 70 + [33], [1] * 71, [0] * 71, [0] * 71),
+    ([700, 129, 2100, 64, 1000], [1, 1, 3, 1, 4], [0, 0, 1, 0, 3], [0, 0, 0, 0, 1]),
+    ([131072, 5, 40], [8, 1, 1], [7, 0, 0], [1, 0, 0]),
+]
+
+
+def _plan(shape, heads, d):
+    from paper_2505_19609_amd import binding as B
+    return B.skrull_attn_plan(*shape[:3], heads[0], heads[1], d, d ** -0.5, shard_cut=shape[3])
+
+
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+@pytest.mark.parametrize("heads,d,rotary_dim", [((4, 4), 64, 64), ((14, 2), 64, 32), ((32, 8), 128, 128), ((3, 1), 128, 48), ((1, 1), 64, 16)])
+@pytest.mark.parametrize("interleaved", [0, 1])
+def test_rotary_both_ways(shape, heads, d, rotary_dim, interleaved):
+    from paper_2505_19609_amd import binding as B
+    if heads == (32, 8) and shape == 4 and interleaved:
+        heads = (8, 2)   # (the same rows with fewer heads)
+    plan, (pq, pk) = _plan(SHAPES[shape], heads, d), _positions(*SHAPES[shape])
+    assert (len(pq), len(pk)) == (plan.total_q, plan.total_k)
+    gen = _gen(shape)
+    q, k = _randn(gen, len(pq), heads[0], d), _randn(gen, len(pk), heads[1], d)
+    rotary = B.skrull_rotary_init(d, rotary_dim, interleaved, 5e5)
+    f = _frequencies(rotary_dim, 5e5)
+    for inverse in (False, True):
+        q_out, k_out = torch.full_like(q, float("nan")), torch.full_like(k, float("nan"))
+        B.skrull_rotary(plan, rotary, q, k, q_out, k_out, inverse=inverse)
+        for name, x, out, pos in (("q", q, q_out, pq), ("k", k, k_out, pk)):
+            want, size = _turned(x, pos, f, interleaved, inverse=inverse)
+            # (angle: turns in 64 bits, rounded to fp32 once; sine, cosine and two products a few fp32 roundings more)
+            _within(out, want, BF16 * want.abs() + 16 * FP32 * size + TINY, (name, inverse))
+            assert torch.equal(out[..., rotary_dim:], x[..., rotary_dim:])
+    plan.destroy()
+
+
+@pytest.mark.parametrize("kw", [dict(scaling="linear", factor=4.0), dict(scaling="ntk", factor=8.0), dict(scaling="parts", factor=8.0, original=8192, low=1.0, high=4.0),
+                                dict(scaling="parts", factor=32.0, original=4096, low=1.0, high=32.0), dict(scaling="parts", factor=1.0, original=100, low=0.0, high=1.0)])
+def test_rotary_scaled(kw):
+    from paper_2505_19609_amd import binding as B
+    plan, (pq, pk) = _plan(SHAPES[4], (2, 1), 128), _positions(*SHAPES[4])
+    gen = _gen(5)
+    q, k = _randn(gen, len(pq), 2, 128), _randn(gen, len(pk), 1, 128)
+    kinds = {"linear": B.ROTARY_LINEAR, "ntk": B.ROTARY_NTK, "parts": B.ROTARY_PARTS}
+    rotary = B.skrull_rotary_init(128, 128, B.ROTARY_HALF, 1e4, kinds[kw["scaling"]], kw["factor"], kw.get("original", 0), kw.get("low", 0),
+                                  kw.get("high", 0), amplitude=1.2079)
+    q_out, k_out = torch.empty_like(q), torch.empty_like(k)
+    B.skrull_rotary(plan, rotary, q, k, q_out, k_out)
+    f = _frequencies(128, 1e4, **kw)
+    for x, out, pos in ((q, q_out, pq), (k, k_out, pk)):
+        want, size = _turned(x, pos, f, False, amplitude=1.2079)
+        _within(out, want, BF16 * want.abs() + 16 * FP32 * size + TINY, kw)
+    plan.destroy()
+
+
+def test_rotary_strides_in_place_own_rows_and_single_tensors():
+    """Parts of a projection's rows, turned into other memory and in place: the same bits as contiguous tensors, and nothing
+    between them is touched; K of this rank's own tokens has the positions of Q; a tensor alone is the same as beside another."""
+    from paper_2505_19609_amd import binding as B
+    hq, hkv, d = 6, 2, 64
+    shape = SHAPES[3]
+    plan, rotary = _plan(shape, (hq, hkv), d), B.skrull_rotary_init(d, 32, B.ROTARY_HALF)
+    gen = _gen(9)
+    rows = _randn(gen, plan.total_q, (hq + 2 * hkv) * d + 8)
+    q, k = rows[:, :hq * d].unflatten(1, (hq, d)), rows[:, hq * d:(hq + hkv) * d].unflatten(1, (hkv, d))
+    want_q, want_k = torch.empty(q.shape, dtype=q.dtype, device="cuda"), torch.empty(k.shape, dtype=k.dtype, device="cuda")
+    B.skrull_rotary(plan, rotary, q.contiguous(), k.contiguous(), want_q, want_k, k_rows=B.ROWS_Q)
+    pq, _ = _positions(*shape)
+    w, size = _turned(k, pq, _frequencies(32, 1e4), False)
+    _within(want_k, w, BF16 * w.abs() + 16 * FP32 * size + TINY, "own rows")
+    q_out, k_out = torch.empty_like(want_q), torch.empty_like(want_k)
+    B.skrull_rotary(plan, rotary, q, None, q_out, None)
+    B.skrull_rotary(plan, rotary, None, k, None, k_out, k_rows=B.ROWS_Q)
+    assert torch.equal(q_out, want_q) and torch.equal(k_out, want_k)
+    before = rows.clone()
+    B.skrull_rotary(plan, rotary, q, k, q, k, k_rows=B.ROWS_Q)
+    assert torch.equal(q, want_q) and torch.equal(k, want_k)
+    assert torch.equal(rows[:, (hq + hkv) * d:], before[:, (hq + hkv) * d:])
+    other = torch.full_like(rows, 7.0)
+    B.skrull_rotary(plan, rotary, q_out, None, other[:, 64:64 + hq * d].unflatten(1, (hq, d)), None, inverse=True)
+    assert (other[:, :64] == 7).all() and (other[:, 64 + hq * d:] == 7).all()
+    for bad in (rows[:, 4:4 + hq * d].unflatten(1, (hq, d)),):     # (8 bytes off)
+        with pytest.raises(B.SkrullError, match="aligned"):
+            B.skrull_rotary(plan, rotary, bad, None, q_out, None)
+    with pytest.raises(B.SkrullError, match="overlaps"):
+        B.skrull_rotary(plan, rotary, q, None, rows[:, 8:8 + hq * d].unflatten(1, (hq, d)), None)
+    with pytest.raises(B.SkrullError, match="head_dim"):
+        B.skrull_rotary(plan, B.skrull_rotary_init(128), q, None, q_out, None)
+    plan.destroy()
+
+
+def test_rotary_gradient():
+    from paper_2505_19609_amd import binding as B
+    from paper_2505_19609_amd.autograd import skrull_rotary
+    hq, hkv, d = 4, 2, 64
+    plan, rotary = _plan(SHAPES[1], (hq, hkv), d), B.skrull_rotary_init(d, 64, B.ROTARY_INTERLEAVED, amplitude=1.5)
+    gen = _gen(3)
+    rows = _randn(gen, plan.total_q, (hq + 2 * hkv) * d).requires_grad_()
+    q, k, v = rows.split([hq * d, hkv * d, hkv * d], 1)
+    q2, k2 = skrull_rotary(q.unflatten(1, (hq, d)), k.unflatten(1, (hkv, d)), plan, rotary)
+    assert q2.is_contiguous() and k2.is_contiguous()
+    dq, dk = _randn(gen, *q2.shape), _randn(gen, hkv, plan.total_k, d).transpose(0, 1)   # (another layout of dK)
+    (got,) = torch.autograd.grad((q2, k2), rows, (dq, dk))
+    pos, _ = _positions(*SHAPES[1])
+    f = _frequencies(64, 1e4)
+    for g, x in ((got[:, :hq * d], dq), (got[:, hq * d:(hq + hkv) * d], dk)):
+        want, size = _turned(x, pos, f, True, amplitude=1.5, inverse=True)
+        _within(g, want.flatten(1), (BF16 * want.abs() + 16 * FP32 * size + TINY).flatten(1), "gradient")
+    assert (got[:, (hq + hkv) * d:] == 0).all()
+    plan.destroy()
+
+
+# ---- norm -----------------------------------------------------------------------------------------------------------
+
+def _norm_in_64_bits(x, w, b, dy, eps, layer):
+    x, w, dy = x.double(), w.double(), dy.double()
+    n = x.shape[1]
+    mean = x.mean(1, keepdim=True) if layer else torch.zeros_like(x[:, :1])
+    rstd = 1 / ((x - mean).square().mean(1, keepdim=True) + eps).sqrt()
+    h = (x - mean) * rstd
+    g = dy * w
+    dx = rstd * (g - h * (g * h).mean(1, keepdim=True) - (g.mean(1, keepdim=True) if layer else 0.0))
+    y = h * w + (b.double() if b is not None else 0.0)
+    # n_sum: fp32 roundings of a sum over a row: 16 in a lane, 6 across a wavefront, 16 across wavefronts, and a few of the formula
+    n_sum = 64 * FP32
+    eh = n_sum * (h.abs() + x.abs().mean(1, keepdim=True) * rstd)             # of h
+    ey = w.abs() * eh + 4 * FP32 * y.abs() + FP32 * (b.double().abs() if b is not None else 0.0)
+    mgh = (g * h).abs().mean(1, keepdim=True)
+    eg = (g.abs() * eh).mean(1, keepdim=True) + n_sum * mgh                      # of mean(g h)
+    edx = rstd * (n_sum * (g.abs() + h.abs() * mgh + g.abs().mean(1, keepdim=True)) + eh * mgh + h.abs() * eg)
+    rows = x.shape[0]
+    sums = (rows + 64) * FP32
+    edw = (dy.abs() * eh).sum(0) + sums * (dy * h).abs().sum(0)
+    edb = sums * dy.abs().sum(0)
+    return {"y": (y, ey), "dx": (dx, edx), "dw": ((dy * h).sum(0), edw), "db": (dy.sum(0), edb)}
+
+
+NORM_SHAPES = [(1, 1), (1, 64), (3, 7), (5, 896), (64, 512), (33, 513), (2, 1024), (130, 1025), (9, 2048), (700, 3584), (17, 4096), (6, 4097), (3, 8192), (2050, 104)]
+
+
+@pytest.mark.parametrize("rows,cols", NORM_SHAPES)
+@pytest.mark.parametrize("kind,bias", [("rms", False), ("layer", True), ("layer", False)])
+@pytest.mark.parametrize("t,wt", [(torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32), (torch.float32, torch.float32), (torch.float32, torch.bfloat16)])
+def test_norm(rows, cols, kind, bias, t, wt):
+    from paper_2505_19609_amd.autograd import skrull_norm
+    gen = _gen(rows * 10007 + cols)
+    x = (_randn(gen, rows, cols, dtype=torch.float32) * _randn(gen, rows, 1, dtype=torch.float32).exp() + 3.0).to(t).requires_grad_()
+    w = (_randn(gen, cols, dtype=torch.float32, scale=0.3) + 1.0).to(wt).requires_grad_()
+    b = _randn(gen, cols, dtype=wt).requires_grad_() if bias else None
+    dy = _randn(gen, rows, cols, dtype=t)
+    eps = 1e-3
+    y = skrull_norm(x, w, b, eps, kind)
+    assert y.dtype == t
+    wanted = [v for v in (x, w, b) if v is not None]
+    got = dict(zip(("dx", "dw", "db"), torch.autograd.grad(y, wanted, dy)), y=y.detach())
+    want = _norm_in_64_bits(x.detach(), w.detach(), None if b is None else b.detach(), dy, eps, kind == "layer")
+    for name, value in got.items():
+        exact, error = want[name]
+        out = value.dtype
+        _within(value, exact, error * 1.01 + (BF16 if out == torch.bfloat16 else FP32) * (exact.abs() + error) + TINY, name)
+
+
+@pytest.mark.parametrize("cols,pad", [(896, 8), (896, 3), (4096, 24), (1001, 7)])
+def test_norm_strides_and_in_place(cols, pad):
+    """Rows inside wider ones, aligned and not: what contiguous rows give, up to the same bits, and nothing beside them is
+    touched; y in the place of x and dx in the place of dy are the same bits too."""
+    from paper_2505_19609_amd import binding as B
+    gen, rows = _gen(cols + pad), 37
+    x, dy, w, b = _randn(gen, rows, cols), _randn(gen, rows, cols), _randn(gen, cols), _randn(gen, cols)
+
+    def both(x, dy, y, dx):
+        mean, rstd = torch.empty((2, rows), device="cuda")
+        dw, db = torch.empty_like(w), torch.empty_like(b)
+        B.skrull_norm_fwd(x, w, b, y, mean, rstd, 1e-5, B.NORM_LAYER)
+        kept = y.clone()
+        ws = torch.full((B.skrull_norm_workspace(x, w, B.NORM_LAYER),), 0xFF, dtype=torch.uint8, device="cuda")
+        B.skrull_norm_bwd(x if y is not x else x0, w, mean, rstd, dy, dx, dw, db, ws, B.NORM_LAYER)
+        return kept, dx, dw, db
+
+    x0 = x.clone()
+    want = [t.clone() for t in both(x, dy, torch.empty_like(x), torch.empty_like(x))]
+    wides, views = zip(*(_padded(t, pad, 5.0) for t in (x, dy, x, x)))
+    got = both(*views)
+    assert all(torch.equal(a, c) for a, c in zip(got, want))
+    assert all((t[:, cols:] == 5).all() for t in wides)
+    got = both(x, dy, x, dy)
+    assert all(torch.equal(a, c) for a, c in zip(got, want))
+
+
+def test_norm_without_rows_and_with_a_row_of_infinities():
+    from paper_2505_19609_amd.autograd import skrull_norm
+    w, b = (torch.ones(96, device="cuda", requires_grad=True) for _ in range(2))
+    x = torch.empty(0, 96, device="cuda", requires_grad=True)
+    y = skrull_norm(x, w, b)
+    dx, dw, db = torch.autograd.grad(y, (x, w, b), torch.empty(0, 96, device="cuda"))
+    assert y.shape == (0, 96) and dx.shape == (0, 96) and (dw == 0).all() and (db == 0).all()
+    x = torch.ones(5, 96, device="cuda")
+    x[2, 3] = math.inf
+    x[3] = 0.0
+    y = skrull_norm(x, w, None, 0.25, "rms")
+    assert torch.isnan(y[2, 3]) and torch.isfinite(y[[0, 1, 3, 4]]).all() and (y[3] == 0).all()   # (a row's own trouble stays its own)
+    assert torch.equal(y[0], y[4])
+
+
+def test_norm_backward_for_some_of_its_inputs():
+    from paper_2505_19609_amd.autograd import skrull_norm
+    gen = _gen(77)
+    x, w, b, dy = _randn(gen, 40, 640), _randn(gen, 640), _randn(gen, 640), _randn(gen, 40, 640)
+    want = None
+    for need in ((1, 1, 1), (1, 0, 0), (0, 1, 0), (0, 0, 1), (1, 0, 1)):
+        given = [t.clone().requires_grad_(bool(n)) for t, n in zip((x, w, b), need)]
+        grads = torch.autograd.grad(skrull_norm(*given), [t for t in given if t.requires_grad], dy)
+        want = want or grads
+        assert all(torch.equal(g, want[i]) for g, i in zip(grads, [i for i in range(3) if need[i]]))
+
+
+# ---- loss -----------------------------------------------------------------------------------------------------------
+
+def _loss_in_64_bits(x, w, target, d):
+    """loss, lse, dx, dw and their tolerances, over the rows that have a target."""
+    has = target >= 0
+    idx = torch.nonzero(has)[:, 0]
+    xs, wd, ds = x[idx].double(), w.double(), d[idx].double()[:, None]
+    H, V = w.shape[1], w.shape[0]
+    z = xs @ wd.t()
+    zs = xs.abs() @ wd.abs().t()
+    lse = torch.logsumexp(z, 1) if len(idx) else z.sum(1)
+    n = torch.arange(len(idx), device="cuda")
+    tz = z[n, target[idx]]
+    ez = (H + 8) * FP32 * zs + 4 * FP32 * z.abs()                    # of a logit, through its product with log2 e
+    p = (z - lse[:, None]).exp()
+    elog = (p * ez).sum(1) + (V / 128 + 256) * FP32 + 8 * FP32 * lse.abs()   # of lse: its logits', the sums', its own
+    one = torch.zeros_like(p)
+    one[n, target[idx]] = 1.0
+    dz = ds * (p - one)
+    edz = ds.abs() * (p * (ez + elog[:, None] + 16 * FP32) * 1.1 + 4 * FP32 * (p + one))
+    edz = edz + BF16 * (dz.abs() + edz)                                # rounded to bf16 for the products
+    T = len(idx)
+    out = {}
+    for name, value, error, shape in (("loss", lse - tz, elog + ez[n, target[idx]] + FP32 * (lse.abs() + tz.abs()), (x.shape[0],)),
+                                      ("lse", lse, elog, (x.shape[0],)),
+                                      ("dx", dz @ wd, edz @ wd.abs() + (V + 64) * FP32 * (dz.abs() @ wd.abs()), x.shape)):
+        full, e = (torch.zeros(shape, dtype=torch.float64, device="cuda") for _ in range(2))
+        full[idx], e[idx] = value, error
+        out[name] = (full, e)
+    out["dw"] = (dz.t() @ xs, edz.t() @ xs.abs() + (T + 64) * FP32 * (dz.abs().t() @ xs.abs()))
+    return out
+
+
+def _loss_case(rows, hidden, vocab, ignored, seed=0):
+    gen = _gen(rows * 31 + hidden * 7 + vocab + seed)
+    x, w = _randn(gen, rows, hidden), _randn(gen, vocab, hidden, scale=1.5 * hidden ** -0.5)
+    target = torch.randint(0, vocab, (rows,), generator=gen, device="cuda")
+    target[torch.rand(rows, generator=gen, device="cuda") < ignored] = -100
+    d = _randn(gen, rows, dtype=torch.float32)
+    return x, w, target, d
+
+
+def _check_loss(x, w, target, d, want=None):
+    from paper_2505_19609_amd.autograd import skrull_cross_entropy
+    x, w = x.detach().requires_grad_(), w.detach().requires_grad_()
+    loss = skrull_cross_entropy(x, w, target)
+    dx, dw = torch.autograd.grad(loss, (x, w), d)
+    want = want or _loss_in_64_bits(x.detach(), w.detach(), target, d)
+    for name, got in (("loss", loss.detach()), ("dx", dx), ("dw", dw)):
+        exact, error = want[name]
+        _within(got, exact, error + (BF16 if got.dtype == torch.bfloat16 else FP32) * (exact.abs() + error) + TINY, name)
+    return loss.detach(), dx, dw
+
+
+@pytest.mark.parametrize("rows,hidden,vocab", [(1, 8, 1), (1, 64, 257), (2, 128, 128), (37, 64, 300), (255, 72, 1000), (256, 896, 513), (257, 136, 2049), (300, 896, 1000),
+                                               (1000, 1032, 777), (64, 3584, 4099), (2100, 200, 4000)])
+@pytest.mark.parametrize("ignored", [0.0, 0.4])
+def test_loss(rows, hidden, vocab, ignored):
+    _check_loss(*_loss_case(rows, hidden, vocab, ignored))
+
+
+def test_loss_of_many_row_blocks_and_target_patterns():
+    """More rows than one pass of the row list (8,192), rows with a target in runs and one by one."""
+    x, w, target, d = _loss_case(20011, 64, 96, 0.0)
+    target[:8200] = -1
+    target[9000:17000:2] = -5
+    target[20000:] = -100
+    loss, dx, _ = _check_loss(x, w, target, d)
+    assert (loss[target < 0] == 0).all() and (dx[target < 0] == 0).all()
+
+
+def test_loss_in_pieces_of_the_vocabulary():
+    """dz of 8,192 rows and 140,000 words is 2.3 GB: two pieces, the second one ragged."""
+    from paper_2505_19609_amd import binding as B
+    x, w, target, d = _loss_case(8192, 64, 140003, 0.0)
+    target[:7] = torch.tensor([0, 139999, 140002, 70143, 70144, 69999, 70000], device="cuda")
+    assert B.skrull_loss_workspace(x, w, True) < 3 << 30
+    # (64 bits a part of the rows at a time)
+    parts = [_loss_in_64_bits(x[i:i + 1024], w, target[i:i + 1024], d[i:i + 1024]) for i in range(0, 8192, 1024)]
+    want = {n: tuple(torch.cat([p[n][k] for p in parts]) for k in (0, 1)) for n in ("loss", "dx")}
+    want["dw"] = tuple(sum(p["dw"][k] for p in parts) for k in (0, 1))
+    want["dw"] = (want["dw"][0], want["dw"][1] + 8192 * FP32 * (d.double().abs()[:, None] * x.double().abs()).sum(0) / 1e3)
+    _check_loss(x, w, target, d, want)
+
+
+@pytest.mark.parametrize("pad", [8, 5])
+def test_loss_strides_and_repeated_calls(pad):
+    """Rows inside wider ones give the same bits, and so does every call."""
+    x, w, target, d = _loss_case(300, 328, 1100, 0.2)
+    want = _check_loss(x, w, target, d)
+    _, view = _padded(x, pad)
+    for given in (view, x, x.t().contiguous().t()):
+        assert all(torch.equal(a, b) for a, b in zip(_check_loss(given, w, target, d), want))
+
+
+def test_loss_of_rows_without_a_target():
+    """Whatever such rows hold stays out of the sums; with no other rows everything is zero."""
+    from paper_2505_19609_amd.autograd import skrull_cross_entropy
+    x, w, target, d = _loss_case(600, 128, 500, 0.5)
+    want = _check_loss(x, w, target, d)
+    for bad in (math.nan, math.inf):
+        y = x.clone()
+        y[target < 0] = bad
+        e = torch.where(target < 0, bad, d)
+        assert all(torch.equal(a, b) for a, b in zip(_check_loss(y, w, target, e, _loss_in_64_bits(x, w, target, d)), want))
+    x.requires_grad_(), w.requires_grad_()
+    loss = skrull_cross_entropy(x, w, torch.full_like(target, -1))
+    dx, dw = torch.autograd.grad(loss, (x, w), d)
+    assert (loss == 0).all() and (dx == 0).all() and (dw == 0).all()
+    empty = x.detach()[:0].requires_grad_()
+    loss = skrull_cross_entropy(empty, w, target[:0])
+    dx, dw = torch.autograd.grad(loss, (empty, w), d[:0])
+    assert loss.shape == (0,) and dx.shape == (0, 128) and (dw == 0).all()
+
+
+def test_loss_of_targets_outside_the_vocabulary_and_infinite_logits():
+    from paper_2505_19609_amd.autograd import skrull_cross_entropy
+    x, w, target, d = _loss_case(300, 64, 500, 0.0)
+    target[5] = 500
+    target[6] = 1 << 40
+    x.requires_grad_()
+    loss = skrull_cross_entropy(x, w, target)
+    (dx,) = torch.autograd.grad(loss, x, d)
+    bad = torch.zeros(300, dtype=torch.bool, device="cuda")
+    bad[5:7] = True
+    assert torch.isnan(loss[bad]).all() and torch.isnan(dx[bad]).all() and torch.isfinite(loss[~bad]).all() and torch.isfinite(dx[~bad]).all()
+    # a word of minus infinity has no probability, a word of plus infinity all of it
+    with torch.no_grad():
+        x = torch.zeros(3, 64, dtype=torch.bfloat16, device="cuda")
+        x[:, 0] = torch.tensor([1.0, 1.0, -1.0])
+        w = torch.zeros(300, 64, dtype=torch.bfloat16, device="cuda")
+        w[7, 0] = -math.inf
+        loss = skrull_cross_entropy(x, w, torch.tensor([7, 3, 3], device="cuda"))
+        assert loss[0] == math.inf and abs(loss[1].item() - math.log(299)) < 1e-5 and loss[2] == math.inf
+
+
+def test_loss_extremes_do_not_overflow():
+    """Logits of some thousands: the largest one is taken off before the exponential."""
+    x, w, target, d = _loss_case(64, 64, 300, 0.0)
+    _check_loss(x * 512, w * 8, target, d)
+
+
+def test_loss_gradients_one_at_a_time():
+    from paper_2505_19609_amd.autograd import skrull_cross_entropy
+    x, w, target, d = _loss_case(100, 64, 300, 0.1)
+    _, dx, dw = _check_loss(x, w, target, d)
+    y = x.clone().requires_grad_()
+    assert torch.equal(torch.autograd.grad(skrull_cross_entropy(y, w, target), y, d)[0], dx)
+    y = w.clone().requires_grad_()
+    assert torch.equal(torch.autograd.grad(skrull_cross_entropy(x, y, target), y, d.expand(100))[0], dw)
+    one = torch.ones((), device="cuda").expand(100)      # (a sum's gradient: one value, stride 0)
+    y = x.clone().requires_grad_()
+    skrull_cross_entropy(y, w, target).sum().backward()
+    z = x.clone().requires_grad_()
+    assert torch.equal(torch.autograd.grad(skrull_cross_entropy(z, w, target), z, one)[0], y.grad)
+
+
+def test_gradients_against_differences():
+    """The loss's change along its gradient, and the norm's, is what the gradient says (differences of the 64-bit forms)."""
+    x, w, target, d = _loss_case(50, 64, 200, 0.2)
+    _, dx, dw = _check_loss(x, w, target, d)
+    total = lambda x, w: (_loss_in_64_bits(x, w, target, d)["loss"][0] * d.double()).sum().item()
+    step = 1e-4
+    for got, f in ((dx, lambda s: total(x.double() + s * dx.double(), w.double())), (dw, lambda s: total(x.double(), w.double() + s * dw.double()))):
+        slope = (f(step) - f(-step)) / (2 * step)
+        # (bf16 gradients, dz in bf16: 2^-8 each of every element; a difference's own error is of the order step^2)
+        assert abs(slope - got.double().square().sum().item()) <= (2 * BF16 + 1e-3) * got.double().square().sum().item()
+
+
+# ---- streams, graphs, all of them together --------------------------------------------------------------------------
+
+def _training_path(plan, rotary, heads, d, params, x, target):
+    """norm -> projection -> rotary -> attention -> projection -> norm -> loss"""
+    from paper_2505_19609_amd.autograd import skrull_attention, skrull_cross_entropy, skrull_norm, skrull_rotary
+    (hq, hkv), (w1, wqkv, wo, w2, b2, vocab) = heads, params
+    rows = skrull_norm(x, w1, None, 1e-5, "rms") @ wqkv
+    q, k, v = rows.split([hq * d, hkv * d, hkv * d], 1)
+    q, k = skrull_rotary(q.unflatten(1, (hq, d)), k.unflatten(1, (hkv, d)), plan, rotary)
+    o = skrull_attention(q, k, v.unflatten(1, (hkv, d)).contiguous(), plan)
+    x = x + o.flatten(1) @ wo
+    return skrull_cross_entropy(skrull_norm(x, w2, b2), vocab, target)
+
+
+def _training_case(S=(37, 128, 1, 300), heads=(4, 2), d=64, hidden=264, vocab=700):
+    from paper_2505_19609_amd import binding as B
+    plan = B.skrull_attn_plan(list(S), [1] * len(S), [0] * len(S), heads[0], heads[1], d, d ** -0.5)
+    gen = _gen(123)
+    T = sum(S)
+    params = [1 + _randn(gen, hidden, scale=0.2), _randn(gen, hidden, (heads[0] + 2 * heads[1]) * d, scale=hidden ** -0.5),
+              _randn(gen, heads[0] * d, hidden, scale=(heads[0] * d) ** -0.5), 1 + _randn(gen, hidden, scale=0.2), _randn(gen, hidden, scale=0.1),
+              _randn(gen, vocab, hidden, scale=1.5 * hidden ** -0.5)]
+    x = _randn(gen, T, hidden)
+    target = torch.randint(0, vocab, (T,), generator=gen, device="cuda")
+    target[torch.tensor(np.cumsum(S) - 1, device="cuda")] = -1    # a sequence's last token has no next one
+    return plan, B.skrull_rotary_init(d, base=5e5), heads, d, params, x, target
+
+
+def test_training_path_against_64_bits():
+    plan, rotary, (hq, hkv), d, params, x, target = _training_case()
+    leaves = [t.requires_grad_() for t in [x] + params]
+    loss = _training_path(plan, rotary, (hq, hkv), d, leaves[1:], leaves[0], target)
+    weight = torch.rand(len(target), device="cuda")
+    grads = torch.autograd.grad((loss * weight).sum(), leaves)
+
+    plain = [t.detach().double().requires_grad_() for t in leaves]
+    X, (w1, wqkv, wo, w2, b2, vocab) = plain[0], plain[1:]
+    S = (37, 128, 1, 300)
+    pos, _ = _positions(S, [1] * 4, [0] * 4, [0] * 4)
+    f = _frequencies(d, 5e5)
+    ang = torch.from_numpy(pos[:, None] * f).cuda()[:, None]
+    turn = lambda t: torch.cat((t[..., :d // 2] * ang.cos() - t[..., d // 2:] * ang.sin(), t[..., :d // 2] * ang.sin() + t[..., d // 2:] * ang.cos()), -1)
+    rows = (X * (X.square().mean(1, keepdim=True) + 1e-5).rsqrt() * w1) @ wqkv
+    q, k, v = (t.unflatten(1, (-1, d)) for t in rows.split([hq * d, hkv * d, hkv * d], 1))
+    q, k = turn(q), turn(k)
+    seq = torch.repeat_interleave(torch.arange(4), torch.tensor(S)).cuda()
+    seen = (seq[:, None] == seq[None]) & (torch.arange(len(seq), device="cuda")[:, None] >= torch.arange(len(seq), device="cuda")[None])
+    o = []
+    for h in range(hq):
+        s = (q[:, h] @ k[:, h // (hq // hkv)].t() * d ** -0.5).masked_fill(~seen, -math.inf)
+        o.append(s.softmax(1) @ v[:, h // (hq // hkv)])
+    Y = X + torch.cat(o, 1) @ wo
+    Y = (Y - Y.mean(1, keepdim=True)) / (Y.var(1, unbiased=False, keepdim=True) + 1e-5).sqrt() * w2 + b2
+    want = torch.nn.functional.cross_entropy(Y @ vocab.t(), target.clamp(min=0), reduction="none") * (target >= 0)
+    wanted = torch.autograd.grad((want * weight).sum(), plain)
+    # About fifteen tensors are rounded to bf16 on the way there and back, each by 2^-8 of its values at most and by 2^-8 / sqrt(12) on average: their
+    # errors in 2-norm add to at most 15 * 2^-8 = 6 % of a gradient's.
+    assert ((loss.double() - want).norm() / want.norm()).item() <= 15 * BF16
+    for name, a, b in zip(("x", "w1", "wqkv", "wo", "w2", "b2", "vocab"), grads, wanted):
+        assert ((a.double() - b).norm() / b.norm()).item() <= 15 * BF16, name
+    plan.destroy()
+
+
+def test_calls_on_other_streams():
+    plan, rotary, heads, d, params, x, target = _training_case()
+    with torch.no_grad():
+        want = _training_path(plan, rotary, heads, d, params, x, target)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    for _ in range(3):
+        out = []
+        for st in streams:
+            st.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(st), torch.no_grad():
+                out.append(_training_path(plan, rotary, heads, d, params, x, target))
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, want) for o in out)
+    plan.destroy()
+
+
+def test_graph_replays_equal_eager():
+    """Forward and gradients of the three operators, captured with a workspace each: every replay is the eager result, on new
+    values and another pattern of targets too."""
+    from paper_2505_19609_amd import binding as B
+    heads, d, hidden, vocab = (4, 2), 64, 264, 700
+    plan, rotary, _, _, params, x, target = _training_case(hidden=hidden, vocab=vocab)
+    gen = _gen(55)
+    T = plan.total_q
+    q, k, w, weight, bias = _randn(gen, T, 4, d), _randn(gen, T, 2, d), params[5], params[3], params[4]
+    dy, dl = _randn(gen, T, hidden), torch.rand(T, generator=gen, device="cuda")
+    out = {"q": torch.empty_like(q), "k": torch.empty_like(k), "q2": torch.empty_like(q), "y": torch.empty_like(x), "dx": torch.empty_like(x),
+           "dw": torch.empty_like(weight), "db": torch.empty_like(weight), "loss": torch.empty(T, device="cuda"),
+           "lse": torch.empty(T, device="cuda"), "dh": torch.empty_like(x), "dv": torch.empty_like(w)}
+    mean, rstd = torch.empty((2, T), device="cuda")
+    ws = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in
+          (B.skrull_norm_workspace(x, weight), B.skrull_loss_workspace(x, w, False), B.skrull_loss_workspace(x, w, True))]
+
+    def step():
+        B.skrull_rotary(plan, rotary, q, k, out["q"], out["k"])
+        B.skrull_rotary(plan, rotary, out["q"], None, out["q2"], None, inverse=True)
+        B.skrull_norm_fwd(x, weight, bias, out["y"], mean, rstd)
+        B.skrull_norm_bwd(x, weight, mean, rstd, dy, out["dx"], out["dw"], out["db"], ws[0])
+        B.skrull_loss_fwd(out["y"], w, target, out["loss"], out["lse"], ws[1])
+        B.skrull_loss_bwd(out["y"], w, target, out["lse"], dl, out["dh"], out["dv"], ws[2])
+
+    side = torch.cuda.Stream()
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for rep in range(4):
+        if rep >= 2:
+            x.copy_(_randn(gen, *x.shape))
+            target.copy_(torch.where(torch.rand(T, generator=gen, device="cuda") < 0.3 * rep, -1, target.abs()))
+        step()
+        torch.cuda.synchronize()
+        eager = {n: t.clone() for n, t in out.items()}
+        for t in list(out.values()) + ws:
+            t.view(torch.uint8).fill_(0xFF if rep % 2 else 0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for n, t in out.items():
+            assert torch.equal(t, eager[n]), (rep, n)
+    plan.destroy()
