@@ -100,16 +100,20 @@ struct Operand {
                 read[t] = (8 * h + (s >> 2)) * 512 + ((4 * (4 * part + (t ^ (s >> 2))) + 2 * ((n >> 4) & 1) + ((s & 3) >> 1)) << 4) + 8 * (s & 1);
         }
     }
-    // 8 instructions of a wavefront fill a quarter of the tile.  `tail`: elements of the contraction that are left, where
-    // rows may end inside the step (ROWS): what is behind them reads as zero.
-    __device__ __forceinline__ void fetch(const Source &src, uint32_t lds, int wave, int lane, int tail, int q) const
+    // This lane's offsets of a step.  `tail`: elements of the contraction that are left, where rows may end inside the
+    // step (ROWS): what is behind them reads as zero.
+    __device__ __forceinline__ void offsets(int lane, int tail, int off[2]) const
     {
-        int off = load[q & 1];
-        if (!COLS && tail < kStep) {
-            const int piece = (lane & 7) ^ (4 * (q & 1) + (lane >> 4));
-            if (piece * 8 >= tail) off = (int)0x80000000;   // (past every descriptor's end)
+#pragma unroll
+        for (int o = 0; o < 2; ++o) {
+            off[o] = load[o];
+            if (!COLS && ((lane & 7) ^ (4 * o + (lane >> 4))) * 8 >= tail) off[o] = (int)0x80000000;   // (past every descriptor's end)
         }
-        dma_b128(src.words(), lds + (wave * 8 + q) * 1024, off, (int)(q * (COLS ? 2 : 8) * src.pitch));
+    }
+    // 8 instructions of a wavefront fill a quarter of the tile.
+    __device__ __forceinline__ static void fetch(i32x4 words, const int off[2], uint32_t pitch, uint32_t lds, int wave, int q)
+    {
+        dma_b128(words, lds + (wave * 8 + q) * 1024, off[q & 1], (int)(q * (COLS ? 2 : 8) * pitch));
     }
     // fragment b (32 rows or columns) of sixteenth-step k: 8 consecutive elements of the contraction
     __device__ __forceinline__ bf16x8 get(const unsigned char *t, int b, int k) const
@@ -209,14 +213,68 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
     B.init(lane, wave, wn, b_pitch);
     const uint32_t lds0 = lds_addr(lds);
 
-    const int die = blockIdx.x & 7, per_die = (work.total + 7) / 8;
-    const int end = min(work.total, (die + 1) * per_die);
-    for (int i = die * per_die + (blockIdx.x >> 3); i < end; i += gridDim.x >> 3) {
+    const int die = blockIdx.x & 7, per_die = (work.total + 7) / 8, stride = gridDim.x >> 3;
+    const int begin = die * per_die + (blockIdx.x >> 3), end = min(work.total, (die + 1) * per_die);
+
+    // The steps of this workgroup's tiles are one sequence, two of them in LDS at any time: the loads run ahead across the end of a tile.
+    Source sa = {}, sb = {};
+    int next_tile = begin, next_left = 0, next_tail = 0, parity = 0;   // of the loads
+    auto find = [&]() {
+        while (next_left == 0 && next_tile < end) {
+            int m, nn, s;
+            work.locate(next_tile, m, nn, s);
+            next_left = work.steps_of(p, s);
+            work.sources(p, m, nn, s, sa, sb);
+            next_tail = K == kForward || K == kAgain ? p.H : 0x7fffffff;   // elements of the contraction
+            next_tile += stride;
+        }
+    };
+    struct Fetch {
+        i32x4 a, b;
+        int a_off[2], b_off[2];
+        uint32_t lds;
+    };
+    auto take = [&]() {   // what the loads of the next step need; behind the last one they read nothing
+        Fetch f;
+        find();
+        if (next_left == 0) sa.left = sb.left = 0;
+        f.a = sa.words();
+        f.b = sb.words();
+        A.offsets(lane, next_tail, f.a_off);
+        B.offsets(lane, kStep, f.b_off);
+        f.lds = lds0 + parity * kBufferBytes;
+        sa.next();
+        sb.next();
+        next_tail -= kStep;
+        next_left -= next_left > 0;
+        parity ^= 1;
+        return f;
+    };
+    auto load = [&](const Fetch &f, int i) {   // the i-th of 16
+        if (i & 1) B.fetch(f.b, f.b_off, b_pitch, f.lds + kOperandBytes, wave, i >> 1);
+        else A.fetch(f.a, f.a_off, a_pitch, f.lds, wave, i >> 1);
+    };
+    bf16x8 fa[2][4], fb[2][4];   // fragments: of the sixteenth-step under way and of the next
+    auto read = [&](const unsigned char *t, int k, int to, int i) {   // the i-th of 8
+        if (i < 4) fb[to][i] = B.get(t + kOperandBytes, i, k);
+        else fa[to][i - 4] = A.get(t, i - 4, k);
+    };
+#pragma unroll
+    for (int step = 0; step < 2; ++step) {
+        const Fetch f = take();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) load(f, i);
+    }
+    asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) read(lds, 0, 0, i);
+    int at = 0;   // LDS offset of the step under way
+    for (int i = begin; i < end; i += stride) {
         int m, nn, s;
         work.locate(i, m, nn, s);
         const int steps = work.steps_of(p, s);
-        Source sa, sb;
-        work.sources(p, m, nn, s, sa, sb);
         f32x16 acc[4][4];
 #pragma unroll
         for (int x = 0; x < 4; ++x)
@@ -224,52 +282,36 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
             for (int y = 0; y < 4; ++y)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) acc[x][y][v] = 0.0f;
-        const int a_tail = K == kForward || K == kAgain ? p.H : 0x7fffffff;   // elements of the contraction
-
-        auto fetch = [&](int step, int q) {
-            const uint32_t to = lds0 + (step & 1) * kBufferBytes;
-            A.fetch(sa, to, wave, lane, a_tail - step * kStep, q);
-            B.fetch(sb, to + kOperandBytes, wave, lane, kStep, q);
-        };
-        __syncthreads();   // the tile before has been read
-        if (steps > 0) {
-#pragma unroll
-            for (int q = 0; q < 8; ++q) fetch(0, q);
-            sa.next();
-            sb.next();
-        }
-        if (steps > 1) {
-#pragma unroll
-            for (int q = 0; q < 8; ++q) fetch(1, q);
-            sa.next();
-            sb.next();
-        }
         for (int step = 0; step < steps; ++step) {
-            // 16 loads of the next step may be under way
-            if (step + 1 < steps) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
-            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            const unsigned char *t = lds + at;
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    SB();
+                    acc[j >> 2][j & 3] = mfma32(fa[k & 1][j >> 2], fb[k & 1][j & 3], acc[j >> 2][j & 3]);
+                    SB();
+                    if (j % 2 == 0) read(t, k + 1, (k + 1) & 1, j / 2);
+                }
+            }
+            SB();
+            // This step has been read to its last fragment, by every wavefront: the step after next may take its place.  The
+            // next one, whose loads were the last ones before, is there.
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            const unsigned char *ta = lds + (step & 1) * kBufferBytes, *tb = ta + kOperandBytes;
+            at ^= kBufferBytes;
+            t = lds + at;
+            const Fetch f = take();
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                bf16x8 a[4], b[4];
-#pragma unroll
-                for (int x = 0; x < 4; ++x) { a[x] = A.get(ta, x, k); b[x] = B.get(tb, x, k); }
-#pragma unroll
-                for (int x = 0; x < 4; ++x)
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) acc[x][y] = mfma32(a[x], b[y], acc[x][y]);
+            for (int j = 0; j < 16; ++j) {
+                SB();
+                acc[j >> 2][j & 3] = mfma32(fa[1][j >> 2], fb[1][j & 3], acc[j >> 2][j & 3]);
+                SB();
+                load(f, j);
+                if (j % 2 == 0) read(t, 0, 0, j / 2);
             }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            if (step + 2 < steps) {
-#pragma unroll
-                for (int q = 0; q < 8; ++q) fetch(step + 2, q);
-                sa.next();
-                sb.next();
-            }
+            SB();
         }
 
         // (the compiler does not see that what follows reads results of the matrix pipe: the distance it would keep)
@@ -376,6 +418,7 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
             }
         }
     }
+    wait_vmem();   // (no load to LDS outlives the workgroup)
 }
 
 // Which rows have a target, in order: one workgroup, 8 rows to a thread at a time.
