@@ -25,7 +25,7 @@ namespace {
 
 constexpr int kTile = 256;       // rows and columns of a result tile
 constexpr int kStep = 64;        // of the contraction
-constexpr int kOperandBytes = kTile * kStep * 2, kBufferBytes = 2 * kOperandBytes;
+constexpr int kOperandBytes = kTile * kStep * 2, kHalfBytes = kOperandBytes / 2, kBufferBytes = 2 * kOperandBytes;
 constexpr int kGrid = 256;       // workgroups: one per compute unit, each as much LDS as allows no second one
 constexpr int kStrip = 128;      // words whose largest logit and sum the forward keeps together
 constexpr int64_t kPieceBytes = (int64_t)2 << 30;  // of dz at most
@@ -72,32 +72,33 @@ struct Source {
     __device__ __forceinline__ void next() { at += step; left -= step; }
 };
 
-// A tile's operand in LDS, 32 KB, in one of two forms.  Its 16-byte pieces are laid out by the loads (slot = lane), so the
-// arrangement is made on the global side: a lane fetches the piece that belongs where it writes.
-//   ROWS  256 rows x 64 of the contraction (128 bytes a row): piece c of row r lies at c ^ (r / 2 & 7), so 16 rows' pieces of
+// A tile's operand in LDS: two halves of 16 KB, each of what the wavefronts read in a half of their blocks (of every 128 rows or columns
+// the first or the second 64).  A load's 64 pieces of 16 bytes lie one behind the other, so the arrangement is made on the global
+// side: a lane fetches the piece that belongs where it writes.
+//   ROWS  128 rows x 64 of the contraction (128 bytes a row): piece c of row r lies at c ^ (r / 2 & 7), so 16 rows' pieces of
 //         one c, which are read together, are 16 different slots of the 256 bytes that the banks span.
-//   COLS  64 of the contraction x 256 columns (512 bytes a row): piece c of row r lies at c ^ (r & 3) << 2, so the 4 rows x 64 bytes
+//   COLS  64 of the contraction x 128 columns (256 bytes a row): piece c of row r lies at c ^ (r & 3) << 2, so the 4 rows x 64 bytes
 //         that a transposing read takes together are 16 different slots too.
 template <bool COLS>
 struct Operand {
     int load[2];     // byte offsets of this lane's pieces in the tile's matrix: of even and odd instructions
-    int read[4];     // LDS offsets of its fragments: ROWS by sixteenth-step, COLS by block of 32 columns
+    int read[4];     // LDS offsets of its fragments: ROWS by sixteenth-step, COLS by block of 32 columns (two)
 
     __device__ __forceinline__ void init(int lane, int wave, int part, uint32_t pitch)
     {
         const int n = lane & 31, h = lane >> 5;
         if (!COLS) {
 #pragma unroll
-            for (int o = 0; o < 2; ++o) load[o] = (wave * 64 + (lane >> 3)) * (int)pitch + (((lane & 7) ^ (4 * o + (lane >> 4))) << 4);
+            for (int o = 0; o < 2; ++o)
+                load[o] = ((wave >> 1) * 128 + (wave & 1) * 32 + (lane >> 3)) * (int)pitch + (((lane & 7) ^ (4 * o + (lane >> 4))) << 4);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) read[k] = (part * 128 + n) * 128 + (((2 * k + h) ^ ((n >> 1) & 7)) << 4);
+            for (int k = 0; k < 4; ++k) read[k] = (part * 64 + n) * 128 + (((2 * k + h) ^ ((n >> 1) & 7)) << 4);
         } else {
+            const int piece = (lane & 15) ^ ((lane >> 4) << 2), s = lane & 15;
+            load[0] = load[1] = (wave * 16 + (lane >> 4)) * (int)pitch + (piece >> 3) * 256 + (piece & 7) * 16;
 #pragma unroll
-            for (int o = 0; o < 2; ++o) load[o] = (wave * 16 + (lane >> 5)) * (int)pitch + (((lane & 31) ^ ((2 * o + (lane >> 5)) << 2)) << 4);
-            const int s = lane & 15;
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-                read[t] = (8 * h + (s >> 2)) * 512 + ((4 * (4 * part + (t ^ (s >> 2))) + 2 * ((n >> 4) & 1) + ((s & 3) >> 1)) << 4) + 8 * (s & 1);
+            for (int t = 0; t < 2; ++t)
+                read[t] = (8 * h + (s >> 2)) * 256 + (((8 * part + 4 * t + 2 * ((n >> 4) & 1) + ((s & 3) >> 1)) ^ ((s >> 2) << 2)) << 4) + 8 * (s & 1);
         }
     }
     // This lane's offsets of a step.  `tail`: elements of the contraction that are left, where rows may end inside the
@@ -110,19 +111,19 @@ struct Operand {
             if (!COLS && ((lane & 7) ^ (4 * o + (lane >> 4))) * 8 >= tail) off[o] = (int)0x80000000;   // (past every descriptor's end)
         }
     }
-    // 8 instructions of a wavefront fill a quarter of the tile.
-    __device__ __forceinline__ static void fetch(i32x4 words, const int off[2], uint32_t pitch, uint32_t lds, int wave, int q)
+    // 4 instructions of each wavefront fill a half.
+    __device__ __forceinline__ static void fetch(i32x4 words, const int off[2], uint32_t pitch, uint32_t lds, int wave, int half, int q)
     {
-        dma_b128(words, lds + (wave * 8 + q) * 1024, off[q & 1], (int)(q * (COLS ? 2 : 8) * pitch));
+        dma_b128(words, lds + half * kHalfBytes + (wave * 4 + q) * 1024, off[q & 1], COLS ? half * 128 + (int)(q * 4 * pitch) : (int)((half * 64 + q * 8) * pitch));
     }
-    // fragment b (32 rows or columns) of sixteenth-step k: 8 consecutive elements of the contraction
-    __device__ __forceinline__ bf16x8 get(const unsigned char *t, int b, int k) const
+    // fragment b (32 rows or columns, 0 or 1) of a half and sixteenth-step k: 8 consecutive elements of the contraction
+    __device__ __forceinline__ bf16x8 get(const unsigned char *t, int half, int b, int k) const
     {
-        if (!COLS) return *(const bf16x8 *)(t + read[k] + b * 4096);
+        if (!COLS) return *(const bf16x8 *)(t + read[k] + half * kHalfBytes + b * 4096);
         typedef s16x4 __attribute__((address_space(3))) * lds_ptr_t;
-        const unsigned char *p = t + read[b] + k * 8192;
+        const unsigned char *p = t + read[b] + half * kHalfBytes + k * 4096;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)p);
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(p + 2048));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(p + 1024));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };
@@ -216,66 +217,99 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
     const int die = blockIdx.x & 7, per_die = (work.total + 7) / 8, stride = gridDim.x >> 3;
     const int begin = die * per_die + (blockIdx.x >> 3), end = min(work.total, (die + 1) * per_die);
 
-    // The steps of this workgroup's tiles are one sequence, two of them in LDS at any time: the loads run ahead across the end of a tile.
-    Source sa = {}, sb = {};
-    int next_tile = begin, next_left = 0, next_tail = 0, parity = 0;   // of the loads
-    auto find = [&]() {
-        while (next_left == 0 && next_tile < end) {
-            int m, nn, s;
-            work.locate(next_tile, m, nn, s);
-            next_left = work.steps_of(p, s);
-            work.sources(p, m, nn, s, sa, sb);
-            next_tail = K == kForward || K == kAgain ? p.H : 0x7fffffff;   // elements of the contraction
-            next_tile += stride;
-        }
+    // The steps of this workgroup's tiles are one sequence, and the loads run ahead in it across the end of a tile.
+    struct Cursor {
+        int tile, left, tail, parity;
+        Source a, b;
     };
-    struct Fetch {
+    struct Fetch {   // what the loads of a step need
         i32x4 a, b;
         int a_off[2], b_off[2];
         uint32_t lds;
     };
-    auto take = [&]() {   // what the loads of the next step need; behind the last one they read nothing
+    auto take = [&](Cursor &c) {   // the next step; behind the last one the loads read nothing
+        while (c.left == 0 && c.tile < end) {
+            int m, nn, s;
+            work.locate(c.tile, m, nn, s);
+            c.left = work.steps_of(p, s);
+            work.sources(p, m, nn, s, c.a, c.b);
+            c.tail = K == kForward || K == kAgain ? p.H : 0x7fffffff;   // elements of the contraction
+            c.tile += stride;
+        }
+        if (c.left == 0) c.a.left = c.b.left = 0;
         Fetch f;
-        find();
-        if (next_left == 0) sa.left = sb.left = 0;
-        f.a = sa.words();
-        f.b = sb.words();
-        A.offsets(lane, next_tail, f.a_off);
+        f.a = c.a.words();
+        f.b = c.b.words();
+        A.offsets(lane, c.tail, f.a_off);
         B.offsets(lane, kStep, f.b_off);
-        f.lds = lds0 + parity * kBufferBytes;
-        sa.next();
-        sb.next();
-        next_tail -= kStep;
-        next_left -= next_left > 0;
-        parity ^= 1;
+        f.lds = lds0 + c.parity * kBufferBytes;
+        c.a.next();
+        c.b.next();
+        c.tail -= kStep;
+        c.left -= c.left > 0;
+        c.parity ^= 1;
         return f;
     };
-    auto load = [&](const Fetch &f, int i) {   // the i-th of 16
-        if (i & 1) B.fetch(f.b, f.b_off, b_pitch, f.lds + kOperandBytes, wave, i >> 1);
-        else A.fetch(f.a, f.a_off, a_pitch, f.lds, wave, i >> 1);
+    auto load_a = [&](const Fetch &f, int half, int q) { A.fetch(f.a, f.a_off, a_pitch, f.lds, wave, half, q); };
+    auto load_b = [&](const Fetch &f, int half, int q) { B.fetch(f.b, f.b_off, b_pitch, f.lds + kOperandBytes, wave, half, q); };
+
+    // A step in four quarters, 16 products each: the results of (first half of A, first of B), (first, second), (second, second), (second, first).
+    // The halves' fragments are read a quarter before they are used, so a half's place in LDS is free long before the step
+    // ends, and its loads have five or six quarters until they are waited for:
+    //   quarter  products   reads                     loads (of the step after next, and A's first half of the one behind that)
+    //   1        A0 B0      B1
+    //   2        A0 B1      A1                        B0 B1
+    //   3        A1 B1      A0 of the next step       A1
+    //   4        A1 B0      B0 of the next step       A0
+    // Each quarter ends with a barrier: what was read in it (B0: in the one before) may be overwritten, and what the next one reads is there.  24 loads (20
+    // behind the first quarter) are younger than those.
+    bf16x8 a0[2][4], a1[2][4], b0[2][4], b1[2][4];
+    f32x16 acc[4][4];
+    auto quarter_end = [&](int which) {
+        SB();
+        if (which == 1) asm volatile("s_waitcnt vmcnt(20) lgkmcnt(0)" ::: "memory");
+        else if (which < 4) asm volatile("s_waitcnt vmcnt(24) lgkmcnt(0)" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(24)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        SB();
     };
-    bf16x8 fa[2][4], fb[2][4];   // fragments: of the sixteenth-step under way and of the next
-    auto read = [&](const unsigned char *t, int k, int to, int i) {   // the i-th of 8
-        if (i < 4) fb[to][i] = B.get(t + kOperandBytes, i, k);
-        else fa[to][i - 4] = A.get(t, i - 4, k);
-    };
+    Cursor ahead = {begin, 0, 0, 0, {}, {}}, rest = ahead;   // of A's first half, of the other three
 #pragma unroll
     for (int step = 0; step < 2; ++step) {
-        const Fetch f = take();
+        const Fetch f = take(ahead), g = take(rest);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) load(f, i);
+        for (int q = 0; q < 4; ++q) load_a(f, 0, q);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) load_b(g, 0, q);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) load_b(g, 1, q);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) load_a(g, 1, q);
     }
-    asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(24)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < 8; ++i) read(lds, 0, 0, i);
+    for (int j = 0; j < 8; ++j) {
+        a0[j & 1][j >> 1] = A.get(lds, 0, j & 1, j >> 1);
+        b0[j & 1][j >> 1] = B.get(lds + kOperandBytes, 0, j & 1, j >> 1);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    {
+        const Fetch f = take(ahead);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) load_a(f, 0, q);
+    }
+    quarter_end(4);
+
     int at = 0;   // LDS offset of the step under way
     for (int i = begin; i < end; i += stride) {
         int m, nn, s;
         work.locate(i, m, nn, s);
         const int steps = work.steps_of(p, s);
-        f32x16 acc[4][4];
 #pragma unroll
         for (int x = 0; x < 4; ++x)
 #pragma unroll
@@ -283,35 +317,46 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) acc[x][y][v] = 0.0f;
         for (int step = 0; step < steps; ++step) {
-            const unsigned char *t = lds + at;
-#pragma unroll
-            for (int k = 0; k < 3; ++k) {
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    SB();
-                    acc[j >> 2][j & 3] = mfma32(fa[k & 1][j >> 2], fb[k & 1][j & 3], acc[j >> 2][j & 3]);
-                    SB();
-                    if (j % 2 == 0) read(t, k + 1, (k + 1) & 1, j / 2);
-                }
-            }
-            SB();
-            // This step has been read to its last fragment, by every wavefront: the step after next may take its place.  The
-            // next one, whose loads were the last ones before, is there.
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            at ^= kBufferBytes;
-            t = lds + at;
-            const Fetch f = take();
+            const unsigned char *t = lds + at, *next = lds + (at ^ kBufferBytes);
+            // product j of a quarter: sixteenth-step j / 4, blocks j % 4 / 2 and j % 2
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
+                acc[j >> 1 & 1][j & 1] = mfma32(a0[j >> 1 & 1][j >> 2], b0[j & 1][j >> 2], acc[j >> 1 & 1][j & 1]);
                 SB();
-                acc[j >> 2][j & 3] = mfma32(fa[1][j >> 2], fb[1][j & 3], acc[j >> 2][j & 3]);
+                if (j < 8) b1[j & 1][j >> 1] = B.get(t + kOperandBytes, 1, j & 1, j >> 1);
                 SB();
-                load(f, j);
-                if (j % 2 == 0) read(t, 0, 0, j / 2);
             }
-            SB();
+            quarter_end(1);
+            const Fetch f = take(rest);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                acc[j >> 1 & 1][2 + (j & 1)] = mfma32(a0[j >> 1 & 1][j >> 2], b1[j & 1][j >> 2], acc[j >> 1 & 1][2 + (j & 1)]);
+                SB();
+                if (j < 8) a1[j & 1][j >> 1] = A.get(t, 1, j & 1, j >> 1);
+                if (j % 2 == 1) load_b(f, j >> 3, j >> 1 & 3);
+                SB();
+            }
+            quarter_end(2);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                acc[2 + (j >> 1 & 1)][2 + (j & 1)] = mfma32(a1[j >> 1 & 1][j >> 2], b1[j & 1][j >> 2], acc[2 + (j >> 1 & 1)][2 + (j & 1)]);
+                SB();
+                if (j < 8) a0[j & 1][j >> 1] = A.get(next, 0, j & 1, j >> 1);
+                if (j % 4 == 3) load_a(f, 1, j >> 2);
+                SB();
+            }
+            quarter_end(3);
+            const Fetch g = take(ahead);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                acc[2 + (j >> 1 & 1)][j & 1] = mfma32(a1[j >> 1 & 1][j >> 2], b0[j & 1][j >> 2], acc[2 + (j >> 1 & 1)][j & 1]);
+                SB();
+                if (j % 4 >= 2) b0[j & 1][j >> 2] = B.get(next + kOperandBytes, 0, j & 1, j >> 2);   // (its last product of the two has been issued)
+                else if (j % 4 == 1) load_a(g, 0, j >> 2);
+                SB();
+            }
+            quarter_end(4);
+            at ^= kBufferBytes;
         }
 
         // (the compiler does not see that what follows reads results of the matrix pipe: the distance it would keep)
