@@ -29,15 +29,17 @@ constexpr int kOperandBytes = kTile * kStep * 2, kHalfBytes = kOperandBytes / 2,
 constexpr int kGrid = 256;       // workgroups: one per compute unit, each as much LDS as allows no second one
 constexpr int kStrip = 128;      // words whose largest logit and sum the forward keeps together
 constexpr int64_t kPieceBytes = (int64_t)2 << 30;  // of dz at most
+// Rows of dz and of the gathered x are this much longer where their length is a multiple of 4 KB: the 256 rows of a tile would lie in few of the L2's sets.
+constexpr int kPitchPad = 64;
 constexpr int kMaxPieceWords = 1 << 20;            // (32-bit offsets within a tile of dz)
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 enum Kind { kForward, kAgain, kDx, kDw };
 
 struct LossArgs {
-    const uint16_t *x;       // gathered rows [.., Hp]
+    const uint16_t *x;       // gathered rows [.., xp], Hp of them used
     const uint16_t *w;       // [V, H]
-    uint16_t *dz;            // [.., vc]
+    uint16_t *dz;            // [.., zp], vc of them used
     const int32_t *n_rows;   // rows that have a target
     const int32_t *target;   // of the gathered rows
     const float *lse, *d;    // of the gathered rows (kAgain)
@@ -47,6 +49,7 @@ struct LossArgs {
     uint16_t *dw;            // [V, H] (kDw)
     int64_t Tp;
     int32_t V, H, Hp, v0, vc;
+    int32_t xp, zp;          // elements between rows of x and of dz
     int32_t first;           // kDx: the first piece (slabs are written, not added to)
 };
 
@@ -170,19 +173,19 @@ struct Product {
     }
     __device__ __forceinline__ void sources(const LossArgs &p, int m, int n, int s, Source &a, Source &b) const
     {
-        const int64_t H2 = (int64_t)p.H * 2, Hp2 = (int64_t)p.Hp * 2, vc2 = (int64_t)p.vc * 2;
+        const int64_t H2 = (int64_t)p.H * 2, xp2 = (int64_t)p.xp * 2, zp2 = (int64_t)p.zp * 2;
         if (K == kForward || K == kAgain) {
             const int64_t v = p.v0 + (int64_t)m * kTile;
             a = Source{(const unsigned char *)p.w + v * H2, min((int64_t)kTile, p.V - v) * H2, (uint32_t)H2, kStep * 2};
-            b = Source{(const unsigned char *)p.x + (int64_t)n * kTile * Hp2, kTile * Hp2, (uint32_t)Hp2, kStep * 2};
+            b = Source{(const unsigned char *)p.x + (int64_t)n * kTile * xp2, kTile * xp2, (uint32_t)xp2, kStep * 2};
         } else if (K == kDx) {
             const int64_t k0 = (int64_t)s * steps * kStep;
-            a = Source{(const unsigned char *)p.dz + (int64_t)m * kTile * vc2 + k0 * 2, kTile * vc2 - k0 * 2, (uint32_t)vc2, kStep * 2};
+            a = Source{(const unsigned char *)p.dz + (int64_t)m * kTile * zp2 + k0 * 2, kTile * zp2 - k0 * 2, (uint32_t)zp2, kStep * 2};
             b = Source{(const unsigned char *)p.w + (p.v0 + k0) * H2 + n * kTile * 2, (p.V - p.v0 - k0) * H2 - n * kTile * 2, (uint32_t)H2, kStep * H2};
         } else {
             const int64_t rows = (int64_t)steps * kStep;
-            a = Source{(const unsigned char *)p.x + m * kTile * 2, rows * Hp2 - m * kTile * 2, (uint32_t)Hp2, kStep * Hp2};
-            b = Source{(const unsigned char *)p.dz + (int64_t)n * kTile * 2, rows * vc2 - (int64_t)n * kTile * 2, (uint32_t)vc2, kStep * vc2};
+            a = Source{(const unsigned char *)p.x + m * kTile * 2, rows * xp2 - m * kTile * 2, (uint32_t)xp2, kStep * xp2};
+            b = Source{(const unsigned char *)p.dz + (int64_t)n * kTile * 2, rows * zp2 - (int64_t)n * kTile * 2, (uint32_t)zp2, kStep * zp2};
         }
     }
 };
@@ -196,18 +199,31 @@ __device__ __forceinline__ float result(float f)
     return r;
 }
 
+// Of the two lanes of a result column, one has rows 0..3 and 8..11 in e[0..7], the other rows 4..7 and 12..15: in bf16, the first one gets rows 0..7, the
+// second one rows 8..15.
+__device__ __forceinline__ uint4 eight_of(const float *e)
+{
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    const u32x2 a = __builtin_amdgcn_permlane32_swap(pack_bf16(e[0], e[1]), pack_bf16(e[4], e[5]), false, false);
+    const u32x2 b = __builtin_amdgcn_permlane32_swap(pack_bf16(e[2], e[3]), pack_bf16(e[6], e[7]), false, false);
+    return make_uint4(a[0], b[0], a[1], b[1]);
+}
+
 template <Kind K>
 __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
 {
     constexpr bool A_COLS = K == kDw, B_COLS = K == kDx || K == kDw;
-    __shared__ __align__(1024) unsigned char lds[2 * kBufferBytes];
+    // (what the results of a tile need of its rows comes by loads to LDS too, in two places by turns: a load to registers would be waited for
+    // together with all that are under way)
+    constexpr int kRowBytes = K == kForward ? kTile * 4 : K == kAgain ? 3 * kTile * 4 : 0;
+    __shared__ __align__(1024) unsigned char lds[2 * kBufferBytes + 2 * kRowBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1;
     const int n = lane & 31, h = lane >> 5;
     const int n_rows = __builtin_amdgcn_readfirstlane(*p.n_rows);
     Product<K> work;
     work.init(p, n_rows);
 
-    const uint32_t a_pitch = (uint32_t)(K == kDx ? p.vc : K == kDw ? p.Hp : p.H) * 2, b_pitch = (uint32_t)(K == kDx ? p.H : K == kDw ? p.vc : p.Hp) * 2;
+    const uint32_t a_pitch = (uint32_t)(K == kDx ? p.zp : K == kDw ? p.xp : p.H) * 2, b_pitch = (uint32_t)(K == kDx ? p.H : K == kDw ? p.zp : p.xp) * 2;
     Operand<A_COLS> A;
     Operand<B_COLS> B;
     A.init(lane, wave, wm, a_pitch);
@@ -305,11 +321,22 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
     }
     quarter_end(4);
 
-    int at = 0;   // LDS offset of the step under way
+    int at = 0, row_at = 2 * kBufferBytes;   // LDS offsets of the step under way and of the tile's row data
     for (int i = begin; i < end; i += stride) {
         int m, nn, s;
         work.locate(i, m, nn, s);
         const int steps = work.steps_of(p, s);
+        if (K == kForward || K == kAgain) {
+            const int row0 = nn * kTile + wave * 64;   // (a step has barriers enough until they are read)
+            dma_b32(rsrc_words(p.target + row0, 256), lds0 + row_at + wave * 256, lane * 4, 0);
+            if (K == kAgain) {
+                dma_b32(rsrc_words(p.lse + row0, 256), lds0 + row_at + 1024 + wave * 256, lane * 4, 0);
+                dma_b32(rsrc_words(p.d + row0, 256), lds0 + row_at + 2048 + wave * 256, lane * 4, 0);
+            }
+        }
+        const int *row_targets = (const int *)(lds + row_at);
+        const float *row_lse = (const float *)(lds + row_at + 1024), *row_d = (const float *)(lds + row_at + 2048);
+        row_at ^= (2 * kBufferBytes) ^ (2 * kBufferBytes + kRowBytes);
 #pragma unroll
         for (int x = 0; x < 4; ++x)
 #pragma unroll
@@ -361,69 +388,82 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
 
         // (the compiler does not see that what follows reads results of the matrix pipe: the distance it would keep)
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+        if ((K == kForward || K == kAgain) && steps < 2) {   // (the row data is older than the last 16 loads, not than 24)
+            asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        }
         // acc[x][y][v] is row 128 wm + 32 x + 8 (v / 4) + 4 h + v % 4 and column 128 wn + 32 y + n of the tile
         if (K == kForward) {
             const int strip = m * 2 + wm;
             const int words = p.V - strip * kStrip - 4 * h;   // of the strip, from this lane's first one on
+            const bool whole = (m * 2 + wm + 1) * kStrip <= p.V;
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
-                const int row = nn * kTile + wn * 128 + y * 32 + n;
+                const int in_tile = wn * 128 + y * 32 + n, row = nn * kTile + in_tile;
                 SB();
-                float most = -INFINITY;
+                float z[64];
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    SB();
+                for (int j = 0; j < 64; ++j) z[j] = result(acc[j >> 4][y][j & 15]);
+                if (!whole) {
 #pragma unroll
-                    for (int v = 0; v < 16; ++v)
-                        if (x * 32 + 8 * (v >> 2) + (v & 3) < words) most = fmaxf(most, result(acc[x][y][v]));
+                    for (int j = 0; j < 64; ++j)
+                        if (8 * (j >> 2) + (j & 3) >= words) z[j] = -INFINITY;
                 }
-                most = fmaxf(most, __shfl_xor(most, 32));
+                float most[4] = {z[0], z[1], z[2], z[3]};
+#pragma unroll
+                for (int j = 4; j < 64; ++j) most[j & 3] = fmaxf(most[j & 3], z[j]);
+                most[0] = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+                most[0] = fmaxf(most[0], __shfl_xor(most[0], 32));
                 // (no word at all, or an infinite logit: nothing is subtracted, so the sum is 0 or infinite and not NaN)
-                const float shift = fabsf(most) < INFINITY ? most * kLog2e : 0.0f;
-                float sum = 0.0f;
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    SB();
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        const float e = fast_exp2(result(acc[x][y][v]) * kLog2e - shift);
-                        sum += x * 32 + 8 * (v >> 2) + (v & 3) < words ? e : 0.0f;
-                    }
-                }
-                sum += __shfl_xor(sum, 32);
-                if (h == 0) p.strips[(int64_t)strip * p.Tp + row] = make_float2(most, sum);
-                const int t = p.target[row] - (m * kTile + wm * kStrip);   // (gathered rows are padded to whole tiles)
+                const float shift = fabsf(most[0]) < INFINITY ? most[0] * kLog2e : 0.0f;
+                const int t = row_targets[in_tile] - strip * kStrip;
                 if (__any(t >= 0 && t < kStrip)) {
+                    const int mine = (t & 4) == 4 * h && t >= 0 && t < kStrip && row < n_rows ? (t >> 3) * 4 + (t & 3) : -1;
 #pragma unroll
-                    for (int x = 0; x < 4; ++x)
-#pragma unroll
-                        for (int v = 0; v < 16; ++v)
-                            if (t == x * 32 + 8 * (v >> 2) + 4 * h + (v & 3) && row < n_rows) p.z_target[row] = result(acc[x][y][v]);
+                    for (int j = 0; j < 64; ++j)
+                        if (j == mine) p.z_target[row] = z[j];
                 }
+                float sum[4] = {};
+#pragma unroll
+                for (int j = 0; j < 64; ++j) sum[j & 3] += fast_exp2(z[j] * kLog2e - shift);
+                sum[0] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                sum[0] += __shfl_xor(sum[0], 32);
+                if (h == 0) p.strips[(int64_t)strip * p.Tp + row] = make_float2(most[0], sum[0]);
             }
         } else if (K == kAgain) {
-            const int word0 = p.v0 + m * kTile + wm * kStrip + 4 * h;
+            const int word0 = m * kTile + wm * kStrip;   // of the piece
+            const int words = p.V - p.v0 - word0 - 4 * h;
+            const bool whole = p.v0 + word0 + kStrip <= p.V;
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
-                const int row = nn * kTile + wn * 128 + y * 32 + n;
-                const float lse = p.lse[row] * kLog2e, d = p.d[row];
-                const int t = p.target[row] - word0;
-                uint16_t *out = p.dz + (int64_t)row * p.vc + (word0 - p.v0);
+                const int in_tile = wn * 128 + y * 32 + n, row = nn * kTile + in_tile;
+                const float lse = row_lse[in_tile] * kLog2e, d = row_d[in_tile];
+                const int t = row_targets[in_tile] - p.v0 - word0;
+                const bool hit = __any(t >= 0 && t < kStrip);
+                const int mine = (t & 4) == 4 * h && t >= 0 && t < kStrip ? (t >> 3) * 4 + (t & 3) : -1;
+                uint16_t *out = p.dz + (int64_t)row * p.zp + word0 + 8 * h;
 #pragma unroll
-                for (int x = 0; x < 4; ++x)
+                for (int x = 0; x < 4; ++x) {
+                    SB();
+                    float e[16];
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        SB();
-                        float e[4];
+                    for (int v = 0; v < 16; ++v) e[v] = fast_exp2(result(acc[x][y][v]) * kLog2e - lse);
+                    if (hit) {
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const int word = x * 32 + 8 * g + r;
-                            float f = fast_exp2(result(acc[x][y][4 * g + r]) * kLog2e - lse);
-                            if (word == t) f -= 1.0f;
-                            e[r] = word0 + word < p.V ? f * d : 0.0f;
-                        }
-                        *(uint2 *)(out + x * 32 + 8 * g) = make_uint2(pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]));
+                        for (int v = 0; v < 16; ++v)
+                            if (16 * x + v == mine) e[v] -= 1.0f;
                     }
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) e[v] *= d;
+                    if (!whole) {
+#pragma unroll
+                        for (int v = 0; v < 16; ++v)
+                            if (32 * x + 8 * (v >> 2) + (v & 3) >= words) e[v] = 0.0f;
+                    }
+                    *(uint4 *)(out + x * 32) = eight_of(e);
+                    *(uint4 *)(out + x * 32 + 16) = eight_of(e + 8);
+                }
             }
         } else if (K == kDx) {
             float *out = p.slabs + ((int64_t)(s * work.mt + m) * kTile + wm * 128) * p.Hp + nn * kTile + wn * 128;   // (the same for all lanes)
@@ -446,19 +486,20 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
                 }
             }
         } else {
-            const int col0 = m * kTile + wm * 128 + 4 * h;
+            const int col0 = m * kTile + wm * 128 + 8 * h;
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
                 const int word = p.v0 + nn * kTile + wn * 128 + y * 32 + n;
-                if (word < p.V) {
-                    uint16_t *out = p.dw + (int64_t)word * p.H + col0;
+                uint16_t *out = p.dw + (int64_t)word * p.H + col0;
 #pragma unroll
-                    for (int x = 0; x < 4; ++x)
+                for (int x = 0; x < 4; ++x) {
+                    SB();
+                    float e[16];
 #pragma unroll
-                        for (int g = 0; g < 4; ++g)
-                            if (col0 + x * 32 + 8 * g < p.H)
-                                *(uint2 *)(out + x * 32 + 8 * g) = make_uint2(pack_bf16(result(acc[x][y][4 * g]), result(acc[x][y][4 * g + 1])),
-                                                                              pack_bf16(result(acc[x][y][4 * g + 2]), result(acc[x][y][4 * g + 3])));
+                    for (int v = 0; v < 16; ++v) e[v] = result(acc[x][y][v]);
+                    const uint4 lo = eight_of(e), hi = eight_of(e + 8);
+                    if (word < p.V && col0 + x * 32 < p.H) *(uint4 *)(out + x * 32) = lo;
+                    if (word < p.V && col0 + x * 32 + 16 < p.H) *(uint4 *)(out + x * 32 + 16) = hi;
                 }
             }
         }
@@ -541,12 +582,12 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(const RowsArgs a)
 
 // X: the gathered rows, padded with zeros.
 __global__ __launch_bounds__(256) void loss_gather_kernel(const uint16_t *x, int64_t x_stride, int wide, const int32_t *n_rows, const int32_t *row,
-                                                          uint16_t *out, int H, int Hp)
+                                                          uint16_t *out, int H, int Hp, int xp)
 {
     const int n = *n_rows, padded = max(1, (n + kTile - 1) / kTile) * kTile;
     for (int r = blockIdx.x; r < padded; r += gridDim.x) {
         const uint16_t *in = r < n ? x + (int64_t)row[r] * x_stride : nullptr;
-        uint16_t *to = out + (int64_t)r * Hp;
+        uint16_t *to = out + (int64_t)r * xp;
         for (int c = threadIdx.x * 8; c < Hp; c += 256 * 8) {
             uint4 v = make_uint4(0, 0, 0, 0);
             if (in && c < H) {
@@ -617,13 +658,14 @@ __global__ __launch_bounds__(256) void loss_dx_kernel(const float *slabs, const 
 
 // The workspace, from sizes alone.
 struct Layout {
-    int64_t Tp, Hp, vc, pieces;
+    int64_t Tp, Hp, xp, vc, zp, pieces;
     int64_t n_rows, slot, row, target, lse, d, z_target, x, strips, dz, slabs, bytes;
     Layout(const skrull_loss_t &p, bool backward)
     {
         Tp = (p.rows + kTile - 1) / kTile * kTile;
         if (Tp == 0) Tp = kTile;
         Hp = (p.hidden + kStep - 1) / kStep * kStep;
+        xp = Hp * 2 % 4096 == 0 ? Hp + kPitchPad : Hp;
         const int64_t words = ((int64_t)p.vocab + kTile - 1) / kTile * kTile;
         int64_t most = kPieceBytes / (Tp * 2) / kTile * kTile;
         most = most < kTile ? kTile : most > kMaxPieceWords ? kMaxPieceWords : most;
@@ -636,12 +678,13 @@ struct Layout {
         slot = take(p.rows * 4);
         row = take(Tp * 4);
         target = take(Tp * 4);
-        x = take(Tp * Hp * 2);
-        lse = d = z_target = strips = dz = slabs = 0;
+        x = take(Tp * xp * 2);
+        lse = d = z_target = strips = dz = slabs = zp = 0;
         if (backward) {
             lse = take(Tp * 4);
             d = take(Tp * 4);
-            dz = take(Tp * vc * 2);
+            zp = vc * 2 % 4096 == 0 ? vc + kPitchPad : vc;
+            dz = take(Tp * zp * 2);
             // (parts of the vocabulary are made only where there are fewer tiles than compute units)
             const int64_t h_tiles = (p.hidden + kTile - 1) / kTile, parted = kGrid / h_tiles * kTile;
             slabs = take((Tp > parted ? Tp : parted) * Hp * 4);
@@ -675,7 +718,7 @@ hipError_t gather(const skrull_loss_t &p, const Layout &l, unsigned char *ws, co
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int wide = aligned_to(x, 16) && p.x_stride % 8 == 0;
-    loss_gather_kernel<<<(int)(l.Tp < 2048 ? l.Tp : 2048), 256, 0, st>>>((const uint16_t *)x, p.x_stride, wide, a.n_rows, a.row, (uint16_t *)(ws + l.x), p.hidden, (int)l.Hp);
+    loss_gather_kernel<<<(int)(l.Tp < 2048 ? l.Tp : 2048), 256, 0, st>>>((const uint16_t *)x, p.x_stride, wide, a.n_rows, a.row, (uint16_t *)(ws + l.x), p.hidden, (int)l.Hp, (int)l.xp);
     return hipGetLastError();
 }
 
@@ -684,7 +727,7 @@ LossArgs args_of(const skrull_loss_t &p, const Layout &l, unsigned char *ws, con
     LossArgs a = {};
     a.x = (const uint16_t *)(ws + l.x); a.w = (const uint16_t *)w;
     a.n_rows = (const int32_t *)(ws + l.n_rows); a.target = (const int32_t *)(ws + l.target);
-    a.Tp = l.Tp; a.V = p.vocab; a.H = p.hidden; a.Hp = (int32_t)l.Hp;
+    a.Tp = l.Tp; a.V = p.vocab; a.H = p.hidden; a.Hp = (int32_t)l.Hp; a.xp = (int32_t)l.xp;
     return a;
 }
 
@@ -749,6 +792,7 @@ int skrull_loss_bwd(const skrull_loss_t *p, const void *x, const void *w, const 
     a.slabs = (float *)(ws + l.slabs);
     a.dw = (uint16_t *)dw;
     a.vc = (int32_t)l.vc;
+    a.zp = (int32_t)l.zp;
     for (int64_t i = 0; i < l.pieces && e == hipSuccess; ++i) {
         a.v0 = (int32_t)(i * l.vc);
         a.first = i == 0;
