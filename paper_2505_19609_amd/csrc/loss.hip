@@ -269,39 +269,29 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
     auto load_a = [&](const Fetch &f, int half, int q) { A.fetch(f.a, f.a_off, a_pitch, f.lds, wave, half, q); };
     auto load_b = [&](const Fetch &f, int half, int q) { B.fetch(f.b, f.b_off, b_pitch, f.lds + kOperandBytes, wave, half, q); };
 
-    // A step in four quarters, 16 products each: the results of (first half of A, first of B), (first, second), (second, second), (second, first).
-    // The halves' fragments are read a quarter before they are used, so a half's place in LDS is free long before the step
-    // ends, and its loads have five or six quarters until they are waited for:
-    //   quarter  products   reads                     loads (of the step after next, and A's first half of the one behind that)
-    //   1        A0 B0      B1
-    //   2        A0 B1      A1                        B0 B1
-    //   3        A1 B1      A0 of the next step       A1
-    //   4        A1 B0      B0 of the next step       A0
-    // Each quarter ends with a barrier: what was read in it (B0: in the one before) may be overwritten, and what the next one reads is there.  24 loads (20
-    // behind the first quarter) are younger than those.
+    // A step in two halves of 32 products.  What a half of the blocks needs is read half a step before its first product, so its place
+    // in LDS is free early, and its loads have a step until they are waited for:
+    //   half  products        reads                       loads (of the step after next)
+    //   1     A0 B0, A0 B1    B1, A1                      A0 B0
+    //   2     A1 B0, A1 B1    A0, B0 of the next step     B1 A1
+    // Each half ends with a barrier: what was read in it may be overwritten, and what the next one reads is there (16 loads are younger).
     bf16x8 a0[2][4], a1[2][4], b0[2][4], b1[2][4];
     f32x16 acc[4][4];
-    auto quarter_end = [&](int which) {
+    auto half_end = [&]() {
         SB();
-        if (which == 1) asm volatile("s_waitcnt vmcnt(20) lgkmcnt(0)" ::: "memory");
-        else if (which < 4) asm volatile("s_waitcnt vmcnt(24) lgkmcnt(0)" ::: "memory");
-        else asm volatile("s_waitcnt vmcnt(24)" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(16) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         SB();
     };
-    Cursor ahead = {begin, 0, 0, 0, {}, {}}, rest = ahead;   // of A's first half, of the other three
+    Cursor cursor = {begin, 0, 0, 0, {}, {}};
 #pragma unroll
     for (int step = 0; step < 2; ++step) {
-        const Fetch f = take(ahead), g = take(rest);
+        const Fetch f = take(cursor);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) load_a(f, 0, q);
+        for (int q = 0; q < 4; ++q) { load_a(f, 0, q); load_b(f, 0, q); }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) load_b(g, 0, q);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) load_b(g, 1, q);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) load_a(g, 1, q);
+        for (int q = 0; q < 4; ++q) { load_b(f, 1, q); load_a(f, 1, q); }
     }
     asm volatile("s_waitcnt vmcnt(24)" ::: "memory");
     __builtin_amdgcn_s_barrier();
@@ -311,15 +301,7 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
         a0[j & 1][j >> 1] = A.get(lds, 0, j & 1, j >> 1);
         b0[j & 1][j >> 1] = B.get(lds + kOperandBytes, 0, j & 1, j >> 1);
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    {
-        const Fetch f = take(ahead);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) load_a(f, 0, q);
-    }
-    quarter_end(4);
+    half_end();
 
     int at = 0, row_at = 2 * kBufferBytes;   // LDS offsets of the step under way and of the tile's row data
     for (int i = begin; i < end; i += stride) {
@@ -327,7 +309,7 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
         work.locate(i, m, nn, s);
         const int steps = work.steps_of(p, s);
         if (K == kForward || K == kAgain) {
-            const int row0 = nn * kTile + wave * 64;   // (a step has barriers enough until they are read)
+            const int row0 = nn * kTile + wave * 64;   // (older than a step's 16 loads: there when the first one ends)
             dma_b32(rsrc_words(p.target + row0, 256), lds0 + row_at + wave * 256, lane * 4, 0);
             if (K == kAgain) {
                 dma_b32(rsrc_words(p.lse + row0, 256), lds0 + row_at + 1024 + wave * 256, lane * 4, 0);
@@ -345,54 +327,47 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
                 for (int v = 0; v < 16; ++v) acc[x][y][v] = 0.0f;
         for (int step = 0; step < steps; ++step) {
             const unsigned char *t = lds + at, *next = lds + (at ^ kBufferBytes);
+            const Fetch f = take(cursor);
             // product j of a quarter: sixteenth-step j / 4, blocks j % 4 / 2 and j % 2
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
                 acc[j >> 1 & 1][j & 1] = mfma32(a0[j >> 1 & 1][j >> 2], b0[j & 1][j >> 2], acc[j >> 1 & 1][j & 1]);
                 SB();
                 if (j < 8) b1[j & 1][j >> 1] = B.get(t + kOperandBytes, 1, j & 1, j >> 1);
+                else if (j & 1) load_b(f, 0, j - 8 >> 1);
+                else load_a(f, 0, j - 8 >> 1);
                 SB();
             }
-            quarter_end(1);
-            const Fetch f = take(rest);
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
                 acc[j >> 1 & 1][2 + (j & 1)] = mfma32(a0[j >> 1 & 1][j >> 2], b1[j & 1][j >> 2], acc[j >> 1 & 1][2 + (j & 1)]);
                 SB();
                 if (j < 8) a1[j & 1][j >> 1] = A.get(t, 1, j & 1, j >> 1);
-                if (j % 2 == 1) load_b(f, j >> 3, j >> 1 & 3);
                 SB();
             }
-            quarter_end(2);
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                acc[2 + (j >> 1 & 1)][2 + (j & 1)] = mfma32(a1[j >> 1 & 1][j >> 2], b1[j & 1][j >> 2], acc[2 + (j >> 1 & 1)][2 + (j & 1)]);
-                SB();
-                if (j < 8) a0[j & 1][j >> 1] = A.get(next, 0, j & 1, j >> 1);
-                if (j % 4 == 3) load_a(f, 1, j >> 2);
-                SB();
-            }
-            quarter_end(3);
-            const Fetch g = take(ahead);
+            half_end();
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
                 acc[2 + (j >> 1 & 1)][j & 1] = mfma32(a1[j >> 1 & 1][j >> 2], b0[j & 1][j >> 2], acc[2 + (j >> 1 & 1)][j & 1]);
                 SB();
-                if (j % 4 >= 2) b0[j & 1][j >> 2] = B.get(next + kOperandBytes, 0, j & 1, j >> 2);   // (its last product of the two has been issued)
-                else if (j % 4 == 1) load_a(g, 0, j >> 2);
+                if (j < 8) a0[j & 1][j >> 1] = A.get(next, 0, j & 1, j >> 1);
+                else if (j & 1) load_a(f, 1, j - 8 >> 1);
+                else load_b(f, 1, j - 8 >> 1);
                 SB();
             }
-            quarter_end(4);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                acc[2 + (j >> 1 & 1)][2 + (j & 1)] = mfma32(a1[j >> 1 & 1][j >> 2], b1[j & 1][j >> 2], acc[2 + (j >> 1 & 1)][2 + (j & 1)]);
+                SB();
+                if (j < 8) b0[j & 1][j >> 1] = B.get(next + kOperandBytes, 0, j & 1, j >> 1);
+                SB();
+            }
+            half_end();
             at ^= kBufferBytes;
         }
 
         // (the compiler does not see that what follows reads results of the matrix pipe: the distance it would keep)
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
-        if ((K == kForward || K == kAgain) && steps < 2) {   // (the row data is older than the last 16 loads, not than 24)
-            asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-        }
         // acc[x][y][v] is row 128 wm + 32 x + 8 (v / 4) + 4 h + v % 4 and column 128 wn + 32 y + n of the tile
         if (K == kForward) {
             const int strip = m * 2 + wm;
