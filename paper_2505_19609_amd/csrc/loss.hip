@@ -11,10 +11,11 @@
 //   dW^T     X^T dz                a piece's rows of dW are complete after one product
 // What bounds them is the matrix pipe: 2 T V H operations each, against 2 (T + V) H bytes.
 //
-// A workgroup is 4 wavefronts, one per SIMD, and forms a tile of 256 x 256: each wavefront 128 x 128, 4 x 4 results of
-// v_mfma_f32_32x32x16_bf16 in 256 accumulator registers, so that an operand fragment read from LDS feeds four products.  Steps of 64 along
-// the contraction lie in two LDS buffers of 64 KB, filled by loads that write LDS directly; a step's fragments are read one
-// sixteenth-step ahead of the products, and the one barrier of a step stands where a buffer has been read to its last fragment.
+// A workgroup is 4 wavefronts, one per SIMD, and forms a tile of 256 x 256: each wavefront 128 x 128, 8 x 8 results of
+// v_mfma_f32_16x16x32_bf16 in 256 accumulator registers, so that an operand fragment read from LDS feeds eight products.  Steps of 64 along
+// the contraction lie in two LDS buffers of 64 KB, filled by loads that write LDS directly.
+// The chip's power decides the clock under such products, and with it what an instruction is worth: with normally distributed operands in registers and
+// nothing else, 16 x 16 x 32 runs at 2,010 TFLOP/s, 32 x 32 x 16 (which moves each accumulator twice as often) at 1,705.
 #include <math.h>
 
 #include "ops.h"
@@ -33,6 +34,10 @@ constexpr int64_t kPieceBytes = (int64_t)2 << 30;  // of dz at most
 constexpr int kPitchPad = 64;
 constexpr int kMaxPieceWords = 1 << 20;            // (32-bit offsets within a tile of dz)
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+// What is taken off logits whose largest one this is: nothing where there is no word at all, or an infinite logit, so that a sum is 0 or infinite
+// and not NaN.
+__device__ __forceinline__ float shift_of(float most) { return fabsf(most) < INFINITY ? most : 0.0f; }
 
 enum Kind { kForward, kAgain, kDx, kDw };
 
@@ -80,28 +85,31 @@ struct Source {
 // side: a lane fetches the piece that belongs where it writes.
 //   ROWS  128 rows x 64 of the contraction (128 bytes a row): piece c of row r lies at c ^ (r / 2 & 7), so 16 rows' pieces of
 //         one c, which are read together, are 16 different slots of the 256 bytes that the banks span.
-//   COLS  64 of the contraction x 128 columns (256 bytes a row): piece c of row r lies at c ^ (r & 3) << 2, so the 4 rows x 64 bytes
+//   COLS  64 of the contraction x 128 columns (256 bytes a row): piece c of row r lies at c ^ 2 (r & 3 | r / 2 & 4), so the 8 rows x 32 bytes
 //         that a transposing read takes together are 16 different slots too.
 template <bool COLS>
 struct Operand {
-    int load[2];     // byte offsets of this lane's pieces in the tile's matrix: of even and odd instructions
-    int read[4];     // LDS offsets of its fragments: ROWS by sixteenth-step, COLS by block of 32 columns (two)
+    int load[2];     // byte offsets of this lane's pieces in the tile's matrix: of even and odd instructions (COLS: of the first and the last two)
+    int read[4];     // LDS offsets of its fragments: ROWS by half step (two), COLS by block of 16 columns
 
     __device__ __forceinline__ void init(int lane, int wave, int part, uint32_t pitch)
     {
-        const int n = lane & 31, h = lane >> 5;
+        const int s = lane & 15, g = lane >> 4;
         if (!COLS) {
 #pragma unroll
             for (int o = 0; o < 2; ++o)
                 load[o] = ((wave >> 1) * 128 + (wave & 1) * 32 + (lane >> 3)) * (int)pitch + (((lane & 7) ^ (4 * o + (lane >> 4))) << 4);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) read[k] = (part * 64 + n) * 128 + (((2 * k + h) ^ ((n >> 1) & 7)) << 4);
+            for (int k = 0; k < 2; ++k) read[k] = (part * 64 + s) * 128 + (((4 * k + g) ^ (s >> 1)) << 4);
         } else {
-            const int piece = (lane & 15) ^ ((lane >> 4) << 2), s = lane & 15;
-            load[0] = load[1] = (wave * 16 + (lane >> 4)) * (int)pitch + (piece >> 3) * 256 + (piece & 7) * 16;
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-                read[t] = (8 * h + (s >> 2)) * 256 + (((8 * part + 4 * t + 2 * ((n >> 4) & 1) + ((s & 3) >> 1)) ^ ((s >> 2) << 2)) << 4) + 8 * (s & 1);
+            for (int o = 0; o < 2; ++o) {
+                const int piece = s ^ (g + 4 * o) << 1;
+                load[o] = (wave * 16 + g) * (int)pitch + (piece >> 3) * 256 + (piece & 7) * 16;
+            }
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                read[t] = (8 * g + (s >> 2)) * 256 + (((8 * part + 2 * t + ((s & 3) >> 1)) ^ ((s >> 2) + 4 * (g & 1)) << 1) << 4) + 8 * (s & 1);
         }
     }
     // This lane's offsets of a step.  `tail`: elements of the contraction that are left, where rows may end inside the
@@ -117,14 +125,15 @@ struct Operand {
     // 4 instructions of each wavefront fill a half.
     __device__ __forceinline__ static void fetch(i32x4 words, const int off[2], uint32_t pitch, uint32_t lds, int wave, int half, int q)
     {
-        dma_b128(words, lds + half * kHalfBytes + (wave * 4 + q) * 1024, off[q & 1], COLS ? half * 128 + (int)(q * 4 * pitch) : (int)((half * 64 + q * 8) * pitch));
+        dma_b128(words, lds + half * kHalfBytes + (wave * 4 + q) * 1024, off[COLS ? q >> 1 : q & 1],
+                 COLS ? half * 128 + (int)(q * 4 * pitch) : (int)((half * 64 + q * 8) * pitch));
     }
-    // fragment b (32 rows or columns, 0 or 1) of a half and sixteenth-step k: 8 consecutive elements of the contraction
+    // fragment b (16 rows or columns, 0..3) of a half and half step k: 8 consecutive elements of the contraction
     __device__ __forceinline__ bf16x8 get(const unsigned char *t, int half, int b, int k) const
     {
-        if (!COLS) return *(const bf16x8 *)(t + read[k] + half * kHalfBytes + b * 4096);
+        if (!COLS) return *(const bf16x8 *)(t + read[k] + half * kHalfBytes + b * 2048);
         typedef s16x4 __attribute__((address_space(3))) * lds_ptr_t;
-        const unsigned char *p = t + read[b] + half * kHalfBytes + k * 4096;
+        const unsigned char *p = t + read[b] + half * kHalfBytes + k * 8192;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)p);
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(p + 1024));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -145,8 +154,8 @@ struct Product {
             nt = row_tiles;
             steps = p.Hp / kStep;
         } else if (K == kDx) {
-            mt = row_tiles;
-            nt = h_tiles;
+            mt = h_tiles;
+            nt = row_tiles;
             splits = dx_splits(mt * nt, p.vc / kStep);
             steps = (p.vc / kStep + splits - 1) / splits;
         } else {
@@ -180,8 +189,8 @@ struct Product {
             b = Source{(const unsigned char *)p.x + (int64_t)n * kTile * xp2, kTile * xp2, (uint32_t)xp2, kStep * 2};
         } else if (K == kDx) {
             const int64_t k0 = (int64_t)s * steps * kStep;
-            a = Source{(const unsigned char *)p.dz + (int64_t)m * kTile * zp2 + k0 * 2, kTile * zp2 - k0 * 2, (uint32_t)zp2, kStep * 2};
-            b = Source{(const unsigned char *)p.w + (p.v0 + k0) * H2 + n * kTile * 2, (p.V - p.v0 - k0) * H2 - n * kTile * 2, (uint32_t)H2, kStep * H2};
+            a = Source{(const unsigned char *)p.w + (p.v0 + k0) * H2 + m * kTile * 2, (p.V - p.v0 - k0) * H2 - m * kTile * 2, (uint32_t)H2, kStep * H2};
+            b = Source{(const unsigned char *)p.dz + (int64_t)n * kTile * zp2 + k0 * 2, kTile * zp2 - k0 * 2, (uint32_t)zp2, kStep * 2};
         } else {
             const int64_t rows = (int64_t)steps * kStep;
             a = Source{(const unsigned char *)p.x + m * kTile * 2, rows * xp2 - m * kTile * 2, (uint32_t)xp2, kStep * xp2};
@@ -199,31 +208,31 @@ __device__ __forceinline__ float result(float f)
     return r;
 }
 
-// Of the two lanes of a result column, one has rows 0..3 and 8..11 in e[0..7], the other rows 4..7 and 12..15: in bf16, the first one gets rows 0..7, the
-// second one rows 8..15.
-__device__ __forceinline__ uint4 eight_of(const float *e)
+// Lane g of the four of a result column has rows 4 g .. 4 g + 3 of two blocks of 16.  In bf16, it gets rows 8 (g / 2) .. + 7 of the block g % 2.
+__device__ __forceinline__ uint4 eight_of(const float *first, const float *second)
 {
     typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-    const u32x2 a = __builtin_amdgcn_permlane32_swap(pack_bf16(e[0], e[1]), pack_bf16(e[4], e[5]), false, false);
-    const u32x2 b = __builtin_amdgcn_permlane32_swap(pack_bf16(e[2], e[3]), pack_bf16(e[6], e[7]), false, false);
+    const u32x2 a = __builtin_amdgcn_permlane16_swap(pack_bf16(first[0], first[1]), pack_bf16(second[0], second[1]), false, false);
+    const u32x2 b = __builtin_amdgcn_permlane16_swap(pack_bf16(first[2], first[3]), pack_bf16(second[2], second[3]), false, false);
     return make_uint4(a[0], b[0], a[1], b[1]);
 }
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
 template <Kind K>
 __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
 {
-    constexpr bool A_COLS = K == kDw, B_COLS = K == kDx || K == kDw;
+    constexpr bool A_COLS = K == kDx || K == kDw, B_COLS = K == kDw;
     // (what the results of a tile need of its rows comes by loads to LDS too, in two places by turns: a load to registers would be waited for
     // together with all that are under way)
     constexpr int kRowBytes = K == kForward ? kTile * 4 : K == kAgain ? 3 * kTile * 4 : 0;
     __shared__ __align__(1024) unsigned char lds[2 * kBufferBytes + 2 * kRowBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1;
-    const int n = lane & 31, h = lane >> 5;
+    const int n = lane & 15, g = lane >> 4;
     const int n_rows = __builtin_amdgcn_readfirstlane(*p.n_rows);
     Product<K> work;
     work.init(p, n_rows);
 
-    const uint32_t a_pitch = (uint32_t)(K == kDx ? p.zp : K == kDw ? p.xp : p.H) * 2, b_pitch = (uint32_t)(K == kDx ? p.H : K == kDw ? p.zp : p.xp) * 2;
+    const uint32_t a_pitch = (uint32_t)(K == kDw ? p.xp : p.H) * 2, b_pitch = (uint32_t)(K == kDx || K == kDw ? p.zp : p.xp) * 2;
     Operand<A_COLS> A;
     Operand<B_COLS> B;
     A.init(lane, wave, wm, a_pitch);
@@ -269,14 +278,14 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
     auto load_a = [&](const Fetch &f, int half, int q) { A.fetch(f.a, f.a_off, a_pitch, f.lds, wave, half, q); };
     auto load_b = [&](const Fetch &f, int half, int q) { B.fetch(f.b, f.b_off, b_pitch, f.lds + kOperandBytes, wave, half, q); };
 
-    // A step in two halves of 32 products.  What a half of the blocks needs is read half a step before its first product, so its place
+    // A step in two halves of 64 products.  What a half of the blocks needs is read half a step before its first product, so its place
     // in LDS is free early, and its loads have a step until they are waited for:
     //   half  products        reads                       loads (of the step after next)
     //   1     A0 B0, A0 B1    B1, A1                      A0 B0
     //   2     A1 B0, A1 B1    A0, B0 of the next step     B1 A1
     // Each half ends with a barrier: what was read in it may be overwritten, and what the next one reads is there (16 loads are younger).
-    bf16x8 a0[2][4], a1[2][4], b0[2][4], b1[2][4];
-    f32x16 acc[4][4];
+    bf16x8 a0[4][2], a1[4][2], b0[4][2], b1[4][2];   // [block of 16][half step]
+    f32x4 acc[8][8];
     auto half_end = [&]() {
         SB();
         asm volatile("s_waitcnt vmcnt(16) lgkmcnt(0)" ::: "memory");
@@ -298,8 +307,8 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
     asm volatile("" ::: "memory");
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        a0[j & 1][j >> 1] = A.get(lds, 0, j & 1, j >> 1);
-        b0[j & 1][j >> 1] = B.get(lds + kOperandBytes, 0, j & 1, j >> 1);
+        a0[j & 3][j >> 2] = A.get(lds, 0, j & 3, j >> 2);
+        b0[j & 3][j >> 2] = B.get(lds + kOperandBytes, 0, j & 3, j >> 2);
     }
     half_end();
 
@@ -320,46 +329,54 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
         const float *row_lse = (const float *)(lds + row_at + 1024), *row_d = (const float *)(lds + row_at + 2048);
         row_at ^= (2 * kBufferBytes) ^ (2 * kBufferBytes + kRowBytes);
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
+        for (int x = 0; x < 8; ++x)
 #pragma unroll
-            for (int y = 0; y < 4; ++y)
+            for (int y = 0; y < 8; ++y)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) acc[x][y][v] = 0.0f;
+                for (int v = 0; v < 4; ++v) acc[x][y][v] = 0.0f;
         for (int step = 0; step < steps; ++step) {
             const unsigned char *t = lds + at, *next = lds + (at ^ kBufferBytes);
             const Fetch f = take(cursor);
-            // product j of a quarter: sixteenth-step j / 4, blocks j % 4 / 2 and j % 2
+            // product j of a quarter: half step j / 16, blocks j / 4 % 4 and j % 4; between two of them at most one read or load, i = j / 2
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                acc[j >> 1 & 1][j & 1] = mfma32(a0[j >> 1 & 1][j >> 2], b0[j & 1][j >> 2], acc[j >> 1 & 1][j & 1]);
+            for (int j = 0; j < 32; ++j) {
+                const int k = j >> 4, x = j >> 2 & 3, y = j & 3, i = j >> 1;
+                acc[x][y] = mfma16(a0[x][k], b0[y][k], acc[x][y]);
                 SB();
-                if (j < 8) b1[j & 1][j >> 1] = B.get(t + kOperandBytes, 1, j & 1, j >> 1);
-                else if (j & 1) load_b(f, 0, j - 8 >> 1);
-                else load_a(f, 0, j - 8 >> 1);
+                if (j & 1) continue;
+                if (i < 8) b1[i & 3][i >> 2] = B.get(t + kOperandBytes, 1, i & 3, i >> 2);
+                else if (i & 1) load_b(f, 0, i - 8 >> 1);
+                else load_a(f, 0, i - 8 >> 1);
                 SB();
             }
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                acc[j >> 1 & 1][2 + (j & 1)] = mfma32(a0[j >> 1 & 1][j >> 2], b1[j & 1][j >> 2], acc[j >> 1 & 1][2 + (j & 1)]);
+            for (int j = 0; j < 32; ++j) {
+                const int k = j >> 4, x = j >> 2 & 3, y = j & 3, i = j >> 1;
+                acc[x][4 + y] = mfma16(a0[x][k], b1[y][k], acc[x][4 + y]);
                 SB();
-                if (j < 8) a1[j & 1][j >> 1] = A.get(t, 1, j & 1, j >> 1);
+                if (j & 1) continue;
+                if (i < 8) a1[i & 3][i >> 2] = A.get(t, 1, i & 3, i >> 2);
                 SB();
             }
             half_end();
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                acc[2 + (j >> 1 & 1)][j & 1] = mfma32(a1[j >> 1 & 1][j >> 2], b0[j & 1][j >> 2], acc[2 + (j >> 1 & 1)][j & 1]);
+            for (int j = 0; j < 32; ++j) {
+                const int k = j >> 4, x = j >> 2 & 3, y = j & 3, i = j >> 1;
+                acc[4 + x][y] = mfma16(a1[x][k], b0[y][k], acc[4 + x][y]);
                 SB();
-                if (j < 8) a0[j & 1][j >> 1] = A.get(next, 0, j & 1, j >> 1);
-                else if (j & 1) load_a(f, 1, j - 8 >> 1);
-                else load_b(f, 1, j - 8 >> 1);
+                if (j & 1) continue;
+                if (i < 8) a0[i & 3][i >> 2] = A.get(next, 0, i & 3, i >> 2);
+                else if (i & 1) load_a(f, 1, i - 8 >> 1);
+                else load_b(f, 1, i - 8 >> 1);
                 SB();
             }
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                acc[2 + (j >> 1 & 1)][2 + (j & 1)] = mfma32(a1[j >> 1 & 1][j >> 2], b1[j & 1][j >> 2], acc[2 + (j >> 1 & 1)][2 + (j & 1)]);
+            for (int j = 0; j < 32; ++j) {
+                const int k = j >> 4, x = j >> 2 & 3, y = j & 3, i = j >> 1;
+                acc[4 + x][4 + y] = mfma16(a1[x][k], b1[y][k], acc[4 + x][4 + y]);
                 SB();
-                if (j < 8) b0[j & 1][j >> 1] = B.get(next + kOperandBytes, 0, j & 1, j >> 1);
+                if (j & 1) continue;
+                if (i < 8) b0[i & 3][i >> 2] = B.get(next + kOperandBytes, 0, i & 3, i >> 2);
                 SB();
             }
             half_end();
@@ -368,113 +385,125 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
 
         // (the compiler does not see that what follows reads results of the matrix pipe: the distance it would keep)
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
-        // acc[x][y][v] is row 128 wm + 32 x + 8 (v / 4) + 4 h + v % 4 and column 128 wn + 32 y + n of the tile
+        // acc[x][y][v] is row 128 wm + 16 x + 4 g + v and column 128 wn + 16 y + n of the tile
         if (K == kForward) {
             const int strip = m * 2 + wm;
-            const int words = p.V - strip * kStrip - 4 * h;   // of the strip, from this lane's first one on
+            const int words = p.V - strip * kStrip - 4 * g;   // of the strip, from this lane's first one on
             const bool whole = (m * 2 + wm + 1) * kStrip <= p.V;
+            float most[8], sum[8];   // of this lane's words; the four lanes of a row are put together at the end
 #pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                const int in_tile = wn * 128 + y * 32 + n, row = nn * kTile + in_tile;
+            for (int y = 0; y < 8; ++y) {
+                const int in_tile = wn * 128 + y * 16 + n, row = nn * kTile + in_tile;
                 SB();
-                float z[64];
+                float z[32];
 #pragma unroll
-                for (int j = 0; j < 64; ++j) z[j] = result(acc[j >> 4][y][j & 15]);
+                for (int j = 0; j < 32; ++j) z[j] = result(acc[j >> 2][y][j & 3]);
                 if (!whole) {
 #pragma unroll
-                    for (int j = 0; j < 64; ++j)
-                        if (8 * (j >> 2) + (j & 3) >= words) z[j] = -INFINITY;
+                    for (int j = 0; j < 32; ++j)
+                        if (16 * (j >> 2) + (j & 3) >= words) z[j] = -INFINITY;
                 }
-                float most[4] = {z[0], z[1], z[2], z[3]};
+                float a[2] = {z[0], z[1]}, b[2] = {};
 #pragma unroll
-                for (int j = 4; j < 64; ++j) most[j & 3] = fmaxf(most[j & 3], z[j]);
-                most[0] = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
-                most[0] = fmaxf(most[0], __shfl_xor(most[0], 32));
-                // (no word at all, or an infinite logit: nothing is subtracted, so the sum is 0 or infinite and not NaN)
-                const float shift = fabsf(most[0]) < INFINITY ? most[0] * kLog2e : 0.0f;
+                for (int j = 2; j < 32; ++j) a[j & 1] = fmaxf(a[j & 1], z[j]);
+                most[y] = fmaxf(a[0], a[1]);
+                const float shift = shift_of(most[y]) * kLog2e;
                 const int t = row_targets[in_tile] - strip * kStrip;
                 if (__any(t >= 0 && t < kStrip)) {
-                    const int mine = (t & 4) == 4 * h && t >= 0 && t < kStrip && row < n_rows ? (t >> 3) * 4 + (t & 3) : -1;
+                    const int mine = (t >> 2 & 3) == g && t >= 0 && t < kStrip ? (t >> 4) * 4 + (t & 3) : -1;
+                    float found = z[0];
 #pragma unroll
-                    for (int j = 0; j < 64; ++j)
-                        if (j == mine) p.z_target[row] = z[j];
+                    for (int j = 1; j < 32; ++j) found = j == mine ? z[j] : found;
+                    if (mine >= 0) p.z_target[row] = found;
                 }
-                float sum[4] = {};
 #pragma unroll
-                for (int j = 0; j < 64; ++j) sum[j & 3] += fast_exp2(z[j] * kLog2e - shift);
-                sum[0] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                sum[0] += __shfl_xor(sum[0], 32);
-                if (h == 0) p.strips[(int64_t)strip * p.Tp + row] = make_float2(most[0], sum[0]);
+                for (int j = 0; j < 32; ++j) b[j & 1] += fast_exp2(z[j] * kLog2e - shift);
+                sum[y] = b[0] + b[1];
+                asm volatile("" : "+v"(most[y]), "+v"(sum[y]));   // (formed here, not for all y at the end, with all logits in registers)
             }
+            SB();
+#pragma unroll
+            for (int y = 0; y < 8; ++y) {
+                const float all = fmaxf(fmaxf(most[y], __shfl_xor(most[y], 16)), fmaxf(__shfl_xor(most[y], 32), __shfl_xor(most[y], 48)));
+                sum[y] *= fast_exp2((shift_of(most[y]) - shift_of(all)) * kLog2e);
+                most[y] = all;
+            }
+#pragma unroll
+            for (int y = 0; y < 8; ++y) sum[y] += __shfl_xor(sum[y], 16);
+#pragma unroll
+            for (int y = 0; y < 8; ++y) sum[y] += __shfl_xor(sum[y], 32);
+            float2 *out = p.strips + (int64_t)strip * p.Tp + nn * kTile + wn * 128 + n;
+#pragma unroll
+            for (int y = 0; y < 8; ++y)
+                if (g == (y & 3)) out[y * 16] = make_float2(most[y], sum[y]);
         } else if (K == kAgain) {
             const int word0 = m * kTile + wm * kStrip;   // of the piece
-            const int words = p.V - p.v0 - word0 - 4 * h;
+            const int words = p.V - p.v0 - word0 - 4 * g;
             const bool whole = p.v0 + word0 + kStrip <= p.V;
 #pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                const int in_tile = wn * 128 + y * 32 + n, row = nn * kTile + in_tile;
+            for (int y = 0; y < 8; ++y) {
+                const int in_tile = wn * 128 + y * 16 + n, row = nn * kTile + in_tile;
                 const float lse = row_lse[in_tile] * kLog2e, d = row_d[in_tile];
                 const int t = row_targets[in_tile] - p.v0 - word0;
                 const bool hit = __any(t >= 0 && t < kStrip);
-                const int mine = (t & 4) == 4 * h && t >= 0 && t < kStrip ? (t >> 3) * 4 + (t & 3) : -1;
-                uint16_t *out = p.dz + (int64_t)row * p.zp + word0 + 8 * h;
+                const int mine = (t >> 2 & 3) == g && t >= 0 && t < kStrip ? (t >> 4) * 4 + (t & 3) : -1;
+                uint16_t *out = p.dz + (int64_t)row * p.zp + word0 + 16 * (g & 1) + 8 * (g >> 1);
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
+                for (int x = 0; x < 8; x += 2) {
                     SB();
-                    float e[16];
+                    float e[8];   // of two blocks
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) e[v] = fast_exp2(result(acc[x][y][v]) * kLog2e - lse);
+                    for (int v = 0; v < 8; ++v) e[v] = fast_exp2(result(acc[x + (v >> 2)][y][v & 3]) * kLog2e - lse);
                     if (hit) {
 #pragma unroll
-                        for (int v = 0; v < 16; ++v)
-                            if (16 * x + v == mine) e[v] -= 1.0f;
+                        for (int v = 0; v < 8; ++v)
+                            if (4 * x + v == mine) e[v] -= 1.0f;
                     }
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) e[v] *= d;
+                    for (int v = 0; v < 8; ++v) e[v] *= d;
                     if (!whole) {
 #pragma unroll
-                        for (int v = 0; v < 16; ++v)
-                            if (32 * x + 8 * (v >> 2) + (v & 3) >= words) e[v] = 0.0f;
+                        for (int v = 0; v < 8; ++v)
+                            if (16 * (x + (v >> 2)) + (v & 3) >= words) e[v] = 0.0f;
                     }
-                    *(uint4 *)(out + x * 32) = eight_of(e);
-                    *(uint4 *)(out + x * 32 + 16) = eight_of(e + 8);
+                    *(uint4 *)(out + x * 16) = eight_of(e, e + 4);
                 }
             }
         } else if (K == kDx) {
-            float *out = p.slabs + ((int64_t)(s * work.mt + m) * kTile + wm * 128) * p.Hp + nn * kTile + wn * 128;   // (the same for all lanes)
+            float *out = p.slabs + ((int64_t)(s * work.nt + nn) * kTile + wn * 128) * p.Hp + m * kTile + wm * 128;   // (the same for all lanes)
+            const int cols = p.H - m * kTile - wm * 128;
 #pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                if (nn * kTile + wn * 128 + y * 32 + n < p.H) {
-                    const uint32_t mine = 4 * h * p.Hp + y * 32 + n;
+            for (int y = 0; y < 8; ++y) {
+                float *row = out + y * 16 * p.Hp;
+                const uint32_t mine = n * p.Hp + 4 * g;
 #pragma unroll
-                    for (int x = 0; x < 4; ++x)
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            SB();
-                            float *rows = out + (x * 32 + 8 * g) * p.Hp;
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) {
-                                float *to = rows + r * p.Hp + mine, f = result(acc[x][y][4 * g + r]);
-                                *to = p.first ? f : *to + f;
-                            }
+                for (int x = 0; x < 8; ++x) {
+                    SB();
+                    if (x * 16 + 4 * g < cols) {   // (a whole number of fours)
+                        float4 *to = (float4 *)(row + x * 16 + mine);
+                        float4 f = make_float4(result(acc[x][y][0]), result(acc[x][y][1]), result(acc[x][y][2]), result(acc[x][y][3]));
+                        if (!p.first) {
+                            const float4 old = *to;
+                            f.x += old.x; f.y += old.y; f.z += old.z; f.w += old.w;
                         }
+                        *to = f;
+                    }
                 }
             }
         } else {
-            const int col0 = m * kTile + wm * 128 + 8 * h;
+            const int col0 = m * kTile + wm * 128 + 16 * (g & 1) + 8 * (g >> 1);
 #pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                const int word = p.v0 + nn * kTile + wn * 128 + y * 32 + n;
+            for (int y = 0; y < 8; ++y) {
+                const int word = p.v0 + nn * kTile + wn * 128 + y * 16 + n;
                 uint16_t *out = p.dw + (int64_t)word * p.H + col0;
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
+                for (int x = 0; x < 8; x += 2) {
                     SB();
-                    float e[16];
+                    float e[8];
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) e[v] = result(acc[x][y][v]);
-                    const uint4 lo = eight_of(e), hi = eight_of(e + 8);
-                    if (word < p.V && col0 + x * 32 < p.H) *(uint4 *)(out + x * 32) = lo;
-                    if (word < p.V && col0 + x * 32 + 16 < p.H) *(uint4 *)(out + x * 32 + 16) = hi;
+                    for (int v = 0; v < 8; ++v) e[v] = result(acc[x + (v >> 2)][y][v & 3]);
+                    const uint4 u = eight_of(e, e + 4);
+                    if (word < p.V && col0 + x * 16 < p.H) *(uint4 *)(out + x * 16) = u;
                 }
             }
         }
@@ -587,8 +616,7 @@ __global__ __launch_bounds__(1024) void loss_sums_kernel(const float2 *strips, i
     __shared__ float2 part[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = blockIdx.x * 64 + lane, n = *n_rows;
     if ((int)blockIdx.x * 64 >= n) return;
-    // largest logit and the sum of exponentials relative to it (0 where that is not finite)
-    auto shift_of = [](float most) { return fabsf(most) < INFINITY ? most : 0.0f; };
+    // largest logit and the sum of exponentials relative to it
     auto add = [&](float &most, float &sum, float2 b) {
         const float m = fmaxf(most, b.x), s = shift_of(m);
         sum = sum * fast_exp2((shift_of(most) - s) * kLog2e) + b.y * fast_exp2((shift_of(b.x) - s) * kLog2e);
