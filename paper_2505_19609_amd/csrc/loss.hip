@@ -216,6 +216,13 @@ __device__ __forceinline__ uint4 eight_of(const float *first, const float *secon
     const u32x2 b = __builtin_amdgcn_permlane16_swap(pack_bf16(first[2], first[3]), pack_bf16(second[2], second[3]), false, false);
     return make_uint4(a[0], b[0], a[1], b[1]);
 }
+// `x`, of which the compiler does not know that it is the same everywhere.  (What a seldom taken branch works out of it is worked out there then, and
+// not ahead of them all.)
+__device__ __forceinline__ int here(int x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
 template <Kind K>
@@ -337,46 +344,47 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
         for (int step = 0; step < steps; ++step) {
             const unsigned char *t = lds + at, *next = lds + (at ^ kBufferBytes);
             const Fetch f = take(cursor);
-            // product j of a quarter: half step j / 16, blocks j / 4 % 4 and j % 4; between two of them at most one read or load, i = j / 2
+            // product j of a quarter: blocks j / 8 and j / 2 % 4, half step j % 2 (two products in a row on one accumulator need less power: 1.7 % of the
+            // time against j / 16 for the half step); between pairs of them at most one read or load, i = j / 2
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
-                const int k = j >> 4, x = j >> 2 & 3, y = j & 3, i = j >> 1;
+                const int k = j & 1, x = j >> 3 & 3, y = j >> 1 & 3, i = j >> 1;
                 acc[x][y] = mfma16(a0[x][k], b0[y][k], acc[x][y]);
                 SB();
                 if (j & 1) continue;
-                if (i < 8) b1[i & 3][i >> 2] = B.get(t + kOperandBytes, 1, i & 3, i >> 2);
+                if (i < 8) b1[i >> 1][i & 1] = B.get(t + kOperandBytes, 1, i >> 1, i & 1);
                 else if (i & 1) load_b(f, 0, i - 8 >> 1);
                 else load_a(f, 0, i - 8 >> 1);
                 SB();
             }
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
-                const int k = j >> 4, x = j >> 2 & 3, y = j & 3, i = j >> 1;
+                const int k = j & 1, x = j >> 3 & 3, y = j >> 1 & 3, i = j >> 1;
                 acc[x][4 + y] = mfma16(a0[x][k], b1[y][k], acc[x][4 + y]);
                 SB();
                 if (j & 1) continue;
-                if (i < 8) a1[i & 3][i >> 2] = A.get(t, 1, i & 3, i >> 2);
+                if (i < 8) a1[i >> 1][i & 1] = A.get(t, 1, i >> 1, i & 1);
                 SB();
             }
             half_end();
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
-                const int k = j >> 4, x = j >> 2 & 3, y = j & 3, i = j >> 1;
+                const int k = j & 1, x = j >> 3 & 3, y = j >> 1 & 3, i = j >> 1;
                 acc[4 + x][y] = mfma16(a1[x][k], b0[y][k], acc[4 + x][y]);
                 SB();
                 if (j & 1) continue;
-                if (i < 8) a0[i & 3][i >> 2] = A.get(next, 0, i & 3, i >> 2);
+                if (i < 8) a0[i >> 1][i & 1] = A.get(next, 0, i >> 1, i & 1);
                 else if (i & 1) load_a(f, 1, i - 8 >> 1);
                 else load_b(f, 1, i - 8 >> 1);
                 SB();
             }
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
-                const int k = j >> 4, x = j >> 2 & 3, y = j & 3, i = j >> 1;
+                const int k = j & 1, x = j >> 3 & 3, y = j >> 1 & 3, i = j >> 1;
                 acc[4 + x][4 + y] = mfma16(a1[x][k], b1[y][k], acc[4 + x][4 + y]);
                 SB();
                 if (j & 1) continue;
-                if (i < 8) b0[i & 3][i >> 2] = B.get(next + kOperandBytes, 0, i & 3, i >> 2);
+                if (i < 8) b0[i >> 1][i & 1] = B.get(next + kOperandBytes, 0, i >> 1, i & 1);
                 SB();
             }
             half_end();
@@ -399,11 +407,12 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
 #pragma unroll
                 for (int j = 0; j < 32; ++j) z[j] = result(acc[j >> 2][y][j & 3]);
                 if (!whole) {
+                    const int left = here(words);
 #pragma unroll
                     for (int j = 0; j < 32; ++j)
-                        if (16 * (j >> 2) + (j & 3) >= words) z[j] = -INFINITY;
+                        if (16 * (j >> 2) + (j & 3) >= left) z[j] = -INFINITY;
                 }
-                float a[2] = {z[0], z[1]}, b[2] = {};
+                float a[2] = {z[0], z[1]}, b[8];
 #pragma unroll
                 for (int j = 2; j < 32; ++j) a[j & 1] = fmaxf(a[j & 1], z[j]);
                 most[y] = fmaxf(a[0], a[1]);
@@ -417,8 +426,15 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
                     if (mine >= 0) p.z_target[row] = found;
                 }
 #pragma unroll
-                for (int j = 0; j < 32; ++j) b[j & 1] += fast_exp2(z[j] * kLog2e - shift);
-                sum[y] = b[0] + b[1];
+                for (int i = 0; i < 4; ++i) {   // (eight at a time: an exponential's result is not ready for the next instruction)
+                    float e[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) e[j] = fast_exp2(z[8 * i + j] * kLog2e - shift);
+                    SB();
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) b[j] = i == 0 ? e[j] : b[j] + e[j];
+                }
+                sum[y] = ((b[0] + b[1]) + (b[2] + b[3])) + ((b[4] + b[5]) + (b[6] + b[7]));
                 asm volatile("" : "+v"(most[y]), "+v"(sum[y]));   // (formed here, not for all y at the end, with all logits in registers)
             }
             SB();
@@ -455,16 +471,18 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
 #pragma unroll
                     for (int v = 0; v < 8; ++v) e[v] = fast_exp2(result(acc[x + (v >> 2)][y][v & 3]) * kLog2e - lse);
                     if (hit) {
+                        const int at = here(mine) - 4 * x;
 #pragma unroll
                         for (int v = 0; v < 8; ++v)
-                            if (4 * x + v == mine) e[v] -= 1.0f;
+                            if (v == at) e[v] -= 1.0f;
                     }
 #pragma unroll
                     for (int v = 0; v < 8; ++v) e[v] *= d;
                     if (!whole) {
+                        const int left = here(words) - 16 * x;
 #pragma unroll
                         for (int v = 0; v < 8; ++v)
-                            if (16 * (x + (v >> 2)) + (v & 3) >= words) e[v] = 0.0f;
+                            if (16 * (v >> 2) + (v & 3) >= left) e[v] = 0.0f;
                     }
                     *(uint4 *)(out + x * 16) = eight_of(e, e + 4);
                 }
