@@ -52,10 +52,9 @@ struct LossArgs {
     float2 *strips;          // [strips][Tp] (kForward)
     float *slabs;            // [splits][rows][Hp] (kDx)
     uint16_t *dw;            // [V, H] (kDw)
-    int64_t Tp;
-    int32_t V, H, Hp, v0, vc;
-    int32_t xp, zp;          // elements between rows of x and of dz
-    int32_t first;           // kDx: the first piece (slabs are written, not added to)
+    int64_t Tp, dz_room;
+    int32_t V, H, Hp, xp;    // xp: elements between rows of x
+    int32_t piece;           // of the vocabulary, backward
 };
 
 // How many parts the vocabulary of a piece is cut into for dX, so that all compute units have a tile: the partial sums are slabs
@@ -65,6 +64,36 @@ __host__ __device__ inline int dx_splits(int tiles, int steps)
     const int s = kGrid / tiles;
     return s < 1 ? 1 : s > steps ? steps : s;
 }
+
+__host__ __device__ inline int row_tiles_of(int64_t rows) { return rows > 0 ? (int)((rows + kTile - 1) / kTile) : 1; }
+
+// The pieces that the backward takes the vocabulary in: as few as the room for dz (in elements) allows for the rows there are, of equal
+// size, or of one that gives dW fewer rounds of tiles on all compute units together.
+struct Piece {
+    int tiles, pitch;   // tiles of 256 words of a piece (the last one may have fewer); elements between rows of dz
+    int most_pieces;    // with these rows or fewer
+    __host__ __device__ Piece(int row_tiles, int V, int H, int64_t room)
+    {
+        const int words = (V + kTile - 1) / kTile, h_tiles = (H + kTile - 1) / kTile;
+        int64_t most = (room / ((int64_t)row_tiles * kTile) - kPitchPad) / kTile;
+        most = most < 1 ? 1 : most > kMaxPieceWords / kTile ? kMaxPieceWords / kTile : most;
+        const int count = (int)((words + most - 1) / most);
+        tiles = (words + count - 1) / count;
+        most_pieces = count;
+        int whole = kGrid;   // tiles that make whole rounds
+        for (int h = h_tiles; whole > 1 && h % 2 == 0; h /= 2) whole /= 2;
+        if (count > 1 && most >= whole) {
+            const int other = (int)(most / whole * whole);
+            if ((words + other - 1) / other <= most_pieces && rounds(words, other, h_tiles) < rounds(words, tiles, h_tiles)) tiles = other;
+        }
+        pitch = tiles * kTile + (tiles % 8 == 0 ? kPitchPad : 0);
+    }
+    __host__ __device__ static int rounds(int words, int tiles, int h_tiles)
+    {
+        const int rest = words % tiles;
+        return words / tiles * ((tiles * h_tiles + kGrid - 1) / kGrid) + (rest * h_tiles + kGrid - 1) / kGrid;
+    }
+};
 
 // Where an operand's step lies and how much of its matrix is behind that address.
 struct Source {
@@ -144,26 +173,37 @@ struct Operand {
 template <Kind K>
 struct Product {
     int mt, nt, splits, steps, total;   // tiles of M and N; parts of the contraction, steps of a part
+    int v0, zp, all_steps;              // first word of the piece; elements between rows of dz; kDx: steps of all parts
 
     __device__ __forceinline__ void init(const LossArgs &p, int n_rows)
     {
-        const int row_tiles = max(1, (n_rows + kTile - 1) / kTile), h_tiles = (p.H + kTile - 1) / kTile;
+        const int row_tiles = row_tiles_of(n_rows), h_tiles = (p.H + kTile - 1) / kTile, words = (p.V + kTile - 1) / kTile;
         splits = 1;
+        v0 = zp = all_steps = 0;
+        int piece_tiles = words;
+        if (K != kForward) {
+            const Piece piece(row_tiles, p.V, p.H, p.dz_room);
+            zp = piece.pitch;
+            v0 = p.piece * piece.tiles * kTile;
+            piece_tiles = max(0, min(piece.tiles, words - p.piece * piece.tiles));   // (no tile: there are fewer pieces than launches)
+            splits = K == kDx ? dx_splits(h_tiles * row_tiles, piece.tiles * (kTile / kStep)) : 1;
+        }
         if (K == kForward || K == kAgain) {
-            mt = K == kForward ? (p.V + kTile - 1) / kTile : p.vc / kTile;
+            mt = piece_tiles;
             nt = row_tiles;
             steps = p.Hp / kStep;
         } else if (K == kDx) {
-            mt = h_tiles;
+            mt = piece_tiles ? h_tiles : 0;
             nt = row_tiles;
-            splits = dx_splits(mt * nt, p.vc / kStep);
-            steps = (p.vc / kStep + splits - 1) / splits;
+            all_steps = piece_tiles * (kTile / kStep);
+            steps = (all_steps + splits - 1) / splits;
         } else {
             mt = h_tiles;
-            nt = p.vc / kTile;
+            nt = piece_tiles;
             steps = max(1, (n_rows + kStep - 1) / kStep);
         }
         total = mt * nt * splits;
+        for (int *f : {&mt, &nt, &splits, &steps, &total, &v0, &zp, &all_steps}) *f = __builtin_amdgcn_readfirstlane(*f);   // (quotients come from vector instructions)
     }
     // Tiles in the order of work: blocks of 8 tiles of M, through all of N.  Neighbours in it run at the same time on one die, 8 x 4 tiles
     // that share their operands in its L2.
@@ -174,22 +214,23 @@ struct Product {
         const int block = i / (8 * nt), r = i - block * (8 * nt), width = min(8, mt - block * 8);
         n = r / width;
         m = block * 8 + r - n * width;
+        for (int *f : {&m, &n, &s}) *f = __builtin_amdgcn_readfirstlane(*f);
     }
     // steps of part s (the last one may have fewer, or none)
-    __device__ __forceinline__ int steps_of(const LossArgs &p, int s) const
+    __device__ __forceinline__ int steps_of(int s) const
     {
-        return K == kDx ? max(0, min(steps, p.vc / kStep - s * steps)) : steps;
+        return K == kDx ? max(0, min(steps, all_steps - s * steps)) : steps;
     }
     __device__ __forceinline__ void sources(const LossArgs &p, int m, int n, int s, Source &a, Source &b) const
     {
-        const int64_t H2 = (int64_t)p.H * 2, xp2 = (int64_t)p.xp * 2, zp2 = (int64_t)p.zp * 2;
+        const int64_t H2 = (int64_t)p.H * 2, xp2 = (int64_t)p.xp * 2, zp2 = (int64_t)zp * 2;
         if (K == kForward || K == kAgain) {
-            const int64_t v = p.v0 + (int64_t)m * kTile;
+            const int64_t v = v0 + (int64_t)m * kTile;
             a = Source{(const unsigned char *)p.w + v * H2, min((int64_t)kTile, p.V - v) * H2, (uint32_t)H2, kStep * 2};
             b = Source{(const unsigned char *)p.x + (int64_t)n * kTile * xp2, kTile * xp2, (uint32_t)xp2, kStep * 2};
         } else if (K == kDx) {
             const int64_t k0 = (int64_t)s * steps * kStep;
-            a = Source{(const unsigned char *)p.w + (p.v0 + k0) * H2 + m * kTile * 2, (p.V - p.v0 - k0) * H2 - m * kTile * 2, (uint32_t)H2, kStep * H2};
+            a = Source{(const unsigned char *)p.w + (v0 + k0) * H2 + m * kTile * 2, (p.V - v0 - k0) * H2 - m * kTile * 2, (uint32_t)H2, kStep * H2};
             b = Source{(const unsigned char *)p.dz + (int64_t)n * kTile * zp2 + k0 * 2, kTile * zp2 - k0 * 2, (uint32_t)zp2, kStep * 2};
         } else {
             const int64_t rows = (int64_t)steps * kStep;
@@ -239,7 +280,7 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
     Product<K> work;
     work.init(p, n_rows);
 
-    const uint32_t a_pitch = (uint32_t)(K == kDw ? p.xp : p.H) * 2, b_pitch = (uint32_t)(K == kDx || K == kDw ? p.zp : p.xp) * 2;
+    const uint32_t a_pitch = (uint32_t)(K == kDw ? p.xp : p.H) * 2, b_pitch = (uint32_t)(K == kDx || K == kDw ? work.zp : p.xp) * 2;
     Operand<A_COLS> A;
     Operand<B_COLS> B;
     A.init(lane, wave, wm, a_pitch);
@@ -263,7 +304,7 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
         while (c.left == 0 && c.tile < end) {
             int m, nn, s;
             work.locate(c.tile, m, nn, s);
-            c.left = work.steps_of(p, s);
+            c.left = work.steps_of(s);
             work.sources(p, m, nn, s, c.a, c.b);
             c.tail = K == kForward || K == kAgain ? p.H : 0x7fffffff;   // elements of the contraction
             c.tile += stride;
@@ -323,7 +364,7 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
     for (int i = begin; i < end; i += stride) {
         int m, nn, s;
         work.locate(i, m, nn, s);
-        const int steps = work.steps_of(p, s);
+        const int steps = work.steps_of(s);
         if (K == kForward || K == kAgain) {
             const int row0 = nn * kTile + wave * 64;   // (older than a step's 16 loads: there when the first one ends)
             dma_b32(rsrc_words(p.target + row0, 256), lds0 + row_at + wave * 256, lane * 4, 0);
@@ -454,16 +495,16 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
                 if (g == (y & 3)) out[y * 16] = make_float2(most[y], sum[y]);
         } else if (K == kAgain) {
             const int word0 = m * kTile + wm * kStrip;   // of the piece
-            const int words = p.V - p.v0 - word0 - 4 * g;
-            const bool whole = p.v0 + word0 + kStrip <= p.V;
+            const int words = p.V - work.v0 - word0 - 4 * g;
+            const bool whole = work.v0 + word0 + kStrip <= p.V;
 #pragma unroll
             for (int y = 0; y < 8; ++y) {
                 const int in_tile = wn * 128 + y * 16 + n, row = nn * kTile + in_tile;
                 const float lse = row_lse[in_tile] * kLog2e, d = row_d[in_tile];
-                const int t = row_targets[in_tile] - p.v0 - word0;
+                const int t = row_targets[in_tile] - work.v0 - word0;
                 const bool hit = __any(t >= 0 && t < kStrip);
                 const int mine = (t >> 2 & 3) == g && t >= 0 && t < kStrip ? (t >> 4) * 4 + (t & 3) : -1;
-                uint16_t *out = p.dz + (int64_t)row * p.zp + word0 + 16 * (g & 1) + 8 * (g >> 1);
+                uint16_t *out = p.dz + (int64_t)row * work.zp + word0 + 16 * (g & 1) + 8 * (g >> 1);
 #pragma unroll
                 for (int x = 0; x < 8; x += 2) {
                     SB();
@@ -500,7 +541,7 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
                     if (x * 16 + 4 * g < cols) {   // (a whole number of fours)
                         float4 *to = (float4 *)(row + x * 16 + mine);
                         float4 f = make_float4(result(acc[x][y][0]), result(acc[x][y][1]), result(acc[x][y][2]), result(acc[x][y][3]));
-                        if (!p.first) {
+                        if (p.piece > 0) {
                             const float4 old = *to;
                             f.x += old.x; f.y += old.y; f.z += old.z; f.w += old.w;
                         }
@@ -512,7 +553,7 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
             const int col0 = m * kTile + wm * 128 + 16 * (g & 1) + 8 * (g >> 1);
 #pragma unroll
             for (int y = 0; y < 8; ++y) {
-                const int word = p.v0 + nn * kTile + wn * 128 + y * 16 + n;
+                const int word = work.v0 + nn * kTile + wn * 128 + y * 16 + n;
                 uint16_t *out = p.dw + (int64_t)word * p.H + col0;
 #pragma unroll
                 for (int x = 0; x < 8; x += 2) {
@@ -529,126 +570,134 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
     wait_vmem();   // (no load to LDS outlives the workgroup)
 }
 
-// Which rows have a target, in order: one workgroup, 8 rows to a thread at a time.
-struct RowsArgs {
+// X: the rows that have a target, in order, then zeros to a whole tile; and what else the products need of them.  A workgroup has `each` rows; how many
+// of those before them have a target it counts itself, 8 bytes a row that lie in the L2 (16,384 rows, 896 hidden: rows
+// and copies 12 us; with one workgroup for the rows and a launch of its own for the copies 36).
+struct GatherArgs {
+    const uint16_t *x;
+    int64_t x_stride;
     const int64_t *target;   // [T]
     const float *lse, *d;    // [T], backward
     int64_t T;
-    int32_t V;
+    int32_t V, H, Hp, xp, each, wide;
     int32_t *n_rows, *slot, *row, *target_of;  // count; [T] gathered row or -1; [Tp] its row; [Tp] its target
+    uint16_t *out;           // [Tp][xp]
     float *lse_of, *d_of;    // [Tp], backward
     float *loss, *lse_out;   // [T], forward: zeros where there is no target
     float *z_target;         // [Tp], forward: NaN until the product finds the target's word
 };
+constexpr int kGatherWaves = 16;
 template <bool BACKWARD>
-__global__ __launch_bounds__(1024) void loss_rows_kernel(const RowsArgs a)
+__global__ __launch_bounds__(64 * kGatherWaves) void loss_gather_kernel(const GatherArgs a)
 {
-    constexpr int EACH = 8;
-    __shared__ int counts[16];
-    __shared__ int before;
+    __shared__ int counts[2][kGatherWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (threadIdx.x == 0) before = 0;
+    const int64_t first = (int64_t)blockIdx.x * a.each, end = min(a.T, first + a.each);
+    int before = 0, n = 0;
+#pragma unroll 8
+    for (int64_t t = threadIdx.x; t < a.T; t += 64 * kGatherWaves) {
+        const int has = a.target[t] >= 0;
+        n += has;
+        before += t < first ? has : 0;
+    }
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) {
+        n += __shfl_xor(n, m);
+        before += __shfl_xor(before, m);
+    }
+    if (lane == 0) {
+        counts[0][wave] = before;
+        counts[1][wave] = n;
+    }
     __syncthreads();
-    for (int64_t base = 0; base < a.T; base += 1024 * EACH) {
-        const int64_t t0 = base + threadIdx.x * EACH;
-        int64_t target[EACH];
-        int mine = 0;
+    int at = 0;
+    n = 0;
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            target[i] = t0 + i < a.T ? a.target[t0 + i] : -1;
-            mine += target[i] >= 0;
-        }
-        int upto = mine;   // of this thread and those before it in the wavefront
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) {
-            const int o = __shfl_up(upto, m);
-            if (lane >= m) upto += o;
-        }
-        if (lane == 63) counts[wave] = upto;
-        __syncthreads();
-        int at = before + upto - mine;
-#pragma unroll
-        for (int k = 0; k < 16; ++k) at += k < wave ? counts[k] : 0;
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const int64_t t = t0 + i;
-            if (t >= a.T) break;
-            if (target[i] < 0) {
-                a.slot[t] = -1;
-                if (!BACKWARD) { a.loss[t] = 0.0f; a.lse_out[t] = 0.0f; }
-                continue;
-            }
-            const bool outside = target[i] >= a.V;
-            a.slot[t] = at;
-            a.row[at] = (int32_t)t;
-            a.target_of[at] = outside ? -1 : (int32_t)target[i];
-            if (BACKWARD) {
-                a.lse_of[at] = a.lse[t];
-                a.d_of[at] = outside ? NAN : a.d[t];
-            } else {
-                a.z_target[at] = NAN;
-            }
-            ++at;
-        }
-        __syncthreads();
-        if (threadIdx.x == 1023) before = at;
-        __syncthreads();
+    for (int k = 0; k < kGatherWaves; ++k) {
+        at += counts[0][k];
+        n += counts[1][k];
     }
-    const int n = before, padded = max(1, (n + kTile - 1) / kTile) * kTile;
-    if (threadIdx.x == 0) *a.n_rows = n;
-    for (int i = n + threadIdx.x; i < padded; i += 1024) {   // rows that fill the last tile: no gradient, no word
-        a.target_of[i] = -1;
-        if (BACKWARD) { a.lse_of[i] = 0.0f; a.d_of[i] = 0.0f; }
-    }
-}
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.n_rows = n;
 
-// X: the gathered rows, padded with zeros.
-__global__ __launch_bounds__(256) void loss_gather_kernel(const uint16_t *x, int64_t x_stride, int wide, const int32_t *n_rows, const int32_t *row,
-                                                          uint16_t *out, int H, int Hp, int xp)
-{
-    const int n = *n_rows, padded = max(1, (n + kTile - 1) / kTile) * kTile;
-    for (int r = blockIdx.x; r < padded; r += gridDim.x) {
-        const uint16_t *in = r < n ? x + (int64_t)row[r] * x_stride : nullptr;
-        uint16_t *to = out + (int64_t)r * xp;
-        for (int c = threadIdx.x * 8; c < Hp; c += 256 * 8) {
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (in && c < H) {
-                if (wide) {
-                    v = *(const uint4 *)(in + c);
+    for (int64_t t0 = first; t0 < end; t0 += 64) {
+        const int64_t t = t0 + lane, target = t < end ? a.target[t] : -1;
+        const uint64_t has = __ballot(target >= 0);
+        if (wave == 0 && t < end) {
+            const int s = at + __popcll(has & (((uint64_t)1 << lane) - 1));
+            a.slot[t] = target >= 0 ? s : -1;
+            if (target >= 0) {
+                const bool outside = target >= a.V;
+                a.row[s] = (int32_t)t;
+                a.target_of[s] = outside ? -1 : (int32_t)target;
+                if (BACKWARD) {
+                    a.lse_of[s] = a.lse[t];
+                    a.d_of[s] = outside ? NAN : a.d[t];
                 } else {
-                    uint16_t e[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) e[i] = in[c + i];
-                    v = make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
+                    a.z_target[s] = NAN;
                 }
+            } else if (!BACKWARD) {
+                a.loss[t] = 0.0f;
+                a.lse_out[t] = 0.0f;
             }
-            *(uint4 *)(to + c) = v;
+        }
+        for (int i = wave; i < 64; i += kGatherWaves) {
+            if (!(has >> i & 1)) continue;
+            const uint16_t *in = a.x + (t0 + i) * a.x_stride;
+            uint16_t *to = a.out + (int64_t)(at + __popcll(has & (((uint64_t)1 << i) - 1))) * a.xp;
+#pragma unroll 4
+            for (int c = lane * 8; c < a.Hp; c += 64 * 8) {
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (c < a.H) {
+                    if (a.wide) {
+                        v = *(const uint4 *)(in + c);
+                    } else {
+                        uint16_t e[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) e[k] = in[c + k];
+                        v = make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
+                    }
+                }
+                *(uint4 *)(to + c) = v;
+            }
+        }
+        at += __popcll(has);
+    }
+    const int padded = row_tiles_of(n) * kTile;
+    for (int r = n + blockIdx.x; r < padded; r += gridDim.x) {   // rows that fill the last tile: no gradient, no word
+        for (int c = threadIdx.x * 8; c < a.Hp; c += 64 * kGatherWaves * 8) *(uint4 *)(a.out + (int64_t)r * a.xp + c) = make_uint4(0, 0, 0, 0);
+        if (threadIdx.x == 0) {
+            a.target_of[r] = -1;
+            if (BACKWARD) { a.lse_of[r] = 0.0f; a.d_of[r] = 0.0f; }
         }
     }
 }
 
-// lse and loss from the strips: 64 rows to a workgroup, 16 wavefronts share the strips.
+// lse and loss from the strips: 16 rows to a workgroup, 64 lanes of a row share its strips.
+constexpr int kSumRows = 16;
 __global__ __launch_bounds__(1024) void loss_sums_kernel(const float2 *strips, int n_strips, int64_t Tp, const int32_t *n_rows, const int32_t *row,
                                                          const float *z_target, float *loss, float *lse)
 {
-    __shared__ float2 part[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = blockIdx.x * 64 + lane, n = *n_rows;
-    if ((int)blockIdx.x * 64 >= n) return;
+    __shared__ float2 part[64][kSumRows + 1];
+    const int i = threadIdx.x % kSumRows, share = threadIdx.x / kSumRows, r0 = blockIdx.x * kSumRows, n = *n_rows;
+    if (r0 >= n) return;
     // largest logit and the sum of exponentials relative to it
-    auto add = [&](float &most, float &sum, float2 b) {
-        const float m = fmaxf(most, b.x), s = shift_of(m);
-        sum = sum * fast_exp2((shift_of(most) - s) * kLog2e) + b.y * fast_exp2((shift_of(b.x) - s) * kLog2e);
-        most = m;
+    auto add = [&](float2 &a, float2 b) {
+        const float m = fmaxf(a.x, b.x), s = shift_of(m);
+        a.y = a.y * fast_exp2((shift_of(a.x) - s) * kLog2e) + b.y * fast_exp2((shift_of(b.x) - s) * kLog2e);
+        a.x = m;
     };
-    float most = -INFINITY, sum = 0.0f;
-#pragma unroll 4
-    for (int i = wave; i < n_strips; i += 16) add(most, sum, strips[(int64_t)i * Tp + r]);   // (r is within the padded rows)
-    part[wave][lane] = make_float2(most, sum);
+    float2 sum = make_float2(-INFINITY, 0.0f);
+#pragma unroll 8
+    for (int k = share; k < n_strips; k += 64) add(sum, strips[k * Tp + r0 + i]);   // (within the padded rows)
+    part[share][i] = sum;
     __syncthreads();
-    if (wave == 0 && r < n) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;   // a wavefront to a row
+    sum = part[lane][wave];
 #pragma unroll
-        for (int k = 1; k < 16; ++k) add(most, sum, part[k][lane]);
-        const float l = shift_of(most) + logf(sum);
+    for (int m = 32; m >= 1; m >>= 1) add(sum, make_float2(__shfl_xor(sum.x, m), __shfl_xor(sum.y, m)));
+    const int r = r0 + wave;
+    if (lane == 0 && r < n) {
+        const float l = shift_of(sum.x) + logf(sum.y);
         const int t = row[r];
         lse[t] = l;
         loss[t] = l - z_target[r];
@@ -656,56 +705,63 @@ __global__ __launch_bounds__(1024) void loss_sums_kernel(const float2 *strips, i
 }
 
 // dx of every row: the parts' sums, or zeros.
-__global__ __launch_bounds__(256) void loss_dx_kernel(const float *slabs, const int32_t *n_rows, const int32_t *slot, uint16_t *dx, int64_t T, int H, int Hp,
-                                                      int steps)
+__global__ __launch_bounds__(256) void loss_dx_kernel(const float *slabs, const int32_t *n_rows, const int32_t *slot, uint16_t *dx, int64_t T, int V, int H, int Hp,
+                                                      int64_t dz_room)
 {
-    const int tiles = max(1, (*n_rows + kTile - 1) / kTile), splits = dx_splits(tiles * ((H + kTile - 1) / kTile), steps);
+    const int tiles = row_tiles_of(*n_rows), splits = dx_splits(tiles * ((H + kTile - 1) / kTile), Piece(tiles, V, H, dz_room).tiles * (kTile / kStep));
     const int64_t slab = (int64_t)tiles * kTile * Hp;
-    for (int64_t t = blockIdx.x; t < T; t += gridDim.x) {
-        const int s = slot[t];
-        for (int c = threadIdx.x * 8; c < H; c += 256 * 8) {
-            float f[8] = {};
-            if (s >= 0) {
-                const float *from = slabs + (int64_t)s * Hp + c;
-                for (int k = 0; k < splits; ++k, from += slab) {
-                    const float4 u = ((const float4 *)from)[0], v = ((const float4 *)from)[1];
-                    f[0] += u.x; f[1] += u.y; f[2] += u.z; f[3] += u.w; f[4] += v.x; f[5] += v.y; f[6] += v.z; f[7] += v.w;
-                }
+    const int pieces = H / 4, blocks = (pieces + 255) / 256;   // 4 columns to a thread
+    for (int64_t i = blockIdx.x; i < T * blocks; i += gridDim.x) {
+        const int64_t t = i / blocks;
+        const int c = ((int)(i - t * blocks) * 256 + threadIdx.x) * 4, s = slot[t];
+        if (c >= H) continue;
+        float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (s >= 0) {
+            const float *from = slabs + (int64_t)s * Hp + c;
+            int k = 0;
+            for (; k + 8 <= splits; k += 8, from += 8 * slab) {
+                float4 u[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) u[j] = *(const float4 *)(from + j * slab);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) { f.x += u[j].x; f.y += u[j].y; f.z += u[j].z; f.w += u[j].w; }
             }
-            *(uint4 *)(dx + t * H + c) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+            for (; k < splits; ++k, from += slab) {
+                const float4 u = *(const float4 *)from;
+                f.x += u.x; f.y += u.y; f.z += u.z; f.w += u.w;
+            }
         }
+        *(uint2 *)(dx + t * H + c) = make_uint2(pack_bf16(f.x, f.y), pack_bf16(f.z, f.w));
     }
 }
 
 // The workspace, from sizes alone.
 struct Layout {
-    int64_t Tp, Hp, xp, vc, zp, pieces;
+    int64_t Tp, Hp, xp, dz_room, pieces;
     int64_t n_rows, slot, row, target, lse, d, z_target, x, strips, dz, slabs, bytes;
     Layout(const skrull_loss_t &p, bool backward)
     {
-        Tp = (p.rows + kTile - 1) / kTile * kTile;
-        if (Tp == 0) Tp = kTile;
+        const int64_t row_tiles = row_tiles_of(p.rows);
+        Tp = row_tiles * kTile;
         Hp = (p.hidden + kStep - 1) / kStep * kStep;
         xp = Hp * 2 % 4096 == 0 ? Hp + kPitchPad : Hp;
         const int64_t words = ((int64_t)p.vocab + kTile - 1) / kTile * kTile;
-        int64_t most = kPieceBytes / (Tp * 2) / kTile * kTile;
-        most = most < kTile ? kTile : most > kMaxPieceWords ? kMaxPieceWords : most;
-        pieces = (words + most - 1) / most;
-        vc = (words / kTile + pieces - 1) / pieces * kTile;
-        pieces = (words + vc - 1) / vc;
-        bytes = 0;
+        bytes = dz_room = pieces = 0;
         auto take = [&](int64_t n) { const int64_t at = bytes; bytes += (n + 255) & ~(int64_t)255; return at; };
         n_rows = take(4);
         slot = take(p.rows * 4);
         row = take(Tp * 4);
         target = take(Tp * 4);
         x = take(Tp * xp * 2);
-        lse = d = z_target = strips = dz = slabs = zp = 0;
+        lse = d = z_target = strips = dz = slabs = 0;
         if (backward) {
             lse = take(Tp * 4);
             d = take(Tp * 4);
-            zp = vc * 2 % 4096 == 0 ? vc + kPitchPad : vc;
-            dz = take(Tp * zp * 2);
+            // (one tile of the vocabulary at least, however many rows there are)
+            const int64_t all = Tp * ((words < kMaxPieceWords ? words : kMaxPieceWords) + kPitchPad), least = Tp * (kTile + kPitchPad);
+            dz_room = all < kPieceBytes / 2 ? all : kPieceBytes / 2 > least ? kPieceBytes / 2 : least;
+            pieces = Piece((int)row_tiles, p.vocab, p.hidden, dz_room).most_pieces;
+            dz = take(dz_room * 2);
             // (parts of the vocabulary are made only where there are fewer tiles than compute units)
             const int64_t h_tiles = (p.hidden + kTile - 1) / kTile, parted = kGrid / h_tiles * kTile;
             slabs = take((Tp > parted ? Tp : parted) * Hp * 4);
@@ -726,20 +782,19 @@ int check(const skrull_loss_t *p)
     return SKRULL_OK;
 }
 
-// Gathers the rows; the first two kernels of either direction.
+// The first kernel of either direction.
 template <bool BACKWARD>
 hipError_t gather(const skrull_loss_t &p, const Layout &l, unsigned char *ws, const void *x, const int64_t *target, const float *lse, const float *d,
                   float *loss, float *lse_out, hipStream_t st)
 {
-    RowsArgs a = {};
-    a.target = target; a.lse = lse; a.d = d; a.T = p.rows; a.V = p.vocab;
+    GatherArgs a = {};
+    a.x = (const uint16_t *)x; a.x_stride = p.x_stride; a.target = target; a.lse = lse; a.d = d; a.T = p.rows; a.V = p.vocab;
+    a.H = p.hidden; a.Hp = (int32_t)l.Hp; a.xp = (int32_t)l.xp; a.wide = aligned_to(x, 16) && p.x_stride % 8 == 0;
+    a.each = (int32_t)((p.rows + 511) / 512 < 4 ? 4 : (p.rows + 511) / 512);
     a.n_rows = (int32_t *)(ws + l.n_rows); a.slot = (int32_t *)(ws + l.slot); a.row = (int32_t *)(ws + l.row); a.target_of = (int32_t *)(ws + l.target);
-    a.lse_of = (float *)(ws + l.lse); a.d_of = (float *)(ws + l.d); a.loss = loss; a.lse_out = lse_out; a.z_target = (float *)(ws + l.z_target);
-    loss_rows_kernel<BACKWARD><<<1, 1024, 0, st>>>(a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    const int wide = aligned_to(x, 16) && p.x_stride % 8 == 0;
-    loss_gather_kernel<<<(int)(l.Tp < 2048 ? l.Tp : 2048), 256, 0, st>>>((const uint16_t *)x, p.x_stride, wide, a.n_rows, a.row, (uint16_t *)(ws + l.x), p.hidden, (int)l.Hp, (int)l.xp);
+    a.out = (uint16_t *)(ws + l.x); a.lse_of = (float *)(ws + l.lse); a.d_of = (float *)(ws + l.d); a.loss = loss; a.lse_out = lse_out; a.z_target = (float *)(ws + l.z_target);
+    const int64_t blocks = (p.rows + a.each - 1) / a.each;
+    loss_gather_kernel<BACKWARD><<<(int)(blocks < 1 ? 1 : blocks), 64 * kGatherWaves, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -783,7 +838,7 @@ int skrull_loss_fwd(const skrull_loss_t *p, const void *x, const void *w, const 
         loss_product_kernel<kForward><<<kGrid, 256, 0, st>>>(a);
         e = hipGetLastError();
         if (e == hipSuccess) {
-            loss_sums_kernel<<<(int)(l.Tp / 64), 1024, 0, st>>>(a.strips, (p->vocab + kTile - 1) / kTile * 2, l.Tp, a.n_rows, (const int32_t *)(ws + l.row), a.z_target, loss, lse);
+            loss_sums_kernel<<<(int)(l.Tp / kSumRows), 1024, 0, st>>>(a.strips, (p->vocab + kTile - 1) / kTile * 2, l.Tp, a.n_rows, (const int32_t *)(ws + l.row), a.z_target, loss, lse);
             e = hipGetLastError();
         }
     }
@@ -812,11 +867,9 @@ int skrull_loss_bwd(const skrull_loss_t *p, const void *x, const void *w, const 
     a.dz = (uint16_t *)(ws + l.dz);
     a.slabs = (float *)(ws + l.slabs);
     a.dw = (uint16_t *)dw;
-    a.vc = (int32_t)l.vc;
-    a.zp = (int32_t)l.zp;
-    for (int64_t i = 0; i < l.pieces && e == hipSuccess; ++i) {
-        a.v0 = (int32_t)(i * l.vc);
-        a.first = i == 0;
+    a.dz_room = l.dz_room;
+    for (int64_t i = 0; i < l.pieces && e == hipSuccess; ++i) {   // (there may be fewer pieces: the last launches find no tiles then)
+        a.piece = (int32_t)i;
         loss_product_kernel<kAgain><<<kGrid, 256, 0, st>>>(a);
         e = hipGetLastError();
         if (e == hipSuccess && dx) {
@@ -829,7 +882,8 @@ int skrull_loss_bwd(const skrull_loss_t *p, const void *x, const void *w, const 
         }
     }
     if (e == hipSuccess && dx && p->rows > 0) {
-        loss_dx_kernel<<<(int)(p->rows < 4096 ? p->rows : 4096), 256, 0, st>>>(a.slabs, a.n_rows, (const int32_t *)(ws + l.slot), (uint16_t *)dx, p->rows, p->hidden, (int)l.Hp, (int)(l.vc / kStep));
+const int64_t blocks = p->rows * ((p->hidden / 4 + 255) / 256);
+        loss_dx_kernel<<<(int)(blocks < 4096 ? blocks : 4096), 256, 0, st>>>(a.slabs, a.n_rows, (const int32_t *)(ws + l.slot), (uint16_t *)dx, p->rows, p->vocab, p->hidden, (int)l.Hp, l.dz_room);
         e = hipGetLastError();
     }
     return e == hipSuccess ? SKRULL_OK : launch_failed(e, "loss launch");
