@@ -9,7 +9,7 @@
  * and for a gradient dy, with g = dy * w:
  *     dx = rstd * (g - mean(g) - h * mean(g * h))   (SKRULL_NORM_RMS: without mean(g))
  *     dw = sum over rows of dy * h,   db = sum over rows of dy
- * All sums are held in fp32, in an order that the sizes alone decide: results are bit-reproducible.  y and dx are
+ * All sums are held in fp32, in an order that sizes and alignment decide: results are bit-reproducible.  y and dx are
  * rounded once to the type of x, dw and db to the type of w.
  *
  * Tensors are caller-owned DEVICE memory, x, y, dy and dx of one type (`type`), w, b, dw and db of one

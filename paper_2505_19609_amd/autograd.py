@@ -4,9 +4,12 @@ attention runs in the HIP kernels behind the C ABI.  The marshalling is native c
 nothing watches the call from Python, else the Function below: the same checks, outputs and errors."""
 from __future__ import annotations
 
+import ctypes
+import sys
 import warnings
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as B
 
@@ -83,9 +86,28 @@ def skrull_attention(q, k, v, plan):
     return _SkrullAttention.apply(q, k, v, plan)
 
 
-# ---- rotary positions, norm, loss: the same, on the binding's calls ----------------------------------------------------
+# ---- rotary positions, norm, loss: the same way ---------------------------------------------------------------------
 
 _KINDS = {"layer": B.NORM_LAYER, "rms": B.NORM_RMS}
+
+
+def _module():
+    """The native module, or None where it cannot be loaded."""
+    if _native is None:
+        _load_native()
+    return sys.modules.get(__package__ + "._autograd") if _native else None
+
+
+def _native_for(*tensors):
+    """The native module for a call that nothing watches from Python, else None."""
+    return _module() if all(type(t) in _TENSORS or t is None for t in tensors) and not _watched() else None
+
+
+def _refuse_captured(*tensors):
+    if any(t is not None and t.is_cuda for t in tensors) and torch.cuda.is_current_stream_capturing():
+        module = _module()
+        if module is not None:
+            module.refuse_captured(*tensors)
 
 
 def _workspace(n, device):
@@ -101,6 +123,7 @@ class _SkrullRotary(torch.autograd.Function):
         return tuple(out)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dq, dk):
         given = [_rows_of_heads(t) for t in (dq, dk)]
         out = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in given]
@@ -110,16 +133,24 @@ class _SkrullRotary(torch.autograd.Function):
 
 def _rows_of_heads(t):
     """`t` [rows, heads, head_dim] as the library takes it: strides as they are where it can."""
+    if t.dim() != 3:
+        raise ValueError("q and k must be [rows, heads, head_dim]")
     heads, d = t.shape[1:]
-    fits = t.stride(2) == 1 and (heads == 1 or t.stride(1) == d) and t.stride(0) >= heads * d and t.stride(0) % 8 == 0 and t.data_ptr() % 16 == 0
-    return t if fits else t.contiguous()
+    fits = t.stride(2) == 1 and (heads == 1 or t.stride(1) == d) and t.data_ptr() % 16 == 0 and \
+        (t.shape[0] < 2 or (t.stride(0) >= heads * d and t.stride(0) % 8 == 0))
+    return t if fits else t.clone(memory_format=torch.contiguous_format)
 
 
 def skrull_rotary(q, k, plan, rotary, k_rows=B.ROWS_K):
     """q and k turned by the positions of the rows of `plan` (a binding.Plan); differentiable.  `rotary`: from
     binding.skrull_rotary_init.  k holds the gathered prefixes, or with k_rows=binding.ROWS_Q this rank's own tokens.
     q and k may be parts of one projection's rows; what comes back is contiguous, as skrull_attention takes it."""
-    return _SkrullRotary.apply(_rows_of_heads(q), _rows_of_heads(k), plan, rotary, k_rows)
+    module = _native_for(q, k) if type(plan) is B.Plan and type(rotary) is B.Rotary else None
+    out = module.rotary(q, k, plan, ctypes.addressof(rotary), k_rows) if module is not None else None
+    if out is None:
+        _refuse_captured(q, k)
+        out = _SkrullRotary.apply(_rows_of_heads(q), _rows_of_heads(k), plan, rotary, k_rows)
+    return out
 
 
 class _SkrullNorm(torch.autograd.Function):
@@ -133,9 +164,10 @@ class _SkrullNorm(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, weight, mean, rstd = ctx.saved_tensors
-        dy = dy if dy.stride(1) == 1 and dy.stride(0) >= dy.shape[1] else dy.contiguous()
+        dy = _rows(dy)
         dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         need_w, need_b = ctx.needs_input_grad[1], ctx.bias and ctx.needs_input_grad[2]
         dw = torch.empty_like(weight) if need_w else None
@@ -145,6 +177,11 @@ class _SkrullNorm(torch.autograd.Function):
         return dx, dw, db, None, None
 
 
+def _rows(t):
+    """`t` [rows, cols] with contiguous rows, one behind the other."""
+    return t if t.dim() != 2 or (t.stride(1) == 1 and (t.stride(0) >= t.shape[1] or t.shape[0] < 2)) else t.contiguous()
+
+
 def skrull_norm(x, weight, bias=None, eps=1e-5, kind="layer"):
     """The norm of the rows of x [rows, cols] (bf16 or fp32) with weight and bias [cols]: "layer", or "rms" without mean and
     bias; differentiable with respect to x, weight and bias."""
@@ -152,9 +189,12 @@ def skrull_norm(x, weight, bias=None, eps=1e-5, kind="layer"):
         raise ValueError(f"kind must be one of {sorted(_KINDS)}")
     if x.dim() != 2:
         raise ValueError("x must be [rows, cols]")
-    if x.stride(1) != 1 or x.stride(0) < x.shape[1]:
-        x = x.contiguous()
-    return _SkrullNorm.apply(x, weight.contiguous(), None if bias is None else bias.contiguous(), eps, _KINDS[kind])
+    module = _native_for(x, weight, bias)
+    y = module.norm(x, weight, bias, eps, _KINDS[kind]) if module is not None else None
+    if y is None:
+        _refuse_captured(x, weight, bias)
+        y = _SkrullNorm.apply(_rows(x), weight.contiguous(), None if bias is None else bias.contiguous(), eps, _KINDS[kind])
+    return y
 
 
 class _SkrullCrossEntropy(torch.autograd.Function):
@@ -166,6 +206,7 @@ class _SkrullCrossEntropy(torch.autograd.Function):
         return loss
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, d_loss):
         x, weight, target, lse = ctx.saved_tensors
         dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if ctx.needs_input_grad[0] else None
@@ -179,6 +220,9 @@ def skrull_cross_entropy(x, weight, target):
     """The softmax cross entropy of each row of x [rows, hidden] times the vocabulary's weight [vocab, hidden] against
     target [rows] (int64; a negative one: the row has none, and a loss of 0), fp32 [rows], without keeping the logits;
     differentiable with respect to x and weight."""
-    if x.dim() == 2 and (x.stride(1) != 1 or x.stride(0) < x.shape[1]):
-        x = x.contiguous()
-    return _SkrullCrossEntropy.apply(x, weight.contiguous(), target.contiguous())
+    module = _native_for(x, weight, target)
+    loss = module.cross_entropy(x, weight, target) if module is not None else None
+    if loss is None:
+        _refuse_captured(x, weight)
+        loss = _SkrullCrossEntropy.apply(_rows(x), weight.contiguous(), target.contiguous())
+    return loss

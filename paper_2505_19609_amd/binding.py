@@ -413,7 +413,7 @@ def _refuse(why):
 def _on_current_device(*tensors):
     import torch
     for t in tensors:
-        if t is not None and not (t.is_cuda and t.device.index == torch.cuda.current_device()):
+        if t is not None and (not t.is_cuda or t.get_device() != torch.cuda.current_device()):
             _refuse(f"a tensor is on {t.device}, not on the current GPU")
 
 
@@ -426,25 +426,26 @@ def skrull_rotary_init(head_dim, rotary_dim=None, layout=ROTARY_HALF, base=10000
     return r
 
 
-def _rotary_tensor(plan, x, out, rows):
+def _rotary_tensor(info, x, out, rows):
     import torch
-    want = plan.total_q if rows == ROWS_Q else plan.total_k
+    want, d = info.total_q if rows == ROWS_Q else info.total_k, info.head_dim
+    shape, strides = x.shape, []
     for t in (x, out):
-        if t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[0] != want or t.shape[2] != plan.head_dim or t.shape != x.shape:
-            _refuse(f"a tensor of bf16 [{want}, heads, {plan.head_dim}] is needed, got {t.dtype} {list(t.shape)}")
-        if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != plan.head_dim):
+        if t.dtype is not torch.bfloat16 or len(shape) != 3 or shape[0] != want or shape[2] != d or t.shape != shape:
+            _refuse(f"a tensor of bf16 [{want}, heads, {d}] is needed, got {t.dtype} {list(t.shape)}")
+        row, head, one = t.stride()
+        if one != 1 or (head != d and shape[1] > 1):
             _refuse("the heads of a row must be contiguous")
-    # (a single row's stride says nothing)
-    width = x.shape[1] * plan.head_dim
-    strides = [t.stride(0) if want > 1 else width for t in (x, out)]
-    return RotaryTensor(_ptr(x), _ptr(out), strides[0], strides[1], x.shape[1], rows)
+        strides.append(row if want > 1 else shape[1] * d)   # (a single row's stride says nothing)
+    return RotaryTensor(x.data_ptr(), out.data_ptr(), strides[0], strides[1], shape[1], rows)
 
 
 def skrull_rotary(plan: Plan, rotary: Rotary, q, k, q_out, k_out, inverse=False, k_rows=ROWS_K, stream=None):
     """q_out, k_out = q, k turned by the positions of the plan's rows (`inverse`: turned back).  q or k may be None.  k_rows: whether
     k holds the gathered prefixes (ROWS_K) or this rank's own tokens (ROWS_Q)."""
     _on_current_device(q, k, q_out, k_out)
-    t = [_rotary_tensor(plan, x, out, rows) for x, out, rows in ((q, q_out, ROWS_Q), (k, k_out, k_rows)) if x is not None]
+    info = plan.info
+    t = [_rotary_tensor(info, x, out, rows) for x, out, rows in ((q, q_out, ROWS_Q), (k, k_out, k_rows)) if x is not None]
     if not t:
         _refuse("neither q nor k")
     _check(lib().skrull_rotary(plan.handle, ctypes.byref(rotary), ctypes.byref(t[0]),

@@ -1,4 +1,4 @@
-// The differentiable call of the package (autograd.py) in native code: checks, output tensors and bookkeeping around
+// The differentiable calls of the package (autograd.py) in native code: checks, output tensors and bookkeeping around
 // skrull_attn_fwd and skrull_attn_bwd.  A pass of 932 tokens, 4/4 heads of 64, forward and gradients, takes the GPU 34 us;
 // written in Python the calls around it kept the host busy for 50 us in a process whose threads run close to each other and
 // 107 in one where they do not (the backward runs in a thread of the autograd engine, and every Python object it touches
@@ -7,15 +7,20 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
 #include <memory>
 
 #include "skrull_attn.h"
+#include "skrull_loss.h"
+#include "skrull_norm.h"
+#include "skrull_rotary.h"
 
 namespace {
 
@@ -146,6 +151,265 @@ PyObject *attention(PyObject *, PyObject *const *args, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- rotary positions, norm, loss.  A call whose tensors are not as the library takes them returns None: the Function in autograd.py then brings
+// them into that form, or raises. ----
+
+struct PlanHolder : torch::CustomClassHolder {
+    std::shared_ptr<PlanObject> plan;
+    explicit PlanHolder(std::shared_ptr<PlanObject> p) : plan(std::move(p)) {}
+};
+
+// Whether `t` is on the current GPU.
+bool here(const at::Tensor &t) { return t.is_cuda() && t.get_device() == c10::hip::current_device(); }
+bool is_bf16(const at::Tensor &t) { return t.scalar_type() == at::kBFloat16; }
+// The library's number of a type, -1 for one that it does not take.
+int type_of(const at::Tensor &t)
+{
+    return t.scalar_type() == at::kBFloat16 ? SKRULL_TYPE_BF16 : t.scalar_type() == at::kFloat ? SKRULL_TYPE_FP32 : -1;
+}
+// Rows of contiguous elements, each at or behind the end of the one before.
+bool is_rows(const at::Tensor &t) { return t.dim() == 2 && t.size(1) > 0 && (t.stride(1) == 1 || t.size(1) == 1) && (t.stride(0) >= t.size(1) || t.size(0) < 2); }
+int64_t row_stride(const at::Tensor &t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }
+void *address(const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
+at::Tensor bytes_like(const at::Tensor &t, int64_t n) { return at::empty({std::max<int64_t>(n, 16)}, t.options().dtype(at::kByte)); }
+
+// A gradient that is asked for with create_graph cannot be differentiated again.
+variable_list once(const variable_list &grads, variable_list out)
+{
+    if (!at::GradMode::is_enabled() || !std::any_of(grads.begin(), grads.end(), [](const at::Tensor &g) { return g.defined() && g.requires_grad(); })) return out;
+    const auto error = std::make_shared<torch::autograd::DelayedError>("the gradients of this operator cannot be differentiated again", (int)out.size());
+    variable_list given;
+    for (const at::Tensor &t : out) given.push_back(t.defined() ? t.detach().requires_grad_() : t);
+    return (*error)(std::move(given));
+}
+
+struct Norm : torch::autograd::Function<Norm> {
+    static Variable forward(AutogradContext *ctx, const Variable &x, const Variable &w, const std::optional<at::Tensor> &b, double eps, int64_t kind)
+    {
+        at::Tensor y = at::empty(x.sizes(), x.options()), stats = at::empty({2, x.size(0)}, x.options().dtype(at::kFloat));
+        skrull_norm_t p = sizes(x, w, (float)eps, kind);
+        p.y_stride = x.size(1);
+        float *mean = (float *)stats.data_ptr();
+        check(skrull_norm_fwd(&p, x.data_ptr(), w.data_ptr(), b ? b->data_ptr() : nullptr, y.data_ptr(), mean, mean + x.size(0), current_stream()));
+        ctx->saved_data["kind"] = kind;
+        ctx->saved_data["bias"] = b.has_value();
+        ctx->save_for_backward({x, w, stats});
+        return y;
+    }
+    static variable_list backward(AutogradContext *ctx, variable_list grads)
+    {
+        const variable_list saved = ctx->get_saved_variables();
+        const at::Tensor &x = saved[0], &w = saved[1], &stats = saved[2];
+        const at::Tensor dy = is_rows(grads[0]) ? grads[0] : grads[0].contiguous();
+        at::Tensor dx = at::empty(x.sizes(), x.options()), dw, db, ws;
+        if (ctx->needs_input_grad(1)) dw = at::empty_like(w);
+        if (ctx->saved_data["bias"].toBool() && ctx->needs_input_grad(2)) db = at::empty_like(w);
+        skrull_norm_t p = sizes(x, w, 0.0f, ctx->saved_data["kind"].toInt());
+        p.dy_stride = row_stride(dy);
+        p.dx_stride = x.size(1);
+        const int64_t bytes = dw.defined() || db.defined() ? skrull_norm_workspace(&p) : 0;
+        if (bytes) ws = bytes_like(x, bytes);
+        const float *mean = (const float *)stats.data_ptr();
+        check(skrull_norm_bwd(&p, x.data_ptr(), w.data_ptr(), mean, mean + x.size(0), dy.data_ptr(), dx.data_ptr(), address(dw), address(db), address(ws), (size_t)bytes,
+                              current_stream()));
+        return once(grads, {dx, dw, db, at::Tensor(), at::Tensor()});
+    }
+    static skrull_norm_t sizes(const at::Tensor &x, const at::Tensor &w, float eps, int64_t kind)
+    {
+        skrull_norm_t p = {};
+        p.rows = x.size(0);
+        p.cols = (int32_t)x.size(1);
+        p.kind = (int32_t)kind;
+        p.type = type_of(x);
+        p.weight_type = type_of(w);
+        p.eps = eps;
+        p.x_stride = row_stride(x);
+        return p;
+    }
+};
+
+struct CrossEntropy : torch::autograd::Function<CrossEntropy> {
+    static Variable forward(AutogradContext *ctx, const Variable &x, const Variable &w, const Variable &target)
+    {
+        at::Tensor loss = at::empty({x.size(0)}, x.options().dtype(at::kFloat)), lse = at::empty_like(loss);
+        const skrull_loss_t p = sizes(x, w);
+        const int64_t bytes = skrull_loss_workspace(&p, 0);
+        const at::Tensor ws = bytes_like(x, bytes);
+        check(skrull_loss_fwd(&p, x.data_ptr(), w.data_ptr(), (const int64_t *)target.data_ptr(), (float *)loss.data_ptr(), (float *)lse.data_ptr(), ws.data_ptr(), (size_t)bytes,
+                              current_stream()));
+        ctx->save_for_backward({x, w, target, lse});
+        return loss;
+    }
+    static variable_list backward(AutogradContext *ctx, variable_list grads)
+    {
+        const variable_list saved = ctx->get_saved_variables();
+        const at::Tensor &x = saved[0], &w = saved[1], &target = saved[2], &lse = saved[3];
+        const at::Tensor d = grads[0].contiguous();
+        at::Tensor dx, dw;
+        if (ctx->needs_input_grad(0)) dx = at::empty(x.sizes(), x.options());
+        if (ctx->needs_input_grad(1)) dw = at::empty_like(w);
+        const skrull_loss_t p = sizes(x, w);
+        const int64_t bytes = skrull_loss_workspace(&p, 1);
+        const at::Tensor ws = bytes_like(x, bytes);
+        check(skrull_loss_bwd(&p, x.data_ptr(), w.data_ptr(), (const int64_t *)target.data_ptr(), (const float *)lse.data_ptr(), (const float *)d.data_ptr(), address(dx), address(dw),
+                              ws.data_ptr(), (size_t)bytes, current_stream()));
+        return once(grads, {dx, dw, at::Tensor()});
+    }
+    static skrull_loss_t sizes(const at::Tensor &x, const at::Tensor &w)
+    {
+        return skrull_loss_t{x.size(0), (int32_t)x.size(1), (int32_t)w.size(0), row_stride(x)};
+    }
+};
+
+// [rows, heads, head_dim] as skrull_rotary takes it
+bool is_heads(const at::Tensor &t)
+{
+    return t.dim() == 3 && t.stride(2) == 1 && (t.size(1) == 1 || t.stride(1) == t.size(2)) && (t.size(0) < 2 || (t.stride(0) >= t.size(1) * t.size(2) && t.stride(0) % 8 == 0)) &&
+           (uintptr_t)t.data_ptr() % 16 == 0;
+}
+
+struct Rotary : torch::autograd::Function<Rotary> {
+    static variable_list forward(AutogradContext *ctx, const Variable &q, const Variable &k, const std::shared_ptr<PlanObject> &plan, const skrull_attn_plan_t *handle,
+                                 const std::string &rotary, int64_t k_rows)
+    {
+        ctx->saved_data["plan"] = c10::IValue::make_capsule(c10::make_intrusive<PlanHolder>(plan));
+        ctx->saved_data["rotary"] = rotary;
+        ctx->saved_data["k_rows"] = k_rows;
+        return turn(handle, rotary, q, k, k_rows, 0);
+    }
+    static variable_list backward(AutogradContext *ctx, variable_list grads)
+    {
+        const auto holder = c10::static_intrusive_pointer_cast<PlanHolder>(ctx->saved_data["plan"].toCapsule());
+        const skrull_attn_plan_t *handle;
+        {
+            const PyGILState_STATE gil = PyGILState_Ensure();
+            try {
+                handle = handle_of(holder->plan->plan);
+            } catch (python_error &e) {
+                e.persist();
+                PyGILState_Release(gil);
+                throw;
+            }
+            PyGILState_Release(gil);
+        }
+        const at::Tensor dq = is_heads(grads[0]) ? grads[0] : grads[0].contiguous(), dk = is_heads(grads[1]) ? grads[1] : grads[1].contiguous();
+        variable_list out = turn(handle, ctx->saved_data["rotary"].toStringRef(), dq, dk, ctx->saved_data["k_rows"].toInt(), 1);
+        return once(grads, {out[0], out[1], at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor()});
+    }
+    static variable_list turn(const skrull_attn_plan_t *handle, const std::string &rotary, const at::Tensor &q, const at::Tensor &k, int64_t k_rows, int inverse)
+    {
+        variable_list out = {at::empty(q.sizes(), q.options()), at::empty(k.sizes(), k.options())};
+        const skrull_rotary_tensor_t t[2] = {tensor(q, out[0], SKRULL_ROWS_Q), tensor(k, out[1], (int32_t)k_rows)};
+        check(skrull_rotary(handle, (const skrull_rotary_t *)rotary.data(), &t[0], &t[1], inverse, current_stream()));
+        return out;
+    }
+    static skrull_rotary_tensor_t tensor(const at::Tensor &in, const at::Tensor &out, int32_t rows)
+    {
+        const int64_t width = in.size(1) * in.size(2);
+        return skrull_rotary_tensor_t{in.data_ptr(), out.data_ptr(), in.size(0) > 1 ? in.stride(0) : width, width, (int32_t)in.size(1), rows};
+    }
+};
+
+// While a graph is captured, a backward pass that reaches a leaf through a node which an eager graph keeps alive waits for that node's own
+// stream, which is not captured: the process ends there.  So such a call is refused before it records anything.
+void refuse_captured(std::initializer_list<const at::Tensor *> inputs)
+{
+    const c10::hip::HIPStream stream = c10::hip::getCurrentHIPStream();
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(stream.stream(), &capture) != hipSuccess || capture == hipStreamCaptureStatusNone || !at::GradMode::is_enabled()) return;
+    for (const at::Tensor *t : inputs) {
+        if (!t->defined() || !t->requires_grad() || !t->is_leaf()) continue;
+        const auto node = torch::autograd::impl::try_get_grad_accumulator(*t);
+        if (!node) continue;
+        const auto other = node->stream();
+        TORCH_CHECK_VALUE(!other || *other == stream.unwrap(),
+                          "a graph made outside this capture is alive and has the same leaf: release it (its outputs) before a backward pass is captured");
+    }
+}
+
+#define SKRULL_TENSOR(i) THPVariable_Unpack(args[i])
+
+// norm(x, weight, bias or None, eps, kind)
+PyObject *norm(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    TORCH_CHECK_TYPE(n == 5 && THPVariable_Check(args[0]) && THPVariable_Check(args[1]) && (args[2] == Py_None || THPVariable_Check(args[2])), "norm(x, weight, bias, eps, kind)");
+    const at::Tensor &x = SKRULL_TENSOR(0), &w = SKRULL_TENSOR(1), b = args[2] == Py_None ? at::Tensor() : SKRULL_TENSOR(2);
+    const double eps = PyFloat_AsDouble(args[3]);
+    const int64_t kind = PyLong_AsLongLong(args[4]);
+    if (PyErr_Occurred()) return nullptr;
+    if (!here(x) || !here(w) || !is_rows(x) || x.size(1) > SKRULL_NORM_MAX_COLS || type_of(x) < 0 || type_of(w) < 0 || w.dim() != 1 || w.size(0) != x.size(1) || !w.is_contiguous() ||
+        (b.defined() && (!here(b) || b.scalar_type() != w.scalar_type() || b.dim() != 1 || b.size(0) != x.size(1) || !b.is_contiguous())))
+        Py_RETURN_NONE;
+    at::Tensor y;
+    {
+        pybind11::gil_scoped_release no_gil;
+        refuse_captured({&x, &w, &b});
+        y = Norm::apply(x, w, b.defined() ? std::optional<at::Tensor>(b) : std::nullopt, eps, kind);
+    }
+    return THPVariable_Wrap(std::move(y));
+    END_HANDLE_TH_ERRORS
+}
+
+// cross_entropy(x, weight, target)
+PyObject *cross_entropy(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    TORCH_CHECK_TYPE(n == 3 && THPVariable_Check(args[0]) && THPVariable_Check(args[1]) && THPVariable_Check(args[2]), "cross_entropy(x, weight, target)");
+    const at::Tensor &x = SKRULL_TENSOR(0), &w = SKRULL_TENSOR(1), &target = SKRULL_TENSOR(2);
+    if (!here(x) || !here(w) || !here(target) || !is_rows(x) || !is_bf16(x) || !is_bf16(w) || w.dim() != 2 || w.size(1) != x.size(1) || !w.is_contiguous() || w.size(0) > INT32_MAX ||
+        x.size(1) > INT32_MAX || target.scalar_type() != at::kLong || target.dim() != 1 || target.size(0) != x.size(0) || !target.is_contiguous())
+        Py_RETURN_NONE;
+    at::Tensor loss;
+    {
+        pybind11::gil_scoped_release no_gil;
+        refuse_captured({&x, &w});
+        loss = CrossEntropy::apply(x, w, target);
+    }
+    return THPVariable_Wrap(std::move(loss));
+    END_HANDLE_TH_ERRORS
+}
+
+// rotary(q, k, plan, address of the skrull_rotary_t, k_rows)
+PyObject *rotary(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    TORCH_CHECK_TYPE(n == 5 && THPVariable_Check(args[0]) && THPVariable_Check(args[1]), "rotary(q, k, plan, rotary, k_rows)");
+    const at::Tensor &q = SKRULL_TENSOR(0), &k = SKRULL_TENSOR(1);
+    const void *given = PyLong_AsVoidPtr(args[3]);
+    const int64_t k_rows = PyLong_AsLongLong(args[4]);
+    if (PyErr_Occurred()) return nullptr;
+    const skrull_attn_plan_t *handle = handle_of(args[2]);
+    skrull_attn_plan_info_t info;
+    if (skrull_attn_plan_info(handle, &info) != SKRULL_OK || (k_rows != SKRULL_ROWS_Q && k_rows != SKRULL_ROWS_K)) Py_RETURN_NONE;
+    if (!here(q) || !here(k) || !is_bf16(q) || !is_bf16(k) || !is_heads(q) || !is_heads(k) || q.size(0) != info.total_q ||
+        k.size(0) != (k_rows == SKRULL_ROWS_Q ? info.total_q : info.total_k) || q.size(2) != info.head_dim || k.size(2) != info.head_dim)
+        Py_RETURN_NONE;
+    const std::string copy((const char *)given, sizeof(skrull_rotary_t));
+    auto plan = std::make_shared<PlanObject>(args[2]);
+    variable_list out;
+    {
+        pybind11::gil_scoped_release no_gil;
+        refuse_captured({&q, &k});
+        out = Rotary::apply(q, k, plan, handle, copy, k_rows);
+    }
+    PyObject *both = PyTuple_New(2);
+    if (!both) throw python_error();
+    for (int i = 0; i < 2; ++i) PyTuple_SET_ITEM(both, i, THPVariable_Wrap(std::move(out[i])));
+    return both;
+    END_HANDLE_TH_ERRORS
+}
+
+// refuse_captured(tensors): the same for calls that take the Function in autograd.py
+PyObject *refuse_captured_of(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    for (Py_ssize_t i = 0; i < n; ++i)
+        if (THPVariable_Check(args[i])) refuse_captured({&SKRULL_TENSOR(i)});
+    Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
 PyObject *set_check(PyObject *, PyObject *f)
 {
     Py_INCREF(f);
@@ -154,6 +418,10 @@ PyObject *set_check(PyObject *, PyObject *f)
 }
 
 PyMethodDef methods[] = {{"attention", (PyCFunction)(void (*)())attention, METH_FASTCALL, "the differentiable call"},
+                         {"norm", (PyCFunction)(void (*)())norm, METH_FASTCALL, "the differentiable norm"},
+                         {"cross_entropy", (PyCFunction)(void (*)())cross_entropy, METH_FASTCALL, "the differentiable loss"},
+                         {"rotary", (PyCFunction)(void (*)())rotary, METH_FASTCALL, "the differentiable rotary positions"},
+                         {"refuse_captured", (PyCFunction)(void (*)())refuse_captured_of, METH_FASTCALL, "refuses leaves that an eager graph has"},
                          {"set_check", set_check, METH_O, "the callable that raises what an error code stands for"},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_autograd", "autograd of skrull_attn", -1, methods, nullptr, nullptr, nullptr, nullptr};

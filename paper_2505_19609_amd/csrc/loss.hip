@@ -394,8 +394,8 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
                 SB();
                 if (j & 1) continue;
                 if (i < 8) b1[i >> 1][i & 1] = B.get(t + kOperandBytes, 1, i >> 1, i & 1);
-                else if (i & 1) load_b(f, 0, i - 8 >> 1);
-                else load_a(f, 0, i - 8 >> 1);
+                else if (i & 1) load_b(f, 0, (i - 8) >> 1);
+                else load_a(f, 0, (i - 8) >> 1);
                 SB();
             }
 #pragma unroll
@@ -415,8 +415,8 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
                 SB();
                 if (j & 1) continue;
                 if (i < 8) a0[i >> 1][i & 1] = A.get(next, 0, i >> 1, i & 1);
-                else if (i & 1) load_a(f, 1, i - 8 >> 1);
-                else load_b(f, 1, i - 8 >> 1);
+                else if (i & 1) load_a(f, 1, (i - 8) >> 1);
+                else load_b(f, 1, (i - 8) >> 1);
                 SB();
             }
 #pragma unroll

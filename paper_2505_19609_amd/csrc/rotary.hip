@@ -1,9 +1,9 @@
 // Rotary positions of a plan's packed rows (include/skrull_rotary.h).
 //
 // What bounds it: every element of Q and K is read and written once, 4 bytes, and meets two products; the
-// sines and cosines are one pair per (row, pair of elements), shared by all heads of the row.  So a workgroup takes a few whole rows,
-// forms their sines and cosines once into LDS and streams the heads through, 16 bytes per load and store.  The positions come from
-// the plan's descriptor (which segment a row is in), so nothing but the tensors themselves is read per element.
+// sines and cosines are one pair per (row, pair of elements), shared by all heads of the row.  So a workgroup takes a few whole rows, of Q and K
+// together where both hold the same rows, forms their sines and cosines once into LDS and streams the heads through, 16 bytes per load and
+// store.  The positions come from the plan's descriptor (which segment a row is in), so nothing but the tensors themselves is read per element.
 #include <math.h>
 
 #include <hip/hip_bf16.h>
@@ -22,16 +22,20 @@ struct Tensor {
     const uint16_t *in;
     uint16_t *out;
     int64_t in_stride, out_stride;
+    int32_t heads, copies;  // copies: `out` is other memory, the elements that are not turned go along
+    uint64_t inv_row, inv_head;  // ceil(2^40 / units of a row, of a head)
+};
+// Rows that workgroups share out, and the tensors that hold them.
+struct Rows {
     const int32_t *cu;      // [NS+1] first row of each segment
     const int32_t *begin;   // [NS] position of its first row, or null: 0
-    int32_t heads, rows, rows_per_block, blocks;
-    uint64_t inv_row;       // ceil(2^40 / units of a row)
+    int32_t rows, each, blocks, tensors;   // rows of a workgroup; workgroups; one or two tensors
+    Tensor t[2];
 };
 
 struct Args {
-    Tensor t[2];
-    int32_t NS, head_dim, rotary_dim, scaling, copies;   // copies: `out` is other memory, the elements that are not turned go along
-    uint64_t inv_unit;      // ceil(2^40 / units of a head)
+    Rows r[2];
+    int32_t NS, head_dim, rotary_dim, scaling;
     double log2_base, factor, turns_scale, low_turns, high_turns;   // turns_scale: original_length
     float amplitude, sign;
 };
@@ -55,50 +59,41 @@ __device__ double turns_of(const Args &a, int i)
 __device__ __forceinline__ float lo_of(uint32_t u) { return __builtin_bit_cast(float, u << 16); }
 __device__ __forceinline__ float hi_of(uint32_t u) { return __builtin_bit_cast(float, u & 0xffff0000u); }
 
-template <bool INTERLEAVED>
-__global__ __launch_bounds__(kThreads) void rotary_kernel(const Args a)
+// The positions of `rows` (at most 32) rows from row0 on, in the lanes of one wavefront: 64 segments' first rows are compared at a time, so
+// a row's segment is two or three loads away in any micro-batch.
+__device__ __forceinline__ int position_of(const Rows &w, int NS, int row0, int rows, int lane)
 {
-    __shared__ double freq[kMaxPairs];
-    __shared__ int pos[kMaxRows];
-    __shared__ float2 turn[kMaxRows * kMaxPairs];   // cos, sin
-    const int which = (int)blockIdx.x >= a.t[0].blocks;
-    const Tensor &t = a.t[which];
-    const int row0 = ((int)blockIdx.x - (which ? a.t[0].blocks : 0)) * t.rows_per_block;
-    const int rows = min(t.rows_per_block, t.rows - row0);
+    int lo = 0, len = NS;   // row0 lies in one of the segments lo .. lo + len - 1
+    while (len > 31) {
+        const int step = (len + 63) / 64, i = lane * step;
+        const int first = i < len ? w.cu[lo + i] : INT32_MAX;
+        lo += (__popcll(__ballot(first <= row0)) - 1) * step;
+        len = min(step, NS - lo);
+    }
+    const int first = lo + lane < NS ? w.cu[lo + lane] : INT32_MAX;   // (31 segments and one more per row are in reach)
+    int segment = lo;
+    for (int r = 0; r < rows; ++r) {
+        const int s = lo + __popcll(__ballot(first <= row0 + r)) - 1;
+        if (lane == r) segment = s;
+    }
+    return row0 + lane - __shfl(first, segment - lo) + (w.begin ? w.begin[segment] : 0);
+}
+
+template <bool INTERLEAVED>
+__device__ __forceinline__ void turn_rows(const Args &a, const Tensor &t, const float2 *turn, int row0, int rows, int tid)
+{
     const int pairs = a.rotary_dim / 2;
-    const int tid = threadIdx.x;
-
-    if (tid < pairs) freq[tid] = turns_of(a, tid);
-    if (tid >= kThreads - kMaxRows && tid - (kThreads - kMaxRows) < rows) {   // (other wavefronts than those of the frequencies)
-        const int r = tid - (kThreads - kMaxRows), row = row0 + r;
-        int lo = 0, hi = a.NS;   // the last segment that begins at or before the row
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (t.cu[mid] <= row) lo = mid;
-            else hi = mid;
-        }
-        pos[r] = row - t.cu[lo] + (t.begin ? t.begin[lo] : 0);
-    }
-    __syncthreads();
-    for (int i = tid; i < rows * pairs; i += kThreads) {
-        const int r = i / pairs, p = i - r * pairs;
-        const double turns = (double)pos[r] * freq[p];
-        float s, c;
-        sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
-        turn[i] = make_float2(c * a.amplitude, s * a.amplitude * a.sign);
-    }
-    __syncthreads();
-
     // A unit is what a lane moves at a time.  Half layout: 8 pairs (two pieces of 16 bytes), then the pieces behind rotary_dim;
     // interleaved: a piece of 16 bytes, 4 pairs.
     const int turned = INTERLEAVED ? a.rotary_dim / 8 : a.rotary_dim / 16;
-    const int units = turned + (a.copies >> which & 1 ? (a.head_dim - a.rotary_dim) / 8 : 0);
+    const int units = turned + (t.copies ? (a.head_dim - a.rotary_dim) / 8 : 0);
     const int row_units = units * t.heads;
+#pragma unroll 2
     for (int i = tid; i < rows * row_units; i += kThreads) {
         const int r = quotient40(i, t.inv_row), x = i - r * row_units;
-        const int head = units == turned ? x / turned : x / units, u = x - head * units;
-        const uint16_t *in = t.in + (int64_t)(row0 + r) * t.in_stride + (int64_t)head * a.head_dim;
-        uint16_t *out = t.out + (int64_t)(row0 + r) * t.out_stride + (int64_t)head * a.head_dim;
+        const int head = quotient40(x, t.inv_head), u = x - head * units;
+        const uint16_t *in = t.in + (int64_t)(row0 + r) * t.in_stride + head * a.head_dim;
+        uint16_t *out = t.out + (int64_t)(row0 + r) * t.out_stride + head * a.head_dim;
         if (u >= turned) {
             const int e = a.rotary_dim + (u - turned) * 8;
             *(uint4 *)(out + e) = *(const uint4 *)(in + e);
@@ -128,6 +123,37 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const Args a)
             *(uint4 *)(out + e1) = make_uint4(a1[0], a1[1], a1[2], a1[3]);
         }
     }
+}
+
+template <bool INTERLEAVED>
+__global__ __launch_bounds__(kThreads) void rotary_kernel(const Args a)
+{
+    __shared__ double freq[kMaxPairs];
+    __shared__ int pos[kMaxRows];
+    __shared__ float2 turn[kMaxRows * kMaxPairs];   // cos, sin
+    const int which = (int)blockIdx.x >= a.r[0].blocks;
+    const Rows &w = a.r[which];
+    const int row0 = ((int)blockIdx.x - (which ? a.r[0].blocks : 0)) * w.each;
+    const int rows = min(w.each, w.rows - row0);
+    const int pairs = a.rotary_dim / 2;
+    const int tid = threadIdx.x;
+
+    if (tid < pairs) freq[tid] = turns_of(a, tid);
+    if (tid >= 64 && tid < 128) {   // (another wavefront than that of the frequencies)
+        const int p = position_of(w, a.NS, row0, rows, tid - 64);
+        if (tid - 64 < rows) pos[tid - 64] = p;
+    }
+    __syncthreads();
+    for (int i = tid; i < rows * pairs; i += kThreads) {
+        const int r = i / pairs, p = i - r * pairs;
+        const double turns = (double)pos[r] * freq[p];
+        float s, c;
+        sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
+        turn[i] = make_float2(c * a.amplitude, s * a.amplitude * a.sign);
+    }
+    __syncthreads();
+    turn_rows<INTERLEAVED>(a, w.t[0], turn, row0, rows, tid);
+    if (w.tensors > 1) turn_rows<INTERLEAVED>(a, w.t[1], turn, row0, rows, tid);
 }
 
 uint64_t inverse40(int d) { return ((1ull << 40) + (uint64_t)d - 1) / (uint64_t)d; }
@@ -178,33 +204,48 @@ int skrull_rotary(const skrull_attn_plan_t *plan, const skrull_rotary_t *r, cons
     a.sign = inverse ? -1.0f : 1.0f;
     const skrull_rotary_tensor_t *given[2] = {first, second};
     int64_t blocks = 0;
+    int groups = 0;
     for (int i = 0; i < 2; ++i) {
         const skrull_rotary_tensor_t *g = given[i];
         if (!g) continue;
-        Tensor &t = a.t[i];
         if (!g->in || !g->out || !aligned_to(g->in, 16) || !aligned_to(g->out, 16)) return refuse("rotary: tensor %d is null or not 16-byte aligned", i);
         if (g->heads < 1 || g->heads > 4096) return refuse("rotary: tensor %d has %d heads", i, g->heads);
         if (g->rows != SKRULL_ROWS_Q && g->rows != SKRULL_ROWS_K) return refuse("rotary: tensor %d is of unknown rows %d", i, g->rows);
         const int64_t width = (int64_t)g->heads * r->head_dim;
         if (g->in_stride < width || g->out_stride < width || g->in_stride % 8 != 0 || g->out_stride % 8 != 0)
             return refuse("rotary: strides of tensor %d must be multiples of 8 and at least heads * head_dim", i);
-        t.rows = g->rows == SKRULL_ROWS_Q ? plan->total_q : plan->total_k;
-        const int64_t in_bytes = ((t.rows - 1) * g->in_stride + width) * 2, out_bytes = ((t.rows - 1) * g->out_stride + width) * 2;
+        // (sequences that are whole have the same rows in both packings; any other has more keys than queries)
+        const bool q_rows = g->rows == SKRULL_ROWS_Q || plan->total_q == plan->total_k;
+        const int64_t n = q_rows ? plan->total_q : plan->total_k;
+        if (g->in_stride > INT64_MAX / 4 / n || g->out_stride > INT64_MAX / 4 / n) return refuse("rotary: stride of tensor %d", i);
+        const int64_t in_bytes = ((n - 1) * g->in_stride + width) * 2, out_bytes = ((n - 1) * g->out_stride + width) * 2;
         const bool in_place = g->in == g->out && g->in_stride == g->out_stride;
         if (!in_place && overlap(g->in, in_bytes, g->out, out_bytes)) return refuse("rotary: out of tensor %d overlaps its in", i);
-        if (!in_place) a.copies |= 1 << i;
+        const int32_t *cu = q_rows ? plan->cu_q : plan->cu_k;
+        Rows &w = groups > 0 && a.r[0].cu == cu ? a.r[0] : a.r[groups++];
+        w.cu = cu;
+        w.begin = q_rows ? plan->q_begin : nullptr;
+        w.rows = (int32_t)n;
+        Tensor &t = w.t[w.tensors++];
         t.in = (const uint16_t *)g->in;
         t.out = (uint16_t *)g->out;
         t.in_stride = g->in_stride;
         t.out_stride = g->out_stride;
-        t.cu = g->rows == SKRULL_ROWS_Q ? plan->cu_q : plan->cu_k;
-        t.begin = g->rows == SKRULL_ROWS_Q ? plan->q_begin : nullptr;
         t.heads = g->heads;
-        t.rows_per_block = (int32_t)(width >= 8192 ? 4 : width >= 4096 ? 8 : width >= 2048 ? 16 : 32);
-        t.blocks = (t.rows + t.rows_per_block - 1) / t.rows_per_block;
-        const int turned = r->rotary_dim / (r->layout == SKRULL_ROTARY_INTERLEAVED ? 8 : 16);
-        t.inv_row = inverse40(g->heads * (turned + (in_place ? 0 : (r->head_dim - r->rotary_dim) / 8)));
-        blocks += t.blocks;
+        t.copies = !in_place;
+        const int units = r->rotary_dim / (r->layout == SKRULL_ROTARY_INTERLEAVED ? 8 : 16) + (in_place ? 0 : (r->head_dim - r->rotary_dim) / 8);
+        t.inv_head = inverse40(units);
+        t.inv_row = inverse40(g->heads * units);
+    }
+    for (int i = 0; i < groups; ++i) {
+        Rows &w = a.r[i];
+        // about 32 KB in a workgroup's rows, fewer where that leaves compute units without one
+        const int64_t width = (int64_t)(w.t[0].heads + w.t[1].heads) * r->head_dim;
+        int32_t each = kMaxRows;
+        while (each > 1 && (each * width > 16384 || (int64_t)w.rows < each * 512)) each /= 2;
+        w.each = each;
+        w.blocks = (w.rows + each - 1) / each;
+        blocks += w.blocks;
     }
     if (int rc = plan_on_current_device(plan)) return rc;
     if (blocks > INT32_MAX) return refuse("rotary: too many rows");

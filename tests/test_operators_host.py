@@ -174,9 +174,9 @@ def test_rotary_tensors_are_checked():
     plan = B.Plan(None, B.PlanInfo(total_q=4, total_k=6, num_q_heads=2, num_kv_heads=1, head_dim=64))
     q = torch.zeros(4, 2, 64, dtype=torch.bfloat16)
     k = torch.zeros(6, 1, 64, dtype=torch.bfloat16)
-    assert B._rotary_tensor(plan, q, q, B.ROWS_Q).in_stride == 128
-    assert B._rotary_tensor(plan, k, k, B.ROWS_K).heads == 1
+    assert B._rotary_tensor(plan.info, q, q, B.ROWS_Q).in_stride == 128
+    assert B._rotary_tensor(plan.info, k, k, B.ROWS_K).heads == 1
     for x, out, rows in ((q, q, B.ROWS_K), (q, k, B.ROWS_Q), (q.float(), q, B.ROWS_Q), (q[:, :, :32], q, B.ROWS_Q),
                          (q.transpose(0, 1), q, B.ROWS_Q), (torch.zeros(4, 64, 2, dtype=torch.bfloat16).transpose(1, 2), q, B.ROWS_Q)):
         with pytest.raises(B.SkrullError):
-            B._rotary_tensor(plan, x, out, rows)
+            B._rotary_tensor(plan.info, x, out, rows)
