@@ -24,7 +24,7 @@ struct NormArgs {
     float *partial;          // [workgroups][dw, then db: cols each], or null
     int64_t x_stride, y_stride, dy_stride;
     int64_t rows;
-    int32_t cols, weight_type, wide;  // wide: 16-byte loads and stores are aligned
+    int32_t cols, weight_type;
     float eps, inv_cols;
 };
 
@@ -35,10 +35,11 @@ struct Bf16 {
     typedef uint16_t type;
     static __device__ __forceinline__ float get(uint16_t u) { return bf16_at(u); }
     static __device__ __forceinline__ uint16_t put(float f) { return to_bf16(f); }
-    static __device__ __forceinline__ void load8(const uint16_t *p, float f[8])
+    struct Raw { uint4 v; };   // 8 values as they lie in memory
+    static __device__ __forceinline__ Raw load8(const uint16_t *p) { return Raw{*(const uint4 *)p}; }
+    static __device__ __forceinline__ void widen(const Raw &r, float f[8])
     {
-        const uint4 v = *(const uint4 *)p;
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        const uint32_t w[4] = {r.v.x, r.v.y, r.v.z, r.v.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             f[2 * i] = __builtin_bit_cast(float, w[i] << 16);
@@ -54,10 +55,11 @@ struct Fp32 {
     typedef float type;
     static __device__ __forceinline__ float get(float u) { return u; }
     static __device__ __forceinline__ float put(float f) { return f; }
-    static __device__ __forceinline__ void load8(const float *p, float f[8])
+    struct Raw { float4 a, b; };
+    static __device__ __forceinline__ Raw load8(const float *p) { return Raw{((const float4 *)p)[0], ((const float4 *)p)[1]}; }
+    static __device__ __forceinline__ void widen(const Raw &r, float f[8])
     {
-        const float4 a = ((const float4 *)p)[0], b = ((const float4 *)p)[1];
-        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+        f[0] = r.a.x; f[1] = r.a.y; f[2] = r.a.z; f[3] = r.a.w; f[4] = r.b.x; f[5] = r.b.y; f[6] = r.b.z; f[7] = r.b.w;
     }
     static __device__ __forceinline__ void store8(float *p, const float f[8])
     {
@@ -67,49 +69,61 @@ struct Fp32 {
 };
 
 // The columns of a lane's piece c, i = 0..7: with wide loads 8 neighbours, else every lane's i-th column beside the next lane's, so that
-// the lanes' single loads fill whole lines (7,013 rows of 1,001 bf16: forward 41 us with 8 neighbours, %s this way).
+// the lanes' single loads fill whole lines (7,013 rows of 1,001 bf16, forward: 40 us with 8 neighbours, 19 this way).
+template <bool WIDE>
 struct Columns {
     int first, step, cols;
-    bool wide;
-    __device__ __forceinline__ void init(int c, int lane, int lanes, int n, bool w)
+    __device__ __forceinline__ void init(int c, int lane, int lanes, int n)
     {
-        wide = w;
         cols = n;
-        first = w ? (c * lanes + lane) * 8 : c * 8 * lanes + lane;
-        step = w ? 1 : lanes;
+        first = WIDE ? (c * lanes + lane) * 8 : c * 8 * lanes + lane;
+        step = WIDE ? 1 : lanes;
     }
-    __device__ __forceinline__ int at(int i) const { return first + i * step; }
-    __device__ __forceinline__ bool has(int i) const { return at(i) < cols; }
+    __device__ __forceinline__ int at(int i) const { return first + (WIDE ? i : i * step); }
+    __device__ __forceinline__ bool has(int i) const { return (WIDE ? first : at(i)) < cols; }   // (wide pieces are whole)
 };
 
-// A lane's piece of a row (or of w), zero behind the last column.
-template <class T>
-__device__ __forceinline__ void load_piece(const typename T::type *row, const Columns &k, float f[8])
-{
-    if (k.wide) {
-        if (k.first < k.cols) {
-            T::load8(row + k.first, f);
-            return;
+// A lane's pieces of a row, zero behind the last column.  With wide loads they are fetched a row ahead of their use, so that they
+// arrive while the row before is summed up (13,312 rows of 3,584 bf16: forward and backward 52 and 101 us without, 46 and 61 with).
+template <class T, int C, bool WIDE>
+struct RowPieces {
+    typename T::Raw raw[C];
+    __device__ __forceinline__ void fetch(const typename T::type *row, const Columns<WIDE> col[C])
+    {
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                if (col[c].has(0)) raw[c] = T::load8(row + col[c].first);
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = 0.0f;
-        return;
     }
+    __device__ __forceinline__ void get(const typename T::type *row, const Columns<WIDE> col[C], float f[C][8]) const
+    {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = k.has(i) ? T::get(row[k.at(i)]) : 0.0f;
-}
-template <class T>
-__device__ __forceinline__ void store_piece(typename T::type *row, const Columns &k, const float f[8])
+        for (int c = 0; c < C; ++c) {
+            if constexpr (WIDE) {
+                T::widen(raw[c], f[c]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[c][i] = col[c].has(0) ? f[c][i] : 0.0f;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[c][i] = col[c].has(i) ? T::get(row[col[c].at(i)]) : 0.0f;
+            }
+        }
+    }
+};
+template <class T, bool WIDE>
+__device__ __forceinline__ void store_piece(typename T::type *row, const Columns<WIDE> &k, const float f[8])
 {
-    if (k.wide) {
-        if (k.first < k.cols) T::store8(row + k.first, f);
-        return;
-    }
+    if constexpr (WIDE) {
+        if (k.has(0)) T::store8(row + k.first, f);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (k.has(i)) row[k.at(i)] = T::put(f[i]);
+        for (int i = 0; i < 8; ++i)
+            if (k.has(i)) row[k.at(i)] = T::put(f[i]);
+    }
 }
-__device__ __forceinline__ void load_weight(const void *w, int type, const Columns &k, float f[8])
+template <bool WIDE>
+__device__ __forceinline__ void load_weight(const void *w, int type, const Columns<WIDE> &k, float f[8])
 {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -142,7 +156,7 @@ __device__ __forceinline__ void row_sums(float v[N], float *lds, int &turn)
     }
 }
 
-template <class T, int WAVES, int C, bool CENTER>
+template <class T, int WAVES, int C, bool CENTER, bool WIDE>
 __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void norm_fwd_kernel(const NormArgs a)
 {
     constexpr int ROWS = WAVES == 1 ? 4 : 1;   // rows of a workgroup at a time
@@ -150,22 +164,24 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void norm_fwd_kernel(cons
     int turn = 0;
     const int slot = ROWS > 1 ? threadIdx.x >> 6 : 0, lane = ROWS > 1 ? threadIdx.x & 63 : threadIdx.x;
     float w[C][8], b[C][8];
-    Columns col[C];
+    Columns<WIDE> col[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        col[c].init(c, lane, 64 * WAVES, a.cols, a.wide);
+        col[c].init(c, lane, 64 * WAVES, a.cols);
         load_weight(a.w, a.weight_type, col[c], w[c]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) b[c][i] = 0.0f;
         if (a.b) load_weight(a.b, a.weight_type, col[c], b[c]);
     }
-    for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < a.rows; row0 += (int64_t)gridDim.x * ROWS) {
-        const int64_t row = row0 + slot;
-        if (ROWS > 1 && row >= a.rows) return;   // (a wavefront to a row: nobody waits for it)
-        const typename T::type *xr = (const typename T::type *)a.x + row * a.x_stride;
+    const typename T::type *X = (const typename T::type *)a.x;
+    const int64_t stride = (int64_t)gridDim.x * ROWS;
+    int64_t row = (int64_t)blockIdx.x * ROWS + slot;   // (a wavefront to a row, or all of them: no wavefront waits for one that has left)
+    RowPieces<T, C, WIDE> next;
+    if (row < a.rows) next.fetch(X + row * a.x_stride, col);
+    for (; row < a.rows; row += stride) {
         float x[C][8];
-#pragma unroll
-        for (int c = 0; c < C; ++c) load_piece<T>(xr, col[c], x[c]);
+        next.get(X + row * a.x_stride, col, x);
+        if (row + stride < a.rows) next.fetch(X + (row + stride) * a.x_stride, col);
         float mean = 0.0f;
         if constexpr (CENTER) {
             float s[1] = {0.0f};
@@ -197,12 +213,12 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void norm_fwd_kernel(cons
             float y[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) y[i] = x[c][i] * rstd * w[c][i] + b[c][i];
-            store_piece<T>(yr, col[c], y);
+            store_piece<T, WIDE>(yr, col[c], y);
         }
     }
 }
 
-template <class T, int WAVES, int C, bool CENTER>
+template <class T, int WAVES, int C, bool CENTER, bool WIDE>
 __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void norm_bwd_kernel(const NormArgs a)
 {
     constexpr int ROWS = WAVES == 1 ? 4 : 1;
@@ -210,26 +226,32 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void norm_bwd_kernel(cons
     int turn = 0;
     const int slot = ROWS > 1 ? threadIdx.x >> 6 : 0, lane = ROWS > 1 ? threadIdx.x & 63 : threadIdx.x;
     float w[C][8], dw[C][8], db[C][8];
-    Columns col[C];
+    Columns<WIDE> col[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        col[c].init(c, lane, 64 * WAVES, a.cols, a.wide);
+        col[c].init(c, lane, 64 * WAVES, a.cols);
         load_weight(a.w, a.weight_type, col[c], w[c]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) dw[c][i] = db[c][i] = 0.0f;
     }
-    for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < a.rows; row0 += (int64_t)gridDim.x * ROWS) {
-        const int64_t row = row0 + slot;
-        if (ROWS > 1 && row >= a.rows) break;
-        const float mean = CENTER ? a.mean[row] : 0.0f, rstd = a.rstd[row];
-        const typename T::type *xr = (const typename T::type *)a.x + row * a.x_stride;
-        const typename T::type *dr = (const typename T::type *)a.dy + row * a.dy_stride;
+    const typename T::type *X = (const typename T::type *)a.x, *DY = (const typename T::type *)a.dy;
+    const int64_t stride = (int64_t)gridDim.x * ROWS;
+    int64_t row = (int64_t)blockIdx.x * ROWS + slot;
+    RowPieces<T, C, WIDE> next_x, next_dy;
+    float next_mean = 0.0f, next_rstd = 0.0f;
+    auto fetch = [&](int64_t r) {
+        next_x.fetch(X + r * a.x_stride, col);
+        next_dy.fetch(DY + r * a.dy_stride, col);
+        if (CENTER) next_mean = a.mean[r];
+        next_rstd = a.rstd[r];
+    };
+    if (row < a.rows) fetch(row);
+    for (; row < a.rows; row += stride) {
+        const float mean = next_mean, rstd = next_rstd;
         float h[C][8], g[C][8];
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            load_piece<T>(xr, col[c], h[c]);
-            load_piece<T>(dr, col[c], g[c]);
-        }
+        next_x.get(X + row * a.x_stride, col, h);
+        next_dy.get(DY + row * a.dy_stride, col, g);
+        if (row + stride < a.rows) fetch(row + stride);
         float s[2] = {0.0f, 0.0f};   // sum g h, sum g
 #pragma unroll
         for (int c = 0; c < C; ++c)
@@ -251,7 +273,7 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void norm_bwd_kernel(cons
             float dx[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) dx[i] = (g[c][i] - m1 - h[c][i] * m0) * rstd;
-            store_piece<T>(out, col[c], dx);
+            store_piece<T, WIDE>(out, col[c], dx);
         }
     }
     if (!a.partial) return;
@@ -352,23 +374,27 @@ bool wide_rows(const void *ptr, int64_t stride, const skrull_norm_t *p)
 
 int waves_of(int cols) { return cols <= 1024 ? 1 : cols <= 4096 ? 4 : 16; }
 
-// Workgroups of the backward, each with a line of partial sums: as many as run at once.
+// Workgroups of the backward, each with a line of partial sums.  With wide loads, which are fetched a row ahead, as many as have 32 KB of rows among
+// them on a compute unit: one to four (13,312 x 3,584 bf16: 61 us with two, 66 with one or four; 32,768 x 4,096 fp32: 286 with one, 313 with
+// two or four; 26,624 x 896 bf16: 34 with two, 38 with four).  Else four (7,013 x 1,001 bf16: 34 us, 50 with two).
 constexpr int kComputeUnits = 256;
-int64_t bwd_blocks(const skrull_norm_t *p)
+int64_t bwd_blocks(const skrull_norm_t *p, bool wide)
 {
     const int waves = waves_of(p->cols), rows = waves == 1 ? 4 : 1;
-    const int64_t most = waves == 16 ? kComputeUnits : 4 * kComputeUnits, need = (p->rows + rows - 1) / rows;
+    const int64_t row_bytes = (int64_t)rows * p->cols * size_of(p->type) * 2, fit = 32768 / row_bytes;
+    const int64_t most = (wide ? fit < 1 ? 1 : fit > 4 ? 4 : fit : waves == 16 ? 1 : 4) * kComputeUnits, need = (p->rows + rows - 1) / rows;
     return need < most ? need : most;
 }
 
-template <class T, bool CENTER>
+// `wide`: 16-byte loads and stores are aligned and pieces whole
+template <class T, bool CENTER, bool WIDE>
 void launch(bool backward, const NormArgs &a, int blocks, hipStream_t st)
 {
     const int cols = a.cols;
 #define SKRULL_NORM_CASE(WAVES, C)                                                                                                     \
     do {                                                                                                                               \
-        if (backward) norm_bwd_kernel<T, WAVES, C, CENTER><<<blocks, WAVES == 16 ? 1024 : 256, 0, st>>>(a);                            \
-        else norm_fwd_kernel<T, WAVES, C, CENTER><<<blocks, WAVES == 16 ? 1024 : 256, 0, st>>>(a);                                     \
+        if (backward) norm_bwd_kernel<T, WAVES, C, CENTER, WIDE><<<blocks, WAVES == 16 ? 1024 : 256, 0, st>>>(a);                      \
+        else norm_fwd_kernel<T, WAVES, C, CENTER, WIDE><<<blocks, WAVES == 16 ? 1024 : 256, 0, st>>>(a);                               \
     } while (0)
     if (cols <= 512) SKRULL_NORM_CASE(1, 1);
     else if (cols <= 1024) SKRULL_NORM_CASE(1, 2);
@@ -377,15 +403,16 @@ void launch(bool backward, const NormArgs &a, int blocks, hipStream_t st)
     else SKRULL_NORM_CASE(16, 1);
 #undef SKRULL_NORM_CASE
 }
-void launch(bool backward, const skrull_norm_t *p, const NormArgs &a, int blocks, hipStream_t st)
+template <class T>
+void launch(bool backward, bool wide, int kind, const NormArgs &a, int blocks, hipStream_t st)
 {
-    if (p->type == SKRULL_TYPE_BF16) {
-        if (p->kind == SKRULL_NORM_LAYER) launch<Bf16, true>(backward, a, blocks, st);
-        else launch<Bf16, false>(backward, a, blocks, st);
-    } else {
-        if (p->kind == SKRULL_NORM_LAYER) launch<Fp32, true>(backward, a, blocks, st);
-        else launch<Fp32, false>(backward, a, blocks, st);
-    }
+    if (kind == SKRULL_NORM_LAYER) wide ? launch<T, true, true>(backward, a, blocks, st) : launch<T, true, false>(backward, a, blocks, st);
+    else wide ? launch<T, false, true>(backward, a, blocks, st) : launch<T, false, false>(backward, a, blocks, st);
+}
+void launch(bool backward, bool wide, const skrull_norm_t *p, const NormArgs &a, int blocks, hipStream_t st)
+{
+    if (p->type == SKRULL_TYPE_BF16) launch<Bf16>(backward, wide, p->kind, a, blocks, st);
+    else launch<Fp32>(backward, wide, p->kind, a, blocks, st);
 }
 
 }  // namespace
@@ -409,18 +436,21 @@ int skrull_norm_fwd(const skrull_norm_t *p, const void *x, const void *w, const 
     NormArgs a = {};
     a.x = x; a.w = w; a.b = b; a.y = y; a.mean = mean; a.rstd = rstd;
     a.x_stride = p->x_stride; a.y_stride = p->y_stride; a.rows = p->rows; a.cols = p->cols; a.weight_type = p->weight_type;
-    a.wide = p->cols % 8 == 0 && wide_rows(x, p->x_stride, p) && wide_rows(y, p->y_stride, p);
+    const bool wide = p->cols % 8 == 0 && wide_rows(x, p->x_stride, p) && wide_rows(y, p->y_stride, p);
     a.eps = p->eps; a.inv_cols = 1.0f / (float)p->cols;
     const int waves = waves_of(p->cols), rows = waves == 1 ? 4 : 1;
-    const int64_t most = (int64_t)compute_units * (waves == 16 ? 2 : 8), need = (p->rows + rows - 1) / rows;
-    launch(false, p, a, (int)(need < most ? need : most), (hipStream_t)hip_stream);
+    // (13,312 x 3,584 bf16: 41 us with four workgroups to a compute unit, 46 with eight; 26,624 x 896: 21 and 27)
+    const int64_t most = (int64_t)compute_units * (waves == 16 ? 2 : 4), need = (p->rows + rows - 1) / rows;
+    launch(false, wide, p, a, (int)(need < most ? need : most), (hipStream_t)hip_stream);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? SKRULL_OK : launch_failed(e, "norm launch");
 }
 
 int64_t skrull_norm_workspace(const skrull_norm_t *p)
 {
-    return check(p) == SKRULL_OK ? bwd_blocks(p) * 2 * p->cols * 4 + 16 : 0;
+    if (check(p) != SKRULL_OK) return 0;
+    const int64_t a = bwd_blocks(p, true), b = bwd_blocks(p, false);
+    return (a > b ? a : b) * 2 * p->cols * 4 + 16;
 }
 
 int skrull_norm_bwd(const skrull_norm_t *p, const void *x, const void *w, const float *mean, const float *rstd, const void *dy,
@@ -448,19 +478,21 @@ int skrull_norm_bwd(const skrull_norm_t *p, const void *x, const void *w, const 
     if (int rc = current_device(&compute_units)) return rc;
     hipStream_t st = (hipStream_t)hip_stream;
     hipError_t e = hipSuccess;
+    int blocks = 0;
     if (p->rows > 0) {
         NormArgs a = {};
         a.x = x; a.w = w; a.dy = dy; a.y = dx; a.mean = const_cast<float *>(mean); a.rstd = const_cast<float *>(rstd);
         a.partial = sums ? (float *)workspace : nullptr;
         a.x_stride = p->x_stride; a.y_stride = p->dx_stride; a.dy_stride = p->dy_stride; a.rows = p->rows; a.cols = p->cols;
         a.weight_type = p->weight_type;
-        a.wide = p->cols % 8 == 0 && wide_rows(x, p->x_stride, p) && wide_rows(dy, p->dy_stride, p) && wide_rows(dx, p->dx_stride, p);
+        const bool wide = p->cols % 8 == 0 && wide_rows(x, p->x_stride, p) && wide_rows(dy, p->dy_stride, p) && wide_rows(dx, p->dx_stride, p);
         a.inv_cols = 1.0f / (float)p->cols;
-        launch(true, p, a, (int)bwd_blocks(p), st);
+        blocks = (int)bwd_blocks(p, wide);
+        launch(true, wide, p, a, blocks, st);
         e = hipGetLastError();
     }
     if (e == hipSuccess && sums) {
-        norm_sums_kernel<<<dim3((unsigned)((p->cols + 63) / 64), 2), 1024, 0, st>>>((const float *)workspace, (int)bwd_blocks(p), p->cols, dw, db, p->weight_type);
+        norm_sums_kernel<<<dim3((unsigned)((p->cols + 63) / 64), 2), 1024, 0, st>>>((const float *)workspace, blocks, p->cols, dw, db, p->weight_type);
         e = hipGetLastError();
     }
     return e == hipSuccess ? SKRULL_OK : launch_failed(e, "norm launch");
