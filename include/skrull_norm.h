@@ -9,12 +9,11 @@
  * and for a gradient dy, with g = dy * w:
  *     dx = rstd * (g - mean(g) - h * mean(g * h))   (SKRULL_NORM_RMS: without mean(g))
  *     dw = sum over rows of dy * h,   db = sum over rows of dy
- * All sums are held in fp32, in an order that sizes and alignment decide: results are bit-reproducible.  y and dx are
+ * All sums are held in fp32, in an order that the sizes alone decide: results are bit-reproducible.  y and dx are
  * rounded once to the type of x, dw and db to the type of w.
  *
  * Tensors are caller-owned DEVICE memory, x, y, dy and dx of one type (`type`), w, b, dw and db of one
- * (`weight_type`).  Rows of a tensor begin `stride` elements apart and are contiguous within; rows of any alignment, width and stride
- * are taken (those of 16-byte alignment and of widths and strides that are multiples of 16 bytes by wide loads).
+ * (`weight_type`).  Rows of a tensor begin `stride` elements apart and are contiguous within; rows of any alignment, width and stride are taken.
  */
 #ifndef SKRULL_NORM_H
 #define SKRULL_NORM_H

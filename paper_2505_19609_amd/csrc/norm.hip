@@ -36,7 +36,19 @@ struct Bf16 {
     static __device__ __forceinline__ float get(uint16_t u) { return bf16_at(u); }
     static __device__ __forceinline__ uint16_t put(float f) { return to_bf16(f); }
     struct Raw { uint4 v; };   // 8 values as they lie in memory
-    static __device__ __forceinline__ Raw load8(const uint16_t *p) { return Raw{*(const uint4 *)p}; }
+    static __device__ __forceinline__ Raw load8(const uint16_t *p)
+    {
+        Raw r;
+        __builtin_memcpy(&r, p, sizeof r);
+        return r;
+    }
+    static __device__ __forceinline__ Raw load_some(const uint16_t *p, int n)
+    {
+        uint32_t e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = i < n ? p[i] : 0;
+        return Raw{make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16)};
+    }
     static __device__ __forceinline__ void widen(const Raw &r, float f[8])
     {
         const uint32_t w[4] = {r.v.x, r.v.y, r.v.z, r.v.w};
@@ -48,7 +60,8 @@ struct Bf16 {
     }
     static __device__ __forceinline__ void store8(uint16_t *p, const float f[8])
     {
-        *(uint4 *)p = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+        const uint4 v = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+        __builtin_memcpy(p, &v, sizeof v);
     }
 };
 struct Fp32 {
@@ -56,78 +69,92 @@ struct Fp32 {
     static __device__ __forceinline__ float get(float u) { return u; }
     static __device__ __forceinline__ float put(float f) { return f; }
     struct Raw { float4 a, b; };
-    static __device__ __forceinline__ Raw load8(const float *p) { return Raw{((const float4 *)p)[0], ((const float4 *)p)[1]}; }
+    static __device__ __forceinline__ Raw load8(const float *p)
+    {
+        Raw r;
+        __builtin_memcpy(&r, p, sizeof r);
+        return r;
+    }
+    static __device__ __forceinline__ Raw load_some(const float *p, int n)
+    {
+        float e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = i < n ? p[i] : 0.0f;
+        return Raw{make_float4(e[0], e[1], e[2], e[3]), make_float4(e[4], e[5], e[6], e[7])};
+    }
     static __device__ __forceinline__ void widen(const Raw &r, float f[8])
     {
         f[0] = r.a.x; f[1] = r.a.y; f[2] = r.a.z; f[3] = r.a.w; f[4] = r.b.x; f[5] = r.b.y; f[6] = r.b.z; f[7] = r.b.w;
     }
     static __device__ __forceinline__ void store8(float *p, const float f[8])
     {
-        ((float4 *)p)[0] = make_float4(f[0], f[1], f[2], f[3]);
-        ((float4 *)p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+        __builtin_memcpy(p, f, 32);
     }
 };
 
-// The columns of a lane's piece c, i = 0..7: with wide loads 8 neighbours, else every lane's i-th column beside the next lane's, so that
-// the lanes' single loads fill whole lines (7,013 rows of 1,001 bf16, forward: 40 us with 8 neighbours, 19 this way).
-template <bool WIDE>
+// A lane's piece of 8 columns.  The last piece of a row whose width is no multiple of 8 is its last 8 columns, of which the first ones
+// belong to the lane before; rows narrower than 8 (SMALL) have one piece that is loaded value by value.  Rows need no alignment but their type's: the hardware takes 16 bytes
+// from any address (7,013 rows of 1,001 bf16, forward: 19 us with a load for each value, the lanes' side by side, 18 this way; backward 34 and 19).
+template <bool SMALL>
 struct Columns {
-    int first, step, cols;
-    __device__ __forceinline__ void init(int c, int lane, int lanes, int n)
+    int first, skip;   // the piece's values from `skip` on are this lane's (8: none); SMALL: those below 8 - skip
+    __device__ __forceinline__ void init(int c, int lane, int lanes, int cols)
     {
-        cols = n;
-        first = WIDE ? (c * lanes + lane) * 8 : c * 8 * lanes + lane;
-        step = WIDE ? 1 : lanes;
+        first = (c * lanes + lane) * 8;
+        skip = max(0, min(8, first + 8 - cols));
+        if (!SMALL && skip < 8) first -= skip;
     }
-    __device__ __forceinline__ int at(int i) const { return first + (WIDE ? i : i * step); }
-    __device__ __forceinline__ bool has(int i) const { return (WIDE ? first : at(i)) < cols; }   // (wide pieces are whole)
+    __device__ __forceinline__ bool has(int i) const { return SMALL ? i < 8 - skip : i >= skip; }
 };
 
-// A lane's pieces of a row, zero behind the last column.  With wide loads they are fetched a row ahead of their use, so that they
-// arrive while the row before is summed up (13,312 rows of 3,584 bf16: forward and backward 52 and 101 us without, 46 and 61 with).
-template <class T, int C, bool WIDE>
+// A lane's pieces of a row, zero where they are not its own.  They are fetched a row ahead of their use, so that they arrive while the row before is
+// summed up (13,312 rows of 3,584 bf16: forward and backward 52 and 101 us without, 41 and 61 with).
+template <class T, int C, bool SMALL>
 struct RowPieces {
     typename T::Raw raw[C];
-    __device__ __forceinline__ void fetch(const typename T::type *row, const Columns<WIDE> col[C])
+    __device__ __forceinline__ void init()
     {
-        if constexpr (WIDE) {
 #pragma unroll
-            for (int c = 0; c < C; ++c)
-                if (col[c].has(0)) raw[c] = T::load8(row + col[c].first);
-        }
+        for (int c = 0; c < C; ++c) raw[c] = typename T::Raw{};
     }
-    __device__ __forceinline__ void get(const typename T::type *row, const Columns<WIDE> col[C], float f[C][8]) const
+    __device__ __forceinline__ void fetch(const typename T::type *row, const Columns<SMALL> col[C])
     {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            if constexpr (WIDE) {
-                T::widen(raw[c], f[c]);
+            if constexpr (SMALL) raw[c] = T::load_some(row + col[c].first, 8 - col[c].skip);
+            else if (col[c].skip < 8) raw[c] = T::load8(row + col[c].first);
+        }
+    }
+    __device__ __forceinline__ void get(const Columns<SMALL> col[C], float f[C][8]) const
+    {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) f[c][i] = col[c].has(0) ? f[c][i] : 0.0f;
-            } else {
+        for (int c = 0; c < C; ++c) {
+            T::widen(raw[c], f[c]);
+            if constexpr (!SMALL) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) f[c][i] = col[c].has(i) ? T::get(row[col[c].at(i)]) : 0.0f;
+                for (int i = 0; i < 7; ++i) f[c][i] = col[c].has(i) ? f[c][i] : 0.0f;   // (the eighth is, or was never loaded)
             }
         }
     }
 };
-template <class T, bool WIDE>
-__device__ __forceinline__ void store_piece(typename T::type *row, const Columns<WIDE> &k, const float f[8])
+template <class T, bool SMALL>
+__device__ __forceinline__ void store_piece(typename T::type *row, const Columns<SMALL> &k, const float f[8])
 {
-    if constexpr (WIDE) {
-        if (k.has(0)) T::store8(row + k.first, f);
-    } else {
+    if (k.skip == 0) {
+        T::store8(row + k.first, f);
+    } else if (k.skip < 8) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (k.has(i)) row[k.at(i)] = T::put(f[i]);
+            if (k.has(i)) row[k.first + i] = T::put(f[i]);
+        asm volatile("");   // (else the last one becomes a store of both branches, and the wide one is cut up for it)
     }
 }
-template <bool WIDE>
-__device__ __forceinline__ void load_weight(const void *w, int type, const Columns<WIDE> &k, float f[8])
+template <bool SMALL>
+__device__ __forceinline__ void load_weight(const void *w, int type, const Columns<SMALL> &k, float f[8])
 {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        f[i] = !k.has(i) ? 0.0f : type == SKRULL_TYPE_BF16 ? bf16_at(((const uint16_t *)w)[k.at(i)]) : ((const float *)w)[k.at(i)];
+        f[i] = !k.has(i) ? 0.0f : type == SKRULL_TYPE_BF16 ? bf16_at(((const uint16_t *)w)[k.first + i]) : ((const float *)w)[k.first + i];
 }
 
 // Sums of N values over the lanes of a row, in every lane.  `lds`: room for 2 x 16 x N floats of this row, used by turns.
@@ -156,7 +183,7 @@ __device__ __forceinline__ void row_sums(float v[N], float *lds, int &turn)
     }
 }
 
-template <class T, int WAVES, int C, bool CENTER, bool WIDE>
+template <class T, int WAVES, int C, bool CENTER, bool SMALL>
 __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void norm_fwd_kernel(const NormArgs a)
 {
     constexpr int ROWS = WAVES == 1 ? 4 : 1;   // rows of a workgroup at a time
@@ -164,7 +191,7 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void norm_fwd_kernel(cons
     int turn = 0;
     const int slot = ROWS > 1 ? threadIdx.x >> 6 : 0, lane = ROWS > 1 ? threadIdx.x & 63 : threadIdx.x;
     float w[C][8], b[C][8];
-    Columns<WIDE> col[C];
+    Columns<SMALL> col[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         col[c].init(c, lane, 64 * WAVES, a.cols);
@@ -176,11 +203,12 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void norm_fwd_kernel(cons
     const typename T::type *X = (const typename T::type *)a.x;
     const int64_t stride = (int64_t)gridDim.x * ROWS;
     int64_t row = (int64_t)blockIdx.x * ROWS + slot;   // (a wavefront to a row, or all of them: no wavefront waits for one that has left)
-    RowPieces<T, C, WIDE> next;
+    RowPieces<T, C, SMALL> next;
+    next.init();
     if (row < a.rows) next.fetch(X + row * a.x_stride, col);
     for (; row < a.rows; row += stride) {
         float x[C][8];
-        next.get(X + row * a.x_stride, col, x);
+        next.get(col, x);
         if (row + stride < a.rows) next.fetch(X + (row + stride) * a.x_stride, col);
         float mean = 0.0f;
         if constexpr (CENTER) {
@@ -213,12 +241,12 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void norm_fwd_kernel(cons
             float y[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) y[i] = x[c][i] * rstd * w[c][i] + b[c][i];
-            store_piece<T, WIDE>(yr, col[c], y);
+            store_piece<T, SMALL>(yr, col[c], y);
         }
     }
 }
 
-template <class T, int WAVES, int C, bool CENTER, bool WIDE>
+template <class T, int WAVES, int C, bool CENTER, bool SMALL>
 __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void norm_bwd_kernel(const NormArgs a)
 {
     constexpr int ROWS = WAVES == 1 ? 4 : 1;
@@ -226,7 +254,7 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void norm_bwd_kernel(cons
     int turn = 0;
     const int slot = ROWS > 1 ? threadIdx.x >> 6 : 0, lane = ROWS > 1 ? threadIdx.x & 63 : threadIdx.x;
     float w[C][8], dw[C][8], db[C][8];
-    Columns<WIDE> col[C];
+    Columns<SMALL> col[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         col[c].init(c, lane, 64 * WAVES, a.cols);
@@ -237,7 +265,9 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void norm_bwd_kernel(cons
     const typename T::type *X = (const typename T::type *)a.x, *DY = (const typename T::type *)a.dy;
     const int64_t stride = (int64_t)gridDim.x * ROWS;
     int64_t row = (int64_t)blockIdx.x * ROWS + slot;
-    RowPieces<T, C, WIDE> next_x, next_dy;
+    RowPieces<T, C, SMALL> next_x, next_dy;
+    next_x.init();
+    next_dy.init();
     float next_mean = 0.0f, next_rstd = 0.0f;
     auto fetch = [&](int64_t r) {
         next_x.fetch(X + r * a.x_stride, col);
@@ -249,8 +279,8 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void norm_bwd_kernel(cons
     for (; row < a.rows; row += stride) {
         const float mean = next_mean, rstd = next_rstd;
         float h[C][8], g[C][8];
-        next_x.get(X + row * a.x_stride, col, h);
-        next_dy.get(DY + row * a.dy_stride, col, g);
+        next_x.get(col, h);
+        next_dy.get(col, g);
         if (row + stride < a.rows) fetch(row + stride);
         float s[2] = {0.0f, 0.0f};   // sum g h, sum g
 #pragma unroll
@@ -273,7 +303,7 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void norm_bwd_kernel(cons
             float dx[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) dx[i] = (g[c][i] - m1 - h[c][i] * m0) * rstd;
-            store_piece<T, WIDE>(out, col[c], dx);
+            store_piece<T, SMALL>(out, col[c], dx);
         }
     }
     if (!a.partial) return;
@@ -284,8 +314,8 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void norm_bwd_kernel(cons
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (col[c].has(i)) {
-                    line[col[c].at(i)] = dw[c][i];
-                    if (CENTER) line[a.cols + col[c].at(i)] = db[c][i];
+                    line[col[c].first + i] = dw[c][i];
+                    if (CENTER) line[a.cols + col[c].first + i] = db[c][i];
                 }
     } else {   // the wavefronts' own sums first
         __shared__ float sums[ROWS][C * 8][64];
@@ -303,7 +333,7 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void norm_bwd_kernel(cons
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
                         if (col[c].has(i))
-                            line[which * a.cols + col[c].at(i)] = (sums[0][c * 8 + i][lane] + sums[1][c * 8 + i][lane]) + (sums[2][c * 8 + i][lane] + sums[3][c * 8 + i][lane]);
+                            line[which * a.cols + col[c].first + i] = (sums[0][c * 8 + i][lane] + sums[1][c * 8 + i][lane]) + (sums[2][c * 8 + i][lane] + sums[3][c * 8 + i][lane]);
             }
         }
     }
@@ -367,52 +397,45 @@ int check_apart(const char *out_name, const void *out, int64_t out_stride, const
     return SKRULL_OK;
 }
 
-bool wide_rows(const void *ptr, int64_t stride, const skrull_norm_t *p)
-{
-    return aligned_to(ptr, 16) && stride * size_of(p->type) % 16 == 0;
-}
-
 int waves_of(int cols) { return cols <= 1024 ? 1 : cols <= 4096 ? 4 : 16; }
 
-// Workgroups of the backward, each with a line of partial sums.  With wide loads, which are fetched a row ahead, as many as have 32 KB of rows among
-// them on a compute unit: one to four (13,312 x 3,584 bf16: 61 us with two, 66 with one or four; 32,768 x 4,096 fp32: 286 with one, 313 with
-// two or four; 26,624 x 896 bf16: 34 with two, 38 with four).  Else four (7,013 x 1,001 bf16: 34 us, 50 with two).
+// Workgroups of the backward, each with a line of partial sums: as many as have 32 KB of rows among them on a compute unit, one to four (13,312 x 3,584 bf16: 61 us with two, 66 with one or four; 32,768 x 4,096 fp32: 286 with one, 313 with
+// two or four; 26,624 x 896 bf16: 34 with two, 38 with four).
 constexpr int kComputeUnits = 256;
-int64_t bwd_blocks(const skrull_norm_t *p, bool wide)
+int64_t bwd_blocks(const skrull_norm_t *p)
 {
     const int waves = waves_of(p->cols), rows = waves == 1 ? 4 : 1;
     const int64_t row_bytes = (int64_t)rows * p->cols * size_of(p->type) * 2, fit = 32768 / row_bytes;
-    const int64_t most = (wide ? fit < 1 ? 1 : fit > 4 ? 4 : fit : waves == 16 ? 1 : 4) * kComputeUnits, need = (p->rows + rows - 1) / rows;
+    const int64_t most = (fit < 1 ? 1 : fit > 4 ? 4 : fit) * kComputeUnits, need = (p->rows + rows - 1) / rows;
     return need < most ? need : most;
 }
 
-// `wide`: 16-byte loads and stores are aligned and pieces whole
-template <class T, bool CENTER, bool WIDE>
+template <class T, bool CENTER>
 void launch(bool backward, const NormArgs &a, int blocks, hipStream_t st)
 {
     const int cols = a.cols;
-#define SKRULL_NORM_CASE(WAVES, C)                                                                                                     \
+#define SKRULL_NORM_CASE(WAVES, C, SMALL)                                                                                                     \
     do {                                                                                                                               \
-        if (backward) norm_bwd_kernel<T, WAVES, C, CENTER, WIDE><<<blocks, WAVES == 16 ? 1024 : 256, 0, st>>>(a);                      \
-        else norm_fwd_kernel<T, WAVES, C, CENTER, WIDE><<<blocks, WAVES == 16 ? 1024 : 256, 0, st>>>(a);                               \
+        if (backward) norm_bwd_kernel<T, WAVES, C, CENTER, SMALL><<<blocks, WAVES == 16 ? 1024 : 256, 0, st>>>(a);                     \
+        else norm_fwd_kernel<T, WAVES, C, CENTER, SMALL><<<blocks, WAVES == 16 ? 1024 : 256, 0, st>>>(a);                                     \
     } while (0)
-    if (cols <= 512) SKRULL_NORM_CASE(1, 1);
-    else if (cols <= 1024) SKRULL_NORM_CASE(1, 2);
-    else if (cols <= 2048) SKRULL_NORM_CASE(4, 1);
-    else if (cols <= 4096) SKRULL_NORM_CASE(4, 2);
-    else SKRULL_NORM_CASE(16, 1);
+    if (cols < 8) SKRULL_NORM_CASE(1, 1, true);
+    else if (cols <= 512) SKRULL_NORM_CASE(1, 1, false);
+    else if (cols <= 1024) SKRULL_NORM_CASE(1, 2, false);
+    else if (cols <= 2048) SKRULL_NORM_CASE(4, 1, false);
+    else if (cols <= 4096) SKRULL_NORM_CASE(4, 2, false);
+    else SKRULL_NORM_CASE(16, 1, false);
 #undef SKRULL_NORM_CASE
 }
-template <class T>
-void launch(bool backward, bool wide, int kind, const NormArgs &a, int blocks, hipStream_t st)
+void launch(bool backward, const skrull_norm_t *p, const NormArgs &a, int blocks, hipStream_t st)
 {
-    if (kind == SKRULL_NORM_LAYER) wide ? launch<T, true, true>(backward, a, blocks, st) : launch<T, true, false>(backward, a, blocks, st);
-    else wide ? launch<T, false, true>(backward, a, blocks, st) : launch<T, false, false>(backward, a, blocks, st);
-}
-void launch(bool backward, bool wide, const skrull_norm_t *p, const NormArgs &a, int blocks, hipStream_t st)
-{
-    if (p->type == SKRULL_TYPE_BF16) launch<Bf16>(backward, wide, p->kind, a, blocks, st);
-    else launch<Fp32>(backward, wide, p->kind, a, blocks, st);
+    if (p->type == SKRULL_TYPE_BF16) {
+        if (p->kind == SKRULL_NORM_LAYER) launch<Bf16, true>(backward, a, blocks, st);
+        else launch<Bf16, false>(backward, a, blocks, st);
+    } else {
+        if (p->kind == SKRULL_NORM_LAYER) launch<Fp32, true>(backward, a, blocks, st);
+        else launch<Fp32, false>(backward, a, blocks, st);
+    }
 }
 
 }  // namespace
@@ -436,21 +459,18 @@ int skrull_norm_fwd(const skrull_norm_t *p, const void *x, const void *w, const 
     NormArgs a = {};
     a.x = x; a.w = w; a.b = b; a.y = y; a.mean = mean; a.rstd = rstd;
     a.x_stride = p->x_stride; a.y_stride = p->y_stride; a.rows = p->rows; a.cols = p->cols; a.weight_type = p->weight_type;
-    const bool wide = p->cols % 8 == 0 && wide_rows(x, p->x_stride, p) && wide_rows(y, p->y_stride, p);
     a.eps = p->eps; a.inv_cols = 1.0f / (float)p->cols;
     const int waves = waves_of(p->cols), rows = waves == 1 ? 4 : 1;
     // (13,312 x 3,584 bf16: 41 us with four workgroups to a compute unit, 46 with eight; 26,624 x 896: 21 and 27)
     const int64_t most = (int64_t)compute_units * (waves == 16 ? 2 : 4), need = (p->rows + rows - 1) / rows;
-    launch(false, wide, p, a, (int)(need < most ? need : most), (hipStream_t)hip_stream);
+    launch(false, p, a, (int)(need < most ? need : most), (hipStream_t)hip_stream);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? SKRULL_OK : launch_failed(e, "norm launch");
 }
 
 int64_t skrull_norm_workspace(const skrull_norm_t *p)
 {
-    if (check(p) != SKRULL_OK) return 0;
-    const int64_t a = bwd_blocks(p, true), b = bwd_blocks(p, false);
-    return (a > b ? a : b) * 2 * p->cols * 4 + 16;
+    return check(p) == SKRULL_OK ? bwd_blocks(p) * 2 * p->cols * 4 + 16 : 0;
 }
 
 int skrull_norm_bwd(const skrull_norm_t *p, const void *x, const void *w, const float *mean, const float *rstd, const void *dy,
@@ -485,10 +505,9 @@ int skrull_norm_bwd(const skrull_norm_t *p, const void *x, const void *w, const 
         a.partial = sums ? (float *)workspace : nullptr;
         a.x_stride = p->x_stride; a.y_stride = p->dx_stride; a.dy_stride = p->dy_stride; a.rows = p->rows; a.cols = p->cols;
         a.weight_type = p->weight_type;
-        const bool wide = p->cols % 8 == 0 && wide_rows(x, p->x_stride, p) && wide_rows(dy, p->dy_stride, p) && wide_rows(dx, p->dx_stride, p);
-        a.inv_cols = 1.0f / (float)p->cols;
-        blocks = (int)bwd_blocks(p, wide);
-        launch(true, wide, p, a, blocks, st);
+            a.inv_cols = 1.0f / (float)p->cols;
+        blocks = (int)bwd_blocks(p);
+        launch(true, p, a, blocks, st);
         e = hipGetLastError();
     }
     if (e == hipSuccess && sums) {

@@ -350,9 +350,8 @@ def test_norm(rows, cols, kind, bias, t, wt):
 
 @pytest.mark.parametrize("cols,pad", [(896, 8), (896, 3), (4096, 24), (1001, 7)])
 def test_norm_strides_and_in_place(cols, pad):
-    """Rows inside wider ones, aligned and not: what contiguous rows give, and nothing beside them is touched; y in the place of x and dx in the
-    place of dy are the same bits.  (So are aligned rows, and any of a width that is never aligned; where alignment changes which columns
-    a lane adds up, the fp32 sums have another order, and each is held to the bound of the 64-bit form.)"""
+    """Rows inside wider ones, aligned and not: what contiguous rows give, up to the same bits, and nothing beside them is
+    touched; y in the place of x and dx in the place of dy are the same bits too."""
     from paper_2505_19609_amd import binding as B
     gen, rows = _gen(cols + pad), 37
     x, dy, w, b = _randn(gen, rows, cols), _randn(gen, rows, cols), _randn(gen, cols), _randn(gen, cols)
@@ -370,12 +369,7 @@ def test_norm_strides_and_in_place(cols, pad):
     want = [t.clone() for t in both(x, dy, torch.empty_like(x), torch.empty_like(x))]
     wides, views = zip(*(_padded(t, pad, 5.0) for t in (x, dy, x, x)))
     got = both(*views)
-    if (cols, pad) == (896, 3):
-        exact = _norm_in_64_bits(x, w, b, dy, 1e-5, True)
-        for name, value in zip(("y", "dx", "dw", "db"), got):
-            _within(value, exact[name][0], exact[name][1] * 1.01 + BF16 * (exact[name][0].abs() + exact[name][1]) + TINY, name)
-    else:
-        assert all(torch.equal(a, c) for a, c in zip(got, want))
+    assert all(torch.equal(a, c) for a, c in zip(got, want))
     assert all((t[:, cols:] == 5).all() for t in wides)
     got = both(x, dy, x, dy)
     assert all(torch.equal(a, c) for a, c in zip(got, want))
