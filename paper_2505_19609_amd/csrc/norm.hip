@@ -149,12 +149,22 @@ __device__ __forceinline__ void store_piece(typename T::type *row, const Columns
         asm volatile("");   // (else the last one becomes a store of both branches, and the wide one is cut up for it)
     }
 }
+// The same piece of w (or b).
+template <class W, bool SMALL>
+__device__ __forceinline__ void load_weight(const void *w, const Columns<SMALL> &k, float f[8])
+{
+    typename W::Raw raw = {};
+    if constexpr (SMALL) raw = W::load_some((const typename W::type *)w + k.first, 8 - k.skip);
+    else if (k.skip < 8) raw = W::load8((const typename W::type *)w + k.first);
+    W::widen(raw, f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = k.has(i) ? f[i] : 0.0f;
+}
 template <bool SMALL>
 __device__ __forceinline__ void load_weight(const void *w, int type, const Columns<SMALL> &k, float f[8])
 {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        f[i] = !k.has(i) ? 0.0f : type == SKRULL_TYPE_BF16 ? bf16_at(((const uint16_t *)w)[k.first + i]) : ((const float *)w)[k.first + i];
+    if (type == SKRULL_TYPE_BF16) load_weight<Bf16>(w, k, f);
+    else load_weight<Fp32>(w, k, f);
 }
 
 // Sums of N values over the lanes of a row, in every lane.  `lds`: room for 2 x 16 x N floats of this row, used by turns.
@@ -310,13 +320,10 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void norm_bwd_kernel(cons
     float *line = a.partial + (int64_t)blockIdx.x * 2 * a.cols;
     if constexpr (ROWS == 1) {
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (col[c].has(i)) {
-                    line[col[c].first + i] = dw[c][i];
-                    if (CENTER) line[a.cols + col[c].first + i] = db[c][i];
-                }
+        for (int c = 0; c < C; ++c) {
+            store_piece<Fp32, SMALL>(line, col[c], dw[c]);
+            if (CENTER) store_piece<Fp32, SMALL>(line + a.cols, col[c], db[c]);
+        }
     } else {   // the wavefronts' own sums first
         __shared__ float sums[ROWS][C * 8][64];
 #pragma unroll
@@ -329,11 +336,12 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void norm_bwd_kernel(cons
             __syncthreads();
             if (slot == 0) {
 #pragma unroll
-                for (int c = 0; c < C; ++c)
+                for (int c = 0; c < C; ++c) {
+                    float f[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (col[c].has(i))
-                            line[which * a.cols + col[c].first + i] = (sums[0][c * 8 + i][lane] + sums[1][c * 8 + i][lane]) + (sums[2][c * 8 + i][lane] + sums[3][c * 8 + i][lane]);
+                    for (int i = 0; i < 8; ++i) f[i] = (sums[0][c * 8 + i][lane] + sums[1][c * 8 + i][lane]) + (sums[2][c * 8 + i][lane] + sums[3][c * 8 + i][lane]);
+                    store_piece<Fp32, SMALL>(line + which * a.cols, col[c], f);
+                }
             }
         }
     }
