@@ -26,7 +26,7 @@ namespace {
 
 constexpr int kTile = 256;       // rows and columns of a result tile
 constexpr int kStep = 64;        // of the contraction
-constexpr int kOperandBytes = kTile * kStep * 2, kHalfBytes = kOperandBytes / 2, kBufferBytes = 2 * kOperandBytes;
+constexpr int kOperandBytes = kTile * kStep * 2;   // of a step in LDS
 constexpr int kGrid = 256;       // workgroups: one per compute unit, each as much LDS as allows no second one
 constexpr int kStrip = 128;      // words whose largest logit and sum the forward keeps together
 constexpr int64_t kPieceBytes = (int64_t)2 << 30;  // of dz at most
@@ -109,15 +109,17 @@ struct Source {
     __device__ __forceinline__ void next() { at += step; left -= step; }
 };
 
-// A tile's operand in LDS: two halves of 16 KB, each of what the wavefronts read in a half of their blocks (of every 128 rows or columns
-// the first or the second 64).  A load's 64 pieces of 16 bytes lie one behind the other, so the arrangement is made on the global
-// side: a lane fetches the piece that belongs where it writes.
-//   ROWS  128 rows x 64 of the contraction (128 bytes a row): piece c of row r lies at c ^ (r / 2 & 7), so 16 rows' pieces of
+// A tile's operand in LDS: two halves, each of what the wavefronts read in a half of their blocks (of every 32 NB rows or columns
+// the first or the second 16 NB; NB = 4: 16 KB a half).  A load's 64 pieces of 16 bytes lie one behind the other, so the arrangement is made
+// on the global side: a lane fetches the piece that belongs where it writes.
+//   ROWS  32 NB rows x 64 of the contraction (128 bytes a row): piece c of row r lies at c ^ (r / 2 & 7), so 16 rows' pieces of
 //         one c, which are read together, are 16 different slots of the 256 bytes that the banks span.
 //   COLS  64 of the contraction x 128 columns (256 bytes a row): piece c of row r lies at c ^ 2 (r & 3 | r / 2 & 4), so the 8 rows x 32 bytes
 //         that a transposing read takes together are 16 different slots too.
-template <bool COLS>
+template <bool COLS, int NB>
 struct Operand {
+    static_assert(NB == 4 || (NB == 1 && !COLS), "");
+    static constexpr int kHalfBytes = 4096 * NB;
     int load[2];     // byte offsets of this lane's pieces in the tile's matrix: of even and odd instructions (COLS: of the first and the last two)
     int read[4];     // LDS offsets of its fragments: ROWS by half step (two), COLS by block of 16 columns
 
@@ -127,9 +129,9 @@ struct Operand {
         if (!COLS) {
 #pragma unroll
             for (int o = 0; o < 2; ++o)
-                load[o] = ((wave >> 1) * 128 + (wave & 1) * 32 + (lane >> 3)) * (int)pitch + (((lane & 7) ^ (4 * o + (lane >> 4))) << 4);
+                load[o] = ((wave >> 1) * 32 * NB + (wave & 1) * 8 * NB + (lane >> 3)) * (int)pitch + (((lane & 7) ^ (4 * odd(o, wave) + (lane >> 4))) << 4);
 #pragma unroll
-            for (int k = 0; k < 2; ++k) read[k] = (part * 64 + s) * 128 + (((4 * k + g) ^ (s >> 1)) << 4);
+            for (int k = 0; k < 2; ++k) read[k] = (part * 16 * NB + s) * 128 + (((4 * k + g) ^ (s >> 1)) << 4);
         } else {
 #pragma unroll
             for (int o = 0; o < 2; ++o) {
@@ -143,19 +145,21 @@ struct Operand {
     }
     // This lane's offsets of a step.  `tail`: elements of the contraction that are left, where rows may end inside the
     // step (ROWS): what is behind them reads as zero.
-    __device__ __forceinline__ void offsets(int lane, int tail, int off[2]) const
+    __device__ __forceinline__ void offsets(int lane, int wave, int tail, int off[2]) const
     {
 #pragma unroll
         for (int o = 0; o < 2; ++o) {
             off[o] = load[o];
-            if (!COLS && ((lane & 7) ^ (4 * o + (lane >> 4))) * 8 >= tail) off[o] = (int)0x80000000;   // (past every descriptor's end)
+            if (!COLS && ((lane & 7) ^ (4 * odd(o, wave) + (lane >> 4))) * 8 >= tail) off[o] = (int)0x80000000;   // (past every descriptor's end)
         }
     }
-    // 4 instructions of each wavefront fill a half.
+    // whether an instruction fills an odd group of 8 rows: every second one of a wavefront does, or, where it has only one, every second wavefront's
+    static __device__ __forceinline__ int odd(int o, int wave) { return NB == 1 ? wave & 1 : o; }
+    // NB instructions of each wavefront fill a half.
     __device__ __forceinline__ static void fetch(i32x4 words, const int off[2], uint32_t pitch, uint32_t lds, int wave, int half, int q)
     {
-        dma_b128(words, lds + half * kHalfBytes + (wave * 4 + q) * 1024, off[COLS ? q >> 1 : q & 1],
-                 COLS ? half * 128 + (int)(q * 4 * pitch) : (int)((half * 64 + q * 8) * pitch));
+        dma_b128(words, lds + half * kHalfBytes + (wave * NB + q) * 1024, off[COLS ? q >> 1 : q & 1],
+                 COLS ? half * 128 + (int)(q * 4 * pitch) : (int)((half * 16 * NB + q * 8) * pitch));
     }
     // fragment b (16 rows or columns, 0..3) of a half and half step k: 8 consecutive elements of the contraction
     __device__ __forceinline__ bf16x8 get(const unsigned char *t, int half, int b, int k) const
@@ -170,19 +174,20 @@ struct Operand {
 };
 
 // The tiles of a product and their operands.
-template <Kind K>
+template <Kind K, int NB>
 struct Product {
+    static constexpr int kRows = 64 * NB;   // columns of a tile: rows of x, but for kDw
     int mt, nt, splits, steps, total;   // tiles of M and N; parts of the contraction, steps of a part
     int v0, zp, all_steps;              // first word of the piece; elements between rows of dz; kDx: steps of all parts
 
     __device__ __forceinline__ void init(const LossArgs &p, int n_rows)
     {
-        const int row_tiles = row_tiles_of(n_rows), h_tiles = (p.H + kTile - 1) / kTile, words = (p.V + kTile - 1) / kTile;
+        const int row_tiles = max(1, (n_rows + kRows - 1) / kRows), h_tiles = (p.H + kTile - 1) / kTile, words = (p.V + kTile - 1) / kTile;
         splits = 1;
         v0 = zp = all_steps = 0;
         int piece_tiles = words;
         if (K != kForward) {
-            const Piece piece(row_tiles, p.V, p.H, p.dz_room);
+            const Piece piece(row_tiles_of(n_rows), p.V, p.H, p.dz_room);
             zp = piece.pitch;
             v0 = p.piece * piece.tiles * kTile;
             piece_tiles = max(0, min(piece.tiles, words - p.piece * piece.tiles));   // (no tile: there are fewer pieces than launches)
@@ -227,11 +232,11 @@ struct Product {
         if (K == kForward || K == kAgain) {
             const int64_t v = v0 + (int64_t)m * kTile;
             a = Source{(const unsigned char *)p.w + v * H2, min((int64_t)kTile, p.V - v) * H2, (uint32_t)H2, kStep * 2};
-            b = Source{(const unsigned char *)p.x + (int64_t)n * kTile * xp2, kTile * xp2, (uint32_t)xp2, kStep * 2};
+            b = Source{(const unsigned char *)p.x + (int64_t)n * kRows * xp2, kRows * xp2, (uint32_t)xp2, kStep * 2};
         } else if (K == kDx) {
             const int64_t k0 = (int64_t)s * steps * kStep;
             a = Source{(const unsigned char *)p.w + (v0 + k0) * H2 + m * kTile * 2, (p.V - v0 - k0) * H2 - m * kTile * 2, (uint32_t)H2, kStep * H2};
-            b = Source{(const unsigned char *)p.dz + (int64_t)n * kTile * zp2 + k0 * 2, kTile * zp2 - k0 * 2, (uint32_t)zp2, kStep * 2};
+            b = Source{(const unsigned char *)p.dz + (int64_t)n * kRows * zp2 + k0 * 2, kRows * zp2 - k0 * 2, (uint32_t)zp2, kStep * 2};
         } else {
             const int64_t rows = (int64_t)steps * kStep;
             a = Source{(const unsigned char *)p.x + m * kTile * 2, rows * xp2 - m * kTile * 2, (uint32_t)xp2, kStep * xp2};
@@ -266,23 +271,24 @@ __device__ __forceinline__ int here(int x)
 }
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-template <Kind K>
+template <Kind K, int NB>
 __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
 {
     constexpr bool A_COLS = K == kDx || K == kDw, B_COLS = K == kDw;
     // (what the results of a tile need of its rows comes by loads to LDS too, in two places by turns: a load to registers would be waited for
     // together with all that are under way)
-    constexpr int kRowBytes = K == kForward ? kTile * 4 : K == kAgain ? 3 * kTile * 4 : 0;
+    constexpr int kRows = 64 * NB, kBufferBytes = kOperandBytes + 8192 * NB;
+    constexpr int kRowBytes = K == kForward ? kRows * 4 : K == kAgain ? 3 * kRows * 4 : 0;
     __shared__ __align__(1024) unsigned char lds[2 * kBufferBytes + 2 * kRowBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1;
     const int n = lane & 15, g = lane >> 4;
     const int n_rows = __builtin_amdgcn_readfirstlane(*p.n_rows);
-    Product<K> work;
+    Product<K, NB> work;
     work.init(p, n_rows);
 
     const uint32_t a_pitch = (uint32_t)(K == kDw ? p.xp : p.H) * 2, b_pitch = (uint32_t)(K == kDx || K == kDw ? work.zp : p.xp) * 2;
-    Operand<A_COLS> A;
-    Operand<B_COLS> B;
+    Operand<A_COLS, 4> A;
+    Operand<B_COLS, NB> B;
     A.init(lane, wave, wm, a_pitch);
     B.init(lane, wave, wn, b_pitch);
     const uint32_t lds0 = lds_addr(lds);
@@ -313,8 +319,8 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
         Fetch f;
         f.a = c.a.words();
         f.b = c.b.words();
-        A.offsets(lane, c.tail, f.a_off);
-        B.offsets(lane, kStep, f.b_off);
+        A.offsets(lane, wave, c.tail, f.a_off);
+        B.offsets(lane, wave, kStep, f.b_off);
         f.lds = lds0 + c.parity * kBufferBytes;
         c.a.next();
         c.b.next();
@@ -326,17 +332,17 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
     auto load_a = [&](const Fetch &f, int half, int q) { A.fetch(f.a, f.a_off, a_pitch, f.lds, wave, half, q); };
     auto load_b = [&](const Fetch &f, int half, int q) { B.fetch(f.b, f.b_off, b_pitch, f.lds + kOperandBytes, wave, half, q); };
 
-    // A step in two halves of 64 products.  What a half of the blocks needs is read half a step before its first product, so its place
+    // A step in two halves, of 64 products with NB = 4.  What a half of the blocks needs is read half a step before its first product, so its place
     // in LDS is free early, and its loads have a step until they are waited for:
     //   half  products        reads                       loads (of the step after next)
     //   1     A0 B0, A0 B1    B1, A1                      A0 B0
     //   2     A1 B0, A1 B1    A0, B0 of the next step     B1 A1
-    // Each half ends with a barrier: what was read in it may be overwritten, and what the next one reads is there (16 loads are younger).
-    bf16x8 a0[4][2], a1[4][2], b0[4][2], b1[4][2];   // [block of 16][half step]
-    f32x4 acc[8][8];
+    // Each half ends with a barrier: what was read in it may be overwritten, and what the next one reads is there (a step's loads, 16 with NB = 4, are younger).
+    bf16x8 a0[4][2], a1[4][2], b0[NB][2], b1[NB][2];   // [block of 16][half step]
+    f32x4 acc[8][2 * NB];
     auto half_end = [&]() {
         SB();
-        asm volatile("s_waitcnt vmcnt(16) lgkmcnt(0)" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * (4 + NB)) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         SB();
@@ -346,17 +352,25 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
     for (int step = 0; step < 2; ++step) {
         const Fetch f = take(cursor);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) { load_a(f, 0, q); load_b(f, 0, q); }
+        for (int q = 0; q < 4; ++q) {
+            load_a(f, 0, q);
+            if (q < NB) load_b(f, 0, q);
+        }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) { load_b(f, 1, q); load_a(f, 1, q); }
+        for (int q = 0; q < 4; ++q) {
+            if (q < NB) load_b(f, 1, q);
+            load_a(f, 1, q);
+        }
     }
-    asm volatile("s_waitcnt vmcnt(24)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * (4 + NB)) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
+    auto read_a = [&](const unsigned char *t, int half, bf16x8 to[4][2], int i) { to[i & 3][i >> 2] = A.get(t, half, i & 3, i >> 2); };
+    auto read_b = [&](const unsigned char *t, int half, bf16x8 to[NB][2], int i) { to[i % NB][i / NB] = B.get(t + kOperandBytes, half, i % NB, i / NB); };
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        a0[j & 3][j >> 2] = A.get(lds, 0, j & 3, j >> 2);
-        b0[j & 3][j >> 2] = B.get(lds + kOperandBytes, 0, j & 3, j >> 2);
+        read_a(lds, 0, a0, j);
+        if (j < 2 * NB) read_b(lds, 0, b0, j);
     }
     half_end();
 
@@ -366,83 +380,115 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
         work.locate(i, m, nn, s);
         const int steps = work.steps_of(s);
         if (K == kForward || K == kAgain) {
-            const int row0 = nn * kTile + wave * 64;   // (older than a step's 16 loads: there when the first one ends)
-            dma_b32(rsrc_words(p.target + row0, 256), lds0 + row_at + wave * 256, lane * 4, 0);
-            if (K == kAgain) {
-                dma_b32(rsrc_words(p.lse + row0, 256), lds0 + row_at + 1024 + wave * 256, lane * 4, 0);
-                dma_b32(rsrc_words(p.d + row0, 256), lds0 + row_at + 2048 + wave * 256, lane * 4, 0);
+            const int row0 = nn * kRows + wave * 64;   // (older than a step's loads: there when the first one ends)
+            if (wave < NB) {
+                dma_b32(rsrc_words(p.target + row0, 256), lds0 + row_at + wave * 256, lane * 4, 0);
+                if (K == kAgain) {
+                    dma_b32(rsrc_words(p.lse + row0, 256), lds0 + row_at + 4 * kRows + wave * 256, lane * 4, 0);
+                    dma_b32(rsrc_words(p.d + row0, 256), lds0 + row_at + 8 * kRows + wave * 256, lane * 4, 0);
+                }
             }
         }
         const int *row_targets = (const int *)(lds + row_at);
-        const float *row_lse = (const float *)(lds + row_at + 1024), *row_d = (const float *)(lds + row_at + 2048);
+        const float *row_lse = (const float *)(lds + row_at + 4 * kRows), *row_d = (const float *)(lds + row_at + 8 * kRows);
         row_at ^= (2 * kBufferBytes) ^ (2 * kBufferBytes + kRowBytes);
 #pragma unroll
         for (int x = 0; x < 8; ++x)
 #pragma unroll
-            for (int y = 0; y < 8; ++y)
+            for (int y = 0; y < 2 * NB; ++y)
 #pragma unroll
                 for (int v = 0; v < 4; ++v) acc[x][y][v] = 0.0f;
         for (int step = 0; step < steps; ++step) {
             const unsigned char *t = lds + at, *next = lds + (at ^ kBufferBytes);
             const Fetch f = take(cursor);
-            // product j of a quarter: blocks j / 8 and j / 2 % 4, half step j % 2 (two products in a row on one accumulator need less power: 1.7 % of the
-            // time against j / 16 for the half step); between pairs of them at most one read or load, i = j / 2
+            if constexpr (NB == 4) {
+                // Product j of a quarter: blocks j / 8 and j / 2 % 4, half step j % 2 (two products in a row on one accumulator need less power:
+                // 1.7 % of the time against j / 16 for the half step); between pairs of them at most one read or load, i = j / 2.
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                const int k = j & 1, x = j >> 3 & 3, y = j >> 1 & 3, i = j >> 1;
-                acc[x][y] = mfma16(a0[x][k], b0[y][k], acc[x][y]);
-                SB();
-                if (j & 1) continue;
-                if (i < 8) b1[i >> 1][i & 1] = B.get(t + kOperandBytes, 1, i >> 1, i & 1);
-                else if (i & 1) load_b(f, 0, (i - 8) >> 1);
-                else load_a(f, 0, (i - 8) >> 1);
-                SB();
-            }
+                for (int j = 0; j < 32; ++j) {
+                    const int k = j & 1, x = j >> 3 & 3, y = j >> 1 & 3, i = j >> 1;
+                    acc[x][y] = mfma16(a0[x][k], b0[y][k], acc[x][y]);
+                    SB();
+                    if (j & 1) continue;
+                    if (i < 8) b1[i >> 1][i & 1] = B.get(t + kOperandBytes, 1, i >> 1, i & 1);
+                    else if (i & 1) load_b(f, 0, (i - 8) >> 1);
+                    else load_a(f, 0, (i - 8) >> 1);
+                    SB();
+                }
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                const int k = j & 1, x = j >> 3 & 3, y = j >> 1 & 3, i = j >> 1;
-                acc[x][4 + y] = mfma16(a0[x][k], b1[y][k], acc[x][4 + y]);
-                SB();
-                if (j & 1) continue;
-                if (i < 8) a1[i >> 1][i & 1] = A.get(t, 1, i >> 1, i & 1);
-                SB();
-            }
-            half_end();
+                for (int j = 0; j < 32; ++j) {
+                    const int k = j & 1, x = j >> 3 & 3, y = j >> 1 & 3, i = j >> 1;
+                    acc[x][4 + y] = mfma16(a0[x][k], b1[y][k], acc[x][4 + y]);
+                    SB();
+                    if (j & 1) continue;
+                    if (i < 8) a1[i >> 1][i & 1] = A.get(t, 1, i >> 1, i & 1);
+                    SB();
+                }
+                half_end();
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                const int k = j & 1, x = j >> 3 & 3, y = j >> 1 & 3, i = j >> 1;
-                acc[4 + x][y] = mfma16(a1[x][k], b0[y][k], acc[4 + x][y]);
-                SB();
-                if (j & 1) continue;
-                if (i < 8) a0[i >> 1][i & 1] = A.get(next, 0, i >> 1, i & 1);
-                else if (i & 1) load_a(f, 1, (i - 8) >> 1);
-                else load_b(f, 1, (i - 8) >> 1);
-                SB();
-            }
+                for (int j = 0; j < 32; ++j) {
+                    const int k = j & 1, x = j >> 3 & 3, y = j >> 1 & 3, i = j >> 1;
+                    acc[4 + x][y] = mfma16(a1[x][k], b0[y][k], acc[4 + x][y]);
+                    SB();
+                    if (j & 1) continue;
+                    if (i < 8) a0[i >> 1][i & 1] = A.get(next, 0, i >> 1, i & 1);
+                    else if (i & 1) load_a(f, 1, (i - 8) >> 1);
+                    else load_b(f, 1, (i - 8) >> 1);
+                    SB();
+                }
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                const int k = j & 1, x = j >> 3 & 3, y = j >> 1 & 3, i = j >> 1;
-                acc[4 + x][4 + y] = mfma16(a1[x][k], b1[y][k], acc[4 + x][4 + y]);
-                SB();
-                if (j & 1) continue;
-                if (i < 8) b0[i >> 1][i & 1] = B.get(next + kOperandBytes, 0, i >> 1, i & 1);
-                SB();
+                for (int j = 0; j < 32; ++j) {
+                    const int k = j & 1, x = j >> 3 & 3, y = j >> 1 & 3, i = j >> 1;
+                    acc[4 + x][4 + y] = mfma16(a1[x][k], b1[y][k], acc[4 + x][4 + y]);
+                    SB();
+                    if (j & 1) continue;
+                    if (i < 8) b0[i >> 1][i & 1] = B.get(next + kOperandBytes, 0, i >> 1, i & 1);
+                    SB();
+                }
+                half_end();
+            } else {   // (few products: memory is what is waited for, so the loads go first)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) load_a(f, 0, i);
+                load_b(f, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) read_b(t, 1, b1, i);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) read_a(t, 1, a1, i);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[j >> 1][0] = mfma16(a0[j >> 1][j & 1], b0[0][j & 1], acc[j >> 1][0]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[j >> 1][1] = mfma16(a0[j >> 1][j & 1], b1[0][j & 1], acc[j >> 1][1]);
+                half_end();
+                load_b(f, 1, 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) load_a(f, 1, i);
+                bf16x8 b2[1][2];   // (the first products of this half still need b0)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) read_b(next, 0, b2, i);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) read_a(next, 0, a0, i);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[4 + (j >> 1)][0] = mfma16(a1[j >> 1][j & 1], b0[0][j & 1], acc[4 + (j >> 1)][0]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[4 + (j >> 1)][1] = mfma16(a1[j >> 1][j & 1], b1[0][j & 1], acc[4 + (j >> 1)][1]);
+                b0[0][0] = b2[0][0];
+                b0[0][1] = b2[0][1];
+                half_end();
             }
-            half_end();
             at ^= kBufferBytes;
         }
 
         // (the compiler does not see that what follows reads results of the matrix pipe: the distance it would keep)
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
-        // acc[x][y][v] is row 128 wm + 16 x + 4 g + v and column 128 wn + 16 y + n of the tile
+        // acc[x][y][v] is row 128 wm + 16 x + 4 g + v and column 32 NB wn + 16 y + n of the tile
         if (K == kForward) {
             const int strip = m * 2 + wm;
             const int words = p.V - strip * kStrip - 4 * g;   // of the strip, from this lane's first one on
             const bool whole = (m * 2 + wm + 1) * kStrip <= p.V;
-            float most[8], sum[8];   // of this lane's words; the four lanes of a row are put together at the end
+            float most[2 * NB], sum[2 * NB];   // of this lane's words; the four lanes of a row are put together at the end
 #pragma unroll
-            for (int y = 0; y < 8; ++y) {
-                const int in_tile = wn * 128 + y * 16 + n, row = nn * kTile + in_tile;
+            for (int y = 0; y < 2 * NB; ++y) {
+                const int in_tile = wn * 32 * NB + y * 16 + n, row = nn * kRows + in_tile;
                 SB();
                 float z[32];
 #pragma unroll
@@ -480,26 +526,27 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
             }
             SB();
 #pragma unroll
-            for (int y = 0; y < 8; ++y) {
+            for (int y = 0; y < 2 * NB; ++y) {
                 const float all = fmaxf(fmaxf(most[y], __shfl_xor(most[y], 16)), fmaxf(__shfl_xor(most[y], 32), __shfl_xor(most[y], 48)));
                 sum[y] *= fast_exp2((shift_of(most[y]) - shift_of(all)) * kLog2e);
                 most[y] = all;
             }
 #pragma unroll
-            for (int y = 0; y < 8; ++y) sum[y] += __shfl_xor(sum[y], 16);
+            for (int y = 0; y < 2 * NB; ++y) sum[y] += __shfl_xor(sum[y], 16);
 #pragma unroll
-            for (int y = 0; y < 8; ++y) sum[y] += __shfl_xor(sum[y], 32);
-            float2 *out = p.strips + (int64_t)strip * p.Tp + nn * kTile + wn * 128 + n;
+            for (int y = 0; y < 2 * NB; ++y) sum[y] += __shfl_xor(sum[y], 32);
+            float2 *out = p.strips + (int64_t)strip * p.Tp + nn * kRows + wn * 32 * NB + n;
 #pragma unroll
-            for (int y = 0; y < 8; ++y)
+            for (int y = 0; y < 2 * NB; ++y)
                 if (g == (y & 3)) out[y * 16] = make_float2(most[y], sum[y]);
         } else if (K == kAgain) {
             const int word0 = m * kTile + wm * kStrip;   // of the piece
             const int words = p.V - work.v0 - word0 - 4 * g;
             const bool whole = work.v0 + word0 + kStrip <= p.V;
+            const int rows = max(1, (n_rows + kStep - 1) / kStep) * kStep;   // that dW's product reads
 #pragma unroll
-            for (int y = 0; y < 8; ++y) {
-                const int in_tile = wn * 128 + y * 16 + n, row = nn * kTile + in_tile;
+            for (int y = 0; y < 2 * NB; ++y) {
+                const int in_tile = wn * 32 * NB + y * 16 + n, row = nn * kRows + in_tile;
                 const float lse = row_lse[in_tile] * kLog2e, d = row_d[in_tile];
                 const int t = row_targets[in_tile] - work.v0 - word0;
                 const bool hit = __any(t >= 0 && t < kStrip);
@@ -525,20 +572,21 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
                         for (int v = 0; v < 8; ++v)
                             if (16 * (v >> 2) + (v & 3) >= left) e[v] = 0.0f;
                     }
-                    *(uint4 *)(out + x * 16) = eight_of(e, e + 4);
+                    const uint4 u = eight_of(e, e + 4);
+                    if (row < rows) *(uint4 *)(out + x * 16) = u;
                 }
             }
         } else if (K == kDx) {
-            float *out = p.slabs + ((int64_t)(s * work.nt + nn) * kTile + wn * 128) * p.Hp + m * kTile + wm * 128;   // (the same for all lanes)
+            float *out = p.slabs + ((int64_t)(s * work.nt + nn) * kRows + wn * 32 * NB) * p.Hp + m * kTile + wm * 128;   // (the same for all lanes)
             const int cols = p.H - m * kTile - wm * 128;
 #pragma unroll
-            for (int y = 0; y < 8; ++y) {
+            for (int y = 0; y < 2 * NB; ++y) {
                 float *row = out + y * 16 * p.Hp;
                 const uint32_t mine = n * p.Hp + 4 * g;
 #pragma unroll
                 for (int x = 0; x < 8; ++x) {
                     SB();
-                    if (x * 16 + 4 * g < cols) {   // (a whole number of fours)
+                    if (x * 16 + 4 * g < cols && nn * kRows + wn * 32 * NB + y * 16 + n < n_rows) {   // (a whole number of fours)
                         float4 *to = (float4 *)(row + x * 16 + mine);
                         float4 f = make_float4(result(acc[x][y][0]), result(acc[x][y][1]), result(acc[x][y][2]), result(acc[x][y][3]));
                         if (p.piece > 0) {
@@ -552,7 +600,7 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
         } else {
             const int col0 = m * kTile + wm * 128 + 16 * (g & 1) + 8 * (g >> 1);
 #pragma unroll
-            for (int y = 0; y < 8; ++y) {
+            for (int y = 0; y < 2 * NB; ++y) {
                 const int word = work.v0 + nn * kTile + wn * 128 + y * 16 + n;
                 uint16_t *out = p.dw + (int64_t)word * p.H + col0;
 #pragma unroll
@@ -706,10 +754,11 @@ __global__ __launch_bounds__(1024) void loss_sums_kernel(const float2 *strips, i
 
 // dx of every row: the parts' sums, or zeros.
 __global__ __launch_bounds__(256) void loss_dx_kernel(const float *slabs, const int32_t *n_rows, const int32_t *slot, uint16_t *dx, int64_t T, int V, int H, int Hp,
-                                                      int64_t dz_room)
+                                                      int64_t dz_room, int tile_rows)
 {
-    const int tiles = row_tiles_of(*n_rows), splits = dx_splits(tiles * ((H + kTile - 1) / kTile), Piece(tiles, V, H, dz_room).tiles * (kTile / kStep));
-    const int64_t slab = (int64_t)tiles * kTile * Hp;
+    const int n = *n_rows, tiles = max(1, (n + tile_rows - 1) / tile_rows);
+    const int splits = dx_splits(tiles * ((H + kTile - 1) / kTile), Piece(row_tiles_of(n), V, H, dz_room).tiles * (kTile / kStep));
+    const int64_t slab = (int64_t)tiles * tile_rows * Hp;
     const int pieces = H / 4, blocks = (pieces + 255) / 256;   // 4 columns to a thread
     for (int64_t i = blockIdx.x; i < T * blocks; i += gridDim.x) {
         const int64_t t = i / blocks;
@@ -782,6 +831,15 @@ int check(const skrull_loss_t *p)
     return SKRULL_OK;
 }
 
+// Whether the products with rows of x take them 64 at a time, not 256: where no more rows are, so that memory is what is waited for, or where tiles of
+// 256 rows leave compute units without one.  Forward and backward in us, 64 at a time and 256: 37 rows, 896 hidden, 32,003 words 25 and 60, 38 and 80; 64, 3,584,
+// 128,000: 172 and 658, 210 and 724; 128, 896, 32,003: 24 and 66, 37 and 86; 256, 896, 32,003: 34 and 91, 36 and 99; 600, 128, 4,000: 17 and 46, 22 and 62;
+// but 128, 3,584, 128,000: 236 and 823, 218 and 792; 512, 896, 150,000: 210 and 641, 141 and 481.
+bool few_rows(const skrull_loss_t &p)
+{
+    return p.rows <= 64 || (p.rows + 63) / 64 * ((p.vocab + kTile - 1) / kTile) <= 2 * kGrid;
+}
+
 // The first kernel of either direction.
 template <bool BACKWARD>
 hipError_t gather(const skrull_loss_t &p, const Layout &l, unsigned char *ws, const void *x, const int64_t *target, const float *lse, const float *d,
@@ -835,7 +893,8 @@ int skrull_loss_fwd(const skrull_loss_t *p, const void *x, const void *w, const 
         LossArgs a = args_of(*p, l, ws, w);
         a.z_target = (float *)(ws + l.z_target);
         a.strips = (float2 *)(ws + l.strips);
-        loss_product_kernel<kForward><<<kGrid, 256, 0, st>>>(a);
+        if (few_rows(*p)) loss_product_kernel<kForward, 1><<<kGrid, 256, 0, st>>>(a);
+        else loss_product_kernel<kForward, 4><<<kGrid, 256, 0, st>>>(a);
         e = hipGetLastError();
         if (e == hipSuccess) {
             loss_sums_kernel<<<(int)(l.Tp / kSumRows), 1024, 0, st>>>(a.strips, (p->vocab + kTile - 1) / kTile * 2, l.Tp, a.n_rows, (const int32_t *)(ws + l.row), a.z_target, loss, lse);
@@ -868,22 +927,25 @@ int skrull_loss_bwd(const skrull_loss_t *p, const void *x, const void *w, const 
     a.slabs = (float *)(ws + l.slabs);
     a.dw = (uint16_t *)dw;
     a.dz_room = l.dz_room;
+    const bool few = few_rows(*p);
     for (int64_t i = 0; i < l.pieces && e == hipSuccess; ++i) {   // (there may be fewer pieces: the last launches find no tiles then)
         a.piece = (int32_t)i;
-        loss_product_kernel<kAgain><<<kGrid, 256, 0, st>>>(a);
+        if (few) loss_product_kernel<kAgain, 1><<<kGrid, 256, 0, st>>>(a);
+        else loss_product_kernel<kAgain, 4><<<kGrid, 256, 0, st>>>(a);
         e = hipGetLastError();
         if (e == hipSuccess && dx) {
-            loss_product_kernel<kDx><<<kGrid, 256, 0, st>>>(a);
+            if (few) loss_product_kernel<kDx, 1><<<kGrid, 256, 0, st>>>(a);
+            else loss_product_kernel<kDx, 4><<<kGrid, 256, 0, st>>>(a);
             e = hipGetLastError();
         }
         if (e == hipSuccess && dw) {
-            loss_product_kernel<kDw><<<kGrid, 256, 0, st>>>(a);
+            loss_product_kernel<kDw, 4><<<kGrid, 256, 0, st>>>(a);
             e = hipGetLastError();
         }
     }
     if (e == hipSuccess && dx && p->rows > 0) {
 const int64_t blocks = p->rows * ((p->hidden / 4 + 255) / 256);
-        loss_dx_kernel<<<(int)(blocks < 4096 ? blocks : 4096), 256, 0, st>>>(a.slabs, a.n_rows, (const int32_t *)(ws + l.slot), (uint16_t *)dx, p->rows, p->vocab, p->hidden, (int)l.Hp, l.dz_room);
+        loss_dx_kernel<<<(int)(blocks < 4096 ? blocks : 4096), 256, 0, st>>>(a.slabs, a.n_rows, (const int32_t *)(ws + l.slot), (uint16_t *)dx, p->rows, p->vocab, p->hidden, (int)l.Hp, l.dz_room, few ? 64 : kTile);
         e = hipGetLastError();
     }
     return e == hipSuccess ? SKRULL_OK : launch_failed(e, "loss launch");
