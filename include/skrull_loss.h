@@ -12,7 +12,8 @@
  *
  * The products run on the matrix cores in bf16 with fp32 sums; logits stay in fp32 registers.  The backward
  * forms them again, in pieces of the vocabulary that fit the workspace, and rounds dz to bf16 (by 2^-8 relative to
- * its value at most, as x and w are) for the two products with w and x.  dx and dw are summed in fp32 and rounded to bf16 once.
+ * its value at most, as x and w are; where up to 128 rows have a target, to the sum of two bf16, by 2^-16) for the two products with w and x.
+ * dx and dw are summed in fp32 and rounded to bf16 once.
  * No sum depends on the order in which workgroups run: results are bit-reproducible.
  *
  * Tensors are caller-owned DEVICE memory: x bf16 [rows, hidden], row t x_stride elements after row t - 1; w bf16 [vocab, hidden]

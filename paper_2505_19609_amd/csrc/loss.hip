@@ -33,6 +33,10 @@ constexpr int64_t kPieceBytes = (int64_t)2 << 30;  // of dz at most
 // Rows of dz and of the gathered x are this much longer where their length is a multiple of 4 KB: the 256 rows of a tile would lie in few of the L2's sets.
 constexpr int kPitchPad = 64;
 constexpr int kMaxPieceWords = 1 << 20;            // (32-bit offsets within a tile of dz)
+// With so few rows or fewer the backward has each of them twice, the second time with what rounding dz to bf16 leaves: dx and dw are as exact as with dz in
+// 16 bits.  It costs little, since a tile has 256 rows (64 rows, 3,584 hidden, 128,000 words: 728 us and not 657).  (Where many rows add up, dz's roundings cost as much as the
+// result's own: 2.4e-3 of a gradient's norm against 1.7e-3.  A single row's are all or nothing.)
+constexpr int kTwice = kTile / 2;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // What is taken off logits whose largest one this is: nothing where there is no word at all, or an infinite logit, so that a sum is 0 or infinite
@@ -45,7 +49,7 @@ struct LossArgs {
     const uint16_t *x;       // gathered rows [.., xp], Hp of them used
     const uint16_t *w;       // [V, H]
     uint16_t *dz;            // [.., zp], vc of them used
-    const int32_t *n_rows;   // rows that have a target
+    const int32_t *n_rows;   // rows of dz, of them rows that have a target (the second time they begin at the next multiple of 64)
     const int32_t *target;   // of the gathered rows
     const float *lse, *d;    // of the gathered rows (kAgain)
     float *z_target;         // of the gathered rows (kForward)
@@ -118,7 +122,7 @@ struct Source {
 //         that a transposing read takes together are 16 different slots too.
 template <bool COLS, int NB>
 struct Operand {
-    static_assert(NB == 4 || (NB == 1 && !COLS), "");
+    static_assert(NB == 4 || !COLS, "");
     static constexpr int kHalfBytes = 4096 * NB;
     int load[2];     // byte offsets of this lane's pieces in the tile's matrix: of even and odd instructions (COLS: of the first and the last two)
     int read[4];     // LDS offsets of its fragments: ROWS by half step (two), COLS by block of 16 columns
@@ -282,7 +286,7 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
     __shared__ __align__(1024) unsigned char lds[2 * kBufferBytes + 2 * kRowBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1;
     const int n = lane & 15, g = lane >> 4;
-    const int n_rows = __builtin_amdgcn_readfirstlane(*p.n_rows);
+    const int n_rows = __builtin_amdgcn_readfirstlane(p.n_rows[K == kForward || K == kAgain]);
     Product<K, NB> work;
     work.init(p, n_rows);
 
@@ -446,33 +450,37 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
                     SB();
                 }
                 half_end();
-            } else {   // (few products: memory is what is waited for, so the loads go first)
+            } else {   // (fewer products: memory is what is waited for, so the loads go first)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) load_a(f, 0, i);
-                load_b(f, 0, 0);
 #pragma unroll
-                for (int i = 0; i < 2; ++i) read_b(t, 1, b1, i);
+                for (int i = 0; i < NB; ++i) load_b(f, 0, i);
+#pragma unroll
+                for (int i = 0; i < 2 * NB; ++i) read_b(t, 1, b1, i);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) read_a(t, 1, a1, i);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) acc[j >> 1][0] = mfma16(a0[j >> 1][j & 1], b0[0][j & 1], acc[j >> 1][0]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[j >> 1][1] = mfma16(a0[j >> 1][j & 1], b1[0][j & 1], acc[j >> 1][1]);
+                for (int j = 0; j < 16 * NB; ++j) {   // block of 16 rows of B, of A, half step
+                    const int y = j / 8, x = j / 2 % 4, k = j & 1;
+                    acc[x][y] = mfma16(a0[x][k], y < NB ? b0[y][k] : b1[y - NB][k], acc[x][y]);
+                }
                 half_end();
-                load_b(f, 1, 0);
+#pragma unroll
+                for (int i = 0; i < NB; ++i) load_b(f, 1, i);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) load_a(f, 1, i);
-                bf16x8 b2[1][2];   // (the first products of this half still need b0)
+                bf16x8 b2[NB][2];   // (the first products of this half still need b0)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) read_b(next, 0, b2, i);
+                for (int i = 0; i < 2 * NB; ++i) read_b(next, 0, b2, i);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) read_a(next, 0, a0, i);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) acc[4 + (j >> 1)][0] = mfma16(a1[j >> 1][j & 1], b0[0][j & 1], acc[4 + (j >> 1)][0]);
+                for (int j = 0; j < 16 * NB; ++j) {
+                    const int y = j / 8, x = j / 2 % 4, k = j & 1;
+                    acc[4 + x][y] = mfma16(a1[x][k], y < NB ? b0[y][k] : b1[y - NB][k], acc[4 + x][y]);
+                }
 #pragma unroll
-                for (int j = 0; j < 8; ++j) acc[4 + (j >> 1)][1] = mfma16(a1[j >> 1][j & 1], b1[0][j & 1], acc[4 + (j >> 1)][1]);
-                b0[0][0] = b2[0][0];
-                b0[0][1] = b2[0][1];
+                for (int i = 0; i < 2 * NB; ++i) b0[i / 2][i & 1] = b2[i / 2][i & 1];
                 half_end();
             }
             at ^= kBufferBytes;
@@ -544,6 +552,7 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
             const int words = p.V - work.v0 - word0 - 4 * g;
             const bool whole = work.v0 + word0 + kStrip <= p.V;
             const int rows = max(1, (n_rows + kStep - 1) / kStep) * kStep;   // that dW's product reads
+            const bool twice = p.n_rows[0] > rows;
 #pragma unroll
             for (int y = 0; y < 2 * NB; ++y) {
                 const int in_tile = wn * 32 * NB + y * 16 + n, row = nn * kRows + in_tile;
@@ -574,6 +583,12 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
                     }
                     const uint4 u = eight_of(e, e + 4);
                     if (row < rows) *(uint4 *)(out + x * 16) = u;
+                    if (twice) {
+#pragma unroll
+                        for (int v = 0; v < 8; ++v) e[v] -= __builtin_bit_cast(float, pack_bf16(0.0f, e[v]) & 0xffff0000u);
+                        const uint4 rest = eight_of(e, e + 4);
+                        if (row < rows) *(uint4 *)(out + (int64_t)rows * work.zp + x * 16) = rest;
+                    }
                 }
             }
         } else if (K == kDx) {
@@ -628,7 +643,7 @@ struct GatherArgs {
     const float *lse, *d;    // [T], backward
     int64_t T;
     int32_t V, H, Hp, xp, each, wide;
-    int32_t *n_rows, *slot, *row, *target_of;  // count; [T] gathered row or -1; [Tp] its row; [Tp] its target
+    int32_t *n_rows, *slot, *row, *target_of;  // [2], see LossArgs; [T] gathered row or -1; [Tp] its row; [Tp] its target
     uint16_t *out;           // [Tp][xp]
     float *lse_of, *d_of;    // [Tp], backward
     float *loss, *lse_out;   // [T], forward: zeros where there is no target
@@ -665,7 +680,12 @@ __global__ __launch_bounds__(64 * kGatherWaves) void loss_gather_kernel(const Ga
         at += counts[0][k];
         n += counts[1][k];
     }
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.n_rows = n;
+    const bool twice = BACKWARD && n > 0 && n <= kTwice;
+    const int again = (n + kStep - 1) / kStep * kStep;   // the second time
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        a.n_rows[0] = twice ? 2 * again : n;
+        a.n_rows[1] = n;
+    }
 
     for (int64_t t0 = first; t0 < end; t0 += 64) {
         const int64_t t = t0 + lane, target = t < end ? a.target[t] : -1;
@@ -706,17 +726,19 @@ __global__ __launch_bounds__(64 * kGatherWaves) void loss_gather_kernel(const Ga
                     }
                 }
                 *(uint4 *)(to + c) = v;
+                if (twice) *(uint4 *)(to + (int64_t)again * a.xp + c) = v;
             }
         }
         at += __popcll(has);
     }
     const int padded = row_tiles_of(n) * kTile;
     for (int r = n + blockIdx.x; r < padded; r += gridDim.x) {   // rows that fill the last tile: no gradient, no word
-        for (int c = threadIdx.x * 8; c < a.Hp; c += 64 * kGatherWaves * 8) *(uint4 *)(a.out + (int64_t)r * a.xp + c) = make_uint4(0, 0, 0, 0);
         if (threadIdx.x == 0) {
             a.target_of[r] = -1;
             if (BACKWARD) { a.lse_of[r] = 0.0f; a.d_of[r] = 0.0f; }
         }
+        if (twice && r >= again && r < again + n) continue;
+        for (int c = threadIdx.x * 8; c < a.Hp; c += 64 * kGatherWaves * 8) *(uint4 *)(a.out + (int64_t)r * a.xp + c) = make_uint4(0, 0, 0, 0);
     }
 }
 
@@ -756,7 +778,7 @@ __global__ __launch_bounds__(1024) void loss_sums_kernel(const float2 *strips, i
 __global__ __launch_bounds__(256) void loss_dx_kernel(const float *slabs, const int32_t *n_rows, const int32_t *slot, uint16_t *dx, int64_t T, int V, int H, int Hp,
                                                       int64_t dz_room, int tile_rows)
 {
-    const int n = *n_rows, tiles = max(1, (n + tile_rows - 1) / tile_rows);
+    const int n = n_rows[0], again = (n_rows[1] + kStep - 1) / kStep * kStep, tiles = max(1, (n + tile_rows - 1) / tile_rows);
     const int splits = dx_splits(tiles * ((H + kTile - 1) / kTile), Piece(row_tiles_of(n), V, H, dz_room).tiles * (kTile / kStep));
     const int64_t slab = (int64_t)tiles * tile_rows * Hp;
     const int pieces = H / 4, blocks = (pieces + 255) / 256;   // 4 columns to a thread
@@ -779,6 +801,16 @@ __global__ __launch_bounds__(256) void loss_dx_kernel(const float *slabs, const 
                 const float4 u = *(const float4 *)from;
                 f.x += u.x; f.y += u.y; f.z += u.z; f.w += u.w;
             }
+            if (n > again) {   // what was left of it
+                from = slabs + (int64_t)(s + again) * Hp + c;
+                float4 rest = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+                for (k = 0; k < splits; ++k) {
+                    const float4 u = *(const float4 *)(from + k * slab);
+                    rest.x += u.x; rest.y += u.y; rest.z += u.z; rest.w += u.w;
+                }
+                f.x += rest.x; f.y += rest.y; f.z += rest.z; f.w += rest.w;
+            }
         }
         *(uint2 *)(dx + t * H + c) = make_uint2(pack_bf16(f.x, f.y), pack_bf16(f.z, f.w));
     }
@@ -797,7 +829,7 @@ struct Layout {
         const int64_t words = ((int64_t)p.vocab + kTile - 1) / kTile * kTile;
         bytes = dz_room = pieces = 0;
         auto take = [&](int64_t n) { const int64_t at = bytes; bytes += (n + 255) & ~(int64_t)255; return at; };
-        n_rows = take(4);
+        n_rows = take(8);
         slot = take(p.rows * 4);
         row = take(Tp * 4);
         target = take(Tp * 4);
@@ -831,13 +863,34 @@ int check(const skrull_loss_t *p)
     return SKRULL_OK;
 }
 
-// Whether the products with rows of x take them 64 at a time, not 256: where no more rows are, so that memory is what is waited for, or where tiles of
-// 256 rows leave compute units without one.  Forward and backward in us, 64 at a time and 256: 37 rows, 896 hidden, 32,003 words 25 and 60, 38 and 80; 64, 3,584,
-// 128,000: 172 and 658, 210 and 724; 128, 896, 32,003: 24 and 66, 37 and 86; 256, 896, 32,003: 34 and 91, 36 and 99; 600, 128, 4,000: 17 and 46, 22 and 62;
-// but 128, 3,584, 128,000: 236 and 823, 218 and 792; 512, 896, 150,000: 210 and 641, 141 and 481.
-bool few_rows(const skrull_loss_t &p)
+// How many rows of x the products with the vocabulary's words take at a time: 64 where tiles of 256 leave compute units without one, as many as there
+// are where they are up to 128, so that memory is what is waited for.  In us, of the forward:
+//   rows, hidden, words     64 at a time  128  256
+//   37, 896, 32,003                   25         38
+//   64, 3,584, 128,000               172        210
+//   128, 896, 32,003                  24   29    37
+//   128, 3,584, 128,000              236  181   215
+//   192, 896, 150,000                 90         89
+//   256, 896, 32,003                  34         36
+//   512, 896, 150,000                210        141
+int tile_rows_of(int64_t rows, int vocab)
 {
-    return p.rows <= 64 || (p.rows + 63) / 64 * ((p.vocab + kTile - 1) / kTile) <= 2 * kGrid;
+    if (rows <= 64 || (rows + 63) / 64 * ((vocab + kTile - 1) / kTile) <= 2 * kGrid) return 64;
+    return rows <= 128 ? 128 : kTile;
+}
+// The same of dX's product, whose parts fill the compute units anyhow.  Up to kTwice rows may be there twice.
+int dx_tile_rows_of(int64_t rows)
+{
+    if (rows <= kTwice) rows = 2 * ((rows + kStep - 1) / kStep * kStep);
+    return rows <= 128 ? 128 : kTile;
+}
+template <Kind K>
+hipError_t launch(int tile_rows, const LossArgs &a, hipStream_t st)
+{
+    if (tile_rows == 64) loss_product_kernel<K, 1><<<kGrid, 256, 0, st>>>(a);
+    else if (tile_rows == 128) loss_product_kernel<K, 2><<<kGrid, 256, 0, st>>>(a);
+    else loss_product_kernel<K, 4><<<kGrid, 256, 0, st>>>(a);
+    return hipGetLastError();
 }
 
 // The first kernel of either direction.
@@ -893,9 +946,7 @@ int skrull_loss_fwd(const skrull_loss_t *p, const void *x, const void *w, const 
         LossArgs a = args_of(*p, l, ws, w);
         a.z_target = (float *)(ws + l.z_target);
         a.strips = (float2 *)(ws + l.strips);
-        if (few_rows(*p)) loss_product_kernel<kForward, 1><<<kGrid, 256, 0, st>>>(a);
-        else loss_product_kernel<kForward, 4><<<kGrid, 256, 0, st>>>(a);
-        e = hipGetLastError();
+        e = launch<kForward>(tile_rows_of(p->rows, p->vocab), a, st);
         if (e == hipSuccess) {
             loss_sums_kernel<<<(int)(l.Tp / kSumRows), 1024, 0, st>>>(a.strips, (p->vocab + kTile - 1) / kTile * 2, l.Tp, a.n_rows, (const int32_t *)(ws + l.row), a.z_target, loss, lse);
             e = hipGetLastError();
@@ -927,14 +978,13 @@ int skrull_loss_bwd(const skrull_loss_t *p, const void *x, const void *w, const 
     a.slabs = (float *)(ws + l.slabs);
     a.dw = (uint16_t *)dw;
     a.dz_room = l.dz_room;
-    const bool few = few_rows(*p);
+    const int tile_rows = tile_rows_of(p->rows, p->vocab);
+    const int dx_rows = dx_tile_rows_of(p->rows);
     for (int64_t i = 0; i < l.pieces && e == hipSuccess; ++i) {   // (there may be fewer pieces: the last launches find no tiles then)
         a.piece = (int32_t)i;
-        if (few) loss_product_kernel<kAgain, 1><<<kGrid, 256, 0, st>>>(a);
-        else loss_product_kernel<kAgain, 4><<<kGrid, 256, 0, st>>>(a);
-        e = hipGetLastError();
+        e = launch<kAgain>(tile_rows, a, st);
         if (e == hipSuccess && dx) {
-            if (few) loss_product_kernel<kDx, 1><<<kGrid, 256, 0, st>>>(a);
+            if (dx_rows == 128) loss_product_kernel<kDx, 2><<<kGrid, 256, 0, st>>>(a);
             else loss_product_kernel<kDx, 4><<<kGrid, 256, 0, st>>>(a);
             e = hipGetLastError();
         }
@@ -945,7 +995,7 @@ int skrull_loss_bwd(const skrull_loss_t *p, const void *x, const void *w, const 
     }
     if (e == hipSuccess && dx && p->rows > 0) {
 const int64_t blocks = p->rows * ((p->hidden / 4 + 255) / 256);
-        loss_dx_kernel<<<(int)(blocks < 4096 ? blocks : 4096), 256, 0, st>>>(a.slabs, a.n_rows, (const int32_t *)(ws + l.slot), (uint16_t *)dx, p->rows, p->vocab, p->hidden, (int)l.Hp, l.dz_room, few ? 64 : kTile);
+        loss_dx_kernel<<<(int)(blocks < 4096 ? blocks : 4096), 256, 0, st>>>(a.slabs, a.n_rows, (const int32_t *)(ws + l.slot), (uint16_t *)dx, p->rows, p->vocab, p->hidden, (int)l.Hp, l.dz_room, dx_rows);
         e = hipGetLastError();
     }
     return e == hipSuccess ? SKRULL_OK : launch_failed(e, "loss launch");

@@ -696,3 +696,22 @@ def test_graph_replays_equal_eager():
         for n, t in out.items():
             assert torch.equal(t, eager[n]), (rep, n)
     plan.destroy()
+
+
+@pytest.mark.parametrize("rows", [1, 5, 64, 128])
+def test_loss_of_few_rows_is_as_exact_as_its_result_s_type(rows):
+    """Up to 128 rows dz is two bf16, so that rounding it (2^-16) is not seen beside the result's own rounding."""
+    from paper_2505_19609_amd.autograd import skrull_cross_entropy
+    x, w, target, d = _loss_case(300, 200, 900, 0.0)
+    target[rows:] = -1
+    x.requires_grad_(), w.requires_grad_()
+    dx, dw = torch.autograd.grad(skrull_cross_entropy(x, w, target), (x, w), d)
+    want = _loss_in_64_bits(x.detach(), w.detach(), target, d)
+    dz = d.double()[:rows, None].abs() * torch.ones(1, 900, dtype=torch.float64, device="cuda")   # (no dz is larger)
+    p = (x.detach()[:rows].double() @ w.detach().double().t()).softmax(1)
+    p[torch.arange(rows), target[:rows]] -= 1.0
+    dz = dz * p.abs()
+    xs, ws = x.detach().double().abs()[:rows], w.detach().double().abs()
+    for got, exact, size in ((dx[:rows], want["dx"][0][:rows], dz @ ws), (dw, want["dw"][0], dz.t() @ xs)):
+        # 2^-16 of every dz, 2^-8 of the result, and 2^-12 of dz for the sums and the logits' errors (their own bound, in the tests above, is of the order H 2^-24 = 2^-16)
+        _within(got, exact, BF16 * exact.abs() + 2.0 ** -12 * size + TINY, rows)
