@@ -35,7 +35,7 @@ extern "C" {
 typedef struct {
     int64_t rows;      /* 0..2^24; with no rows nothing but dw is written, as zeros             */
     int32_t hidden;    /* a multiple of 8, 8..65536                                             */
-    int32_t vocab;     /* 1..2^24                                                               */
+    int32_t vocab;     /* 1..2^22                                                               */
     int64_t x_stride;  /* elements, at least hidden                                             */
 } skrull_loss_t;
 

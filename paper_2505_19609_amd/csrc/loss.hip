@@ -9,13 +9,15 @@
 //            and again             the backward writes dz = d (exp(z - lse) - [word = target]) in bf16, a piece of the vocabulary at a time
 //   dX       dz W                  fp32, added up over the pieces (and over parts of the vocabulary where there are few tiles)
 //   dW^T     X^T dz                a piece's rows of dW are complete after one product
-// What bounds them is the matrix pipe: 2 T V H operations each, against 2 (T + V) H bytes.
+// What bounds them is the matrix pipe: 2 T V H operations each, against 2 (T + V) H bytes; with few rows reading W.
 //
 // A workgroup is 4 wavefronts, one per SIMD, and forms a tile of 256 x 256: each wavefront 128 x 128, 8 x 8 results of
 // v_mfma_f32_16x16x32_bf16 in 256 accumulator registers, so that an operand fragment read from LDS feeds eight products.  Steps of 64 along
 // the contraction lie in two LDS buffers of 64 KB, filled by loads that write LDS directly.
 // The chip's power decides the clock under such products, and with it what an instruction is worth: with normally distributed operands in registers and
-// nothing else, 16 x 16 x 32 runs at 2,010 TFLOP/s, 32 x 32 x 16 (which moves each accumulator twice as often) at 1,705.
+// nothing else, 16 x 16 x 32 runs at 2,010 TFLOP/s, 32 x 32 x 16 (which moves each accumulator twice as often) at 1,705.  Here it is 1,340 to 1,400 (13,312 rows, 3,584
+// hidden, 131,072 words: forward 9.0 ms, backward 28.1; products of this size by the library run at 1,440 to 1,520 on the same chip), whether the steps' barriers and
+// waits are there or not: without them the matrix pipe is busier and the clock lower.
 #include <math.h>
 
 #include "ops.h"
@@ -37,7 +39,7 @@ constexpr int kMaxPieceWords = 1 << 20;            // (32-bit offsets within a t
 // 16 bits.  It costs little, since a tile has 256 rows (64 rows, 3,584 hidden, 128,000 words: 728 us and not 657).  (Where many rows add up, dz's roundings cost as much as the
 // result's own: 2.4e-3 of a gradient's norm against 1.7e-3.  A single row's are all or nothing.)
 constexpr int kTwice = kTile / 2;
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kLog2e = 1.44269504088896340736f;
 
 // What is taken off logits whose largest one this is: nothing where there is no word at all, or an infinite logit, so that a sum is 0 or infinite
 // and not NaN.
@@ -48,7 +50,7 @@ enum Kind { kForward, kAgain, kDx, kDw };
 struct LossArgs {
     const uint16_t *x;       // gathered rows [.., xp], Hp of them used
     const uint16_t *w;       // [V, H]
-    uint16_t *dz;            // [.., zp], vc of them used
+    uint16_t *dz;            // [.., pitch of the pieces]
     const int32_t *n_rows;   // rows of dz, of them rows that have a target (the second time they begin at the next multiple of 64)
     const int32_t *target;   // of the gathered rows
     const float *lse, *d;    // of the gathered rows (kAgain)
@@ -858,7 +860,7 @@ int check(const skrull_loss_t *p)
     if (!p) return refuse("loss: null pointer");
     if (p->rows < 0 || p->rows > 1 << 24) return refuse("loss: %lld rows", (long long)p->rows);
     if (p->hidden < 8 || p->hidden > 65536 || p->hidden % 8 != 0) return refuse("loss: hidden %d is not a multiple of 8 from 8 to 65536", p->hidden);
-    if (p->vocab < 1 || p->vocab > 1 << 24) return refuse("loss: vocab %d", p->vocab);
+    if (p->vocab < 1 || p->vocab > 1 << 22) return refuse("loss: vocab %d", p->vocab);
     if (p->x_stride < p->hidden || p->x_stride > (int64_t)1 << 32) return refuse("loss: x_stride %lld", (long long)p->x_stride);
     return SKRULL_OK;
 }
@@ -878,11 +880,13 @@ int tile_rows_of(int64_t rows, int vocab)
     if (rows <= 64 || (rows + 63) / 64 * ((vocab + kTile - 1) / kTile) <= 2 * kGrid) return 64;
     return rows <= 128 ? 128 : kTile;
 }
-// The same of dX's product, whose parts fill the compute units anyhow.  Up to kTwice rows may be there twice.
-int dx_tile_rows_of(int64_t rows)
+// The same of dX's product, whose parts fill the compute units: 64 where even so the tiles are few (256 rows, 896 hidden, 32,003 words: backward 91 us,
+// 96 with 256; 600, 128, 4,000: 48 and 55; but 512, 896, 150,000: 562 and 480).  Up to kTwice rows may be there twice.
+int dx_tile_rows_of(int64_t rows, int hidden)
 {
     if (rows <= kTwice) rows = 2 * ((rows + kStep - 1) / kStep * kStep);
-    return rows <= 128 ? 128 : kTile;
+    if (rows <= 128) return 128;
+    return (rows + 63) / 64 * ((hidden + kTile - 1) / kTile) <= 16 ? 64 : kTile;
 }
 template <Kind K>
 hipError_t launch(int tile_rows, const LossArgs &a, hipStream_t st)
@@ -979,14 +983,12 @@ int skrull_loss_bwd(const skrull_loss_t *p, const void *x, const void *w, const 
     a.dw = (uint16_t *)dw;
     a.dz_room = l.dz_room;
     const int tile_rows = tile_rows_of(p->rows, p->vocab);
-    const int dx_rows = dx_tile_rows_of(p->rows);
+    const int dx_rows = dx_tile_rows_of(p->rows, p->hidden);
     for (int64_t i = 0; i < l.pieces && e == hipSuccess; ++i) {   // (there may be fewer pieces: the last launches find no tiles then)
         a.piece = (int32_t)i;
         e = launch<kAgain>(tile_rows, a, st);
         if (e == hipSuccess && dx) {
-            if (dx_rows == 128) loss_product_kernel<kDx, 2><<<kGrid, 256, 0, st>>>(a);
-            else loss_product_kernel<kDx, 4><<<kGrid, 256, 0, st>>>(a);
-            e = hipGetLastError();
+            e = launch<kDx>(dx_rows, a, st);
         }
         if (e == hipSuccess && dw) {
             loss_product_kernel<kDw, 4><<<kGrid, 256, 0, st>>>(a);

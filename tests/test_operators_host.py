@@ -105,7 +105,7 @@ def _loss(**kw):
     return B.Loss(**p)
 
 
-BAD_LOSSES = [dict(rows=-1), dict(rows=(1 << 24) + 1), dict(hidden=0), dict(hidden=60), dict(hidden=65544, x_stride=65544), dict(vocab=0), dict(vocab=(1 << 24) + 1),
+BAD_LOSSES = [dict(rows=-1), dict(rows=(1 << 24) + 1), dict(hidden=0), dict(hidden=60), dict(hidden=65544, x_stride=65544), dict(vocab=0), dict(vocab=(1 << 22) + 1),
               dict(x_stride=63)]
 
 
