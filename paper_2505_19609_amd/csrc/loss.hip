@@ -734,13 +734,13 @@ __global__ __launch_bounds__(64 * kGatherWaves) void loss_gather_kernel(const Ga
         at += __popcll(has);
     }
     const int padded = row_tiles_of(n) * kTile;
-    for (int r = n + blockIdx.x; r < padded; r += gridDim.x) {   // rows that fill the last tile: no gradient, no word
-        if (threadIdx.x == 0) {
+    for (int r = n + blockIdx.x + wave * gridDim.x; r < padded; r += gridDim.x * kGatherWaves) {   // rows that fill the last tile: no gradient, no word
+        if (lane == 0) {
             a.target_of[r] = -1;
             if (BACKWARD) { a.lse_of[r] = 0.0f; a.d_of[r] = 0.0f; }
         }
         if (twice && r >= again && r < again + n) continue;
-        for (int c = threadIdx.x * 8; c < a.Hp; c += 64 * kGatherWaves * 8) *(uint4 *)(a.out + (int64_t)r * a.xp + c) = make_uint4(0, 0, 0, 0);
+        for (int c = lane * 8; c < a.Hp; c += 64 * 8) *(uint4 *)(a.out + (int64_t)r * a.xp + c) = make_uint4(0, 0, 0, 0);
     }
 }
 
@@ -776,46 +776,52 @@ __global__ __launch_bounds__(1024) void loss_sums_kernel(const float2 *strips, i
     }
 }
 
-// dx of every row: the parts' sums, or zeros.
+// dx of every row: the parts' sums, or zeros.  A thread has 4 columns, SHARES threads share their parts: 4 where there are 32 parts or more, whose loads
+// would be many waits one after another (37 rows, 896 hidden, 63 parts: 5.5 us, 10.0 by one thread; 2,000 rows, 8 parts: 22.6, 16.4 by one).
+template <int SHARES>
+__device__ __forceinline__ void sum_parts(const float *slabs, int64_t slab, int splits, int64_t rest, const int32_t *slot, uint16_t *dx, int64_t T, int H, int Hp)
+{
+    constexpr int kThreads = 256 / SHARES;
+    __shared__ float4 part[SHARES][SHARES > 1 ? kThreads : 1];
+    const int share = threadIdx.x / kThreads, blocks = (H / 4 + kThreads - 1) / kThreads;
+    for (int64_t i = blockIdx.x; i < T * blocks; i += gridDim.x) {
+        const int64_t t = i / blocks;
+        const int c = ((int)(i - t * blocks) * kThreads + threadIdx.x % kThreads) * 4, s = slot[t];
+        float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        auto add = [&](float4 u) { f.x += u.x; f.y += u.y; f.z += u.z; f.w += u.w; };
+        if (s >= 0 && c < H) {
+            const float *from = slabs + (int64_t)s * Hp + c + share * slab;
+            for (int times = rest ? 2 : 1; times > 0; --times, from = slabs + (int64_t)s * Hp + c + share * slab + rest) {
+                int k = share;
+                for (; k + 7 * SHARES < splits; k += 8 * SHARES, from += 8 * SHARES * slab) {
+                    float4 u[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) u[j] = *(const float4 *)(from + j * SHARES * slab);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) add(u[j]);
+                }
+                for (; k < splits; k += SHARES, from += SHARES * slab) add(*(const float4 *)from);
+            }
+        }
+        if constexpr (SHARES > 1) {
+            __syncthreads();   // (what the row before left is read)
+            part[share][threadIdx.x % kThreads] = f;
+            __syncthreads();
+            if (share == 0)
+#pragma unroll
+                for (int k = 1; k < SHARES; ++k) add(part[k][threadIdx.x]);
+        }
+        if (share == 0 && c < H) *(uint2 *)(dx + t * H + c) = make_uint2(pack_bf16(f.x, f.y), pack_bf16(f.z, f.w));
+    }
+}
 __global__ __launch_bounds__(256) void loss_dx_kernel(const float *slabs, const int32_t *n_rows, const int32_t *slot, uint16_t *dx, int64_t T, int V, int H, int Hp,
                                                       int64_t dz_room, int tile_rows)
 {
     const int n = n_rows[0], again = (n_rows[1] + kStep - 1) / kStep * kStep, tiles = max(1, (n + tile_rows - 1) / tile_rows);
     const int splits = dx_splits(tiles * ((H + kTile - 1) / kTile), Piece(row_tiles_of(n), V, H, dz_room).tiles * (kTile / kStep));
-    const int64_t slab = (int64_t)tiles * tile_rows * Hp;
-    const int pieces = H / 4, blocks = (pieces + 255) / 256;   // 4 columns to a thread
-    for (int64_t i = blockIdx.x; i < T * blocks; i += gridDim.x) {
-        const int64_t t = i / blocks;
-        const int c = ((int)(i - t * blocks) * 256 + threadIdx.x) * 4, s = slot[t];
-        if (c >= H) continue;
-        float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (s >= 0) {
-            const float *from = slabs + (int64_t)s * Hp + c;
-            int k = 0;
-            for (; k + 8 <= splits; k += 8, from += 8 * slab) {
-                float4 u[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) u[j] = *(const float4 *)(from + j * slab);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) { f.x += u[j].x; f.y += u[j].y; f.z += u[j].z; f.w += u[j].w; }
-            }
-            for (; k < splits; ++k, from += slab) {
-                const float4 u = *(const float4 *)from;
-                f.x += u.x; f.y += u.y; f.z += u.z; f.w += u.w;
-            }
-            if (n > again) {   // what was left of it
-                from = slabs + (int64_t)(s + again) * Hp + c;
-                float4 rest = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 8
-                for (k = 0; k < splits; ++k) {
-                    const float4 u = *(const float4 *)(from + k * slab);
-                    rest.x += u.x; rest.y += u.y; rest.z += u.z; rest.w += u.w;
-                }
-                f.x += rest.x; f.y += rest.y; f.z += rest.z; f.w += rest.w;
-            }
-        }
-        *(uint2 *)(dx + t * H + c) = make_uint2(pack_bf16(f.x, f.y), pack_bf16(f.z, f.w));
-    }
+    const int64_t slab = (int64_t)tiles * tile_rows * Hp, rest = n > again ? (int64_t)again * Hp : 0;   // rest: to the products of what was left of dz
+    if (splits >= 32) sum_parts<4>(slabs, slab, splits, rest, slot, dx, T, H, Hp);
+    else sum_parts<1>(slabs, slab, splits, rest, slot, dx, T, H, Hp);
 }
 
 // The workspace, from sizes alone.
@@ -996,7 +1002,7 @@ int skrull_loss_bwd(const skrull_loss_t *p, const void *x, const void *w, const 
         }
     }
     if (e == hipSuccess && dx && p->rows > 0) {
-const int64_t blocks = p->rows * ((p->hidden / 4 + 255) / 256);
+        const int64_t blocks = p->rows * ((p->hidden / 4 + 63) / 64);
         loss_dx_kernel<<<(int)(blocks < 4096 ? blocks : 4096), 256, 0, st>>>(a.slabs, a.n_rows, (const int32_t *)(ws + l.slot), (uint16_t *)dx, p->rows, p->vocab, p->hidden, (int)l.Hp, l.dz_room, dx_rows);
         e = hipGetLastError();
     }
