@@ -715,3 +715,74 @@ def test_loss_of_few_rows_is_as_exact_as_its_result_s_type(rows):
     for got, exact, size in ((dx[:rows], want["dx"][0][:rows], dz @ ws), (dw, want["dw"][0], dz.t() @ xs)):
         # 2^-16 of every dz, 2^-8 of the result, and 2^-12 of dz for the sums and the logits' errors (their own bound, in the tests above, is of the order H 2^-24 = 2^-16)
         _within(got, exact, BF16 * exact.abs() + 2.0 ** -12 * size + TINY, rows)
+
+
+# ---- offsets that 32 bits do not hold ---------------------------------------------------------------------------------
+
+def _far_apart(t, stride):
+    """The rows of `t`, `stride` elements apart."""
+    wide = torch.empty((t.shape[0] - 1) * stride + t[0].numel(), dtype=t.dtype, device=t.device)
+    view = wide.as_strided(t.shape, (stride, *t.stride()[1:]))
+    view.copy_(t)
+    return view
+
+
+def test_rotary_and_norm_of_rows_far_apart():
+    """Rows 2^31 elements and more apart: the bits of contiguous ones."""
+    from paper_2505_19609_amd import binding as B
+    gen = _gen(91)
+    plan, rotary = _plan(([3], [1], [0], [0]), (2, 1), 64), B.skrull_rotary_init(64)
+    q, k = _randn(gen, 3, 2, 64), _randn(gen, 3, 1, 64)
+    want = torch.empty_like(q), torch.empty_like(k)
+    B.skrull_rotary(plan, rotary, q, k, *want)
+    far = [_far_apart(t, (1 << 31) + 8) for t in (q, k)]
+    B.skrull_rotary(plan, rotary, *far, *far)
+    assert all(torch.equal(f, w) for f, w in zip(far, want))
+    plan.destroy()
+    del far
+    x, dy, w, b = _randn(gen, 3, 136), _randn(gen, 3, 136), _randn(gen, 136), _randn(gen, 136)
+    results = []
+    for place in (torch.Tensor.clone, lambda t: _far_apart(t, (1 << 31) + 3)):
+        y, dx, (mean, rstd), dw, db = place(x), place(dy), torch.empty((2, 3), device="cuda"), torch.empty_like(w), torch.empty_like(b)
+        B.skrull_norm_fwd(y, w, b, y, mean, rstd, 1e-5, B.NORM_LAYER)
+        ws = torch.empty(B.skrull_norm_workspace(x, w, B.NORM_LAYER), dtype=torch.uint8, device="cuda")
+        B.skrull_norm_bwd(x, w, mean, rstd, dx, dx, dw, db, ws, B.NORM_LAYER)
+        results.append((y, dx, dw, db))
+    assert all(torch.equal(a, c) for a, c in zip(*results))
+
+
+def test_loss_of_a_weight_past_32_bits():
+    """A weight of more than 2^31 elements and rows of x 2^31 apart: targets, sums and gradients of the last words as of the first ones."""
+    from paper_2505_19609_amd import binding as B
+    gen, rows, hidden, vocab = _gen(92), 3, 4104, (1 << 19) + 5000
+    x, w = _randn(gen, rows, hidden), torch.empty(vocab, hidden, dtype=torch.bfloat16, device="cuda").normal_(0, 1.5 * hidden ** -0.5, generator=gen)
+    target, d = torch.tensor([vocab - 1, 7, vocab - 2500], device="cuda"), torch.tensor([1.0, -0.5, 0.25], device="cuda")
+    far = _far_apart(x, (1 << 31) + 8)
+    loss, lse = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    B.skrull_loss_fwd(far, w, target, loss, lse, torch.empty(B.skrull_loss_workspace(far, w, False), dtype=torch.uint8, device="cuda"))
+    B.skrull_loss_bwd(far, w, target, lse, d, dx, dw, torch.empty(B.skrull_loss_workspace(far, w, True), dtype=torch.uint8, device="cuda"))
+    del far
+    step = 1 << 16
+    z, zs = (torch.cat([f(x.double()) @ f(w[i:i + step].double()).t() for i in range(0, vocab, step)], 1) for f in (lambda t: t, torch.abs))
+    want_lse = torch.logsumexp(z, 1)
+    n = torch.arange(rows, device="cuda")
+    # as in _loss_in_64_bits
+    ez = (hidden + 8) * FP32 * zs + 4 * FP32 * z.abs()
+    p = (z - want_lse[:, None]).exp()
+    elog = (p * ez).sum(1) + (vocab / 128 + 256) * FP32 + 8 * FP32 * want_lse.abs()
+    _within(lse, want_lse, elog + FP32 * want_lse.abs(), "lse")
+    want_loss = want_lse - z[n, target]
+    _within(loss, want_loss, elog + ez[n, target] + FP32 * (want_lse.abs() + z[n, target].abs()) + FP32 * want_loss.abs(), "loss")
+    one = torch.zeros_like(p)
+    one[n, target] = 1.0
+    dz = d.double()[:, None] * (p - one)
+    edz = d.double().abs()[:, None] * (p * (ez + elog[:, None] + 16 * FP32) * 1.1 + 4 * FP32 * (p + one))
+    edz = edz + BF16 * (dz.abs() + edz)
+    want_dx = sum(dz[:, i:i + step] @ w[i:i + step].double() for i in range(0, vocab, step))
+    edx = sum(edz[:, i:i + step] @ w[i:i + step].double().abs() + (vocab + 64) * FP32 * (dz[:, i:i + step].abs() @ w[i:i + step].double().abs()) for i in range(0, vocab, step))
+    _within(dx, want_dx, edx + BF16 * (want_dx.abs() + edx) + TINY, "dx")
+    for i in range(0, vocab, step):
+        want_dw = dz[:, i:i + step].t() @ x.double()
+        edw = edz[:, i:i + step].t() @ x.double().abs() + (rows + 64) * FP32 * (dz[:, i:i + step].abs().t() @ x.double().abs())
+        _within(dw[i:i + step], want_dw, edw + BF16 * (want_dw.abs() + edw) + TINY, ("dw", i))
