@@ -68,8 +68,9 @@ typedef struct {
 int skrull_rotary_check(const skrull_rotary_t *rotary);
 
 /*
- * Turn one or two tensors of `plan`'s rows (`second` may be NULL); neither's `out` may hold elements of the other one's tensors.  Bytes between the rows of `out` stay as they were.  Only enqueues one kernel on
- * `hip_stream`; allocates nothing, may be captured.  Calls may overlap where their tensors do not.
+ * Turn one or two tensors of `plan`'s rows (`second` may be NULL); neither's `out` may hold elements of the other one's tensors.
+ * Bytes between the rows of `out` stay as they were.  Only enqueues one kernel on `hip_stream`; allocates nothing, may be captured.
+ * Calls may overlap where their tensors do not.
  * SKRULL_EINVAL: a null pointer, a value outside the limits above, rotary->head_dim other than the plan's, `out` that overlaps `in`
  * otherwise, or the current device not the one the plan was made on.
  */
