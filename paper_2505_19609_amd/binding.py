@@ -412,8 +412,9 @@ def _refuse(why):
 
 def _on_current_device(*tensors):
     import torch
+    device = torch.cuda.current_device() if torch.cuda.is_initialized() else -2   # (-1: of a tensor that is on no GPU)
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != torch.cuda.current_device()):
+        if t is not None and t.get_device() != device:
             _refuse(f"a tensor is on {t.device}, not on the current GPU")
 
 
@@ -440,9 +441,27 @@ def _rotary_tensor(info, x, out, rows):
     return RotaryTensor(x.data_ptr(), out.data_ptr(), strides[0], strides[1], shape[1], rows)
 
 
+_turn = None
+
+
+def _native_turn():
+    """The native marshalling of skrull_rotary, False where it cannot be loaded."""
+    global _turn
+    if _turn is None:
+        from . import autograd
+        module = autograd._module()
+        _turn = module.turn if module is not None else False
+    return _turn
+
+
 def skrull_rotary(plan: Plan, rotary: Rotary, q, k, q_out, k_out, inverse=False, k_rows=ROWS_K, stream=None):
     """q_out, k_out = q, k turned by the positions of the plan's rows (`inverse`: turned back).  q or k may be None.  k_rows: whether
     k holds the gathered prefixes (ROWS_K) or this rank's own tokens (ROWS_Q)."""
+    # (932 rows, 4/4 heads of 64, which the GPU turns in 3.4 us: 3.6 us a call in native code, 9.1 by what follows)
+    turn = _native_turn()
+    if turn and type(rotary) is Rotary and turn(plan, ctypes.addressof(rotary), q, k, q_out, k_out, inverse, k_rows,
+                                                None if stream is None else _stream_ptr(stream)):
+        return
     _on_current_device(q, k, q_out, k_out)
     info = plan.info
     t = [_rotary_tensor(info, x, out, rows) for x, out, rows in ((q, q_out, ROWS_Q), (k, k_out, k_rows)) if x is not None]

@@ -173,6 +173,12 @@ int64_t row_stride(const at::Tensor &t) { return t.size(0) > 1 ? t.stride(0) : t
 void *address(const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
 at::Tensor bytes_like(const at::Tensor &t, int64_t n) { return at::empty({std::max<int64_t>(n, 16)}, t.options().dtype(at::kByte)); }
 
+// Whether a call of these has to be kept for a backward pass.  (One that has not is made without a Function around it.)
+bool differentiable(std::initializer_list<const at::Tensor *> inputs)
+{
+    return at::GradMode::is_enabled() && std::any_of(inputs.begin(), inputs.end(), [](const at::Tensor *t) { return t->defined() && t->requires_grad(); });
+}
+
 // A gradient that is asked for with create_graph cannot be differentiated again.
 variable_list once(const variable_list &grads, variable_list out)
 {
@@ -186,11 +192,8 @@ variable_list once(const variable_list &grads, variable_list out)
 struct Norm : torch::autograd::Function<Norm> {
     static Variable forward(AutogradContext *ctx, const Variable &x, const Variable &w, const std::optional<at::Tensor> &b, double eps, int64_t kind)
     {
-        at::Tensor y = at::empty(x.sizes(), x.options()), stats = at::empty({2, x.size(0)}, x.options().dtype(at::kFloat));
-        skrull_norm_t p = sizes(x, w, (float)eps, kind);
-        p.y_stride = x.size(1);
-        float *mean = (float *)stats.data_ptr();
-        check(skrull_norm_fwd(&p, x.data_ptr(), w.data_ptr(), b ? b->data_ptr() : nullptr, y.data_ptr(), mean, mean + x.size(0), current_stream()));
+        const at::Tensor stats = at::empty({2, x.size(0)}, x.options().dtype(at::kFloat));
+        at::Tensor y = run(x, w, b ? b->data_ptr() : nullptr, eps, kind, (float *)stats.data_ptr());
         ctx->saved_data["kind"] = kind;
         ctx->saved_data["bias"] = b.has_value();
         ctx->save_for_backward({x, w, stats});
@@ -214,6 +217,14 @@ struct Norm : torch::autograd::Function<Norm> {
                               current_stream()));
         return once(grads, {dx, dw, db, at::Tensor(), at::Tensor()});
     }
+    static at::Tensor run(const at::Tensor &x, const at::Tensor &w, const void *b, double eps, int64_t kind, float *stats)
+    {
+        at::Tensor y = at::empty(x.sizes(), x.options());
+        skrull_norm_t p = sizes(x, w, (float)eps, kind);
+        p.y_stride = x.size(1);
+        check(skrull_norm_fwd(&p, x.data_ptr(), w.data_ptr(), b, y.data_ptr(), stats, stats ? stats + x.size(0) : nullptr, current_stream()));
+        return y;
+    }
     static skrull_norm_t sizes(const at::Tensor &x, const at::Tensor &w, float eps, int64_t kind)
     {
         skrull_norm_t p = {};
@@ -231,12 +242,8 @@ struct Norm : torch::autograd::Function<Norm> {
 struct CrossEntropy : torch::autograd::Function<CrossEntropy> {
     static Variable forward(AutogradContext *ctx, const Variable &x, const Variable &w, const Variable &target)
     {
-        at::Tensor loss = at::empty({x.size(0)}, x.options().dtype(at::kFloat)), lse = at::empty_like(loss);
-        const skrull_loss_t p = sizes(x, w);
-        const int64_t bytes = skrull_loss_workspace(&p, 0);
-        const at::Tensor ws = bytes_like(x, bytes);
-        check(skrull_loss_fwd(&p, x.data_ptr(), w.data_ptr(), (const int64_t *)target.data_ptr(), (float *)loss.data_ptr(), (float *)lse.data_ptr(), ws.data_ptr(), (size_t)bytes,
-                              current_stream()));
+        const at::Tensor lse = at::empty({x.size(0)}, x.options().dtype(at::kFloat));
+        at::Tensor loss = run(x, w, target, lse);
         ctx->save_for_backward({x, w, target, lse});
         return loss;
     }
@@ -254,6 +261,16 @@ struct CrossEntropy : torch::autograd::Function<CrossEntropy> {
         check(skrull_loss_bwd(&p, x.data_ptr(), w.data_ptr(), (const int64_t *)target.data_ptr(), (const float *)lse.data_ptr(), (const float *)d.data_ptr(), address(dx), address(dw),
                               ws.data_ptr(), (size_t)bytes, current_stream()));
         return once(grads, {dx, dw, at::Tensor()});
+    }
+    static at::Tensor run(const at::Tensor &x, const at::Tensor &w, const at::Tensor &target, const at::Tensor &lse)
+    {
+        at::Tensor loss = at::empty_like(lse);
+        const skrull_loss_t p = sizes(x, w);
+        const int64_t bytes = skrull_loss_workspace(&p, 0);
+        const at::Tensor ws = bytes_like(x, bytes);
+        check(skrull_loss_fwd(&p, x.data_ptr(), w.data_ptr(), (const int64_t *)target.data_ptr(), (float *)loss.data_ptr(), (float *)lse.data_ptr(), ws.data_ptr(), (size_t)bytes,
+                              current_stream()));
+        return loss;
     }
     static skrull_loss_t sizes(const at::Tensor &x, const at::Tensor &w)
     {
@@ -299,14 +316,15 @@ struct Rotary : torch::autograd::Function<Rotary> {
     static variable_list turn(const skrull_attn_plan_t *handle, const std::string &rotary, const at::Tensor &q, const at::Tensor &k, int64_t k_rows, int inverse)
     {
         variable_list out = {at::empty(q.sizes(), q.options()), at::empty(k.sizes(), k.options())};
-        const skrull_rotary_tensor_t t[2] = {tensor(q, out[0], SKRULL_ROWS_Q), tensor(k, out[1], (int32_t)k_rows)};
+        const skrull_rotary_tensor_t t[2] = {tensor(q, out[0], SKRULL_ROWS_Q), tensor(k, out[1], k_rows)};
         check(skrull_rotary(handle, (const skrull_rotary_t *)rotary.data(), &t[0], &t[1], inverse, current_stream()));
         return out;
     }
-    static skrull_rotary_tensor_t tensor(const at::Tensor &in, const at::Tensor &out, int32_t rows)
+    static skrull_rotary_tensor_t tensor(const at::Tensor &in, const at::Tensor &out, int64_t rows)
     {
         const int64_t width = in.size(1) * in.size(2);
-        return skrull_rotary_tensor_t{in.data_ptr(), out.data_ptr(), in.size(0) > 1 ? in.stride(0) : width, width, (int32_t)in.size(1), rows};
+        const bool many = in.size(0) > 1;   // (a single row's stride says nothing)
+        return skrull_rotary_tensor_t{in.data_ptr(), out.data_ptr(), many ? in.stride(0) : width, many ? out.stride(0) : width, (int32_t)in.size(1), (int32_t)rows};
     }
 };
 
@@ -344,8 +362,12 @@ PyObject *norm(PyObject *, PyObject *const *args, Py_ssize_t n)
     at::Tensor y;
     {
         pybind11::gil_scoped_release no_gil;
-        refuse_captured({&x, &w, &b});
-        y = Norm::apply(x, w, b.defined() ? std::optional<at::Tensor>(b) : std::nullopt, eps, kind);
+        if (differentiable({&x, &w, &b})) {
+            refuse_captured({&x, &w, &b});
+            y = Norm::apply(x, w, b.defined() ? std::optional<at::Tensor>(b) : std::nullopt, eps, kind);
+        } else {
+            y = Norm::run(x, w, address(b), eps, kind, nullptr);
+        }
     }
     return THPVariable_Wrap(std::move(y));
     END_HANDLE_TH_ERRORS
@@ -363,8 +385,12 @@ PyObject *cross_entropy(PyObject *, PyObject *const *args, Py_ssize_t n)
     at::Tensor loss;
     {
         pybind11::gil_scoped_release no_gil;
-        refuse_captured({&x, &w});
-        loss = CrossEntropy::apply(x, w, target);
+        if (differentiable({&x, &w})) {
+            refuse_captured({&x, &w});
+            loss = CrossEntropy::apply(x, w, target);
+        } else {
+            loss = CrossEntropy::run(x, w, target, at::empty({x.size(0)}, x.options().dtype(at::kFloat)));
+        }
     }
     return THPVariable_Wrap(std::move(loss));
     END_HANDLE_TH_ERRORS
@@ -386,17 +412,55 @@ PyObject *rotary(PyObject *, PyObject *const *args, Py_ssize_t n)
         k.size(0) != (k_rows == SKRULL_ROWS_Q ? info.total_q : info.total_k) || q.size(2) != info.head_dim || k.size(2) != info.head_dim)
         Py_RETURN_NONE;
     const std::string copy((const char *)given, sizeof(skrull_rotary_t));
-    auto plan = std::make_shared<PlanObject>(args[2]);
     variable_list out;
-    {
+    if (differentiable({&q, &k})) {
+        auto plan = std::make_shared<PlanObject>(args[2]);
         pybind11::gil_scoped_release no_gil;
         refuse_captured({&q, &k});
         out = Rotary::apply(q, k, plan, handle, copy, k_rows);
+    } else {
+        pybind11::gil_scoped_release no_gil;
+        out = Rotary::turn(handle, copy, q, k, k_rows, 0);
     }
     PyObject *both = PyTuple_New(2);
     if (!both) throw python_error();
     for (int i = 0; i < 2; ++i) PyTuple_SET_ITEM(both, i, THPVariable_Wrap(std::move(out[i])));
     return both;
+    END_HANDLE_TH_ERRORS
+}
+
+// turn(plan, address of the skrull_rotary_t, q, k, q_out, k_out, inverse, k_rows, stream or None): binding.skrull_rotary, False where that has
+// to look at the tensors itself.
+PyObject *turn(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    TORCH_CHECK_TYPE(n == 9, "turn(plan, rotary, q, k, q_out, k_out, inverse, k_rows, stream)");
+    const void *rotary = PyLong_AsVoidPtr(args[1]);
+    const int inverse = PyObject_IsTrue(args[6]);
+    const int64_t k_rows = PyLong_AsLongLong(args[7]);
+    void *stream = args[8] == Py_None ? nullptr : PyLong_AsVoidPtr(args[8]);
+    if (PyErr_Occurred()) return nullptr;
+    const skrull_attn_plan_t *handle = handle_of(args[0]);
+    skrull_attn_plan_info_t info;
+    if (skrull_attn_plan_info(handle, &info) != SKRULL_OK || (k_rows != SKRULL_ROWS_Q && k_rows != SKRULL_ROWS_K)) Py_RETURN_FALSE;
+    skrull_rotary_tensor_t t[2];
+    int count = 0;
+    for (int i = 0; i < 2; ++i) {
+        if (args[2 + i] == Py_None) continue;
+        if (!THPVariable_CheckExact(args[2 + i]) || !THPVariable_CheckExact(args[4 + i])) Py_RETURN_FALSE;
+        const at::Tensor &in = SKRULL_TENSOR(2 + i), &out = SKRULL_TENSOR(4 + i);
+        const int64_t rows = i ? k_rows : SKRULL_ROWS_Q;
+        if (!here(in) || !here(out) || !is_bf16(in) || !is_bf16(out) || !is_heads(in) || !is_heads(out) || in.sizes() != out.sizes() || in.size(2) != info.head_dim ||
+            in.size(0) != (rows == SKRULL_ROWS_Q ? info.total_q : info.total_k))
+            Py_RETURN_FALSE;
+        t[count++] = Rotary::tensor(in, out, rows);
+    }
+    if (!count) Py_RETURN_FALSE;
+    {
+        pybind11::gil_scoped_release no_gil;
+        check(skrull_rotary(handle, (const skrull_rotary_t *)rotary, &t[0], count > 1 ? &t[1] : nullptr, inverse, args[8] == Py_None ? current_stream() : stream));
+    }
+    Py_RETURN_TRUE;
     END_HANDLE_TH_ERRORS
 }
 
@@ -421,6 +485,7 @@ PyMethodDef methods[] = {{"attention", (PyCFunction)(void (*)())attention, METH_
                          {"norm", (PyCFunction)(void (*)())norm, METH_FASTCALL, "the differentiable norm"},
                          {"cross_entropy", (PyCFunction)(void (*)())cross_entropy, METH_FASTCALL, "the differentiable loss"},
                          {"rotary", (PyCFunction)(void (*)())rotary, METH_FASTCALL, "the differentiable rotary positions"},
+                         {"turn", (PyCFunction)(void (*)())turn, METH_FASTCALL, "binding.skrull_rotary"},
                          {"refuse_captured", (PyCFunction)(void (*)())refuse_captured_of, METH_FASTCALL, "refuses leaves that an eager graph has"},
                          {"set_check", set_check, METH_O, "the callable that raises what an error code stands for"},
                          {nullptr, nullptr, 0, nullptr}};

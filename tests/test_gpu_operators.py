@@ -170,6 +170,47 @@ def test_rotary_strides_in_place_own_rows_and_single_tensors():
     plan.destroy()
 
 
+def test_rotary_by_native_marshalling_and_by_python(monkeypatch):
+    """The same bits and the same refusals, whichever of the two looks at the tensors."""
+    from paper_2505_19609_amd import binding as B
+    native = B._native_turn()
+    assert native
+    gen = _gen(10)
+    plan, rotary = _plan(SHAPES[3], (3, 1), 64), B.skrull_rotary_init(64, 48)
+    rows, k = _randn(gen, plan.total_q, 4 * 64 + 8), _randn(gen, plan.total_k, 1, 64)
+    q = rows[:, :192].unflatten(1, (3, 64))
+    gone = _plan(SHAPES[3], (3, 1), 64)
+    gone.destroy()
+    stream = torch.cuda.Stream()
+    good = [dict(), dict(inverse=True), dict(k=None), dict(q=None), dict(stream=stream), dict(k=q[:, 2:], k_rows=B.ROWS_Q)]
+    bad = [dict(q=q.float()), dict(q=q[:-1]), dict(q=q.cpu()), dict(q=rows[:, 4:196].unflatten(1, (3, 64))), dict(k=k[:, :, :32]), dict(q=q.transpose(0, 1)), dict(q=None, k=None),
+           dict(plan=gone), dict(k_rows=2), dict(q_out=q[1:]), dict(q_out=rows[:, 8:200].unflatten(1, (3, 64)))]
+    results = []
+    for turn in (native, False):
+        monkeypatch.setattr(B, "_turn", turn)
+        for kw in good + bad:
+            args = dict(dict(plan=plan, rotary=rotary, q=q, k=k), **kw)
+            for n in "qk":
+                if args[n] is not None:
+                    args.setdefault(n + "_out", torch.zeros(args[n].shape, dtype=args[n].dtype, device=args[n].device))
+                else:
+                    args[n + "_out"] = None
+            stream.wait_stream(torch.cuda.current_stream())
+            try:
+                B.skrull_rotary(**args)
+            except (B.SkrullError, ValueError, RuntimeError) as e:
+                assert any(kw is b for b in bad)
+                results.append(str(e))
+            else:
+                assert any(kw is g for g in good)
+                torch.cuda.synchronize()
+                results.append([args[n] for n in ("q_out", "k_out") if args[n] is not None])
+    half = len(results) // 2
+    for kw, a, b in zip(good + bad, results[:half], results[half:]):
+        assert a == b if isinstance(a, str) else all(torch.equal(x, y) and x.any() for x, y in zip(a, b)), kw
+    plan.destroy()
+
+
 def test_rotary_gradient():
     from paper_2505_19609_amd import binding as B
     from paper_2505_19609_amd.autograd import skrull_rotary
