@@ -52,7 +52,8 @@ int64_t skrull_loss_workspace(const skrull_loss_t *p, int backward);
 int skrull_loss_fwd(const skrull_loss_t *p, const void *x, const void *w, const int64_t *target, float *loss, float *lse,
                     void *workspace, size_t workspace_bytes, void *hip_stream);
 
-/* dx and dw, given the forward's lse; either may be NULL where it is not wanted.  As skrull_loss_fwd otherwise, with skrull_loss_workspace(p, 1) bytes. */
+/* dx and dw, given the forward's lse; either may be NULL where it is not wanted.  dx may lie where x does (all of x is read before); dx and dw overlap
+ * neither w nor each other.  As skrull_loss_fwd otherwise, with skrull_loss_workspace(p, 1) bytes. */
 int skrull_loss_bwd(const skrull_loss_t *p, const void *x, const void *w, const int64_t *target, const float *lse, const float *d_loss,
                     void *dx, void *dw, void *workspace, size_t workspace_bytes, void *hip_stream);
 

@@ -1,7 +1,7 @@
-"""torch.autograd wrapper around the library's forward / backward, for callers that
+"""torch.autograd wrappers around the library's forwards and backwards (attention, rotary positions, norm, loss), for callers that
 train with PyTorch: argument marshalling and bookkeeping only, every step of the
-attention runs in the HIP kernels behind the C ABI.  The marshalling is native code where
-nothing watches the call from Python, else the Function below: the same checks, outputs and errors."""
+operators runs in the HIP kernels behind the C ABI.  The marshalling is native code where
+nothing watches the call from Python, else the Functions below: the same checks, outputs and errors."""
 from __future__ import annotations
 
 import ctypes

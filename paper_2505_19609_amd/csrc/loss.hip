@@ -977,6 +977,9 @@ int skrull_loss_bwd(const skrull_loss_t *p, const void *x, const void *w, const 
         return refuse("loss: null or misaligned pointer");
     const Layout l(*p, true);
     if ((int64_t)workspace_bytes < l.bytes) return refuse("loss: workspace below %lld bytes", (long long)l.bytes);
+    const int64_t w_bytes = (int64_t)p->vocab * p->hidden * 2, dx_bytes = p->rows * p->hidden * 2;
+    if ((dw && overlap(w, w_bytes, dw, w_bytes)) || (dx && overlap(w, w_bytes, dx, dx_bytes)) || (dx && dw && overlap(dw, w_bytes, dx, dx_bytes)))
+        return refuse("loss: dx or dw overlaps w or the other");
     int compute_units = 0;
     if (int rc = current_device(&compute_units)) return rc;
     unsigned char *ws = (unsigned char *)workspace;

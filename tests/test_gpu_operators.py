@@ -827,3 +827,17 @@ def test_loss_of_a_weight_past_32_bits():
         want_dw = dz[:, i:i + step].t() @ x.double()
         edw = edz[:, i:i + step].t() @ x.double().abs() + (rows + 64) * FP32 * (dz[:, i:i + step].abs().t() @ x.double().abs())
         _within(dw[i:i + step], want_dw, edw + BF16 * (want_dw.abs() + edw) + TINY, ("dw", i))
+
+
+def test_loss_gradient_in_the_place_of_its_rows():
+    from paper_2505_19609_amd import binding as B
+    x, w, target, d = _loss_case(300, 328, 1100, 0.3)
+    loss, lse, d = torch.empty(300, device="cuda"), torch.empty(300, device="cuda"), d.contiguous()
+    B.skrull_loss_fwd(x, w, target, loss, lse, torch.empty(B.skrull_loss_workspace(x, w, False), dtype=torch.uint8, device="cuda"))
+    ws = torch.empty(B.skrull_loss_workspace(x, w, True), dtype=torch.uint8, device="cuda")
+    want, dw, again = torch.empty_like(x), torch.empty_like(w), torch.empty_like(w)
+    B.skrull_loss_bwd(x, w, target, lse, d, want, dw, ws)
+    B.skrull_loss_bwd(x, w, target, lse, d, x, again, ws)
+    assert torch.equal(x, want) and torch.equal(dw, again)
+    with pytest.raises(B.SkrullError, match="overlaps"):
+        B.skrull_loss_bwd(x, w, target, lse, d, x, w, ws)

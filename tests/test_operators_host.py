@@ -127,9 +127,17 @@ def test_loss_fwd_refuses_pointers(at, value):
 
 @pytest.mark.parametrize("at,value", [(0, None), (1, None), (1, ONE + 8), (2, None), (3, None), (4, None), (5, ONE + 8), (6, ONE + 8), (7, None), (8, 1000)])
 def test_loss_bwd_refuses_pointers(at, value):
-    args = [ONE] * 8 + [1 << 40, None]
+    args = [ONE + (i << 32) for i in range(8)] + [1 << 40, None]
     args[at] = value
     assert B.lib().skrull_loss_bwd(ctypes.byref(_loss()), *args) == B.SKRULL_EINVAL
+
+
+@pytest.mark.parametrize("at,other,by", [(6, 1, 0), (6, 1, 100 * 64 * 2 - 16), (5, 1, 16), (5, 6, 100 * 64 * 2 - 16), (5, 6, 16 - 4 * 64 * 2)])
+def test_loss_bwd_refuses_overlaps(at, other, by):
+    args = [ONE + (i << 32) for i in range(8)] + [1 << 40, None]
+    args[at] = args[other] + by
+    assert B.lib().skrull_loss_bwd(ctypes.byref(_loss()), *args) == B.SKRULL_EINVAL
+    assert "overlaps" in B.skrull_attn_strerror(B.SKRULL_EINVAL)
 
 
 def test_loss_workspace_is_bounded():
