@@ -29,9 +29,7 @@ namespace {
 
 constexpr int kTile = 256;       // rows and columns of a result tile
 constexpr int kStep = 64;        // of the contraction
-constexpr int kOperandBytes = kTile * kStep * 2;   // of a step in LDS
 constexpr int kGrid = 256;       // workgroups: one per compute unit, each as much LDS as allows no second one
-constexpr int kStrip = 128;      // words whose largest logit and sum the forward keeps together
 constexpr int64_t kPieceBytes = (int64_t)2 << 30;  // of dz at most
 // Rows of dz and of the gathered x are this much longer where their length is a multiple of 4 KB: the 256 rows of a tile would lie in few of the L2's sets.
 constexpr int kPitchPad = 64;
@@ -181,9 +179,10 @@ struct Operand {
 };
 
 // The tiles of a product and their operands.
-template <Kind K, int NB>
+template <Kind K, int NA, int NB>
 struct Product {
     static constexpr int kRows = 64 * NB;   // columns of a tile: rows of x, but for kDw
+    static constexpr int kWords = 64 * NA;  // its rows: words, or (256) hidden values
     int mt, nt, splits, steps, total;   // tiles of M and N; parts of the contraction, steps of a part
     int v0, zp, all_steps;              // first word of the piece; elements between rows of dz; kDx: steps of all parts
 
@@ -192,12 +191,12 @@ struct Product {
         const int row_tiles = max(1, (n_rows + kRows - 1) / kRows), h_tiles = (p.H + kTile - 1) / kTile, words = (p.V + kTile - 1) / kTile;
         splits = 1;
         v0 = zp = all_steps = 0;
-        int piece_tiles = words;
+        int piece_tiles = (p.V + kWords - 1) / kWords;
         if (K != kForward) {
             const Piece piece(row_tiles_of(n_rows), p.V, p.H, p.dz_room);
             zp = piece.pitch;
             v0 = p.piece * piece.tiles * kTile;
-            piece_tiles = max(0, min(piece.tiles, words - p.piece * piece.tiles));   // (no tile: there are fewer pieces than launches)
+            piece_tiles = max(0, min(piece.tiles, words - p.piece * piece.tiles)) * (kTile / kWords);   // (no tile: there are fewer pieces than launches)
             splits = K == kDx ? dx_splits(h_tiles * row_tiles, piece.tiles * (kTile / kStep)) : 1;
         }
         if (K == kForward || K == kAgain) {
@@ -237,8 +236,8 @@ struct Product {
     {
         const int64_t H2 = (int64_t)p.H * 2, xp2 = (int64_t)p.xp * 2, zp2 = (int64_t)zp * 2;
         if (K == kForward || K == kAgain) {
-            const int64_t v = v0 + (int64_t)m * kTile;
-            a = Source{(const unsigned char *)p.w + v * H2, min((int64_t)kTile, p.V - v) * H2, (uint32_t)H2, kStep * 2};
+            const int64_t v = v0 + (int64_t)m * kWords;
+            a = Source{(const unsigned char *)p.w + v * H2, min((int64_t)kWords, p.V - v) * H2, (uint32_t)H2, kStep * 2};
             b = Source{(const unsigned char *)p.x + (int64_t)n * kRows * xp2, kRows * xp2, (uint32_t)xp2, kStep * 2};
         } else if (K == kDx) {
             const int64_t k0 = (int64_t)s * steps * kStep;
@@ -278,23 +277,25 @@ __device__ __forceinline__ int here(int x)
 }
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-template <Kind K, int NB>
+// The tile is 64 NA x 64 NB: 256 x 256, x 128 or 64 with few rows, 64 x 64 with few words too (the logits).
+template <Kind K, int NA, int NB>
 __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
 {
+    static_assert(NA == 4 || (NA == 1 && NB == 1 && (K == kForward || K == kAgain)), "");
     constexpr bool A_COLS = K == kDx || K == kDw, B_COLS = K == kDw;
     // (what the results of a tile need of its rows comes by loads to LDS too, in two places by turns: a load to registers would be waited for
     // together with all that are under way)
-    constexpr int kRows = 64 * NB, kBufferBytes = kOperandBytes + 8192 * NB;
+    constexpr int kRows = 64 * NB, kOperandBytes = 8192 * NA, kBufferBytes = kOperandBytes + 8192 * NB, kStrip = 32 * NA;
     constexpr int kRowBytes = K == kForward ? kRows * 4 : K == kAgain ? 3 * kRows * 4 : 0;
     __shared__ __align__(1024) unsigned char lds[2 * kBufferBytes + 2 * kRowBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1;
     const int n = lane & 15, g = lane >> 4;
     const int n_rows = __builtin_amdgcn_readfirstlane(p.n_rows[K == kForward || K == kAgain]);
-    Product<K, NB> work;
+    Product<K, NA, NB> work;
     work.init(p, n_rows);
 
     const uint32_t a_pitch = (uint32_t)(K == kDw ? p.xp : p.H) * 2, b_pitch = (uint32_t)(K == kDx || K == kDw ? work.zp : p.xp) * 2;
-    Operand<A_COLS, 4> A;
+    Operand<A_COLS, NA> A;
     Operand<B_COLS, NB> B;
     A.init(lane, wave, wm, a_pitch);
     B.init(lane, wave, wn, b_pitch);
@@ -345,11 +346,11 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
     //   1     A0 B0, A0 B1    B1, A1                      A0 B0
     //   2     A1 B0, A1 B1    A0, B0 of the next step     B1 A1
     // Each half ends with a barrier: what was read in it may be overwritten, and what the next one reads is there (a step's loads, 16 with NB = 4, are younger).
-    bf16x8 a0[4][2], a1[4][2], b0[NB][2], b1[NB][2];   // [block of 16][half step]
-    f32x4 acc[8][2 * NB];
+    bf16x8 a0[NA][2], a1[NA][2], b0[NB][2], b1[NB][2];   // [block of 16][half step]
+    f32x4 acc[2 * NA][2 * NB];
     auto half_end = [&]() {
         SB();
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * (4 + NB)) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * (NA + NB)) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         SB();
@@ -359,23 +360,23 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
     for (int step = 0; step < 2; ++step) {
         const Fetch f = take(cursor);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (int q = 0; q < NA; ++q) {
             load_a(f, 0, q);
             if (q < NB) load_b(f, 0, q);
         }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (int q = 0; q < NA; ++q) {
             if (q < NB) load_b(f, 1, q);
             load_a(f, 1, q);
         }
     }
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * (4 + NB)) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * (NA + NB)) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    auto read_a = [&](const unsigned char *t, int half, bf16x8 to[4][2], int i) { to[i & 3][i >> 2] = A.get(t, half, i & 3, i >> 2); };
+    auto read_a = [&](const unsigned char *t, int half, bf16x8 to[NA][2], int i) { to[i % NA][i / NA] = A.get(t, half, i % NA, i / NA); };
     auto read_b = [&](const unsigned char *t, int half, bf16x8 to[NB][2], int i) { to[i % NB][i / NB] = B.get(t + kOperandBytes, half, i % NB, i / NB); };
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < 2 * NA; ++j) {
         read_a(lds, 0, a0, j);
         if (j < 2 * NB) read_b(lds, 0, b0, j);
     }
@@ -400,7 +401,7 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
         const float *row_lse = (const float *)(lds + row_at + 4 * kRows), *row_d = (const float *)(lds + row_at + 8 * kRows);
         row_at ^= (2 * kBufferBytes) ^ (2 * kBufferBytes + kRowBytes);
 #pragma unroll
-        for (int x = 0; x < 8; ++x)
+        for (int x = 0; x < 2 * NA; ++x)
 #pragma unroll
             for (int y = 0; y < 2 * NB; ++y)
 #pragma unroll
@@ -455,32 +456,32 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
                 half_end();
             } else {   // (fewer products: memory is what is waited for, so the loads go first)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) load_a(f, 0, i);
+                for (int i = 0; i < NA; ++i) load_a(f, 0, i);
 #pragma unroll
                 for (int i = 0; i < NB; ++i) load_b(f, 0, i);
 #pragma unroll
                 for (int i = 0; i < 2 * NB; ++i) read_b(t, 1, b1, i);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) read_a(t, 1, a1, i);
+                for (int i = 0; i < 2 * NA; ++i) read_a(t, 1, a1, i);
 #pragma unroll
-                for (int j = 0; j < 16 * NB; ++j) {   // block of 16 rows of B, of A, half step
-                    const int y = j / 8, x = j / 2 % 4, k = j & 1;
+                for (int j = 0; j < 4 * NA * NB; ++j) {   // block of 16 rows of B, of A, half step
+                    const int y = j / (2 * NA), x = j / 2 % NA, k = j & 1;
                     acc[x][y] = mfma16(a0[x][k], y < NB ? b0[y][k] : b1[y - NB][k], acc[x][y]);
                 }
                 half_end();
 #pragma unroll
                 for (int i = 0; i < NB; ++i) load_b(f, 1, i);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) load_a(f, 1, i);
+                for (int i = 0; i < NA; ++i) load_a(f, 1, i);
                 bf16x8 b2[NB][2];   // (the first products of this half still need b0)
 #pragma unroll
                 for (int i = 0; i < 2 * NB; ++i) read_b(next, 0, b2, i);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) read_a(next, 0, a0, i);
+                for (int i = 0; i < 2 * NA; ++i) read_a(next, 0, a0, i);
 #pragma unroll
-                for (int j = 0; j < 16 * NB; ++j) {
-                    const int y = j / 8, x = j / 2 % 4, k = j & 1;
-                    acc[4 + x][y] = mfma16(a1[x][k], y < NB ? b0[y][k] : b1[y - NB][k], acc[4 + x][y]);
+                for (int j = 0; j < 4 * NA * NB; ++j) {
+                    const int y = j / (2 * NA), x = j / 2 % NA, k = j & 1;
+                    acc[NA + x][y] = mfma16(a1[x][k], y < NB ? b0[y][k] : b1[y - NB][k], acc[NA + x][y]);
                 }
 #pragma unroll
                 for (int i = 0; i < 2 * NB; ++i) b0[i / 2][i & 1] = b2[i / 2][i & 1];
@@ -491,7 +492,7 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
 
         // (the compiler does not see that what follows reads results of the matrix pipe: the distance it would keep)
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
-        // acc[x][y][v] is row 128 wm + 16 x + 4 g + v and column 32 NB wn + 16 y + n of the tile
+        // acc[x][y][v] is row 32 NA wm + 16 x + 4 g + v and column 32 NB wn + 16 y + n of the tile
         if (K == kForward) {
             const int strip = m * 2 + wm;
             const int words = p.V - strip * kStrip - 4 * g;   // of the strip, from this lane's first one on
@@ -501,18 +502,18 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
             for (int y = 0; y < 2 * NB; ++y) {
                 const int in_tile = wn * 32 * NB + y * 16 + n, row = nn * kRows + in_tile;
                 SB();
-                float z[32];
+                float z[8 * NA];
 #pragma unroll
-                for (int j = 0; j < 32; ++j) z[j] = result(acc[j >> 2][y][j & 3]);
+                for (int j = 0; j < 8 * NA; ++j) z[j] = result(acc[j >> 2][y][j & 3]);
                 if (!whole) {
                     const int left = here(words);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
+                    for (int j = 0; j < 8 * NA; ++j)
                         if (16 * (j >> 2) + (j & 3) >= left) z[j] = -INFINITY;
                 }
                 float a[2] = {z[0], z[1]}, b[8];
 #pragma unroll
-                for (int j = 2; j < 32; ++j) a[j & 1] = fmaxf(a[j & 1], z[j]);
+                for (int j = 2; j < 8 * NA; ++j) a[j & 1] = fmaxf(a[j & 1], z[j]);
                 most[y] = fmaxf(a[0], a[1]);
                 const float shift = shift_of(most[y]) * kLog2e;
                 const int t = row_targets[in_tile] - strip * kStrip;
@@ -520,11 +521,11 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
                     const int mine = (t >> 2 & 3) == g && t >= 0 && t < kStrip ? (t >> 4) * 4 + (t & 3) : -1;
                     float found = z[0];
 #pragma unroll
-                    for (int j = 1; j < 32; ++j) found = j == mine ? z[j] : found;
+                    for (int j = 1; j < 8 * NA; ++j) found = j == mine ? z[j] : found;
                     if (mine >= 0) p.z_target[row] = found;
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {   // (eight at a time: an exponential's result is not ready for the next instruction)
+                for (int i = 0; i < NA; ++i) {   // (eight at a time: an exponential's result is not ready for the next instruction)
                     float e[8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j) e[j] = fast_exp2(z[8 * i + j] * kLog2e - shift);
@@ -551,7 +552,7 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
             for (int y = 0; y < 2 * NB; ++y)
                 if (g == (y & 3)) out[y * 16] = make_float2(most[y], sum[y]);
         } else if (K == kAgain) {
-            const int word0 = m * kTile + wm * kStrip;   // of the piece
+            const int word0 = m * work.kWords + wm * kStrip;   // of the piece
             const int words = p.V - work.v0 - word0 - 4 * g;
             const bool whole = work.v0 + word0 + kStrip <= p.V;
             const int rows = max(1, (n_rows + kStep - 1) / kStep) * kStep;   // that dW's product reads
@@ -565,7 +566,7 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
                 const int mine = (t >> 2 & 3) == g && t >= 0 && t < kStrip ? (t >> 4) * 4 + (t & 3) : -1;
                 uint16_t *out = p.dz + (int64_t)row * work.zp + word0 + 16 * (g & 1) + 8 * (g >> 1);
 #pragma unroll
-                for (int x = 0; x < 8; x += 2) {
+                for (int x = 0; x < 2 * NA; x += 2) {
                     SB();
                     float e[8];   // of two blocks
 #pragma unroll
@@ -760,8 +761,14 @@ __global__ __launch_bounds__(1024) void loss_sums_kernel(const float2 *strips, i
         a.x = m;
     };
     float2 sum = make_float2(-INFINITY, 0.0f);
-#pragma unroll 8
-    for (int k = share; k < n_strips; k += 64) add(sum, strips[k * Tp + r0 + i]);   // (within the padded rows)
+    for (int k = share; k < n_strips; k += 64 * 8) {   // (eight loads at a time, to the last one)
+        float2 part_of[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) part_of[j] = strips[min(k + 64 * j, n_strips - 1) * Tp + r0 + i];   // (within the padded rows)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (k + 64 * j < n_strips) add(sum, part_of[j]);
+    }
     part[share][i] = sum;
     __syncthreads();
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;   // a wavefront to a row
@@ -825,6 +832,27 @@ __global__ __launch_bounds__(256) void loss_dx_kernel(const float *slabs, const 
     else sum_parts<1>(slabs, slab, splits, rest, slot, dx, T, H, Hp);
 }
 
+// How many rows of x the products with the vocabulary's words take at a time: 64 where tiles of 256 leave compute units without one, as many as there
+// are where they are up to 128, so that memory is what is waited for.  In us, of the forward:
+//   rows, hidden, words     64 at a time  128  256
+//   37, 896, 32,003                   25         38
+//   64, 3,584, 128,000               172        210
+//   128, 896, 32,003                  24   29    37
+//   128, 3,584, 128,000              236  181   215
+//   192, 896, 150,000                 90         89
+//   256, 896, 32,003                  34         36
+//   512, 896, 150,000                210        141
+// And 64 words, four workgroups to a compute unit, where that leaves half of the compute units without a tile still (forward's product and backward's, us:
+// 100 rows, 896 hidden, 4,000 words 9.7 and 10.0, with 256 words 14.6 and 16.0; 300, 1,200, 5,000 14.8 and 14.8, 18.8 and 19.4; 37, 896, 32,003 13.0 and 14.2, 15.1 and
+// 17.0; but 128, 896, 32,003 17.1 and 19.3, 15.0 and 19.0).
+struct Tile { int words, rows; };
+Tile logits_tile(int64_t rows, int vocab)
+{
+    const int64_t tiles = (rows + 63) / 64 * ((vocab + kTile - 1) / kTile);
+    if (2 * tiles <= kGrid) return {64, 64};
+    if (rows <= 64 || tiles <= 2 * kGrid) return {kTile, 64};
+    return {kTile, rows <= 128 ? 128 : kTile};
+}
 // The workspace, from sizes alone.
 struct Layout {
     int64_t Tp, Hp, xp, dz_room, pieces;
@@ -857,7 +885,7 @@ struct Layout {
             slabs = take((Tp > parted ? Tp : parted) * Hp * 4);
         } else {
             z_target = take(Tp * 4);
-            strips = take(words / kStrip * Tp * 8);
+            strips = take(words / (logits_tile(p.rows, p.vocab).words / 2) * Tp * 8);
         }
     }
 };
@@ -872,21 +900,6 @@ int check(const skrull_loss_t *p)
     return SKRULL_OK;
 }
 
-// How many rows of x the products with the vocabulary's words take at a time: 64 where tiles of 256 leave compute units without one, as many as there
-// are where they are up to 128, so that memory is what is waited for.  In us, of the forward:
-//   rows, hidden, words     64 at a time  128  256
-//   37, 896, 32,003                   25         38
-//   64, 3,584, 128,000               172        210
-//   128, 896, 32,003                  24   29    37
-//   128, 3,584, 128,000              236  181   215
-//   192, 896, 150,000                 90         89
-//   256, 896, 32,003                  34         36
-//   512, 896, 150,000                210        141
-int tile_rows_of(int64_t rows, int vocab)
-{
-    if (rows <= 64 || (rows + 63) / 64 * ((vocab + kTile - 1) / kTile) <= 2 * kGrid) return 64;
-    return rows <= 128 ? 128 : kTile;
-}
 // The same of dX's product, whose parts fill the compute units: 64 where even so the tiles are few (256 rows, 896 hidden, 32,003 words: backward 91 us,
 // 96 with 256; 600, 128, 4,000: 48 and 55; but 512, 896, 150,000: 562 and 480).  Up to kTwice rows may be there twice.
 int dx_tile_rows_of(int64_t rows, int hidden)
@@ -896,11 +909,16 @@ int dx_tile_rows_of(int64_t rows, int hidden)
     return (rows + 63) / 64 * ((hidden + kTile - 1) / kTile) <= 16 ? 64 : kTile;
 }
 template <Kind K>
-hipError_t launch(int tile_rows, const LossArgs &a, hipStream_t st)
+hipError_t launch(Tile tile, const LossArgs &a, hipStream_t st)
 {
-    if (tile_rows == 64) loss_product_kernel<K, 1><<<kGrid, 256, 0, st>>>(a);
-    else if (tile_rows == 128) loss_product_kernel<K, 2><<<kGrid, 256, 0, st>>>(a);
-    else loss_product_kernel<K, 4><<<kGrid, 256, 0, st>>>(a);
+    if constexpr (K == kForward || K == kAgain)
+        if (tile.words == 64) {
+            loss_product_kernel<K, 1, 1><<<4 * kGrid, 256, 0, st>>>(a);   // (as many fit the compute units)
+            return hipGetLastError();
+        }
+    if (tile.rows == 64) loss_product_kernel<K, 4, 1><<<kGrid, 256, 0, st>>>(a);
+    else if (tile.rows == 128) loss_product_kernel<K, 4, 2><<<kGrid, 256, 0, st>>>(a);
+    else loss_product_kernel<K, 4, 4><<<kGrid, 256, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -915,8 +933,8 @@ hipError_t gather(const skrull_loss_t &p, const Layout &l, unsigned char *ws, co
     a.each = (int32_t)((p.rows + 511) / 512 < 4 ? 4 : (p.rows + 511) / 512);
     a.n_rows = (int32_t *)(ws + l.n_rows); a.slot = (int32_t *)(ws + l.slot); a.row = (int32_t *)(ws + l.row); a.target_of = (int32_t *)(ws + l.target);
     a.out = (uint16_t *)(ws + l.x); a.lse_of = (float *)(ws + l.lse); a.d_of = (float *)(ws + l.d); a.loss = loss; a.lse_out = lse_out; a.z_target = (float *)(ws + l.z_target);
-    const int64_t blocks = (p.rows + a.each - 1) / a.each;
-    loss_gather_kernel<BACKWARD><<<(int)(blocks < 1 ? 1 : blocks), 64 * kGatherWaves, 0, st>>>(a);
+    const int64_t blocks = (p.rows + a.each - 1) / a.each;   // (16 and more: a few rows' workgroups write the zeros behind them too)
+    loss_gather_kernel<BACKWARD><<<(int)(blocks < 16 ? 16 : blocks), 64 * kGatherWaves, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -957,9 +975,10 @@ int skrull_loss_fwd(const skrull_loss_t *p, const void *x, const void *w, const 
         LossArgs a = args_of(*p, l, ws, w);
         a.z_target = (float *)(ws + l.z_target);
         a.strips = (float2 *)(ws + l.strips);
-        e = launch<kForward>(tile_rows_of(p->rows, p->vocab), a, st);
+        const Tile tile = logits_tile(p->rows, p->vocab);
+        e = launch<kForward>(tile, a, st);
         if (e == hipSuccess) {
-            loss_sums_kernel<<<(int)(l.Tp / kSumRows), 1024, 0, st>>>(a.strips, (p->vocab + kTile - 1) / kTile * 2, l.Tp, a.n_rows, (const int32_t *)(ws + l.row), a.z_target, loss, lse);
+            loss_sums_kernel<<<(int)(l.Tp / kSumRows), 1024, 0, st>>>(a.strips, (p->vocab + tile.words - 1) / tile.words * 2, l.Tp, a.n_rows, (const int32_t *)(ws + l.row), a.z_target, loss, lse);
             e = hipGetLastError();
         }
     }
@@ -992,16 +1011,16 @@ int skrull_loss_bwd(const skrull_loss_t *p, const void *x, const void *w, const 
     a.slabs = (float *)(ws + l.slabs);
     a.dw = (uint16_t *)dw;
     a.dz_room = l.dz_room;
-    const int tile_rows = tile_rows_of(p->rows, p->vocab);
+    const Tile tile = logits_tile(p->rows, p->vocab);
     const int dx_rows = dx_tile_rows_of(p->rows, p->hidden);
     for (int64_t i = 0; i < l.pieces && e == hipSuccess; ++i) {   // (there may be fewer pieces: the last launches find no tiles then)
         a.piece = (int32_t)i;
-        e = launch<kAgain>(tile_rows, a, st);
+        e = launch<kAgain>(tile, a, st);
         if (e == hipSuccess && dx) {
-            e = launch<kDx>(dx_rows, a, st);
+            e = launch<kDx>(Tile{kTile, dx_rows}, a, st);
         }
         if (e == hipSuccess && dw) {
-            loss_product_kernel<kDw, 4><<<kGrid, 256, 0, st>>>(a);
+            loss_product_kernel<kDw, 4, 4><<<kGrid, 256, 0, st>>>(a);
             e = hipGetLastError();
         }
     }

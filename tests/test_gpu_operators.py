@@ -498,7 +498,7 @@ def _check_loss(x, w, target, d, want=None):
 
 
 @pytest.mark.parametrize("rows,hidden,vocab", [(1, 8, 1), (1, 64, 257), (2, 128, 128), (37, 64, 300), (255, 72, 1000), (256, 896, 513), (257, 136, 2049), (300, 896, 1000),
-                                               (1000, 1032, 777), (64, 3584, 4099), (2100, 200, 4000)])
+                                               (1000, 1032, 777), (64, 3584, 4099), (2100, 200, 4000), (500, 136, 5000), (100, 64, 70001)])
 @pytest.mark.parametrize("ignored", [0.0, 0.4])
 def test_loss(rows, hidden, vocab, ignored):
     _check_loss(*_loss_case(rows, hidden, vocab, ignored))
