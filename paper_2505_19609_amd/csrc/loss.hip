@@ -10,14 +10,14 @@
 //   dX       dz W                  fp32, added up over the pieces (and over parts of the vocabulary where there are few tiles)
 //   dW^T     X^T dz                a piece's rows of dW are complete after one product
 // What bounds them is the matrix pipe: 2 T V H operations each, against 2 (T + V) H bytes; with few rows reading W (37 rows, 896 hidden, 32,003 words, 57 MB:
-// forward 23 us of which the product takes 15, backward 67).
+// forward 23 us of which the product takes 13, backward 65).
 //
 // A workgroup is 4 wavefronts, one per SIMD, and forms a tile of 256 x 256 (x 64 or 128 where there are few rows): each wavefront 128 x 128, 8 x 8 results of
 // v_mfma_f32_16x16x32_bf16 in 256 accumulator registers, so that an operand fragment read from LDS feeds eight products.  Steps of 64 along
 // the contraction lie in two LDS buffers of 64 KB, filled by loads that write LDS directly.
 // The chip's power decides the clock under such products, and with it what an instruction is worth: with normally distributed operands in registers and
 // nothing else, 16 x 16 x 32 runs at 2,010 TFLOP/s, 32 x 32 x 16 (which moves each accumulator twice as often) at 1,705.  Here it is 1,340 to 1,400 (13,312 rows, 3,584
-// hidden, 131,072 words: forward 9.0 ms, backward 28.1; products of this size by the library run at 1,440 to 1,520 on the same chip), whether the steps' barriers and
+// hidden, 131,072 words: forward 9.0 ms, backward 28.2; torch's plain products of this size run at 1,440 to 1,520 on the same chip), whether the steps' barriers and
 // waits are there or not: without them the matrix pipe is busier and the clock lower.
 #include <math.h>
 
