@@ -457,7 +457,7 @@ def _native_turn():
 def skrull_rotary(plan: Plan, rotary: Rotary, q, k, q_out, k_out, inverse=False, k_rows=ROWS_K, stream=None):
     """q_out, k_out = q, k turned by the positions of the plan's rows (`inverse`: turned back).  q or k may be None.  k_rows: whether
     k holds the gathered prefixes (ROWS_K) or this rank's own tokens (ROWS_Q)."""
-    # (932 rows, 4/4 heads of 64, which the GPU turns in 3.4 us: 3.6 us a call in native code, 9.1 by what follows)
+    # (932 rows, 4/4 heads of 64, which the GPU turns in 2.9 us: 3.6 us a call in native code, 9.1 by what follows)
     turn = _native_turn()
     if turn and type(rotary) is Rotary and turn(plan, ctypes.addressof(rotary), q, k, q_out, k_out, inverse, k_rows,
                                                 None if stream is None else _stream_ptr(stream)):

@@ -2,8 +2,8 @@
 //
 // What bounds it: every element of Q and K is read and written once, 4 bytes, and meets two products; the
 // sines and cosines are one pair per (row, pair of elements), shared by all heads of the row.  So a workgroup takes a few whole rows, of Q and K
-// together where both hold the same rows, forms their sines and cosines once into LDS and streams the heads through, 16 bytes per load and
-// store.  The positions come from the plan's descriptor (which segment a row is in), so nothing but the tensors themselves is read per element.
+// together where both hold the same rows, asks for their heads, 16 bytes per load, forms their sines and cosines once into LDS and
+// stores what it makes of both.  The positions come from the plan's descriptor (which segment a row is in), so nothing but the tensors themselves is read per element.
 // 32,768 tokens, 32/8 heads of 128, out of a projection's rows: 671 MB in 118 us, 5.7 TB/s; a large copy reaches 5.1 to 5.4.
 #include <math.h>
 
@@ -23,7 +23,7 @@ struct Tensor {
     const uint16_t *in;
     uint16_t *out;
     int64_t in_stride, out_stride;
-    int32_t heads, copies;  // copies: `out` is other memory, the elements that are not turned go along
+    int32_t heads, head_units, row_units;   // units of a head: those that are turned, and the others where `out` is other memory
     uint64_t inv_row, inv_head;  // ceil(2^40 / units of a row, of a head)
 };
 // Rows that workgroups share out, and the tensors that hold them.
@@ -80,51 +80,63 @@ __device__ __forceinline__ int position_of(const Rows &w, int NS, int row0, int 
     return row0 + lane - __shfl(first, segment - lo) + (w.begin ? w.begin[segment] : 0);
 }
 
+// What a lane moves at a time: 16 bytes of a head, 4 pairs (interleaved), or two pieces of 16 bytes, 8 pairs (half; behind rotary_dim two pieces side by side).
 template <bool INTERLEAVED>
-__device__ __forceinline__ void turn_rows(const Args &a, const Tensor &t, const float2 *turn, int row0, int rows, int tid)
-{
-    const int pairs = a.rotary_dim / 2;
-    // A unit is what a lane moves at a time.  Half layout: 8 pairs (two pieces of 16 bytes), then the pieces behind rotary_dim;
-    // interleaved: a piece of 16 bytes, 4 pairs.
-    const int turned = INTERLEAVED ? a.rotary_dim / 8 : a.rotary_dim / 16;
-    const int units = turned + (t.copies ? (a.head_dim - a.rotary_dim) / 8 : 0);
-    const int row_units = units * t.heads;
-#pragma unroll 2
-    for (int i = tid; i < rows * row_units; i += kThreads) {
-        const int r = quotient40(i, t.inv_row), x = i - r * row_units;
-        const int head = quotient40(x, t.inv_head), u = x - head * units;
-        const uint16_t *in = t.in + (int64_t)(row0 + r) * t.in_stride + head * a.head_dim;
-        uint16_t *out = t.out + (int64_t)(row0 + r) * t.out_stride + head * a.head_dim;
-        if (u >= turned) {
-            const int e = a.rotary_dim + (u - turned) * 8;
-            *(uint4 *)(out + e) = *(const uint4 *)(in + e);
-        } else if (INTERLEAVED) {
-            const uint4 v = *(const uint4 *)(in + u * 8);
-            const float2 *cs = turn + r * pairs + u * 4;
-            uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float x0 = lo_of(w[j]), x1 = hi_of(w[j]), c = cs[j].x, s = cs[j].y;
-                w[j] = pack_bf16(x0 * c - x1 * s, x0 * s + x1 * c);
-            }
-            *(uint4 *)(out + u * 8) = make_uint4(w[0], w[1], w[2], w[3]);
-        } else {
-            const int e0 = u * 8, e1 = e0 + pairs;
-            const uint4 v0 = *(const uint4 *)(in + e0), v1 = *(const uint4 *)(in + e1);
-            const float2 *cs = turn + r * pairs + e0;
-            uint32_t a0[4] = {v0.x, v0.y, v0.z, v0.w}, a1[4] = {v1.x, v1.y, v1.z, v1.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float p0 = lo_of(a0[j]), p1 = hi_of(a0[j]), q0 = lo_of(a1[j]), q1 = hi_of(a1[j]);
-                const float c0 = cs[2 * j].x, s0 = cs[2 * j].y, c1 = cs[2 * j + 1].x, s1 = cs[2 * j + 1].y;
-                a0[j] = pack_bf16(p0 * c0 - q0 * s0, p1 * c1 - q1 * s1);
-                a1[j] = pack_bf16(p0 * s0 + q0 * c0, p1 * s1 + q1 * c1);
-            }
-            *(uint4 *)(out + e0) = make_uint4(a0[0], a0[1], a0[2], a0[3]);
-            *(uint4 *)(out + e1) = make_uint4(a1[0], a1[1], a1[2], a1[3]);
-        }
+struct Unit {
+    static constexpr int kPieces = INTERLEAVED ? 1 : 2;
+    uint16_t *out;
+    int second, angle;   // elements to the second piece; the first pair's place among the angles, -1: as it is, -2: there is no such unit
+    uint4 v[kPieces];
+    // Unit i of the workgroup's rows, first one tensor's, then the other's; loaded.
+    __device__ __forceinline__ void load(const Args &a, const Rows &w, int i, int units0, int units, int row0)
+    {
+        angle = -2;
+        if (i >= units) return;
+        const bool other = i >= units0;
+        const Tensor &t = w.t[other];
+        i -= other ? units0 : 0;
+        const int r = quotient40(i, t.inv_row), x = i - r * t.row_units, head = quotient40(x, t.inv_head), u = x - head * t.head_units;
+        const int pairs = a.rotary_dim / 2, turned = pairs / (4 * kPieces);
+        const bool turns = u < turned;
+        const int64_t row = row0 + r;
+        const int at = head * a.head_dim + (INTERLEAVED ? u * 8 : turns ? u * 8 : a.rotary_dim + (u - turned) * 16);
+        second = turns ? pairs : 8;
+        angle = turns ? r * pairs + u * (4 * kPieces) : -1;
+        const uint16_t *in = t.in + row * t.in_stride + at;
+        out = t.out + row * t.out_stride + at;
+        v[0] = *(const uint4 *)in;
+        if constexpr (!INTERLEAVED) v[1] = *(const uint4 *)(in + second);
     }
-}
+    __device__ __forceinline__ void store(const float2 *turn)
+    {
+        if (angle == -2) return;
+        if (angle >= 0) {
+            const float2 *cs = turn + angle;
+            if constexpr (INTERLEAVED) {
+                uint32_t w[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float x0 = lo_of(w[j]), x1 = hi_of(w[j]), c = cs[j].x, s = cs[j].y;
+                    w[j] = pack_bf16(x0 * c - x1 * s, x0 * s + x1 * c);
+                }
+                v[0] = make_uint4(w[0], w[1], w[2], w[3]);
+            } else {
+                uint32_t a0[4] = {v[0].x, v[0].y, v[0].z, v[0].w}, a1[4] = {v[1].x, v[1].y, v[1].z, v[1].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float p0 = lo_of(a0[j]), p1 = hi_of(a0[j]), q0 = lo_of(a1[j]), q1 = hi_of(a1[j]);
+                    const float c0 = cs[2 * j].x, s0 = cs[2 * j].y, c1 = cs[2 * j + 1].x, s1 = cs[2 * j + 1].y;
+                    a0[j] = pack_bf16(p0 * c0 - q0 * s0, p1 * c1 - q1 * s1);
+                    a1[j] = pack_bf16(p0 * s0 + q0 * c0, p1 * s1 + q1 * c1);
+                }
+                v[0] = make_uint4(a0[0], a0[1], a0[2], a0[3]);
+                v[1] = make_uint4(a1[0], a1[1], a1[2], a1[3]);
+            }
+        }
+        *(uint4 *)out = v[0];
+        if constexpr (!INTERLEAVED) *(uint4 *)(out + second) = v[1];
+    }
+};
 
 template <bool INTERLEAVED>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(const Args a)
@@ -138,6 +150,14 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const Args a)
     const int rows = min(w.each, w.rows - row0);
     const int pairs = a.rotary_dim / 2;
     const int tid = threadIdx.x;
+
+    // The first units are on their way while the angles are formed (26,624 tokens, 14/2 heads of 64, half of each turned: 27 us, 31 with the angles first;
+    // 932 tokens, 4/4 heads: 2.9 and 3.4).
+    constexpr int kUnits = INTERLEAVED ? 4 : 2;
+    const int units0 = rows * w.t[0].row_units, units = units0 + rows * w.t[1].row_units;
+    Unit<INTERLEAVED> unit[kUnits];
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j) unit[j].load(a, w, tid + j * kThreads, units0, units, row0);
 
     if (tid < pairs) freq[tid] = turns_of(a, tid);
     if (tid >= 64 && tid < 128) {   // (another wavefront than that of the frequencies)
@@ -153,8 +173,13 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const Args a)
         turn[i] = make_float2(c * a.amplitude, s * a.amplitude * a.sign);
     }
     __syncthreads();
-    turn_rows<INTERLEAVED>(a, w.t[0], turn, row0, rows, tid);
-    if (w.tensors > 1) turn_rows<INTERLEAVED>(a, w.t[1], turn, row0, rows, tid);
+    for (int base = kUnits * kThreads;; base += kUnits * kThreads) {
+#pragma unroll
+        for (int j = 0; j < kUnits; ++j) unit[j].store(turn);
+        if (base >= units) break;
+#pragma unroll
+        for (int j = 0; j < kUnits; ++j) unit[j].load(a, w, base + tid + j * kThreads, units0, units, row0);
+    }
 }
 
 uint64_t inverse40(int d) { return ((1ull << 40) + (uint64_t)d - 1) / (uint64_t)d; }
@@ -233,15 +258,15 @@ int skrull_rotary(const skrull_attn_plan_t *plan, const skrull_rotary_t *r, cons
         t.in_stride = g->in_stride;
         t.out_stride = g->out_stride;
         t.heads = g->heads;
-        t.copies = !in_place;
-        const int units = r->rotary_dim / (r->layout == SKRULL_ROTARY_INTERLEAVED ? 8 : 16) + (in_place ? 0 : (r->head_dim - r->rotary_dim) / 8);
-        t.inv_head = inverse40(units);
-        t.inv_row = inverse40(g->heads * units);
+        t.head_units = (in_place ? r->rotary_dim : r->head_dim) / (r->layout == SKRULL_ROTARY_INTERLEAVED ? 8 : 16);
+        t.row_units = t.head_units * g->heads;
+        t.inv_head = inverse40(t.head_units);
+        t.inv_row = inverse40(t.row_units);
     }
     for (int i = 0; i < groups; ++i) {
         Rows &w = a.r[i];
         // up to 16 KB in a workgroup's rows (32,768 tokens, 32/8 heads of 128: 117 us, 123 with 32 KB), fewer where that makes less than 512 of them
-        // (3,991 tokens, 14/2 heads of 64: 5.8 us; 6.2 without this, 8.5 with single rows)
+        // (3,991 tokens, 14/2 heads of 64, the angles first: 5.8 us; 6.2 without this, 8.5 with single rows)
         const int64_t width = (int64_t)(w.t[0].heads + w.t[1].heads) * r->head_dim;
         int32_t each = kMaxRows;
         while (each > 1 && (each * width > 8192 || (int64_t)w.rows < each * 512)) each /= 2;
