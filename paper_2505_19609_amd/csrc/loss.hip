@@ -598,14 +598,17 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
         } else if (K == kDx) {
             float *out = p.slabs + ((int64_t)(s * work.nt + nn) * kRows + wn * 32 * NB) * p.Hp + m * kTile + wm * 128;   // (the same for all lanes)
             const int cols = p.H - m * kTile - wm * 128;
+            const int valid = p.n_rows[1], again = (valid + kStep - 1) / kStep * kStep;
 #pragma unroll
             for (int y = 0; y < 2 * NB; ++y) {
                 float *row = out + y * 16 * p.Hp;
+                const int r = nn * kRows + wn * 32 * NB + y * 16 + n;
+                const bool stored = r < valid || (r < n_rows && r >= again && r - again < valid);   // (not the zeros behind either time)
                 const uint32_t mine = n * p.Hp + 4 * g;
 #pragma unroll
                 for (int x = 0; x < 8; ++x) {
                     SB();
-                    if (x * 16 + 4 * g < cols && nn * kRows + wn * 32 * NB + y * 16 + n < n_rows) {   // (a whole number of fours)
+                    if (stored && x * 16 + 4 * g < cols) {   // (a whole number of fours)
                         float4 *to = (float4 *)(row + x * 16 + mine);
                         float4 f = make_float4(result(acc[x][y][0]), result(acc[x][y][1]), result(acc[x][y][2]), result(acc[x][y][3]));
                         if (p.piece > 0) {
