@@ -38,6 +38,12 @@ constexpr int kMaxPieceWords = 1 << 20;            // (32-bit offsets within a t
 // type's.  It costs little where W is what the products wait for (64 rows, 3,584 hidden, 128,000 words: 728 us and not 657; 37, 896, 32,003: 72 and 61).  (Where many
 // rows add up, dz's roundings cost as much as the result's own: 2.4e-3 of a gradient's norm against 1.7e-3.  A single row's are all or nothing.)
 constexpr int kTwice = kTile / 2;
+// The second time begins at a multiple of 32: both together are a whole number of steps of dW (20 rows, 3,584 hidden, 60,000 words: dX and dW 189 us, 222 with
+// multiples of 64).
+constexpr int kTimes = kStep / 2;
+__host__ __device__ inline int times_of(int64_t rows) { return (int)((rows + kTimes - 1) / kTimes * kTimes); }
+// Where it begins, given the rows of dz and those that have a target; 0 if there is none.
+__device__ __forceinline__ int second_of(const int32_t *n_rows) { return n_rows[0] > n_rows[1] ? n_rows[0] / 2 : 0; }
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // What is taken off logits whose largest one this is: nothing where there is no word at all, or an infinite logit, so that a sum is 0 or infinite
@@ -50,7 +56,7 @@ struct LossArgs {
     const uint16_t *x;       // gathered rows [.., xp], Hp of them used
     const uint16_t *w;       // [V, H]
     uint16_t *dz;            // [.., pitch of the pieces]
-    const int32_t *n_rows;   // rows of dz, of them rows that have a target (the second time they begin at the next multiple of 64)
+    const int32_t *n_rows;   // rows of dz, of them rows that have a target (and once more, second_of)
     const int32_t *target;   // of the gathered rows
     const float *lse, *d;    // of the gathered rows (kAgain)
     float *z_target;         // of the gathered rows (kForward)
@@ -555,8 +561,8 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
             const int word0 = m * work.kWords + wm * kStrip;   // of the piece
             const int words = p.V - work.v0 - word0 - 4 * g;
             const bool whole = work.v0 + word0 + kStrip <= p.V;
-            const int rows = max(1, (n_rows + kStep - 1) / kStep) * kStep;   // that dW's product reads
-            const bool twice = p.n_rows[0] > rows;
+            const int second = second_of(p.n_rows), rows = second ? second : max(1, (n_rows + kStep - 1) / kStep) * kStep;   // rows: that dW's product reads, each time
+            const bool twice = second > 0;
 #pragma unroll
             for (int y = 0; y < 2 * NB; ++y) {
                 const int in_tile = wn * 32 * NB + y * 16 + n, row = nn * kRows + in_tile;
@@ -598,12 +604,12 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
         } else if (K == kDx) {
             float *out = p.slabs + ((int64_t)(s * work.nt + nn) * kRows + wn * 32 * NB) * p.Hp + m * kTile + wm * 128;   // (the same for all lanes)
             const int cols = p.H - m * kTile - wm * 128;
-            const int valid = p.n_rows[1], again = (valid + kStep - 1) / kStep * kStep;
+            const int valid = p.n_rows[1], again = second_of(p.n_rows);
 #pragma unroll
             for (int y = 0; y < 2 * NB; ++y) {
                 float *row = out + y * 16 * p.Hp;
                 const int r = nn * kRows + wn * 32 * NB + y * 16 + n;
-                const bool stored = r < valid || (r < n_rows && r >= again && r - again < valid);   // (not the zeros behind either time)
+                const bool stored = r < valid || (again && r >= again && r - again < valid);   // (not the zeros behind either time)
                 const uint32_t mine = n * p.Hp + 4 * g;
 #pragma unroll
                 for (int x = 0; x < 8; ++x) {
@@ -688,7 +694,7 @@ __global__ __launch_bounds__(64 * kGatherWaves) void loss_gather_kernel(const Ga
         n += counts[1][k];
     }
     const bool twice = BACKWARD && n > 0 && n <= kTwice;
-    const int again = (n + kStep - 1) / kStep * kStep;   // the second time
+    const int again = times_of(n);   // the second time
     if (blockIdx.x == 0 && threadIdx.x == 0) {
         a.n_rows[0] = twice ? 2 * again : n;
         a.n_rows[1] = n;
@@ -828,9 +834,9 @@ __device__ __forceinline__ void sum_parts(const float *slabs, int64_t slab, int 
 __global__ __launch_bounds__(256) void loss_dx_kernel(const float *slabs, const int32_t *n_rows, const int32_t *slot, uint16_t *dx, int64_t T, int V, int H, int Hp,
                                                       int64_t dz_room, int tile_rows)
 {
-    const int n = n_rows[0], again = (n_rows[1] + kStep - 1) / kStep * kStep, tiles = max(1, (n + tile_rows - 1) / tile_rows);
+    const int n = n_rows[0], tiles = max(1, (n + tile_rows - 1) / tile_rows);
     const int splits = dx_splits(tiles * ((H + kTile - 1) / kTile), Piece(row_tiles_of(n), V, H, dz_room).tiles * (kTile / kStep));
-    const int64_t slab = (int64_t)tiles * tile_rows * Hp, rest = n > again ? (int64_t)again * Hp : 0;   // rest: to the products of what was left of dz
+    const int64_t slab = (int64_t)tiles * tile_rows * Hp, rest = (int64_t)second_of(n_rows) * Hp;   // rest: to the products of what was left of dz
     if (splits >= 32) sum_parts<4>(slabs, slab, splits, rest, slot, dx, T, H, Hp);
     else sum_parts<1>(slabs, slab, splits, rest, slot, dx, T, H, Hp);
 }
@@ -907,8 +913,8 @@ int check(const skrull_loss_t *p)
 // 96 with 256; 600, 128, 4,000: 48 and 55; but 512, 896, 150,000: 562 and 480).  Up to kTwice rows may be there twice.
 int dx_tile_rows_of(int64_t rows, int hidden)
 {
-    if (rows <= kTwice) rows = 2 * ((rows + kStep - 1) / kStep * kStep);
-    if (rows <= 128) return 128;
+    if (rows <= kTwice) rows = 2 * times_of(rows);
+    if (rows <= 128) return rows <= 64 ? 64 : 128;
     return (rows + 63) / 64 * ((hidden + kTile - 1) / kTile) <= 16 ? 64 : kTile;
 }
 template <Kind K>
