@@ -429,6 +429,8 @@ def skrull_rotary_init(head_dim, rotary_dim=None, layout=ROTARY_HALF, base=10000
 
 def _rotary_tensor(info, x, out, rows):
     import torch
+    if out is None:
+        _refuse("a tensor to turn has no output")
     want, d = info.total_q if rows == ROWS_Q else info.total_k, info.head_dim
     shape, strides = x.shape, []
     for t in (x, out):
@@ -495,6 +497,15 @@ def _vector(t, n, dtype, name):
     return None if t is None else _ptr(t)
 
 
+def _scratch(t):
+    """The address and size of a workspace."""
+    if t is None:
+        return None, 0
+    if not t.is_contiguous():
+        _refuse("workspace must be contiguous")
+    return _ptr(t), t.numel() * t.element_size()
+
+
 def skrull_norm_fwd(x, weight, bias, y, mean, rstd, eps=1e-5, kind=NORM_LAYER, stream=None):
     """y = the norm of the rows of x; mean and rstd (fp32 [rows], may be None) for the backward."""
     import torch
@@ -518,8 +529,7 @@ def skrull_norm_bwd(x, weight, mean, rstd, dy, dx, dweight, dbias, workspace, ki
     cols, wt, rows = p.cols, weight.dtype, p.rows
     _check(lib().skrull_norm_bwd(ctypes.byref(p), _ptr(x), _vector(weight, cols, wt, "weight"), _vector(mean, rows, torch.float32, "mean"),
                                  _vector(rstd, rows, torch.float32, "rstd"), _ptr(dy), _ptr(dx), _vector(dweight, cols, wt, "dweight"),
-                                 _vector(dbias, cols, wt, "dbias"), None if workspace is None else _ptr(workspace),
-                                 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+                                 _vector(dbias, cols, wt, "dbias"), *_scratch(workspace), _stream_ptr(stream)))
 
 
 def _loss_of(x, weight, target) -> Loss:
@@ -547,8 +557,7 @@ def skrull_loss_fwd(x, weight, target, loss, lse, workspace, stream=None):
     _on_current_device(x, weight, target, loss, lse, workspace)
     p = _loss_of(x, weight, target)
     _check(lib().skrull_loss_fwd(ctypes.byref(p), _ptr(x), _ptr(weight), _ptr(target), _vector(loss, p.rows, torch.float32, "loss"),
-                                 _vector(lse, p.rows, torch.float32, "lse"), _ptr(workspace),
-                                 workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+                                 _vector(lse, p.rows, torch.float32, "lse"), *_scratch(workspace), _stream_ptr(stream)))
 
 
 def skrull_loss_bwd(x, weight, target, lse, d_loss, dx, dweight, workspace, stream=None):
@@ -561,5 +570,4 @@ def skrull_loss_bwd(x, weight, target, lse, d_loss, dx, dweight, workspace, stre
             _refuse(f"{name} must be contiguous bf16 {list(like.shape)}")
     _check(lib().skrull_loss_bwd(ctypes.byref(p), _ptr(x), _ptr(weight), _ptr(target), _vector(lse, p.rows, torch.float32, "lse"),
                                  _vector(d_loss, p.rows, torch.float32, "d_loss"), None if dx is None else _ptr(dx),
-                                 None if dweight is None else _ptr(dweight), _ptr(workspace),
-                                 workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+                                 None if dweight is None else _ptr(dweight), *_scratch(workspace), _stream_ptr(stream)))

@@ -184,7 +184,7 @@ def test_rotary_by_native_marshalling_and_by_python(monkeypatch):
     stream = torch.cuda.Stream()
     good = [dict(), dict(inverse=True), dict(k=None), dict(q=None), dict(stream=stream), dict(k=q[:, 2:], k_rows=B.ROWS_Q)]
     bad = [dict(q=q.float()), dict(q=q[:-1]), dict(q=q.cpu()), dict(q=rows[:, 4:196].unflatten(1, (3, 64))), dict(k=k[:, :, :32]), dict(q=q.transpose(0, 1)), dict(q=None, k=None),
-           dict(plan=gone), dict(k_rows=2), dict(q_out=q[1:]), dict(q_out=rows[:, 8:200].unflatten(1, (3, 64)))]
+           dict(plan=gone), dict(k_rows=2), dict(q_out=None), dict(q_out=q[1:]), dict(q_out=rows[:, 8:200].unflatten(1, (3, 64)))]
     results = []
     for turn in (native, False):
         monkeypatch.setattr(B, "_turn", turn)
@@ -841,3 +841,16 @@ def test_loss_gradient_in_the_place_of_its_rows():
     assert torch.equal(x, want) and torch.equal(dw, again)
     with pytest.raises(B.SkrullError, match="overlaps"):
         B.skrull_loss_bwd(x, w, target, lse, d, x, w, ws)
+
+
+def test_scratch_that_is_not_whole_and_missing_ones_are_refused():
+    from paper_2505_19609_amd import binding as B
+    x, w, target, d = _loss_case(20, 64, 300, 0.0)
+    loss, lse, dx, dw = torch.empty(20, device="cuda"), torch.empty(20, device="cuda"), torch.empty_like(x), torch.empty_like(w)
+    n = B.skrull_loss_workspace(x, w, True)
+    weight, mean, rstd = torch.ones(64, dtype=torch.bfloat16, device="cuda"), torch.ones(20, device="cuda"), torch.ones(20, device="cuda")
+    for ws in (torch.empty(1, dtype=torch.uint8, device="cuda").expand(n), torch.empty(2 * n, dtype=torch.uint8, device="cuda")[::2], torch.empty(64, dtype=torch.uint8, device="cuda"), None):
+        for call in (lambda: B.skrull_loss_fwd(x, w, target, loss, lse, ws), lambda: B.skrull_loss_bwd(x, w, target, lse, d, dx, dw, ws),
+                     lambda: B.skrull_norm_bwd(x, weight, mean, rstd, x, dx, torch.empty_like(weight), None, ws)):
+            with pytest.raises(B.SkrullError):
+                call()
