@@ -12,6 +12,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
+#include <torch/csrc/autograd/functions/utils.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
@@ -189,33 +190,54 @@ variable_list once(const variable_list &grads, variable_list out)
     return (*error)(std::move(given));
 }
 
-struct Norm : torch::autograd::Function<Norm> {
-    static Variable forward(AutogradContext *ctx, const Variable &x, const Variable &w, const std::optional<at::Tensor> &b, double eps, int64_t kind)
+// A node of its own and not a Function, whose tables and wrappers a small norm waits for (932 x 896, forward and gradients, 14 us of the GPU: 57 us of the host, 61
+// as a Function).
+struct Norm : torch::autograd::Node {
+    torch::autograd::SavedVariable x, w;
+    at::Tensor stats;
+    int64_t kind = 0;
+    bool bias = false;
+
+    static at::Tensor forward(const at::Tensor &x, const at::Tensor &w, const at::Tensor &b, double eps, int64_t kind)
     {
-        const at::Tensor stats = at::empty({2, x.size(0)}, x.options().dtype(at::kFloat));
-        at::Tensor y = run(x, w, b ? b->data_ptr() : nullptr, eps, kind, (float *)stats.data_ptr());
-        ctx->saved_data["kind"] = kind;
-        ctx->saved_data["bias"] = b.has_value();
-        ctx->save_for_backward({x, w, stats});
+        const std::shared_ptr<Norm> node(new Norm, torch::autograd::deleteNode);
+        node->set_next_edges(torch::autograd::collect_next_edges(x, w, b));
+        node->stats = at::empty({2, x.size(0)}, x.options().dtype(at::kFloat));
+        at::Tensor y = run(x, w, address(b), eps, kind, (float *)node->stats.data_ptr());
+        node->x = torch::autograd::SavedVariable(x, false);
+        node->w = torch::autograd::SavedVariable(w, false);
+        node->kind = kind;
+        node->bias = b.defined();
+        torch::autograd::set_history(y, node);
         return y;
     }
-    static variable_list backward(AutogradContext *ctx, variable_list grads)
+    variable_list apply(variable_list &&grads) override
     {
-        const variable_list saved = ctx->get_saved_variables();
-        const at::Tensor &x = saved[0], &w = saved[1], &stats = saved[2];
+        std::lock_guard<std::mutex> lock(mutex_);
+        const at::Tensor x = this->x.unpack(), w = this->w.unpack();
+        variable_list out(3);
+        if (!grads[0].defined()) return out;
         const at::Tensor dy = is_rows(grads[0]) ? grads[0] : grads[0].contiguous();
-        at::Tensor dx = at::empty(x.sizes(), x.options()), dw, db, ws;
-        if (ctx->needs_input_grad(1)) dw = at::empty_like(w);
-        if (ctx->saved_data["bias"].toBool() && ctx->needs_input_grad(2)) db = at::empty_like(w);
-        skrull_norm_t p = sizes(x, w, 0.0f, ctx->saved_data["kind"].toInt());
+        at::Tensor dx = at::empty(x.sizes(), x.options()), ws;
+        if (task_should_compute_output(1)) out[1] = at::empty_like(w);
+        if (bias && task_should_compute_output(2)) out[2] = at::empty_like(w);
+        skrull_norm_t p = sizes(x, w, 0.0f, kind);
         p.dy_stride = row_stride(dy);
         p.dx_stride = x.size(1);
-        const int64_t bytes = dw.defined() || db.defined() ? skrull_norm_workspace(&p) : 0;
+        const int64_t bytes = out[1].defined() || out[2].defined() ? skrull_norm_workspace(&p) : 0;
         if (bytes) ws = bytes_like(x, bytes);
         const float *mean = (const float *)stats.data_ptr();
-        check(skrull_norm_bwd(&p, x.data_ptr(), w.data_ptr(), mean, mean + x.size(0), dy.data_ptr(), dx.data_ptr(), address(dw), address(db), address(ws), (size_t)bytes,
+        check(skrull_norm_bwd(&p, x.data_ptr(), w.data_ptr(), mean, mean + x.size(0), dy.data_ptr(), dx.data_ptr(), address(out[1]), address(out[2]), address(ws), (size_t)bytes,
                               current_stream()));
-        return once(grads, {dx, dw, db, at::Tensor(), at::Tensor()});
+        if (task_should_compute_output(0)) out[0] = std::move(dx);
+        return once(grads, std::move(out));
+    }
+    void release_variables() override
+    {
+        std::lock_guard<std::mutex> lock(mutex_);
+        x.reset_data();
+        w.reset_data();
+        stats.reset();
     }
     static at::Tensor run(const at::Tensor &x, const at::Tensor &w, const void *b, double eps, int64_t kind, float *stats)
     {
@@ -364,7 +386,7 @@ PyObject *norm(PyObject *, PyObject *const *args, Py_ssize_t n)
         pybind11::gil_scoped_release no_gil;
         if (differentiable({&x, &w, &b})) {
             refuse_captured({&x, &w, &b});
-            y = Norm::apply(x, w, b.defined() ? std::optional<at::Tensor>(b) : std::nullopt, eps, kind);
+            y = Norm::forward(x, w, b, eps, kind);
         } else {
             y = Norm::run(x, w, address(b), eps, kind, nullptr);
         }

@@ -282,6 +282,36 @@ def test_gradients_are_not_differentiated_again(monkeypatch, i, watched):
 
 
 @pytest.mark.parametrize("watched", [False, True])
+@pytest.mark.parametrize("i", range(5))
+def test_a_graph_is_freed_by_its_backward_pass_and_sees_changed_inputs(monkeypatch, i, watched):
+    from paper_2505_19609_amd import autograd as A
+    monkeypatch.setattr(A, "_watched", lambda: watched)
+    inputs, call = _calls()[i]
+
+    def outputs():
+        given = [t.clone().requires_grad_() for t in inputs]
+        out = call(*given)
+        out = out if isinstance(out, tuple) else (out,)
+        return given, out, [torch.ones_like(o) for o in out]
+
+    given, out, d = outputs()
+    first = torch.autograd.grad(out, given, d, retain_graph=True)
+    assert all(torch.equal(a, b) for a, b in zip(first, torch.autograd.grad(out, given, d)))
+    if i == 0:
+        return    # (rotary keeps no tensor)
+    with pytest.raises(RuntimeError, match="second time"):
+        torch.autograd.grad(out, given, d)
+    given, out, d = outputs()
+    with torch.no_grad():
+        given[1].mul_(2)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        torch.autograd.grad(out, given, d)
+    given, out, d = outputs()
+    del given
+    out[0].sum().backward()      # (leaves that only the graph holds)
+
+
+@pytest.mark.parametrize("watched", [False, True])
 @pytest.mark.parametrize("i", [0, 1, 4])
 def test_a_captured_call_is_refused_while_an_eager_graph_has_its_leaves(monkeypatch, i, watched):
     from paper_2505_19609_amd import autograd as A
