@@ -49,6 +49,9 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // What is taken off logits whose largest one this is: nothing where there is no word at all, or an infinite logit, so that a sum is 0 or infinite
 // and not NaN.
 __device__ __forceinline__ float shift_of(float most) { return fabsf(most) < INFINITY ? most : 0.0f; }
+// What a sum of exponentials is multiplied by where its largest logit is `most` and that of all sums put together `all`: 1 at most.  (A sum of no words has nothing
+// taken off; relative to logits of -100 its factor would be e^100 without the limit, relative to -89 and below infinite, and infinity times its zero no number.)
+__device__ __forceinline__ float scale_of(float most, float all) { return fast_exp2(fminf((shift_of(most) - shift_of(all)) * kLog2e, 0.0f)); }
 
 enum Kind { kForward, kAgain, kDx, kDw };
 
@@ -546,7 +549,7 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
 #pragma unroll
             for (int y = 0; y < 2 * NB; ++y) {
                 const float all = fmaxf(fmaxf(most[y], __shfl_xor(most[y], 16)), fmaxf(__shfl_xor(most[y], 32), __shfl_xor(most[y], 48)));
-                sum[y] *= fast_exp2((shift_of(most[y]) - shift_of(all)) * kLog2e);
+                sum[y] *= scale_of(most[y], all);
                 most[y] = all;
             }
 #pragma unroll
@@ -765,8 +768,8 @@ __global__ __launch_bounds__(1024) void loss_sums_kernel(const float2 *strips, i
     if (r0 >= n) return;
     // largest logit and the sum of exponentials relative to it
     auto add = [&](float2 &a, float2 b) {
-        const float m = fmaxf(a.x, b.x), s = shift_of(m);
-        a.y = a.y * fast_exp2((shift_of(a.x) - s) * kLog2e) + b.y * fast_exp2((shift_of(b.x) - s) * kLog2e);
+        const float m = fmaxf(a.x, b.x);
+        a.y = a.y * scale_of(a.x, m) + b.y * scale_of(b.x, m);
         a.x = m;
     };
     float2 sum = make_float2(-INFINITY, 0.0f);
