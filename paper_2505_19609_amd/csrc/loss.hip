@@ -566,6 +566,7 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
             const bool whole = work.v0 + word0 + kStrip <= p.V;
             const int second = second_of(p.n_rows), rows = second ? second : max(1, (n_rows + kStep - 1) / kStep) * kStep;   // rows: that dW's product reads, each time
             const bool twice = second > 0;
+            const bool filled = (nn + 1) * kRows > n_rows;   // (with rows that fill the last tile)
 #pragma unroll
             for (int y = 0; y < 2 * NB; ++y) {
                 const int in_tile = wn * 32 * NB + y * 16 + n, row = nn * kRows + in_tile;
@@ -593,6 +594,11 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
 #pragma unroll
                         for (int v = 0; v < 8; ++v)
                             if (16 * (v >> 2) + (v & 3) >= left) e[v] = 0.0f;
+                    }
+                    if (filled) {   // (their logits are 0 times w, which may hold infinities: no number, and nor is its product with a d of 0)
+                        const bool none = here(row) >= n_rows;
+#pragma unroll
+                        for (int v = 0; v < 8; ++v) e[v] = none ? 0.0f : e[v];
                     }
                     const uint4 u = eight_of(e, e + 4);
                     if (row < rows) *(uint4 *)(out + x * 16) = u;

@@ -1,10 +1,12 @@
 """Rotary positions, norm and loss where test_gpu_operators.py does not reach: logits far from zero, weights of infinities beside rows that fill
 a tile, gradients that come in unaligned, gradients of gradients, and the loops, pieces and tiles that larger calls take.  The 64-bit forms and their
 tolerances are that file's."""
+import math
+
 import pytest
 import torch
 
-from test_gpu_operators import _check_loss, _loss_case
+from test_gpu_operators import BF16, FP32, TINY, _check_loss, _loss_case, _loss_in_64_bits, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -24,3 +26,62 @@ def test_loss_of_logits_with_a_common_offset(rows, hidden, vocab, offset):
     target[0] = vocab - 1
     x[:, 0], w[:, 0] = offset / 8, 8.0
     _check_loss(x, w, target, d)
+
+
+@pytest.mark.parametrize("offset", [-100.0, 100.0])
+@pytest.mark.parametrize("rows,hidden,vocab", [(37, 64, 300), (500, 136, 4099), (1100, 200, 19971)])
+def test_loss_of_strips_whose_words_are_all_masked(rows, hidden, vocab, offset):
+    """128 words of minus infinity, and the last ones: what the words without them give."""
+    from paper_2505_19609_amd.autograd import skrull_cross_entropy
+    x, w, target, d = _loss_case(rows, hidden, vocab, 0.25)
+    x[:, 0], w[:, 0], x[:, 1] = offset / 8, 8.0, 1.0
+    masked = torch.zeros(vocab, dtype=torch.bool, device="cuda")
+    masked[128:256] = True
+    masked[vocab - vocab % 64:] = True
+    kept = torch.nonzero(~masked)[:, 0]
+    target = torch.where(target < 0, target, kept[target % len(kept)])
+    want = _loss_in_64_bits(x, w[kept], torch.where(target < 0, target, (torch.cumsum(~masked, 0) - 1)[target.clamp(min=0)]), d)
+    w[masked, 1] = -math.inf
+    x.requires_grad_(), w.requires_grad_()
+    loss = skrull_cross_entropy(x, w, target)
+    dx, dw = torch.autograd.grad(loss, (x, w), d)
+    columns = torch.arange(hidden, device="cuda") != 1     # (0 times infinity there, by the formula too)
+    for name, got, part in (("loss", loss.detach(), lambda t: t), ("dx", dx[:, columns], lambda t: t[:, columns]), ("dw", dw[kept], lambda t: t)):
+        exact, error = (part(t) for t in want[name])
+        _within(got, exact, error + (BF16 if got.dtype == torch.bfloat16 else FP32) * (exact.abs() + error) + TINY, name)
+    assert (dw[masked] == 0).all()
+
+
+# ---- loss: rows that fill a tile ---------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("targets", [1, 3, 31, 32, 65, 128, 130, 200, 256])
+@pytest.mark.parametrize("rows,hidden,vocab", [(300, 64, 500), (1100, 72, 19971)])
+def test_loss_gradients_of_a_masked_word_at_any_number_of_rows(rows, hidden, vocab, targets):
+    """A word of minus infinity has a gradient of zero, however many rows fill the last tile."""
+    from paper_2505_19609_amd.autograd import skrull_cross_entropy
+    x, w, target, d = _loss_case(rows, hidden, vocab, 0.0)
+    x[:, 0] = 1.0
+    target[target == 7] = 8
+    target[targets:] = -1
+    kept = torch.arange(vocab, device="cuda") != 7
+    want = _loss_in_64_bits(x, w[kept], target - (target > 7).long(), d)
+    w[7, 0] = -math.inf
+    x.requires_grad_(), w.requires_grad_()
+    loss = skrull_cross_entropy(x, w, target)
+    dx, dw = torch.autograd.grad(loss, (x, w), d)
+    assert (dw[7] == 0).all()
+    for name, got, part in (("loss", loss.detach(), lambda t: t), ("dx", dx[:, 1:], lambda t: t[:, 1:]), ("dw", dw[kept], lambda t: t)):
+        exact, error = (part(t) for t in want[name])
+        _within(got, exact, error + (BF16 if got.dtype == torch.bfloat16 else FP32) * (exact.abs() + error) + TINY, name)
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("rows,hidden,vocab", [(1, 64, 500), (300, 64, 500), (1100, 72, 19971)])
+def test_loss_without_a_target_adds_nothing_whatever_the_weight_holds(rows, hidden, vocab, bad):
+    from paper_2505_19609_amd.autograd import skrull_cross_entropy
+    x, w, target, d = _loss_case(rows, hidden, vocab, 0.0)
+    w[7, 3], w[vocab - 1] = bad, bad
+    x.requires_grad_(), w.requires_grad_()
+    loss = skrull_cross_entropy(x, w, torch.full_like(target, -1))
+    dx, dw = torch.autograd.grad(loss, (x, w), d)
+    assert (loss == 0).all() and (dx == 0).all() and (dw == 0).all()
