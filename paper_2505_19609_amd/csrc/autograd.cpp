@@ -331,7 +331,9 @@ struct Rotary : torch::autograd::Function<Rotary> {
             }
             PyGILState_Release(gil);
         }
-        const at::Tensor dq = is_heads(grads[0]) ? grads[0] : grads[0].contiguous(), dk = is_heads(grads[1]) ? grads[1] : grads[1].contiguous();
+        // (cloned and not made contiguous, which a part of a flat buffer is already, at whatever address)
+        const auto taken = [](const at::Tensor &t) { return is_heads(t) ? t : t.clone(at::MemoryFormat::Contiguous); };
+        const at::Tensor dq = taken(grads[0]), dk = taken(grads[1]);
         variable_list out = turn(handle, ctx->saved_data["rotary"].toStringRef(), dq, dk, ctx->saved_data["k_rows"].toInt(), 1);
         return once(grads, {out[0], out[1], at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor()});
     }

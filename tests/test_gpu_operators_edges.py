@@ -6,7 +6,7 @@ import math
 import pytest
 import torch
 
-from test_gpu_operators import BF16, FP32, TINY, _check_loss, _loss_case, _loss_in_64_bits, _within
+from test_gpu_operators import BF16, FP32, TINY, _calls, _check_loss, _gen, _loss_case, _loss_in_64_bits, _randn, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -85,3 +85,23 @@ def test_loss_without_a_target_adds_nothing_whatever_the_weight_holds(rows, hidd
     loss = skrull_cross_entropy(x, w, torch.full_like(target, -1))
     dx, dw = torch.autograd.grad(loss, (x, w), d)
     assert (loss == 0).all() and (dx == 0).all() and (dw == 0).all()
+
+
+# ---- autograd ----------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("watched", [False, True])
+def test_rotary_takes_gradients_of_any_alignment(monkeypatch, watched):
+    """Gradients that are parts of a flat buffer, 2 bytes off."""
+    from paper_2505_19609_amd import autograd as A
+    monkeypatch.setattr(A, "_watched", lambda: watched)
+    (q, k), call = _calls()[0]
+    given = [t.clone().requires_grad_() for t in (q, k)]
+    out = call(*given)
+    d = [_randn(_gen(5), *o.shape) for o in out]
+    want = torch.autograd.grad(out, given, d, retain_graph=True)
+    flat = torch.empty(1 + sum(t.numel() for t in d), dtype=torch.bfloat16, device="cuda")
+    parts = [p.view(t.shape) for p, t in zip(flat[1:].split([t.numel() for t in d]), d)]
+    for p, t in zip(parts, d):
+        p.copy_(t)
+        assert p.is_contiguous() and p.data_ptr() % 16 != 0
+    assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(out, given, parts), want))
