@@ -110,6 +110,20 @@ def _refuse_captured(*tensors):
             module.refuse_captured(*tensors)
 
 
+def _once(varies):
+    """once_differentiable, also where the gradients that come in need none: `varies(ctx)` says whether the ones that go out depend on inputs that do, and
+    then they must not pass for constants."""
+    def decorate(backward):
+        refused = once_differentiable(backward)
+
+        def wrapped(ctx, *grads):
+            if torch.is_grad_enabled() and not any(g.requires_grad for g in grads) and varies(ctx):
+                grads = [g.detach().requires_grad_() for g in grads]
+            return refused(ctx, *grads)
+        return wrapped
+    return decorate
+
+
 def _workspace(n, device):
     return torch.empty(max(int(n), 16), dtype=torch.uint8, device=device)
 
@@ -164,7 +178,7 @@ class _SkrullNorm(torch.autograd.Function):
         return y
 
     @staticmethod
-    @once_differentiable
+    @_once(lambda ctx: ctx.needs_input_grad[0])   # (without x's, dx is not asked for, and dw and db depend on no weight)
     def backward(ctx, dy):
         x, weight, mean, rstd = ctx.saved_tensors
         dy = _rows(dy)
@@ -206,7 +220,7 @@ class _SkrullCrossEntropy(torch.autograd.Function):
         return loss
 
     @staticmethod
-    @once_differentiable
+    @_once(lambda ctx: True)
     def backward(ctx, d_loss):
         x, weight, target, lse = ctx.saved_tensors
         dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if ctx.needs_input_grad[0] else None

@@ -180,10 +180,12 @@ bool differentiable(std::initializer_list<const at::Tensor *> inputs)
     return at::GradMode::is_enabled() && std::any_of(inputs.begin(), inputs.end(), [](const at::Tensor *t) { return t->defined() && t->requires_grad(); });
 }
 
-// A gradient that is asked for with create_graph cannot be differentiated again.
-variable_list once(const variable_list &grads, variable_list out)
+// A gradient that is asked for with create_graph cannot be differentiated again.  `varies`: whether it depends on inputs that need gradients, so that it is
+// no constant where the gradients that come in are.
+variable_list once(const variable_list &grads, variable_list out, bool varies = false)
 {
-    if (!at::GradMode::is_enabled() || !std::any_of(grads.begin(), grads.end(), [](const at::Tensor &g) { return g.defined() && g.requires_grad(); })) return out;
+    if (!at::GradMode::is_enabled()) return out;
+    if (!varies && !std::any_of(grads.begin(), grads.end(), [](const at::Tensor &g) { return g.defined() && g.requires_grad(); })) return out;
     const auto error = std::make_shared<torch::autograd::DelayedError>("the gradients of this operator cannot be differentiated again", (int)out.size());
     variable_list given;
     for (const at::Tensor &t : out) given.push_back(t.defined() ? t.detach().requires_grad_() : t);
@@ -230,7 +232,7 @@ struct Norm : torch::autograd::Node {
         check(skrull_norm_bwd(&p, x.data_ptr(), w.data_ptr(), mean, mean + x.size(0), dy.data_ptr(), dx.data_ptr(), address(out[1]), address(out[2]), address(ws), (size_t)bytes,
                               current_stream()));
         if (task_should_compute_output(0)) out[0] = std::move(dx);
-        return once(grads, std::move(out));
+        return once(grads, std::move(out), x.requires_grad());   // (without x's, dx is not asked for, and dw and db depend on no weight)
     }
     void release_variables() override
     {
@@ -282,7 +284,7 @@ struct CrossEntropy : torch::autograd::Function<CrossEntropy> {
         const at::Tensor ws = bytes_like(x, bytes);
         check(skrull_loss_bwd(&p, x.data_ptr(), w.data_ptr(), (const int64_t *)target.data_ptr(), (const float *)lse.data_ptr(), (const float *)d.data_ptr(), address(dx), address(dw),
                               ws.data_ptr(), (size_t)bytes, current_stream()));
-        return once(grads, {dx, dw, at::Tensor()});
+        return once(grads, {dx, dw, at::Tensor()}, true);
     }
     static at::Tensor run(const at::Tensor &x, const at::Tensor &w, const at::Tensor &target, const at::Tensor &lse)
     {

@@ -105,3 +105,41 @@ def test_rotary_takes_gradients_of_any_alignment(monkeypatch, watched):
         p.copy_(t)
         assert p.is_contiguous() and p.data_ptr() % 16 != 0
     assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(out, given, parts), want))
+
+
+@pytest.mark.parametrize("watched", [False, True])
+@pytest.mark.parametrize("i", [1, 2, 4])
+def test_gradients_of_gradients_are_refused_and_not_left_out(monkeypatch, i, watched):
+    """The norm's and the loss's gradients depend on their inputs, whether the gradient that comes in needs one or not: a penalty on them cannot
+    be differentiated, and must not pass for a constant."""
+    from paper_2505_19609_amd import autograd as A
+    monkeypatch.setattr(A, "_watched", lambda: watched)
+    inputs, call = _calls()[i]
+    given = [t.clone().requires_grad_() for t in inputs]
+    out = call(*given)
+    grads = torch.autograd.grad(out, given, torch.ones_like(out), create_graph=True)
+    with pytest.raises(RuntimeError, match="differentiate"):
+        (out.float().sum() + grads[0].float().square().sum()).backward()
+
+
+@pytest.mark.parametrize("watched", [False, True])
+def test_gradients_that_depend_on_nothing_are_constants(monkeypatch, watched):
+    """Rotary's gradients depend on the ones that come in alone; so do the norm's of weight and bias where x is given."""
+    from paper_2505_19609_amd import autograd as A
+    monkeypatch.setattr(A, "_watched", lambda: watched)
+    calls = _calls()
+    (q, k), call = calls[0]
+    given = [t.clone().requires_grad_() for t in (q, k)]
+    out = call(*given)
+    d = [torch.ones_like(o) for o in out]
+    want = torch.autograd.grad(out, given, d, retain_graph=True)
+    grads = torch.autograd.grad(out, given, d, create_graph=True)
+    (out[0].float().sum() + out[1].float().sum() + grads[0].float().sum()).backward()
+    assert all(torch.equal(t.grad, g) for t, g in zip(given, want))
+    (x, w, b), call = calls[1]
+    w, b = w.clone().requires_grad_(), b.clone().requires_grad_()
+    y = call(x, w, b)
+    want = torch.autograd.grad(y, (w, b), torch.ones_like(y), retain_graph=True)
+    grads = torch.autograd.grad(y, (w, b), torch.ones_like(y), create_graph=True)
+    (y.float().sum() + grads[0].float().square().sum()).backward()
+    assert torch.equal(w.grad, want[0]) and torch.equal(b.grad, want[1])
