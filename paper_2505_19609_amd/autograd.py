@@ -131,7 +131,7 @@ def _workspace(n, device):
 class _SkrullRotary(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, plan, rotary, k_rows):
-        ctx.plan, ctx.rotary, ctx.k_rows = plan, rotary, k_rows
+        ctx.plan, ctx.rotary, ctx.k_rows = plan, B.Rotary.from_buffer_copy(rotary), k_rows   # (the program may change its own)
         out = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k)]
         B.skrull_rotary(plan, rotary, q, k, *out, k_rows=k_rows)
         return tuple(out)

@@ -6,7 +6,7 @@ import math
 import pytest
 import torch
 
-from test_gpu_operators import BF16, FP32, TINY, _calls, _check_loss, _gen, _loss_case, _loss_in_64_bits, _randn, _within
+from test_gpu_operators import BF16, FP32, SHAPES, TINY, _calls, _check_loss, _gen, _loss_case, _loss_in_64_bits, _plan, _randn, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -143,3 +143,20 @@ def test_gradients_that_depend_on_nothing_are_constants(monkeypatch, watched):
     grads = torch.autograd.grad(y, (w, b), torch.ones_like(y), create_graph=True)
     (y.float().sum() + grads[0].float().square().sum()).backward()
     assert torch.equal(w.grad, want[0]) and torch.equal(b.grad, want[1])
+
+
+@pytest.mark.parametrize("watched", [False, True])
+def test_rotary_turns_back_by_what_it_was_called_with(monkeypatch, watched):
+    """The frequencies of the forward, also where the program has changed its struct since."""
+    from paper_2505_19609_amd import autograd as A
+    from paper_2505_19609_amd import binding as B
+    monkeypatch.setattr(A, "_watched", lambda: watched)
+    gen = _gen(6)
+    plan, rotary = _plan(SHAPES[3], (4, 2), 64), B.skrull_rotary_init(64)
+    q, k = (_randn(gen, n, h, 64).requires_grad_() for n, h in ((plan.total_q, 4), (plan.total_k, 2)))
+    out = A.skrull_rotary(q, k, plan, rotary)
+    d = [_randn(gen, *o.shape) for o in out]
+    want = torch.autograd.grad(out, (q, k), d, retain_graph=True)
+    rotary.base = 5e5
+    assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(out, (q, k), d), want))
+    plan.destroy()
