@@ -6,7 +6,8 @@ import math
 import pytest
 import torch
 
-from test_gpu_operators import BF16, FP32, SHAPES, TINY, _calls, _check_loss, _gen, _loss_case, _loss_in_64_bits, _plan, _randn, _within
+from test_gpu_operators import (BF16, FP32, SHAPES, TINY, _calls, _check_loss, _gen, _loss_case, _loss_in_64_bits, _norm_in_64_bits, _plan,
+                                _randn, _within)
 
 pytestmark = pytest.mark.gpu
 
@@ -160,3 +161,123 @@ def test_rotary_turns_back_by_what_it_was_called_with(monkeypatch, watched):
     rotary.base = 5e5
     assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(out, (q, k), d), want))
     plan.destroy()
+
+
+# ---- norm: several rows to a wavefront or workgroup --------------------------------------------------------------------
+
+# Each of the six forms (lanes of a row, pieces of a lane, narrow rows) with three rows and more to every wavefront or workgroup of the forward and the
+# backward, and an uneven end.
+LOOPED = [(13001, 5), (13000, 136), (9001, 1001), (3100, 1032), (3100, 4096), (1600, 8192)]
+
+
+@pytest.mark.parametrize("rows,cols", LOOPED)
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("t", [torch.bfloat16, torch.float32])
+def test_norm_of_several_rows_to_a_workgroup(rows, cols, kind, t):
+    from paper_2505_19609_amd import binding as B
+    gen = _gen(rows + cols)
+    layer = kind == "layer"
+    x = (_randn(gen, rows, cols, dtype=torch.float32) * _randn(gen, rows, 1, dtype=torch.float32).exp() + 3.0).to(t)
+    w = (_randn(gen, cols, dtype=torch.float32, scale=0.3) + 1.0).to(t)
+    b = _randn(gen, cols, dtype=t) if layer else None
+    dy = _randn(gen, rows, cols, dtype=t)
+    eps, number = 1e-3, B.NORM_LAYER if layer else B.NORM_RMS
+    mean, rstd = torch.empty((2, rows), device="cuda")
+
+    def both(x, given_x, y, dy, dx):
+        dw, db = torch.empty_like(w), torch.empty_like(w) if layer else None
+        B.skrull_norm_fwd(x, w, b, y, mean, rstd, eps, number)
+        y = y.clone()
+        ws = torch.full((B.skrull_norm_workspace(x, w, number),), 0xFF, dtype=torch.uint8, device="cuda")
+        B.skrull_norm_bwd(given_x, w, mean, rstd, dy, dx, dw, db, ws, number)
+        return {"y": y, "dx": dx.clone(), "dw": dw, **({"db": db} if layer else {})}
+
+    got = both(x, x, torch.empty_like(x), dy, torch.empty_like(x))
+    want = _norm_in_64_bits(x, w, b, dy, eps, layer)
+    for name, value in got.items():
+        exact, error = want[name]
+        _within(value, exact, error * 1.01 + (BF16 if t == torch.bfloat16 else FP32) * (exact.abs() + error) + TINY, name)
+    del want
+    # y in the place of x, dx in the place of dy, then of x: the same bits
+    place = x.clone()
+    again = both(place, x, place, dy, dy)
+    assert all(torch.equal(again[n], got[n]) for n in got)
+    dy = _randn(gen, rows, cols, dtype=t)
+    want = both(x, x, place, dy, torch.empty_like(x))
+    again = both(x, x, place, dy, x)
+    assert all(torch.equal(again[n], want[n]) for n in want)
+
+
+# ---- loss: what larger calls take --------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("rows", [33001, 70001])
+def test_loss_of_more_than_64_rows_to_a_gathering_workgroup(rows):
+    """A workgroup gathers rows / 512 rows, 64 at a time."""
+    x, w, target, d = _loss_case(rows, 64, 96, 0.3)
+    target[1000:9000] = -1
+    target[20000:30000:2] = -5
+    loss, dx, _ = _check_loss(x, w, target, d)
+    assert (loss[target < 0] == 0).all() and (dx[target < 0] == 0).all()
+
+
+def test_loss_of_several_tiles_to_a_workgroup():
+    """Tiles of 256 x 256, more of them than workgroups, several steps each and the last one ragged: loads run ahead across the ends of tiles."""
+    _check_loss(*_loss_case(1100, 200, 20003, 0.1))
+    _check_loss(*_loss_case(2300, 328, 20003, 0.0))
+
+
+def _pieces(rows, vocab, hidden):
+    """The rule for the backward's pieces of the vocabulary (csrc/loss.hip: Piece), where all rows have a target: tiles of 256 words of an even cut, of the
+    other one, and whether that is taken."""
+    row_tiles, words, h_tiles = -(-rows // 256), -(-vocab // 256), -(-hidden // 256)
+    room = min(row_tiles * 256 * (min(words * 256, 1 << 20) + 64), max(1 << 30, row_tiles * 256 * 320))
+    most = min(max((room // (row_tiles * 256) - 64) // 256, 1), 4096)
+    count = -(-words // most)
+    even, whole, h = -(-words // count), 256, h_tiles
+    while whole > 1 and h % 2 == 0:
+        whole, h = whole // 2, h // 2
+    other = most // whole * whole
+
+    def rounds(tiles):
+        return words // tiles * -(-tiles * h_tiles // 256) + -(-(words % tiles) * h_tiles // 256)
+    return even, other, count > 1 and most >= whole and -(-words // other) <= count and rounds(other) < rounds(even)
+
+
+def test_loss_in_pieces_that_make_whole_rounds_of_tiles():
+    """Two pieces of unequal size, 384 tiles of words and 163, with more than one tile of hidden values."""
+    rows, hidden, vocab = 8192, 264, 140003
+    assert _pieces(rows, vocab, hidden) == (274, 384, True)
+    x, w, target, d = _loss_case(rows, hidden, vocab, 0.0)
+    border = 384 * 256
+    target[:6] = torch.tensor([0, border - 1, border, border + 1, vocab - 2, vocab - 1], device="cuda")
+    parts = [_loss_in_64_bits(x[i:i + 1024], w, target[i:i + 1024], d[i:i + 1024]) for i in range(0, rows, 1024)]
+    want = {n: tuple(torch.cat([p[n][k] for p in parts]) for k in (0, 1)) for n in ("loss", "dx")}
+    # (a sum over all rows has rows + 64 roundings, not the 1,024 + 64 of a part's bound, each of at most 2^-24 of the sum of |dz x|, and |dz| <= |d| (p + [target]))
+    want["dw"] = tuple(sum(p["dw"][k] for p in parts) for k in (0, 1))
+    p_at_most = torch.zeros(vocab, hidden, dtype=torch.float64, device="cuda")
+    for i in range(0, rows, 1024):
+        p = (x[i:i + 1024].double() @ w.double().t()).softmax(1)
+        p[torch.arange(1024, device="cuda"), target[i:i + 1024]] += 1.0
+        p_at_most += (p * d[i:i + 1024, None].double().abs()).t() @ x[i:i + 1024].double().abs()
+    want["dw"] = (want["dw"][0], want["dw"][1] + (rows + 64) * FP32 * p_at_most)
+    _check_loss(x, w, target, d, want)
+
+
+@pytest.mark.parametrize("rows,offset", [(5, 0.0), (5, -200.0), (70, 0.0)])
+def test_loss_of_few_rows_in_pieces(rows, offset):
+    """More than 2^20 words: two pieces, dz in two bf16, parts of dX added to over the pieces, the second one with fewer steps than parts."""
+    hidden, vocab = 24, (1 << 20) + 777
+    assert _pieces(rows, vocab, hidden) == (2050, 4096, True)
+    x, w, target, d = _loss_case(rows, hidden, vocab, 0.0)
+    if offset:
+        x[:, 0], w[:, 0] = offset / 8, 8.0
+    target[:5] = torch.tensor([0, (1 << 20) - 1, 1 << 20, vocab - 1, vocab - 10], device="cuda")
+    _check_loss(x, w, target, d)
+
+
+def test_loss_of_a_short_last_tile_with_few_rows_and_a_target_in_it():
+    """The last word alone in its tile, strip and step, as target and not."""
+    for vocab in (257, 4097, 65537):
+        x, w, target, d = _loss_case(97, 64, vocab, 0.2)
+        target[:3] = torch.tensor([vocab - 1, vocab - 2, 0], device="cuda")
+        _check_loss(x, w, target, d)
