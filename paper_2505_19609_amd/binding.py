@@ -410,6 +410,14 @@ def _refuse(why):
     raise SkrullError(SKRULL_EINVAL, f"invalid argument ({why})")
 
 
+def _int32(value, name):
+    """`value` for a field of 32 bits, of which ctypes would keep the low ones."""
+    value = int(value)
+    if not -(1 << 31) <= value < 1 << 31:
+        _refuse(f"{name} {value}")
+    return value
+
+
 def _on_current_device(*tensors):
     import torch
     device = torch.cuda.current_device() if torch.cuda.is_initialized() else -2   # (-1: of a tensor that is on no GPU)
@@ -421,8 +429,8 @@ def _on_current_device(*tensors):
 def skrull_rotary_init(head_dim, rotary_dim=None, layout=ROTARY_HALF, base=10000.0, scaling=ROTARY_PLAIN, factor=1.0,
                        original_length=0.0, low_turns=0.0, high_turns=0.0, amplitude=1.0) -> Rotary:
     """What skrull_rotary needs to know of the model, checked."""
-    r = Rotary(int(head_dim), int(head_dim if rotary_dim is None else rotary_dim), int(layout), int(scaling), float(base),
-               float(factor), float(original_length), float(low_turns), float(high_turns), float(amplitude))
+    r = Rotary(_int32(head_dim, "head_dim"), _int32(head_dim if rotary_dim is None else rotary_dim, "rotary_dim"), _int32(layout, "layout"),
+               _int32(scaling, "scaling"), float(base), float(factor), float(original_length), float(low_turns), float(high_turns), float(amplitude))
     _check(lib().skrull_rotary_check(ctypes.byref(r)))
     return r
 
@@ -440,7 +448,7 @@ def _rotary_tensor(info, x, out, rows):
         if one != 1 or (head != d and shape[1] > 1):
             _refuse("the heads of a row must be contiguous")
         strides.append(row if want > 1 else shape[1] * d)   # (a single row's stride says nothing)
-    return RotaryTensor(x.data_ptr(), out.data_ptr(), strides[0], strides[1], shape[1], rows)
+    return RotaryTensor(x.data_ptr(), out.data_ptr(), strides[0], strides[1], _int32(shape[1], "heads"), _int32(rows, "rows"))
 
 
 _turn = None
@@ -483,7 +491,7 @@ def _type_of(t):
 
 
 def _norm_of(x, weight, eps, kind, **rows) -> Norm:
-    p = Norm(x.shape[0] if x.dim() == 2 else -1, x.shape[-1], int(kind), _type_of(x), _type_of(weight), float(eps))
+    p = Norm(x.shape[0] if x.dim() == 2 else -1, _int32(x.shape[-1], "cols"), _int32(kind, "kind"), _type_of(x), _type_of(weight), float(eps))
     for name, t in dict(rows, x=x).items():
         if t.dim() != 2 or t.shape != x.shape or t.dtype != x.dtype or (t.shape[1] > 1 and t.stride(1) != 1):
             _refuse(f"{name} must be {x.dtype} [rows, cols] with contiguous rows, as x is")
@@ -540,7 +548,7 @@ def _loss_of(x, weight, target) -> Loss:
         _refuse(f"weight must be contiguous bf16 [vocab, {x.shape[1]}], got {weight.dtype} {list(weight.shape)}")
     if target is not None and (target.dtype != torch.int64 or target.shape != (x.shape[0],) or not target.is_contiguous()):
         _refuse(f"target must be contiguous int64 [{x.shape[0]}], got {target.dtype} {list(target.shape)}")
-    return Loss(x.shape[0], x.shape[1], weight.shape[0], x.stride(0) if x.shape[0] > 1 else x.shape[1])
+    return Loss(x.shape[0], _int32(x.shape[1], "hidden"), _int32(weight.shape[0], "vocab"), x.stride(0) if x.shape[0] > 1 else x.shape[1])
 
 
 def skrull_loss_workspace(x, weight, backward: bool) -> int:
