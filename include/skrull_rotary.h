@@ -13,7 +13,7 @@
  *   SKRULL_ROTARY_PLAIN   as it is
  *   SKRULL_ROTARY_LINEAR  f_i / factor
  *   SKRULL_ROTARY_NTK     with the base times factor^(r / (r - 2)), r = rotary_dim: the first pair keeps its frequency, the
- *                         last one's is divided by factor (r = 2 has one pair, which keeps its frequency)
+ *                         last one's is divided by factor
  *   SKRULL_ROTARY_PARTS   by the turns n_i = original_length * f_i / (2 pi) that the pair makes in the original length:
  *                         f_i * (g + (1 - g) / factor) with g = (n_i - low_turns) / (high_turns - low_turns) within 0 and 1
  * The angle's whole turns are taken off in 64 bits (an angle of 131,072 radians has steps of 0.008 in 32), its sine and cosine

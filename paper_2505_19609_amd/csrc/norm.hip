@@ -29,12 +29,10 @@ struct NormArgs {
     float eps, inv_cols;
 };
 
-__device__ __forceinline__ float bf16_at(uint16_t u) { return __builtin_bit_cast(float, (uint32_t)u << 16); }
 __device__ __forceinline__ uint16_t to_bf16(float f) { return (uint16_t)pack_bf16(f, f); }
 
 struct Bf16 {
     typedef uint16_t type;
-    static __device__ __forceinline__ float get(uint16_t u) { return bf16_at(u); }
     static __device__ __forceinline__ uint16_t put(float f) { return to_bf16(f); }
     struct Raw { uint4 v; };   // 8 values as they lie in memory
     static __device__ __forceinline__ Raw load8(const uint16_t *p)
@@ -67,7 +65,6 @@ struct Bf16 {
 };
 struct Fp32 {
     typedef float type;
-    static __device__ __forceinline__ float get(float u) { return u; }
     static __device__ __forceinline__ float put(float f) { return f; }
     struct Raw { float4 a, b; };
     static __device__ __forceinline__ Raw load8(const float *p)

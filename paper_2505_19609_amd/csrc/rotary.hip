@@ -220,7 +220,7 @@ int skrull_rotary(const skrull_attn_plan_t *plan, const skrull_rotary_t *r, cons
     a.rotary_dim = r->rotary_dim;
     a.scaling = r->scaling;
     a.log2_base = log2(r->base);
-    if (r->scaling == SKRULL_ROTARY_NTK && r->rotary_dim > 2)
+    if (r->scaling == SKRULL_ROTARY_NTK)
         a.log2_base += log2(r->factor) * (double)r->rotary_dim / (double)(r->rotary_dim - 2);
     a.factor = r->factor;
     a.turns_scale = r->original_length;
