@@ -29,6 +29,15 @@ def test_loss_of_logits_with_a_common_offset(rows, hidden, vocab, offset):
     _check_loss(x, w, target, d)
 
 
+@pytest.mark.parametrize("offset", [-3e10, 3e10, -1e20, 1e20, -1e30, 1e30])
+@pytest.mark.parametrize("rows,hidden,vocab", [(37, 64, 300), (500, 136, 4099), (100, 64, 70019), (1100, 200, 19971)])
+def test_loss_of_finite_logits_is_finite(rows, hidden, vocab, offset):
+    """Of any size: what is left of such a row's differences is within fp32's spacing, which is the bounds' too."""
+    x, w, target, d = _loss_case(rows, hidden, vocab, 0.25)
+    x[:, 0], w[:, 0] = offset / 8, 8.0
+    _check_loss(x, w, target, d)
+
+
 @pytest.mark.parametrize("offset", [-100.0, 100.0])
 @pytest.mark.parametrize("rows,hidden,vocab", [(37, 64, 300), (500, 136, 4099), (1100, 200, 19971)])
 def test_loss_of_strips_whose_words_are_all_masked(rows, hidden, vocab, offset):
