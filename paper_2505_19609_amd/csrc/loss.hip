@@ -10,7 +10,7 @@
 //   dX       dz W                  fp32, added up over the pieces (and over parts of the vocabulary where there are few tiles)
 //   dW^T     X^T dz                a piece's rows of dW are complete after one product
 // What bounds them is the matrix pipe: 2 T V H operations each, against 2 (T + V) H bytes; with few rows reading W (37 rows, 896 hidden, 32,003 words, 57 MB:
-// forward 23 us of which the product takes 13, backward 65).
+// forward 23 us of which the product takes 13, backward 60 with W in the caches; 26 and 70 from memory).
 //
 // A workgroup is 4 wavefronts, one per SIMD, and forms a tile of 256 x 256 (x 64 or 128 where there are few rows): each wavefront 128 x 128, 8 x 8 results of
 // v_mfma_f32_16x16x32_bf16 in 256 accumulator registers, so that an operand fragment read from LDS feeds eight products.  Steps of 64 along
@@ -30,12 +30,12 @@ namespace {
 constexpr int kTile = 256;       // rows and columns of a result tile
 constexpr int kStep = 64;        // of the contraction
 constexpr int kGrid = 256;       // workgroups: one per compute unit, each as much LDS as allows no second one
-constexpr int64_t kPieceBytes = (int64_t)2 << 30;  // of dz at most
+constexpr int64_t kPieceBytes = (int64_t)2 << 30;  // of dz at most, but for one tile of words of all rows: 640 bytes a row, more than that from 3.4 million rows on
 // Rows of dz and of the gathered x are this much longer where their length is a multiple of 4 KB: the 256 rows of a tile would lie in few of the L2's sets.
 constexpr int kPitchPad = 64;
 constexpr int kMaxPieceWords = 1 << 20;            // (32-bit offsets within a tile of dz)
 // With so few rows or fewer the backward has each of them twice, the second time with what rounding dz to bf16 leaves: dx and dw have no error but their own
-// type's.  It costs little where W is what the products wait for (64 rows, 3,584 hidden, 128,000 words: 728 us and not 657; 37, 896, 32,003: 72 and 61).  (Where many
+// type's.  It costs little where W is what the products wait for (64 rows, 3,584 hidden, 128,000 words: backward 731 us and not 655; 37, 896, 32,003: 70 and 61).  (Where many
 // rows add up, dz's roundings cost as much as the result's own: 2.4e-3 of a gradient's norm against 1.7e-3.  A single row's are all or nothing.)
 constexpr int kTwice = kTile / 2;
 // The second time begins at a multiple of 32: both together are a whole number of steps of dW (20 rows, 3,584 hidden, 60,000 words: dX and dW 189 us, 222 with

@@ -92,7 +92,7 @@ struct Fp32 {
 
 // A lane's piece of 8 columns.  The last piece of a row whose width is no multiple of 8 is its last 8 columns, of which the first ones
 // belong to the lane before; rows narrower than 8 (SMALL) have one piece that is loaded value by value.  Rows need no alignment but their type's: the hardware takes 16 bytes
-// from any address (7,013 rows of 1,001 bf16, backward: 34 us with a load for each value, the lanes' side by side, 19 this way).
+// from any address (7,013 rows of 1,001 bf16, backward: 34 us with a load for each value, the lanes' side by side, 17 this way).
 template <bool SMALL>
 struct Columns {
     int first, skip;   // the piece's values from `skip` on are this lane's (8: none); SMALL: those below 8 - skip
@@ -106,7 +106,8 @@ struct Columns {
 };
 
 // A lane's pieces of a row, zero where they are not its own.  They are fetched a row ahead of their use, so that they arrive while the row before is
-// summed up (13,312 rows of 3,584 bf16: forward and backward 52 and 101 us without, 41 and 61 with).
+// summed up (backward of 32,768 rows of 4,096 fp32: 313 us without, 285 with; of 8,192 of 8,192 bf16 82 and 77; 13,312 of 3,584 bf16 61 and 60, and there the
+// forward 37 and 38).
 template <class T, int C, bool SMALL>
 struct RowPieces {
     typename T::Raw raw[C];
@@ -165,7 +166,7 @@ __device__ __forceinline__ void load_weight(const void *w, int type, const Colum
     else load_weight<Fp32>(w, k, f);
 }
 
-// Sums of N values over the lanes of a row, in every lane.  `lds`: room for 2 x 16 x N floats of this row, used by turns.
+// Sums of N values over the lanes of a row, in every lane.  `lds`: room for 2 x WAVES x N floats, used by turns.
 template <int WAVES, int N>
 __device__ __forceinline__ void row_sums(float v[N], float *lds, int &turn)
 {
@@ -406,7 +407,7 @@ int check_apart(const char *out_name, const void *out, int64_t out_stride, const
 int waves_of(int cols) { return cols <= 1024 ? 1 : cols <= 4096 ? 4 : 16; }
 
 // Workgroups of the backward, each with a line of partial sums: as many as have 32 KB of rows among them on a compute unit, one to four (13,312 x 3,584 bf16:
-// 61 us with two, 66 with one or four; 32,768 x 4,096 fp32: 286 with one, 313 with two or four; 26,624 x 896 bf16: 34 with two, 38 with four).
+// 60 us with two, 64 with one or four; 32,768 x 4,096 fp32: 285 with one, 311 with two or four; 26,624 x 896 bf16: 33 with two, 36 with one, 40 with four).
 constexpr int kComputeUnits = 256;
 int64_t bwd_blocks(const skrull_norm_t *p)
 {
@@ -467,7 +468,7 @@ int skrull_norm_fwd(const skrull_norm_t *p, const void *x, const void *w, const 
     a.x_stride = p->x_stride; a.y_stride = p->y_stride; a.rows = p->rows; a.cols = p->cols; a.weight_type = p->weight_type;
     a.eps = p->eps; a.inv_cols = 1.0f / (float)p->cols;
     const int waves = waves_of(p->cols), rows = waves == 1 ? 4 : 1;
-    // (13,312 x 3,584 bf16: 41 us with four workgroups to a compute unit, 46 with eight; 26,624 x 896: 21 and 27)
+    // (13,312 x 3,584 bf16, layer norm: 39 us with four workgroups to a compute unit, 43 with eight; 26,624 x 896 without a mean: 19 and 20.5)
     const int64_t most = (int64_t)compute_units * (waves == 16 ? 2 : 4), need = (p->rows + rows - 1) / rows;
     launch(false, p, a, (int)(need < most ? need : most), (hipStream_t)hip_stream);
     const hipError_t e = hipGetLastError();
