@@ -211,6 +211,43 @@ def skrull_norm(x, weight, bias=None, eps=1e-5, kind="layer"):
     return y
 
 
+class _SkrullResidualNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, r, z, weight, bias, post_weight, post_bias, gate, scale, eps, kind):
+        r_out, y = torch.empty(r.shape, dtype=r.dtype, device=r.device), torch.empty(z.shape, dtype=z.dtype, device=z.device)
+        stats = torch.empty((4, z.shape[0]), dtype=torch.float32, device=z.device)
+        B.skrull_residual_fwd(r, z, weight, bias, post_weight, post_bias, gate, r_out, y, stats, scale, eps, kind)
+        ctx.scale, ctx.kind, ctx.bias = scale, kind, bias is not None
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(r, z, weight, post_weight, post_bias, gate, stats)
+        return r_out, y
+
+    @staticmethod
+    @_once(lambda ctx: any(ctx.needs_input_grad[:7]))
+    def backward(ctx, d_r_out, dy):
+        r, z, weight, post_weight, post_bias, gate, stats = ctx.saved_tensors
+        d_r_out, dy = (None if t is None else _rows(t) for t in (d_r_out, dy))
+        dr, dz = torch.empty(r.shape, dtype=r.dtype, device=r.device), torch.empty(z.shape, dtype=z.dtype, device=z.device)
+        vectors = [torch.empty_like(weight) if there and needed else None
+                   for there, needed in zip((True, ctx.bias, post_weight is not None, post_bias is not None, gate is not None), ctx.needs_input_grad[2:7])]
+        ws = _workspace(B.skrull_residual_workspace(r, z, weight, ctx.kind), z.device) if any(t is not None for t in vectors) else None
+        B.skrull_residual_bwd(r, z, weight, post_weight, post_bias, gate, stats, d_r_out, dy, dr, dz, *vectors, ws, ctx.scale, ctx.kind)
+        return dr, dz, *vectors, None, None, None
+
+
+def skrull_residual_norm(r, z, weight, bias=None, post_weight=None, post_bias=None, gate=None, scale=1.0, eps=1e-5, kind="layer"):
+    """The residual stream r [rows, cols] after a block whose output is z: (scale * r + gate * n, the norm of that with weight and bias), where n is the norm of
+    z with post_weight and post_bias, or z itself.  Vectors [cols], of one type; "layer", or "rms" without means and biases.  z is bf16 or fp32, r of the same
+    type or fp32.  Differentiable with respect to all tensors."""
+    if kind not in _KINDS:
+        raise ValueError(f"kind must be one of {sorted(_KINDS)}")
+    if r.dim() != 2 or z.dim() != 2:
+        raise ValueError("r and z must be [rows, cols]")
+    vectors = (weight, bias, post_weight, post_bias, gate)
+    _refuse_captured(r, z, *vectors)
+    return _SkrullResidualNorm.apply(_rows(r), _rows(z), *(None if t is None else t.contiguous() for t in vectors), float(scale), float(eps), _KINDS[kind])
+
+
 class _SkrullCrossEntropy(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, target):

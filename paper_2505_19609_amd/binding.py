@@ -31,6 +31,8 @@ EXPORTED_SYMBOLS = ("skrull_attn_plan", "skrull_attn_plan_info", "skrull_attn_pl
 # the operators around attention (skrull_rotary.h, skrull_norm.h, skrull_loss.h)
 OPERATOR_SYMBOLS = ("skrull_rotary_check", "skrull_rotary", "skrull_norm_fwd", "skrull_norm_workspace", "skrull_norm_bwd",
                     "skrull_loss_workspace", "skrull_loss_fwd", "skrull_loss_bwd")
+# what else a block is made of (skrull_residual.h)
+BLOCK_SYMBOLS = ("skrull_residual_fwd", "skrull_residual_workspace", "skrull_residual_bwd")
 
 
 class Problem(ctypes.Structure):
@@ -94,6 +96,13 @@ class Norm(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int32), ("kind", ctypes.c_int32), ("type", ctypes.c_int32),
                 ("weight_type", ctypes.c_int32), ("eps", ctypes.c_float), ("x_stride", ctypes.c_int64),
                 ("y_stride", ctypes.c_int64), ("dy_stride", ctypes.c_int64), ("dx_stride", ctypes.c_int64)]
+
+
+class Residual(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int32), ("kind", ctypes.c_int32), ("type", ctypes.c_int32),
+                ("residual_type", ctypes.c_int32), ("weight_type", ctypes.c_int32), ("eps", ctypes.c_float), ("scale", ctypes.c_float),
+                ("r_stride", ctypes.c_int64), ("z_stride", ctypes.c_int64), ("r_out_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64),
+                ("d_r_out_stride", ctypes.c_int64), ("dy_stride", ctypes.c_int64), ("dr_stride", ctypes.c_int64), ("dz_stride", ctypes.c_int64)]
 
 
 class Loss(ctypes.Structure):
@@ -171,10 +180,14 @@ def lib():
         L.skrull_norm_fwd.argtypes = [norm] + [vp] * 7
         L.skrull_norm_workspace.argtypes = [norm]
         L.skrull_norm_bwd.argtypes = [norm] + [vp] * 9 + [ctypes.c_size_t, vp]
+        residual = ctypes.POINTER(Residual)
+        L.skrull_residual_fwd.argtypes = [residual] + [vp] * 11
+        L.skrull_residual_workspace.argtypes = [residual]
+        L.skrull_residual_bwd.argtypes = [residual] + [vp] * 17 + [ctypes.c_size_t, vp]
         L.skrull_loss_workspace.argtypes = [loss, ctypes.c_int]
         L.skrull_loss_fwd.argtypes = [loss] + [vp] * 6 + [ctypes.c_size_t, vp]
         L.skrull_loss_bwd.argtypes = [loss] + [vp] * 8 + [ctypes.c_size_t, vp]
-        for name in OPERATOR_SYMBOLS:
+        for name in OPERATOR_SYMBOLS + BLOCK_SYMBOLS:
             getattr(L, name).restype = ctypes.c_int64 if name.endswith("workspace") else ctypes.c_int
         _lib = L
     return _lib
@@ -538,6 +551,54 @@ def skrull_norm_bwd(x, weight, mean, rstd, dy, dx, dweight, dbias, workspace, ki
     _check(lib().skrull_norm_bwd(ctypes.byref(p), _ptr(x), _vector(weight, cols, wt, "weight"), _vector(mean, rows, torch.float32, "mean"),
                                  _vector(rstd, rows, torch.float32, "rstd"), _ptr(dy), _ptr(dx), _vector(dweight, cols, wt, "dweight"),
                                  _vector(dbias, cols, wt, "dbias"), *_scratch(workspace), _stream_ptr(stream)))
+
+
+def _residual_of(r, z, weight, scale, eps, kind, **rows) -> Residual:
+    p = Residual(z.shape[0] if z.dim() == 2 else -1, _int32(z.shape[-1], "cols"), _int32(kind, "kind"), _type_of(z), _type_of(r), _type_of(weight),
+                 float(eps), float(scale))
+    stream = ("r", "r_out", "d_r_out", "dr")
+    for name, t in dict(rows, r=r, z=z).items():
+        if t is None:
+            continue
+        like = r if name in stream else z
+        if t.dim() != 2 or t.shape != z.shape or t.dtype != like.dtype or (t.shape[1] > 1 and t.stride(1) != 1):
+            _refuse(f"{name} must be {like.dtype} {list(z.shape)} with contiguous rows, as {'r' if name in stream else 'z'} is")
+        setattr(p, name + "_stride", t.stride(0) if t.shape[0] > 1 else t.shape[1])
+    return p
+
+
+def _stats(stats, rows):
+    import torch
+    if stats is not None and (stats.shape != (4, rows) or stats.dtype != torch.float32 or not stats.is_contiguous()):
+        _refuse(f"stats must be contiguous torch.float32 [4, {rows}]")
+    return None if stats is None else _ptr(stats)
+
+
+def skrull_residual_fwd(r, z, weight, bias, post_weight, post_bias, gate, r_out, y, stats, scale=1.0, eps=1e-5, kind=NORM_LAYER, stream=None):
+    """r_out = scale r + gate n with n the norm of z (without post_weight: z), y = the norm of that sum; bias, post_weight, post_bias and gate may be
+    None.  stats (fp32 [4, rows], may be None) for the backward."""
+    _on_current_device(r, z, weight, bias, post_weight, post_bias, gate, r_out, y, stats)
+    p = _residual_of(r, z, weight, scale, eps, kind, r_out=r_out, y=y)
+    vectors = [_vector(t, p.cols, weight.dtype, n) for n, t in (("weight", weight), ("bias", bias), ("post_weight", post_weight), ("post_bias", post_bias),
+                                                                ("gate", gate))]
+    _check(lib().skrull_residual_fwd(ctypes.byref(p), _ptr(r), _ptr(z), *vectors, _ptr(r_out), _ptr(y), _stats(stats, p.rows), _stream_ptr(stream)))
+
+
+def skrull_residual_workspace(r, z, weight, kind=NORM_LAYER) -> int:
+    """Bytes that skrull_residual_bwd asks for."""
+    return int(lib().skrull_residual_workspace(ctypes.byref(_residual_of(r, z, weight, 1.0, 0.0, kind))))
+
+
+def skrull_residual_bwd(r, z, weight, post_weight, post_bias, gate, stats, d_r_out, dy, dr, dz, dweight, dbias, dpost_weight, dpost_bias, dgate, workspace,
+                        scale=1.0, kind=NORM_LAYER, stream=None):
+    """dr and dz, and the vectors' gradients where they are wanted (else None).  d_r_out or dy may be None: no gradient comes that way."""
+    _on_current_device(r, z, weight, post_weight, post_bias, gate, stats, d_r_out, dy, dr, dz, dweight, dbias, dpost_weight, dpost_bias, dgate, workspace)
+    p = _residual_of(r, z, weight, scale, 0.0, kind, d_r_out=d_r_out, dy=dy, dr=dr, dz=dz)
+    v = [_vector(t, p.cols, weight.dtype, n) for n, t in (("weight", weight), ("post_weight", post_weight), ("post_bias", post_bias), ("gate", gate),
+                                                          ("dweight", dweight), ("dbias", dbias), ("dpost_weight", dpost_weight),
+                                                          ("dpost_bias", dpost_bias), ("dgate", dgate))]
+    _check(lib().skrull_residual_bwd(ctypes.byref(p), _ptr(r), _ptr(z), *v[:4], _stats(stats, p.rows), None if d_r_out is None else _ptr(d_r_out),
+                                     None if dy is None else _ptr(dy), _ptr(dr), _ptr(dz), *v[4:], *_scratch(workspace), _stream_ptr(stream)))
 
 
 def _loss_of(x, weight, target) -> Loss:

@@ -1,0 +1,113 @@
+"""The operators that a block is made of (the residual stream) without a GPU: symbols, struct layouts and what the
+entry points refuse."""
+import ctypes
+import math
+import os
+import re
+
+import pytest
+import torch
+
+from paper_2505_19609_amd import autograd as A
+from paper_2505_19609_amd import binding as B
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+ONE = 1 << 20   # an address that is aligned and never read: the call fails first
+HEADERS = ("skrull_residual.h",)
+
+
+def test_library_exports_every_declared_operator():
+    header = "".join(open(os.path.join(ROOT, "include", f)).read() for f in HEADERS)
+    declared = set(re.findall(r"\b(skrull_(?:residual)(?:_[a-z]+)*)\s*\(", header))
+    assert declared == set(B.BLOCK_SYMBOLS)
+    for name in declared:
+        assert getattr(B.lib(), name) is not None
+
+
+def test_argument_counts_match_headers():
+    """What ctypes is told of each call is what the header declares."""
+    for f in HEADERS:
+        header = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", f)).read(), flags=re.S)
+        for name, args in re.findall(r"\b(skrull_[a-z_]+)\s*\(([^)]*)\)\s*;", header):
+            assert len(getattr(B.lib(), name).argtypes) == len(args.split(",")), name
+
+
+def test_struct_layouts_match_headers():
+    assert ctypes.sizeof(B.Residual) == 8 + 7 * 4 + 4 + 8 * 8   # (scale and its padding)
+
+
+# ---- the residual stream --------------------------------------------------------------------------------------------
+
+STRIDES = ("r_stride", "z_stride", "r_out_stride", "y_stride", "d_r_out_stride", "dy_stride", "dr_stride", "dz_stride")
+
+
+def _residual(**kw):
+    p = dict(rows=4, cols=64, kind=B.NORM_LAYER, type=B.TYPE_BF16, residual_type=B.TYPE_BF16, weight_type=B.TYPE_BF16, eps=1e-5, scale=1.0, **{s: 64 for s in STRIDES})
+    p.update(kw)
+    return B.Residual(**p)
+
+
+def _fwd(p, b=None, **kw):
+    a = dict(r=ONE, z=2 * ONE, w=3 * ONE, b=b, post_w=None, post_b=None, gate=None, r_out=4 * ONE, y=5 * ONE, stats=6 * ONE)
+    a.update(kw)
+    return B.lib().skrull_residual_fwd(ctypes.byref(p), *a.values(), None)
+
+
+def _bwd(p, workspace_bytes=1 << 30, **kw):
+    a = dict(r=ONE, z=2 * ONE, w=3 * ONE, post_w=None, post_b=None, gate=None, stats=6 * ONE, d_r_out=7 * ONE, dy=8 * ONE, dr=9 * ONE, dz=10 * ONE, dw=11 * ONE, db=None,
+             dpost_w=None, dpost_b=None, dgate=None, workspace=20 * ONE)
+    a.update(kw)
+    return B.lib().skrull_residual_bwd(ctypes.byref(p), *a.values(), workspace_bytes, None)
+
+
+WIDE = {s: 8193 for s in STRIDES}
+BAD = [dict(rows=-1), dict(rows=1 << 31), dict(cols=0), dict(cols=8193, **WIDE), dict(kind=2), dict(type=2), dict(residual_type=2),
+       dict(type=B.TYPE_FP32, residual_type=B.TYPE_BF16), dict(weight_type=-1), dict(eps=-1.0), dict(eps=math.nan), dict(scale=math.inf), dict(scale=math.nan),
+       dict(r_stride=63), dict(z_stride=-64)]
+
+
+@pytest.mark.parametrize("kw", BAD + [dict(r_out_stride=63), dict(y_stride=1 << 62)])
+def test_residual_fwd_refuses(kw):
+    assert _fwd(_residual(**kw)) == B.SKRULL_EINVAL
+    assert "residual" in B.skrull_attn_strerror(B.SKRULL_EINVAL)
+
+
+@pytest.mark.parametrize("kw", BAD + [dict(d_r_out_stride=63), dict(dy_stride=0), dict(dr_stride=63), dict(dz_stride=63)])
+def test_residual_bwd_refuses(kw):
+    assert _bwd(_residual(**kw)) == B.SKRULL_EINVAL
+    assert "residual" in B.skrull_attn_strerror(B.SKRULL_EINVAL)
+
+
+@pytest.mark.parametrize("kw", [dict(r=None), dict(z=None), dict(w=None), dict(r_out=None), dict(y=None), dict(r=ONE + 1), dict(w=3 * ONE + 1), dict(stats=6 * ONE + 2),
+                                dict(post_b=ONE), dict(r_out=ONE + 128), dict(y=2 * ONE + 2), dict(r_out=2 * ONE), dict(y=ONE), dict(y=4 * ONE), dict(gate=ONE + 1)])
+def test_residual_fwd_refuses_pointers(kw):
+    assert _fwd(_residual(), **kw) == B.SKRULL_EINVAL
+
+
+@pytest.mark.parametrize("kw", [dict(r=None), dict(z=None), dict(w=None), dict(stats=None), dict(dr=None), dict(dz=None), dict(workspace=None), dict(workspace=20 * ONE + 8), dict(workspace_bytes=64),
+                                dict(post_b=ONE), dict(dpost_w=ONE), dict(dpost_b=ONE), dict(dw=ONE + 1), dict(dr=7 * ONE), dict(dz=8 * ONE), dict(dz=9 * ONE + 2), dict(dr=ONE), dict(dz=2 * ONE)])
+def test_residual_bwd_refuses_pointers(kw):
+    assert _bwd(_residual(), **kw) == B.SKRULL_EINVAL
+
+
+def test_residual_refuses_biases_without_a_mean():
+    p = _residual(kind=B.NORM_RMS)
+    assert _fwd(p, b=ONE) == _fwd(p, post_w=ONE, post_b=ONE) == B.SKRULL_EINVAL
+    assert _bwd(p, db=ONE) == _bwd(p, post_w=ONE, post_b=ONE) == _bwd(p, post_w=ONE, dpost_b=ONE) == B.SKRULL_EINVAL
+
+
+def test_residual_workspace():
+    assert B.lib().skrull_residual_workspace(ctypes.byref(_residual(cols=0))) == 0
+    assert B.lib().skrull_residual_workspace(ctypes.byref(_residual())) >= 4 * 64 * 4
+    # (bounded however many rows there are)
+    assert B.lib().skrull_residual_workspace(ctypes.byref(_residual(rows=(1 << 31) - 1, cols=8192, **{s: 8192 for s in STRIDES}))) <= 64 << 20
+
+
+def test_residual_wrappers_refuse():
+    r, z, w = torch.zeros(4, 64), torch.zeros(4, 64), torch.zeros(64)
+    with pytest.raises(ValueError, match="kind"):
+        A.skrull_residual_norm(r, z, w, kind="batch")
+    with pytest.raises(ValueError, match="rows, cols"):
+        A.skrull_residual_norm(r[0], z, w)
+    with pytest.raises(B.SkrullError, match="current GPU"):
+        A.skrull_residual_norm(r, z, w)

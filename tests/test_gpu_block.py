@@ -1,0 +1,221 @@
+"""What a block is made of besides its attention, rotary positions and loss, on the GPU against plain implementations in 64 bits: the residual stream
+between two blocks.
+
+Tolerances are bounds, not observations: a rounding to bf16 is off by at most 2^-8 of the value (half a step is 2^-9 of the next power of two), one
+of fp32 by 2^-24, and a sum of n fp32 terms by at most n 2^-24 of the sum of their magnitudes; TINY covers results below bf16's normal numbers."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+BF16, FP32, TINY = 2.0 ** -8, 2.0 ** -24, 1e-30
+TYPES = {torch.bfloat16: BF16, torch.float32: FP32}
+
+
+def _randn(gen, *shape, dtype=torch.bfloat16, scale=1.0, mean=0.0):
+    return (torch.randn(shape, generator=gen, device="cuda") * scale + mean).to(dtype)
+
+
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _within(got, want, error, what):
+    """`error`: of the result before it is rounded to its type"""
+    assert got.shape == want.shape, what
+    assert torch.isfinite(got).all(), what
+    tolerance = error * 1.05 + TYPES[got.dtype] * (want.abs() + error) + TINY   # (5 %: products of two errors)
+    excess = ((got.double() - want).abs() - tolerance).max().item() if want.numel() else 0.0
+    assert excess <= 0.0, (what, excess, (got.double() - want).abs().max().item())
+
+
+def _padded(t, pad=24, fill=float("nan")):
+    """The rows of `t` inside wider ones: (the wider tensor, a view that equals t)."""
+    wide = torch.full((t.shape[0], t.shape[1] + pad), fill, dtype=t.dtype, device=t.device)
+    view = wide[:, :t.shape[1]]
+    view.copy_(t)
+    return wide, view
+
+
+# ---- the residual stream between two blocks -------------------------------------------------------------------------
+
+# roundings of a sum over a row: 8 values of a lane, 6 across a wavefront, 16 across wavefronts, and a few of the formula
+ROW = 64 * FP32
+
+
+def _mean(t):
+    return t.mean(1, keepdim=True)
+
+
+def _normed(x, ex, eps, layer):
+    """The normed x, 1 / its deviation, and the errors of both (the second one relative), given x's."""
+    mean = _mean(x) if layer else torch.zeros_like(x[:, :1])
+    rstd = 1 / (_mean((x - mean).square()) + eps).sqrt()
+    h = (x - mean) * rstd
+    e = ex + ROW * x.abs() + (_mean(ex) + ROW * _mean(x.abs()) if layer else 0.0)   # of x less its mean
+    relative = ROW + rstd * _mean(h.abs() * e)
+    return h, rstd, rstd * e + h.abs() * relative, relative
+
+
+def _norm_back(g, eg, h, eh, rstd, relative, layer):
+    m, size = _mean(g * h), _mean((g * h).abs())
+    em = _mean(g.abs() * eh + h.abs() * eg) + ROW * size
+    d, ed = g - h * m, eg + eh * m.abs() + h.abs() * em + ROW * (g.abs() + h.abs() * size)
+    if layer:
+        d, ed = d - _mean(g), ed + _mean(eg) + ROW * _mean(g.abs())
+    return d * rstd, ed * rstd + relative * (d * rstd).abs()
+
+
+def _residual_in_64_bits(r, z, w, b, pw, pb, gate, scale, d_r, dy, eps, layer):
+    """{name: (value, error)}: of each result in 64 bits, and what an evaluation in 32 bits may be off"""
+    r, z, w, b, pw, pb, gate, d_r, dy = (None if t is None else t.detach().double() for t in (r, z, w, b, pw, pb, gate, d_r, dy))
+    zero, rows = torch.zeros_like(z), len(z)
+    one, none = torch.ones_like(w), torch.zeros_like(w)
+    g, b1, b2 = (d if t is None else t for t, d in ((gate, one), (pb, none), (b, none)))
+    w1 = one if pw is None else pw
+    h1, rstd1, eh1, rel1 = (z, None, zero, None) if pw is None else _normed(z, zero, eps, layer)
+    n = h1 * w1 + b1
+    en = w1.abs() * eh1 + 4 * FP32 * ((h1 * w1).abs() + b1.abs())
+    x = scale * r + g * n
+    ex = g.abs() * en + 4 * FP32 * ((scale * r).abs() + g.abs() * ((h1 * w1).abs() + b1.abs()))
+    h2, rstd2, eh2, rel2 = _normed(x, ex, eps, layer)
+    out = {"r": (x, ex), "y": (h2 * w + b2, w.abs() * eh2 + 4 * FP32 * ((h2 * w).abs() + b2.abs()))}
+    if d_r is None and dy is None:
+        return out
+    e, ee = (zero, zero) if dy is None else _norm_back(dy * w, FP32 * (dy * w).abs(), h2, eh2, rstd2, rel2, layer)
+    if d_r is not None:
+        e, ee = e + d_r, ee + 2 * FP32 * (e.abs() + d_r.abs())
+    if dy is None:
+        dy = zero
+    out["dr"] = (scale * e, abs(scale) * ee + 2 * FP32 * (scale * e).abs())
+    g1, eg1 = e * g * w1, (g * w1).abs() * (ee + 4 * FP32 * e.abs())
+    out["dz"] = (g1, eg1) if pw is None else _norm_back(g1, eg1, h1, eh1, rstd1, rel1, layer)
+    sums = (rows + 64) * FP32
+    E1, eE1 = (e * h1).sum(0), (h1.abs() * ee + e.abs() * eh1 + sums * (e * h1).abs()).sum(0)
+    E0, eE0 = e.sum(0), (ee + sums * e.abs()).sum(0)
+    out.update(dw=((dy * h2).sum(0), (dy.abs() * eh2 + sums * (dy * h2).abs()).sum(0)), db=(dy.sum(0), sums * dy.abs().sum(0)),
+               dpw=(g * E1, g.abs() * eE1 + 2 * FP32 * (g * E1).abs()), dpb=(g * E0, g.abs() * eE0 + 2 * FP32 * (g * E0).abs()),
+               dgate=(w1 * E1 + b1 * E0, w1.abs() * eE1 + b1.abs() * eE0 + 4 * FP32 * ((w1 * E1).abs() + (b1 * E0).abs())))
+    return out
+
+
+RESIDUAL_SHAPES = [(1, 1), (1, 64), (3, 7), (5, 8), (3, 9), (5, 896), (64, 512), (33, 513), (2, 1024), (130, 1025), (9, 2048), (700, 3584), (17, 4096), (6, 4097), (3, 8192), (600, 8190),
+                   (5000, 104)]
+NAMES = ("r", "z", "w", "b", "pw", "pb", "gate")
+
+
+def _residual_inputs(gen, rows, cols, t, rt, wt, b, pw, pb, gate):
+    r = (_randn(gen, rows, cols, dtype=torch.float32) * _randn(gen, rows, 1, dtype=torch.float32).exp() + 2.0).to(rt)
+    vectors = [_randn(gen, cols, dtype=wt, scale=0.3, mean=m) if there else None for m, there in ((1.0, True), (0.0, b), (1.0, pw), (0.0, pb), (0.5, gate))]
+    return [r, _randn(gen, rows, cols, dtype=t, mean=0.5), *vectors]
+
+
+@pytest.mark.parametrize("rows,cols", RESIDUAL_SHAPES)
+@pytest.mark.parametrize("kind,b,pw,pb,gate", [("rms", 0, 0, 0, 0), ("rms", 0, 1, 0, 1), ("layer", 1, 1, 1, 1), ("layer", 0, 0, 0, 1), ("layer", 1, 1, 0, 0)])
+@pytest.mark.parametrize("t,rt,wt", [(torch.bfloat16, torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32, torch.float32), (torch.float32, torch.float32, torch.bfloat16)])
+def test_residual_norm(rows, cols, kind, b, pw, pb, gate, t, rt, wt):
+    from paper_2505_19609_amd.autograd import skrull_residual_norm
+    gen = _gen(rows * 10007 + cols)
+    given = [None if v is None else v.requires_grad_() for v in _residual_inputs(gen, rows, cols, t, rt, wt, b, pw, pb, gate)]
+    d_r, dy = _randn(gen, rows, cols, dtype=rt), _randn(gen, rows, cols, dtype=t)
+    eps, scale = 1e-3, 0.75
+    out = skrull_residual_norm(*given, scale, eps, kind)
+    assert out[0].dtype == rt and out[1].dtype == t
+    wanted = {n: v for n, v in zip(NAMES, given) if v is not None}
+    grads = torch.autograd.grad(out, list(wanted.values()), (d_r, dy))
+    got = {"r": out[0].detach(), "y": out[1].detach(), **{"d" + n: g for n, g in zip(wanted, grads)}}
+    want = _residual_in_64_bits(*given, scale, d_r, dy, eps, kind == "layer")
+    for name, value in got.items():
+        _within(value, *want[name], name)
+
+
+@pytest.mark.parametrize("which", [0, 1])
+@pytest.mark.parametrize("cols", [77, 896, 8192])
+def test_residual_norm_with_one_gradient(which, cols):
+    """Only the stream's gradient, or only the normed rows': the other one's is as if it were zero, the same bits."""
+    from paper_2505_19609_amd.autograd import skrull_residual_norm
+    gen = _gen(cols)
+    given = [v.requires_grad_() for v in _residual_inputs(gen, 37, cols, torch.bfloat16, torch.float32, torch.bfloat16, 1, 1, 1, 1)]
+    d = [_randn(gen, 37, cols, dtype=torch.float32), _randn(gen, 37, cols)]
+    out = skrull_residual_norm(*given)
+    used = [n for i, n in enumerate(given) if not (which == 0 and i in (2, 3))]
+    got = torch.autograd.grad(out[which], used, d[which], retain_graph=True)
+    want = torch.autograd.grad(out, used, [v if i == which else torch.zeros_like(v) for i, v in enumerate(d)])
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("cols,pad", [(896, 8), (896, 3), (4096, 24), (1001, 7), (5, 2)])
+def test_residual_strides_and_in_place(cols, pad):
+    """Rows inside wider ones, aligned and not: what contiguous rows give, to the same bits, and nothing beside them is touched; the new stream in the
+    place of the old one and y in the place of z are the same bits too, and stats may be left out."""
+    from paper_2505_19609_amd import binding as B
+    gen, rows = _gen(cols + pad), 41
+    r, z, *vectors = _residual_inputs(gen, rows, cols, torch.bfloat16, torch.bfloat16, torch.bfloat16, 1, 1, 1, 1)
+    d_r, dy = _randn(gen, rows, cols), _randn(gen, rows, cols)
+
+    def both(r, z, d_r, dy, r_out, y, dr, dz):
+        stats = torch.empty(4, rows, device="cuda")
+        grads = [torch.full_like(v, float("nan")) for v in vectors]
+        B.skrull_residual_fwd(r, z, *vectors, r_out, y, stats, 1.25, 1e-5, B.NORM_LAYER)
+        ws = torch.full((B.skrull_residual_workspace(r, z, vectors[0], B.NORM_LAYER),), 0xFF, dtype=torch.uint8, device="cuda")
+        w, _, pw, pb, gate = vectors
+        B.skrull_residual_bwd(r, z, w, pw, pb, gate, stats, d_r, dy, dr, dz, *grads, ws, 1.25, B.NORM_LAYER)
+        return [r_out, y, dr, dz, *grads]
+
+    fresh = [torch.empty_like(r) for _ in range(4)]
+    want = both(r, z, d_r, dy, *fresh)
+    wides, views = zip(*(_padded(t, pad, 5.0) for t in (r, z, d_r, dy, r, r, r, r)))
+    got = both(*views)
+    assert all(torch.equal(a, c) for a, c in zip(got, want))
+    assert all((t[:, cols:] == 5).all() for t in wides)
+    r2, z2 = r.clone(), z.clone()
+    B.skrull_residual_fwd(r2, z2, *vectors, r2, z2, None, 1.25, 1e-5, B.NORM_LAYER)
+    assert torch.equal(r2, want[0]) and torch.equal(z2, want[1])
+
+
+def test_residual_without_rows_and_with_a_row_of_infinities():
+    from paper_2505_19609_amd.autograd import skrull_residual_norm
+    vectors = [torch.ones(96, device="cuda", requires_grad=True) for _ in range(5)]
+    r, z = (torch.empty(0, 96, device="cuda", requires_grad=True) for _ in range(2))
+    out = skrull_residual_norm(r, z, *vectors)
+    grads = torch.autograd.grad(out, (r, z, *vectors), [torch.empty(0, 96, device="cuda")] * 2)
+    assert all(t.shape == (0, 96) for t in (*out, *grads[:2])) and all((g == 0).all() for g in grads[2:])
+    r, z = torch.ones(5, 96, device="cuda"), torch.ones(5, 96, device="cuda")
+    r[2, 3] = math.inf
+    r[3], z[3] = -1.0, 0.5
+    stream, y = skrull_residual_norm(r, z, vectors[0], eps=0.25, kind="rms")
+    assert stream[2, 3] == math.inf and torch.isnan(y[2, 3]) and torch.isfinite(y[[0, 1, 3, 4]]).all()   # (a row's own trouble stays its own)
+    assert torch.equal(y[0], y[4]) and (stream[3] == -0.5).all()
+
+
+def test_residual_backward_for_some_of_its_inputs():
+    from paper_2505_19609_amd.autograd import skrull_residual_norm
+    gen = _gen(78)
+    given = _residual_inputs(gen, 40, 640, torch.bfloat16, torch.bfloat16, torch.float32, 1, 1, 1, 1)
+    d = _randn(gen, 40, 640), _randn(gen, 40, 640)
+    want = None
+    for need in ((1,) * 7, (1, 1, 0, 0, 0, 0, 0), (0, 0, 1, 0, 0, 0, 0), (0, 0, 0, 1, 0, 0, 1), (0, 1, 0, 0, 1, 0, 0), (0, 0, 0, 0, 0, 1, 0)):
+        leaves = [t.clone().requires_grad_(bool(n)) for t, n in zip(given, need)]
+        grads = torch.autograd.grad(skrull_residual_norm(*leaves), [t for t in leaves if t.requires_grad], d)
+        want = want or grads
+        assert all(torch.equal(g, want[i]) for g, i in zip(grads, [i for i in range(7) if need[i]]))
+
+
+def test_residual_gradient_against_differences():
+    """The change of both results along the gradient is what the gradient says (differences of the 64-bit form)."""
+    from paper_2505_19609_amd.autograd import skrull_residual_norm
+    gen = _gen(5)
+    given = [t.requires_grad_() for t in _residual_inputs(gen, 9, 96, *[torch.float32] * 3, 1, 1, 1, 1)]
+    d = [_randn(gen, 9, 96, dtype=torch.float32) for _ in range(2)]
+    grads = torch.autograd.grad(skrull_residual_norm(*given, 0.75, 1e-3), given, d)
+
+    def value(step):
+        out = _residual_in_64_bits(*[t.detach().double() + step * g.double() for t, g in zip(given, grads)], 0.75, None, None, 1e-3, True)
+        return sum((out[n][0] * v.double()).sum().item() for n, v in zip("ry", d))
+    step = 1e-6
+    slope = (value(step) - value(-step)) / (2 * step)
+    square = sum(g.double().square().sum().item() for g in grads)
+    # (the gradients' own errors, some 2^-20 of them, and the differences' third derivatives and roundings)
+    assert abs(slope - square) <= 1e-4 * square
