@@ -211,6 +211,38 @@ def skrull_norm(x, weight, bias=None, eps=1e-5, kind="layer"):
     return y
 
 
+class _SkrullWindowAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, plan, window, sinks):
+        o = torch.empty_like(q)
+        lse = torch.empty((plan.num_q_heads, plan.total_q), dtype=torch.float32, device=q.device)
+        B.skrull_window_fwd(plan, q, k, v, o, lse, window, sinks)
+        ctx.plan, ctx.window, ctx.sinks = plan, window, sinks
+        ctx.save_for_backward(q, k, v, o, lse)
+        return o
+
+    @staticmethod
+    @_once(lambda ctx: True)
+    def backward(ctx, d_o):
+        q, k, v, o, lse = ctx.saved_tensors
+        dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+        ws = _workspace(B.skrull_window_workspace(ctx.plan, ctx.window, ctx.sinks), q.device)
+        B.skrull_window_bwd(ctx.plan, q, k, v, o, lse, _aligned(d_o), dq, dk, dv, ws, ctx.window, ctx.sinks)
+        return dq, dk, dv, None, None, None
+
+
+def _aligned(t):
+    """`t` contiguous, at a multiple of 16 bytes."""
+    return t if t.is_contiguous() and t.data_ptr() % 16 == 0 else t.clone(memory_format=torch.contiguous_format)
+
+
+def skrull_window_attention(q, k, v, plan, window, sinks=0):
+    """O = packed varlen causal attention of the micro-batch `plan` describes (a binding.Plan), where a query sees the last `window` keys up to its own and
+    the first `sinks` ones of its sequence; differentiable with respect to q, k, v."""
+    _refuse_captured(q, k, v)
+    return _SkrullWindowAttention.apply(_aligned(q), _aligned(k), _aligned(v), plan, window, sinks)
+
+
 class _SkrullResidualNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, r, z, weight, bias, post_weight, post_bias, gate, scale, eps, kind):

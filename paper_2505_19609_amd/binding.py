@@ -31,8 +31,9 @@ EXPORTED_SYMBOLS = ("skrull_attn_plan", "skrull_attn_plan_info", "skrull_attn_pl
 # the operators around attention (skrull_rotary.h, skrull_norm.h, skrull_loss.h)
 OPERATOR_SYMBOLS = ("skrull_rotary_check", "skrull_rotary", "skrull_norm_fwd", "skrull_norm_workspace", "skrull_norm_bwd",
                     "skrull_loss_workspace", "skrull_loss_fwd", "skrull_loss_bwd")
-# what else a block is made of (skrull_residual.h)
-BLOCK_SYMBOLS = ("skrull_residual_fwd", "skrull_residual_workspace", "skrull_residual_bwd")
+# what else a block is made of (skrull_window.h, skrull_residual.h)
+BLOCK_SYMBOLS = ("skrull_window_fwd", "skrull_window_workspace", "skrull_window_bwd",
+                 "skrull_residual_fwd", "skrull_residual_workspace", "skrull_residual_bwd")
 
 
 class Problem(ctypes.Structure):
@@ -96,6 +97,10 @@ class Norm(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int32), ("kind", ctypes.c_int32), ("type", ctypes.c_int32),
                 ("weight_type", ctypes.c_int32), ("eps", ctypes.c_float), ("x_stride", ctypes.c_int64),
                 ("y_stride", ctypes.c_int64), ("dy_stride", ctypes.c_int64), ("dx_stride", ctypes.c_int64)]
+
+
+class Window(ctypes.Structure):
+    _fields_ = [("window", ctypes.c_int32), ("sinks", ctypes.c_int32)]
 
 
 class Residual(ctypes.Structure):
@@ -180,7 +185,10 @@ def lib():
         L.skrull_norm_fwd.argtypes = [norm] + [vp] * 7
         L.skrull_norm_workspace.argtypes = [norm]
         L.skrull_norm_bwd.argtypes = [norm] + [vp] * 9 + [ctypes.c_size_t, vp]
-        residual = ctypes.POINTER(Residual)
+        window, residual = ctypes.POINTER(Window), ctypes.POINTER(Residual)
+        L.skrull_window_fwd.argtypes = [vp, window] + [vp] * 6
+        L.skrull_window_workspace.argtypes = [vp, window]
+        L.skrull_window_bwd.argtypes = [vp, window] + [vp] * 10 + [ctypes.c_size_t, vp]
         L.skrull_residual_fwd.argtypes = [residual] + [vp] * 11
         L.skrull_residual_workspace.argtypes = [residual]
         L.skrull_residual_bwd.argtypes = [residual] + [vp] * 17 + [ctypes.c_size_t, vp]
@@ -551,6 +559,51 @@ def skrull_norm_bwd(x, weight, mean, rstd, dy, dx, dweight, dbias, workspace, ki
     _check(lib().skrull_norm_bwd(ctypes.byref(p), _ptr(x), _vector(weight, cols, wt, "weight"), _vector(mean, rows, torch.float32, "mean"),
                                  _vector(rstd, rows, torch.float32, "rstd"), _ptr(dy), _ptr(dx), _vector(dweight, cols, wt, "dweight"),
                                  _vector(dbias, cols, wt, "dbias"), *_scratch(workspace), _stream_ptr(stream)))
+
+
+def _window_of(window, sinks):
+    return ctypes.byref(Window(_int32(window, "window"), _int32(sinks, "sinks")))
+
+
+def _heads(plan, q=(), k=()):
+    """Refuses tensors of q's or of k's kind that are not what `plan` says."""
+    import torch
+    i = plan.info
+    for tensors, shape in ((q, (i.total_q, i.num_q_heads, i.head_dim)), (k, (i.total_k, i.num_kv_heads, i.head_dim))):
+        for t in tensors:
+            if t.dtype is not torch.bfloat16 or t.shape != shape or not t.is_contiguous():
+                _refuse(f"a tensor of contiguous bf16 {list(shape)} is needed, got {t.dtype} {list(t.shape)}")
+
+
+def _lse(plan, lse):
+    import torch
+    shape = (plan.info.num_q_heads, plan.info.total_q)
+    if lse.dtype is not torch.float32 or lse.shape != shape or not lse.is_contiguous():
+        _refuse(f"lse must be contiguous torch.float32 {list(shape)}, got {lse.dtype} {list(lse.shape)}")
+    return _ptr(lse)
+
+
+def skrull_window_fwd(plan: Plan, q, k, v, o, lse, window, sinks=0, stream=None):
+    """o, lse of attention to the last `window` keys and the first `sinks` ones of a sequence."""
+    _on_current_device(q, k, v, o, lse)
+    _heads(plan, (q, o), (k, v))
+    _check(lib().skrull_window_fwd(plan.handle, _window_of(window, sinks), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _lse(plan, lse), _stream_ptr(stream)))
+
+
+def skrull_window_workspace(plan: Plan, window, sinks=0) -> int:
+    """Bytes that skrull_window_bwd asks for."""
+    n = int(lib().skrull_window_workspace(plan.handle, _window_of(window, sinks)))
+    if n == 0:
+        _check(SKRULL_EINVAL)
+    return n
+
+
+def skrull_window_bwd(plan: Plan, q, k, v, o, lse, d_o, dq, dk, dv, workspace, window, sinks=0, stream=None):
+    """dq, dk and dv, every row of them."""
+    _on_current_device(q, k, v, o, lse, d_o, dq, dk, dv, workspace)
+    _heads(plan, (q, o, d_o, dq), (k, v, dk, dv))
+    _check(lib().skrull_window_bwd(plan.handle, _window_of(window, sinks), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _lse(plan, lse), _ptr(d_o), _ptr(dq),
+                                   _ptr(dk), _ptr(dv), *_scratch(workspace), _stream_ptr(stream)))
 
 
 def _residual_of(r, z, weight, scale, eps, kind, **rows) -> Residual:

@@ -74,6 +74,7 @@ struct BwdParams {
     // stored, of each (item, KV head) or, for very many of these, of all of them; pieces of the sums of these that have been handed out
     int32_t *rows_ready, *parts_stored, *next_sum;
     int32_t n_parts;                  // work items that are parts of shared dK/dV items; 0: they are counted for each item
+    int32_t window, sinks;            // of the windowed kernels
 };
 
 // ---------------------------------------------------------------------------
@@ -163,8 +164,8 @@ __device__ __forceinline__ void count_one(int32_t *counter)
 
 // Does work item `bid`, whose rows are `rb`; returns the next one and leaves its rows in `rb`.
 // ONE: dK/dV follows in the same launch, so -D and LSE are stored when they are known, and the item is counted
-// as ready once they are in memory.
-template <int D, int NWQ, bool PIPED, bool ONE>
+// as ready once they are in memory.  WINDOW: a row sees the `window` last keys and the `sinks` first ones.
+template <int D, int NWQ, bool PIPED, bool ONE, bool WINDOW>
 __device__ __forceinline__ int dq_work(const int bid, RowBlocks &rb, DqFeed &feed, unsigned char *lds)
 {
     const kernarg_t<BwdParams> prm = kernarg<BwdParams>();
@@ -197,7 +198,9 @@ __device__ __forceinline__ int dq_work(const int bid, RowBlocks &rb, DqFeed &fee
     const uint64_t trace_t0 = trace_begin(prm->trace_dq);
     const int p0 = rb.p0;  // global position of the item's first query
     const int rows = rb.rows, qrow0 = rb.qrow0;
-    const int n_tiles = (p0 + min(rb.block(0) * 32 + 32, rows) + KT - 1) / KT;  // for the workgroup's last row block
+    KeyWalk<WINDOW> walk;
+    walk.init(WINDOW ? p0 + rb.lowest(NWQ) * 32 : 0, prm->window, prm->sinks);
+    const int n_tiles = walk.tile((p0 + min(rb.block(0) * 32 + 32, rows) + KT - 1) / KT);  // for the workgroup's last row block
     const float cs = prm->scale_log2;
 
     const bool wave_active = rb.has(wave);
@@ -206,9 +209,10 @@ __device__ __forceinline__ int dq_work(const int bid, RowBlocks &rb, DqFeed &fee
     const int my_i = wrow0 + n;
     const int w_pmin = p0 + wrow0;
     const int w_pmax = p0 + min(wrow0 + 31, rows - 1);
-    // half tiles (32 keys) of this wave: 0..L hold a visible key, those below n_full only visible keys
-    const int L = wave_active ? w_pmax / 32 : -1;
-    const int n_full = wave_active ? (w_pmin + 1) / 32 : 0;
+    walk.wave(w_pmin, w_pmax);
+    // half tiles (32 keys) of this wave: 0..L hold a visible key (of those that `walk` has), those below n_full only visible keys
+    const int L = wave_active ? walk.half(w_pmax / 32) : -1;
+    const int n_full = wave_active ? walk.half((w_pmin + 1) / 32) : 0;
 
     const i32x4 rk = ld.rsrc(prm->k + ((size_t)kbase * prm->Hkv + c) * D, kvl);
     const i32x4 rv = ld.rsrc(prm->v + ((size_t)kbase * prm->Hkv + c) * D, kvl);
@@ -219,29 +223,29 @@ __device__ __forceinline__ int dq_work(const int bid, RowBlocks &rb, DqFeed &fee
     int kslot = 0;  // slot of K tile t (t mod KSL), advanced at the end of every period
     auto fetch = [&](int t) __attribute__((always_inline)) {
         if (SMALL) {
-            ld.load(rk, ring_k + (uint32_t)(PIPED ? (kslot == 2 ? 0 : kslot + 1) : (t + 1) & 1) * TB, (t + 1) * KT, wave);
-            ld.load(rv, ring_v + (uint32_t)((t + 1) & 1) * TB, (t + 1) * KT, wave);
+            ld.load(rk, ring_k + (uint32_t)(PIPED ? (kslot == 2 ? 0 : kslot + 1) : (t + 1) & 1) * TB, walk.key(t + 1), wave);
+            ld.load(rv, ring_v + (uint32_t)((t + 1) & 1) * TB, walk.key(t + 1), wave);
         } else if (WIDE) {
 #pragma unroll
             for (int x = 2; x < 4; ++x) {
-                ld.load(rk, ring_k + (uint32_t)((t + x) & 3) * TB, (t + x) * KT, wave);
-                ld.load(rv, ring_v + (uint32_t)((t + x) & 3) * TB, (t + x) * KT, wave);
+                ld.load(rk, ring_k + (uint32_t)((t + x) & 3) * TB, walk.key(t + x), wave);
+                ld.load(rv, ring_v + (uint32_t)((t + x) & 3) * TB, walk.key(t + x), wave);
             }
         } else {
             const int k2 = kslot >= 3 ? kslot - 3 : kslot + 2, k3 = kslot >= 2 ? kslot - 2 : kslot + 3;
-            ld.load(rk, ring_k + (uint32_t)k2 * TB, (t + 2) * KT, wave);
-            ld.load(rv, ring_v + (uint32_t)((t + 2) & 3) * TB, (t + 2) * KT, wave);
-            ld.load(rk, ring_k + (uint32_t)k3 * TB, (t + 3) * KT, wave);
-            ld.load(rv, ring_v + (uint32_t)((t + 3) & 3) * TB, (t + 3) * KT, wave);
+            ld.load(rk, ring_k + (uint32_t)k2 * TB, walk.key(t + 2), wave);
+            ld.load(rv, ring_v + (uint32_t)((t + 2) & 3) * TB, walk.key(t + 2), wave);
+            ld.load(rk, ring_k + (uint32_t)k3 * TB, walk.key(t + 3), wave);
+            ld.load(rv, ring_v + (uint32_t)((t + 3) & 3) * TB, walk.key(t + 3), wave);
         }
     };
     // start-up: the tiles of the first period(s).  The fetch group of period 0 follows after the
     // barrier below, because until then its slots stage this item's rows of Q, dO and O.
-    ld.load(rk, ring_k, 0, wave);
-    ld.load(rv, ring_v, 0, wave);
+    ld.load(rk, ring_k, walk.key(0), wave);
+    ld.load(rv, ring_v, walk.key(0), wave);
     if (!SMALL) {
-        ld.load(rk, ring_k + TB, KT, wave);
-        ld.load(rv, ring_v + TB, KT, wave);
+        ld.load(rk, ring_k + TB, walk.key(1), wave);
+        ld.load(rv, ring_v + TB, walk.key(1), wave);
     }
     // this wave's staging region: half a ring slot that holds no tile yet (large shape: K slots
     // 2-4 for waves 0-5 and V slots 2-3 for waves 6-7; wide shape: K slots 2-3, V slots 2-3 and a
@@ -393,7 +397,7 @@ __device__ __forceinline__ int dq_work(const int bid, RowBlocks &rb, DqFeed &fee
     auto generic = [&](int j, const unsigned char *kp, const unsigned char *vp, const unsigned char *kt,
                        const f32x16 &s_in, const f32x16 &g_in, f32x16 &s_out, f32x16 &g_out)
                        __attribute__((always_inline)) {
-        if (j + 1 <= L) {  // A(j+1)
+        if (j + 1 <= L && walk.live(j + 1)) {  // A(j+1)
 #pragma unroll
             for (int v = 0; v < 16; ++v) { s_out[v] = 0.0f; g_out[v] = nd; }
 #pragma unroll
@@ -403,18 +407,19 @@ __device__ __forceinline__ int dq_work(const int bid, RowBlocks &rb, DqFeed &fee
                 if (ks % 4 == 3) SB();
             }
         }
-        if (j >= 0 && j <= L) {  // V(j), B(j)
+        if (j >= 0 && j <= L && walk.live(j)) {  // V(j), B(j)
             f32x16 ds;
 #pragma unroll
             for (int v = 0; v < 16; ++v) ds[v] = fast_exp2(__builtin_fmaf(s_in[v], cs, -lse2)) * g_in[v];
-            if (j >= n_full) {  // half tile touches the diagonal for this wave
+            if (j >= n_full || !walk.full(j)) {  // half tile touches the diagonal, or the window's start, for this wave
                 // relative position from an opaque copy of the lane index: the sixteen
                 // per-register thresholds are formed here rather than kept for the whole kernel
                 int li = lane;
                 asm volatile("" : "+v"(li));
-                const int rel = p0 + wrow0 + (li & 31) - 32 * j - 4 * (li >> 5);  // my_pos - 32j - 4h
+                const int rel = p0 + wrow0 + (li & 31) - walk.half_key(j) - 4 * (li >> 5);  // my_pos - first key - 4h
+                const int sinks_rel = WINDOW ? walk.sinks - walk.half_key(j) - 4 * (li >> 5) : 0;
 #pragma unroll
-                for (int v = 0; v < 16; ++v) ds[v] = (8 * (v >> 2) + (v & 3) > rel) ? 0.0f : ds[v];
+                for (int v = 0; v < 16; ++v) ds[v] = walk.hidden(8 * (v >> 2) + (v & 3), rel, sinks_rel) ? 0.0f : ds[v];
             }
             SB();
 #pragma unroll
@@ -456,15 +461,16 @@ __device__ __forceinline__ int dq_work(const int bid, RowBlocks &rb, DqFeed &fee
             // such a reader of its result (12 for these on gfx950; s_nop n is n + 1 of them): they are here.  (Without
             // them the first scores were read before they were written where a wavefront had its SIMD to itself.)
             asm volatile("s_nop 11" : "+v"(s), "+v"(g));
-            if (__builtin_expect(j >= n_full, 0)) {  // half tile touches the diagonal for this wave
+            if (__builtin_expect(j >= n_full || !walk.full(j), 0)) {  // half tile touches the diagonal, or the window's start, for this wave
                 int li = lane;
                 asm volatile("" : "+v"(li));
-                const int rel = p0 + wrow0 + (li & 31) - 32 * j - 4 * (li >> 5);  // my_pos - 32j - 4h
+                const int rel = p0 + wrow0 + (li & 31) - walk.half_key(j) - 4 * (li >> 5);  // my_pos - first key - 4h
+                const int sinks_rel = WINDOW ? walk.sinks - walk.half_key(j) - 4 * (li >> 5) : 0;
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
-                    const bool late = 8 * (v >> 2) + (v & 3) > rel;
-                    s[v] = late ? -INFINITY : s[v];
-                    g[v] = late ? 0.0f : g[v];
+                    const bool hidden = walk.hidden(8 * (v >> 2) + (v & 3), rel, sinks_rel);
+                    s[v] = hidden ? -INFINITY : s[v];
+                    g[v] = hidden ? 0.0f : g[v];
                 }
             }
             uint32_t pw[8];
@@ -487,8 +493,8 @@ __device__ __forceinline__ int dq_work(const int bid, RowBlocks &rb, DqFeed &fee
             if (t > 0 && (SMALL ? t + 1 < n_tiles : (t & 1) == 0 && t + 2 < n_tiles)) fetch(t);
             if (t == n_tiles - 1) feed.ask();
             const unsigned char *tk = lds_k[t & (KSL - 1)], *tv = lds_v[t & (VSL - 1)];
-            if (2 * t <= L) half(2 * t, tk, tv);
-            if (2 * t + 1 <= L) half(2 * t + 1, tk + HALF, tv + HALF);
+            if (2 * t <= L && walk.live(2 * t)) half(2 * t, tk, tv);
+            if (2 * t + 1 <= L && walk.live(2 * t + 1)) half(2 * t + 1, tk + HALF, tv + HALF);
             if (SMALL || (t & 1)) {
                 wait_vmem();
                 __syncthreads();
@@ -543,8 +549,14 @@ __device__ __forceinline__ int dq_work(const int bid, RowBlocks &rb, DqFeed &fee
         }
         period_end(t);
     };
-    plain_period(0);
     int t = 1;
+    if (WINDOW) {
+        const int t_steady = min(walk.first_full_period(), n_tiles + 1);
+#pragma unroll 1
+        for (t = 0; t < t_steady; ++t) plain_period(t);
+    } else {
+        plain_period(0);
+    }
     for (; t <= t_steady_end; ++t) {
         period_begin(t);
         const unsigned char *tk = lds_k[kslot], *tv = lds_v[t & (VSL - 1)];
@@ -588,7 +600,7 @@ __device__ __forceinline__ int dq_work(const int bid, RowBlocks &rb, DqFeed &fee
 }
 
 // Does dQ work items until none is left.
-template <int D, int NWQ, bool PIPED, bool ONE>
+template <int D, int NWQ, bool PIPED, bool ONE, bool WINDOW = false>
 __device__ __forceinline__ void dq_loop(DqFeed &feed, unsigned char *lds)
 {
     constexpr int NW = ONE ? 0 : NWQ;
@@ -596,7 +608,7 @@ __device__ __forceinline__ void dq_loop(DqFeed &feed, unsigned char *lds)
     RowBlocks rb = row_blocks<NW>(kernarg<BwdParams>(), kernarg<BwdParams>()->fwd_items, max(w, 0));
     while (w >= 0) {
         if (rb.has(0)) {
-            w = dq_work<D, NWQ, PIPED, ONE>(w, rb, feed, lds);
+            w = dq_work<D, NWQ, PIPED, ONE, WINDOW>(w, rb, feed, lds);
             if (w == kQueueEmpty) {
                 w = feed.other();
                 rb = row_blocks<NW>(kernarg<BwdParams>(), kernarg<BwdParams>()->fwd_items, max(w, 0));
@@ -609,14 +621,14 @@ __device__ __forceinline__ void dq_loop(DqFeed &feed, unsigned char *lds)
     }
 }
 
-template <int D, int NWQ, bool PIPED = NWQ == NWQ_LARGE>
+template <int D, int NWQ, bool PIPED = NWQ == NWQ_LARGE, bool WINDOW = false>
 __global__ __launch_bounds__(64 * NWQ, PIPED ? 2 : 3) void dq_kernel(const BwdParams prm)
 {
     __shared__ __align__(16) unsigned char lds[DqLds<D, NWQ, PIPED>::BYTES];
     __shared__ int work_slot[2];
     if (prm.clear && blockIdx.x == 0) clear_state(prm.clear, SKRULL_BWD_STATE_INTS);
     DqFeed feed{{}, 0, 0, work_slot};
-    dq_loop<D, NWQ, PIPED, false>(feed, lds);
+    dq_loop<D, NWQ, PIPED, false, WINDOW>(feed, lds);
 }
 
 // ---------------------------------------------------------------------------
@@ -784,8 +796,9 @@ struct DkvLds {
 
 // Does work item `bid`, whose keys are `kb`; returns the next one and leaves its keys in `kb`.
 // ONE: in one launch with dQ.  `rows_seen`: this workgroup has waited for the rows of dQ's items.  `part_owed`: the part of a shared item
-// (KeyBlock::shared) that it did last, stored but not counted yet, or 0; on return this item's.
-template <int D, int PAIRS, bool ONE>
+// (KeyBlock::shared) that it did last, stored but not counted yet, or 0; on return this item's.  WINDOW: a row sees the `window` last keys and the
+// `sinks` first ones.
+template <int D, int PAIRS, bool ONE, bool WINDOW>
 __device__ __forceinline__ int dkv_work(const int bid, KeyBlock &kb, DkvFeed &feed, unsigned char *ring, unsigned char *exchange, bool &rows_seen, int &part_owed)
 {
     const kernarg_t<BwdParams> prm = kernarg<BwdParams>();
@@ -840,11 +853,15 @@ __device__ __forceinline__ int dkv_work(const int bid, KeyBlock &kb, DkvFeed &fe
     // Query tiles that can see key kv0, numbered 0 .. n_qt-1 in position order: those of
     // the early chunk (segment seq-1, when this prefix is shared by two chunks and the
     // pass starts inside the early chunk's own prefix) and then those of segment seq.
+    // With a window only those that see one of its keys, of which there may be none; a key below `sinks` all later ones see.
+    const int window = WINDOW ? prm->window : 0, sinks = WINDOW ? prm->sinks : 0;
+    const int q_last = WINDOW && kv0 >= sinks ? kv0 + krows - 1 + window - 1 : 1 << 30;  // last position that sees a key of the pass
     const int i_first = (max(0, kv0 - qb) / QT) * QT;
-    const int n_qt_own = (ql - i_first + QT - 1) / QT;
+    const int n_qt_own = WINDOW ? max(0, min(ql, q_last - qb + 1) - i_first + QT - 1) / QT : (ql - i_first + QT - 1) / QT;
     const int qb_e = kb.qb_e, ql_e = kb.ql_e, qbase_e = kb.qbase_e;
     const int i_first_e = (max(0, kv0 - qb_e) / QT) * QT;
-    const int n_qt_e = ql_e > 0 ? (ql_e - i_first_e + QT - 1) / QT : 0;
+    const int n_qt_e = WINDOW   ? max(0, min(ql_e, q_last - qb_e + 1) - i_first_e + QT - 1) / QT
+                       : ql_e > 0 ? (ql_e - i_first_e + QT - 1) / QT : 0;
     const int n_qt = n_qt_e + n_qt_own;
     // (head, query tile) pairs of the walk described below: this part takes n_iter of them from r0 on
     const bool all = kb.pieces == 1;
@@ -894,7 +911,7 @@ __device__ __forceinline__ int dkv_work(const int bid, KeyBlock &kb, DkvFeed &fe
         __syncthreads();  // (-D and LSE are read past the L2: with a fence by each workgroup, which empties it, dK/dV began 30 us later)
         rows_seen = true;
     }
-    fetch(head0, tile0, 0);
+    if (!WINDOW || n_iter > 0) fetch(head0, tile0, 0);
     wait_vmem();
     __syncthreads();
     if (ONE && part_owed && tid == 0) count_part(part_owed);  // (everyone's stores of the item before are done)
@@ -914,7 +931,8 @@ __device__ __forceinline__ int dkv_work(const int bid, KeyBlock &kb, DkvFeed &fe
     auto tile_live = [&](int t) __attribute__((always_inline)) {
         return tile_qb(t) + tile_i0(t) + QT - 1 >= wj0;
     };
-    int n_live = 0;  // live rounds of this pair
+    // With a window the highest tiles may be dead too, those that none of the pair's keys reaches, unless it has sinks.
+    int n_live = 0, first_live = 0;  // live rounds of this pair: from first_live on, below n_live
     if (wave_active) {
         int dead_tiles = 0;
         if (n_qt_e > 0) {  // the early chunk's lowest tile may be dead; the late chunk's never is
@@ -923,6 +941,13 @@ __device__ __forceinline__ int dkv_work(const int bid, KeyBlock &kb, DkvFeed &fe
             while (dead_tiles < n_qt && !tile_live(dead_tiles)) ++dead_tiles;
         }
         n_live = max(0, min(n_iter, (n_qt - dead_tiles) * g - r0));
+        if (WINDOW && wj0 >= sinks) {
+            const int last = wj0 + 31 + window - 1;  // last position that sees a key of the pair
+            auto below = [&](int qb_s, int i_s, int count) { return max(0, min(count, (last - qb_s - i_s + QT) / QT)); };  // of `count` tiles from i_s on, those that begin at or before it
+            const int own = last < qb + i_first ? 0 : below(qb, i_first, n_qt_own), early = last < qb_e + i_first_e ? 0 : below(qb_e, i_first_e, n_qt_e);
+            first_live = max(0, (n_qt - (own > 0 ? n_qt_e + own : early)) * g - r0);
+            if (first_live >= n_live) first_live = n_live = 0;
+        }
     }
     int nh = head0 + 1, nq = tile0, cq = tile0, slot = 0;  // cq: tile of this round; (nh, nq): head, tile of the next
     if (nh == g) { nh = 0; --nq; }
@@ -938,6 +963,13 @@ __device__ __forceinline__ int dkv_work(const int bid, KeyBlock &kb, DkvFeed &fe
         if (++nh == g) { nh = 0; --nq; }
     };
     int T = 0;
+    if (WINDOW) {
+#pragma unroll 1
+        for (; T < first_live; ++T) {
+            round_begin(T);
+            round_end();
+        }
+    }
     if (role == 0) {
 #pragma unroll 1
         for (; T < n_live; ++T) {
@@ -948,8 +980,8 @@ __device__ __forceinline__ int dkv_work(const int bid, KeyBlock &kb, DkvFeed &fe
             const unsigned char *tq = cur, *tdo = cur + TB;
             const float *t_lse = (const float *)(cur + 2 * TB);
             unsigned char *px = lds_p[pw][T & 1][0];
-            // masked pairs: key past the query (causal) or query row past the end
-            const bool need_mask = (qb_t + i0 < wj0 + 31) || (i0 + QT > ql_t);
+            // masked pairs: key past the query (causal), query row past the end, or key in front of the query's window and no sink
+            const bool need_mask = (qb_t + i0 < wj0 + 31) || (i0 + QT > ql_t) || (WINDOW && wj0 + 31 >= sinks && qb_t + i0 + QT - 1 >= wj0 + window);
             // scores of masked pairs become -inf (probability 0) before the exponentials
             auto mask_block = [&](f32x16 &sb, int b) __attribute__((always_inline)) {
                 // (the asm also keeps this block behind its branch: turned into selects it
@@ -960,7 +992,8 @@ __device__ __forceinline__ int dkv_work(const int bid, KeyBlock &kb, DkvFeed &fe
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
                     const int i = row0 + 8 * (v >> 2) + (v & 3);
-                    sb[v] = (wj0 + (li & 31) > qb_t + i || i >= ql_t) ? -INFINITY : sb[v];
+                    const int key = wj0 + (li & 31);
+                    sb[v] = (key > qb_t + i || i >= ql_t || (WINDOW && key >= sinks && key <= qb_t + i - window)) ? -INFINITY : sb[v];
                 }
             };
             f32x16 s[2];
@@ -1230,7 +1263,7 @@ __device__ __forceinline__ int dkv_work(const int bid, KeyBlock &kb, DkvFeed &fe
 }
 
 // Does dK/dV work items until none is left.
-template <int D, int PAIRS, bool ONE>
+template <int D, int PAIRS, bool ONE, bool WINDOW = false>
 __device__ __forceinline__ void dkv_loop(DkvFeed &feed, unsigned char *ring, unsigned char *exchange)
 {
     bool rows_seen = !ONE;
@@ -1239,7 +1272,7 @@ __device__ __forceinline__ void dkv_loop(DkvFeed &feed, unsigned char *ring, uns
     KeyBlock kb = key_block(kernarg<BwdParams>(), 32 * PAIRS, max(w, 0));
     while (w >= 0) {
         if (kb.item_rows > 0) {
-            w = dkv_work<D, PAIRS, ONE>(w, kb, feed, ring, exchange, rows_seen, part_owed);
+            w = dkv_work<D, PAIRS, ONE, WINDOW>(w, kb, feed, ring, exchange, rows_seen, part_owed);
             if (w == kQueueEmpty) {
                 if (ONE && part_owed) {  // (the search takes microseconds)
                     wait_vmem();
@@ -1263,14 +1296,14 @@ __device__ __forceinline__ void dkv_loop(DkvFeed &feed, unsigned char *ring, uns
     }
 }
 
-template <int D, int PAIRS>
+template <int D, int PAIRS, bool WINDOW = false>
 __global__ __launch_bounds__(128 * PAIRS, PAIRS == PAIRS_12W ? 3 : 2) void dkv_kernel(const BwdParams prm)
 {
     // (two arrays: in one, the compiler took a store to the exchange for one to the ring, and dK/dV of long chains 0.5 % longer)
     __shared__ __align__(16) unsigned char ring[DkvLds<D, PAIRS>::RING], exchange[DkvLds<D, PAIRS>::P];
     __shared__ int work_slot[2];
     DkvFeed feed{{}, 0, 0, work_slot};
-    dkv_loop<D, PAIRS, false>(feed, ring, exchange);
+    dkv_loop<D, PAIRS, false, WINDOW>(feed, ring, exchange);
 }
 
 // Sums of the partial gradients of the items that several workgroups shared, rounded once (the same as
@@ -1424,21 +1457,23 @@ __global__ __launch_bounds__(256) void dkv_reduce_kernel(const BwdParams prm)
 
 int dkv_pairs(const skrull_attn_plan_t *p) { return (p->d == 64 && p->BN == 32 * PAIRS_12W) ? PAIRS_12W : PAIRS_8W; }
 
+template <bool WINDOW = false>
 RowLaunch rows_dq_alone(const skrull_attn_plan_t *p)
 {
-    if (p->d == 128) return row_launch<dq_kernel<128, NWQ_LARGE>>(p, NWQ_LARGE);
-    if (p->dq_waves == NWQ_SMALL && p->dq_piped) return row_launch<dq_kernel<64, NWQ_SMALL, true>>(p, NWQ_SMALL);
-    if (p->dq_waves == NWQ_SMALL) return row_launch<dq_kernel<64, NWQ_SMALL>>(p, NWQ_SMALL);
-    if (p->dq_waves == NWQ_WIDE) return row_launch<dq_kernel<64, NWQ_WIDE>>(p, NWQ_WIDE);
-    return row_launch<dq_kernel<64, NWQ_LARGE>>(p, NWQ_LARGE);
+    if (p->d == 128) return row_launch<dq_kernel<128, NWQ_LARGE, true, WINDOW>>(p, NWQ_LARGE);
+    if (p->dq_waves == NWQ_SMALL && p->dq_piped) return row_launch<dq_kernel<64, NWQ_SMALL, true, WINDOW>>(p, NWQ_SMALL);
+    if (p->dq_waves == NWQ_SMALL) return row_launch<dq_kernel<64, NWQ_SMALL, false, WINDOW>>(p, NWQ_SMALL);
+    if (p->dq_waves == NWQ_WIDE) return row_launch<dq_kernel<64, NWQ_WIDE, false, WINDOW>>(p, NWQ_WIDE);
+    return row_launch<dq_kernel<64, NWQ_LARGE, true, WINDOW>>(p, NWQ_LARGE);
 }
 
 // Whether a launch of dK/dV has more work items than the chip holds at once.
+template <bool WINDOW = false>
 bool dkv_queued(const skrull_attn_plan_t *p)
 {
     const int n = grid_dkv(p);
-    if (p->d == 128) return wants_queue<dkv_kernel<128, PAIRS_8W>>(128 * PAIRS_8W, n);
-    return dkv_pairs(p) == PAIRS_12W ? wants_queue<dkv_kernel<64, PAIRS_12W>>(128 * PAIRS_12W, n) : wants_queue<dkv_kernel<64, PAIRS_8W>>(128 * PAIRS_8W, n);
+    if (p->d == 128) return wants_queue<dkv_kernel<128, PAIRS_8W, WINDOW>>(128 * PAIRS_8W, n);
+    return dkv_pairs(p) == PAIRS_12W ? wants_queue<dkv_kernel<64, PAIRS_12W, WINDOW>>(128 * PAIRS_12W, n) : wants_queue<dkv_kernel<64, PAIRS_8W, WINDOW>>(128 * PAIRS_8W, n);
 }
 
 // Whether a backward is one launch, of workgroups that take dQ items, then dK/dV items.
@@ -1521,26 +1556,33 @@ hipError_t launch_one(const skrull_attn_plan_t *p, const BwdParams &prm, hipStre
     bwd_kernel<D, PAIRS><<<(int)(work < resident ? work : resident), 128 * PAIRS, 0, st>>>(prm);
     return hipGetLastError();
 }
-template <int D>
-hipError_t launch_d(const skrull_attn_plan_t *p, const BwdParams &prm, bool one, hipStream_t st, hipEvent_t *ev)
+// dQ, dK/dV and sums as separate launches.
+template <int D, bool WINDOW>
+hipError_t launch_apart(const skrull_attn_plan_t *p, const BwdParams &prm, hipStream_t st, hipEvent_t *ev)
 {
-    if (one) {
-        if constexpr (D == 64)
-            if (dkv_pairs(p) == PAIRS_12W) return launch_one<D, PAIRS_12W>(p, prm, st);
-        return launch_one<D, PAIRS_8W>(p, prm, st);
-    }
     if constexpr (D == 64) {  // dQ has its other shapes, and dK/dV its 12-wavefront one, only here
+        constexpr auto wide = dkv_kernel<D, PAIRS_12W, WINDOW>, narrow = dkv_kernel<D, PAIRS_8W, WINDOW>;
+        constexpr auto piped = dq_kernel<D, NWQ_SMALL, true, WINDOW>, small = dq_kernel<D, NWQ_SMALL, false, WINDOW>, twelve = dq_kernel<D, NWQ_WIDE, false, WINDOW>;
         if (dkv_pairs(p) == PAIRS_12W) {
-            if (p->dq_waves == NWQ_SMALL && p->dq_piped) return launch_pair<D, dq_kernel<D, NWQ_SMALL, true>, dkv_kernel<D, PAIRS_12W>>(p, prm, 64 * NWQ_SMALL, 128 * PAIRS_12W, st, ev);
-            if (p->dq_waves == NWQ_SMALL) return launch_pair<D, dq_kernel<D, NWQ_SMALL>, dkv_kernel<D, PAIRS_12W>>(p, prm, 64 * NWQ_SMALL, 128 * PAIRS_12W, st, ev);
-            if (p->dq_waves == NWQ_WIDE) return launch_pair<D, dq_kernel<D, NWQ_WIDE>, dkv_kernel<D, PAIRS_12W>>(p, prm, 64 * NWQ_WIDE, 128 * PAIRS_12W, st, ev);
-            return launch_pair<D, dq_kernel<D, NWQ_LARGE>, dkv_kernel<D, PAIRS_12W>>(p, prm, 64 * NWQ_LARGE, 128 * PAIRS_12W, st, ev);
+            if (p->dq_waves == NWQ_SMALL && p->dq_piped) return launch_pair<D, piped, wide>(p, prm, 64 * NWQ_SMALL, 128 * PAIRS_12W, st, ev);
+            if (p->dq_waves == NWQ_SMALL) return launch_pair<D, small, wide>(p, prm, 64 * NWQ_SMALL, 128 * PAIRS_12W, st, ev);
+            if (p->dq_waves == NWQ_WIDE) return launch_pair<D, twelve, wide>(p, prm, 64 * NWQ_WIDE, 128 * PAIRS_12W, st, ev);
+            return launch_pair<D, dq_kernel<D, NWQ_LARGE, true, WINDOW>, wide>(p, prm, 64 * NWQ_LARGE, 128 * PAIRS_12W, st, ev);
         }
-        if (p->dq_waves == NWQ_SMALL && p->dq_piped) return launch_pair<D, dq_kernel<D, NWQ_SMALL, true>, dkv_kernel<D, PAIRS_8W>>(p, prm, 64 * NWQ_SMALL, 128 * PAIRS_8W, st, ev);
-        if (p->dq_waves == NWQ_SMALL) return launch_pair<D, dq_kernel<D, NWQ_SMALL>, dkv_kernel<D, PAIRS_8W>>(p, prm, 64 * NWQ_SMALL, 128 * PAIRS_8W, st, ev);
-        if (p->dq_waves == NWQ_WIDE) return launch_pair<D, dq_kernel<D, NWQ_WIDE>, dkv_kernel<D, PAIRS_8W>>(p, prm, 64 * NWQ_WIDE, 128 * PAIRS_8W, st, ev);
+        if (p->dq_waves == NWQ_SMALL && p->dq_piped) return launch_pair<D, piped, narrow>(p, prm, 64 * NWQ_SMALL, 128 * PAIRS_8W, st, ev);
+        if (p->dq_waves == NWQ_SMALL) return launch_pair<D, small, narrow>(p, prm, 64 * NWQ_SMALL, 128 * PAIRS_8W, st, ev);
+        if (p->dq_waves == NWQ_WIDE) return launch_pair<D, twelve, narrow>(p, prm, 64 * NWQ_WIDE, 128 * PAIRS_8W, st, ev);
     }
-    return launch_pair<D, dq_kernel<D, NWQ_LARGE>, dkv_kernel<D, PAIRS_8W>>(p, prm, 64 * NWQ_LARGE, 128 * PAIRS_8W, st, ev);
+    return launch_pair<D, dq_kernel<D, NWQ_LARGE, true, WINDOW>, dkv_kernel<D, PAIRS_8W, WINDOW>>(p, prm, 64 * NWQ_LARGE, 128 * PAIRS_8W, st, ev);
+}
+template <int D>
+hipError_t launch_d(const skrull_attn_plan_t *p, const BwdParams &prm, bool one, bool window, hipStream_t st, hipEvent_t *ev)
+{
+    if (window) return launch_apart<D, true>(p, prm, st, ev);
+    if (!one) return launch_apart<D, false>(p, prm, st, ev);
+    if constexpr (D == 64)
+        if (dkv_pairs(p) == PAIRS_12W) return launch_one<D, PAIRS_12W>(p, prm, st);
+    return launch_one<D, PAIRS_8W>(p, prm, st);
 }
 
 }  // namespace
@@ -1563,9 +1605,11 @@ int grid_dkv(const skrull_attn_plan_t *p)
 
 hipError_t launch_bwd(const skrull_attn_plan_t *p, const void *q, const void *k, const void *v,
                       const void *o, const float *lse, const void *d_o, void *dq, void *dk,
-                      void *dv, float *delta, hipStream_t st, hipEvent_t *ev, WgTrace *trace)
+                      void *dv, float *delta, hipStream_t st, hipEvent_t *ev, WgTrace *trace, const KeyWindow *window)
 {
     BwdParams prm;
+    prm.window = window ? window->keys : 0;
+    prm.sinks = window ? window->sinks : 0;
     prm.trace_dq = trace;
     DefaultStream &own = *p->default_stream;
     std::unique_lock<std::mutex> held(own.lock);
@@ -1573,9 +1617,9 @@ hipError_t launch_bwd(const skrull_attn_plan_t *p, const void *q, const void *k,
     // Events are to time dQ and dK/dV by themselves.  Calls without a set of the plan's have the 256 bytes in the workspace alone for what
     // workgroups share, two lines, and workgroups that wait would poll the line of dQ's queues: replayed from a graph, 838 tokens in 10
     // sequences, 32/8 heads of 128, 39 us as three launches, 74 in one; 17,205 in 62, 8/4 heads, 204 and 295.
-    const bool one = in_turn && !ev && is_one(p);
-    const RowLaunch rows_q = one ? rows_dq_first(p) : rows_dq_alone(p);
-    in_turn = in_turn && (one || rows_q.queued || dkv_queued(p));  // (two plain grids share nothing)
+    const bool one = in_turn && !ev && !window && is_one(p);
+    const RowLaunch rows_q = window ? rows_dq_alone<true>(p) : one ? rows_dq_first(p) : rows_dq_alone(p);
+    in_turn = in_turn && (one || rows_q.queued || (window ? dkv_queued<true>(p) : dkv_queued(p)));  // (two plain grids share nothing)
     if (!in_turn) held.unlock();
     prm.trace_dkv = trace ? trace + grid_dq(p) : nullptr;  // (one launch has as many dQ items or fewer)
     prm.q = (const uint16_t *)q; prm.k = (const uint16_t *)k; prm.v = (const uint16_t *)v;
@@ -1619,7 +1663,8 @@ hipError_t launch_bwd(const skrull_attn_plan_t *p, const void *q, const void *k,
         prm.queue_dkv = prm.queue_dq + 8 * kQueueStrideWorkspace;
         prm.rows_ready = prm.parts_stored = prm.next_sum = prm.clear = nullptr;
     }
-    const hipError_t e = p->d == 128 ? launch_d<128>(p, prm, one, st, ev) : p->d == 64 ? launch_d<64>(p, prm, one, st, ev) : hipErrorInvalidValue;
+    const bool windowed = window != nullptr;
+    const hipError_t e = p->d == 128 ? launch_d<128>(p, prm, one, windowed, st, ev) : p->d == 64 ? launch_d<64>(p, prm, one, windowed, st, ev) : hipErrorInvalidValue;
     if (in_turn) {
         if (e == hipSuccess) ++own.bwd;
         else own.lost = true;

@@ -208,11 +208,15 @@ int64_t plan_radix_ints(int32_t cap_fwd, int32_t cap_dkv, int32_t cost_bound);
 // fwd.hip / bwd.hip
 // `trace` (may be null): room for one WgTrace per workgroup of every kernel launched, in
 // launch order (launch_bwd: dQ's records, then dK/dV's); grid sizes from the functions below
+// `window`: null, or what a row sees: its last keys and the first ones of its sequence
+struct KeyWindow {
+    int32_t keys, sinks;
+};
 hipError_t launch_fwd(const skrull_attn_plan_t *p, const void *q, const void *k, const void *v,
-                      void *o, float *lse, hipStream_t st, WgTrace *trace);
+                      void *o, float *lse, hipStream_t st, WgTrace *trace, const KeyWindow *window = nullptr);
 hipError_t launch_bwd(const skrull_attn_plan_t *p, const void *q, const void *k, const void *v,
                       const void *o, const float *lse, const void *d_o, void *dq, void *dk,
-                      void *dv, float *delta, hipStream_t st, hipEvent_t *ev, WgTrace *trace);
+                      void *dv, float *delta, hipStream_t st, hipEvent_t *ev, WgTrace *trace, const KeyWindow *window = nullptr);
 int grid_fwd(const skrull_attn_plan_t *p);
 int grid_dq(const skrull_attn_plan_t *p);
 int grid_dkv(const skrull_attn_plan_t *p);

@@ -54,6 +54,7 @@ struct FwdParams {
     WorkQueue *queue;  // work queue of the persistent launch, zero when it starts
     WorkQueue *clear;  // null, or the one that the stream's next launch will use: zeroed by this one
     int32_t n_work, n_first;  // work items: what a plain grid would have as workgroups; workgroups launched
+    int32_t window, sinks;    // of the windowed kernels
 };
 
 // Shapes of the one kernel.  Large: 8 wavefronts = 8 row blocks per workgroup and
@@ -130,7 +131,8 @@ struct FwdSource {
 using FwdFeed = WorkFeed<true, FwdSource>;
 
 // Does work item `bid`, whose rows are `rb`; returns the next one and leaves its rows in `rb`.
-template <int D, int NW, int NSLOT>
+// WINDOW: a row sees the `window` last keys and the `sinks` first ones.
+template <int D, int NW, int NSLOT, bool WINDOW>
 __device__ __forceinline__ int fwd_work(const int bid, RowBlocks &rb, FwdFeed &feed)
 {
     const kernarg_t<FwdParams> prm = kernarg<FwdParams>();
@@ -170,16 +172,19 @@ __device__ __forceinline__ int fwd_work(const int bid, RowBlocks &rb, FwdFeed &f
 
     const int p0 = rb.p0;  // global position of the item's first query
     const int rows = rb.rows, qrow0 = rb.qrow0;
-    const int n_tiles = (p0 + min(rb.block(0) * 32 + 32, rows) + KT - 1) / KT;  // for the workgroup's last row block
+    KeyWalk<WINDOW> walk;
+    walk.init(WINDOW ? p0 + rb.lowest(NW) * 32 : 0, prm->window, prm->sinks);
+    const int n_tiles = walk.tile((p0 + min(rb.block(0) * 32 + 32, rows) + KT - 1) / KT);  // for the workgroup's last row block
 
     const bool wave_active = rb.has(wave);
     const int wrow0 = wave_active ? rb.block(wave) * 32 : 0;  // first row of this wave's block inside the item
     const int head = rb.head(wave);
     const int w_pmin = p0 + wrow0;
     const int w_pmax = p0 + min(wrow0 + 31, rows - 1);
-    // half tiles (32 keys) of this wave: 0..L hold a visible key, those below n_full only visible keys
-    const int L = wave_active ? w_pmax / 32 : -1;
-    const int n_full = wave_active ? (w_pmin + 1) / 32 : 0;
+    walk.wave(w_pmin, w_pmax);
+    // half tiles (32 keys) of this wave: 0..L hold a visible key (of those that `walk` has), those below n_full only visible keys
+    const int L = wave_active ? walk.half(w_pmax / 32) : -1;
+    const int n_full = wave_active ? walk.half((w_pmin + 1) / 32) : 0;
 
     // Q fragments (B operand of S^T): this lane's query row, 8 head-dims per k-step
     // (loaded below, behind the first tile fetches)
@@ -205,7 +210,8 @@ __device__ __forceinline__ int fwd_work(const int bid, RowBlocks &rb, FwdFeed &f
     // rescale of the running sum and of O when some lane's maximum moved
     auto finish = [&](float m_new, float rs) __attribute__((always_inline)) {
         if (__builtin_expect(__builtin_amdgcn_ballot_w64(m_new != m_run) != 0, 0)) {
-            const float alpha = fast_exp2(m_run - m_new);
+            // (a row that has seen no key yet has no bound, and nothing to rescale)
+            const float alpha = fast_exp2(m_run - (WINDOW && m_new == -INFINITY ? 0.0f : m_new));
             l_run *= alpha;
 #pragma unroll
             for (int tt = 0; tt < TT; ++tt)
@@ -302,7 +308,7 @@ __device__ __forceinline__ int fwd_work(const int bid, RowBlocks &rb, FwdFeed &f
     // ---- plain step j with run-time guards (start, end and diagonal of the wave's range)
     auto generic = [&](int j, const unsigned char *kp, const unsigned char *vp, const f32x16 &s_in,
                        f32x16 &s_out, const bf16x8 (&p_in)[2], bf16x8 (&p_out)[2]) __attribute__((always_inline)) {
-        if (j - 1 >= 0 && j - 1 <= L) {  // O += V(j-1) P(j-1)
+        if (j - 1 >= 0 && j - 1 <= L && walk.live(j - 1)) {  // O += V(j-1) P(j-1)
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
@@ -310,7 +316,7 @@ __device__ __forceinline__ int fwd_work(const int bid, RowBlocks &rb, FwdFeed &f
                 SB();
             }
         }
-        if (j + 1 <= L) {  // S(j+1)
+        if (j + 1 <= L && walk.live(j + 1)) {  // S(j+1)
 #pragma unroll
             for (int v = 0; v < 16; ++v) s_out[v] = 0.0f;
 #pragma unroll
@@ -319,22 +325,27 @@ __device__ __forceinline__ int fwd_work(const int bid, RowBlocks &rb, FwdFeed &f
                 if (ks % 4 == 3) SB();
             }
         }
-        if (j >= 0 && j <= L) {  // softmax(j)
+        if (WINDOW && !walk.live(j)) {
+            const uint4 z4 = make_uint4(0, 0, 0, 0);  // (a pipelined step that follows multiplies them with V)
+            p_out[0] = p_out[1] = as_bf16x8(z4);
+        } else if (j >= 0 && j <= L) {  // softmax(j)
             f32x16 s = s_in;
-            if (j >= n_full) {  // half tile touches the diagonal for this wave
+            if (j >= n_full || !walk.full(j)) {  // half tile touches the diagonal, or the window's start, for this wave
                 // relative position from an opaque copy of the lane index: the sixteen
                 // per-register thresholds are formed here rather than kept for the whole kernel
                 int li = lane;
                 asm volatile("" : "+v"(li));
-                const int rel = p0 + wrow0 + (li & 31) - 32 * j - 4 * (li >> 5);  // this lane's query position - 32j - 4h
+                const int rel = p0 + wrow0 + (li & 31) - walk.half_key(j) - 4 * (li >> 5);  // this lane's query position - first key - 4h
+                const int sinks_rel = WINDOW ? walk.sinks - walk.half_key(j) - 4 * (li >> 5) : 0;
 #pragma unroll
-                for (int v = 0; v < 16; ++v) s[v] = (8 * (v >> 2) + (v & 3) > rel) ? -INFINITY : s[v];
+                for (int v = 0; v < 16; ++v) s[v] = walk.hidden(8 * (v >> 2) + (v & 3), rel, sinks_rel) ? -INFINITY : s[v];
             }
             const float m_new = row_max(s);
+            const float shift = WINDOW && m_new == -INFINITY ? 0.0f : m_new;  // (a row that has seen no key yet: exponentials of 0)
             float rs = 0.0f;
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
-                s[v] = fast_exp2(__builtin_fmaf(s[v], cs, -m_new));
+                s[v] = fast_exp2(__builtin_fmaf(s[v], cs, -shift));
                 rs += s[v];
             }
             p_out[0] = acc_to_b(s, 0);
@@ -349,21 +360,21 @@ __device__ __forceinline__ int fwd_work(const int bid, RowBlocks &rb, FwdFeed &f
     // fetching K tile t+1 and V tile t into the slots period t-1 has left.
     auto fetch = [&](int t) __attribute__((always_inline)) {
         if (NSLOT == 4) {
-            ld.load(rk, ring_k + (uint32_t)((t + 2) & 3) * TB, (t + 2) * KT, wave);
-            ld.load(rv, ring_v + (uint32_t)((t + 1) & 3) * TB, (t + 1) * KT, wave);
-            ld.load(rk, ring_k + (uint32_t)((t + 3) & 3) * TB, (t + 3) * KT, wave);
-            ld.load(rv, ring_v + (uint32_t)((t + 2) & 3) * TB, (t + 2) * KT, wave);
+            ld.load(rk, ring_k + (uint32_t)((t + 2) & 3) * TB, walk.key(t + 2), wave);
+            ld.load(rv, ring_v + (uint32_t)((t + 1) & 3) * TB, walk.key(t + 1), wave);
+            ld.load(rk, ring_k + (uint32_t)((t + 3) & 3) * TB, walk.key(t + 3), wave);
+            ld.load(rv, ring_v + (uint32_t)((t + 2) & 3) * TB, walk.key(t + 2), wave);
         } else {
-            ld.load(rk, ring_k + (uint32_t)((t + 1) & 1) * TB, (t + 1) * KT, wave);
-            ld.load(rv, ring_v + (uint32_t)(t & 1) * TB, t * KT, wave);
+            ld.load(rk, ring_k + (uint32_t)((t + 1) & 1) * TB, walk.key(t + 1), wave);
+            ld.load(rv, ring_v + (uint32_t)(t & 1) * TB, walk.key(t), wave);
         }
     };
 
     // Start-up: the tiles of the first period.  The rest of period 0's fetch group follows after
     // the barrier below, because until then its slots stage this item's rows of Q.
-    ld.load(rk, ring_k, 0, wave);  // K tile 0
-    if (NSLOT == 4) ld.load(rk, ring_k + TB, KT, wave);  // K tile 1
-    ld.load(rv, ring_v, 0, wave);  // V tile 0
+    ld.load(rk, ring_k, walk.key(0), wave);  // K tile 0
+    if (NSLOT == 4) ld.load(rk, ring_k + TB, walk.key(1), wave);  // K tile 1
+    ld.load(rv, ring_v, walk.key(0), wave);  // V tile 0
     // this wave's staging region: half a ring slot that holds no tile yet (four slots: K slots
     // 2-3 for waves 0-3, V slots 1-2 for waves 4-7; two slots: K slot 1 for waves 0-1, V slot 1
     // for waves 2-3)
@@ -394,7 +405,7 @@ __device__ __forceinline__ int fwd_work(const int bid, RowBlocks &rb, FwdFeed &f
     if (NSLOT == 4) {
         if (1 < n_tiles) fetch(0);
     } else {
-        ld.load(rk, ring_k + TB, KT, wave);  // K tile 1
+        ld.load(rk, ring_k + TB, walk.key(1), wave);  // K tile 1
     }
 
     f32x16 sx, sy;         // S of the current / next half tile, ping-pong
@@ -443,8 +454,14 @@ __device__ __forceinline__ int fwd_work(const int bid, RowBlocks &rb, FwdFeed &f
         }
         period_end(t);
     };
-    plain_period(0);
     int t = 1;
+    if (WINDOW) {
+        const int t_steady = min(walk.first_full_period(), n_tiles + 1);
+#pragma unroll 1
+        for (t = 0; t < t_steady; ++t) plain_period(t);
+    } else {
+        plain_period(0);
+    }
     // the pipelined loop proper: S and P ping-pong between two register sets
     for (; t <= t_steady_end; ++t) {
         period_begin(t);
@@ -492,7 +509,7 @@ __device__ __forceinline__ int fwd_work(const int bid, RowBlocks &rb, FwdFeed &f
     return next;
 }
 
-template <int D, int NW, int NSLOT>
+template <int D, int NW, int NSLOT, bool WINDOW = false>
 __global__ __launch_bounds__(64 * NW, NW == NW_WIDE ? 3 : 2) void fwd_kernel(const FwdParams prm)
 {
     __shared__ int work_slot[2];
@@ -504,7 +521,7 @@ __global__ __launch_bounds__(64 * NW, NW == NW_WIDE ? 3 : 2) void fwd_kernel(con
     if (w != (int)blockIdx.x) rb = row_blocks<NW>(kernarg<FwdParams>(), prm.items, max(w, 0));
     while (w >= 0) {
         if (rb.has(0)) {
-            w = fwd_work<D, NW, NSLOT>(w, rb, feed);
+            w = fwd_work<D, NW, NSLOT, WINDOW>(w, rb, feed);
             if (w == kQueueEmpty) {
                 w = feed.other();
                 rb = row_blocks<NW>(kernarg<FwdParams>(), prm.items, max(w, 0));
@@ -530,32 +547,38 @@ hipError_t launch_shape(FwdParams prm, int threads, hipStream_t st)
     return hipGetLastError();
 }
 
-template <int D>
+template <int D, bool WINDOW>
 hipError_t launch_one(const FwdParams &prm, hipStream_t st)
 {
-    if (prm.variant == 0) return launch_shape<fwd_kernel<D, NW_SMALL, NSLOT_SMALL>>(prm, 64 * NW_SMALL, st);
+    if (prm.variant == 0) return launch_shape<fwd_kernel<D, NW_SMALL, NSLOT_SMALL, WINDOW>>(prm, 64 * NW_SMALL, st);
     if constexpr (D == 64)
-        if (prm.variant == 2) return launch_shape<fwd_kernel<D, NW_WIDE, NSLOT_LARGE>>(prm, 64 * NW_WIDE, st);
-    return launch_shape<fwd_kernel<D, NW_LARGE, NSLOT_LARGE>>(prm, 64 * NW_LARGE, st);
+        if (prm.variant == 2) return launch_shape<fwd_kernel<D, NW_WIDE, NSLOT_LARGE, WINDOW>>(prm, 64 * NW_WIDE, st);
+    return launch_shape<fwd_kernel<D, NW_LARGE, NSLOT_LARGE, WINDOW>>(prm, 64 * NW_LARGE, st);
+}
+template <bool WINDOW>
+hipError_t launch_one(const skrull_attn_plan_t *p, const FwdParams &prm, hipStream_t st)
+{
+    return p->d == 128 ? launch_one<128, WINDOW>(prm, st) : p->d == 64 ? launch_one<64, WINDOW>(prm, st) : hipErrorInvalidValue;
 }
 
-template <int D>
+template <int D, bool WINDOW>
 RowLaunch rows_fwd(const skrull_attn_plan_t *p)
 {
-    if (p->fwd_waves == NW_SMALL) return row_launch<fwd_kernel<D, NW_SMALL, NSLOT_SMALL>>(p, NW_SMALL);
+    if (p->fwd_waves == NW_SMALL) return row_launch<fwd_kernel<D, NW_SMALL, NSLOT_SMALL, WINDOW>>(p, NW_SMALL);
     if constexpr (D == 64)
-        if (p->fwd_waves == NW_WIDE) return row_launch<fwd_kernel<D, NW_WIDE, NSLOT_LARGE>>(p, NW_WIDE);
-    return row_launch<fwd_kernel<D, NW_LARGE, NSLOT_LARGE>>(p, NW_LARGE);
+        if (p->fwd_waves == NW_WIDE) return row_launch<fwd_kernel<D, NW_WIDE, NSLOT_LARGE, WINDOW>>(p, NW_WIDE);
+    return row_launch<fwd_kernel<D, NW_LARGE, NSLOT_LARGE, WINDOW>>(p, NW_LARGE);
 }
 
 }  // namespace
 
-static RowLaunch rows_fwd(const skrull_attn_plan_t *p) { return p->d == 128 ? rows_fwd<128>(p) : rows_fwd<64>(p); }
+template <bool WINDOW>
+static RowLaunch rows_fwd(const skrull_attn_plan_t *p) { return p->d == 128 ? rows_fwd<128, WINDOW>(p) : rows_fwd<64, WINDOW>(p); }
 
-int grid_fwd(const skrull_attn_plan_t *p) { return rows_fwd(p).n_work; }
+int grid_fwd(const skrull_attn_plan_t *p) { return rows_fwd<false>(p).n_work; }
 
 hipError_t launch_fwd(const skrull_attn_plan_t *p, const void *q, const void *k, const void *v,
-                      void *o, float *lse, hipStream_t st, WgTrace *trace)
+                      void *o, float *lse, hipStream_t st, WgTrace *trace, const KeyWindow *window)
 {
     FwdParams prm;
     prm.q = (const uint16_t *)q; prm.k = (const uint16_t *)k; prm.v = (const uint16_t *)v;
@@ -563,12 +586,14 @@ hipError_t launch_fwd(const skrull_attn_plan_t *p, const void *q, const void *k,
     prm.items = (const int4 *)p->fwd_items;
     prm.cu_k = p->cu_k; prm.q_begin = p->q_begin; prm.q_len = p->q_len; prm.kv_len = p->kv_len;
     prm.Hq = p->Hq; prm.Hkv = p->Hkv; prm.total_q = p->total_q;
-    const RowLaunch rows = rows_fwd(p);
+    const RowLaunch rows = window ? rows_fwd<true>(p) : rows_fwd<false>(p);
     prm.rows = rows.rows;
     prm.scale_log2 = p->scale * 1.4426950408889634f;
     prm.trace = trace;
     prm.variant = p->fwd_waves / 4 - 1;
     prm.n_work = rows.n_work;
+    prm.window = window ? window->keys : 0;
+    prm.sinks = window ? window->sinks : 0;
     prm.queue = prm.clear = nullptr;
     static_assert(8 * kQueueStride * sizeof(WorkQueue) == 4 * SKRULL_QUEUE_INTS, "a slot holds eight queues");
     DefaultStream &own = *p->default_stream;
@@ -587,7 +612,7 @@ hipError_t launch_fwd(const skrull_attn_plan_t *p, const void *q, const void *k,
             prm.queue = p->fwd_queues + 8 * kQueueStride * (__atomic_fetch_add(&const_cast<skrull_attn_plan_t *>(p)->fwd_calls, 1u, __ATOMIC_RELAXED) % SKRULL_FWD_QUEUE_SLOTS);
         }
     }
-    const hipError_t e = p->d == 128 ? launch_one<128>(prm, st) : p->d == 64 ? launch_one<64>(prm, st) : hipErrorInvalidValue;
+    const hipError_t e = window ? launch_one<true>(p, prm, st) : launch_one<false>(p, prm, st);
     if (in_turn) {
         if (e == hipSuccess) ++own.fwd;
         else own.lost = true;

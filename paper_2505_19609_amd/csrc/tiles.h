@@ -166,6 +166,13 @@ struct RowBlocks {
     int g, first, step, end, nblk;  // heads per KV head; row blocks of this part: first + wave * step, below end
     uint64_t inv_g;
     __device__ __forceinline__ bool has(int wave) const { return first + wave * step < end; }
+    // the lowest of the row blocks of `waves` wavefronts
+    __device__ __forceinline__ int lowest(int waves) const
+    {
+        int w = waves - 1;
+        while (w > 0 && !has(w)) --w;
+        return block(w);
+    }
     __device__ __forceinline__ int block(int wave) const { return nblk - 1 - quotient(first + wave * step, inv_g); }
     __device__ __forceinline__ int head(int wave) const  // query head of the wave's row block
     {
@@ -222,6 +229,57 @@ __device__ __forceinline__ RowBlocks row_blocks(const P prm, const int4 *items, 
     }
     return r;
 }
+
+// ---------------------------------------------------------------------------
+// The keys that a forward / dQ workgroup walks over where its rows see a window of them (the last `window` ones) and the first `sinks`
+// ones of the sequence: the tiles that hold sinks, then those from the first one that the lowest row's window reaches.  Tiles and half tiles (32 keys) are numbered
+// in the order of the walk.  Without a window (WINDOW false) that is every tile from the first.
+// ---------------------------------------------------------------------------
+template <bool WINDOW>
+struct KeyWalk {
+    int skip, sink_tiles;            // tiles that are passed over; those before them
+    int sinks, window;
+    int live_from, full_from;        // a wave's half tiles: those from sinks_end to live_from hold no visible key, those from full_sinks to full_from may hold hidden ones
+    int sinks_end, full_sinks;
+
+    // `lowest`: position of the workgroup's lowest row
+    __device__ __forceinline__ void init(int lowest, int window_, int sinks_)
+    {
+        skip = sink_tiles = 0;
+        if constexpr (WINDOW) {
+            window = window_;
+            sinks = sinks_;
+            const int first = max(0, lowest - window + 1) / TILE_ROWS;
+            sink_tiles = min((sinks + TILE_ROWS - 1) / TILE_ROWS, first);
+            skip = first - sink_tiles;
+            sinks_end = (sinks + 31) / 32;
+            full_sinks = sinks / 32;
+        }
+    }
+    // ... and a wave's rows
+    __device__ __forceinline__ void wave(int lowest, int highest)
+    {
+        if constexpr (WINDOW) {
+            live_from = max(0, lowest - window + 1) / 32 - 2 * skip;
+            full_from = (max(0, highest - window + 1) + 31) / 32 - 2 * skip;
+            if (full_from <= full_sinks) full_from = 0;   // (the sinks reach up to it)
+        }
+    }
+    // first key of tile t
+    __device__ __forceinline__ int key(int t) const { return (WINDOW && t >= sink_tiles ? t + skip : t) * TILE_ROWS; }
+    // the position of a tile or half tile behind the skipped ones, as a number of the walk
+    __device__ __forceinline__ int tile(int t) const { return t - skip; }
+    __device__ __forceinline__ int half(int j) const { return j - 2 * skip; }
+    // first key of half tile j
+    __device__ __forceinline__ int half_key(int j) const { return (WINDOW && j >= 2 * sink_tiles ? j + 2 * skip : j) * 32; }
+    // whether half tile j, at most the wave's last one, holds a visible key; whether all below the diagonal are visible
+    __device__ __forceinline__ bool live(int j) const { return !WINDOW || j < sinks_end || j >= live_from; }
+    __device__ __forceinline__ bool full(int j) const { return !WINDOW || j < full_sinks || j >= full_from; }
+    // the first period (half tiles 2 t - 1 and 2 t) that is full on both sides of the window, without what the sinks alone make full
+    __device__ __forceinline__ int first_full_period() const { return WINDOW ? max(1, (full_from + 2) / 2) : 1; }
+    // whether the key c behind `rel` places before a row is hidden: behind it, or in front of its window and no sink (its sinks end at `sinks_rel`)
+    __device__ __forceinline__ bool hidden(int c, int rel, int sinks_rel) const { return c > rel || (WINDOW && c <= rel - window && c >= sinks_rel); }
+};
 
 // ---------------------------------------------------------------------------
 // Asynchronous fetch of 64-row tiles of one [rows, H, D] matrix restricted to one

@@ -1,4 +1,4 @@
-"""The operators that a block is made of (the residual stream) without a GPU: symbols, struct layouts and what the
+"""The operators that a block is made of (attention to a window, the residual stream) without a GPU: symbols, struct layouts and what the
 entry points refuse."""
 import ctypes
 import math
@@ -13,12 +13,12 @@ from paper_2505_19609_amd import binding as B
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 ONE = 1 << 20   # an address that is aligned and never read: the call fails first
-HEADERS = ("skrull_residual.h",)
+HEADERS = ("skrull_window.h", "skrull_residual.h")
 
 
 def test_library_exports_every_declared_operator():
     header = "".join(open(os.path.join(ROOT, "include", f)).read() for f in HEADERS)
-    declared = set(re.findall(r"\b(skrull_(?:residual)(?:_[a-z]+)*)\s*\(", header))
+    declared = set(re.findall(r"\b(skrull_(?:window|residual)(?:_[a-z]+)*)\s*\(", header))
     assert declared == set(B.BLOCK_SYMBOLS)
     for name in declared:
         assert getattr(B.lib(), name) is not None
@@ -33,6 +33,7 @@ def test_argument_counts_match_headers():
 
 
 def test_struct_layouts_match_headers():
+    assert ctypes.sizeof(B.Window) == 2 * 4
     assert ctypes.sizeof(B.Residual) == 8 + 7 * 4 + 4 + 8 * 8   # (scale and its padding)
 
 
@@ -111,3 +112,47 @@ def test_residual_wrappers_refuse():
         A.skrull_residual_norm(r[0], z, w)
     with pytest.raises(B.SkrullError, match="current GPU"):
         A.skrull_residual_norm(r, z, w)
+
+
+# ---- attention to a window ------------------------------------------------------------------------------------------
+
+def test_window_refuses_null():
+    w = B.Window(4, 0)
+    lib = B.lib()
+    assert lib.skrull_window_fwd(None, ctypes.byref(w), *[ONE] * 5, None) == B.SKRULL_EINVAL
+    assert "window" in B.skrull_attn_strerror(B.SKRULL_EINVAL)
+    assert lib.skrull_window_bwd(None, ctypes.byref(w), *[ONE] * 10, 1 << 30, None) == B.SKRULL_EINVAL
+    assert lib.skrull_window_workspace(None, ctypes.byref(w)) == 0
+    assert lib.skrull_window_fwd(ONE, None, *[ONE] * 5, None) == lib.skrull_window_bwd(ONE, None, *[ONE] * 10, 1 << 30, None) == B.SKRULL_EINVAL
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (-1, 0), (4, -1)])
+def test_window_refuses_values(window, sinks):
+    """(the plan is not looked at before)"""
+    w = B.Window(window, sinks)
+    lib = B.lib()
+    assert lib.skrull_window_fwd(ONE, ctypes.byref(w), *[ONE] * 5, None) == B.SKRULL_EINVAL
+    assert lib.skrull_window_bwd(ONE, ctypes.byref(w), *[ONE] * 10, 1 << 30, None) == B.SKRULL_EINVAL
+    assert lib.skrull_window_workspace(ONE, ctypes.byref(w)) == 0
+
+
+def test_window_wrappers_refuse():
+    q = torch.zeros(4, 2, 64, dtype=torch.bfloat16)
+    info = B.PlanInfo(total_q=4, total_k=4, num_q_heads=2, num_kv_heads=2, head_dim=64)
+    plan = B.Plan(None, info)
+    lse = torch.zeros(2, 4)
+    with pytest.raises(B.SkrullError, match="current GPU"):
+        A.skrull_window_attention(q, q, q, plan, 4)
+    for value in (1 << 31, -(1 << 31) - 1):
+        with pytest.raises(B.SkrullError, match="window"):
+            B._window_of(value, 0)
+        with pytest.raises(B.SkrullError, match="sinks"):
+            B._window_of(1, value)
+    with pytest.raises(B.SkrullError, match="contiguous bf16"):
+        B._heads(plan, (q.float(),))
+    with pytest.raises(B.SkrullError, match="contiguous bf16"):
+        B._heads(plan, (), (q[:3],))
+    with pytest.raises(B.SkrullError, match="contiguous bf16"):
+        B._heads(plan, (torch.zeros(4, 4, 64, dtype=torch.bfloat16)[:, ::2],))
+    with pytest.raises(B.SkrullError, match="lse"):
+        B._lse(plan, lse.t())
