@@ -280,6 +280,54 @@ def skrull_residual_norm(r, z, weight, bias=None, post_weight=None, post_bias=No
     return _SkrullResidualNorm.apply(_rows(r), _rows(z), *(None if t is None else t.contiguous() for t in vectors), float(scale), float(eps), _KINDS[kind])
 
 
+_ACTIVATIONS = {"none": B.LINEAR_NONE, "relu": B.LINEAR_RELU, "gelu": B.LINEAR_GELU, "silu": B.LINEAR_SILU}
+
+
+class _SkrullLinear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, residual, activation, gated):
+        n = weight.shape[0]
+        y = torch.empty((x.shape[0], n // 2 if gated else n), dtype=x.dtype, device=x.device)
+        kept = (gated or activation != B.LINEAR_NONE) and any(ctx.needs_input_grad[:3])
+        z = torch.empty((x.shape[0], n), dtype=x.dtype, device=x.device) if kept else None
+        B.skrull_linear_fwd(x, weight, bias, residual, y, z, _workspace(B.skrull_linear_workspace(x, weight, False, activation, gated), x.device), activation, gated)
+        ctx.activation, ctx.gated = activation, gated
+        ctx.save_for_backward(x, weight, z)
+        return y
+
+    @staticmethod
+    @_once(lambda ctx: any(ctx.needs_input_grad[:2]) or (ctx.needs_input_grad[2] and (ctx.gated or ctx.activation != B.LINEAR_NONE)))
+    def backward(ctx, dy):
+        x, weight, z = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need[0] else None
+        dw = torch.empty_like(weight) if need[1] else None
+        db = torch.empty(weight.shape[0], dtype=weight.dtype, device=weight.device) if need[2] else None
+        if any(need[:3]):
+            ws = _workspace(B.skrull_linear_workspace(x, weight, True, ctx.activation, ctx.gated), x.device)
+            B.skrull_linear_bwd(x, weight, z, _wide_rows(dy), dx, dw, db, ws, ctx.activation, ctx.gated)
+        return dx, dw, db, dy if need[3] else None, None, None
+
+
+def _wide_rows(t):
+    """`t` [rows, cols] as the library's products take it: contiguous rows at multiples of 16 bytes."""
+    fits = t.dim() == 2 and (t.shape[1] < 2 or t.stride(1) == 1) and t.data_ptr() % 16 == 0 and (t.shape[0] < 2 or (t.stride(0) >= t.shape[1] and t.stride(0) % 8 == 0 and
+                                                                                                                    t.stride(0) <= 1 << 20))
+    return t if fits else t.clone(memory_format=torch.contiguous_format)
+
+
+def skrull_linear(x, weight, bias=None, residual=None, activation="none", gated=False):
+    """f(x weight^T + bias) + residual of rows x [rows, inputs] and a weight [n, inputs] (bf16), with f "none", "relu", "gelu" or "silu"; `gated`: f of the first
+    n / 2 columns times the others.  Differentiable with respect to x, weight, bias and residual."""
+    if activation not in _ACTIVATIONS:
+        raise ValueError(f"activation must be one of {sorted(_ACTIVATIONS)}")
+    if x.dim() != 2 or weight.dim() != 2:
+        raise ValueError("x must be [rows, inputs] and weight [n, inputs]")
+    _refuse_captured(x, weight, bias, residual)
+    return _SkrullLinear.apply(_wide_rows(x), _aligned(weight), None if bias is None else _aligned(bias), None if residual is None else _wide_rows(residual),
+                               _ACTIVATIONS[activation], bool(gated))
+
+
 class _SkrullCrossEntropy(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, target):

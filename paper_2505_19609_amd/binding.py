@@ -21,6 +21,7 @@ ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_NTK, ROTARY_PARTS = range(4)
 ROWS_Q, ROWS_K = 0, 1
 NORM_RMS, NORM_LAYER = 0, 1
 TYPE_BF16, TYPE_FP32 = 0, 1
+LINEAR_NONE, LINEAR_RELU, LINEAR_GELU, LINEAR_SILU = range(4)
 
 EXPORTED_SYMBOLS = ("skrull_attn_plan", "skrull_attn_plan_info", "skrull_attn_plan_export",
                     "skrull_attn_fwd", "skrull_attn_bwd", "skrull_attn_bwd_static", "skrull_attn_plan_destroy",
@@ -31,9 +32,10 @@ EXPORTED_SYMBOLS = ("skrull_attn_plan", "skrull_attn_plan_info", "skrull_attn_pl
 # the operators around attention (skrull_rotary.h, skrull_norm.h, skrull_loss.h)
 OPERATOR_SYMBOLS = ("skrull_rotary_check", "skrull_rotary", "skrull_norm_fwd", "skrull_norm_workspace", "skrull_norm_bwd",
                     "skrull_loss_workspace", "skrull_loss_fwd", "skrull_loss_bwd")
-# what else a block is made of (skrull_window.h, skrull_residual.h)
+# what else a block is made of (skrull_window.h, skrull_residual.h, skrull_linear.h)
 BLOCK_SYMBOLS = ("skrull_window_fwd", "skrull_window_workspace", "skrull_window_bwd",
-                 "skrull_residual_fwd", "skrull_residual_workspace", "skrull_residual_bwd")
+                 "skrull_residual_fwd", "skrull_residual_workspace", "skrull_residual_bwd",
+                 "skrull_linear_workspace", "skrull_linear_fwd", "skrull_linear_bwd")
 
 
 class Problem(ctypes.Structure):
@@ -108,6 +110,12 @@ class Residual(ctypes.Structure):
                 ("residual_type", ctypes.c_int32), ("weight_type", ctypes.c_int32), ("eps", ctypes.c_float), ("scale", ctypes.c_float),
                 ("r_stride", ctypes.c_int64), ("z_stride", ctypes.c_int64), ("r_out_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64),
                 ("d_r_out_stride", ctypes.c_int64), ("dy_stride", ctypes.c_int64), ("dr_stride", ctypes.c_int64), ("dz_stride", ctypes.c_int64)]
+
+
+class Linear(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("inputs", ctypes.c_int32), ("outputs", ctypes.c_int32), ("activation", ctypes.c_int32),
+                ("gated", ctypes.c_int32), ("x_stride", ctypes.c_int64), ("residual_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64),
+                ("dy_stride", ctypes.c_int64)]
 
 
 class Loss(ctypes.Structure):
@@ -185,7 +193,10 @@ def lib():
         L.skrull_norm_fwd.argtypes = [norm] + [vp] * 7
         L.skrull_norm_workspace.argtypes = [norm]
         L.skrull_norm_bwd.argtypes = [norm] + [vp] * 9 + [ctypes.c_size_t, vp]
-        window, residual = ctypes.POINTER(Window), ctypes.POINTER(Residual)
+        window, residual, linear = ctypes.POINTER(Window), ctypes.POINTER(Residual), ctypes.POINTER(Linear)
+        L.skrull_linear_workspace.argtypes = [linear, ctypes.c_int]
+        L.skrull_linear_fwd.argtypes = [linear] + [vp] * 7 + [ctypes.c_size_t, vp]
+        L.skrull_linear_bwd.argtypes = [linear] + [vp] * 8 + [ctypes.c_size_t, vp]
         L.skrull_window_fwd.argtypes = [vp, window] + [vp] * 6
         L.skrull_window_workspace.argtypes = [vp, window]
         L.skrull_window_bwd.argtypes = [vp, window] + [vp] * 10 + [ctypes.c_size_t, vp]
@@ -693,3 +704,59 @@ def skrull_loss_bwd(x, weight, target, lse, d_loss, dx, dweight, workspace, stre
     _check(lib().skrull_loss_bwd(ctypes.byref(p), _ptr(x), _ptr(weight), _ptr(target), _vector(lse, p.rows, torch.float32, "lse"),
                                  _vector(d_loss, p.rows, torch.float32, "d_loss"), None if dx is None else _ptr(dx),
                                  None if dweight is None else _ptr(dweight), *_scratch(workspace), _stream_ptr(stream)))
+
+
+# ---- products with what follows them --------------------------------------------------------------------------------
+
+def _linear_of(x, weight, activation, gated, **rows) -> Linear:
+    import torch
+    if x.dim() != 2 or weight.dim() != 2 or weight.shape[1] != x.shape[1] or weight.dtype != torch.bfloat16 or not weight.is_contiguous():
+        _refuse(f"weight must be contiguous bf16 [n, inputs] and x [rows, inputs], got {weight.dtype} {list(weight.shape)} and {list(x.shape)}")
+    n = weight.shape[0]
+    if gated and n % 2:
+        _refuse(f"gated, and {n} rows of weight")
+    outputs = n // 2 if gated else n
+    p = Linear(x.shape[0], _int32(x.shape[1], "inputs"), _int32(outputs, "outputs"), _int32(activation, "activation"), int(bool(gated)))
+    for name, t in dict(rows, x=x).items():
+        if t is None:
+            continue
+        shape = x.shape if name == "x" else (x.shape[0], outputs)
+        if t.dtype != torch.bfloat16 or t.shape != shape or (t.shape[1] > 1 and t.stride(1) != 1):
+            _refuse(f"{name} must be bf16 {list(shape)} with contiguous rows, got {t.dtype} {list(t.shape)}")
+        setattr(p, name + "_stride", t.stride(0) if t.shape[0] > 1 else t.shape[1])
+    return p
+
+
+def _given(t, shape, name):
+    """The address of a contiguous bf16 tensor that may be None."""
+    import torch
+    if t is not None and (t.dtype != torch.bfloat16 or t.shape != tuple(shape) or not t.is_contiguous()):
+        _refuse(f"{name} must be contiguous bf16 {list(shape)}, got {t.dtype} {list(t.shape)}")
+    return None if t is None else _ptr(t)
+
+
+def skrull_linear_workspace(x, weight, backward: bool, activation=LINEAR_NONE, gated=False) -> int:
+    """Bytes that skrull_linear_fwd or skrull_linear_bwd asks for; SkrullError where the sizes are outside the limits."""
+    n = int(lib().skrull_linear_workspace(ctypes.byref(_linear_of(x, weight, activation, gated)), int(backward)))
+    if n < 0:
+        _check(SKRULL_EINVAL)
+    return n
+
+
+def skrull_linear_fwd(x, weight, bias, residual, y, z, workspace, activation=LINEAR_NONE, gated=False, stream=None):
+    """y = f(x weight^T + bias) + residual (gated: f of the first half of the columns times the second); bias and residual may be None.  z (bf16 [rows, n], may
+    be None) for the backward of an activation or a gate."""
+    _on_current_device(x, weight, bias, residual, y, z, workspace)
+    p = _linear_of(x, weight, activation, gated, residual=residual, y=y)
+    n = weight.shape[0]
+    _check(lib().skrull_linear_fwd(ctypes.byref(p), _ptr(x), _ptr(weight), _given(bias, (n,), "bias"), None if residual is None else _ptr(residual), _ptr(y),
+                                   _given(z, (p.rows, n), "z"), *_scratch(workspace), _stream_ptr(stream)))
+
+
+def skrull_linear_bwd(x, weight, z, dy, dx, dweight, dbias, workspace, activation=LINEAR_NONE, gated=False, stream=None):
+    """dx, dweight and dbias where they are wanted (else None), for the gradient dy."""
+    _on_current_device(x, weight, z, dy, dx, dweight, dbias, workspace)
+    p = _linear_of(x, weight, activation, gated, dy=dy)
+    n = weight.shape[0]
+    _check(lib().skrull_linear_bwd(ctypes.byref(p), _ptr(x), _ptr(weight), _given(z, (p.rows, n), "z"), _ptr(dy), _given(dx, x.shape, "dx"),
+                                   _given(dweight, weight.shape, "dweight"), _given(dbias, (n,), "dbias"), *_scratch(workspace), _stream_ptr(stream)))

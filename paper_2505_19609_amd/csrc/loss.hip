@@ -22,14 +22,11 @@
 #include <math.h>
 
 #include "ops.h"
+#include "product.h"
 #include "skrull_loss.h"
-#include "tiles.h"
 
 namespace {
 
-constexpr int kTile = 256;       // rows and columns of a result tile
-constexpr int kStep = 64;        // of the contraction
-constexpr int kGrid = 256;       // workgroups: one per compute unit, each as much LDS as allows no second one
 constexpr int64_t kPieceBytes = (int64_t)2 << 30;  // of dz at most, but for one tile of words of all rows: 640 bytes a row, more than that from 3.4 million rows on
 // Rows of dz and of the gathered x are this much longer where their length is a multiple of 4 KB: the 256 rows of a tile would lie in few of the L2's sets.
 constexpr int kPitchPad = 64;
@@ -111,84 +108,6 @@ struct Piece {
     }
 };
 
-// Where an operand's step lies and how much of its matrix is behind that address.
-struct Source {
-    const unsigned char *at;
-    int64_t left;
-    uint32_t pitch;       // bytes between rows
-    int64_t step;         // bytes from one step to the next
-    __device__ __forceinline__ i32x4 words() const
-    {
-        const int64_t n = left < 0 ? 0 : left > 0x7fffffff ? 0x7fffffff : left;
-        return rsrc_words(at, (uint32_t)n);
-    }
-    __device__ __forceinline__ void next() { at += step; left -= step; }
-};
-
-// A tile's operand in LDS: two halves, each of what the wavefronts read in a half of their blocks (of every 32 NB rows or columns
-// the first or the second 16 NB; NB = 4: 16 KB a half).  A load's 64 pieces of 16 bytes lie one behind the other, so the arrangement is made
-// on the global side: a lane fetches the piece that belongs where it writes.
-//   ROWS  32 NB rows x 64 of the contraction (128 bytes a row): piece c of row r lies at c ^ (r / 2 & 7), so 16 rows' pieces of
-//         one c, which are read together, are 16 different slots of the 256 bytes that the banks span.
-//   COLS  64 of the contraction x 128 columns (256 bytes a row): piece c of row r lies at c ^ 2 (r & 3 | r / 2 & 4), so the 8 rows x 32 bytes
-//         that a transposing read takes together are 16 different slots too.
-template <bool COLS, int NB>
-struct Operand {
-    static_assert(NB == 4 || !COLS, "");
-    static constexpr int kHalfBytes = 4096 * NB;
-    int load[2];     // byte offsets of this lane's pieces in the tile's matrix: of even and odd instructions (COLS: of the first and the last two)
-    int read[4];     // LDS offsets of its fragments: ROWS by half step (two), COLS by block of 16 columns
-
-    __device__ __forceinline__ void init(int lane, int wave, int part, uint32_t pitch)
-    {
-        const int s = lane & 15, g = lane >> 4;
-        if (!COLS) {
-#pragma unroll
-            for (int o = 0; o < 2; ++o)
-                load[o] = ((wave >> 1) * 32 * NB + (wave & 1) * 8 * NB + (lane >> 3)) * (int)pitch + (((lane & 7) ^ (4 * odd(o, wave) + (lane >> 4))) << 4);
-#pragma unroll
-            for (int k = 0; k < 2; ++k) read[k] = (part * 16 * NB + s) * 128 + (((4 * k + g) ^ (s >> 1)) << 4);
-        } else {
-#pragma unroll
-            for (int o = 0; o < 2; ++o) {
-                const int piece = s ^ (g + 4 * o) << 1;
-                load[o] = (wave * 16 + g) * (int)pitch + (piece >> 3) * 256 + (piece & 7) * 16;
-            }
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-                read[t] = (8 * g + (s >> 2)) * 256 + (((8 * part + 2 * t + ((s & 3) >> 1)) ^ ((s >> 2) + 4 * (g & 1)) << 1) << 4) + 8 * (s & 1);
-        }
-    }
-    // This lane's offsets of a step.  `tail`: elements of the contraction that are left, where rows may end inside the
-    // step (ROWS): what is behind them reads as zero.
-    __device__ __forceinline__ void offsets(int lane, int wave, int tail, int off[2]) const
-    {
-#pragma unroll
-        for (int o = 0; o < 2; ++o) {
-            off[o] = load[o];
-            if (!COLS && ((lane & 7) ^ (4 * odd(o, wave) + (lane >> 4))) * 8 >= tail) off[o] = (int)0x80000000;   // (past every descriptor's end)
-        }
-    }
-    // whether an instruction fills an odd group of 8 rows: every second one of a wavefront does, or, where it has only one, every second wavefront's
-    static __device__ __forceinline__ int odd(int o, int wave) { return NB == 1 ? wave & 1 : o; }
-    // NB instructions of each wavefront fill a half.
-    __device__ __forceinline__ static void fetch(i32x4 words, const int off[2], uint32_t pitch, uint32_t lds, int wave, int half, int q)
-    {
-        dma_b128(words, lds + half * kHalfBytes + (wave * NB + q) * 1024, off[COLS ? q >> 1 : q & 1],
-                 COLS ? half * 128 + (int)(q * 4 * pitch) : (int)((half * 16 * NB + q * 8) * pitch));
-    }
-    // fragment b (16 rows or columns, 0..3) of a half and half step k: 8 consecutive elements of the contraction
-    __device__ __forceinline__ bf16x8 get(const unsigned char *t, int half, int b, int k) const
-    {
-        if (!COLS) return *(const bf16x8 *)(t + read[k] + half * kHalfBytes + b * 2048);
-        typedef s16x4 __attribute__((address_space(3))) * lds_ptr_t;
-        const unsigned char *p = t + read[b] + half * kHalfBytes + k * 8192;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)p);
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(p + 1024));
-        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-    }
-};
-
 // The tiles of a product and their operands.
 template <Kind K, int NA, int NB>
 struct Product {
@@ -262,32 +181,6 @@ struct Product {
     }
 };
 
-// A result that lies in an accumulator register.  (Read as ordinary values, all 256 were copied to vector registers at the end of the loop,
-// and what was there before went to scratch memory.)
-__device__ __forceinline__ float result(float f)
-{
-    float r;
-    asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(r) : "a"(f));
-    return r;
-}
-
-// Lane g of the four of a result column has rows 4 g .. 4 g + 3 of two blocks of 16.  In bf16, it gets rows 8 (g / 2) .. + 7 of the block g % 2.
-__device__ __forceinline__ uint4 eight_of(const float *first, const float *second)
-{
-    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-    const u32x2 a = __builtin_amdgcn_permlane16_swap(pack_bf16(first[0], first[1]), pack_bf16(second[0], second[1]), false, false);
-    const u32x2 b = __builtin_amdgcn_permlane16_swap(pack_bf16(first[2], first[3]), pack_bf16(second[2], second[3]), false, false);
-    return make_uint4(a[0], b[0], a[1], b[1]);
-}
-// `x`, of which the compiler does not know that it is the same everywhere.  (What a seldom taken branch works out of it is worked out there then, and
-// not ahead of them all.)
-__device__ __forceinline__ int here(int x)
-{
-    asm volatile("" : "+v"(x));
-    return x;
-}
-__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-
 // The tile is 64 NA x 64 NB: 256 x 256, x 128 or 64 with few rows, 64 x 64 with few words too (the logits).
 template <Kind K, int NA, int NB>
 __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
@@ -296,7 +189,7 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
     constexpr bool A_COLS = K == kDx || K == kDw, B_COLS = K == kDw;
     // (what the results of a tile need of its rows comes by loads to LDS too, in two places by turns: a load to registers would be waited for
     // together with all that are under way)
-    constexpr int kRows = 64 * NB, kOperandBytes = 8192 * NA, kBufferBytes = kOperandBytes + 8192 * NB, kStrip = 32 * NA;
+    constexpr int kRows = 64 * NB, kBufferBytes = kProductBytes<NA, NB>, kStrip = 32 * NA;
     constexpr int kRowBytes = K == kForward ? kRows * 4 : K == kAgain ? 3 * kRows * 4 : 0;
     __shared__ __align__(1024) unsigned char lds[2 * kBufferBytes + 2 * kRowBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1;
@@ -315,89 +208,19 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
     const int die = blockIdx.x & 7, per_die = (work.total + 7) / 8, stride = gridDim.x >> 3;
     const int begin = die * per_die + (blockIdx.x >> 3), end = min(work.total, (die + 1) * per_die);
 
-    // The steps of this workgroup's tiles are one sequence, and the loads run ahead in it across the end of a tile.
-    struct Cursor {
-        int tile, left, tail, parity;
-        Source a, b;
+    int row_at = 2 * kBufferBytes;   // LDS offset of the tile's row data
+    int m = 0, nn = 0, s = 0;
+    const int *row_targets = nullptr;
+    const float *row_lse = nullptr, *row_d = nullptr;
+    auto open = [&](int tile, Source &a, Source &b, int &left, int &a_tail, int &) {
+        int tm, tn, ts;
+        work.locate(tile, tm, tn, ts);
+        left = work.steps_of(ts);
+        work.sources(p, tm, tn, ts, a, b);
+        a_tail = p.H;
     };
-    struct Fetch {   // what the loads of a step need
-        i32x4 a, b;
-        int a_off[2], b_off[2];
-        uint32_t lds;
-    };
-    auto take = [&](Cursor &c) {   // the next step; behind the last one the loads read nothing
-        while (c.left == 0 && c.tile < end) {
-            int m, nn, s;
-            work.locate(c.tile, m, nn, s);
-            c.left = work.steps_of(s);
-            work.sources(p, m, nn, s, c.a, c.b);
-            c.tail = K == kForward || K == kAgain ? p.H : 0x7fffffff;   // elements of the contraction
-            c.tile += stride;
-        }
-        if (c.left == 0) c.a.left = c.b.left = 0;
-        Fetch f;
-        f.a = c.a.words();
-        f.b = c.b.words();
-        A.offsets(lane, wave, c.tail, f.a_off);
-        B.offsets(lane, wave, kStep, f.b_off);
-        f.lds = lds0 + c.parity * kBufferBytes;
-        c.a.next();
-        c.b.next();
-        c.tail -= kStep;
-        c.left -= c.left > 0;
-        c.parity ^= 1;
-        return f;
-    };
-    auto load_a = [&](const Fetch &f, int half, int q) { A.fetch(f.a, f.a_off, a_pitch, f.lds, wave, half, q); };
-    auto load_b = [&](const Fetch &f, int half, int q) { B.fetch(f.b, f.b_off, b_pitch, f.lds + kOperandBytes, wave, half, q); };
-
-    // A step in two halves, of 64 products with NB = 4.  What a half of the blocks needs is read half a step before its first product, so its place
-    // in LDS is free early, and its loads have a step until they are waited for:
-    //   half  products        reads                       loads (of the step after next)
-    //   1     A0 B0, A0 B1    B1, A1                      A0 B0
-    //   2     A1 B0, A1 B1    A0, B0 of the next step     B1 A1
-    // Each half ends with a barrier: what was read in it may be overwritten, and what the next one reads is there (a step's loads, 16 with NB = 4, are younger).
-    bf16x8 a0[NA][2], a1[NA][2], b0[NB][2], b1[NB][2];   // [block of 16][half step]
-    f32x4 acc[2 * NA][2 * NB];
-    auto half_end = [&]() {
-        SB();
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * (NA + NB)) : "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        SB();
-    };
-    Cursor cursor = {begin, 0, 0, 0, {}, {}};
-#pragma unroll
-    for (int step = 0; step < 2; ++step) {
-        const Fetch f = take(cursor);
-#pragma unroll
-        for (int q = 0; q < NA; ++q) {
-            load_a(f, 0, q);
-            if (q < NB) load_b(f, 0, q);
-        }
-#pragma unroll
-        for (int q = 0; q < NA; ++q) {
-            if (q < NB) load_b(f, 1, q);
-            load_a(f, 1, q);
-        }
-    }
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * (NA + NB)) : "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    auto read_a = [&](const unsigned char *t, int half, bf16x8 to[NA][2], int i) { to[i % NA][i / NA] = A.get(t, half, i % NA, i / NA); };
-    auto read_b = [&](const unsigned char *t, int half, bf16x8 to[NB][2], int i) { to[i % NB][i / NB] = B.get(t + kOperandBytes, half, i % NB, i / NB); };
-#pragma unroll
-    for (int j = 0; j < 2 * NA; ++j) {
-        read_a(lds, 0, a0, j);
-        if (j < 2 * NB) read_b(lds, 0, b0, j);
-    }
-    half_end();
-
-    int at = 0, row_at = 2 * kBufferBytes;   // LDS offsets of the step under way and of the tile's row data
-    for (int i = begin; i < end; i += stride) {
-        int m, nn, s;
+    auto tile_begin = [&](int i) {
         work.locate(i, m, nn, s);
-        const int steps = work.steps_of(s);
         if (K == kForward || K == kAgain) {
             const int row0 = nn * kRows + wave * 64;   // (older than a step's loads: there when the first one ends)
             if (wave < NB) {
@@ -408,102 +231,13 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
                 }
             }
         }
-        const int *row_targets = (const int *)(lds + row_at);
-        const float *row_lse = (const float *)(lds + row_at + 4 * kRows), *row_d = (const float *)(lds + row_at + 8 * kRows);
+        row_targets = (const int *)(lds + row_at);
+        row_lse = (const float *)(lds + row_at + 4 * kRows);
+        row_d = (const float *)(lds + row_at + 8 * kRows);
         row_at ^= (2 * kBufferBytes) ^ (2 * kBufferBytes + kRowBytes);
-#pragma unroll
-        for (int x = 0; x < 2 * NA; ++x)
-#pragma unroll
-            for (int y = 0; y < 2 * NB; ++y)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) acc[x][y][v] = 0.0f;
-        for (int step = 0; step < steps; ++step) {
-            const unsigned char *t = lds + at, *next = lds + (at ^ kBufferBytes);
-            const Fetch f = take(cursor);
-            if constexpr (NB == 4) {
-                // Product j of a quarter: blocks j / 8 and j / 2 % 4, half step j % 2 (two products in a row on one accumulator need less power:
-                // 1.7 % of the time against j / 16 for the half step); between pairs of them at most one read or load, i = j / 2.
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    const int k = j & 1, x = j >> 3 & 3, y = j >> 1 & 3, i = j >> 1;
-                    acc[x][y] = mfma16(a0[x][k], b0[y][k], acc[x][y]);
-                    SB();
-                    if (j & 1) continue;
-                    if (i < 8) b1[i >> 1][i & 1] = B.get(t + kOperandBytes, 1, i >> 1, i & 1);
-                    else if (i & 1) load_b(f, 0, (i - 8) >> 1);
-                    else load_a(f, 0, (i - 8) >> 1);
-                    SB();
-                }
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    const int k = j & 1, x = j >> 3 & 3, y = j >> 1 & 3, i = j >> 1;
-                    acc[x][4 + y] = mfma16(a0[x][k], b1[y][k], acc[x][4 + y]);
-                    SB();
-                    if (j & 1) continue;
-                    if (i < 8) a1[i >> 1][i & 1] = A.get(t, 1, i >> 1, i & 1);
-                    SB();
-                }
-                half_end();
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    const int k = j & 1, x = j >> 3 & 3, y = j >> 1 & 3, i = j >> 1;
-                    acc[4 + x][y] = mfma16(a1[x][k], b0[y][k], acc[4 + x][y]);
-                    SB();
-                    if (j & 1) continue;
-                    if (i < 8) a0[i >> 1][i & 1] = A.get(next, 0, i >> 1, i & 1);
-                    else if (i & 1) load_a(f, 1, (i - 8) >> 1);
-                    else load_b(f, 1, (i - 8) >> 1);
-                    SB();
-                }
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    const int k = j & 1, x = j >> 3 & 3, y = j >> 1 & 3, i = j >> 1;
-                    acc[4 + x][4 + y] = mfma16(a1[x][k], b1[y][k], acc[4 + x][4 + y]);
-                    SB();
-                    if (j & 1) continue;
-                    if (i < 8) b0[i >> 1][i & 1] = B.get(next + kOperandBytes, 0, i >> 1, i & 1);
-                    SB();
-                }
-                half_end();
-            } else {   // (fewer products: memory is what is waited for, so the loads go first)
-#pragma unroll
-                for (int i = 0; i < NA; ++i) load_a(f, 0, i);
-#pragma unroll
-                for (int i = 0; i < NB; ++i) load_b(f, 0, i);
-#pragma unroll
-                for (int i = 0; i < 2 * NB; ++i) read_b(t, 1, b1, i);
-#pragma unroll
-                for (int i = 0; i < 2 * NA; ++i) read_a(t, 1, a1, i);
-#pragma unroll
-                for (int j = 0; j < 4 * NA * NB; ++j) {   // block of 16 rows of B, of A, half step
-                    const int y = j / (2 * NA), x = j / 2 % NA, k = j & 1;
-                    acc[x][y] = mfma16(a0[x][k], y < NB ? b0[y][k] : b1[y - NB][k], acc[x][y]);
-                }
-                half_end();
-#pragma unroll
-                for (int i = 0; i < NB; ++i) load_b(f, 1, i);
-#pragma unroll
-                for (int i = 0; i < NA; ++i) load_a(f, 1, i);
-                bf16x8 b2[NB][2];   // (the first products of this half still need b0)
-#pragma unroll
-                for (int i = 0; i < 2 * NB; ++i) read_b(next, 0, b2, i);
-#pragma unroll
-                for (int i = 0; i < 2 * NA; ++i) read_a(next, 0, a0, i);
-#pragma unroll
-                for (int j = 0; j < 4 * NA * NB; ++j) {
-                    const int y = j / (2 * NA), x = j / 2 % NA, k = j & 1;
-                    acc[NA + x][y] = mfma16(a1[x][k], y < NB ? b0[y][k] : b1[y - NB][k], acc[NA + x][y]);
-                }
-#pragma unroll
-                for (int i = 0; i < 2 * NB; ++i) b0[i / 2][i & 1] = b2[i / 2][i & 1];
-                half_end();
-            }
-            at ^= kBufferBytes;
-        }
-
-        // (the compiler does not see that what follows reads results of the matrix pipe: the distance it would keep)
-        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
-        // acc[x][y][v] is row 32 NA wm + 16 x + 4 g + v and column 32 NB wn + 16 y + n of the tile
+        return work.steps_of(s);
+    };
+    auto tile_end = [&](const f32x4 (&acc)[2 * NA][2 * NB]) {
         if (K == kForward) {
             const int strip = m * 2 + wm;
             const int words = p.V - strip * kStrip - 4 * g;   // of the strip, from this lane's first one on
@@ -653,8 +387,8 @@ __global__ __launch_bounds__(256, 1) void loss_product_kernel(const LossArgs p)
                 }
             }
         }
-    }
-    wait_vmem();   // (no load to LDS outlives the workgroup)
+    };
+    product_tiles<A_COLS, B_COLS, NA, NB, K == kForward || K == kAgain, false>(lds, A, B, a_pitch, b_pitch, begin, end, stride, open, tile_begin, tile_end);
 }
 
 // X: the rows that have a target, in order, then zeros to a whole tile; and what else the products need of them.  A workgroup has `each` rows; how many

@@ -1,4 +1,4 @@
-"""The operators that a block is made of (attention to a window, the residual stream) without a GPU: symbols, struct layouts and what the
+"""The operators that a block is made of (attention to a window, the residual stream, products) without a GPU: symbols, struct layouts and what the
 entry points refuse."""
 import ctypes
 import math
@@ -13,12 +13,12 @@ from paper_2505_19609_amd import binding as B
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 ONE = 1 << 20   # an address that is aligned and never read: the call fails first
-HEADERS = ("skrull_window.h", "skrull_residual.h")
+HEADERS = ("skrull_window.h", "skrull_residual.h", "skrull_linear.h")
 
 
 def test_library_exports_every_declared_operator():
     header = "".join(open(os.path.join(ROOT, "include", f)).read() for f in HEADERS)
-    declared = set(re.findall(r"\b(skrull_(?:window|residual)(?:_[a-z]+)*)\s*\(", header))
+    declared = set(re.findall(r"\b(skrull_(?:window|residual|linear)(?:_[a-z]+)*)\s*\(", header))
     assert declared == set(B.BLOCK_SYMBOLS)
     for name in declared:
         assert getattr(B.lib(), name) is not None
@@ -33,6 +33,7 @@ def test_argument_counts_match_headers():
 
 
 def test_struct_layouts_match_headers():
+    assert ctypes.sizeof(B.Linear) == 8 + 4 * 4 + 4 * 8
     assert ctypes.sizeof(B.Window) == 2 * 4
     assert ctypes.sizeof(B.Residual) == 8 + 7 * 4 + 4 + 8 * 8   # (scale and its padding)
 
@@ -156,3 +157,82 @@ def test_window_wrappers_refuse():
         B._heads(plan, (torch.zeros(4, 4, 64, dtype=torch.bfloat16)[:, ::2],))
     with pytest.raises(B.SkrullError, match="lse"):
         B._lse(plan, lse.t())
+
+
+# ---- products -------------------------------------------------------------------------------------------------------
+
+def _linear(**kw):
+    p = dict(rows=16, inputs=64, outputs=128, activation=B.LINEAR_NONE, gated=0, x_stride=64, residual_stride=128, y_stride=128, dy_stride=128)
+    p.update(kw)
+    return B.Linear(**p)
+
+
+def _linear_fwd(p, workspace_bytes=1 << 30, **kw):
+    a = dict(x=ONE, w=2 * ONE, b=3 * ONE, residual=4 * ONE, y=5 * ONE, z=6 * ONE, workspace=40 * ONE)
+    a.update(kw)
+    return B.lib().skrull_linear_fwd(ctypes.byref(p), *a.values(), workspace_bytes, None)
+
+
+def _linear_bwd(p, workspace_bytes=1 << 30, **kw):
+    a = dict(x=ONE, w=2 * ONE, z=3 * ONE, dy=4 * ONE, dx=5 * ONE, dw=6 * ONE, db=7 * ONE, workspace=40 * ONE)
+    a.update(kw)
+    return B.lib().skrull_linear_bwd(ctypes.byref(p), *a.values(), workspace_bytes, None)
+
+
+BAD_LINEAR = [dict(rows=-1), dict(rows=(1 << 24) + 1), dict(inputs=0), dict(inputs=60), dict(inputs=65544, x_stride=65544), dict(outputs=4), dict(outputs=132), dict(outputs=1 << 17),
+              dict(activation=4), dict(activation=-1), dict(gated=2), dict(gated=1, outputs=32768, inputs=32768, x_stride=32768, y_stride=32768, dy_stride=32768, residual_stride=32768),
+              dict(x_stride=56), dict(x_stride=68), dict(x_stride=(1 << 20) + 8)]
+
+
+@pytest.mark.parametrize("kw", BAD_LINEAR + [dict(y_stride=120), dict(y_stride=132), dict(residual_stride=64)])
+def test_linear_fwd_refuses(kw):
+    assert _linear_fwd(_linear(**kw)) == B.SKRULL_EINVAL
+    assert "linear" in B.skrull_attn_strerror(B.SKRULL_EINVAL)
+
+
+@pytest.mark.parametrize("kw", BAD_LINEAR + [dict(dy_stride=120), dict(dy_stride=129)])
+def test_linear_bwd_refuses(kw):
+    assert _linear_bwd(_linear(**kw)) == B.SKRULL_EINVAL
+    assert "linear" in B.skrull_attn_strerror(B.SKRULL_EINVAL)
+
+
+@pytest.mark.parametrize("kw", [dict(x=None), dict(w=None), dict(y=None), dict(x=ONE + 2), dict(w=2 * ONE + 8), dict(b=3 * ONE + 2), dict(residual=4 * ONE + 8), dict(y=5 * ONE + 4), dict(z=6 * ONE + 2),
+                                dict(y=ONE), dict(y=2 * ONE + 16), dict(y=4 * ONE + 16), dict(z=5 * ONE), dict(z=4 * ONE), dict(y=3 * ONE)])
+def test_linear_fwd_refuses_pointers(kw):
+    assert _linear_fwd(_linear(), **kw) == B.SKRULL_EINVAL
+
+
+@pytest.mark.parametrize("kw", [dict(x=None), dict(w=None), dict(dy=None), dict(dx=5 * ONE + 8), dict(dw=6 * ONE + 2), dict(db=7 * ONE + 4), dict(workspace=None), dict(workspace=40 * ONE + 8),
+                                dict(workspace_bytes=16), dict(dx=ONE), dict(dw=2 * ONE), dict(dx=4 * ONE), dict(dw=5 * ONE + 16), dict(db=6 * ONE), dict(dw=40 * ONE)])
+def test_linear_bwd_refuses_pointers(kw):
+    assert _linear_bwd(_linear(), **kw) == B.SKRULL_EINVAL
+
+
+def test_linear_backward_of_an_activation_needs_z():
+    assert _linear_bwd(_linear(activation=B.LINEAR_SILU), z=None) == _linear_bwd(_linear(gated=1), z=None) == B.SKRULL_EINVAL
+
+
+def test_linear_workspace():
+    size = lambda backward, **kw: B.lib().skrull_linear_workspace(ctypes.byref(_linear(**kw)), backward)  # noqa: E731
+    assert size(0, inputs=4) == size(1, activation=9) == -1
+    assert size(0, rows=0) == 0 and size(1, rows=0) >= 0
+    big = dict(rows=32768, inputs=4096, outputs=4096)
+    assert size(0, **big) == 0                                                     # (a tile for every compute unit)
+    assert size(1, activation=B.LINEAR_GELU, **big) >= 32768 * 4096 * 2            # dz
+    assert size(1, **big) < 64 << 20
+
+
+def test_linear_wrappers_refuse():
+    x, w = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(128, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="activation"):
+        A.skrull_linear(x, w, activation="tanh")
+    with pytest.raises(ValueError, match="rows, inputs"):
+        A.skrull_linear(x[0], w)
+    with pytest.raises(B.SkrullError, match="weight"):
+        B._linear_of(x, w[:, :32], 0, False)
+    with pytest.raises(B.SkrullError, match="gated"):
+        B._linear_of(x, w[:127], 0, True)
+    with pytest.raises(B.SkrullError, match="y must be"):
+        B._linear_of(x, w, 0, True, y=torch.zeros(4, 128, dtype=torch.bfloat16))
+    with pytest.raises(B.SkrullError, match="current GPU"):
+        B.skrull_linear_fwd(x, w, None, None, x, None, None)
