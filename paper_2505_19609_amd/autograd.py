@@ -239,8 +239,12 @@ def _aligned(t):
 def skrull_window_attention(q, k, v, plan, window, sinks=0):
     """O = packed varlen causal attention of the micro-batch `plan` describes (a binding.Plan), where a query sees the last `window` keys up to its own and
     the first `sinks` ones of its sequence; differentiable with respect to q, k, v."""
-    _refuse_captured(q, k, v)
-    return _SkrullWindowAttention.apply(_aligned(q), _aligned(k), _aligned(v), plan, window, sinks)
+    module = _native_for(q, k, v) if type(plan) is B.Plan and type(window) is int and type(sinks) is int else None
+    o = module.window_attention(q, k, v, plan, window, sinks) if module is not None else None
+    if o is None:
+        _refuse_captured(q, k, v)
+        o = _SkrullWindowAttention.apply(_aligned(q), _aligned(k), _aligned(v), plan, window, sinks)
+    return o
 
 
 class _SkrullResidualNorm(torch.autograd.Function):
@@ -276,8 +280,12 @@ def skrull_residual_norm(r, z, weight, bias=None, post_weight=None, post_bias=No
     if r.dim() != 2 or z.dim() != 2:
         raise ValueError("r and z must be [rows, cols]")
     vectors = (weight, bias, post_weight, post_bias, gate)
-    _refuse_captured(r, z, *vectors)
-    return _SkrullResidualNorm.apply(_rows(r), _rows(z), *(None if t is None else t.contiguous() for t in vectors), float(scale), float(eps), _KINDS[kind])
+    module = _native_for(r, z, *vectors)
+    out = module.residual_norm(r, z, *vectors, scale, eps, _KINDS[kind]) if module is not None else None
+    if out is None:
+        _refuse_captured(r, z, *vectors)
+        out = _SkrullResidualNorm.apply(_rows(r), _rows(z), *(None if t is None else t.contiguous() for t in vectors), float(scale), float(eps), _KINDS[kind])
+    return out
 
 
 _ACTIVATIONS = {"none": B.LINEAR_NONE, "relu": B.LINEAR_RELU, "gelu": B.LINEAR_GELU, "silu": B.LINEAR_SILU}
@@ -323,9 +331,13 @@ def skrull_linear(x, weight, bias=None, residual=None, activation="none", gated=
         raise ValueError(f"activation must be one of {sorted(_ACTIVATIONS)}")
     if x.dim() != 2 or weight.dim() != 2:
         raise ValueError("x must be [rows, inputs] and weight [n, inputs]")
-    _refuse_captured(x, weight, bias, residual)
-    return _SkrullLinear.apply(_wide_rows(x), _aligned(weight), None if bias is None else _aligned(bias), None if residual is None else _wide_rows(residual),
-                               _ACTIVATIONS[activation], bool(gated))
+    module = _native_for(x, weight, bias, residual)
+    y = module.linear(x, weight, bias, residual, _ACTIVATIONS[activation], gated) if module is not None else None
+    if y is None:
+        _refuse_captured(x, weight, bias, residual)
+        y = _SkrullLinear.apply(_wide_rows(x), _aligned(weight), None if bias is None else _aligned(bias), None if residual is None else _wide_rows(residual),
+                                _ACTIVATIONS[activation], bool(gated))
+    return y
 
 
 class _SkrullCrossEntropy(torch.autograd.Function):

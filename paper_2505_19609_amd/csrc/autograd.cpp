@@ -16,12 +16,16 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
+#include <array>
 #include <memory>
 
 #include "skrull_attn.h"
+#include "skrull_linear.h"
 #include "skrull_loss.h"
 #include "skrull_norm.h"
+#include "skrull_residual.h"
 #include "skrull_rotary.h"
+#include "skrull_window.h"
 
 namespace {
 
@@ -163,6 +167,7 @@ struct PlanHolder : torch::CustomClassHolder {
 // Whether `t` is on the current GPU.
 bool here(const at::Tensor &t) { return t.is_cuda() && t.get_device() == c10::hip::current_device(); }
 bool is_bf16(const at::Tensor &t) { return t.scalar_type() == at::kBFloat16; }
+bool aligned16(const at::Tensor &t) { return (uintptr_t)t.data_ptr() % 16 == 0; }
 // The library's number of a type, -1 for one that it does not take.
 int type_of(const at::Tensor &t)
 {
@@ -354,6 +359,222 @@ struct Rotary : torch::autograd::Function<Rotary> {
     }
 };
 
+// ---- a block's other operators: nodes of their own too ----
+
+// A node of the graph that saves its inputs and what else a kind needs of the forward.
+template <class Kind, int INPUTS>
+struct BlockNode : torch::autograd::Node {
+    torch::autograd::SavedVariable saved[INPUTS];
+    torch::autograd::SavedVariable output;   // ... and what it gave
+    at::Tensor kept;                         // of the forward, for the backward alone
+    bool varies = false;
+    Kind kind;
+
+    explicit BlockNode(Kind k) : kind(std::move(k)) {}
+    void save(const std::array<at::Tensor, INPUTS> &inputs)
+    {
+        for (int i = 0; i < INPUTS; ++i) saved[i] = torch::autograd::SavedVariable(inputs[i], false);
+    }
+    variable_list apply(variable_list &&grads) override
+    {
+        std::lock_guard<std::mutex> lock(mutex_);
+        std::array<at::Tensor, INPUTS> inputs;
+        for (int i = 0; i < INPUTS; ++i) inputs[i] = saved[i].unpack();
+        if (std::none_of(grads.begin(), grads.end(), [](const at::Tensor &g) { return g.defined(); })) return variable_list(num_outputs());
+        return once(grads, kind.backward(*this, inputs, grads), varies);
+    }
+    void release_variables() override
+    {
+        std::lock_guard<std::mutex> lock(mutex_);
+        for (auto &s : saved) s.reset_data();
+        output.reset_data();
+        kept.reset();
+    }
+};
+template <class Kind, int INPUTS>
+std::shared_ptr<BlockNode<Kind, INPUTS>> block_node(Kind kind)
+{
+    return std::shared_ptr<BlockNode<Kind, INPUTS>>(new BlockNode<Kind, INPUTS>(std::move(kind)), torch::autograd::deleteNode);
+}
+
+struct ResidualNorm {
+    double eps;
+    float scale;
+    int64_t kind;
+    using Inputs = std::array<at::Tensor, 7>;   // r, z, weight, bias, post_weight, post_bias, gate
+    using Node = BlockNode<ResidualNorm, 7>;
+
+    skrull_residual_t sizes(const Inputs &t) const
+    {
+        skrull_residual_t p = {};
+        p.rows = t[1].size(0);
+        p.cols = (int32_t)t[1].size(1);
+        p.kind = (int32_t)kind;
+        p.type = type_of(t[1]);
+        p.residual_type = type_of(t[0]);
+        p.weight_type = type_of(t[2]);
+        p.eps = (float)eps;
+        p.scale = scale;
+        p.r_stride = row_stride(t[0]);
+        p.z_stride = row_stride(t[1]);
+        p.r_out_stride = p.y_stride = p.dr_stride = p.dz_stride = p.cols;
+        return p;
+    }
+    variable_list run(const Inputs &t, float *stats) const
+    {
+        variable_list out = {at::empty(t[0].sizes(), t[0].options()), at::empty(t[1].sizes(), t[1].options())};
+        const skrull_residual_t p = sizes(t);
+        check(skrull_residual_fwd(&p, t[0].data_ptr(), t[1].data_ptr(), t[2].data_ptr(), address(t[3]), address(t[4]), address(t[5]), address(t[6]), out[0].data_ptr(), out[1].data_ptr(),
+                                  stats, current_stream()));
+        return out;
+    }
+    variable_list forward(const Inputs &t) const
+    {
+        const auto node = block_node<ResidualNorm, 7>(*this);
+        node->set_next_edges(torch::autograd::collect_next_edges(t[0], t[1], t[2], t[3], t[4], t[5], t[6]));
+        node->kept = at::empty({4, t[1].size(0)}, t[1].options().dtype(at::kFloat));
+        variable_list out = run(t, (float *)node->kept.data_ptr());
+        node->save(t);
+        node->varies = true;
+        torch::autograd::set_history(out, node);
+        return out;
+    }
+    variable_list backward(Node &node, const Inputs &t, const variable_list &grads) const
+    {
+        const auto taken = [](const at::Tensor &g) { return !g.defined() || is_rows(g) ? g : g.contiguous(); };
+        const at::Tensor d_r = taken(grads[0]), dy = taken(grads[1]);
+        variable_list out(7);
+        out[0] = at::empty(t[0].sizes(), t[0].options());
+        out[1] = at::empty(t[1].sizes(), t[1].options());
+        bool vectors = false;
+        for (int i = 2; i < 7; ++i)
+            if (t[i].defined() && node.task_should_compute_output(i)) {
+                out[i] = at::empty_like(t[i]);
+                vectors = true;
+            }
+        skrull_residual_t p = sizes(t);
+        if (d_r.defined()) p.d_r_out_stride = row_stride(d_r);
+        if (dy.defined()) p.dy_stride = row_stride(dy);
+        const int64_t bytes = vectors ? skrull_residual_workspace(&p) : 0;
+        const at::Tensor ws = bytes ? bytes_like(t[1], bytes) : at::Tensor();
+        check(skrull_residual_bwd(&p, t[0].data_ptr(), t[1].data_ptr(), t[2].data_ptr(), address(t[4]), address(t[5]), address(t[6]), (const float *)node.kept.data_ptr(), address(d_r), address(dy),
+                                  out[0].data_ptr(), out[1].data_ptr(), address(out[2]), address(out[3]), address(out[4]), address(out[5]), address(out[6]), address(ws), (size_t)bytes,
+                                  current_stream()));
+        for (int i = 0; i < 2; ++i)
+            if (!node.task_should_compute_output(i)) out[i].reset();
+        return out;
+    }
+};
+
+struct WindowAttention {
+    std::shared_ptr<PlanObject> plan;
+    skrull_window_t window;
+    using Inputs = std::array<at::Tensor, 3>;   // q, k, v
+    using Node = BlockNode<WindowAttention, 3>;
+
+    static at::Tensor run(const skrull_attn_plan_t *handle, const skrull_window_t &window, const at::Tensor &q, const at::Tensor &k, const at::Tensor &v, const at::Tensor &lse)
+    {
+        at::Tensor o = at::empty_like(q);
+        check(skrull_window_fwd(handle, &window, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), (float *)lse.data_ptr(), current_stream()));
+        return o;
+    }
+    at::Tensor forward(const skrull_attn_plan_t *handle, const at::Tensor &q, const at::Tensor &k, const at::Tensor &v, const at::Tensor &lse) const
+    {
+        const auto node = block_node<WindowAttention, 3>(*this);
+        node->set_next_edges(torch::autograd::collect_next_edges(q, k, v));
+        at::Tensor o = run(handle, window, q, k, v, lse);
+        node->kept = lse;
+        node->save({q, k, v});
+        node->varies = true;
+        torch::autograd::set_history(o, node);
+        node->output = torch::autograd::SavedVariable(o, true);
+        return o;
+    }
+    variable_list backward(Node &node, const Inputs &t, const variable_list &grads) const
+    {
+        const skrull_attn_plan_t *handle;
+        {
+            const PyGILState_STATE gil = PyGILState_Ensure();
+            try {
+                handle = handle_of(plan->plan);
+            } catch (python_error &e) {
+                e.persist();
+                PyGILState_Release(gil);
+                throw;
+            }
+            PyGILState_Release(gil);
+        }
+        const at::Tensor o = node.output.unpack(node.getptr());
+        const int64_t bytes = skrull_window_workspace(handle, &window);
+        if (!bytes) check(SKRULL_EINVAL);
+        const at::Tensor d_o = grads[0].is_contiguous() && aligned16(grads[0]) ? grads[0] : grads[0].clone(at::MemoryFormat::Contiguous);
+        variable_list out = {at::empty_like(t[0]), at::empty_like(t[1]), at::empty_like(t[2])};
+        const at::Tensor ws = bytes_like(t[0], bytes);
+        check(skrull_window_bwd(handle, &window, t[0].data_ptr(), t[1].data_ptr(), t[2].data_ptr(), o.data_ptr(), (const float *)node.kept.data_ptr(), d_o.data_ptr(), out[0].data_ptr(),
+                                out[1].data_ptr(), out[2].data_ptr(), ws.data_ptr(), (size_t)bytes, current_stream()));
+        return out;
+    }
+};
+
+struct Linear {
+    int64_t activation;
+    bool gated;
+    using Inputs = std::array<at::Tensor, 2>;   // x, weight
+    using Node = BlockNode<Linear, 2>;
+
+    bool plain() const { return !gated && activation == SKRULL_LINEAR_NONE; }
+    int64_t outputs(const at::Tensor &w) const { return gated ? w.size(0) / 2 : w.size(0); }
+    skrull_linear_t sizes(const at::Tensor &x, const at::Tensor &w) const
+    {
+        const int64_t n = outputs(w);
+        return skrull_linear_t{x.size(0), (int32_t)x.size(1), (int32_t)n, (int32_t)activation, gated, row_stride(x), n, n, n};
+    }
+    // rows as the products take them
+    static bool fits(const at::Tensor &t)
+    {
+        return is_rows(t) && is_bf16(t) && here(t) && aligned16(t) && (t.size(0) < 2 || (t.stride(0) % 8 == 0 && t.stride(0) <= 1 << 20));
+    }
+    at::Tensor run(const at::Tensor &x, const at::Tensor &w, const at::Tensor &b, const at::Tensor &residual, const at::Tensor &z) const
+    {
+        skrull_linear_t p = sizes(x, w);
+        if (residual.defined()) p.residual_stride = row_stride(residual);
+        const int64_t bytes = skrull_linear_workspace(&p, 0);
+        if (bytes < 0) check(SKRULL_EINVAL);
+        at::Tensor y = at::empty({x.size(0), outputs(w)}, x.options());
+        const at::Tensor ws = bytes ? bytes_like(x, bytes) : at::Tensor();
+        check(skrull_linear_fwd(&p, x.data_ptr(), w.data_ptr(), address(b), address(residual), y.data_ptr(), address(z), address(ws), (size_t)bytes, current_stream()));
+        return y;
+    }
+    at::Tensor forward(const at::Tensor &x, const at::Tensor &w, const at::Tensor &b, const at::Tensor &residual) const
+    {
+        const auto node = block_node<Linear, 2>(*this);
+        node->set_next_edges(torch::autograd::collect_next_edges(x, w, b, residual));
+        if (!plain() && differentiable({&x, &w, &b})) node->kept = at::empty({x.size(0), w.size(0)}, x.options());
+        at::Tensor y = run(x, w, b, residual, node->kept);
+        node->save({x, w});
+        // (the residual's gradient alone is a constant, and so is the bias' of a product without an activation)
+        node->varies = differentiable({&x, &w}) || (b.defined() && b.requires_grad() && !plain());
+        torch::autograd::set_history(y, node);
+        return y;
+    }
+    variable_list backward(Node &node, const Inputs &t, const variable_list &grads) const
+    {
+        const at::Tensor &x = t[0], &w = t[1], dy = fits(grads[0]) ? grads[0] : grads[0].clone(at::MemoryFormat::Contiguous);
+        variable_list out(4);
+        if (node.task_should_compute_output(0)) out[0] = at::empty(x.sizes(), x.options());
+        if (node.task_should_compute_output(1)) out[1] = at::empty_like(w);
+        if (node.task_should_compute_output(2)) out[2] = at::empty({w.size(0)}, w.options());
+        if (node.task_should_compute_output(3)) out[3] = grads[0];
+        if (!out[0].defined() && !out[1].defined() && !out[2].defined()) return out;
+        skrull_linear_t p = sizes(x, w);
+        p.dy_stride = row_stride(dy);
+        const int64_t bytes = skrull_linear_workspace(&p, 1);
+        const at::Tensor ws = bytes_like(x, bytes);
+        check(skrull_linear_bwd(&p, x.data_ptr(), w.data_ptr(), address(node.kept), dy.data_ptr(), address(out[0]), address(out[1]), address(out[2]), ws.data_ptr(), (size_t)bytes, current_stream()));
+        return out;
+    }
+};
+
 // While a graph is captured, a backward pass that reaches a leaf through a node which an eager graph keeps alive waits for that node's own
 // stream, which is not captured: the process ends there.  So such a call is refused before it records anything.
 void refuse_captured(std::initializer_list<const at::Tensor *> inputs)
@@ -419,6 +640,117 @@ PyObject *cross_entropy(PyObject *, PyObject *const *args, Py_ssize_t n)
         }
     }
     return THPVariable_Wrap(std::move(loss));
+    END_HANDLE_TH_ERRORS
+}
+
+// A tensor argument, or an undefined one for None.
+bool tensor_or_none(PyObject *o, at::Tensor &t)
+{
+    if (o == Py_None) return true;
+    if (!THPVariable_Check(o)) return false;
+    t = THPVariable_Unpack(o);
+    return true;
+}
+PyObject *two(variable_list out)
+{
+    PyObject *both = PyTuple_New(2);
+    if (!both) throw python_error();
+    for (int i = 0; i < 2; ++i) PyTuple_SET_ITEM(both, i, THPVariable_Wrap(std::move(out[i])));
+    return both;
+}
+
+// residual_norm(r, z, weight, bias, post_weight, post_bias, gate, scale, eps, kind)
+PyObject *residual_norm(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    ResidualNorm::Inputs t;
+    TORCH_CHECK_TYPE(n == 10 && std::all_of(args, args + 3, [](PyObject *o) { return THPVariable_Check(o); }), "residual_norm(r, z, weight, bias, post_weight, post_bias, gate, scale, eps, kind)");
+    for (int i = 0; i < 7; ++i) TORCH_CHECK_TYPE(tensor_or_none(args[i], t[i]), "residual_norm: a tensor or None");
+    const double scale = PyFloat_AsDouble(args[7]), eps = PyFloat_AsDouble(args[8]);
+    const int64_t kind = PyLong_AsLongLong(args[9]);
+    if (PyErr_Occurred()) return nullptr;
+    const at::Tensor &r = t[0], &z = t[1];
+    if (!here(r) || !here(z) || !is_rows(r) || !is_rows(z) || r.sizes() != z.sizes() || z.size(1) > SKRULL_NORM_MAX_COLS || type_of(r) < 0 || type_of(z) < 0 || type_of(t[2]) < 0) Py_RETURN_NONE;
+    for (int i = 2; i < 7; ++i)
+        if (t[i].defined() && (!here(t[i]) || t[i].scalar_type() != t[2].scalar_type() || t[i].dim() != 1 || t[i].size(0) != z.size(1) || !t[i].is_contiguous())) Py_RETURN_NONE;
+    const ResidualNorm op = {eps, (float)scale, kind};
+    variable_list out;
+    {
+        pybind11::gil_scoped_release no_gil;
+        if (differentiable({&t[0], &t[1], &t[2], &t[3], &t[4], &t[5], &t[6]})) {
+            refuse_captured({&t[0], &t[1], &t[2], &t[3], &t[4], &t[5], &t[6]});
+            out = op.forward(t);
+        } else {
+            out = op.run(t, nullptr);
+        }
+    }
+    return two(std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+// window_attention(q, k, v, plan, window, sinks)
+PyObject *window_attention(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    TORCH_CHECK_TYPE(n == 6 && THPVariable_Check(args[0]) && THPVariable_Check(args[1]) && THPVariable_Check(args[2]), "window_attention(q, k, v, plan, window, sinks)");
+    const at::Tensor &q = SKRULL_TENSOR(0), &k = SKRULL_TENSOR(1), &v = SKRULL_TENSOR(2);
+    const int64_t window = PyLong_AsLongLong(args[4]), sinks = PyLong_AsLongLong(args[5]);
+    if (PyErr_Occurred()) {   // (no whole number, or one of more than 64 bits: the Function says so)
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    const skrull_attn_plan_t *handle = handle_of(args[3]);
+    skrull_attn_plan_info_t info;
+    if (skrull_attn_plan_info(handle, &info) != SKRULL_OK || window < INT32_MIN || window > INT32_MAX || sinks < INT32_MIN || sinks > INT32_MAX) Py_RETURN_NONE;
+    const int64_t q_shape[3] = {info.total_q, info.num_q_heads, info.head_dim}, k_shape[3] = {info.total_k, info.num_kv_heads, info.head_dim};
+    for (const at::Tensor *t : {&q, &k, &v})
+        if (!here(*t) || !is_bf16(*t) || !t->is_contiguous() || !aligned16(*t) || t->sizes() != at::IntArrayRef(t == &q ? q_shape : k_shape, 3)) Py_RETURN_NONE;
+    const skrull_window_t keys = {(int32_t)window, (int32_t)sinks};
+    at::Tensor o;
+    const bool kept = differentiable({&q, &k, &v});
+    const auto plan = kept ? std::make_shared<PlanObject>(args[3]) : nullptr;
+    {
+        pybind11::gil_scoped_release no_gil;
+        const at::Tensor lse = at::empty({info.num_q_heads, info.total_q}, q.options().dtype(at::kFloat));
+        if (kept) {
+            refuse_captured({&q, &k, &v});
+            o = WindowAttention{plan, keys}.forward(handle, q, k, v, lse);
+        } else {
+            o = WindowAttention::run(handle, keys, q, k, v, lse);
+        }
+    }
+    return THPVariable_Wrap(std::move(o));
+    END_HANDLE_TH_ERRORS
+}
+
+// linear(x, weight, bias, residual, activation, gated)
+PyObject *linear(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    at::Tensor b, residual;
+    TORCH_CHECK_TYPE(n == 6 && THPVariable_Check(args[0]) && THPVariable_Check(args[1]) && tensor_or_none(args[2], b) && tensor_or_none(args[3], residual),
+                     "linear(x, weight, bias, residual, activation, gated)");
+    const at::Tensor &x = SKRULL_TENSOR(0), &w = SKRULL_TENSOR(1);
+    const int64_t activation = PyLong_AsLongLong(args[4]);
+    const int gated = PyObject_IsTrue(args[5]);
+    if (PyErr_Occurred()) return nullptr;
+    const Linear op = {activation, gated != 0};
+    const auto whole = [](const at::Tensor &t) { return here(t) && is_bf16(t) && t.is_contiguous() && aligned16(t); };
+    if (!Linear::fits(x) || !whole(w) || w.dim() != 2 || w.size(1) != x.size(1) || w.size(0) < 2 || w.size(0) > INT32_MAX || x.size(1) > INT32_MAX || (gated && w.size(0) % 2) ||
+        (b.defined() && (!whole(b) || b.dim() != 1 || b.size(0) != w.size(0))) ||
+        (residual.defined() && (!Linear::fits(residual) || residual.size(0) != x.size(0) || residual.size(1) != op.outputs(w))))
+        Py_RETURN_NONE;
+    at::Tensor y;
+    {
+        pybind11::gil_scoped_release no_gil;
+        if (differentiable({&x, &w, &b, &residual})) {
+            refuse_captured({&x, &w, &b, &residual});
+            y = op.forward(x, w, b, residual);
+        } else {
+            y = op.run(x, w, b, residual, at::Tensor());
+        }
+    }
+    return THPVariable_Wrap(std::move(y));
     END_HANDLE_TH_ERRORS
 }
 
@@ -511,6 +843,9 @@ PyMethodDef methods[] = {{"attention", (PyCFunction)(void (*)())attention, METH_
                          {"norm", (PyCFunction)(void (*)())norm, METH_FASTCALL, "the differentiable norm"},
                          {"cross_entropy", (PyCFunction)(void (*)())cross_entropy, METH_FASTCALL, "the differentiable loss"},
                          {"rotary", (PyCFunction)(void (*)())rotary, METH_FASTCALL, "the differentiable rotary positions"},
+                         {"residual_norm", (PyCFunction)(void (*)())residual_norm, METH_FASTCALL, "the differentiable residual stream"},
+                         {"window_attention", (PyCFunction)(void (*)())window_attention, METH_FASTCALL, "the differentiable attention to a window"},
+                         {"linear", (PyCFunction)(void (*)())linear, METH_FASTCALL, "the differentiable product"},
                          {"turn", (PyCFunction)(void (*)())turn, METH_FASTCALL, "binding.skrull_rotary"},
                          {"refuse_captured", (PyCFunction)(void (*)())refuse_captured_of, METH_FASTCALL, "refuses leaves that an eager graph has"},
                          {"set_check", set_check, METH_O, "the callable that raises what an error code stands for"},

@@ -219,3 +219,192 @@ def test_residual_gradient_against_differences():
     square = sum(g.double().square().sum().item() for g in grads)
     # (the gradients' own errors, some 2^-20 of them, and the differences' third derivatives and roundings)
     assert abs(slope - square) <= 1e-4 * square
+
+
+# ---- the wrappers, of all of a block's operators --------------------------------------------------------------------
+
+def _calls():
+    """Differentiable calls: (inputs, call)."""
+    from paper_2505_19609_amd import autograd as A
+    from paper_2505_19609_amd import binding as B
+    gen = _gen(71)
+    plan = B.skrull_attn_plan([700, 129, 640, 64], [1, 1, 2, 1], [0, 0, 1, 0], 4, 2, 64, 0.125, shard_cut=[0, 0, 1, 0])
+    q, k, v = _randn(gen, plan.total_q, 4, 64), _randn(gen, plan.total_k, 2, 64), _randn(gen, plan.total_k, 2, 64)
+    stream = _residual_inputs(gen, 50, 264, *[torch.bfloat16] * 3, 1, 1, 1, 1)
+    x, w, b, r = _randn(gen, 50, 264), _randn(gen, 128, 264, scale=0.1), _randn(gen, 128), _randn(gen, 50, 64)
+    return [((q, k, v), lambda q, k, v: A.skrull_window_attention(q, k, v, plan, 90, 5)),
+            (stream, lambda *t: A.skrull_residual_norm(*t, 1.5, 1e-4)),
+            ([t.float() for t in stream[:3]], lambda r, z, w: A.skrull_residual_norm(r, z, w, kind="rms")),
+            ((x, w, b, r), lambda x, w, b, r: A.skrull_linear(x, w, b, r, "gelu", True)),
+            ((x, w), lambda x, w: A.skrull_linear(x, w)),
+            ((x, w, b), lambda x, w, b: A.skrull_linear(x, w, b, None, "silu"))]
+
+
+CALLS = range(6)
+
+
+def _tuple(out):
+    return out if isinstance(out, tuple) else (out,)
+
+
+@pytest.mark.parametrize("i", CALLS)
+def test_native_calls_and_functions_give_the_same_bits(monkeypatch, i):
+    from paper_2505_19609_amd import autograd as A
+    inputs, call = _calls()[i]
+    results = []
+    for watched in (False, True):
+        monkeypatch.setattr(A, "_watched", lambda: watched)
+        given = [t.clone().requires_grad_() for t in inputs]
+        out = _tuple(call(*given))
+        gen = _gen(72)
+        d = [_randn(gen, *o.shape, dtype=o.dtype) for o in out]
+        results.append([o.detach() for o in out] + list(torch.autograd.grad(out, given, d)))
+        assert all(("Skrull" in type(o.grad_fn).__name__) == watched for o in out)
+        with torch.no_grad():   # (and what a call without gradients gives)
+            plain = _tuple(call(*inputs))
+        assert all(torch.equal(a, b) and a.grad_fn is None for a, b in zip(plain, results[-1]))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+@pytest.mark.parametrize("watched", [False, True])
+@pytest.mark.parametrize("i", CALLS)
+def test_gradients_are_not_differentiated_again(monkeypatch, i, watched):
+    from paper_2505_19609_amd import autograd as A
+    monkeypatch.setattr(A, "_watched", lambda: watched)
+    inputs, call = _calls()[i]
+    for varies in (True, False):
+        given = [t.clone().requires_grad_() for t in inputs]
+        out = _tuple(call(*given))
+        d = [torch.ones_like(o).requires_grad_(varies) for o in out]
+        grads = torch.autograd.grad(out, given, d, create_graph=True)
+        with pytest.raises(RuntimeError, match="differentiate"):
+            torch.autograd.grad(grads[0].float().sum(), d if varies else given)
+
+
+@pytest.mark.parametrize("watched", [False, True])
+@pytest.mark.parametrize("i", CALLS)
+def test_a_graph_is_freed_by_its_backward_pass_and_sees_changed_inputs(monkeypatch, i, watched):
+    from paper_2505_19609_amd import autograd as A
+    monkeypatch.setattr(A, "_watched", lambda: watched)
+    inputs, call = _calls()[i]
+
+    def outputs():
+        given = [t.clone().requires_grad_() for t in inputs]
+        out = _tuple(call(*given))
+        return given, out, [torch.ones_like(o) for o in out]
+
+    given, out, d = outputs()
+    first = torch.autograd.grad(out, given, d, retain_graph=True)
+    assert all(torch.equal(a, b) for a, b in zip(first, torch.autograd.grad(out, given, d)))
+    with pytest.raises(RuntimeError, match="second time"):
+        torch.autograd.grad(out, given, d)
+    given, out, d = outputs()
+    with torch.no_grad():
+        given[1].mul_(2)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        torch.autograd.grad(out, given, d)
+    given, out, d = outputs()
+    del given
+    out[0].sum().backward()      # (leaves that only the graph holds)
+
+
+@pytest.mark.parametrize("watched", [False, True])
+@pytest.mark.parametrize("i", CALLS)
+def test_a_captured_call_is_refused_while_an_eager_graph_has_its_leaves(monkeypatch, i, watched):
+    from paper_2505_19609_amd import autograd as A
+    inputs, call = _calls()[i]
+    given = [t.clone().requires_grad_() for t in inputs]
+    eager = call(*given)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    monkeypatch.setattr(A, "_watched", lambda: watched)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        given[0].detach().add(1)     # (something to capture)
+        with pytest.raises(ValueError, match="outside this capture"):
+            call(*given)
+        with torch.no_grad():
+            call(*given)             # (without gradients there is nothing to refuse)
+    torch.cuda.synchronize()
+    del eager
+
+
+@pytest.mark.parametrize("i", CALLS)
+def test_captured_training_calls(i):
+    """Forward and gradients through autograd, captured: replays give the eager bits, on new values too."""
+    inputs, call = _calls()[i]
+    given = [t.clone().requires_grad_() for t in inputs]
+    gen = _gen(73)
+
+    def step():
+        out = _tuple(call(*given))
+        return [o.detach() for o in out] + list(torch.autograd.grad(out, given, d))
+
+    with torch.no_grad():
+        d = [_randn(gen, *o.shape, dtype=o.dtype) for o in _tuple(call(*given))]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        captured = step()
+    for rep in range(3):
+        with torch.no_grad():
+            for t in given:
+                t.copy_(_randn(gen, *t.shape, dtype=t.dtype))
+        for t in captured:
+            t.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(captured, want)), rep
+
+
+@pytest.mark.parametrize("i", CALLS)
+def test_calls_on_other_streams(i):
+    """Three at a time, on streams of their own."""
+    inputs, call = _calls()[i]
+    given = [t.clone().requires_grad_() for t in inputs]
+
+    def step():
+        out = _tuple(call(*given))
+        return [o.detach() for o in out] + list(torch.autograd.grad(out, given, [torch.ones_like(o) for o in out]))
+    want = step()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    for _ in range(3):
+        runs = []
+        for st in streams:
+            with torch.cuda.stream(st):
+                runs.append(step())
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for r in runs for a, b in zip(r, want))
+
+
+def test_wrappers_refuse_alike():
+    """Calls that the native module hands back and the Functions refuse."""
+    from paper_2505_19609_amd import autograd as A
+    from paper_2505_19609_amd import binding as B
+    z = torch.zeros(4, 64, dtype=torch.bfloat16, device="cuda")
+    w = torch.zeros(64, dtype=torch.bfloat16, device="cuda")
+    plan = B.skrull_attn_plan([4], [1], [0], 2, 2, 64, 0.125)
+    q = torch.zeros(4, 2, 64, dtype=torch.bfloat16, device="cuda")
+    wide = torch.zeros(64, 64, dtype=torch.bfloat16, device="cuda")
+    for call in (lambda: A.skrull_residual_norm(z, z.float(), w), lambda: A.skrull_residual_norm(z, z, w.float(), w), lambda: A.skrull_residual_norm(z[:3], z, w),
+                 lambda: A.skrull_residual_norm(z, z, w, w, kind="rms"), lambda: A.skrull_residual_norm(z, z, w, post_bias=w), lambda: A.skrull_residual_norm(z, z, w, eps=-1.0),
+                 lambda: A.skrull_residual_norm(z, z, w, scale=math.nan), lambda: A.skrull_residual_norm(z.half(), z.half(), w),
+                 lambda: A.skrull_window_attention(q, q, q, plan, 0), lambda: A.skrull_window_attention(q, q, q, plan, 1, -1), lambda: A.skrull_window_attention(q, q, q[:3], plan, 1),
+                 lambda: A.skrull_window_attention(q, q, q.float(), plan, 1), lambda: A.skrull_window_attention(q, q, q, plan, 1 << 31), lambda: A.skrull_window_attention(q, q, q, plan, 1, 1 << 40),
+                 lambda: A.skrull_linear(z, wide[:, :60]), lambda: A.skrull_linear(z[:, :60], wide[:, :60].contiguous()), lambda: A.skrull_linear(z, wide[:60]),
+                 lambda: A.skrull_linear(z, wide, w[:32]), lambda: A.skrull_linear(z, wide, None, z[:, :32]), lambda: A.skrull_linear(z, wide[:33], gated=True), lambda: A.skrull_linear(z.float(), wide),
+                 lambda: A.skrull_linear(z, wide, w.float())):
+        with pytest.raises(B.SkrullError):
+            call()
+    assert A.skrull_window_attention(q, q, q, plan, 1).shape == q.shape
+    plan.destroy()
+    with pytest.raises(B.SkrullError):
+        A.skrull_window_attention(q, q, q, plan, 1)
