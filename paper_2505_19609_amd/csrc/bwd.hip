@@ -74,8 +74,28 @@ struct BwdParams {
     // stored, of each (item, KV head) or, for very many of these, of all of them; pieces of the sums of these that have been handed out
     int32_t *rows_ready, *parts_stored, *next_sum;
     int32_t n_parts;                  // work items that are parts of shared dK/dV items; 0: they are counted for each item
-    int32_t window, sinks;            // of the windowed kernels
+    // of the windowed kernels; far_rows: query rows of a piece of what sees the sinks from beyond their blocks' windows, 0: there are no such pieces (see FarSums)
+    int32_t window, sinks, far_rows, far_period;
+    float *far_dk, *far_dv;
 };
+
+// dK and dV of sinks (keys that all later queries see) would be one workgroup's chain over all queries of a sequence.  So the queries whose tiles lie behind the windows of a pass' keys
+// are taken in pieces of far_rows rows by workgroups of their own, in a launch before, which leave fp32 sums of the sinks' rows in slots of
+// their own; the pass adds them, in order, to its own.  (24,576 and 8,192 tokens, 32/8 heads of 128, window 4,096, 4 sinks: dK/dV 3.89 ms in one chain.)
+// A segment's slots begin where no other one's end: of two that have such queries, both at least far_period keys long, the second one's number is larger by one at least for the same
+// prefix (two chunks), by two for another, and a last piece that is not whole takes one more than its rows' share.
+struct FarSums {
+    int first, pieces, slot;   // the first row behind the pass' tiles; pieces from there on, the slot of the first one
+    template <typename P>
+    __device__ __forceinline__ void init(const P prm, int first_row, int rows, int qbase, int kbase, int late)
+    {
+        const int far_rows = prm->far_rows, k = first_row / far_rows;
+        first = first_row;
+        pieces = first_row < rows ? (rows - 1) / far_rows + 1 - k : 0;
+        slot = qbase / far_rows + 2 * (kbase / prm->far_period) + late + k;
+    }
+};
+int64_t far_slots(const skrull_attn_plan_t *p, int far_rows, int far_period) { return (int64_t)p->total_q / far_rows + 2 * ((int64_t)p->total_k / far_period) + 3; }
 
 // ---------------------------------------------------------------------------
 // dQ
@@ -411,15 +431,21 @@ __device__ __forceinline__ int dq_work(const int bid, RowBlocks &rb, DqFeed &fee
             f32x16 ds;
 #pragma unroll
             for (int v = 0; v < 16; ++v) ds[v] = fast_exp2(__builtin_fmaf(s_in[v], cs, -lse2)) * g_in[v];
-            if (j >= n_full || !walk.full(j)) {  // half tile touches the diagonal, or the window's start, for this wave
+            if (j >= n_full) {  // half tile touches the diagonal for this wave
                 // relative position from an opaque copy of the lane index: the sixteen
                 // per-register thresholds are formed here rather than kept for the whole kernel
                 int li = lane;
                 asm volatile("" : "+v"(li));
                 const int rel = p0 + wrow0 + (li & 31) - walk.half_key(j) - 4 * (li >> 5);  // my_pos - first key - 4h
-                const int sinks_rel = WINDOW ? walk.sinks - walk.half_key(j) - 4 * (li >> 5) : 0;
 #pragma unroll
-                for (int v = 0; v < 16; ++v) ds[v] = walk.hidden(8 * (v >> 2) + (v & 3), rel, sinks_rel) ? 0.0f : ds[v];
+                for (int v = 0; v < 16; ++v) ds[v] = (8 * (v >> 2) + (v & 3) > rel) ? 0.0f : ds[v];
+            }
+            if (!walk.full(j)) {  // ... or the window's start
+                int li = lane;
+                asm volatile("" : "+v"(li));
+                const int first = walk.half_key(j) + 4 * (li >> 5), rel = p0 + wrow0 + (li & 31) - first;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) ds[v] = walk.hidden(8 * (v >> 2) + (v & 3), rel, first) ? 0.0f : ds[v];
             }
             SB();
 #pragma unroll
@@ -461,14 +487,24 @@ __device__ __forceinline__ int dq_work(const int bid, RowBlocks &rb, DqFeed &fee
             // such a reader of its result (12 for these on gfx950; s_nop n is n + 1 of them): they are here.  (Without
             // them the first scores were read before they were written where a wavefront had its SIMD to itself.)
             asm volatile("s_nop 11" : "+v"(s), "+v"(g));
-            if (__builtin_expect(j >= n_full || !walk.full(j), 0)) {  // half tile touches the diagonal, or the window's start, for this wave
+            if (__builtin_expect(j >= n_full, 0)) {  // half tile touches the diagonal for this wave
                 int li = lane;
                 asm volatile("" : "+v"(li));
                 const int rel = p0 + wrow0 + (li & 31) - walk.half_key(j) - 4 * (li >> 5);  // my_pos - first key - 4h
-                const int sinks_rel = WINDOW ? walk.sinks - walk.half_key(j) - 4 * (li >> 5) : 0;
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
-                    const bool hidden = walk.hidden(8 * (v >> 2) + (v & 3), rel, sinks_rel);
+                    const bool late = 8 * (v >> 2) + (v & 3) > rel;
+                    s[v] = late ? -INFINITY : s[v];
+                    g[v] = late ? 0.0f : g[v];
+                }
+            }
+            if (__builtin_expect(!walk.full(j), 0)) {  // ... or the window's start
+                int li = lane;
+                asm volatile("" : "+v"(li));
+                const int first = walk.half_key(j) + 4 * (li >> 5), rel = p0 + wrow0 + (li & 31) - first;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const bool hidden = walk.hidden(8 * (v >> 2) + (v & 3), rel, first);
                     s[v] = hidden ? -INFINITY : s[v];
                     g[v] = hidden ? 0.0f : g[v];
                 }
@@ -712,6 +748,8 @@ struct KeyBlock {
     int part_row;                  // first row of the pass in a part's partial sums
     int qb, ql, kvl, kbase, qbase; // the (late) segment: position of its first query, rows, keys, packed rows
     int qb_e, ql_e, qbase_e;       // the early chunk that shares the prefix and sees the block (ql_e = 0: none)
+    int late;                      // whether the segment is the second of two that share the prefix
+    int far_begin, far_end, slot;  // a piece of FarSums: its rows of the segment, its slot
 };
 template <typename P>
 __device__ __forceinline__ KeyBlock key_block(const P prm, int SUB, int bid)
@@ -778,6 +816,47 @@ __device__ __forceinline__ KeyBlock key_block(const P prm, int SUB, int bid)
     r.item_rows = r.part < r.parts ? min(BN, r.kvl - block * BN) - sub * SUB : 0;
     r.part_row = prm->keys.part_rows ? item * BN + sub * SUB : r.kbase + r.kv0;
     if (!shares || r.kv0 >= kvl_e) r.ql_e = 0;
+    r.late = shares;
+    return r;
+}
+
+// The last position that sees a key of a pass of `rows` keys from kv0 on through a window, and how many of a segment's tiles hold such rows, from its row i_first on.
+__device__ __forceinline__ int window_end(int kv0, int rows, int window) { return kv0 + rows - 1 + window - 1; }
+__device__ __forceinline__ int first_tile_row(int kv0, int qb) { return max(0, kv0 - qb) / TILE_ROWS * TILE_ROWS; }
+__device__ __forceinline__ int window_tiles(int i_first, int qb, int ql, int q_last) { return max(0, min(ql, q_last - qb + 1) - i_first + TILE_ROWS - 1) / TILE_ROWS; }
+
+// Work item `bid` of the launch for FarSums: a piece of a segment's queries (by the forward's items), a pass over keys that begins with sinks, a KV head; without rows where there is
+// nothing to do.
+template <typename P>
+__device__ __forceinline__ KeyBlock far_block(const P prm, int SUB, int bid)
+{
+    KeyBlock r{};
+    const int BN = prm->keys.BN, passes = prm->keys.passes, Hkv = prm->Hkv, sinks = prm->sinks;
+    const int per_item = Hkv * passes * ((sinks + BN - 1) / BN);
+    const int item = __builtin_amdgcn_readfirstlane(bid / per_item), x = bid - item * per_item, pass = __builtin_amdgcn_readfirstlane(x / Hkv);
+    r.c = x - pass * Hkv;
+    const i32x4 it = plan_value((const i32x4 *)prm->fwd_items, item);
+    const int seq = it.x, row0 = it.y * prm->rows.BM, block = __builtin_amdgcn_readfirstlane(pass / passes), sub = pass - block * passes;
+    r.qb = plan_value(prm->q_begin, seq);
+    r.ql = plan_value(prm->q_len, seq);
+    r.kvl = plan_value(prm->kv_len, seq);
+    r.kbase = plan_value(prm->cu_k, seq);
+    r.qbase = plan_value(prm->cu_q, seq);
+    r.late = plan_value(prm->shares_kv, seq);
+    r.kv0 = block * BN + sub * SUB;
+    const int rows = min(SUB, min(BN, r.kvl - block * BN) - sub * SUB), i_first = first_tile_row(r.kv0, r.qb);
+    FarSums far;
+    far.init(prm, i_first + window_tiles(i_first, r.qb, r.ql, window_end(r.kv0, rows, prm->window)) * TILE_ROWS, r.ql, r.qbase, r.kbase, r.late);
+    r.far_begin = max(far.first, row0);
+    r.far_end = min(r.ql, row0 + prm->far_rows);
+    r.slot = far.slot + row0 / prm->far_rows - far.first / prm->far_rows;
+    r.part = 0;
+    r.parts = 1;
+    r.g = prm->keys.g;
+    r.head_lo = r.c * r.g;
+    r.piece = 0;
+    r.pieces = 1;
+    r.item_rows = rows > 0 && row0 % prm->far_rows == 0 && r.far_begin < r.far_end ? min(rows, sinks - r.kv0) : 0;
     return r;
 }
 
@@ -798,7 +877,8 @@ struct DkvLds {
 // ONE: in one launch with dQ.  `rows_seen`: this workgroup has waited for the rows of dQ's items.  `part_owed`: the part of a shared item
 // (KeyBlock::shared) that it did last, stored but not counted yet, or 0; on return this item's.  WINDOW: a row sees the `window` last keys and the
 // `sinks` first ones.
-template <int D, int PAIRS, bool ONE, bool WINDOW>
+// FAR: a piece of FarSums.
+template <int D, int PAIRS, bool ONE, bool WINDOW, bool FAR = false>
 __device__ __forceinline__ int dkv_work(const int bid, KeyBlock &kb, DkvFeed &feed, unsigned char *ring, unsigned char *exchange, bool &rows_seen, int &part_owed)
 {
     const kernarg_t<BwdParams> prm = kernarg<BwdParams>();
@@ -853,22 +933,30 @@ __device__ __forceinline__ int dkv_work(const int bid, KeyBlock &kb, DkvFeed &fe
     // Query tiles that can see key kv0, numbered 0 .. n_qt-1 in position order: those of
     // the early chunk (segment seq-1, when this prefix is shared by two chunks and the
     // pass starts inside the early chunk's own prefix) and then those of segment seq.
-    // With a window only those that see one of its keys, of which there may be none; a key below `sinks` all later ones see.
-    const int window = WINDOW ? prm->window : 0, sinks = WINDOW ? prm->sinks : 0;
-    const int q_last = WINDOW && kv0 >= sinks ? kv0 + krows - 1 + window - 1 : 1 << 30;  // last position that sees a key of the pass
-    const int i_first = (max(0, kv0 - qb) / QT) * QT;
-    const int n_qt_own = WINDOW ? max(0, min(ql, q_last - qb + 1) - i_first + QT - 1) / QT : (ql - i_first + QT - 1) / QT;
+    // With a window only those that see one of its keys, of which there may be none; a key below `sinks` all later ones see, here or in FarSums.
+    const int window = WINDOW ? prm->window : 0, sinks = WINDOW ? prm->sinks : 0, far_rows = WINDOW && !FAR ? prm->far_rows : 0;
+    const int q_last = WINDOW && (kv0 >= sinks || far_rows) ? window_end(kv0, krows, window) : 1 << 30;
+    const int i_first = FAR ? kb.far_begin : first_tile_row(kv0, qb);
+    const int n_qt_own = FAR ? (kb.far_end - i_first + QT - 1) / QT : WINDOW ? window_tiles(i_first, qb, ql, q_last) : (ql - i_first + QT - 1) / QT;
     const int qb_e = kb.qb_e, ql_e = kb.ql_e, qbase_e = kb.qbase_e;
-    const int i_first_e = (max(0, kv0 - qb_e) / QT) * QT;
-    const int n_qt_e = WINDOW   ? max(0, min(ql_e, q_last - qb_e + 1) - i_first_e + QT - 1) / QT
-                       : ql_e > 0 ? (ql_e - i_first_e + QT - 1) / QT : 0;
+    const int i_first_e = first_tile_row(kv0, qb_e);
+    const int n_qt_e = WINDOW ? window_tiles(i_first_e, qb_e, ql_e, q_last) : ql_e > 0 ? (ql_e - i_first_e + QT - 1) / QT : 0;
     const int n_qt = n_qt_e + n_qt_own;
     // (head, query tile) pairs of the walk described below: this part takes n_iter of them from r0 on
     const bool all = kb.pieces == 1;
     const int r0 = all ? 0 : __builtin_amdgcn_readfirstlane(kb.piece * (n_qt * g) / kb.pieces);
     const int n_iter = (all ? n_qt * g : __builtin_amdgcn_readfirstlane((kb.piece + 1) * (n_qt * g) / kb.pieces)) - r0;
     const int first_up = r0 == 0 ? 0 : __builtin_amdgcn_readfirstlane(r0 / g);
-    const int head0 = r0 - first_up * g, tile0 = n_qt - 1 - first_up;
+    // With a wide window the walk of a part of it is turned: it begins at the tile whose number in the segment is the last of those with one quotient by n_qt, goes down
+    // to the lowest one and on from the highest.  The items that run together on a die are of neighbouring key blocks, whose tiles, mostly the same ones, each would otherwise
+    // come to two tiles after the one before, when its L2, 4 MB, no longer has them.  (24,576 tokens, 32/8 heads of 128, window 4,096: dK/dV 3.08 ms and 2.91 turned; narrower windows only
+    // get the dead rounds.)
+    const bool turned = WINDOW && !FAR && (kv0 >= sinks || far_rows) && n_qt_e == 0 && n_qt * g * D > (4 << 20) / (4 * QT);
+    int top = n_qt - 1;
+    if (WINDOW && __builtin_expect(turned, 0)) top -= __builtin_amdgcn_readfirstlane(i_first / QT % n_qt);
+    int tile0 = top - first_up;
+    if (WINDOW && tile0 < 0) tile0 += n_qt;
+    const int head0 = r0 - first_up * g;
     // tile t -> first global position of its segment, rows of the segment, first row of the tile
     auto tile_qb = [&](int t) __attribute__((always_inline)) { return t < n_qt_e ? qb_e : qb; };
     auto tile_ql = [&](int t) __attribute__((always_inline)) { return t < n_qt_e ? ql_e : ql; };
@@ -941,7 +1029,9 @@ __device__ __forceinline__ int dkv_work(const int bid, KeyBlock &kb, DkvFeed &fe
             while (dead_tiles < n_qt && !tile_live(dead_tiles)) ++dead_tiles;
         }
         n_live = max(0, min(n_iter, (n_qt - dead_tiles) * g - r0));
-        if (WINDOW && wj0 >= sinks) {
+        if (turned) {  // (dead rounds would be in the middle: they are done, all masked)
+            n_live = n_iter;
+        } else if (WINDOW && wj0 >= sinks) {
             const int last = wj0 + 31 + window - 1;  // last position that sees a key of the pair
             auto below = [&](int qb_s, int i_s, int count) { return max(0, min(count, (last - qb_s - i_s + QT) / QT)); };  // of `count` tiles from i_s on, those that begin at or before it
             const int own = last < qb + i_first ? 0 : below(qb, i_first, n_qt_own), early = last < qb_e + i_first_e ? 0 : below(qb_e, i_first_e, n_qt_e);
@@ -951,6 +1041,7 @@ __device__ __forceinline__ int dkv_work(const int bid, KeyBlock &kb, DkvFeed &fe
     }
     int nh = head0 + 1, nq = tile0, cq = tile0, slot = 0;  // cq: tile of this round; (nh, nq): head, tile of the next
     if (nh == g) { nh = 0; --nq; }
+    if (WINDOW && nq < 0) nq = n_qt - 1;
     // start of a round: fetch the next round's tile; end: wait, barrier, advance
     auto round_begin = [&](int T) __attribute__((always_inline)) {
         if (T + 1 < n_iter) fetch(nh, nq, slot == 2 ? 0 : slot + 1);
@@ -961,6 +1052,7 @@ __device__ __forceinline__ int dkv_work(const int bid, KeyBlock &kb, DkvFeed &fe
         slot = slot == 2 ? 0 : slot + 1;
         cq = nq;
         if (++nh == g) { nh = 0; --nq; }
+        if (WINDOW && nq < 0) nq = n_qt - 1;
     };
     int T = 0;
     if (WINDOW) {
@@ -977,11 +1069,14 @@ __device__ __forceinline__ int dkv_work(const int bid, KeyBlock &kb, DkvFeed &fe
             const unsigned char *cur = lds_ring[slot];
             const int i0 = tile_i0(cq);  // first query row of the tile inside its segment
             const int qb_t = tile_qb(cq), ql_t = tile_ql(cq);
+            const int window_from = WINDOW && !FAR ? (wj0 + 31 >= sinks ? wj0 + window - qb_t : 0x7fffffff) : 0;
             const unsigned char *tq = cur, *tdo = cur + TB;
             const float *t_lse = (const float *)(cur + 2 * TB);
             unsigned char *px = lds_p[pw][T & 1][0];
-            // masked pairs: key past the query (causal), query row past the end, or key in front of the query's window and no sink
-            const bool need_mask = (qb_t + i0 < wj0 + 31) || (i0 + QT > ql_t) || (WINDOW && wj0 + 31 >= sinks && qb_t + i0 + QT - 1 >= wj0 + window);
+            // masked pairs: key past the query (causal) or query row past the end
+            const bool need_mask = (qb_t + i0 < wj0 + 31) || (i0 + QT > ql_t);
+            // ... or key in front of the query's window and no sink: from the tile on that the first key's window ends in (FAR: what comes of a key that is no sink is not stored)
+            const bool past_window = WINDOW && !FAR && i0 + QT > window_from;
             // scores of masked pairs become -inf (probability 0) before the exponentials
             auto mask_block = [&](f32x16 &sb, int b) __attribute__((always_inline)) {
                 // (the asm also keeps this block behind its branch: turned into selects it
@@ -992,9 +1087,17 @@ __device__ __forceinline__ int dkv_work(const int bid, KeyBlock &kb, DkvFeed &fe
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
                     const int i = row0 + 8 * (v >> 2) + (v & 3);
-                    const int key = wj0 + (li & 31);
-                    sb[v] = (key > qb_t + i || i >= ql_t || (WINDOW && key >= sinks && key <= qb_t + i - window)) ? -INFINITY : sb[v];
+                    sb[v] = (wj0 + (li & 31) > qb_t + i || i >= ql_t) ? -INFINITY : sb[v];
                 }
+            };
+            auto mask_window = [&](f32x16 &sb, int b) __attribute__((always_inline)) {
+                int li = lane;
+                asm volatile("" : "+v"(li));
+                const int key = wj0 + (li & 31);
+                // the first row of the block that does not see this lane's key
+                const int end = key < sinks ? 0x7fffffff : key + window - qb_t - i0 - 32 * b - 4 * (li >> 5);
+#pragma unroll
+                for (int v = 0; v < 16; ++v) sb[v] = 8 * (v >> 2) + (v & 3) >= end ? -INFINITY : sb[v];
             };
             f32x16 s[2];
             bf16x8 fr[4];
@@ -1016,6 +1119,7 @@ __device__ __forceinline__ int dkv_work(const int bid, KeyBlock &kb, DkvFeed &fe
                 SB();
             }
             if (__builtin_expect(need_mask, 0)) mask_block(s[0], 0);
+            if (WINDOW && __builtin_expect(past_window, 0)) mask_window(s[0], 0);
             // S of the second 32 rows with the probabilities of the first behind its
             // MFMAs, then dV of the first with the probabilities of the second
             uint32_t w[2][8];
@@ -1044,6 +1148,7 @@ __device__ __forceinline__ int dkv_work(const int bid, KeyBlock &kb, DkvFeed &fe
                 SB();
             }
             if (__builtin_expect(need_mask, 0)) mask_block(s[1], 1);
+            if (WINDOW && __builtin_expect(past_window, 0)) mask_window(s[1], 1);
             const bf16x8 pb0 = as_bf16x8(make_uint4(w[0][0], w[0][1], w[0][2], w[0][3]));
             const bf16x8 pb1 = as_bf16x8(make_uint4(w[0][4], w[0][5], w[0][6], w[0][7]));
             // dV of rows 0..31 (2 x TT MFMAs); probabilities of rows 32..63 behind them
@@ -1234,6 +1339,33 @@ __device__ __forceinline__ int dkv_work(const int bid, KeyBlock &kb, DkvFeed &fe
     // first tile goes to slot 0, where nothing is staged)
     const kernarg_t<BwdParams> out = kernarg<BwdParams>();
     const int next = feed.take(), parts = kb.parts, part = kb.part, part_row = kb.part_row;
+    if (FAR) {
+        if (my_j < min(out->sinks, kvl) && wave_active)
+            store_rows_f32<TT>((role == 0 ? out->far_dv : out->far_dk) + (((size_t)kb.slot * out->Hkv + c) * out->sinks + my_j) * D, acc, h);
+        return next;
+    }
+    if (WINDOW && far_rows && wave_active && wj0 < out->sinks && part == 0) {
+#pragma unroll 1
+        for (int e = 0; e < 2; ++e) {  // the pieces of the segment, of the early chunk
+            if (e && ql_e == 0) break;
+            FarSums far;
+            far.init(out, e ? i_first_e + n_qt_e * QT : i_first + n_qt_own * QT, e ? ql_e : ql, e ? qbase_e : qbase, kbase, e ? 0 : kb.late);
+            if (my_j < min(out->sinks, kvl)) {
+                const size_t step = (size_t)out->Hkv * out->sinks * D;
+                const float *from = (role == 0 ? out->far_dv : out->far_dk) + (((size_t)far.slot * out->Hkv + c) * out->sinks + my_j) * D + 4 * h;
+#pragma unroll 1
+                for (int k = 0; k < far.pieces; ++k, from += step) {
+#pragma unroll
+                    for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+                        for (int vb = 0; vb < 4; ++vb) {
+                            const float4 f = *(const float4 *)(from + 32 * tt + 8 * vb);
+                            acc[tt][4 * vb] += f.x; acc[tt][4 * vb + 1] += f.y; acc[tt][4 * vb + 2] += f.z; acc[tt][4 * vb + 3] += f.w;
+                        }
+                }
+            }
+        }
+    }
     KeyBlock kb_next{};
     if (next >= 0) kb_next = key_block(out, SUB, next);  // (its loads are under way during the stores)
     if (wave_active) {
@@ -1304,6 +1436,20 @@ __global__ __launch_bounds__(128 * PAIRS, PAIRS == PAIRS_12W ? 3 : 2) void dkv_k
     __shared__ int work_slot[2];
     DkvFeed feed{{}, 0, 0, work_slot};
     dkv_loop<D, PAIRS, false, WINDOW>(feed, ring, exchange);
+}
+
+// The pieces of FarSums: a workgroup each.
+template <int D, int PAIRS>
+__global__ __launch_bounds__(128 * PAIRS, PAIRS == PAIRS_12W ? 3 : 2) void dkv_far_kernel(const BwdParams prm)
+{
+    __shared__ __align__(16) unsigned char ring[DkvLds<D, PAIRS>::RING], exchange[DkvLds<D, PAIRS>::P];
+    __shared__ int work_slot[2];
+    DkvFeed feed{{}, 0, 0, work_slot};
+    KeyBlock kb = far_block(kernarg<BwdParams>(), 32 * PAIRS, (int)blockIdx.x);
+    if (kb.item_rows <= 0) return;  // (the whole workgroup agrees)
+    bool rows_seen = true;
+    int part_owed = 0;
+    dkv_work<D, PAIRS, false, true, true>((int)blockIdx.x, kb, feed, ring, exchange, rows_seen, part_owed);
 }
 
 // Sums of the partial gradients of the items that several workgroups shared, rounded once (the same as
@@ -1396,7 +1542,7 @@ __device__ __forceinline__ void sums_loop(int *slot)
 // for at the end, the sums cost as much as in a launch of their own: 209 us where this takes 196.)  dQ workgroups have as many wavefronts as those of dK/dV here, 8 or 12, and
 // leave some without work where the plan's units are smaller.  Launches of many units of 4 stay two: three such workgroups share a
 // compute unit there (slices of three long sequences, 14/2 heads of 64: 4.68 ms, in one launch 5.1).
-template <int D, int PAIRS>
+template <int D, int PAIRS, bool WINDOW = false>
 __global__ __launch_bounds__(128 * PAIRS, PAIRS == PAIRS_12W ? 3 : 2) void bwd_kernel(const BwdParams prm)
 {
     constexpr int NW = 2 * PAIRS;
@@ -1410,11 +1556,11 @@ __global__ __launch_bounds__(128 * PAIRS, PAIRS == PAIRS_12W ? 3 : 2) void bwd_k
     if (prm.clear && blockIdx.x == 0) clear_state(prm.clear, SKRULL_BWD_STATE_INTS);
     {
         DqFeed feed{{}, 0, 0, work_slot};
-        dq_loop<D, NW, PIPED, true>(feed, lds);
+        dq_loop<D, NW, PIPED, true, WINDOW>(feed, lds);
     }
     {
         DkvFeed feed{{}, 0, 0, work_slot};
-        dkv_loop<D, PAIRS, true>(feed, lds, D == 64 ? apart : lds + Dkv::RING);
+        dkv_loop<D, PAIRS, true, WINDOW>(feed, lds, D == 64 ? apart : lds + Dkv::RING);
     }
     if (kernarg<BwdParams>()->keys.n_split > 0) sums_loop<D, PAIRS>(work_slot);
 }
@@ -1456,6 +1602,37 @@ __global__ __launch_bounds__(256) void dkv_reduce_kernel(const BwdParams prm)
 }
 
 int dkv_pairs(const skrull_attn_plan_t *p) { return (p->d == 64 && p->BN == 32 * PAIRS_12W) ? PAIRS_12W : PAIRS_8W; }
+
+KeyMap map_dkv(const skrull_attn_plan_t *p)
+{
+    const int SUB = 32 * dkv_pairs(p), passes = (p->BN + SUB - 1) / SUB;
+    return KeyMap{p->BN, p->Hq / p->Hkv, passes, p->Hkv, p->n_split, p->n_whole_first, p->split_parts, p->split_chain,
+                  p->split_compact ? p->n_split * p->BN : 0, inverse_of(passes), inverse_of(p->Hkv), p->dkv_units,
+                  inverse_of(passes * p->Hkv)};
+}
+
+// The pieces of FarSums of a plan: about 32 rounds of a workgroup each.  There are none where the chain of the longest sequence's sinks, in rounds (a tile of queries of a head), is
+// at most half an even share of all rounds, or hardly longer than others, or where there are more than 128 sinks, whose passes are many enough.
+struct FarRows {
+    int32_t rows = 0, period = 1;
+    FarRows(const skrull_attn_plan_t *p, const KeyWindow *window)
+    {
+        if (!window || window->sinks == 0 || window->sinks > 128) return;
+        const int SUB = 32 * dkv_pairs(p), g = p->Hq / p->Hkv;
+        period = (p->BN < SUB ? p->BN : SUB) + window->keys;
+        const int64_t threads = blocks(p, window) * 64 * 2 * dkv_pairs(p);
+        const int64_t queries = p->longest_seq < p->total_q ? p->longest_seq : p->total_q, in_window = (int64_t)p->total_q * window->keys;
+        const int64_t chain = queries / TILE_ROWS * g, others = period / TILE_ROWS * g;
+        const int64_t all = (p->pairs < in_window ? p->pairs : in_window) / (TILE_ROWS * 32 * dkv_pairs(p)) * p->Hq;   // (at most)
+        if (p->longest_seq >= period && chain >= others + 32 && 2 * 256 * chain > all && threads < (int64_t)1 << 32) rows = 256 * ((8 + g - 1) / g);
+    }
+    // work items: the forward's, each for all KV heads and passes that have sinks
+    static int64_t blocks(const skrull_attn_plan_t *p, const KeyWindow *window)
+    {
+        return (int64_t)p->n_fwd * p->Hkv * map_dkv(p).passes * ((window->sinks + p->BN - 1) / p->BN);
+    }
+    int64_t floats(const skrull_attn_plan_t *p, const KeyWindow *window) const { return far_slots(p, rows, period) * p->Hkv * window->sinks * p->d; }
+};
 
 template <bool WINDOW = false>
 RowLaunch rows_dq_alone(const skrull_attn_plan_t *p)
@@ -1536,6 +1713,16 @@ hipError_t launch_pair(const skrull_attn_plan_t *p, BwdParams prm, int threads_q
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (ev) (void)hipEventRecord(ev[1], st);
+    if (prm.far_rows) {
+        BwdParams far = prm;
+        far.queue_dkv = nullptr;
+        const KeyWindow window = {prm.window, prm.sinks};
+        const int64_t blocks = FarRows::blocks(p, &window);
+        if (D == 64 && threads_kv == 128 * PAIRS_12W) dkv_far_kernel<64, PAIRS_12W><<<(unsigned)blocks, threads_kv, 0, st>>>(far);
+        else dkv_far_kernel<D, PAIRS_8W><<<(unsigned)blocks, threads_kv, 0, st>>>(far);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
     KernelKV<<<launch_size<KernelKV>(threads_kv, prm.n_work_dkv, queued_kv), threads_kv, 0, st>>>(prm);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -1548,12 +1735,12 @@ hipError_t launch_pair(const skrull_attn_plan_t *p, BwdParams prm, int threads_q
     return e;
 }
 
-template <int D, int PAIRS>
-hipError_t launch_one(const skrull_attn_plan_t *p, const BwdParams &prm, hipStream_t st)
+template <int D, int PAIRS, bool WINDOW>
+hipError_t launch_one(const BwdParams &prm, hipStream_t st)
 {
     const int64_t work = (int64_t)prm.n_work_dq + prm.n_work_dkv;
-    const int resident = resident_of<bwd_kernel<D, PAIRS>>(128 * PAIRS);
-    bwd_kernel<D, PAIRS><<<(int)(work < resident ? work : resident), 128 * PAIRS, 0, st>>>(prm);
+    const int resident = resident_of<bwd_kernel<D, PAIRS, WINDOW>>(128 * PAIRS);
+    bwd_kernel<D, PAIRS, WINDOW><<<(int)(work < resident ? work : resident), 128 * PAIRS, 0, st>>>(prm);
     return hipGetLastError();
 }
 // dQ, dK/dV and sums as separate launches.
@@ -1578,29 +1765,33 @@ hipError_t launch_apart(const skrull_attn_plan_t *p, const BwdParams &prm, hipSt
 template <int D>
 hipError_t launch_d(const skrull_attn_plan_t *p, const BwdParams &prm, bool one, bool window, hipStream_t st, hipEvent_t *ev)
 {
-    if (window) return launch_apart<D, true>(p, prm, st, ev);
-    if (!one) return launch_apart<D, false>(p, prm, st, ev);
+    if (!one) return window ? launch_apart<D, true>(p, prm, st, ev) : launch_apart<D, false>(p, prm, st, ev);
     if constexpr (D == 64)
-        if (dkv_pairs(p) == PAIRS_12W) return launch_one<D, PAIRS_12W>(p, prm, st);
-    return launch_one<D, PAIRS_8W>(p, prm, st);
+        if (dkv_pairs(p) == PAIRS_12W) return window ? launch_one<D, PAIRS_12W, true>(prm, st) : launch_one<D, PAIRS_12W, false>(prm, st);
+    return window ? launch_one<D, PAIRS_8W, true>(prm, st) : launch_one<D, PAIRS_8W, false>(prm, st);
 }
 
 }  // namespace
 
 int grid_dq(const skrull_attn_plan_t *p) { return rows_dq_alone(p).n_work; }
 
-static KeyMap map_dkv(const skrull_attn_plan_t *p)
-{
-    const int SUB = 32 * dkv_pairs(p), passes = (p->BN + SUB - 1) / SUB;
-    return KeyMap{p->BN, p->Hq / p->Hkv, passes, p->Hkv, p->n_split, p->n_whole_first, p->split_parts, p->split_chain,
-                  p->split_compact ? p->n_split * p->BN : 0, inverse_of(passes), inverse_of(p->Hkv), p->dkv_units,
-                  inverse_of(passes * p->Hkv)};
-}
-
 int grid_dkv(const skrull_attn_plan_t *p)
 {
     const int n = p->dkv_units ? p->n_dkv_units : p->n_dkv + p->n_split * (p->split_parts - 1);
     return n * p->Hkv * map_dkv(p).passes;
+}
+
+// Bytes before the sums of FarSums: what calls without a window ask for.
+static int64_t plain_workspace(const skrull_attn_plan_t *p)
+{
+    skrull_attn_plan_info_t info;
+    (void)skrull_attn_plan_info(p, &info);
+    return (info.bwd_workspace_bytes + 15) & ~(int64_t)15;
+}
+int64_t window_workspace(const skrull_attn_plan_t *p, const KeyWindow *window)
+{
+    const FarRows far(p, window);
+    return plain_workspace(p) + (far.rows ? 2 * 4 * far.floats(p, window) : 0);
 }
 
 hipError_t launch_bwd(const skrull_attn_plan_t *p, const void *q, const void *k, const void *v,
@@ -1610,6 +1801,14 @@ hipError_t launch_bwd(const skrull_attn_plan_t *p, const void *q, const void *k,
     BwdParams prm;
     prm.window = window ? window->keys : 0;
     prm.sinks = window ? window->sinks : 0;
+    const FarRows far_rows(p, window);
+    prm.far_rows = far_rows.rows;
+    prm.far_period = far_rows.period;
+    prm.far_dk = prm.far_dv = nullptr;
+    if (far_rows.rows) {  // behind the workspace of calls without a window
+        prm.far_dk = (float *)((char *)delta + plain_workspace(p));
+        prm.far_dv = prm.far_dk + far_rows.floats(p, window);
+    }
     prm.trace_dq = trace;
     DefaultStream &own = *p->default_stream;
     std::unique_lock<std::mutex> held(own.lock);
@@ -1617,8 +1816,8 @@ hipError_t launch_bwd(const skrull_attn_plan_t *p, const void *q, const void *k,
     // Events are to time dQ and dK/dV by themselves.  Calls without a set of the plan's have the 256 bytes in the workspace alone for what
     // workgroups share, two lines, and workgroups that wait would poll the line of dQ's queues: replayed from a graph, 838 tokens in 10
     // sequences, 32/8 heads of 128, 39 us as three launches, 74 in one; 17,205 in 62, 8/4 heads, 204 and 295.
-    const bool one = in_turn && !ev && !window && is_one(p);
-    const RowLaunch rows_q = window ? rows_dq_alone<true>(p) : one ? rows_dq_first(p) : rows_dq_alone(p);
+    const bool one = in_turn && !ev && !far_rows.rows && is_one(p);
+    const RowLaunch rows_q = one ? rows_dq_first(p) : window ? rows_dq_alone<true>(p) : rows_dq_alone(p);
     in_turn = in_turn && (one || rows_q.queued || (window ? dkv_queued<true>(p) : dkv_queued(p)));  // (two plain grids share nothing)
     if (!in_turn) held.unlock();
     prm.trace_dkv = trace ? trace + grid_dq(p) : nullptr;  // (one launch has as many dQ items or fewer)

@@ -217,6 +217,7 @@ hipError_t launch_fwd(const skrull_attn_plan_t *p, const void *q, const void *k,
 hipError_t launch_bwd(const skrull_attn_plan_t *p, const void *q, const void *k, const void *v,
                       const void *o, const float *lse, const void *d_o, void *dq, void *dk,
                       void *dv, float *delta, hipStream_t st, hipEvent_t *ev, WgTrace *trace, const KeyWindow *window = nullptr);
+int64_t window_workspace(const skrull_attn_plan_t *p, const KeyWindow *window);  // bytes of a backward's
 int grid_fwd(const skrull_attn_plan_t *p);
 int grid_dq(const skrull_attn_plan_t *p);
 int grid_dkv(const skrull_attn_plan_t *p);

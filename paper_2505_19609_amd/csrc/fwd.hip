@@ -330,15 +330,21 @@ __device__ __forceinline__ int fwd_work(const int bid, RowBlocks &rb, FwdFeed &f
             p_out[0] = p_out[1] = as_bf16x8(z4);
         } else if (j >= 0 && j <= L) {  // softmax(j)
             f32x16 s = s_in;
-            if (j >= n_full || !walk.full(j)) {  // half tile touches the diagonal, or the window's start, for this wave
+            if (j >= n_full) {  // half tile touches the diagonal for this wave
                 // relative position from an opaque copy of the lane index: the sixteen
                 // per-register thresholds are formed here rather than kept for the whole kernel
                 int li = lane;
                 asm volatile("" : "+v"(li));
                 const int rel = p0 + wrow0 + (li & 31) - walk.half_key(j) - 4 * (li >> 5);  // this lane's query position - first key - 4h
-                const int sinks_rel = WINDOW ? walk.sinks - walk.half_key(j) - 4 * (li >> 5) : 0;
 #pragma unroll
-                for (int v = 0; v < 16; ++v) s[v] = walk.hidden(8 * (v >> 2) + (v & 3), rel, sinks_rel) ? -INFINITY : s[v];
+                for (int v = 0; v < 16; ++v) s[v] = (8 * (v >> 2) + (v & 3) > rel) ? -INFINITY : s[v];
+            }
+            if (!walk.full(j)) {  // ... or the window's start
+                int li = lane;
+                asm volatile("" : "+v"(li));
+                const int first = walk.half_key(j) + 4 * (li >> 5), rel = p0 + wrow0 + (li & 31) - first;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) s[v] = walk.hidden(8 * (v >> 2) + (v & 3), rel, first) ? -INFINITY : s[v];
             }
             const float m_new = row_max(s);
             const float shift = WINDOW && m_new == -INFINITY ? 0.0f : m_new;  // (a row that has seen no key yet: exponentials of 0)

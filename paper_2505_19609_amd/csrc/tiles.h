@@ -170,7 +170,11 @@ struct RowBlocks {
     __device__ __forceinline__ int lowest(int waves) const
     {
         int w = waves - 1;
-        while (w > 0 && !has(w)) --w;
+        if (step == 1) {
+            w = max(0, min(w, end - 1 - first));
+        } else {
+            while (w > 0 && !has(w)) --w;
+        }
         return block(w);
     }
     __device__ __forceinline__ int block(int wave) const { return nblk - 1 - quotient(first + wave * step, inv_g); }
@@ -277,8 +281,8 @@ struct KeyWalk {
     __device__ __forceinline__ bool full(int j) const { return !WINDOW || j < full_sinks || j >= full_from; }
     // the first period (half tiles 2 t - 1 and 2 t) that is full on both sides of the window, without what the sinks alone make full
     __device__ __forceinline__ int first_full_period() const { return WINDOW ? max(1, (full_from + 2) / 2) : 1; }
-    // whether the key c behind `rel` places before a row is hidden: behind it, or in front of its window and no sink (its sinks end at `sinks_rel`)
-    __device__ __forceinline__ bool hidden(int c, int rel, int sinks_rel) const { return c > rel || (WINDOW && c <= rel - window && c >= sinks_rel); }
+    // whether the key `first` + c is in front of the window of a row `rel` places behind `first`, and no sink
+    __device__ __forceinline__ bool hidden(int c, int rel, int first) const { return WINDOW && c <= rel - window && c >= sinks - first; }
 };
 
 // ---------------------------------------------------------------------------

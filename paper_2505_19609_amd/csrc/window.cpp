@@ -32,12 +32,17 @@ int check(const skrull_attn_plan_t *plan, const skrull_window_t *window)
     return SKRULL_OK;
 }
 
-// (positions are below 2^26, so that no sum of a position and one of these passes 32 bits)
-KeyWindow keys_of(const skrull_window_t *w)
-{
-    const int32_t most = 1 << 30;
-    return KeyWindow{w->window < most ? w->window : most, w->sinks < most ? w->sinks : most};
-}
+// What a launch needs to know.  Where every key is visible, nothing: those of the plain attention do the same with less.
+struct Keys {
+    KeyWindow window;
+    bool all;
+    // (positions are below 2^26, so that no sum of a position and one of these passes 32 bits)
+    Keys(const skrull_attn_plan_t *plan, const skrull_window_t *w)
+        : window{w->window < 1 << 30 ? w->window : 1 << 30, w->sinks < 1 << 30 ? w->sinks : 1 << 30}, all(w->window >= plan->longest_seq || w->sinks >= plan->longest_seq)
+    {
+    }
+    const KeyWindow *get() const { return all ? nullptr : &window; }
+};
 
 struct Sizes {
     int64_t q, k, lse;
@@ -59,8 +64,8 @@ int skrull_window_fwd(const skrull_attn_plan_t *plan, const skrull_window_t *win
     const Span in[] = {{"q", q, n.q}, {"k", k, n.k}, {"v", v, n.k}}, out[] = {{"o", o, n.q}, {"lse", lse, n.lse}};
     if (int rc = check_spans(in, 3, out, 2)) return rc;
     if (int rc = plan_on_current_device(plan)) return rc;
-    const KeyWindow keys = keys_of(window);
-    const hipError_t e = launch_fwd(plan, q, k, v, o, lse, (hipStream_t)hip_stream, nullptr, &keys);
+    const Keys keys(plan, window);
+    const hipError_t e = launch_fwd(plan, q, k, v, o, lse, (hipStream_t)hip_stream, nullptr, keys.get());
     return e == hipSuccess ? SKRULL_OK : launch_failed(e, "window launch");
 }
 
@@ -68,7 +73,8 @@ int64_t skrull_window_workspace(const skrull_attn_plan_t *plan, const skrull_win
 {
     skrull_attn_plan_info_t info;
     if (check(plan, window) != SKRULL_OK || skrull_attn_plan_info(plan, &info) != SKRULL_OK) return 0;
-    return info.bwd_workspace_bytes;
+    const Keys keys(plan, window);
+    return keys.all ? info.bwd_workspace_bytes : window_workspace(plan, &keys.window);
 }
 
 int skrull_window_bwd(const skrull_attn_plan_t *plan, const skrull_window_t *window, const void *q, const void *k, const void *v, const void *o,
@@ -83,8 +89,8 @@ int skrull_window_bwd(const skrull_attn_plan_t *plan, const skrull_window_t *win
     const Span out[] = {{"dq", dq, n.q}, {"dk", dk, n.k}, {"dv", dv, n.k}, {"workspace", workspace, bytes}};
     if (int rc = check_spans(in, 6, out, 4)) return rc;
     if (int rc = plan_on_current_device(plan)) return rc;
-    const KeyWindow keys = keys_of(window);
-    const hipError_t e = launch_bwd(plan, q, k, v, o, lse, d_o, dq, dk, dv, (float *)workspace, (hipStream_t)hip_stream, nullptr, nullptr, &keys);
+    const Keys keys(plan, window);
+    const hipError_t e = launch_bwd(plan, q, k, v, o, lse, d_o, dq, dk, dv, (float *)workspace, (hipStream_t)hip_stream, nullptr, nullptr, keys.get());
     return e == hipSuccess ? SKRULL_OK : launch_failed(e, "window launch");
 }
 

@@ -151,6 +151,26 @@ def test_window_with_other_blocks(shape, block_n, head_split):
     plan.destroy()
 
 
+@pytest.mark.parametrize("shape,heads,d", [(_whole(4200, 40, 3000, 300), (7, 1), 64), (_whole(2100, 700, 1900), (8, 1), 128), (([9000, 300, 6000], [4, 1, 2], [1, 0, 0], [1, 0, 1]), (4, 2), 64),
+                                           (([6000, 2500], [2, 3], [1, 2], [0, 1]), (8, 2), 128)])
+def test_window_sinks_of_long_sequences(shape, heads, d):
+    """Queries far behind the sinks' own windows, in several pieces of several sequences and chunks; the workspace between margins."""
+    from paper_2505_19609_amd import binding as B
+    from gpu_util import guarded, margins_intact
+    plan = _plan(shape, heads, d)
+    x = _inputs(plan, 17)
+    for window, sinks in ((100, 4), (300, 128), (64, 65), (20, 129), (1000, 1)):
+        buf, ws = guarded((B.skrull_window_workspace(plan, window, sinks),), torch.uint8, 0xFF)
+        o, lse = torch.empty_like(x["q"]), torch.empty(heads[0], plan.total_q, device="cuda")
+        B.skrull_window_fwd(plan, x["q"], x["k"], x["v"], o, lse, window, sinks)
+        dq, dk, dv = torch.full_like(o, float("nan")), *(torch.full_like(x["k"], float("nan")) for _ in range(2))
+        B.skrull_window_bwd(plan, x["q"], x["k"], x["v"], o, lse, x["do"], dq, dk, dv, ws, window, sinks)
+        assert margins_intact(buf)
+        _check({"o": o, "lse": lse, "dq": dq, "dk": dk, "dv": dv}, _reference(shape, x["q"], x["k"], x["v"], x["do"], d ** -0.5, window, sinks), (window, sinks))
+        torch.cuda.empty_cache()
+    plan.destroy()
+
+
 def test_window_workgroups_of_twelve():
     """A micro-batch of short sequences at head_dim 64, for which the plan takes workgroups of 12 wavefronts."""
     shape = _whole(*[200 + 37 * i % 300 for i in range(64)])
