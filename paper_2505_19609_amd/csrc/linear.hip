@@ -107,7 +107,9 @@ __global__ __launch_bounds__(256, 1) void linear_product_kernel(const LinearArgs
 {
     constexpr bool A_COLS = K != kForward, B_COLS = K == kDw;
     constexpr int kCols = GATED ? 32 * NA : 64 * NA, kRows = 64 * NB;   // of the result, of a tile
-    __shared__ __align__(1024) unsigned char lds[2 * kProductBytes<NA, NB>];
+    // (a step of a small tile is short beside the latency of its loads, which run four steps ahead there: 64 x 64, 15 steps, 13.9 us with two and 9 with four)
+    constexpr int kBuffers = NB == 4 ? 2 : 4;
+    __shared__ __align__(1024) unsigned char lds[kBuffers * kProductBytes<NA, NB>];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1;
     const int n = lane & 15, g = lane >> 4;
     const uint32_t a_pitch = (uint32_t)p.a_stride * 2, b_pitch = (uint32_t)p.b_stride * 2;
@@ -229,7 +231,7 @@ __global__ __launch_bounds__(256, 1) void linear_product_kernel(const LinearArgs
             }
         }
     };
-    product_tiles<A_COLS, B_COLS, NA, NB, !A_COLS, !B_COLS>(lds, A, B, a_pitch, b_pitch, begin, end, stride, open, tile_begin, tile_end, GATED ? p.J : 16 * NA);
+    product_tiles<A_COLS, B_COLS, NA, NB, !A_COLS, !B_COLS, kBuffers>(lds, A, B, a_pitch, b_pitch, begin, end, stride, open, tile_begin, tile_end, GATED ? p.J : 16 * NA);
 }
 
 // The parts' sums and what follows them: four columns to a thread.
@@ -406,24 +408,43 @@ struct Shape {
     int na, nb, splits, steps;
 };
 int tiles_of(int64_t n, int size) { return (int)((n + size - 1) / size); }
-// Tiles of 256 x 256, of 64 rows where there are 64 or fewer; of 64 x 64 (both operands in rows) where even so few compute units would have one.  The contraction is cut where half of
-// the compute units and more would have no tile, into parts of 4 steps or more.
+// Which tiles, and in how many parts the contraction: what a launch is expected to take, in us, from what tiles of each shape took (37 to 4,096 rows, 896 to 4,096 inputs and
+// outputs):
+//   tile (columns x rows)   workgroups at once   a step                 a tile's start and end
+//   256 x 256               256                  1.2 to 1.65 (power)    9
+//   256 x 64                256                  0.6                    5
+//   64 x 64 (forward)       512                  0.32, two on a unit 0.44   3
+// and parts, whose sums are written, read and added by a launch of its own, 4 and their bytes at 3 MB a us.  In us, this choice against 256 x 256 in parts where there were few
+// (which the forward had 64 x 64 for):
+//   rows, inputs, outputs   forward      dX           dW
+//   37, 896, 1,152          8.8   9.5    10.3  11.8   9.2
+//   1,001, 904, 1,160       12.0  12.1   17.0  24.5   24.4
+//   932, 896, 3,584         15.5  30.7   24.4  29.8   26.4  30.8
+//   4,096, 1,024, 1,024     17.3  33.8   16.9  33.7   31.5  33.7
+//   500, 4,096, 4,096       33.6  35.5   35.5  38.6   22.4
 Shape shape_of(Kind kind, int64_t I, int64_t J, int64_t C, bool gated)
 {
-    const int cols = gated ? kTile / 2 : kTile, steps = tiles_of(C, kStep);
-    Shape s = {4, 4, 1, steps};
-    if (kind != kDw && I <= 64) s.nb = 1;
-    if (kind == kForward && !gated && tiles_of(I, 64) * tiles_of(J, cols) <= kGrid / 2) s = {1, 1, 1, steps};
-    const int tiles = tiles_of(I, 64 * s.nb) * tiles_of(J, s.na == 1 ? 64 : cols);   // (none of no rows)
-    if (tiles > 0 && 2 * tiles <= kGrid) {
-        int parts = kGrid / tiles;
-        if (parts > steps / 4) parts = steps / 4;
-        if (parts > 1) {
-            s.steps = (steps + parts - 1) / parts;
-            s.splits = (steps + s.steps - 1) / s.steps;
+    struct Tile { int na, nb, at_once; double step, shared_step, ends; };
+    static const Tile tiles[] = {{4, 4, kGrid, 1.3, 1.3, 9.0}, {4, 1, kGrid, 0.6, 0.6, 5.0}, {1, 1, 2 * kGrid, 0.32, 0.44, 3.0}};
+    const int steps = tiles_of(C, kStep);
+    Shape best = {4, 4, 1, steps};
+    double least = 0.0;
+    for (const Tile &t : tiles) {
+        if ((kind == kDw && t.nb != 4) || (t.na == 1 && (kind != kForward || gated))) continue;
+        const int64_t n = (int64_t)tiles_of(I, 64 * t.nb) * tiles_of(J, (gated ? 32 : 64) * t.na);   // (none of no rows)
+        for (int parts = 1; parts <= 16 && parts <= steps; ++parts) {
+            const int each = (steps + parts - 1) / parts, real = (steps + each - 1) / each;
+            const double sums = real > 1 ? 4.0 * (gated ? 2 : 1) * (double)real * (double)I * (double)J : 0.0;
+            if (real < parts || sums > (double)(128 << 20)) continue;
+            const double rounds = (double)((n * real + t.at_once - 1) / t.at_once), step = n * real > kGrid ? t.shared_step : t.step;
+            const double us = rounds * (each * step + t.ends) + (real > 1 ? 4.0 + sums / 3e6 : 0.0);
+            if (least == 0.0 || us < least) {
+                least = us;
+                best = {t.na, t.nb, real, each};
+            }
         }
     }
-    return s;
+    return best;
 }
 int64_t slab_bytes(const Shape &s, int64_t I, int64_t width) { return s.splits > 1 ? (int64_t)s.splits * I * width * 4 : 0; }
 
