@@ -85,7 +85,9 @@ struct LinearArgs {
     int32_t a_stride, b_stride;  // elements between their rows
     int32_t I, J, C;             // rows and columns of the result (gated: of y); the contraction
     int32_t splits, steps;       // parts of the contraction, steps of a part
-    float *slabs;                // with more than one part: [parts][I][J, gated 2 J]
+    // The last `tail` tiles, fewer than there are workgroups after whole rounds of the others, have theirs in parts of tail_steps steps each
+    int32_t tail, tail_parts, tail_steps;
+    float *slabs;                // with more than one part: [parts][I][J, gated 2 J]; of a tail [tail][tail_parts][tile's rows][its columns, gated of both halves]
     // the result, and of the forward what else it is made of
     uint16_t *out, *z;           // z [I][J, gated 2 J] or null
     const uint16_t *bias, *residual;
@@ -118,24 +120,43 @@ __global__ __launch_bounds__(256, 1) void linear_product_kernel(const LinearArgs
     A.init(lane, wave, wm, a_pitch, GATED ? 16 * NA : 32 * NA);
     B.init(lane, wave, wn, b_pitch);
 
-    const int mt = (p.J + kCols - 1) / kCols, nt = (p.I + kRows - 1) / kRows, all_steps = (p.C + kStep - 1) / kStep, total = mt * nt * p.splits;
-    const int die = blockIdx.x & 7, per_die = (total + 7) / 8, stride = gridDim.x >> 3;
-    const int begin = die * per_die + (blockIdx.x >> 3), end = min(total, (die + 1) * per_die);
-    // Tiles in the order of work: blocks of 8 tiles of columns, through all rows; neighbours in it run at the same time on one die and share their operands in its L2.
-    auto locate = [&](int i, int &m, int &nn, int &s) {
-        s = i / (mt * nt);
-        i -= s * (mt * nt);
-        const int block = i / (8 * nt), r = i - block * (8 * nt), width = min(8, mt - block * 8);
-        nn = r / width;
-        m = block * 8 + r - nn * width;
-        for (int *f : {&m, &nn, &s}) *f = __builtin_amdgcn_readfirstlane(*f);
+    const int mt = (p.J + kCols - 1) / kCols, nt = (p.I + kRows - 1) / kRows, all_steps = (p.C + kStep - 1) / kStep, whole = mt * nt * p.splits - p.tail, parts = p.tail * p.tail_parts;
+    // A die has a piece of the whole tiles, then one of the tail's parts, its workgroups take them by turns.
+    const int die = blockIdx.x & 7, first = blockIdx.x >> 3, stride = gridDim.x >> 3, per_die = (whole + 7) / 8, parts_per_die = (parts + 7) / 8;
+    auto count = [&](int n, int each) { return max(0, min(n - die * each, each) - first + stride - 1) / stride; };
+    const int n_whole = count(whole, per_die), n_items = n_whole + count(parts, parts_per_die);
+    // Item i of this workgroup: its tile, its part of the contraction, where that begins and how many steps it has.  Tiles in the order of work: blocks of 8 tiles of columns,
+    // through all rows; neighbours in it run at the same time on one die and share their operands in its L2.
+    struct Item { int m, nn, s, from, steps, tail; };   // tail: of its tile among the tail's, -1: whole, or a part of all tiles' parts
+    auto locate = [&](int i) {
+        Item t;
+        int tile;
+        if (i < n_whole) {
+            tile = die * per_die + first + i * stride;
+            t.s = tile / (mt * nt);
+            tile -= t.s * (mt * nt);
+            t.tail = -1;
+            t.from = t.s * p.steps;
+            t.steps = max(0, min(p.steps, all_steps - t.from));
+        } else {
+            const int k = die * parts_per_die + first + (i - n_whole) * stride;
+            t.tail = k / p.tail_parts;
+            t.s = k - t.tail * p.tail_parts;
+            tile = whole + t.tail;
+            t.from = t.s * p.tail_steps;
+            t.steps = max(0, min(p.tail_steps, all_steps - t.from));
+        }
+        const int block = tile / (8 * nt), r = tile - block * (8 * nt), width = min(8, mt - block * 8);
+        t.nn = r / width;
+        t.m = block * 8 + r - t.nn * width;
+        for (int *f : {&t.m, &t.nn, &t.s, &t.from, &t.steps, &t.tail}) *f = __builtin_amdgcn_readfirstlane(*f);
+        return t;
     };
-    auto steps_of = [&](int s) { return max(0, min(p.steps, all_steps - s * p.steps)); };
-    auto open = [&](int tile, Source &a, Source &b, int &left, int &a_tail, int &b_tail) {
-        int m, nn, s;
-        locate(tile, m, nn, s);
-        left = steps_of(s);
-        const int64_t k0 = (int64_t)s * p.steps * kStep;
+    auto open = [&](int i, Source &a, Source &b, int &left, int &a_tail, int &b_tail) {
+        const Item t = locate(i);
+        const int m = t.m, nn = t.nn;
+        left = t.steps;
+        const int64_t k0 = (int64_t)t.from * kStep;
         a_tail = b_tail = (int)(p.C - k0);
         const int64_t ap = a_pitch, bp = b_pitch;
         // (to the end of the matrix' last row: what is behind it reads as zero)
@@ -146,20 +167,32 @@ __global__ __launch_bounds__(256, 1) void linear_product_kernel(const LinearArgs
         a = Source{(const unsigned char *)p.a + a_at, a_end - a_at, a_pitch, A_COLS ? kStep * ap : kStep * 2};
         b = Source{(const unsigned char *)p.b + b_at, b_end - b_at, b_pitch, B_COLS ? kStep * bp : kStep * 2};
     };
-    int m = 0, nn = 0, s = 0;
+    Item t = {};
     auto tile_begin = [&](int i) {
-        locate(i, m, nn, s);
-        return steps_of(s);
+        t = locate(i);
+        return t.steps;
     };
     auto tile_end = [&](const f32x4 (&acc)[2 * NA][2 * NB]) {
         constexpr int XS = GATED ? NA : 2 * NA;   // blocks of 16 columns of a wavefront
-        const int col0 = m * kCols + wm * (kCols / 2), row0 = nn * kRows + wn * 32 * NB + n;
+        const int col0 = t.m * kCols + wm * (kCols / 2), row0 = t.nn * kRows + wn * 32 * NB + n;
+        if (t.tail >= 0) {
+            float *to = p.slabs + ((int64_t)t.tail * p.tail_parts + t.s) * (kRows * 64 * NA) + (wn * 32 * NB + n) * (64 * NA) + wm * (kCols / 2) + 4 * g;
+#pragma unroll
+            for (int y = 0; y < 2 * NB; ++y)
+#pragma unroll
+                for (int x = 0; x < 2 * NA; ++x) {
+                    SB();
+                    *(float4 *)(to + 16 * y * (64 * NA) + 16 * (x % XS) + (x >= XS ? kCols : 0)) =
+                        make_float4(result(acc[x][y][0]), result(acc[x][y][1]), result(acc[x][y][2]), result(acc[x][y][3]));
+                }
+            return;
+        }
         if (p.splits > 1) {
             const int width = GATED ? 2 * p.J : p.J;
 #pragma unroll
             for (int y = 0; y < 2 * NB; ++y) {
                 const int row = row0 + 16 * y;
-                float *to = p.slabs + ((int64_t)s * p.I + row) * width + col0 + 4 * g;
+                float *to = p.slabs + ((int64_t)t.s * p.I + row) * width + col0 + 4 * g;
 #pragma unroll
                 for (int x = 0; x < 2 * NA; ++x) {
                     SB();
@@ -231,9 +264,49 @@ __global__ __launch_bounds__(256, 1) void linear_product_kernel(const LinearArgs
             }
         }
     };
-    product_tiles<A_COLS, B_COLS, NA, NB, !A_COLS, !B_COLS, kBuffers>(lds, A, B, a_pitch, b_pitch, begin, end, stride, open, tile_begin, tile_end, GATED ? p.J : 16 * NA);
+    product_tiles<A_COLS, B_COLS, NA, NB, !A_COLS, !B_COLS, kBuffers>(lds, A, B, a_pitch, b_pitch, 0, n_items, 1, open, tile_begin, tile_end, GATED ? p.J : 16 * NA);
 }
 
+// What follows the sum f of row `row` and columns c .. c + 3 (gated: of both halves).
+template <int ACT, bool GATED>
+__device__ __forceinline__ void finish(const LinearArgs &p, int64_t row, int c, float f[GATED ? 2 : 1][4])
+{
+    const int width = GATED ? 2 * p.J : p.J;
+#pragma unroll
+    for (int half = 0; half < (GATED ? 2 : 1); ++half) {
+        if (p.bias) {
+            float b[4];
+            wide4(*(const uint2 *)(p.bias + half * p.J + c), b);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) f[half][v] += b[v];
+        }
+        if (p.z) *(uint2 *)(p.z + row * width + half * p.J + c) = make_uint2(pack_bf16(f[half][0], f[half][1]), pack_bf16(f[half][2], f[half][3]));
+    }
+    float r[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (p.residual) wide4(*(const uint2 *)(p.residual + row * p.residual_stride + c), r);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+        f[0][v] = activation<ACT>(f[0][v]);
+        if (ACT == SKRULL_LINEAR_NONE && p.relu) f[0][v] = fmaxf(f[0][v], 0.0f);
+        if constexpr (GATED) f[0][v] *= f[1][v];
+        f[0][v] += r[v];
+    }
+    *(uint2 *)(p.out + row * p.out_stride + c) = make_uint2(pack_bf16(f[0][0], f[0][1]), pack_bf16(f[0][2], f[0][3]));
+}
+// The sum of four values of `parts` slabs, in their order.
+__device__ __forceinline__ void sum_parts(const float *from, int64_t slab, int parts, float f[4])
+{
+    float4 t = *(const float4 *)from;
+    for (int k = 1; k < parts; k += 8) {
+        float4 u[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u[j] = *(const float4 *)(from + min(k + j, parts - 1) * slab);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (k + j < parts) { t.x += u[j].x; t.y += u[j].y; t.z += u[j].z; t.w += u[j].w; }
+    }
+    f[0] = t.x; f[1] = t.y; f[2] = t.z; f[3] = t.w;
+}
 // The parts' sums and what follows them: four columns to a thread.
 template <int ACT, bool GATED>
 __global__ __launch_bounds__(256) void linear_sums_kernel(const LinearArgs p)
@@ -245,37 +318,26 @@ __global__ __launch_bounds__(256) void linear_sums_kernel(const LinearArgs p)
         const int c = (int)(i - row * groups) * 4;
         float f[GATED ? 2 : 1][4];
 #pragma unroll
-        for (int half = 0; half < (GATED ? 2 : 1); ++half) {
-            const float *from = p.slabs + row * width + c + half * p.J;
-            float4 t = *(const float4 *)from;
-            for (int k = 1; k < p.splits; k += 8) {
-                float4 u[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) u[j] = *(const float4 *)(from + min(k + j, p.splits - 1) * slab);
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (k + j < p.splits) { t.x += u[j].x; t.y += u[j].y; t.z += u[j].z; t.w += u[j].w; }
-            }
-            f[half][0] = t.x; f[half][1] = t.y; f[half][2] = t.z; f[half][3] = t.w;
-            if (p.bias) {
-                float b[4];
-                wide4(*(const uint2 *)(p.bias + half * p.J + c), b);
-#pragma unroll
-                for (int v = 0; v < 4; ++v) f[half][v] += b[v];
-            }
-            if (p.z) *(uint2 *)(p.z + row * width + half * p.J + c) = make_uint2(pack_bf16(f[half][0], f[half][1]), pack_bf16(f[half][2], f[half][3]));
-        }
-        float r[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (p.residual) wide4(*(const uint2 *)(p.residual + row * p.residual_stride + c), r);
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            f[0][v] = activation<ACT>(f[0][v]);
-            if (ACT == SKRULL_LINEAR_NONE && p.relu) f[0][v] = fmaxf(f[0][v], 0.0f);
-            if constexpr (GATED) f[0][v] *= f[1][v];
-            f[0][v] += r[v];
-        }
-        *(uint2 *)(p.out + row * p.out_stride + c) = make_uint2(pack_bf16(f[0][0], f[0][1]), pack_bf16(f[0][2], f[0][3]));
+        for (int half = 0; half < (GATED ? 2 : 1); ++half) sum_parts(p.slabs + row * width + c + half * p.J, slab, p.splits, f[half]);
+        finish<ACT, GATED>(p, row, c, f);
     }
+}
+// The same of the tail's tiles, of `rows` rows and 256 columns (gated: of 128 and 128): blockIdx.x a tile, blockIdx.y four rows of it (gated: eight).
+template <int ACT, bool GATED>
+__global__ __launch_bounds__(256) void linear_tail_kernel(const LinearArgs p, int rows)
+{
+    constexpr int kCols = GATED ? kTile / 2 : kTile, kGroups = kCols / 4;
+    const int mt = (p.J + kCols - 1) / kCols, nt = (p.I + rows - 1) / rows, tile = mt * nt - p.tail + blockIdx.x;
+    const int block = tile / (8 * nt), r = tile - block * (8 * nt), width = min(8, mt - block * 8), nn = r / width, m = block * 8 + r - nn * width;
+    const int in_tile = blockIdx.y * (256 / kGroups) + threadIdx.x / kGroups, c = threadIdx.x % kGroups * 4;
+    const int64_t row = (int64_t)nn * rows + in_tile;
+    if (row >= p.I || m * kCols + c >= p.J) return;
+    const int64_t slab = (int64_t)rows * kTile;
+    const float *from = p.slabs + (int64_t)blockIdx.x * p.tail_parts * slab + in_tile * kTile + c;
+    float f[GATED ? 2 : 1][4];
+#pragma unroll
+    for (int half = 0; half < (GATED ? 2 : 1); ++half) sum_parts(from + half * kCols, slab, p.tail_parts, f[half]);
+    finish<ACT, GATED>(p, row, m * kCols + c, f);
 }
 
 // ---- dz and the sums of its columns ----
@@ -405,7 +467,7 @@ int check_apart(const Rows &out, std::initializer_list<Rows> others)
 
 // Rows and columns of a product's tile / 64, and the parts of its contraction.
 struct Shape {
-    int na, nb, splits, steps;
+    int na, nb, splits, steps, tail, tail_parts, tail_steps;   // see LinearArgs
 };
 int tiles_of(int64_t n, int size) { return (int)((n + size - 1) / size); }
 // Which tiles, and in how many parts the contraction: what a launch is expected to take, in us, from what tiles of each shape took (37 to 4,096 rows, 896 to 4,096 inputs and
@@ -414,8 +476,9 @@ int tiles_of(int64_t n, int size) { return (int)((n + size - 1) / size); }
 //   256 x 256               256                  1.2 to 1.65 (power)    9
 //   256 x 64                256                  0.6                    5
 //   64 x 64 (forward)       512                  0.32, two on a unit 0.44   3
-// and parts, whose sums are written, read and added by a launch of its own, 4 and their bytes at 3 MB a us.  In us, this choice against 256 x 256 in parts where there were few
-// (which the forward had 64 x 64 for):
+// Where tiles are more than workgroups, the last ones, if they are half a round or less, are cut into parts (4,500 rows, 4,096 to 4,096, 288 tiles: the forward takes 179 us with
+// all whole and 137 so; 13,312 rows, 3,584 to 28,672, 1,568 tiles of dW: 2,105 and 1,931).  Parts, whose sums are written, read and added by a launch of its own, cost 4 and
+// their bytes at 3 MB a us.  In us, this choice against 256 x 256 in parts where there were few (which the forward had 64 x 64 for):
 //   rows, inputs, outputs   forward      dX           dW
 //   37, 896, 1,152          8.8   9.5    10.3  11.8   9.2
 //   1,001, 904, 1,160       12.0  12.1   17.0  24.5   24.4
@@ -427,7 +490,7 @@ Shape shape_of(Kind kind, int64_t I, int64_t J, int64_t C, bool gated)
     struct Tile { int na, nb, at_once; double step, shared_step, ends; };
     static const Tile tiles[] = {{4, 4, kGrid, 1.3, 1.3, 9.0}, {4, 1, kGrid, 0.6, 0.6, 5.0}, {1, 1, 2 * kGrid, 0.32, 0.44, 3.0}};
     const int steps = tiles_of(C, kStep);
-    Shape best = {4, 4, 1, steps};
+    Shape best = {4, 4, 1, steps, 0, 1, 0};
     double least = 0.0;
     for (const Tile &t : tiles) {
         if ((kind == kDw && t.nb != 4) || (t.na == 1 && (kind != kForward || gated))) continue;
@@ -440,13 +503,29 @@ Shape shape_of(Kind kind, int64_t I, int64_t J, int64_t C, bool gated)
             const double us = rounds * (each * step + t.ends) + (real > 1 ? 4.0 + sums / 3e6 : 0.0);
             if (least == 0.0 || us < least) {
                 least = us;
-                best = {t.na, t.nb, real, each};
+                best = {t.na, t.nb, real, each, 0, 1, 0};
             }
+        }
+        // whole rounds, and what is left in parts
+        const int64_t full = n / t.at_once;
+        const int tail = (int)(n - full * t.at_once);
+        if (t.na == 1 || full == 0 || tail == 0 || 2 * tail > t.at_once) continue;
+        int parts = t.at_once / tail;
+        if (parts > 16) parts = 16;
+        if (parts > steps) parts = steps;
+        const int each = (steps + parts - 1) / parts, real = (steps + each - 1) / each;
+        const double us = (double)full * (steps * t.step + t.ends) + each * t.step + t.ends + 4.0 + (double)tail * real * (64 * t.na * 64 * t.nb * 4) / 3e6;
+        if (real > 1 && us < least) {
+            least = us;
+            best = {t.na, t.nb, 1, steps, tail, real, each};
         }
     }
     return best;
 }
-int64_t slab_bytes(const Shape &s, int64_t I, int64_t width) { return s.splits > 1 ? (int64_t)s.splits * I * width * 4 : 0; }
+int64_t slab_bytes(const Shape &s, int64_t I, int64_t width)
+{
+    return s.splits > 1 ? (int64_t)s.splits * I * width * 4 : (int64_t)s.tail * s.tail_parts * (64 * s.na) * (64 * s.nb) * 4;
+}
 
 // Stripes of dz: 2,048 workgroups of a wavefront, or as many as have 4 rows.
 struct Stripes {
@@ -511,10 +590,18 @@ hipError_t multiply(const Shape &s, LinearArgs a, hipStream_t st)
 {
     a.splits = s.splits;
     a.steps = s.steps;
+    a.tail = s.tail;
+    a.tail_parts = s.tail_parts;
+    a.tail_steps = s.tail_steps;
     hipError_t e = launch<K, ACT, GATED>(s, a, st);
     if (e == hipSuccess && s.splits > 1) {
         const int64_t blocks = ((int64_t)a.I * (a.J / 4) + 255) / 256;
         linear_sums_kernel<ACT, GATED><<<(int)(blocks < 4096 ? blocks : 4096), 256, 0, st>>>(a);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess && s.tail > 0) {
+        const int at_once = 256 / ((GATED ? kTile / 2 : kTile) / 4);
+        linear_tail_kernel<ACT, GATED><<<dim3((unsigned)s.tail, (unsigned)(64 * s.nb / at_once)), 256, 0, st>>>(a, 64 * s.nb);
         e = hipGetLastError();
     }
     return e;

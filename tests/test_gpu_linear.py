@@ -122,6 +122,27 @@ def test_linear_of_long_contractions(rows, inputs, outputs, activation, gated):
     _check(got, _reference(x, w, b, None, dy, activation, gated), (activation, gated))
 
 
+@pytest.mark.parametrize("rows,inputs,outputs,activation,gated", [(4400, 4104, 4104, "none", False), (4400, 4104, 4104, "gelu", False), (4400, 4104, 2056, "silu", True), (4352, 1024, 4096, "relu", False)])
+def test_linear_of_a_round_of_tiles_and_some(rows, inputs, outputs, activation, gated):
+    """Some tiles more than there are units, the last ones in parts where they have many steps; workspaces hold NaN before, and their margins stay."""
+    from paper_2505_19609_amd import binding as B
+    from gpu_util import guarded, margins_intact
+    act = {"none": B.LINEAR_NONE, "relu": B.LINEAR_RELU, "gelu": B.LINEAR_GELU, "silu": B.LINEAR_SILU}[activation]
+    x, w, b, r, dy = _inputs(_gen(rows + inputs), rows, inputs, outputs, True, gated, True)
+    n = w.shape[0]
+    sizes = [B.skrull_linear_workspace(x, w, k, act, gated) for k in (False, True)]
+    assert sizes[0] > 0 or inputs < 4096    # (a few steps are not worth it)
+    ws = [guarded((max(16, s),), torch.uint8, 0xFF) for s in sizes]
+    shapes = {"y": (rows, outputs), "dx": (rows, inputs), "dw": (n, inputs), "db": (n,)}
+    bufs = {name: guarded(s, torch.bfloat16, float("nan")) for name, s in shapes.items()}
+    t = {name: v[1] for name, v in bufs.items()}
+    z = torch.empty(rows, n, dtype=torch.bfloat16, device="cuda") if act or gated else None
+    B.skrull_linear_fwd(x, w, b, r, t["y"], z, ws[0][1], act, gated)
+    B.skrull_linear_bwd(x, w, z, dy, t["dx"], t["dw"], t["db"], ws[1][1], act, gated)
+    assert all(margins_intact(v[0]) for v in (*bufs.values(), *ws))
+    _check(t, _reference(x, w, b, r, dy, activation, gated), (activation, gated))
+
+
 def _padded(t, pad, fill=float("nan")):
     wide = torch.full((t.shape[0], t.shape[1] + pad), fill, dtype=t.dtype, device=t.device)
     view = wide[:, :t.shape[1]]
