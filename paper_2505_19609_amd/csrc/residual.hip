@@ -442,12 +442,18 @@ int check_vectors(std::initializer_list<std::pair<const char *, const void *>> v
 int waves_of(int cols) { return cols <= 512 ? 1 : cols <= 1024 ? 2 : cols <= 2048 ? 4 : cols <= 4096 ? 8 : 16; }
 int rows_of(int waves) { return waves == 1 ? 4 : 1; }
 
-// Workgroups of the backward, each with a line of partial sums: as many as fill the compute units with 16 wavefronts.
+// Workgroups, each with a line of partial sums in the backward: 8 wavefronts to a compute unit (16 where a row has them).  With the next row of each under way that
+// keeps the memory busy, and more of them only spread the accesses.  Forward and backward in us, 8, 16 and 32 to a unit (bf16):
+//   32,768 x 4,096     183  194  204     289  316  326
+//   65,536 x 2,048     187  208  215     306  330  352
+//   200,000 x 512      144  165  170     236  246  260
+//   26,000 x 896        32   32   33      66   68   89
+//   8,192 x 8,192      116   94   96     211  156  165
 constexpr int kComputeUnits = 256;
-int64_t bwd_blocks(const skrull_residual_t *p)
+int64_t blocks_of(const skrull_residual_t *p)
 {
     const int waves = waves_of(p->cols), rows = rows_of(waves);
-    const int64_t most = kComputeUnits * 16 / (waves == 1 ? 4 : waves), need = (p->rows + rows - 1) / rows;
+    const int64_t most = kComputeUnits * (waves == 16 ? 1 : 8 / (waves == 1 ? 4 : waves)), need = (p->rows + rows - 1) / rows;
     return need < most ? need : most;
 }
 
@@ -525,16 +531,14 @@ int skrull_residual_fwd(const skrull_residual_t *p, const void *r, const void *z
     ResidualArgs a = args_of(p, r, z, w, post_w, post_b, gate);
     a.b = b; a.r_out = r_out; a.y = y; a.stats = stats;
     a.r_out_stride = p->r_out_stride; a.y_stride = p->y_stride;
-    const int waves = waves_of(p->cols), rows = rows_of(waves);
-    const int64_t most = (int64_t)compute_units * 32 / (waves == 1 ? 4 : waves), need = (p->rows + rows - 1) / rows;
-    launch(false, p, a, (int)(need < most ? need : most), (hipStream_t)hip_stream);
+    launch(false, p, a, (int)blocks_of(p), (hipStream_t)hip_stream);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? SKRULL_OK : launch_failed(e, "residual launch");
 }
 
 int64_t skrull_residual_workspace(const skrull_residual_t *p)
 {
-    return check(p) == SKRULL_OK ? bwd_blocks(p) * 4 * p->cols * 4 + 16 : 0;
+    return check(p) == SKRULL_OK ? blocks_of(p) * 4 * p->cols * 4 + 16 : 0;
 }
 
 int skrull_residual_bwd(const skrull_residual_t *p, const void *r, const void *z, const void *w, const void *post_w, const void *post_b,
@@ -575,7 +579,7 @@ int skrull_residual_bwd(const skrull_residual_t *p, const void *r, const void *z
         a.stats = const_cast<float *>(stats);
         a.partial = sums ? (float *)workspace : nullptr;
         a.d_r_out_stride = p->d_r_out_stride; a.dy_stride = p->dy_stride; a.r_out_stride = p->dr_stride; a.y_stride = p->dz_stride;
-        blocks = (int)bwd_blocks(p);
+        blocks = (int)blocks_of(p);
         launch(true, p, a, blocks, st);
         e = hipGetLastError();
     }
