@@ -81,7 +81,7 @@ struct BwdParams {
 
 // dK and dV of sinks (keys that all later queries see) would be one workgroup's chain over all queries of a sequence.  So the queries whose tiles lie behind the windows of a pass' keys
 // are taken in pieces of far_rows rows by workgroups of their own, in a launch before, which leave fp32 sums of the sinks' rows in slots of
-// their own; the pass adds them, in order, to its own.  (24,576 and 8,192 tokens, 32/8 heads of 128, window 4,096, 4 sinks: dK/dV 3.89 ms in one chain.)
+// their own; the pass adds them, in order, to its own.  (Which plans have them: FarRows.)
 // A segment's slots begin where no other one's end: of two that have such queries, both at least far_period keys long, the second one's number is larger by one at least for the same
 // prefix (two chunks), by two for another, and a last piece that is not whole takes one more than its rows' share.
 struct FarSums {
@@ -949,8 +949,9 @@ __device__ __forceinline__ int dkv_work(const int bid, KeyBlock &kb, DkvFeed &fe
     const int first_up = r0 == 0 ? 0 : __builtin_amdgcn_readfirstlane(r0 / g);
     // With a wide window the walk of a part of it is turned: it begins at the tile whose number in the segment is the last of those with one quotient by n_qt, goes down
     // to the lowest one and on from the highest.  The items that run together on a die are of neighbouring key blocks, whose tiles, mostly the same ones, each would otherwise
-    // come to two tiles after the one before, when its L2, 4 MB, no longer has them.  (24,576 tokens, 32/8 heads of 128, window 4,096: dK/dV 3.08 ms and 2.91 turned; narrower windows only
-    // get the dead rounds.)
+    // come to two tiles after the one before, when its L2, 4 MB, no longer has them.  (Sequences of
+    // 24,576 and 8,192 tokens in short ones, 32/8 heads of 128, window 4,096: the backward takes 5.05 ms and 4.95 turned; 24,576, 28/4 heads: 4.20 and 4.18.  Narrower windows
+    // only get the dead rounds.)
     const bool turned = WINDOW && !FAR && (kv0 >= sinks || far_rows) && n_qt_e == 0 && n_qt * g * D > (4 << 20) / (4 * QT);
     int top = n_qt - 1;
     if (WINDOW && __builtin_expect(turned, 0)) top -= __builtin_amdgcn_readfirstlane(i_first / QT % n_qt);
@@ -1611,20 +1612,30 @@ KeyMap map_dkv(const skrull_attn_plan_t *p)
                   inverse_of(passes * p->Hkv)};
 }
 
-// The pieces of FarSums of a plan: about 32 rounds of a workgroup each.  There are none where the chain of the longest sequence's sinks, in rounds (a tile of queries of a head), is
-// at most half an even share of all rounds, or hardly longer than others, or where there are more than 128 sinks, whose passes are many enough.
+// The pieces of FarSums of a plan: about 32 rounds of a workgroup each.  A round is a tile of queries of a head.  Without them the walk of the longest sequence's sinks, which
+// a plan may have given to several workgroups, takes about as long as its rounds, the launch as an even share of all rounds or the longest of the other walks, if that is longer; with
+// them the launch of their own, the sums' way through memory and two launches for dQ and dK/dV that would be one cost about 112 rounds.  The backward without them and with them, 4 sinks:
+//   tokens, heads of size, window            rounds: sinks, even share     us
+//   8,192, 32/8 of 128, 1,024                 512    128                   971    538
+//   65,536, 14/2 of 64, 8,192                 7,168  2,389                 11,993 6,657
+//   8,192, 8/8 of 128, 256                    128    8                     220    127
+//   8,192, 14/2 of 64, 256 (of 7 workgroups)  128    9                     186    161
+//   16,384 + 8 x 2,048, 14/2 of 64, 1,024     256    149                   547    560
+//   8,192, 28/4 of 128, 1,024                 128    112                   510    614
+//   16 x 1,024, 14/2 of 64, 256               37     19                    125    189
+// With more than 128 sinks their passes are many enough.
 struct FarRows {
     int32_t rows = 0, period = 1;
     FarRows(const skrull_attn_plan_t *p, const KeyWindow *window)
     {
         if (!window || window->sinks == 0 || window->sinks > 128) return;
-        const int SUB = 32 * dkv_pairs(p), g = p->Hq / p->Hkv;
+        const int SUB = 32 * dkv_pairs(p), g = p->Hq / p->Hkv, parts = p->n_split > 0 ? p->split_parts : 1;
         period = (p->BN < SUB ? p->BN : SUB) + window->keys;
         const int64_t threads = blocks(p, window) * 64 * 2 * dkv_pairs(p);
         const int64_t queries = p->longest_seq < p->total_q ? p->longest_seq : p->total_q, in_window = (int64_t)p->total_q * window->keys;
-        const int64_t chain = queries / TILE_ROWS * g, others = period / TILE_ROWS * g;
-        const int64_t all = (p->pairs < in_window ? p->pairs : in_window) / (TILE_ROWS * 32 * dkv_pairs(p)) * p->Hq;   // (at most)
-        if (p->longest_seq >= period && chain >= others + 32 && 2 * 256 * chain > all && threads < (int64_t)1 << 32) rows = 256 * ((8 + g - 1) / g);
+        const int64_t chain = queries / TILE_ROWS * g / parts, others = period / TILE_ROWS * g / parts;
+        const int64_t share = (p->pairs < in_window ? p->pairs : in_window) / (TILE_ROWS * 32 * dkv_pairs(p)) * p->Hq / 256;   // (at most)
+        if (p->longest_seq >= period && chain >= (share > others ? share : others) + 112 && threads < (int64_t)1 << 32) rows = 256 * ((8 + g - 1) / g);
     }
     // work items: the forward's, each for all KV heads and passes that have sinks
     static int64_t blocks(const skrull_attn_plan_t *p, const KeyWindow *window)

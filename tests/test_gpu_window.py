@@ -151,14 +151,20 @@ def test_window_with_other_blocks(shape, block_n, head_split):
     plan.destroy()
 
 
-@pytest.mark.parametrize("shape,heads,d", [(_whole(4200, 40, 3000, 300), (7, 1), 64), (_whole(2100, 700, 1900), (8, 1), 128), (([9000, 300, 6000], [4, 1, 2], [1, 0, 0], [1, 0, 1]), (4, 2), 64),
-                                           (([6000, 2500], [2, 3], [1, 2], [0, 1]), (8, 2), 128)])
-def test_window_sinks_of_long_sequences(shape, heads, d):
-    """Queries far behind the sinks' own windows, in several pieces of several sequences and chunks; the workspace between margins."""
+_CHUNKS = ([24000, 300, 16000], [4, 1, 2], [1, 0, 0], [1, 0, 1])
+
+
+@pytest.mark.parametrize("shape,heads,d,pieces", [(_whole(4200, 40, 3000, 300), (7, 1), 64, False), (_whole(2100, 700, 1900), (8, 1), 128, False),
+                                                  (([9000, 300, 6000], [4, 1, 2], [1, 0, 0], [1, 0, 1]), (4, 2), 64, False), (([6000, 2500], [2, 3], [1, 2], [0, 1]), (8, 2), 128, False),
+                                                  (_whole(8000, 200, 6000), (8, 2), 64, True), (_whole(12000, 300), (8, 2), 128, True), (_CHUNKS, (8, 2), 64, True), (_CHUNKS, (8, 2), 128, True),
+                                                  (_whole(*[2048] * 16), (16, 2), 64, True), (_whole(*[2048 - 70 * i for i in range(16)]), (32, 4), 64, True)])
+def test_window_sinks_of_long_sequences(shape, heads, d, pieces):
+    """Queries far behind the sinks' own windows, of several sequences and chunks; `pieces`: they are many enough to be taken by themselves.  The workspace between margins."""
     from paper_2505_19609_amd import binding as B
     from gpu_util import guarded, margins_intact
     plan = _plan(shape, heads, d)
     x = _inputs(plan, 17)
+    assert (B.skrull_window_workspace(plan, 100, 4) > B.skrull_window_workspace(plan, 100, 0)) == pieces   # (for the pieces' sums)
     for window, sinks in ((100, 4), (300, 128), (64, 65), (20, 129), (1000, 1)):
         buf, ws = guarded((B.skrull_window_workspace(plan, window, sinks),), torch.uint8, 0xFF)
         o, lse = torch.empty_like(x["q"]), torch.empty(heads[0], plan.total_q, device="cuda")
