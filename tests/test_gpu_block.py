@@ -408,3 +408,118 @@ def test_wrappers_refuse_alike():
     plan.destroy()
     with pytest.raises(B.SkrullError):
         A.skrull_window_attention(q, q, q, plan, 1)
+
+
+# ---- all of them together, with the other operators -----------------------------------------------------------------
+
+_LENGTHS, _WINDOW, _SINKS = (37, 200, 1, 410), 100, 3
+
+
+def _block_case(seed=5, heads=(4, 2), d=64, hidden=264, middle=360, vocab=500):
+    from paper_2505_19609_amd import binding as B
+    gen, n = _gen(seed), (heads[0] + 2 * heads[1]) * d
+    plan = B.skrull_attn_plan(list(_LENGTHS), [1] * len(_LENGTHS), [0] * len(_LENGTHS), heads[0], heads[1], d, d ** -0.5)
+    one = lambda: 1 + _randn(gen, hidden, scale=0.2)   # noqa: E731
+    leaves = {"r": _randn(gen, plan.total_q, hidden), "z": _randn(gen, plan.total_q, hidden), "w1": one(), "post": one(), "gate": 0.5 * one(),
+              "wqkv": _randn(gen, n, hidden, scale=hidden ** -0.5), "bqkv": _randn(gen, n, scale=0.2), "wo": _randn(gen, hidden, heads[0] * d, scale=(heads[0] * d) ** -0.5),
+              "w2": one(), "b2": _randn(gen, hidden, scale=0.1), "wgu": _randn(gen, 2 * middle, hidden, scale=hidden ** -0.5),
+              "wd": _randn(gen, hidden, middle, scale=middle ** -0.5), "bd": _randn(gen, hidden, scale=0.2), "w3": one(), "vocab": _randn(gen, vocab, hidden, scale=1.5 * hidden ** -0.5)}
+    target = torch.randint(0, vocab, (plan.total_q,), generator=gen, device="cuda")
+    target[::17] = -1
+    return plan, B.skrull_rotary_init(d, base=1e4), heads, d, {n: t.detach().requires_grad_() for n, t in leaves.items()}, target
+
+
+def _block(plan, rotary, heads, d, p, target):
+    """The stream, a block of windowed attention and a gated one of products, and the loss."""
+    from paper_2505_19609_amd.autograd import skrull_cross_entropy, skrull_linear, skrull_norm, skrull_residual_norm, skrull_rotary, skrull_window_attention
+    hq, hkv = heads
+    r, y = skrull_residual_norm(p["r"], p["z"], p["w1"], None, p["post"], None, p["gate"], 1.0, 1e-5, "rms")
+    q, k, v = (t.unflatten(1, (-1, d)) for t in skrull_linear(y, p["wqkv"], p["bqkv"]).split([hq * d, hkv * d, hkv * d], 1))
+    q, k = skrull_rotary(q, k, plan, rotary)
+    o = skrull_window_attention(q, k, v, plan, _WINDOW, _SINKS)
+    r, y = skrull_residual_norm(r, skrull_linear(o.flatten(1), p["wo"]), p["w2"], p["b2"])
+    r = skrull_linear(skrull_linear(y, p["wgu"], None, None, "silu", True), p["wd"], p["bd"], r)
+    return skrull_cross_entropy(skrull_norm(r, p["w3"], None, 1e-5, "rms"), p["vocab"], target)
+
+
+def _block_in_64_bits(heads, d, p, target):
+    hq, hkv = heads
+    rms = lambda t: t * (t.square().mean(1, keepdim=True) + 1e-5).rsqrt()   # noqa: E731
+    r = p["r"] + p["gate"] * rms(p["z"]) * p["post"]
+    q, k, v = (t.unflatten(1, (-1, d)) for t in ((rms(r) * p["w1"]) @ p["wqkv"].t() + p["bqkv"]).split([hq * d, hkv * d, hkv * d], 1))
+    pos = torch.cat([torch.arange(n) for n in _LENGTHS]).cuda()
+    seq = torch.repeat_interleave(torch.arange(len(_LENGTHS)), torch.tensor(_LENGTHS)).cuda()
+    angle = (pos[:, None].double() * 1e4 ** (-torch.arange(d // 2, device="cuda").double() * 2 / d))[:, None]
+    turn = lambda t: torch.cat((t[..., :d // 2] * angle.cos() - t[..., d // 2:] * angle.sin(), t[..., :d // 2] * angle.sin() + t[..., d // 2:] * angle.cos()), -1)   # noqa: E731
+    q, k = turn(q), turn(k)
+    far = pos[:, None] - pos[None]
+    seen = (seq[:, None] == seq[None]) & (far >= 0) & ((far < _WINDOW) | (pos[None] < _SINKS))
+    o = [(q[:, h] @ k[:, h * hkv // hq].t() * d ** -0.5).masked_fill(~seen, -math.inf).softmax(1) @ v[:, h * hkv // hq] for h in range(hq)]
+    r = r + torch.cat(o, 1) @ p["wo"].t()
+    y = (r - r.mean(1, keepdim=True)) / (r.var(1, unbiased=False, keepdim=True) + 1e-5).sqrt() * p["w2"] + p["b2"]
+    a, b = (y @ p["wgu"].t()).chunk(2, 1)
+    r = r + (a * torch.sigmoid(a) * b) @ p["wd"].t() + p["bd"]
+    return torch.nn.functional.cross_entropy((rms(r) * p["w3"]) @ p["vocab"].t(), target.clamp(min=0), reduction="none") * (target >= 0)
+
+
+def test_block_against_64_bits():
+    plan, rotary, heads, d, p, target = _block_case()
+    weight = torch.rand(len(target), generator=_gen(6), device="cuda")
+    loss = _block(plan, rotary, heads, d, p, target)
+    grads = torch.autograd.grad((loss * weight).sum(), list(p.values()))
+    exact = {n: t.detach().double().requires_grad_() for n, t in p.items()}
+    want = _block_in_64_bits(heads, d, exact, target)
+    wanted = torch.autograd.grad((want * weight).sum(), list(exact.values()))
+    # Thirteen tensors are rounded to bf16 on the way there (two streams, three normed rows, qkv, the turned ones, probabilities, o, three products' rows, the last stream) and
+    # as many on the way back, each by 2^-8 of its values at most: their errors in 2-norm add to at most 26 * 2^-8 = 10 % of a gradient's, and of the loss 13 * 2^-8.
+    assert ((loss.double() - want).norm() / want.norm()).item() <= 13 * BF16
+    for name, a, b in zip(p, grads, wanted):
+        assert ((a.double() - b).norm() / b.norm()).item() <= 26 * BF16, name
+    plan.destroy()
+
+
+def test_block_by_native_calls_and_by_functions_gives_the_same_bits(monkeypatch):
+    from paper_2505_19609_amd import autograd as A
+    plan, rotary, heads, d, p, target = _block_case(seed=8)
+
+    def run():
+        loss = _block(plan, rotary, heads, d, p, target)
+        return [loss.detach(), *torch.autograd.grad(loss.sum(), list(p.values()))]
+    native = run()
+    monkeypatch.setattr(A, "_native_for", lambda *t: None)
+    assert all(torch.equal(a, b) for a, b in zip(native, run()))
+    plan.destroy()
+
+
+def test_block_captured_and_replayed():
+    plan, rotary, heads, d, p, target = _block_case(seed=7)
+    gen = _gen(9)
+    weight = torch.rand(len(target), generator=gen, device="cuda")
+
+    def step():
+        loss = _block(plan, rotary, heads, d, p, target)
+        return [loss.detach(), *torch.autograd.grad(loss, list(p.values()), weight)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        captured = step()
+    for rep in range(4):
+        if rep >= 2:
+            with torch.no_grad():
+                for name in ("r", "z", "wqkv", "gate"):
+                    p[name].mul_(0.9)
+                target.copy_(target.roll(3))
+        for t in captured:
+            t.fill_(7.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(captured, want)), rep
+    plan.destroy()
