@@ -43,10 +43,12 @@ __device__ __forceinline__ float normal_share(float z, float &density)
 }
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + fast_exp2(z * -kLog2e)); }
 
+__device__ __forceinline__ float relu(float z) { return z < 0.0f ? 0.0f : z; }   // (a NaN stays one)
+
 template <int ACT>
 __device__ __forceinline__ float activation(float z)
 {
-    if constexpr (ACT == SKRULL_LINEAR_RELU) return fmaxf(z, 0.0f);
+    if constexpr (ACT == SKRULL_LINEAR_RELU) return relu(z);
     if constexpr (ACT == SKRULL_LINEAR_SILU) return z * sigmoid(z);
     if constexpr (ACT == SKRULL_LINEAR_GELU) {
         float density;
@@ -61,7 +63,7 @@ __device__ __forceinline__ float activation(float z, float &slope)
     slope = 1.0f;
     if constexpr (ACT == SKRULL_LINEAR_RELU) {
         slope = z > 0.0f ? 1.0f : 0.0f;
-        return fmaxf(z, 0.0f);
+        return relu(z);
     }
     if constexpr (ACT == SKRULL_LINEAR_SILU) {
         const float s = sigmoid(z);
@@ -249,7 +251,7 @@ __global__ __launch_bounds__(256, 1) void linear_product_kernel(const LinearArgs
 #pragma unroll
                     for (int v = 0; v < 8; ++v) {
                         f[v] = activation<ACT>(f[v]);
-                        if (ACT == SKRULL_LINEAR_NONE && p.relu) f[v] = fmaxf(f[v], 0.0f);
+                        if (ACT == SKRULL_LINEAR_NONE && p.relu) f[v] = relu(f[v]);
                         if constexpr (GATED) f[v] *= z2[v];
                     }
                     if (residual) {
@@ -287,7 +289,7 @@ __device__ __forceinline__ void finish(const LinearArgs &p, int64_t row, int c, 
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
         f[0][v] = activation<ACT>(f[0][v]);
-        if (ACT == SKRULL_LINEAR_NONE && p.relu) f[0][v] = fmaxf(f[0][v], 0.0f);
+        if (ACT == SKRULL_LINEAR_NONE && p.relu) f[0][v] = relu(f[0][v]);
         if constexpr (GATED) f[0][v] *= f[1][v];
         f[0][v] += r[v];
     }

@@ -327,3 +327,19 @@ def test_linear_offsets_past_32_bits():
     other = torch.ones(rows, dtype=torch.bool, device="cuda")
     other[at] = False
     assert (dx[other] == 0).all()
+
+
+@pytest.mark.parametrize("rows,inputs,outputs", [(70, 72, 136), (1500, 520, 264)])
+@pytest.mark.parametrize("activation,gated", KINDS)
+def test_linear_rows_that_are_not_finite(rows, inputs, outputs, activation, gated):
+    """A row with a NaN gives a row of NaN, and the others what they give beside any values there."""
+    from paper_2505_19609_amd.autograd import skrull_linear
+    x, w, b, r, _ = _inputs(_gen(12), rows, inputs, outputs, True, gated, True)
+    want = skrull_linear(x, w, b, r, activation, gated)
+    bad = torch.tensor([0, 33, rows - 1], device="cuda")
+    x[bad, inputs - 1] = float("nan")
+    got = skrull_linear(x, w, b, r, activation, gated)
+    assert torch.isnan(got[bad]).all()
+    good = torch.ones(rows, dtype=torch.bool, device="cuda")
+    good[bad] = False
+    assert torch.equal(got[good], want[good])
