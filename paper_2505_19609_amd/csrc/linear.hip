@@ -111,9 +111,7 @@ __global__ __launch_bounds__(256, 1) void linear_product_kernel(const LinearArgs
 {
     constexpr bool A_COLS = K != kForward, B_COLS = K == kDw;
     constexpr int kCols = GATED ? 32 * NA : 64 * NA, kRows = 64 * NB;   // of the result, of a tile
-    // (a step of a small tile is short beside the latency of its loads, which run four steps ahead there: 64 x 64, 15 steps, 13.9 us with two and 9 with four)
-    constexpr int kBuffers = NB == 4 ? 2 : 4;
-    __shared__ __align__(1024) unsigned char lds[kBuffers * kProductBytes<NA, NB>];
+    __shared__ __align__(1024) unsigned char lds[2 * kProductBytes<NA, NB>];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1;
     const int n = lane & 15, g = lane >> 4;
     const uint32_t a_pitch = (uint32_t)p.a_stride * 2, b_pitch = (uint32_t)p.b_stride * 2;
@@ -266,7 +264,7 @@ __global__ __launch_bounds__(256, 1) void linear_product_kernel(const LinearArgs
             }
         }
     };
-    product_tiles<A_COLS, B_COLS, NA, NB, !A_COLS, !B_COLS, kBuffers>(lds, A, B, a_pitch, b_pitch, 0, n_items, 1, open, tile_begin, tile_end, GATED ? p.J : 16 * NA);
+    product_tiles<A_COLS, B_COLS, NA, NB, !A_COLS, !B_COLS>(lds, A, B, a_pitch, b_pitch, 0, n_items, 1, open, tile_begin, tile_end, GATED ? p.J : 16 * NA);
 }
 
 // What follows the sum f of row `row` and columns c .. c + 3 (gated: of both halves).
@@ -472,51 +470,58 @@ struct Shape {
     int na, nb, splits, steps, tail, tail_parts, tail_steps;   // see LinearArgs
 };
 int tiles_of(int64_t n, int size) { return (int)((n + size - 1) / size); }
-// Which tiles, and in how many parts the contraction: what a launch is expected to take, in us, from what tiles of each shape took (37 to 4,096 rows, 896 to 4,096 inputs and
+// Which tiles, and in how many parts the contraction: what a launch is expected to take, in us, from what tiles of each shape took (37 to 16,384 rows, 896 to 4,096 inputs and
 // outputs):
-//   tile (columns x rows)   workgroups at once   a step                 a tile's start and end
-//   256 x 256               256                  1.2 to 1.65 (power)    9
-//   256 x 64                256                  0.6                    5
-//   64 x 64 (forward)       512                  0.32, two on a unit 0.44   3
+//   tile (columns x rows)   at once on a unit   a step with 1, 2, 3, 4 of them   a tile's start and end
+//   256 x 256               1                   1.2 to 1.65 (power)              9
+//   256 x 64                2                   0.60  1.03                       5
+//   64 x 64 (forward)       4                   0.35  0.40  0.60  0.80           3
 // Where tiles are more than workgroups, the last ones, if they are half a round or less, are cut into parts (4,500 rows, 4,096 to 4,096, 288 tiles: the forward takes 179 us with
 // all whole and 137 so; 13,312 rows, 3,584 to 28,672, 1,568 tiles of dW: 2,105 and 1,931).  Parts, whose sums are written, read and added by a launch of its own, cost 4 and
-// their bytes at 3 MB a us.  In us, this choice against 256 x 256 in parts where there were few (which the forward had 64 x 64 for):
-//   rows, inputs, outputs   forward      dX           dW
-//   37, 896, 1,152          8.8   9.5    10.3  11.8   9.2
-//   1,001, 904, 1,160       12.0  12.1   17.0  24.5   24.4
-//   932, 896, 3,584         15.5  30.7   24.4  29.8   26.4  30.8
-//   4,096, 1,024, 1,024     17.3  33.8   16.9  33.7   31.5  33.7
-//   500, 4,096, 4,096       33.6  35.5   35.5  38.6   22.4
+// their bytes at 3 MB a us.  In us, each with the parts that suit it best:
+//   rows, inputs, outputs   forward: 256 x 256, 256 x 64, 64 x 64   dX: 256 x 256, 256 x 64
+//   37, 896, 1,152                          13.5  10.6                  14.5  14.2
+//   1,001, 904, 1,160                 26.5  15.8  12.1                  25.4  16.9
+//   4,096, 1,024, 1,024               32.9  17.7  18.2                  28.2  16.8
+//   500, 4,096, 4,096                 38.0  32.3  32.4                  38.7  33.9
+//   3,000, 2,048, 2,048               45.8  36.6  40.4                  45.2  35.6
+//   16,384, 896, 1,152                57.1  48.2  58.6                  34.9  46.2
+//   8,192, 1,024, 4,096               68.3  82.5  109                   73.1  71.6
+//   2,000, 3,584, 4,608               81.8  89.7  100                   73.8  78.4
 Shape shape_of(Kind kind, int64_t I, int64_t J, int64_t C, bool gated)
 {
-    struct Tile { int na, nb, at_once; double step, shared_step, ends; };
-    static const Tile tiles[] = {{4, 4, kGrid, 1.3, 1.3, 9.0}, {4, 1, kGrid, 0.6, 0.6, 5.0}, {1, 1, 2 * kGrid, 0.32, 0.44, 3.0}};
+    struct Tile { int na, nb, on_a_unit; double step[4], ends; };
+    static const Tile tiles[] = {{4, 4, 1, {1.3}, 9.0}, {4, 1, 2, {0.6, 1.03}, 5.0}, {1, 1, 4, {0.35, 0.4, 0.6, 0.8}, 3.0}};
     const int steps = tiles_of(C, kStep);
     Shape best = {4, 4, 1, steps, 0, 1, 0};
     double least = 0.0;
     for (const Tile &t : tiles) {
         if ((kind == kDw && t.nb != 4) || (t.na == 1 && (kind != kForward || gated))) continue;
-        const int64_t n = (int64_t)tiles_of(I, 64 * t.nb) * tiles_of(J, (gated ? 32 : 64) * t.na);   // (none of no rows)
+        const int64_t n = (int64_t)tiles_of(I, 64 * t.nb) * tiles_of(J, (gated ? 32 : 64) * t.na), at_once = (int64_t)t.on_a_unit * kGrid;   // (none of no rows)
+        // `items` of `each` steps
+        auto time = [&](int64_t items, int each) {
+            const int64_t full = items / at_once, rest = items - full * at_once;
+            return (double)full * (each * t.step[t.on_a_unit - 1] + t.ends) + (rest ? each * t.step[(rest - 1) / kGrid] + t.ends : 0.0);
+        };
         for (int parts = 1; parts <= 16 && parts <= steps; ++parts) {
             const int each = (steps + parts - 1) / parts, real = (steps + each - 1) / each;
             const double sums = real > 1 ? 4.0 * (gated ? 2 : 1) * (double)real * (double)I * (double)J : 0.0;
             if (real < parts || sums > (double)(128 << 20)) continue;
-            const double rounds = (double)((n * real + t.at_once - 1) / t.at_once), step = n * real > kGrid ? t.shared_step : t.step;
-            const double us = rounds * (each * step + t.ends) + (real > 1 ? 4.0 + sums / 3e6 : 0.0);
+            const double us = time(n * real, each) + (real > 1 ? 4.0 + sums / 3e6 : 0.0);
             if (least == 0.0 || us < least) {
                 least = us;
                 best = {t.na, t.nb, real, each, 0, 1, 0};
             }
         }
         // whole rounds, and what is left in parts
-        const int64_t full = n / t.at_once;
-        const int tail = (int)(n - full * t.at_once);
-        if (t.na == 1 || full == 0 || tail == 0 || 2 * tail > t.at_once) continue;
-        int parts = t.at_once / tail;
+        const int64_t full = n / at_once;
+        const int tail = (int)(n - full * at_once);
+        if (t.na == 1 || full == 0 || tail == 0 || 2 * tail > at_once) continue;
+        int parts = (int)at_once / tail;
         if (parts > 16) parts = 16;
         if (parts > steps) parts = steps;
         const int each = (steps + parts - 1) / parts, real = (steps + each - 1) / each;
-        const double us = (double)full * (steps * t.step + t.ends) + each * t.step + t.ends + 4.0 + (double)tail * real * (64 * t.na * 64 * t.nb * 4) / 3e6;
+        const double us = time(full * at_once, steps) + time((int64_t)tail * real, each) + 4.0 + (double)tail * real * (64 * t.na * 64 * t.nb * 4) / 3e6;
         if (real > 1 && us < least) {
             least = us;
             best = {t.na, t.nb, 1, steps, tail, real, each};
@@ -576,12 +581,12 @@ hipError_t launch(const Shape &s, const LinearArgs &a, hipStream_t st)
 {
     if constexpr (K == kForward && !GATED)
         if (s.na == 1) {
-            linear_product_kernel<K, 1, 1, ACT, GATED><<<4 * kGrid, 256, 0, st>>>(a);   // (as many fit the compute units)
+            linear_product_kernel<K, 1, 1, ACT, GATED><<<4 * kGrid, 256, 0, st>>>(a);   // (as many fit the units)
             return hipGetLastError();
         }
     if constexpr (K != kDw)
         if (s.nb == 1) {
-            linear_product_kernel<K, 4, 1, ACT, GATED><<<kGrid, 256, 0, st>>>(a);
+            linear_product_kernel<K, 4, 1, ACT, GATED><<<2 * kGrid, 256, 0, st>>>(a);
             return hipGetLastError();
         }
     linear_product_kernel<K, 4, 4, ACT, GATED><<<kGrid, 256, 0, st>>>(a);

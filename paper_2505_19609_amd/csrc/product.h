@@ -119,7 +119,7 @@ __device__ __forceinline__ int here(int x)
 }
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-// Forms the tiles `begin`, `begin` + `stride`, .. below `end`: `lds` holds BUFFERS (a power of two) times kProductBytes<NA, NB>, the steps that loads run ahead.
+// Forms the tiles `begin`, `begin` + `stride`, .. below `end`: `lds` holds two buffers of kProductBytes<NA, NB>.
 //   open(tile, a, b, steps, a_tail, b_tail)  where its operands' steps lie, how many there are (none: the tile has only an end), and, of an operand whose rows may
 //                                            end inside a step (A_TAIL, B_TAIL), how many elements of the contraction
 //   tile_begin(tile)                         before its products; returns the same number of steps
@@ -127,7 +127,7 @@ __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __
 //                                            the tile, g = lane / 16, n = lane % 16
 template <int NA, int NB> constexpr int kProductBytes = 8192 * (NA + NB);
 // `a_half_rows`: see Operand::fetch.
-template <bool A_COLS, bool B_COLS, int NA, int NB, bool A_TAIL, bool B_TAIL, int BUFFERS = 2, class Open, class Begin, class End>
+template <bool A_COLS, bool B_COLS, int NA, int NB, bool A_TAIL, bool B_TAIL, class Open, class Begin, class End>
 __device__ __forceinline__ void product_tiles(unsigned char *lds, const Operand<A_COLS, NA> &A, const Operand<B_COLS, NB> &B, uint32_t a_pitch, uint32_t b_pitch, int begin, int end,
                                               int stride, Open open, Begin tile_begin, End tile_end, int a_half_rows = 16 * NA)
 {
@@ -137,7 +137,7 @@ __device__ __forceinline__ void product_tiles(unsigned char *lds, const Operand<
 
     // The steps of this workgroup's tiles are one sequence, and the loads run ahead in it across the end of a tile.
     struct Cursor {
-        int tile, left, a_tail, b_tail, buffer;
+        int tile, left, a_tail, b_tail, parity;
         Source a, b;
     };
     struct Fetch {   // what the loads of a step need
@@ -156,13 +156,13 @@ __device__ __forceinline__ void product_tiles(unsigned char *lds, const Operand<
         f.b = c.b.words();
         A.offsets(lane, wave, A_TAIL ? c.a_tail : kStep, f.a_off);
         B.offsets(lane, wave, B_TAIL ? c.b_tail : kStep, f.b_off);
-        f.lds = lds0 + c.buffer * kBufferBytes;
+        f.lds = lds0 + c.parity * kBufferBytes;
         c.a.next();
         c.b.next();
         c.a_tail -= kStep;
         c.b_tail -= kStep;
         c.left -= c.left > 0;
-        c.buffer = (c.buffer + 1) & (BUFFERS - 1);
+        c.parity ^= 1;
         return f;
     };
     auto load_a = [&](const Fetch &f, int half, int q) { A.fetch(f.a, f.a_off, a_pitch, f.lds, wave, half, q, a_half_rows); };
@@ -170,7 +170,7 @@ __device__ __forceinline__ void product_tiles(unsigned char *lds, const Operand<
 
     // A step in two halves, of 64 products with NB = 4.  What a half of the blocks needs is read half a step before its first product, so its place
     // in LDS is free early, and its loads have a step until they are waited for:
-    //   half  products        reads                       loads (with two buffers of the step after next)
+    //   half  products        reads                       loads (of the step after next)
     //   1     A0 B0, A0 B1    B1, A1                      A0 B0
     //   2     A1 B0, A1 B1    A0, B0 of the next step     B1 A1
     // Each half ends with a barrier: what was read in it may be overwritten, and what the next one reads is there (a step's loads, 16 with NB = 4, are younger).
@@ -178,14 +178,14 @@ __device__ __forceinline__ void product_tiles(unsigned char *lds, const Operand<
     f32x4 acc[2 * NA][2 * NB];
     auto half_end = [&]() {
         SB();
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * (BUFFERS - 1) * (NA + NB)) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * (NA + NB)) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         SB();
     };
     Cursor cursor = {begin, 0, 0, 0, 0, {}, {}};
 #pragma unroll
-    for (int step = 0; step < BUFFERS; ++step) {
+    for (int step = 0; step < 2; ++step) {
         const Fetch f = take(cursor);
 #pragma unroll
         for (int q = 0; q < NA; ++q) {
@@ -198,7 +198,7 @@ __device__ __forceinline__ void product_tiles(unsigned char *lds, const Operand<
             load_a(f, 1, q);
         }
     }
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((2 * BUFFERS - 1) * (NA + NB)) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * (NA + NB)) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     auto read_a = [&](const unsigned char *t, int half, bf16x8 to[NA][2], int i) { to[i % NA][i / NA] = A.get(t, half, i % NA, i / NA); };
@@ -220,8 +220,7 @@ __device__ __forceinline__ void product_tiles(unsigned char *lds, const Operand<
 #pragma unroll
                 for (int v = 0; v < 4; ++v) acc[x][y][v] = 0.0f;
         for (int step = 0; step < steps; ++step) {
-            const int then = BUFFERS == 2 ? at ^ kBufferBytes : at + kBufferBytes == BUFFERS * kBufferBytes ? 0 : at + kBufferBytes;
-            const unsigned char *t = lds + at, *next = lds + then;
+            const unsigned char *t = lds + at, *next = lds + (at ^ kBufferBytes);
             const Fetch f = take(cursor);
             if constexpr (NB == 4) {
                 // Product j of a quarter: blocks j / 8 and j / 2 % 4, half step j % 2 (two products in a row on one accumulator need less power:
@@ -301,7 +300,7 @@ __device__ __forceinline__ void product_tiles(unsigned char *lds, const Operand<
                 for (int i = 0; i < 2 * NB; ++i) b0[i / 2][i & 1] = b2[i / 2][i & 1];
                 half_end();
             }
-            at = then;
+            at ^= kBufferBytes;
         }
 
         // (the compiler does not see that what follows reads results of the matrix pipe: the distance it would keep)
