@@ -479,15 +479,15 @@ int tiles_of(int64_t n, int size) { return (int)((n + size - 1) / size); }
 // Where tiles are more than workgroups, the last ones, if they are half a round or less, are cut into parts (4,500 rows, 4,096 to 4,096, 288 tiles: the forward takes 179 us with
 // all whole and 137 so; 13,312 rows, 3,584 to 28,672, 1,568 tiles of dW: 2,105 and 1,931).  Parts, whose sums are written, read and added by a launch of its own, cost 4 and
 // their bytes at 3 MB a us.  In us, each with the parts that suit it best:
-//   rows, inputs, outputs   forward: 256 x 256, 256 x 64, 64 x 64   dX: 256 x 256, 256 x 64
-//   37, 896, 1,152                          13.5  10.6                  14.5  14.2
-//   1,001, 904, 1,160                 26.5  15.8  12.1                  25.4  16.9
-//   4,096, 1,024, 1,024               32.9  17.7  18.2                  28.2  16.8
-//   500, 4,096, 4,096                 38.0  32.3  32.4                  38.7  33.9
-//   3,000, 2,048, 2,048               45.8  36.6  40.4                  45.2  35.6
-//   16,384, 896, 1,152                57.1  48.2  58.6                  34.9  46.2
-//   8,192, 1,024, 4,096               68.3  82.5  109                   73.1  71.6
-//   2,000, 3,584, 4,608               81.8  89.7  100                   73.8  78.4
+//   rows, inputs, outputs   forward: 256 x 256, 256 x 64, 64 x 64   dX: 256 x 256, 256 x 64   dW: 256 x 256, 256 x 64
+//   37, 896, 1,152                          13.5  10.6                  14.5  14.2                12.2  11.8
+//   1,001, 904, 1,160                 26.5  15.8  12.1                  25.4  16.9                24.4  15.6
+//   4,096, 1,024, 1,024               32.9  17.7  18.2                  28.2  16.8                32.4  25.0
+//   500, 4,096, 4,096                 38.0  32.3  32.4                  38.7  33.9                23.1  26.8
+//   3,000, 2,048, 2,048               45.8  36.6  40.4                  45.2  35.6                44.3  39.2
+//   16,384, 896, 1,152                57.1  48.2  58.6                  34.9  46.2                54.8  56.3
+//   8,192, 1,024, 4,096               68.3  82.5  109                   73.1  71.6                72.4  85.6
+//   2,000, 3,584, 4,608               81.8  89.7  100                   73.8  78.4                57.1  82.3
 Shape shape_of(Kind kind, int64_t I, int64_t J, int64_t C, bool gated)
 {
     struct Tile { int na, nb, on_a_unit; double step[4], ends; };
@@ -496,7 +496,7 @@ Shape shape_of(Kind kind, int64_t I, int64_t J, int64_t C, bool gated)
     Shape best = {4, 4, 1, steps, 0, 1, 0};
     double least = 0.0;
     for (const Tile &t : tiles) {
-        if ((kind == kDw && t.nb != 4) || (t.na == 1 && (kind != kForward || gated))) continue;
+        if (t.na == 1 && (kind != kForward || gated)) continue;
         const int64_t n = (int64_t)tiles_of(I, 64 * t.nb) * tiles_of(J, (gated ? 32 : 64) * t.na), at_once = (int64_t)t.on_a_unit * kGrid;   // (none of no rows)
         // `items` of `each` steps
         auto time = [&](int64_t items, int each) {
@@ -584,11 +584,10 @@ hipError_t launch(const Shape &s, const LinearArgs &a, hipStream_t st)
             linear_product_kernel<K, 1, 1, ACT, GATED><<<4 * kGrid, 256, 0, st>>>(a);   // (as many fit the units)
             return hipGetLastError();
         }
-    if constexpr (K != kDw)
-        if (s.nb == 1) {
-            linear_product_kernel<K, 4, 1, ACT, GATED><<<2 * kGrid, 256, 0, st>>>(a);
-            return hipGetLastError();
-        }
+    if (s.nb == 1) {
+        linear_product_kernel<K, 4, 1, ACT, GATED><<<2 * kGrid, 256, 0, st>>>(a);
+        return hipGetLastError();
+    }
     linear_product_kernel<K, 4, 4, ACT, GATED><<<kGrid, 256, 0, st>>>(a);
     return hipGetLastError();
 }

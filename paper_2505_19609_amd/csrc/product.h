@@ -34,10 +34,11 @@ struct Source {
 //   ROWS  32 NB rows x 64 of the contraction (128 bytes a row): piece c of row r lies at c ^ (r / 2 & 7), so 16 rows' pieces of
 //         one c, which are read together, are 16 different slots of the 256 bytes that the banks span.
 //   COLS  64 of the contraction x 128 columns (256 bytes a row): piece c of row r lies at c ^ 2 (r & 3 | r / 2 & 4), so the 8 rows x 32 bytes
-//         that a transposing read takes together are 16 different slots too.
+//         that a transposing read takes together are 16 different slots too.  NB = 1: x 32 columns (64 bytes a row), piece c at c ^ 2 (r / 8 & 1).
 template <bool COLS, int NB>
 struct Operand {
-    static_assert(NB == 4 || !COLS, "");
+    static_assert(NB == 4 || NB == 1 || !COLS, "");
+    static constexpr int kRowBytes = 64 * NB;   // (COLS) of a half
     static constexpr int kHalfBytes = 4096 * NB;
     int load[2];     // byte offsets of this lane's pieces in the tile's matrix: of even and odd instructions (COLS: of the first and the last two)
     int read[4];     // LDS offsets of its fragments: ROWS by half step (two), COLS by block of 16 columns
@@ -55,12 +56,12 @@ struct Operand {
         } else {
 #pragma unroll
             for (int o = 0; o < 2; ++o) {
-                const int piece = s ^ (g + 4 * o) << 1;
-                load[o] = (wave * 16 + g) * (int)pitch + (piece >> 3) * 256 + (piece & 7) * 16;
+                const int piece = NB == 4 ? s ^ (g + 4 * o) << 1 : (lane & 3) ^ (lane >> 5) << 1, row = NB == 4 ? g : lane >> 2;
+                load[o] = (wave * 16 + row) * (int)pitch + (piece >> (NB == 4 ? 3 : 1)) * (64 * NB) + (piece & (2 * NB - 1)) * 16;
             }
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-                read[t] = (8 * g + (s >> 2)) * 256 + (((8 * part + 2 * t + ((s & 3) >> 1)) ^ ((s >> 2) + 4 * (g & 1)) << 1) << 4) + 8 * (s & 1);
+                read[t] = (8 * g + (s >> 2)) * kRowBytes + (((2 * NB * part + 2 * t + ((s & 3) >> 1)) ^ (NB == 4 ? (s >> 2) + 4 * (g & 1) : g & 1) << 1) << 4) + 8 * (s & 1);
         }
     }
     // This lane's offsets of a step.  `tail`: elements of the contraction that are left, where rows may end inside the
@@ -79,16 +80,16 @@ struct Operand {
     __device__ __forceinline__ static void fetch(i32x4 words, const int off[2], uint32_t pitch, uint32_t lds, int wave, int half, int q, int half_rows = 16 * NB)
     {
         dma_b128(words, lds + half * kHalfBytes + (wave * NB + q) * 1024, off[COLS ? q >> 1 : q & 1],
-                 COLS ? half * 128 + (int)(q * 4 * pitch) : (int)((half * half_rows + q * 8) * pitch));
+                 COLS ? half * (32 * NB) + (int)(q * 4 * pitch) : (int)((half * half_rows + q * 8) * pitch));
     }
     // fragment b (16 rows or columns, 0..3) of a half and half step k: 8 consecutive elements of the contraction
     __device__ __forceinline__ bf16x8 get(const unsigned char *t, int half, int b, int k) const
     {
         if (!COLS) return *(const bf16x8 *)(t + read[k] + half * kHalfBytes + b * 2048);
         typedef s16x4 __attribute__((address_space(3))) * lds_ptr_t;
-        const unsigned char *p = t + read[b] + half * kHalfBytes + k * 8192;
+        const unsigned char *p = t + read[b] + half * kHalfBytes + k * (32 * kRowBytes);
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)p);
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(p + 1024));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(p + 4 * kRowBytes));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };
