@@ -1,5 +1,5 @@
-"""torch.autograd wrappers around the library's forwards and backwards (attention, rotary positions, norm, loss), for callers that
-train with PyTorch: argument marshalling and bookkeeping only, every step of the
+"""torch.autograd wrappers around the library's forwards and backwards (attention, also to a window, rotary positions, norm, the residual
+stream, products, loss), for callers that train with PyTorch: argument marshalling and bookkeeping only, every step of the
 operators runs in the HIP kernels behind the C ABI.  The marshalling is native code where
 nothing watches the call from Python, else the Functions below: the same checks, outputs and errors."""
 from __future__ import annotations

@@ -6,7 +6,8 @@
 //   dW^T = X^T dZ
 // dz is formed once, by a kernel of its own (dy and z to dz, and the sums over rows for db), since both other products read it.  Without an activation it is dy itself.
 //
-// What bounds them is the matrix pipe, 2 rows n inputs operations each.  Where there are fewer tiles than compute units the contraction is cut into parts, whose
+// What bounds them is the matrix pipe at the clock that power allows, 2 rows n inputs operations each: 13,312 rows, 3,584 to 2 x 14,336 with a gate take 2.37 ms forward
+// (1,150 TFLOP/s), 2.05 for dX and 2.05 for dW (1,340), 32,768 rows, 14,336 to 4,096 3.3 ms (1,160 to 1,180 in a row of calls, 1,410 from a cool start).  Where there are fewer tiles than compute units the contraction is cut into parts, whose
 // fp32 sums a second kernel adds up in their order and finishes (no atomics).
 //
 // With a gate a tile is of 128 outputs: of each wavefront's 128 rows of W the first 64 are of the gate and the others the same ones of the second half, so that a lane has both of
@@ -203,6 +204,9 @@ __global__ __launch_bounds__(256, 1) void linear_product_kernel(const LinearArgs
             }
             return;
         }
+        // (nothing hides the latency of what a tile's end loads, so it loads much at once: 13,312 rows, 3,584 to 3,584 with a residual, 313 us with a block of 16 rows at a time, 288 with
+        // all eight; tiles of 256 x 64 have a second one on the unit)
+        constexpr int kRowsAhead = NB == 4 ? 2 * NB : 1;   // blocks of 16
         const bool bias = K == kForward && p.bias, residual = K == kForward && p.residual, keep = K == kForward && p.z;
 #pragma unroll
         for (int x = 0; x < XS; x += 2) {
@@ -222,6 +226,15 @@ __global__ __launch_bounds__(256, 1) void linear_product_kernel(const LinearArgs
                 const uint4 u = eight_of(f, f + 4);
                 if (row < p.I && stored < p.J) *(uint4 *)(to + (int64_t)row * row_stride + stored) = u;
             };
+            auto given = [&](int row, int v) {   // of the residual
+                const int c = col0 + 16 * (x + v) + 4 * g;
+                return row < p.I && c < p.J ? *(const uint2 *)(p.residual + (int64_t)row * p.residual_stride + c) : uint2{};
+            };
+            uint2 ahead[kRowsAhead][2] = {};
+            if (NB == 4 && residual) {
+#pragma unroll
+                for (int i = 0; i < 2 * kRowsAhead; ++i) ahead[i >> 1][i & 1] = given(row0 + 16 * (i >> 1), i & 1);
+            }
 #pragma unroll
             for (int y = 0; y < 2 * NB; ++y) {
                 SB();
@@ -229,10 +242,7 @@ __global__ __launch_bounds__(256, 1) void linear_product_kernel(const LinearArgs
                 uint2 add[2] = {};
                 if (residual) {
 #pragma unroll
-                    for (int v = 0; v < 2; ++v) {
-                        const int c = col0 + 16 * (x + v) + 4 * g;
-                        if (row < p.I && c < p.J) add[v] = *(const uint2 *)(p.residual + (int64_t)row * p.residual_stride + c);
-                    }
+                    for (int v = 0; v < 2; ++v) add[v] = NB == 4 ? ahead[y % kRowsAhead][v] : given(row, v);
                 }
                 float f[8], z2[8];
 #pragma unroll
@@ -348,7 +358,7 @@ struct DzArgs {
     int64_t dy_stride, rows;
     int32_t outputs, each;    // rows of a stripe
 };
-// A thread has eight columns of y through the rows of a stripe, and of as many rows the loads under way.
+// A thread has eight columns of y through the rows of a stripe, and of four rows the loads under way.  Memory-bound: 13,312 rows of 2 x 14,336 take 375 us, 5.1 TB/s.
 template <int ACT, bool GATED>
 __global__ __launch_bounds__(64) void linear_dz_kernel(const DzArgs a)
 {
@@ -534,7 +544,8 @@ int64_t slab_bytes(const Shape &s, int64_t I, int64_t width)
     return s.splits > 1 ? (int64_t)s.splits * I * width * 4 : (int64_t)s.tail * s.tail_parts * (64 * s.na) * (64 * s.nb) * 4;
 }
 
-// Stripes of dz: 2,048 workgroups of a wavefront, or as many as have 4 rows.
+// Stripes of dz: 2,048 workgroups of a wavefront, or as many as have 4 rows.  db alone in us, with 1,024, 2,048 and 4,096: 13,312 rows of 2 x 14,336 218, 200, 214; 32,768 of
+// 4,096 56, 43, 46; 26,000 of 896 38, 32, 32.
 struct Stripes {
     int count, each;
     Stripes(int64_t rows, int outputs)

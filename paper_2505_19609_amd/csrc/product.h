@@ -12,7 +12,7 @@ namespace {
 
 constexpr int kTile = 256;       // rows and columns of a result tile
 constexpr int kStep = 64;        // of the contraction
-constexpr int kGrid = 256;       // workgroups: one per compute unit, each as much LDS as allows no second one
+constexpr int kGrid = 256;       // workgroups: one per compute unit (tiles of 256 x 256 take as much LDS as allows no second one)
 
 // Where an operand's step lies and how much of its matrix is behind that address.
 struct Source {
