@@ -7,7 +7,8 @@
 // dz is formed once, by a kernel of its own (dy and z to dz, and the sums over rows for db), since both other products read it.  Without an activation it is dy itself.
 //
 // What bounds them is the matrix pipe at the clock that power allows, 2 rows n inputs operations each: 13,312 rows, 3,584 to 2 x 14,336 with a gate take 2.37 ms forward
-// (1,150 TFLOP/s), 2.05 for dX and 2.05 for dW (1,340), 32,768 rows, 14,336 to 4,096 3.3 ms (1,160 to 1,180 in a row of calls, 1,410 from a cool start).  Where there are fewer tiles than compute units the contraction is cut into parts, whose
+// (1,150 TFLOP/s), 2.05 for dX and 2.05 for dW (1,340), 32,768 rows, 16,384 to 4,096 with a
+// residual 3.3 ms (1,325).  Where there are fewer tiles than compute units the contraction is cut into parts, whose
 // fp32 sums a second kernel adds up in their order and finishes (no atomics).
 //
 // With a gate a tile is of 128 outputs: of each wavefront's 128 rows of W the first 64 are of the gate and the others the same ones of the second half, so that a lane has both of
