@@ -249,8 +249,9 @@ def test_far_window_of_a_long_sequence():
     plan.destroy()
 
 
-def test_window_results_are_the_same_bits_each_time_and_on_other_streams():
-    plan = _plan(_whole(3000, 500, 77, 1200), (14, 2), 64)
+@pytest.mark.parametrize("shape", [_whole(3000, 500, 77, 1200), _whole(8000, 500, 77)])
+def test_window_results_are_the_same_bits_each_time_and_on_other_streams(shape):
+    plan = _plan(shape, (14, 2), 64)
     x = _inputs(plan, 21)
     want = _run(plan, x, 400, 4)
     streams = [torch.cuda.Stream() for _ in range(3)]
@@ -269,16 +270,19 @@ def test_window_results_are_the_same_bits_each_time_and_on_other_streams():
     plan.destroy()
 
 
-def test_window_captured_and_replayed():
-    """Forward and gradients through autograd in a graph: every replay is the eager result, on new values too."""
+@pytest.mark.parametrize("shape,heads,d,pieces", [(_whole(900, 60, 2000), (8, 2), 128, False), (_whole(8000, 200, 6000), (8, 2), 64, True)])
+def test_window_captured_and_replayed(shape, heads, d, pieces):
+    """Forward and gradients through autograd in a graph: every replay is the eager result, on new values too.  `pieces`: as above."""
+    from paper_2505_19609_amd import binding as B
     from paper_2505_19609_amd.autograd import skrull_window_attention
-    plan = _plan(_whole(900, 60, 2000), (8, 2), 128)
+    plan = _plan(shape, heads, d)
     x = _inputs(plan, 31)
     leaves = [x[n].requires_grad_() for n in "qkv"]
 
     def step():
-        o = skrull_window_attention(*leaves, plan, 300, 4)
+        o = skrull_window_attention(*leaves, plan, 100, 4)
         return [o.detach(), *torch.autograd.grad(o, leaves, x["do"])]
+    assert (B.skrull_window_workspace(plan, 100, 4) > B.skrull_window_workspace(plan, 100, 0)) == pieces
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
