@@ -175,6 +175,28 @@ def test_residual_strides_and_in_place(cols, pad):
     assert torch.equal(r2, want[0]) and torch.equal(z2, want[1])
 
 
+@pytest.mark.parametrize("cols", [136, 4096])
+def test_residual_of_rows_far_apart(cols):
+    """Rows 2^31 elements and more apart: the bits of contiguous ones."""
+    from paper_2505_19609_amd import binding as B
+    gen = _gen(cols)
+    r, z, *vectors = _residual_inputs(gen, 3, cols, torch.bfloat16, torch.bfloat16, torch.bfloat16, 1, 1, 1, 1)
+    d_r, dy = _randn(gen, 3, cols), _randn(gen, 3, cols)
+    w, _, pw, pb, gate = vectors
+    far = lambda t: torch.empty(2 * ((1 << 31) + 8) + cols, dtype=t.dtype, device="cuda").as_strided((3, cols), ((1 << 31) + 8, 1)).copy_(t)   # noqa: E731
+    results = []
+    for place in (torch.Tensor.clone, far):
+        R, Z, DR, DY, *out = [place(t) for t in (r, z, d_r, dy, r, z, r, z)]
+        stats, grads = torch.empty(4, 3, device="cuda"), [torch.empty_like(v) for v in vectors]
+        B.skrull_residual_fwd(R, Z, *vectors, out[0], out[1], stats, 1.25, 1e-5, B.NORM_LAYER)
+        ws = torch.empty(B.skrull_residual_workspace(R, Z, w, B.NORM_LAYER), dtype=torch.uint8, device="cuda")
+        B.skrull_residual_bwd(R, Z, w, pw, pb, gate, stats, DR, DY, out[2], out[3], *grads, ws, 1.25, B.NORM_LAYER)
+        results.append([t.contiguous() for t in out] + grads)
+        del R, Z, DR, DY, out
+    assert all(torch.equal(a, c) for a, c in zip(*results))
+    torch.cuda.empty_cache()
+
+
 def test_residual_without_rows_and_with_a_row_of_infinities():
     from paper_2505_19609_amd.autograd import skrull_residual_norm
     vectors = [torch.ones(96, device="cuda", requires_grad=True) for _ in range(5)]
