@@ -450,11 +450,13 @@ int rows_of(int waves) { return waves == 1 ? 4 : 1; }
 //   200,000 x 512      144  165  170     236  246  260
 //   26,000 x 896        32   32   33      66   68   89
 //   8,192 x 8,192      116   94   96     211  156  165
+// Few rows: in the backward a workgroup has `least` = 2 of each wavefront's at least, since the second kernel reads a line of each (both kernels: 932 x 896 14.9 us with one, 11.7 with
+// two, 11.4 with four; 300 x 896 9.2, 8.5, 9.2; 500 x 4,096 12.9, 12.7, 13.6).
 constexpr int kComputeUnits = 256;
-int64_t blocks_of(const skrull_residual_t *p)
+int64_t blocks_of(const skrull_residual_t *p, int least)
 {
     const int waves = waves_of(p->cols), rows = rows_of(waves);
-    const int64_t most = kComputeUnits * (waves == 16 ? 1 : 8 / (waves == 1 ? 4 : waves)), need = (p->rows + rows - 1) / rows;
+    const int64_t most = kComputeUnits * (waves == 16 ? 1 : 8 / (waves == 1 ? 4 : waves)), need = (p->rows + rows * least - 1) / (rows * least);
     return need < most ? need : most;
 }
 
@@ -532,14 +534,14 @@ int skrull_residual_fwd(const skrull_residual_t *p, const void *r, const void *z
     ResidualArgs a = args_of(p, r, z, w, post_w, post_b, gate);
     a.b = b; a.r_out = r_out; a.y = y; a.stats = stats;
     a.r_out_stride = p->r_out_stride; a.y_stride = p->y_stride;
-    launch(false, p, a, (int)blocks_of(p), (hipStream_t)hip_stream);
+    launch(false, p, a, (int)blocks_of(p, 1), (hipStream_t)hip_stream);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? SKRULL_OK : launch_failed(e, "residual launch");
 }
 
 int64_t skrull_residual_workspace(const skrull_residual_t *p)
 {
-    return check(p) == SKRULL_OK ? blocks_of(p) * 4 * p->cols * 4 + 16 : 0;
+    return check(p) == SKRULL_OK ? blocks_of(p, 2) * 4 * p->cols * 4 + 16 : 0;
 }
 
 int skrull_residual_bwd(const skrull_residual_t *p, const void *r, const void *z, const void *w, const void *post_w, const void *post_b,
@@ -580,7 +582,7 @@ int skrull_residual_bwd(const skrull_residual_t *p, const void *r, const void *z
         a.stats = const_cast<float *>(stats);
         a.partial = sums ? (float *)workspace : nullptr;
         a.d_r_out_stride = p->d_r_out_stride; a.dy_stride = p->dy_stride; a.r_out_stride = p->dr_stride; a.y_stride = p->dz_stride;
-        blocks = (int)blocks_of(p);
+        blocks = (int)blocks_of(p, 2);
         launch(true, p, a, blocks, st);
         e = hipGetLastError();
     }
