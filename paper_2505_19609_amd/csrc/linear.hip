@@ -505,6 +505,7 @@ Shape shape_of(Kind kind, int64_t I, int64_t J, int64_t C, bool gated)
     static const Tile tiles[] = {{4, 4, 1, {1.3}, 9.0}, {4, 1, 2, {0.6, 1.03}, 5.0}, {1, 1, 4, {0.35, 0.4, 0.6, 0.8}, 3.0}};
     const int steps = tiles_of(C, kStep);
     Shape best = {4, 4, 1, steps, 0, 1, 0};
+    if (I == 0 || C == 0) return best;   // (of no rows: nothing is launched)
     double least = 0.0;
     for (const Tile &t : tiles) {
         if (t.na == 1 && (kind != kForward || gated)) continue;

@@ -1,0 +1,30 @@
+"""Products on the GPU at the edges of what their entry points take."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("inputs,outputs,activation,gated", [(4096, 6144, "none", False), (3584, 14336, "silu", True)])
+@pytest.mark.parametrize("watched", [False, True])
+def test_no_rows_of_a_wide_weight(monkeypatch, inputs, outputs, activation, gated, watched):
+    """An empty micro-batch through a weight whose gradient has more than a round of tiles and a few left over: gradients of zero, by both paths."""
+    from paper_2505_19609_amd import autograd as A
+    monkeypatch.setattr(A, "_watched", lambda: watched)
+    n = outputs * (1 + gated)
+    x, w, b, r = (torch.zeros(s, dtype=torch.bfloat16, device="cuda", requires_grad=True) for s in ((0, inputs), (n, inputs), (n,), (0, outputs)))
+    y = A.skrull_linear(x, w, b, r, activation, gated)
+    assert y.shape == (0, outputs)
+    dx, dw, db, dr = torch.autograd.grad(y, (x, w, b, r), torch.zeros_like(y))
+    assert dx.shape == x.shape and dr.shape == r.shape and dw.shape == w.shape and db.shape == b.shape
+    assert (dw == 0).all() and (db == 0).all()
+
+
+def test_no_rows_write_whole_gradients():
+    from paper_2505_19609_amd import binding as B
+    from gpu_util import guarded, margins_intact
+    x, w, dy = (torch.zeros(s, dtype=torch.bfloat16, device="cuda") for s in ((0, 4096), (6144, 4096), (0, 6144)))
+    bufs = {s: guarded(s, torch.bfloat16, float("nan")) for s in ((6144, 4096), (6144,))}
+    (_, dw), (_, db) = bufs.values()
+    B.skrull_linear_bwd(x, w, None, dy, None, dw, db, None)
+    assert (dw == 0).all() and (db == 0).all() and all(margins_intact(v[0]) for v in bufs.values())
