@@ -64,7 +64,7 @@ __device__ __forceinline__ float activation(float z, float &slope)
 {
     slope = 1.0f;
     if constexpr (ACT == SKRULL_LINEAR_RELU) {
-        slope = z > 0.0f ? 1.0f : 0.0f;
+        slope = z > 0.0f ? 1.0f : z <= 0.0f ? 0.0f : z;   // (a NaN stays one here too: as 0 it would leave gradients that show nothing of it)
         return relu(z);
     }
     if constexpr (ACT == SKRULL_LINEAR_SILU) {

@@ -28,3 +28,27 @@ def test_no_rows_write_whole_gradients():
     (_, dw), (_, db) = bufs.values()
     B.skrull_linear_bwd(x, w, None, dy, None, dw, db, None)
     assert (dw == 0).all() and (db == 0).all() and all(margins_intact(v[0]) for v in bufs.values())
+
+
+@pytest.mark.parametrize("rows,inputs,outputs", [(70, 72, 136), (1500, 520, 264)])
+@pytest.mark.parametrize("activation,gated", [("relu", False), ("gelu", False), ("silu", False), ("none", True), ("relu", True), ("gelu", True), ("silu", True)])
+def test_gradients_of_rows_that_are_not_finite(rows, inputs, outputs, activation, gated):
+    """A row whose z is NaN has a dx of NaN, and so have dw and db, which are sums over it; the other rows' dx is what it is beside any values there."""
+    from paper_2505_19609_amd.autograd import skrull_linear
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    n = outputs * (1 + gated)
+    x, w, b, dy = ((torch.randn(s, generator=gen, device="cuda") * scale).to(torch.bfloat16)
+                   for s, scale in (((rows, inputs), 1.0), ((n, inputs), inputs ** -0.5), ((n,), 0.5), ((rows, outputs), 1.0)))
+    bad = torch.tensor([0, 33, rows - 1], device="cuda")
+    good = torch.ones(rows, dtype=torch.bool, device="cuda")
+    good[bad] = False
+
+    def gradients():
+        leaves = [t.detach().clone().requires_grad_() for t in (x, w, b)]
+        return torch.autograd.grad(skrull_linear(*leaves, None, activation, gated), leaves, dy)
+    want = gradients()
+    assert all(torch.isfinite(t).all() for t in want)
+    x[bad, inputs - 1] = float("nan")
+    dx, dw, db = gradients()
+    assert torch.isnan(dx[bad]).all() and torch.isnan(dw).all() and torch.isnan(db).all()
+    assert torch.equal(dx[good], want[0][good])
