@@ -13,7 +13,7 @@
  * f is one of: z; max(z, 0) (f' = 0 at 0); z P(z) with P(z) the normal distribution's share below z; z / (1 + e^-z).
  *
  * Tensors are caller-owned DEVICE memory, bf16 and 16-byte aligned.  Rows of x, residual, y and dy begin `stride` elements apart, a multiple of 8; everything else is
- * contiguous.  Values are to be finite; a NaN in z passes every f and f' on, to its y and to its dz.
+ * contiguous.  Values are to be finite; a NaN in z gives one in y, and in dz wherever that depends on z (f = z without a gate: dz is dy).
  */
 #ifndef SKRULL_LINEAR_H
 #define SKRULL_LINEAR_H

@@ -6,9 +6,14 @@
 //   dW^T = X^T dZ
 // dz is formed once, by a kernel of its own (dy and z to dz, and the sums over rows for db), since both other products read it.  Without an activation it is dy itself.
 //
+// Two things have fewer bits than 32 on their way.  z is kept in bf16 from the forward to the backward: y is formed before that rounding, and in 32 bits z would be 763 MB more to
+// write and to read again at 13,312 rows of 2 x 14,336, 0.3 ms of 6.8.  dz is bf16 because the matrix pipe multiplies bf16; in two pieces of it, so that nothing is lost, dX and dW would
+// be twice the products.  Against 64 bits dX and dW are 2.4e-3 of their norm off with an activation and 3.0e-3 with a gate too, where the rounding of the results alone is 1.7e-3; db is summed from
+// dz as it is before its rounding.
+//
 // What bounds them is the matrix pipe at the clock that power allows, 2 rows n inputs operations each: 13,312 rows, 3,584 to 2 x 14,336 with a gate take 2.37 ms forward
-// (1,150 TFLOP/s), 2.05 for dX and 2.05 for dW (1,340), 32,768 rows, 16,384 to 4,096 with a
-// residual 3.3 ms (1,325).  Where there are fewer tiles than compute units the contraction is cut into parts, whose
+// (1,150 TFLOP/s), 2.00 for dX and 2.02 for dW (1,360), 32,768 rows, 16,384 to 4,096 with a
+// residual 3.22 ms (1,365).  Where there are fewer tiles than compute units the contraction is cut into parts, whose
 // fp32 sums a second kernel adds up in their order and finishes (no atomics).
 //
 // With a gate a tile is of 128 outputs: of each wavefront's 128 rows of W the first 64 are of the gate and the others the same ones of the second half, so that a lane has both of
@@ -27,7 +32,8 @@ namespace {
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // P(z), the normal distribution's share below z, and e^(-z^2 / 2).  For z < 0 it is e^(-z^2 / 2) G(-z) with G(a) = erfcx(a / sqrt 2) / 2, of which t times a polynomial in
-// t = 1 / (1 + a / 4) is within 1.5e-6 for all a (coefficients by least squares on Chebyshev nodes, weighted towards the largest relative error), however small P(z) is.
+// t = 1 / (1 + a / 4) is within 1.5e-6 for all a (coefficients by least squares on Chebyshev nodes, weighted towards the largest relative error), however small P(z) is.  The exponential's
+// argument is rounded twice, which adds up to 2^-24 z^2 of P(z): its relative error is 1.7e-6 to z = -4, 4e-6 to -8 and 7e-6 to -13, behind which e^(-z^2 / 2) is below fp32's normal numbers.
 __device__ __forceinline__ float normal_share(float z, float &density)
 {
     const float a = fabsf(z), t = __builtin_amdgcn_rcpf(__builtin_fmaf(a, 0.25f, 1.0f));
@@ -359,7 +365,7 @@ struct DzArgs {
     int64_t dy_stride, rows;
     int32_t outputs, each;    // rows of a stripe
 };
-// A thread has eight columns of y through the rows of a stripe, and of four rows the loads under way.  Memory-bound: 13,312 rows of 2 x 14,336 take 375 us, 5.1 TB/s.
+// A thread has eight columns of y through the rows of a stripe, and of four rows the loads under way.  Memory-bound: 13,312 rows of 2 x 14,336 take 378 us, 5.05 TB/s.
 template <int ACT, bool GATED>
 __global__ __launch_bounds__(64) void linear_dz_kernel(const DzArgs a)
 {

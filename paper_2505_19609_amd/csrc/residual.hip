@@ -2,7 +2,7 @@
 //
 // What bounds it: memory.  The forward reads r and z and writes the new stream and y, the backward reads r, z and two gradients and writes two, each once: as in
 // norm.hip a row stays in the registers of its lanes from its loads to its stores, and the next row is asked for before this one is summed.  32,768 rows of 4,096 bf16
-// with both norms and all vectors: 222 us forward (4.8 TB/s), 307 backward (5.2), 8 the vectors' sums.
+// with both norms and all vectors: 214 us forward (5.0 TB/s), 304 backward (5.3), 8 the vectors' sums.
 //
 // Both norms come down to two sums over a row each way, one after the other, since the second norm is of what the first one gives.  The five vectors' gradients
 // come down to four sums over the rows: with c1 = gate * post_w and n = h1 post_w + post_b

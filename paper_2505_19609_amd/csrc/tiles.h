@@ -238,8 +238,8 @@ __device__ __forceinline__ RowBlocks row_blocks(const P prm, const int4 *items, 
 // The keys that a forward / dQ workgroup walks over where its rows see a window of them (the last `window` ones) and the first `sinks`
 // ones of the sequence: the tiles that hold sinks, then those from the first one that the lowest row's window reaches.  Tiles and half tiles (32 keys) are numbered
 // in the order of the walk.  Without a window (WINDOW false) that is every tile from the first.  The loops' bodies are the same ones, so what bounds them is too, and the
-// time is that of the tiles in the walk: sequences of 24,576 and 8,192 tokens in short ones, 32/8 heads of 128, window 4,096, 4 sinks: forward 1.51 ms and backward 5.1, with all keys
-// 4.3 and 14.7.
+// time is that of the tiles in the walk: sequences of 24,576 and 8,192 tokens in short ones, 32/8 heads of 128, window 4,096, 4 sinks: forward 1.52 ms and backward 5.1, with all keys
+// 4.1 and 14.3.
 // ---------------------------------------------------------------------------
 template <bool WINDOW>
 struct KeyWalk {
