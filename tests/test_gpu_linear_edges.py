@@ -52,3 +52,32 @@ def test_gradients_of_rows_that_are_not_finite(rows, inputs, outputs, activation
     dx, dw, db = gradients()
     assert torch.isnan(dx[bad]).all() and torch.isnan(dw).all() and torch.isnan(db).all()
     assert torch.equal(dx[good], want[0][good])
+
+
+@pytest.mark.parametrize("rows,inputs,outputs,activation,gated,stride", [(33, 16312, 65536, "silu", True, 16312), (40, 65536, 65536, "gelu", False, 65536), (1500, 520, 264, "silu", True, 1 << 20)])
+def test_widths_and_strides_at_their_limits(rows, inputs, outputs, activation, gated, stride):
+    """The widest weights, where a gate's second half begins almost 2^31 bytes behind the first, and rows 2^20 elements apart: y and dw at a sample of columns, dx whole, within test_gpu_linear.py's
+    bounds.  (dx's reference adds up pieces of 4,096 columns, whose bound counts 4,096 sums each: more than there are in all, since a product adds 32 columns at once.)"""
+    from paper_2505_19609_amd.autograd import skrull_linear
+    from test_gpu_linear import _check, _reference
+    gen = torch.Generator(device="cuda").manual_seed(outputs)
+    n = outputs * (1 + gated)
+    wide = torch.full((rows, stride), float("nan"), dtype=torch.bfloat16, device="cuda")
+    x = wide[:, :inputs].normal_(generator=gen).requires_grad_()
+    w = torch.empty(n, inputs, dtype=torch.bfloat16, device="cuda").normal_(generator=gen).mul_(inputs ** -0.5).requires_grad_()
+    dy = torch.empty(rows, outputs, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    y = skrull_linear(x, w, None, None, activation, gated)
+    dx, dw = torch.autograd.grad(y, (x, w), dy)
+
+    def reference(cols):
+        at = torch.cat((cols, outputs + cols)) if gated else cols
+        return at, _reference(x, w.detach()[at], None, None, dy[:, cols], activation, gated)
+    at, want = reference(torch.tensor([0, 1, 255, 256, outputs // 2, outputs - 9, outputs - 1], device="cuda"))
+    _check({"y": y.detach()[:, at[:7]], "dw": dw[at]}, want, "sample")
+    exact, error = torch.zeros(2, rows, inputs, dtype=torch.float64, device="cuda")
+    for first in range(0, outputs, 4096):
+        value, off = reference(torch.arange(first, min(first + 4096, outputs), device="cuda"))[1]["dx"]
+        exact += value
+        error += off
+    _check({"dx": dx}, {"dx": (exact, error)}, "dx")
+    torch.cuda.empty_cache()
